@@ -383,7 +383,7 @@ def prepare(case, seed):
         if kind == "attend":
             # as for the first layer of a step: the same plan serves every layer
             st["plan"] = tv.make_paged_plan(case["batch"])
-            tv.paged_plan(st["bank"], st["req"], st["slots"], st["positions"], st["status"], plan=st["plan"],
+            tv.paged_plan(st["bank"], st["req"], st["slots"], st["positions"], st["status"], st["plan"],
                           n_q_heads=case["q_heads"], n_kv_heads=case["kv_heads"], window=case["window"],
                           sink=case["sink"])
             st["ws"] = tv.make_workspace(tv.tb_workspace_size(1, 1, case["kv_heads"], case["q_heads"],
@@ -524,8 +524,8 @@ def _plan(st):
     case = st["case"]
     out = {k: st[k] for k in ("row_start", "slots", "positions", "status", "held_out", "state_out", "ring", "table")}
     if own:
-        st["tv"].paged_plan(st.get("bank"), st["req"], st["slots"], st["positions"], st["status"], pool=st["pool"],
-                            plan=st["plan"] if "tree" in st else None, n_q_heads=case["q_heads"],
+        st["tv"].paged_plan(st.get("bank"), st["req"], st["slots"], st["positions"], st["status"], st["plan"],
+                            pool=st["pool"], n_q_heads=case["q_heads"] if "tree" in st else 0,
                             n_kv_heads=case["kv_heads"])
         return out
     P, L, held, table, ring = case["page"], st["L"].long(), st["held"].long(), st["table"], st["ring"]
