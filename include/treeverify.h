@@ -512,6 +512,226 @@ TB_API tb_status verify_step_scheduled(const tb_bank *bank, const tb_policy *pol
                                        tb_result *result, void *workspace, size_t workspace_bytes, int flags,
                                        tb_stream stream);
 
+/* ------------------------------------------------------------------------
+ * Serving over a paged cache: the step of a batch of requests whose keys and
+ * values live in pages of a pool, whose lengths stay in device memory, and
+ * whose logits obey penalties and grammars.  One step of a batch:
+ *   paged_plan            pages for the new tokens, slots, positions, work split
+ *   per layer: paged_kv_store (the projections' output into the pages), then
+ *              paged_tree_attention
+ *   LM head, logits_process, then greedy acceptance (paged_accept) or another
+ *              rule per request and paged_accept from its results
+ * (the paper decodes one sequence over one contiguous cache; these calls have
+ * no counterpart in it).  None needs a host read of the lengths, so the calls
+ * of a step can be captured into one CUDA graph; all of them are asynchronous
+ * on `stream`.
+ * ---------------------------------------------------------------------- */
+
+#define TB_MAX_REQUESTS 4096 /* request slots of one batch */
+
+#define TB_BF16 0 /* element types of the paged calls */
+#define TB_F16 1
+#define TB_F32 2
+
+/* The pages of a model's layers.  Element (layer, page, kv head g, slot s in
+ * the page, c) of K is at k + layer * layer_stride + page * page_stride + g *
+ * head_stride + s * slot_stride + c, likewise V: either order of heads and
+ * slots within a page, and pools that hold K and V side by side.  Strides are
+ * in elements and multiples of 8; page_size is a power of two from 8 to 1024,
+ * head_dim 64 or 128, dtype TB_BF16 or TB_F16. */
+typedef struct tb_pages {
+    void *k;
+    void *v;
+    int64_t layer_stride, page_stride, head_stride, slot_stride;
+    int32_t n_layers, n_pages, n_kv_heads, page_size, head_dim;
+    int32_t dtype;
+} tb_pages;
+
+/* A batch of request slots; every pointer is device memory.  Request b holds a
+ * prefix of lens[b] tokens and brings the tokens of its tree in this step:
+ * tree[b] is a bank id, or -1 for none (an empty slot, a waiting or a finished
+ * request).  With tree == NULL it brings n_new[b] tokens of a prompt instead
+ * (paged_plan and paged_kv_store only).  Token s of request b lives in page
+ * table[b * max_pages + s / page_size] at s % page_size; table entries past the
+ * request's pages are never read.  The rows of all requests (node order within
+ * a request) lie behind one another: request b's are row_start[b] ..
+ * row_start[b + 1] - 1 of every per-row array. */
+typedef struct tb_requests {
+    int32_t batch;             /* 1..TB_MAX_REQUESTS */
+    int32_t max_pages;         /* entries per row of table */
+    int32_t page_size;
+    int32_t reserved;          /* 0 */
+    const int32_t *tree;       /* [batch] */
+    const int32_t *n_new;      /* [batch], used when tree is NULL */
+    const int32_t *lens;       /* [batch] */
+    const int32_t *key_begin;  /* NULL, or [batch]: the first slot that may be seen (a document's beginning) */
+    int32_t *table;            /* [batch][max_pages] */
+    int32_t *row_start;        /* [batch + 1], written by paged_plan */
+} tb_requests;
+
+/* The free pages: a ring of n_pages page ids in device memory, of which the
+ * state[1] ids from position state[0] on (cyclically) are free; held[b] is the
+ * number of pages that request b holds.  state_out / held_out receive the
+ * values after the call; each may be the input array itself. */
+typedef struct tb_page_pool {
+    int32_t n_pages;
+    int32_t reserved;          /* 0 */
+    int32_t *ring;             /* [n_pages] */
+    const int32_t *state;      /* [2]: position of the first free id, free ids */
+    int32_t *state_out;        /* [2] */
+    const int32_t *held;       /* [batch] */
+    int32_t *held_out;         /* [batch] */
+} tb_page_pool;
+
+/* Bytes of the plan of a batch on `device` (-1: the current one).  The plan is
+ * device memory, zero-filled before its first use (tb_workspace_init). */
+TB_API size_t tb_paged_plan_size(int batch, int device);
+
+/* Brings a batch's block tables to its lengths and lays out its step.
+ *   need[b] = ceil((lens[b] + n[b]) / page_size), n[b] the tokens it brings
+ * Requests with need > held take pages off the front of the ring, in request
+ * order; those with need < held give the last ones back to its end, in
+ * (request, page) order.  pool == NULL: the table is the caller's and already
+ * complete.  Written:
+ *   row_start [batch + 1]; per row (max_rows entries, -1 / 0 past the last row):
+ *   slots     int64  page * page_size + slot in the page
+ *   positions int32  lens[b] + depth(node) (lens[b] + i without trees)
+ *   status    int32 [batch]: TB_OK, or why the request got nothing in this step
+ *             (no rows, no pages taken or given): TB_EINVAL for an unknown
+ *             tree or a negative length, TB_ECAPACITY when it needs more than
+ *             max_pages, its rows do not fit max_rows, or the ring has run out
+ *             (then later requests that need pages get none either)
+ *   plan      the attention's work split for n_q_heads / n_kv_heads, window and
+ *             sink (0, 0: none; see paged_tree_attention), read by
+ *             paged_tree_attention calls of this step; a model whose layers
+ *             differ in them makes one plan for each kind (pool NULL for the
+ *             second).  n_q_heads = 0: no attention follows.
+ * One kernel. */
+TB_API tb_status paged_plan(const tb_bank *bank, const tb_requests *req, const tb_page_pool *pool, int64_t *slots,
+                            int32_t *positions, int max_rows, int32_t *status, int n_q_heads, int n_kv_heads,
+                            int window, int sink, void *plan, size_t plan_bytes, tb_stream stream);
+
+/* Rotary embedding with several position axes (text: one; images and video:
+ * time, height, width), and the store of keys and values into their pages.
+ * Pair i of a head (elements i and i + head_dim / 2) turns by
+ * positions[axis][r] * rope_theta^(-2i / head_dim), where axis 0 has the first
+ * sections[0] pairs, axis 1 the next sections[1], and so on (they sum up to
+ * head_dim / 2).  rope_theta = 0: nothing turns (positions may be NULL). */
+typedef struct tb_rope {
+    float theta;
+    int32_t n_axes;               /* 1..4 */
+    int32_t sections[4];
+    const int32_t *positions;     /* device [n_axes][axis_stride] */
+    int64_t axis_stride;          /* elements between axes, >= n_rows */
+} tb_rope;
+
+/* One operand of paged_kv_store: element (row, head, c) at ptr + row *
+ * row_stride + head * head_stride + c (strides in elements, multiples of 8). */
+typedef struct tb_rows {
+    void *ptr;
+    int64_t row_stride, head_stride;
+} tb_rows;
+
+/* Writes k (turned) and v of every row r into layer `layer` of the pages at
+ * slots[r]; a slot outside the pool (-1: padding) is skipped.  q (n_q_heads
+ * heads; ptr NULL: none) is turned into q_out, which may be q itself.  All
+ * operands have the pages' type; the rotation is taken in 32 bits and rounded
+ * once.  Slots of one call are distinct.  n_rows >= 0; one kernel. */
+TB_API tb_status paged_kv_store(const tb_pages *pages, int layer, const int64_t *slots, int n_rows, const tb_rows *k,
+                                const tb_rows *v, const tb_rows *q, const tb_rows *q_out, int n_q_heads,
+                                const tb_rope *rope, tb_stream stream);
+
+/* Tree attention over the pages of one layer, for every row of the batch.  Row
+ * i of request b (prefix L) sees a slot s >= key_begin[b] when
+ *   s < L (prefix), or s = L + j with j an ancestor of i or i itself, and
+ *   with a window: pos(i) - pos(s) < window, or s < key_begin[b] + sink,
+ * pos being s in the prefix and L + depth for tree nodes, and
+ *   z = cap(scale q.k) - slopes[h] (pos(i) - pos(s)),  cap(x) = softcap tanh(x / softcap)
+ *   out[r, h] = sum_s softmax_s(z) v[s],  lse[r, h] = ln sum_s e^z
+ * (softcap 0: no cap; slopes NULL: no bias).  A row that sees nothing gets out
+ * 0 and lse -inf.  Keys that no row of a request may see do not reach its
+ * outputs, whatever their pages hold (NaN and infinities included); the values
+ * of slots that some rows see and others do not have to be finite.
+ *   q, out [n_rows][n_q_heads][head_dim] of the pages' type, rows as row_start
+ *          numbers them (rows of the plan past n_rows are left out)
+ *   lse    NULL, or float [n_rows][n_q_heads]; slopes: NULL or device float [n_q_heads]
+ * `plan` is the paged_plan of the same batch, lengths and heads.  Scores, sums
+ * and the output are accumulated in 32 bits; the weights enter the second
+ * product in the pages' type.  The workspace needs tb_workspace_size for
+ * head_dim; a plan of other heads or another batch size sets TB_EINVAL in its
+ * status word and leaves out and lse unwritten. */
+TB_API tb_status paged_tree_attention(const tb_bank *bank, const tb_requests *req, const tb_pages *pages, int layer,
+                                      const void *plan, size_t plan_bytes, const void *q, int n_rows, int n_q_heads,
+                                      float scale, float softcap, const float *slopes, void *out, float *lse,
+                                      void *workspace, size_t workspace_bytes, tb_stream stream);
+
+/* Penalties, biases and masks of logits_process; every pointer is device memory
+ * and may be NULL (no such rule). */
+typedef struct tb_logit_rules {
+    const int32_t *history;      /* [batch][history_stride]: the tokens of a request, prompt first */
+    int64_t history_stride;
+    const int32_t *history_len;  /* [batch] */
+    const int32_t *prompt_len;   /* [batch]: how many of them are the prompt's (NULL: none) */
+    const int32_t *draft;        /* [rows]: the draft tokens; a row's root path counts as generated (its
+                                    root is in the history already) */
+    const float *repetition;     /* [batch], > 0 */
+    const float *presence;       /* [batch] */
+    const float *frequency;      /* [batch] */
+    const int32_t *bias_start;   /* [batch + 1]: request b's biases are entries bias_start[b] .. */
+    const int32_t *bias_token;
+    const float *bias_value;
+    const int32_t *mask;         /* bit v % 32 of word v / 32: token v is allowed */
+    int64_t mask_stride;         /* words per mask row, >= ceil(vocab / 32) */
+    const int32_t *mask_row;     /* [rows]: a row's mask row, -1 for none (NULL: row r has mask row r) */
+} tb_logit_rules;
+
+/* Statistics of the processed rows, as lm_head_stats and lm_head_stats_typical
+ * define them; each NULL or device [rows]. */
+typedef struct tb_logit_stats {
+    int32_t *argmax;     /* -1 for a row without an allowed token */
+    float *top1;
+    float *entropy;
+    float *logz_t;       /* at `temperature` */
+    float *entropy_t;
+    float *draft_logit;  /* roots are left unwritten */
+} tb_logit_stats;
+
+/* Applies a request's rules to the logits of its rows, in 32 bits and in this order:
+ *   token in history or on the row's root path: z > 0 ? z / repetition : z * repetition
+ *   z -= frequency * count;  z -= presence (count > 0)    (count: in the generated
+ *                                  part of the history and on the root path)
+ *   z += bias (entries of one token add up, in list order)
+ *   not allowed by the mask: z = -inf (whatever z was, NaN included)
+ * logits [rows][vocab] of type dtype (TB_F32, TB_BF16 or TB_F16), logit_stride
+ * elements apart; out float [rows][vocab], out_stride apart (both strides >=
+ * vocab); out may be logits itself when dtype is TB_F32 and the strides agree.
+ * Tokens outside [0, vocab) in the history, drafts or biases are skipped.  A
+ * row without an allowed token has argmax -1, top1 0, entropy 0 and logz_t
+ * -inf; a NaN among the allowed logits makes the row's statistics NaN.
+ * Requests and rows are req's (batch, row_start, tree; tree NULL: rows without
+ * root paths); rows past n_rows are left out.  One kernel; results do not depend on the launch's
+ * placement. */
+TB_API tb_status logits_process(const tb_bank *bank, const tb_requests *req, const void *logits, int dtype,
+                                int64_t logit_stride, int n_rows, int vocab, const tb_logit_rules *rules,
+                                float temperature, float *out, int64_t out_stride, const tb_logit_stats *stats,
+                                void *workspace, size_t workspace_bytes, tb_stream stream);
+
+/* Bytes of workspace of logits_process (zero-filled before its first use). */
+TB_API size_t tb_logits_workspace_size(int batch, int n_rows, int vocab);
+
+/* Ends a step: greedy acceptance per request (greedy_accept's rule on its rows
+ * of draft_tokens and argmax), the accepted rows moved to the front of the
+ * tree's slots in every layer and kv head of the pages, and the length
+ * advanced: lens_out[b] = lens[b] + accept_len (lens_out may be lens itself).
+ * draft_tokens == NULL: results[b] already holds accept_len and path (another
+ * rule's), which are only moved by.  Requests without a tree keep their length,
+ * and their results get accept_len 0.  results: device tb_result [batch].  A draft
+ * token outside [0, vocab) never matches and sets TB_EINVAL in the request's
+ * result.  pages NULL: nothing to move.  One kernel. */
+TB_API tb_status paged_accept(const tb_bank *bank, const tb_requests *req, const tb_pages *pages,
+                              const int32_t *draft_tokens, const int32_t *argmax, int n_rows, int vocab,
+                              tb_result *results, int32_t *lens_out, tb_stream stream);
+
 /* Message for the last failing call on this thread ("" if none). */
 TB_API const char *tb_last_error(void);
 

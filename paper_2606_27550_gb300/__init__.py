@@ -37,7 +37,8 @@ API = ("tb_canonicalize", "tb_create", "tb_add_topology", "tb_get_topology", "tb
        "tb_schedule_hysteretic_ladder", "tb_schedule_binary", "tb_schedule_threshold_ladder",
        "lm_head_stats_typical", "typical_accept", "verify_step_typical", "verify_step_batched_typical",
        "verify_step_scheduled", "spec_sample_accept", "verify_step_sampled", "tb_debug_bounds_violations",
-       "tb_debug_bounds_build", "tb_launch_count")
+       "tb_debug_bounds_build", "tb_launch_count", "tb_paged_plan_size", "paged_plan", "paged_kv_store",
+       "paged_tree_attention", "logits_process", "tb_logits_workspace_size", "paged_accept")
 
 
 class TreeVerifyError(RuntimeError):
@@ -73,6 +74,52 @@ class TbPolicy(ctypes.Structure):
                 ("bank_ids", ctypes.c_int32 * 8), ("a", ctypes.c_float), ("b", ctypes.c_float),
                 ("edges", ctypes.c_float * 7), ("trace", ctypes.c_void_p), ("n_trace", ctypes.c_int32),
                 ("n_heads", ctypes.c_int32), ("node_stride", ctypes.c_int32)]
+
+
+TB_MAX_REQUESTS = 4096
+TB_BF16, TB_F16, TB_F32 = 0, 1, 2
+
+
+class TbPages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("layer_stride", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64),
+                ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class TbRequests(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("tree", ctypes.c_void_p), ("n_new", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("key_begin", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("row_start", ctypes.c_void_p)]
+
+
+class TbPagePool(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("reserved", ctypes.c_int32), ("ring", ctypes.c_void_p),
+                ("state", ctypes.c_void_p), ("state_out", ctypes.c_void_p), ("held", ctypes.c_void_p),
+                ("held_out", ctypes.c_void_p)]
+
+
+class TbRope(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_float), ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 4),
+                ("positions", ctypes.c_void_p), ("axis_stride", ctypes.c_int64)]
+
+
+class TbRows(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class TbLogitRules(ctypes.Structure):
+    _fields_ = [("history", ctypes.c_void_p), ("history_stride", ctypes.c_int64), ("history_len", ctypes.c_void_p),
+                ("prompt_len", ctypes.c_void_p), ("draft", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("bias_start", ctypes.c_void_p),
+                ("bias_token", ctypes.c_void_p), ("bias_value", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("mask_stride", ctypes.c_int64), ("mask_row", ctypes.c_void_p)]
+
+
+class TbLogitStats(ctypes.Structure):
+    _fields_ = [("argmax", ctypes.c_void_p), ("top1", ctypes.c_void_p), ("entropy", ctypes.c_void_p),
+                ("logz_t", ctypes.c_void_p), ("entropy_t", ctypes.c_void_p), ("draft_logit", ctypes.c_void_p)]
 
 
 # the paper's verification settings (temperature, posterior threshold, mixing coefficient)
@@ -121,6 +168,13 @@ def load(path: str = LIB_PATH):
         "spec_sample_accept": [P, i32, P, P, P, P, P, i32, i32, ctypes.c_float, P, P, P],
         "verify_step_sampled": [P, i32, P, P, i32, P, P, i32, i32, P, P, P, ctypes.c_float, P, P, P, P, P, P, P, sz,
                                 i32, P],
+        "tb_paged_plan_size": [i32, i32],
+        "paged_plan": [P, P, P, P, P, i32, P, i32, i32, i32, i32, P, sz, P],
+        "paged_kv_store": [P, i32, P, i32, P, P, P, P, i32, P, P],
+        "paged_tree_attention": [P, P, P, i32, P, sz, P, i32, i32, ctypes.c_float, ctypes.c_float, P, P, P, P, sz, P],
+        "tb_logits_workspace_size": [i32, i32, i32],
+        "logits_process": [P, P, P, i32, i64, i32, i32, P, ctypes.c_float, P, i64, P, P, sz, P],
+        "paged_accept": [P, P, P, P, P, i32, i32, P, P, P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -132,7 +186,8 @@ def load(path: str = LIB_PATH):
     lib.tb_schedule_threshold_ladder.argtypes = [d, P, i32]
     for f in (lib.tb_schedule_hysteretic_ladder, lib.tb_schedule_binary, lib.tb_schedule_threshold_ladder):
         f.restype = ctypes.c_int
-    lib.tb_workspace_size.restype = ctypes.c_size_t
+    for f in (lib.tb_workspace_size, lib.tb_paged_plan_size, lib.tb_logits_workspace_size):
+        f.restype = ctypes.c_size_t
     lib.tb_last_error.restype = ctypes.c_char_p
     _lib = lib
     return lib
@@ -521,6 +576,246 @@ def verify_step_scheduled(bank: Bank, policy: TbPolicy, state, kv: KvCache, q, h
                                         _ptr(drafts), _ptr(attn_out), _ptr(argmax), _ptr(top1), _ptr(entropy),
                                         _ptr(result), _ptr(ws), ws.numel(), flags, _stream(stream)),
            "verify_step_scheduled")
+
+
+# --------------------------------------------------------------------- serving over a paged cache
+
+
+def _dtype(t, *, f32: bool = False) -> int:
+    import torch
+
+    kinds = {torch.bfloat16: TB_BF16, torch.float16: TB_F16}
+    if f32:
+        kinds[torch.float32] = TB_F32
+    if t.dtype not in kinds:
+        raise TypeError(f"{t.dtype}: {', '.join(map(str, kinds))} expected")
+    return kinds[t.dtype]
+
+
+def _device_array(t, dtype: str, what: str, shape=None) -> int | None:
+    """The address of a contiguous array of the type that the call reads it as,
+    of at least the given shape's first entries."""
+    if t is None:
+        return None
+    if str(t.dtype) != "torch." + dtype:
+        raise TypeError(f"{what}: {t.dtype}, {dtype} expected")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: not contiguous")
+    if shape is not None and (t.dim() != len(shape) or any(a < b for a, b in zip(t.shape, shape)) or
+                              tuple(t.shape[1:]) != tuple(shape[1:])):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, {tuple(shape)} expected")
+    return t.data_ptr()
+
+
+@dataclass
+class Pages:
+    """The paged cache: k and v shaped [n_layers][n_pages][n_kv_heads][page_size][head_dim],
+    views of any strides (multiples of 8, elements of a row contiguous), the same for both."""
+
+    k: object
+    v: object
+
+    def as_c(self) -> TbPages:
+        k, v = self.k, self.v
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(4) != 1:
+            raise ValueError("pages: k and v of one 5-D shape, type and strides, rows contiguous")
+        n_layers, n_pages, heads, page, d = k.shape
+        s = k.stride()
+        return TbPages(k.data_ptr(), v.data_ptr(), s[0], s[1], s[2], s[3], n_layers, n_pages, heads, page, d, _dtype(k))
+
+
+@dataclass
+class Requests:
+    """A batch of request slots (device int32 tensors): lens [B], table [B][max_pages],
+    row_start [B + 1], and tree [B] (bank ids, -1 for none) or n_new [B]; key_begin [B] or None."""
+
+    row_start: object
+    tree: object = None
+    lens: object = None
+    table: object = None
+    page_size: int = 16
+    n_new: object = None
+    key_begin: object = None
+
+    def as_c(self) -> TbRequests:
+        B = self.row_start.shape[0] - 1
+        one = lambda t, what: _device_array(t, "int32", what, (B,))  # noqa: E731
+        return TbRequests(B, 0 if self.table is None else self.table.shape[1], self.page_size, 0,
+                          one(self.tree, "tree"), one(self.n_new, "n_new"), one(self.lens, "lens"),
+                          one(self.key_begin, "key_begin"),
+                          None if self.table is None else _device_array(self.table, "int32", "table",
+                                                                        (B, self.table.shape[1])),
+                          _device_array(self.row_start, "int32", "row_start"))
+
+
+@dataclass
+class PagePool:
+    """The free pages (device int32 tensors): ring [n_pages], state [2] = (first, free), held [B];
+    state_out / held_out receive the new values (None: in place)."""
+
+    ring: object
+    state: object
+    held: object
+    state_out: object = None
+    held_out: object = None
+
+    def as_c(self, batch: int) -> TbPagePool:
+        state_out = self.state if self.state_out is None else self.state_out
+        held_out = self.held if self.held_out is None else self.held_out
+        return TbPagePool(self.ring.shape[0], 0, _device_array(self.ring, "int32", "ring"),
+                          _device_array(self.state, "int32", "state", (2,)),
+                          _device_array(state_out, "int32", "state_out", (2,)),
+                          _device_array(self.held, "int32", "held", (batch,)),
+                          _device_array(held_out, "int32", "held_out", (batch,)))
+
+
+def make_page_pool(n_pages: int, batch: int, device="cuda") -> PagePool:
+    """A pool whose pages 0 .. n_pages - 1 are all free."""
+    import torch
+
+    return PagePool(torch.arange(n_pages, dtype=torch.int32, device=device),
+                    torch.tensor([0, n_pages], dtype=torch.int32, device=device),
+                    torch.zeros(batch, dtype=torch.int32, device=device))
+
+
+def tb_paged_plan_size(batch: int, device: int = -1) -> int:
+    return int(load().tb_paged_plan_size(batch, device))
+
+
+def make_paged_plan(batch: int, device="cuda"):
+    """Zero-filled device memory for the plan of a batch (torch uint8)."""
+    return make_workspace(tb_paged_plan_size(batch), device)
+
+
+def paged_plan(bank, req: Requests, slots, positions, status, plan, pool: PagePool | None = None, n_q_heads: int = 0,
+               n_kv_heads: int = 1, window: int = 0, sink: int = 0, stream=None):
+    """slots int64, positions int32 [max_rows]; status int32 [B]; bank may be None with n_new."""
+    r = req.as_c()
+    c = None if pool is None else pool.as_c(r.batch)
+    rows = slots.shape[0]
+    _check(load().paged_plan(None if bank is None else bank.handle, ctypes.byref(r),
+                             None if c is None else ctypes.byref(c), _device_array(slots, "int64", "slots"),
+                             _device_array(positions, "int32", "positions", (rows,)), rows,
+                             _device_array(status, "int32", "status", (r.batch,)), n_q_heads, n_kv_heads, window, sink,
+                             _ptr(plan), plan.numel(), _stream(stream)), "paged_plan")
+
+
+def _rows_of(t, rows: int, heads: int, pages, what: str) -> TbRows:
+    if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != pages.shape[4] or t.stride(2) != 1:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, ({rows}, {heads}, {pages.shape[4]}) expected, rows contiguous")
+    if t.dtype != pages.dtype:
+        raise TypeError(f"{what}: {t.dtype}, the pages' {pages.dtype} expected")
+    return TbRows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def paged_kv_store(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None, positions=None, sections=None,
+                   rope_theta: float = 0.0, stream=None):
+    """k, v [rows][n_kv_heads][head_dim] and q, q_out [rows][n_q_heads][head_dim] (views of any row
+    and head strides); positions int32 [rows] or [axes][rows]; sections: pairs per axis (None: one axis)."""
+    c = pages.as_c()
+    rows = slots.shape[0]
+    ck, cv = _rows_of(k, rows, c.n_kv_heads, pages.k, "k"), _rows_of(v, rows, c.n_kv_heads, pages.k, "v")
+    cq = co = None
+    heads = 0
+    if q is not None:
+        heads = q.shape[1]
+        cq = _rows_of(q, rows, heads, pages.k, "q")
+        co = _rows_of(q if q_out is None else q_out, rows, heads, pages.k, "q_out")
+    rope = None
+    if rope_theta:
+        rope = TbRope()
+        sections = (c.head_dim // 2,) if sections is None else tuple(sections)
+        if len(sections) > 4:
+            raise ValueError(f"{len(sections)} position axes: at most 4")
+        pos = positions.view(1, -1) if positions.dim() == 1 else positions
+        rope.theta, rope.n_axes = float(rope_theta), len(sections)
+        for i, n in enumerate(sections):
+            rope.sections[i] = n
+        rope.positions = _device_array(pos, "int32", "positions", (len(sections), pos.shape[1]))
+        if pos.shape[1] < rows:
+            raise ValueError(f"positions: {pos.shape[1]} of {rows} rows")
+        rope.axis_stride = pos.shape[1]
+    ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
+    _check(load().paged_kv_store(ctypes.byref(c), layer, _device_array(slots, "int64", "slots"), rows,
+                                 ctypes.byref(ck), ctypes.byref(cv), ref(cq), ref(co), heads, ref(rope),
+                                 _stream(stream)), "paged_kv_store")
+
+
+def paged_tree_attention(bank: Bank, req: Requests, pages: Pages, plan, q, out, ws, layer: int = 0,
+                         scale: float | None = None, softcap: float = 0.0, slopes=None, lse=None, stream=None):
+    """q, out [rows][n_q_heads][head_dim] of the pages' type; lse float [rows][n_q_heads]; slopes float [n_q_heads];
+    scale: 1 / sqrt(head_dim) unless given."""
+    r, c = req.as_c(), pages.as_c()
+    rows, heads, d = q.shape
+    for t, what in ((q, "q"), (out, "out")):
+        if t.dtype != pages.k.dtype or tuple(t.shape) != (rows, heads, c.head_dim) or not t.is_contiguous():
+            raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)}, contiguous {pages.k.dtype} "
+                             f"({rows}, {heads}, {c.head_dim}) expected")
+    _check(load().paged_tree_attention(bank.handle, ctypes.byref(r), ctypes.byref(c), layer, _ptr(plan), plan.numel(),
+                                       _ptr(q), rows, heads, d ** -0.5 if scale is None else float(scale),
+                                       float(softcap), _device_array(slopes, "float32", "slopes", (heads,)), _ptr(out),
+                                       _device_array(lse, "float32", "lse", (rows, heads)), _ptr(ws), ws.numel(),
+                                       _stream(stream)), "paged_tree_attention")
+
+
+def tb_logits_workspace_size(batch: int, n_rows: int, vocab: int) -> int:
+    return int(load().tb_logits_workspace_size(batch, n_rows, vocab))
+
+
+def logits_process(bank, req: Requests, logits, out, ws, draft=None, history=None, history_len=None, prompt_len=None,
+                   repetition=None, presence=None, frequency=None, bias_start=None, bias_token=None, bias_value=None,
+                   mask=None, mask_row=None, temperature: float = 1.0, argmax=None, top1=None, entropy=None,
+                   logz_t=None, entropy_t=None, draft_logit=None, stream=None):
+    """logits [rows][vocab] (float32, bfloat16 or float16; rows may be strided), out float32 (may be logits);
+    history int32 [B][width], mask int32 words [mask rows][width], the rest as the C struct names them."""
+    r = req.as_c()
+    B, (rows, vocab) = r.batch, logits.shape
+    for t, what in ((logits, "logits"), (out, "out")):
+        if tuple(t.shape) != (rows, vocab) or t.stride(1) != 1:
+            raise ValueError(f"{what}: shape {tuple(t.shape)} of strides {t.stride()}, ({rows}, {vocab}) with "
+                             "contiguous rows expected")
+    if _dtype(out, f32=True) != TB_F32:
+        raise TypeError(f"out: {out.dtype}, float32 expected")
+    arr = lambda t, kind, what, n: _device_array(t, kind, what, None if n is None else (n,))  # noqa: E731
+    rules = TbLogitRules(None if history is None else _device_array(history, "int32", "history", (B, history.shape[1])),
+                         0 if history is None else history.shape[1], arr(history_len, "int32", "history_len", B),
+                         arr(prompt_len, "int32", "prompt_len", B), arr(draft, "int32", "draft", rows),
+                         arr(repetition, "float32", "repetition", B), arr(presence, "float32", "presence", B),
+                         arr(frequency, "float32", "frequency", B), arr(bias_start, "int32", "bias_start", B + 1),
+                         arr(bias_token, "int32", "bias_token", None), arr(bias_value, "float32", "bias_value", None),
+                         None if mask is None else _device_array(mask, "int32", "mask"),
+                         0 if mask is None else mask.shape[1], arr(mask_row, "int32", "mask_row", rows))
+    if mask is not None and mask_row is None and mask.shape[0] < rows:
+        raise ValueError(f"mask: {mask.shape[0]} of {rows} rows")
+    st = TbLogitStats(arr(argmax, "int32", "argmax", rows), *(arr(t, "float32", w, rows) for t, w in (
+        (top1, "top1"), (entropy, "entropy"), (logz_t, "logz_t"), (entropy_t, "entropy_t"),
+        (draft_logit, "draft_logit"))))
+    _check(load().logits_process(None if bank is None else bank.handle, ctypes.byref(r), _ptr(logits),
+                                 _dtype(logits, f32=True), logits.stride(0) if rows > 1 else max(vocab, logits.stride(0)),
+                                 rows, vocab, ctypes.byref(rules), float(temperature), _ptr(out),
+                                 out.stride(0) if rows > 1 else max(vocab, out.stride(0)), ctypes.byref(st), _ptr(ws),
+                                 ws.numel(), _stream(stream)), "logits_process")
+
+
+def make_results(batch: int, device="cuda"):
+    """Device buffer for a batch of tb_result blocks (int32 [batch][68])."""
+    import torch
+
+    return torch.zeros((batch, RESULT_INTS), dtype=torch.int32, device=device)
+
+
+def paged_accept(bank: Bank, req: Requests, pages, results, draft=None, argmax=None, vocab: int = 0, lens_out=None,
+                 stream=None):
+    """results int32 [B][68] (make_results); draft, argmax int32 [rows], or draft None to move by the results given;
+    lens_out: None for lens itself; pages None: nothing to move."""
+    r = req.as_c()
+    c = None if pages is None else pages.as_c()
+    rows = 0x7FFFFFFF if draft is None else min(draft.shape[0], argmax.shape[0])
+    _check(load().paged_accept(bank.handle, ctypes.byref(r), None if c is None else ctypes.byref(c),
+                               _device_array(draft, "int32", "draft"), _device_array(argmax, "int32", "argmax"), rows,
+                               vocab, _device_array(results, "int32", "results", (r.batch, RESULT_INTS)),
+                               r.lens if lens_out is None else _device_array(lens_out, "int32", "lens_out", (r.batch,)),
+                               _stream(stream)), "paged_accept")
 
 
 # --------------------------------------------------------------------- per-step tree selection

@@ -1,0 +1,77 @@
+// paged.cuh -- what the kernels of a serving step over a paged cache share: the
+// plan of a step (written by paged_plan, read by paged_tree_attention) and the
+// argument checks of their entry points.
+#pragma once
+
+#include "kernels.cuh"
+
+namespace tv {
+
+constexpr int kTileKeys = 128;  // keys per tile of the paged attention
+
+// One request of a plan.  A unit is one (kv head, block of 128 query rows); its
+// tiles are key tiles [a0, a0 + n1) (the first tokens that a window keeps) and
+// [b0, b0 + T - n1).
+struct PlanReq {
+    long long tile_base;  // first of its tiles in the flattened tile space
+    int L, n, row0, tree;
+    int T, a0, n1, b0;
+    int row_blocks, begin, far_end, b;  // keys before far_end are seen beyond the window
+};
+static_assert(sizeof(PlanReq) == 56, "eight-byte aligned records");
+
+struct PlanHeader {
+    int ticket;  // of paged_plan's CTAs; zero between calls
+    int valid;
+    int batch, n_q_heads, n_kv_heads, window, n_active;
+    int P;       // CTAs that the tiles are split over
+    long long total;
+    int rows, sink, pad[4];
+};
+static_assert(sizeof(PlanHeader) == 64, "");
+
+constexpr int kMaxPlanCtas = 1024;
+
+// header, then the first request of each CTA, then the requests with rows
+// (n_active of them) and one more record whose tile_base is the total
+inline size_t plan_bytes_for(int batch)
+{
+    return sizeof(PlanHeader) + kMaxPlanCtas * sizeof(int) + (size_t)(batch + 1) * sizeof(PlanReq);
+}
+__host__ __device__ inline int *plan_first(void *plan)
+{
+    return reinterpret_cast<int *>(static_cast<unsigned char *>(plan) + sizeof(PlanHeader));
+}
+__host__ __device__ inline PlanReq *plan_reqs(void *plan)
+{
+    return reinterpret_cast<PlanReq *>(static_cast<unsigned char *>(plan) + sizeof(PlanHeader) +
+                                       kMaxPlanCtas * sizeof(int));
+}
+
+// The first tile of CTA c's range when `total` tiles are split over P CTAs, at
+// least one each where there are so many.
+__host__ __device__ inline long long plan_split(long long total, int P, int c)
+{
+    const long long q = total / P, r = total % P;
+    return q * c + (c < r ? c : r);
+}
+
+// argument checks (treeverify.cu); each returns TB_OK or records the error
+tb_status check_device_bank(const tb_bank *bank, const char *fn, const TreeDesc **trees, int *n_trees);
+tb_status check_requests(const tb_requests *req, bool table, const char *fn);
+tb_status check_pages(const tb_pages *pages, const char *fn);
+tb_status check_workspace(const void *ws, size_t bytes, size_t need, const char *fn);
+tb_status launch_result(cudaError_t e, const char *fn);
+int device_sms(int device);  // -1: the current one
+bool ptr_aligned(const void *p, size_t a);
+
+// K or V of one layer's pages: (d, slots of a page, kv heads, pages), box (64, box_slots, 1, 1)
+bool make_tmap_pages(CUtensorMap *map, const tb_pages *pages, const void *base, int box_slots, const char **err);
+
+unsigned int bounds_violations_paged_plan();
+unsigned int bounds_violations_paged_store();
+unsigned int bounds_violations_paged_attention();
+unsigned int bounds_violations_logits();
+unsigned int bounds_violations_paged_accept();
+
+}  // namespace tv

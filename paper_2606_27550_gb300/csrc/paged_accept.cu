@@ -1,0 +1,241 @@
+// paged_accept.cu -- the end of a step over a paged cache: greedy acceptance of
+// every request, the accepted rows moved within their pages, the lengths
+// advanced.
+//
+// Acceptance is the bitset form of accept.cu: with match the set of nodes whose
+// draft token is their parent's greedy token, node i is accepted when
+// (anc[i] & ~match & ~root) == 0; the deepest accepted node (smallest id among
+// equals) ends the path, which is its ancestor set in increasing order.  Slot
+// L + j of every layer and kv head then takes slot L + path[j], through the
+// block table.  path is strictly increasing with path[j] >= j, so a thread that
+// holds one 16-byte piece of a (layer, kv head, K or V) and goes through j in
+// order, a few loads ahead of their stores, reads no slot that it has written.
+//
+// A cluster of CTAs shares a request: each repeats the (tiny) acceptance, moves
+// its share of the pieces, and the first writes the length after all have read
+// it (one cluster barrier), so that the lengths may be advanced in place.
+#include "paged.cuh"
+
+namespace tv {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kCluster = 8;
+constexpr int kAhead = 4;  // moves in flight per thread
+
+struct AcceptArgs {
+    const TreeDesc *trees;
+    int n_trees, batch, max_pages, page_log2, n_rows, vocab;
+    const int32_t *tree, *lens, *row_start, *table, *draft, *argmax;
+    tb_result *results;
+    int32_t *lens_out;
+    uint16_t *k, *v;
+    long long layer_stride, page_stride, head_stride, slot_stride;
+    int n_layers, n_pages, Hkv, d;
+};
+
+// What one request accepts; warp 0 of each CTA fills it in.
+struct Accepted {
+    int len, bonus, status, L;
+    int path[TB_MAX_NODES];
+    long long at[TB_MAX_NODES];   // elements from the layer's first head to slot L + j, -1: no such slot
+    long long src[TB_MAX_NODES];  // the same for slot L + path[j]
+};
+
+__device__ __forceinline__ long long slot_offset(const AcceptArgs &p, const int32_t *table, int slot)
+{
+    const int pg = slot >> p.page_log2;
+    if (pg >= p.max_pages)
+        return -1;
+    const int id = table[pg];
+    if (id < 0 || id >= p.n_pages)
+        return -1;
+    return id * p.page_stride + (slot & ((1 << p.page_log2) - 1)) * p.slot_stride;
+}
+
+__device__ void accept_one(const AcceptArgs &p, int b, Accepted &a)
+{
+    const int lane = threadIdx.x;
+    const int t = p.tree[b], L = p.lens[b], row0 = p.row_start[b], n_here = p.row_start[b + 1] - row0;
+    const bool tree_ok = t >= 0 && t < p.n_trees;
+    const TreeDesc *td = p.trees + (tree_ok ? t : 0);
+    const int n = td->n;
+    // a request that paged_plan gave no rows takes no part in the step
+    const bool live = tree_ok && L >= 0 && row0 >= 0 && n_here == n && row0 + n <= p.n_rows;
+    int len = 0, bonus = -1, status = t >= p.n_trees ? TB_EINVAL : TB_OK;
+    if (live && p.draft) {
+        bool match[2], badtok[2];
+        uint64_t anc[2];
+        int dep[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = lane + 32 * h, par = td->parent[i];
+            anc[h] = td->anc[i];
+            dep[h] = td->depth[i];
+            const int tok = i < n ? p.draft[row0 + i] : 0;
+            badtok[h] = i > 0 && i < n && (tok < 0 || tok >= p.vocab);
+            match[h] = i < n && (i == 0 || (!badtok[h] && tok == p.argmax[row0 + par]));
+        }
+        const uint64_t m = (uint64_t)__ballot_sync(0xffffffffu, match[0]) |
+                           ((uint64_t)__ballot_sync(0xffffffffu, match[1]) << 32);
+        if (__any_sync(0xffffffffu, badtok[0] || badtok[1]))
+            status = TB_EINVAL;
+        // the deepest accepted node, smallest id among equals
+        int best = -1;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = lane + 32 * h;
+            if (i < n && (anc[h] & ~m) == 0)
+                best = max(best, dep[h] * 64 + 63 - i);
+        }
+        best = __reduce_max_sync(0xffffffffu, best);
+        const int j = 63 - (best & 63);
+        const uint64_t on = __shfl_sync(0xffffffffu, j < 32 ? anc[0] : anc[1], j & 31);
+        len = __popcll(on);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = lane + 32 * h;
+            if ((on >> i) & 1)
+                a.path[__popcll(on & ((1ull << i) - 1))] = i;
+        }
+        bonus = p.argmax[row0 + j];
+    } else if (live) {
+        const tb_result &r = p.results[b];
+        len = min(max(r.accept_len, 0), n);
+        for (int j = lane; j < len; j += 32)
+            a.path[j] = min(max(r.path[j], j), n - 1);
+    }
+    __syncwarp();
+    if (p.k && live) {
+        const int32_t *table = p.table + (size_t)b * p.max_pages;
+        for (int j = lane; j < len; j += 32) {
+            a.at[j] = slot_offset(p, table, L + j);
+            a.src[j] = a.path[j] == j ? -1 : slot_offset(p, table, L + a.path[j]);  // in place already: nothing moves
+        }
+    }
+    if (lane == 0) {
+        a.len = len;
+        a.bonus = bonus;
+        a.status = status;
+        a.L = L;
+    }
+}
+
+// Bound by the latency of the chain length, tree, tokens, block table, rows;
+// with many requests by the scattered 128- or 256-byte rows.
+__global__ void __launch_bounds__(kThreads) k_paged_accept(const __grid_constant__ AcceptArgs p)
+{
+    __shared__ Accepted a;
+    pdl_wait();
+    pdl_trigger();
+    const int b = blockIdx.x / kCluster, rank = blockIdx.x % kCluster;
+    if (threadIdx.x < 32)
+        accept_one(p, b, a);
+    __syncthreads();
+    cluster_barrier();  // every CTA of the request has read its length and result
+    if (rank == 0) {
+        tb_result &r = p.results[b];
+        if (p.draft) {
+            if (threadIdx.x < TB_MAX_NODES)
+                r.path[threadIdx.x] = threadIdx.x < a.len ? a.path[threadIdx.x] : 0;
+            if (threadIdx.x == 0) {
+                r.accept_len = a.len;
+                r.bonus_token = a.bonus;
+                r.status = a.status;
+            }
+        }
+        if (threadIdx.x == 0) {
+            r.new_L = a.L + a.len;
+            p.lens_out[b] = a.L + a.len;
+        }
+    }
+    if (!p.k || a.len < 2)
+        return;
+    // pieces: 16 bytes of one (layer, kv head, K or V)
+    const int per_head = p.d >> 3;
+    const long long pieces = 2ll * p.n_layers * p.Hkv * per_head;
+    for (long long x = rank * kThreads + threadIdx.x; x < pieces; x += kCluster * kThreads) {
+        const int c = (int)(x % per_head);
+        const long long y = x / per_head;
+        const int g = (int)(y % p.Hkv);
+        const int lv = (int)(y / p.Hkv);
+        uint16_t *base = ((lv & 1) ? p.v : p.k) + (lv >> 1) * p.layer_stride + g * p.head_stride + 8 * c;
+        for (int j0 = 1; j0 < a.len; j0 += kAhead) {
+            uint4 buf[kAhead];
+            bool move[kAhead];
+#pragma unroll
+            for (int m = 0; m < kAhead; ++m) {
+                const int j = j0 + m;
+                move[m] = j < a.len && a.src[j] >= 0 && a.at[j] >= 0;
+                if (move[m])
+                    buf[m] = *reinterpret_cast<const uint4 *>(base + a.src[j]);
+            }
+#pragma unroll
+            for (int m = 0; m < kAhead; ++m)
+                if (move[m])
+                    *reinterpret_cast<uint4 *>(base + a.at[j0 + m]) = buf[m];
+        }
+    }
+}
+
+}  // namespace
+
+TB_BOUNDS_COUNTER(bounds_violations_paged_accept)
+
+}  // namespace tv
+
+using namespace tv;
+
+extern "C" tb_status paged_accept(const tb_bank *bank, const tb_requests *req, const tb_pages *pages,
+                                  const int32_t *draft_tokens, const int32_t *argmax, int n_rows, int vocab,
+                                  tb_result *results, int32_t *lens_out, tb_stream stream)
+{
+    const char *fn = "paged_accept";
+    AcceptArgs a{};
+    tb_status st = check_device_bank(bank, fn, &a.trees, &a.n_trees);
+    if (st != TB_OK || (st = check_requests(req, true, fn)) != TB_OK)
+        return st;
+    if (!req->tree)
+        return record_error(TB_EINVAL, "%s: req->tree is NULL", fn);
+    if (!results || !lens_out)
+        return record_error(TB_EINVAL, "%s: results or lens_out is NULL", fn);
+    if (draft_tokens && (!argmax || vocab < 1))
+        return record_error(TB_EINVAL, "%s: argmax is NULL or vocab %d < 1", fn, vocab);
+    if (n_rows < 0)
+        return record_error(TB_EINVAL, "%s: n_rows %d", fn, n_rows);
+    if (pages) {
+        if ((st = check_pages(pages, fn)) != TB_OK)
+            return st;
+        if (pages->page_size != req->page_size)
+            return record_error(TB_EINVAL, "%s: pages of %d slots, a table of %d", fn, pages->page_size,
+                                req->page_size);
+        a.k = static_cast<uint16_t *>(pages->k);
+        a.v = static_cast<uint16_t *>(pages->v);
+        a.layer_stride = pages->layer_stride;
+        a.page_stride = pages->page_stride;
+        a.head_stride = pages->head_stride;
+        a.slot_stride = pages->slot_stride;
+        a.n_layers = pages->n_layers;
+        a.n_pages = pages->n_pages;
+        a.Hkv = pages->n_kv_heads;
+        a.d = pages->head_dim;
+    }
+    a.batch = req->batch;
+    a.max_pages = req->max_pages;
+    while ((1 << a.page_log2) < req->page_size)
+        ++a.page_log2;
+    a.n_rows = n_rows;
+    a.vocab = vocab;
+    a.tree = req->tree;
+    a.lens = req->lens;
+    a.row_start = req->row_start;
+    a.table = req->table;
+    a.draft = draft_tokens;
+    a.argmax = argmax;
+    a.results = results;
+    a.lens_out = lens_out;
+    return launch_result(launch_kernel_cluster(k_paged_accept, dim3(req->batch * kCluster), dim3(kThreads), 0,
+                                               (cudaStream_t)stream, true, kCluster, a),
+                         fn);
+}

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "kernels.cuh"
+#include "paged.cuh"
 
 namespace tv {
 
@@ -170,6 +171,30 @@ bool make_tmap_kv(CUtensorMap *map, const void *base, int d, int n_keys, int n_h
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
         *err = "cuTensorMapEncodeTiled (KV cache) rejected the tensor";
+        return false;
+    }
+    return true;
+}
+
+bool make_tmap_pages(CUtensorMap *map, const tb_pages *pages, const void *base, int box_slots, const char **err)
+{
+    if (!get_encode(err))
+        return false;
+    cuuint64_t dims[4] = {(cuuint64_t)pages->head_dim, (cuuint64_t)pages->page_size, (cuuint64_t)pages->n_kv_heads,
+                          (cuuint64_t)pages->n_pages};
+    // the stride of a dimension of one entry is never used, but has to be a valid one
+    const cuuint64_t row = (cuuint64_t)pages->slot_stride * 2;
+    cuuint64_t strides[3] = {row, pages->n_kv_heads > 1 ? (cuuint64_t)pages->head_stride * 2 : row,
+                             pages->n_pages > 1 ? (cuuint64_t)pages->page_stride * 2 : row};
+    cuuint32_t box[4] = {64, (cuuint32_t)box_slots, 1, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    CUresult r = g_encode(map,
+                          pages->dtype == TB_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                          4, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        *err = "cuTensorMapEncodeTiled (pages) rejected the tensor";
         return false;
     }
     return true;
@@ -598,7 +623,9 @@ extern "C" tb_status tb_debug_bounds_violations(uint32_t *count)
         return cuda_fail(e, "tb_debug_bounds_violations");
     unsigned int n = 0;
     for (unsigned int (*f)() : {bounds_violations_attention_tc, bounds_violations_lm_head, bounds_violations_accept,
-                                bounds_violations_rope, bounds_violations_sample}) {
+                                bounds_violations_rope, bounds_violations_sample, bounds_violations_paged_plan,
+                                bounds_violations_paged_store, bounds_violations_paged_attention,
+                                bounds_violations_logits, bounds_violations_paged_accept}) {
         const unsigned int x = f();
         if (x == 0xffffffffu)
             return fail(TB_ECUDA, "tb_debug_bounds_violations: reading a device counter failed");
@@ -663,6 +690,85 @@ static tb_status check_ws(void *ws, size_t bytes, size_t need, const char *fn)
     if (bytes < need)
         return fail(TB_ECAPACITY, "%s: workspace of %zu bytes, %zu needed", fn, bytes, need);
     return TB_OK;
+}
+
+// ------------------------------------------------------------------ checks of the paged calls
+
+tb_status tv::check_device_bank(const tb_bank *bank, const char *fn, const TreeDesc **trees, int *n_trees)
+{
+    if (!bank)
+        return fail(TB_EINVAL, "%s: bank is NULL", fn);
+    if (current_device() != bank->device)
+        return fail(TB_EINVAL, "%s: current device %d is not the bank's device %d", fn, current_device(),
+                    bank->device);
+    *trees = bank->d_desc;
+    *n_trees = bank->count;
+    return TB_OK;
+}
+
+tb_status tv::check_requests(const tb_requests *req, bool table, const char *fn)
+{
+    if (!req)
+        return fail(TB_EINVAL, "%s: req is NULL", fn);
+    if (req->batch < 1 || req->batch > TB_MAX_REQUESTS)
+        return fail(TB_EINVAL, "%s: batch %d outside 1..%d", fn, req->batch, TB_MAX_REQUESTS);
+    if (!req->row_start)
+        return fail(TB_EINVAL, "%s: row_start is NULL", fn);
+    if (!table)
+        return TB_OK;
+    if (!req->lens || !req->table)
+        return fail(TB_EINVAL, "%s: lens or table is NULL", fn);
+    if (req->max_pages < 1)
+        return fail(TB_EINVAL, "%s: max_pages %d", fn, req->max_pages);
+    if (req->page_size < 8 || req->page_size > 1024 || (req->page_size & (req->page_size - 1)))
+        return fail(TB_EINVAL, "%s: page_size %d (a power of two from 8 to 1024)", fn, req->page_size);
+    if ((long long)req->max_pages * req->page_size > 0x7fffffffll - TB_MAX_NODES - kTileKeys)
+        return fail(TB_EINVAL, "%s: max_pages * page_size passes 32 bits", fn);
+    return TB_OK;
+}
+
+tb_status tv::check_pages(const tb_pages *pages, const char *fn)
+{
+    if (!pages || !pages->k || !pages->v)
+        return fail(TB_EINVAL, "%s: pages, pages->k or pages->v is NULL", fn);
+    if (!aligned16(pages->k) || !aligned16(pages->v))
+        return fail(TB_EINVAL, "%s: pages->k / pages->v must be 16-byte aligned", fn);
+    if (pages->dtype != TB_BF16 && pages->dtype != TB_F16)
+        return fail(TB_EUNSUPPORTED, "%s: pages of type %d (TB_BF16 or TB_F16)", fn, pages->dtype);
+    if (pages->head_dim != 64 && pages->head_dim != 128)
+        return fail(TB_EUNSUPPORTED, "%s: head_dim %d (64 or 128 supported)", fn, pages->head_dim);
+    if (pages->n_layers < 1 || pages->n_pages < 1 || pages->n_kv_heads < 1)
+        return fail(TB_EINVAL, "%s: n_layers=%d n_pages=%d n_kv_heads=%d", fn, pages->n_layers, pages->n_pages,
+                    pages->n_kv_heads);
+    if (pages->page_size < 8 || pages->page_size > 1024 || (pages->page_size & (pages->page_size - 1)))
+        return fail(TB_EINVAL, "%s: page_size %d (a power of two from 8 to 1024)", fn, pages->page_size);
+    for (int64_t s : {pages->layer_stride, pages->page_stride, pages->head_stride, pages->slot_stride})
+        if (s < 0 || s % 8)
+            return fail(TB_EINVAL, "%s: strides must be multiples of 8 elements, none negative", fn);
+    if (pages->slot_stride < pages->head_dim || (pages->n_kv_heads > 1 && pages->head_stride < pages->head_dim) ||
+        (pages->n_pages > 1 && pages->page_stride < pages->head_dim))
+        return fail(TB_EINVAL, "%s: slot, head or page stride below head_dim %d", fn, pages->head_dim);
+    return TB_OK;
+}
+
+tb_status tv::check_workspace(const void *ws, size_t bytes, size_t need, const char *fn)
+{
+    return check_ws(const_cast<void *>(ws), bytes, need, fn);
+}
+
+tb_status tv::launch_result(cudaError_t e, const char *fn)
+{
+    return e == cudaSuccess ? ok() : cuda_fail(e, fn);
+}
+
+int tv::device_sms(int device)
+{
+    return sm_count(device < 0 ? current_device() : device);
+}
+
+bool tv::ptr_aligned(const void *p, size_t a)
+{
+    return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0;
 }
 
 // ------------------------------------------------------------------ stages

@@ -1,0 +1,218 @@
+"""logits_process: processed logits bit for bit against the documented 32-bit
+steps, statistics against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paged_reference as ref
+import paper_2606_27550_gb300 as tv
+from paper_2606_27550_gb300 import synth
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def bank():
+    b = tv.Bank(16, 0)
+    for t in ref.trees():
+        b.add(t)
+    yield b
+    b.close()
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return (t if dtype is None else t.to(dtype)).cuda()
+
+
+def pack_bits(allowed):
+    n, V = allowed.shape
+    words = -(-V // 32)
+    full = np.zeros((n, words * 32), bool)
+    full[:, :V] = allowed
+    return np.packbits(full, axis=1, bitorder="little").view(np.uint32).view(np.int32)
+
+
+class Scene:
+    def __init__(self, seed, tree, V, dtype=torch.float32, hist_max=300, pad=0, mask_share=0.7, biases=5, free_rows=None):
+        g = self.g = synth.rng(seed)
+        self.trees, self.tree, self.V = ref.trees(), tree, V
+        B = len(tree)
+        self.n = free_rows or [0 if t < 0 else len(self.trees[t]) for t in tree]
+        self.start = np.concatenate([[0], np.cumsum(self.n)]).astype(np.int32)
+        R = self.R = int(self.start[-1])
+        z = (3 * g.standard_normal((R, V + pad))).astype(np.float32)
+        if R and V > 40:
+            z[:, 7] = z[:, 30] = z.max() + 1  # ties: the lowest index
+        self.logits = dev(z, dtype)[:, :V]
+        self.z = self.logits.float().cpu().numpy()
+        self.hist = g.integers(-2, max(1, min(V, 50)) + 2, (B, hist_max)).astype(np.int32)
+        self.hist_len = g.integers(0, hist_max + 1, B).astype(np.int32)
+        self.hist_len[0] = 0
+        self.prompt = np.array([g.integers(0, x + 1) for x in self.hist_len], np.int32)
+        self.draft = g.integers(-1, max(1, min(V, 60)) + 1, R).astype(np.int32)
+        self.rep = (1 + g.random(B)).astype(np.float32)
+        self.pres, self.freq = g.standard_normal(B).astype(np.float32), g.standard_normal(B).astype(np.float32)
+        counts = g.integers(0, biases * 2 + 1, B)
+        self.bstart = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        self.btok = g.integers(-1, V + 1, self.bstart[-1]).astype(np.int32)
+        self.bval = (5 * g.standard_normal(self.bstart[-1])).astype(np.float32)
+        self.allowed = g.random((R, V)) < mask_share
+        if R > 2:
+            self.allowed[1] = False  # a row without an allowed token
+        self.T = 0.7
+
+    def run(self, bank, rules=("history", "penalty", "bias", "mask", "draft"), in_place=False, mask_row=None, out_pad=0):
+        B, R, V = len(self.tree), self.R, self.V
+        trees = None if bank is None else dev(np.array(self.tree, np.int32))
+        req = tv.Requests(row_start=dev(self.start), tree=trees)
+        out = self.logits if in_place else torch.empty((R, V + out_pad), device="cuda")[:, :V]
+        ws = tv.make_workspace(tv.tb_logits_workspace_size(B, R, V))
+        kw = {}
+        if "history" in rules:
+            kw.update(history=dev(self.hist), history_len=dev(self.hist_len), prompt_len=dev(self.prompt))
+        if "penalty" in rules:
+            kw.update(repetition=dev(self.rep), presence=dev(self.pres), frequency=dev(self.freq))
+        if "bias" in rules:
+            kw.update(bias_start=dev(self.bstart), bias_token=dev(self.btok), bias_value=dev(self.bval))
+        if "draft" in rules:
+            kw.update(draft=dev(self.draft))
+        allowed = None
+        if "mask" in rules:
+            allowed = self.allowed
+            bits = pack_bits(allowed)
+            if mask_row is not None:
+                kw.update(mask_row=dev(mask_row))
+                allowed = np.where(mask_row[:, None] >= 0, allowed[mask_row.clip(0)], True)
+            kw.update(mask=dev(bits))
+        st = {k: torch.full((R,), 55, dtype=torch.int32 if k == "argmax" else torch.float32, device="cuda")
+              for k in ("argmax", "top1", "entropy", "logz_t", "entropy_t")}
+        if "draft" in rules and bank is not None:
+            st["draft_logit"] = torch.full((R,), 55.0, device="cuda")
+        self.call = lambda: tv.logits_process(bank, req, self.logits, out, ws, temperature=self.T, **kw, **st)
+        self.out, self.st = out, st
+        self.call()
+        torch.cuda.synchronize()
+        self.check(rules, bank is not None, allowed)
+        return ws
+
+    def check(self, rules, with_trees, allowed):
+        out = self.out.cpu().numpy()
+        for b in range(len(self.tree)):
+            lo, hi = self.start[b], self.start[b + 1]
+            if lo == hi:
+                continue
+            h = self.hist[b, :self.hist_len[b]].tolist() if "history" in rules else []
+            paths = [[] for _ in range(hi - lo)]
+            parent = None
+            if with_trees and self.tree[b] >= 0:
+                parent = self.trees[self.tree[b]]
+                if "draft" in rules:
+                    anc = ref.ancestors(parent)
+                    paths = [[int(self.draft[lo + j]) for j in range(1, len(parent)) if anc[i, j]]
+                             for i in range(hi - lo)]
+            pen = "penalty" in rules
+            bias = list(zip(self.btok[self.bstart[b]:self.bstart[b + 1]], self.bval[self.bstart[b]:self.bstart[b + 1]]))
+            want = ref.process(self.z[lo:hi], self.rep[b] if pen else 1, self.freq[b] if pen else 0,
+                               self.pres[b] if pen else 0, h[:self.prompt[b]], h[self.prompt[b]:], paths,
+                               bias if "bias" in rules else [], None if allowed is None else allowed[lo:hi])
+            got = out[lo:hi]
+            assert np.array_equal(got, want), f"request {b}: {np.argwhere(got != want)[:4]}"
+            st = {k: v.cpu().numpy() for k, v in self.st.items()}
+            for i in range(hi - lo):
+                a, top1, ent, lz, et = ref.stats(want[i], self.T)
+                assert st["argmax"][lo + i] == a
+                # sums of 2^17 terms and fewer, exponents to 2^-24 of up to 40 each: 1e-5 relative
+                assert abs(st["top1"][lo + i] - top1) <= 1e-5 * top1
+                assert abs(st["entropy"][lo + i] - ent) <= 3e-5 * (1 + ent)
+                assert abs(st["entropy_t"][lo + i] - et) <= 3e-5 * (1 + et)
+                if a < 0:
+                    assert st["logz_t"][lo + i] == -np.inf
+                else:
+                    assert abs(st["logz_t"][lo + i] - lz) <= 2e-5 + 1e-6 * abs(lz)
+            if "draft_logit" in st:
+                for j in range(hi - lo):
+                    tok = int(self.draft[lo + j])
+                    if parent is None or j == 0 or not 0 <= tok < self.V:
+                        assert st["draft_logit"][lo + j] == 55
+                    else:
+                        assert st["draft_logit"][lo + j] == want[parent[j]][tok]
+
+
+@pytest.mark.parametrize("V", [1, 2, 31, 33, 255, 257, 1000, 4099, 32000, 50001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_rules_and_statistics(bank, V, dtype):
+    Scene(V, [5, -1, 0, 8, 3], V, dtype).run(bank)
+
+
+@pytest.mark.parametrize("rules", [(), ("history",), ("penalty",), ("history", "penalty"), ("bias",), ("mask",),
+                                   ("draft",), ("draft", "penalty"), ("mask", "draft", "penalty")])
+def test_each_rule_alone(bank, rules):
+    Scene(len(rules) + 70, [7, 9], 3001).run(bank, rules)
+
+
+def test_many_requests_and_large_chunks(bank):
+    g = synth.rng(4)
+    Scene(5, [int(g.integers(-1, 4)) for _ in range(150)], 5003, hist_max=900, biases=40).run(bank)
+
+
+def test_large_vocabulary(bank):
+    Scene(6, [5, 10, 0, 7], 128256, hist_max=4000, biases=200).run(bank)
+    Scene(7, [3] * 5, 152064, torch.bfloat16).run(bank)
+
+
+def test_rows_without_trees_and_more_than_a_tree_has(bank):
+    Scene(8, [-1, -1, -1], 2000, free_rows=[1, 200, 0]).run(None, ("history", "penalty", "bias", "mask"))
+
+
+def test_in_place_strided_and_shared_masks(bank):
+    Scene(9, [5, 4], 4099).run(bank, in_place=True)
+    Scene(10, [5, 4], 999, pad=7).run(bank, in_place=True)
+    Scene(11, [5, 4], 2048, pad=5).run(bank, out_pad=3)
+    s = Scene(12, [5, 4], 700)
+    s.run(bank, mask_row=s.g.integers(-1, 3, s.R).astype(np.int32))
+
+
+def test_duplicates_add_up_in_list_order(bank):
+    s = Scene(13, [2], 100, biases=60)
+    s.btok[:] = s.btok % 3
+    s.run(bank, ("bias",))
+
+
+def test_masked_nan_and_infinities(bank):
+    s = Scene(14, [3, 3], 1500)
+    s.allowed[:] = True
+    z = s.z
+    bad = s.g.random(z.shape) < 0.3
+    z[bad] = s.g.choice(np.array([np.nan, np.inf, -np.inf], np.float32), int(bad.sum()))
+    s.allowed[bad] = False
+    z[2, 100] = -np.inf  # allowed, never likely
+    s.allowed[2, 100] = True
+    s.logits.copy_(dev(z))
+    s.run(bank)
+
+
+def test_an_allowed_nan_shows_in_the_statistics(bank):
+    s = Scene(15, [1], 600)
+    s.run(bank, ())
+    s.logits[0, 333] = float("nan")
+    s.call()
+    st = {k: v.cpu().numpy() for k, v in s.st.items()}
+    for k in ("top1", "entropy", "logz_t", "entropy_t"):
+        assert np.isnan(st[k][0]) and np.isfinite(st[k][1])
+
+
+def test_temperature_one_and_a_graph(bank):
+    s = Scene(16, [5, 0], 3000)
+    s.T = 1.0
+    s.run(bank)
+    first = s.out.clone(), {k: v.clone() for k, v in s.st.items()}
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        s.call()
+    s.out.zero_()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(s.out, first[0]) and all(torch.equal(s.st[k], v) for k, v in first[1].items())

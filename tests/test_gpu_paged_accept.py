@@ -1,0 +1,145 @@
+"""paged_accept: acceptance against the oracle, moved rows and untouched ones
+byte for byte, lengths in place."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paged_reference as ref
+import paper_2606_27550_gb300 as tv
+from paper_2606_27550_gb300 import synth
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def bank():
+    b = tv.Bank(16, 0)
+    for t in ref.trees():
+        b.add(t)
+    yield b
+    b.close()
+
+
+def i32(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(torch.int32).cuda()
+
+
+class Scene:
+    def __init__(self, seed, lens, tree, layers, H, d, P, layout, vocab=50, match=0.7, refused=()):
+        g = self.g = synth.rng(seed)
+        torch.manual_seed(seed)
+        self.trees, self.lens, self.tree, self.P, self.vocab = ref.trees(), lens, tree, P, vocab
+        B = len(lens)
+        self.n = [0 if t < 0 or b in refused else len(self.trees[t]) for b, t in enumerate(tree)]
+        counts = [-(-(a + b) // P) for a, b in zip(lens, self.n)]
+        n_pages = sum(counts) + 2
+        ids = g.permutation(n_pages)
+        self.table = np.full((B, max(counts) + 1), -1, np.int32)
+        at = 0
+        for b, c in enumerate(counts):
+            self.table[b, :c] = ids[at:at + c]
+            at += c
+        shape = (layers, n_pages, H, P, d) if layout == "heads" else (layers, n_pages, P, H, d)
+        self.pools = []
+        for _ in range(2):
+            t = torch.randint(-30000, 30000, shape, dtype=torch.int16, device="cuda").view(torch.bfloat16)
+            self.pools.append(t if layout == "heads" else t.transpose(2, 3))
+        self.start = np.concatenate([[0], np.cumsum(self.n)])
+        R = int(self.start[-1])
+        self.argmax = g.integers(0, vocab, R).astype(np.int32)
+        self.draft = g.integers(0, vocab, R).astype(np.int32)
+        for b in range(B):
+            p = self.trees[tree[b]] if self.n[b] else []
+            for j in range(1, len(p)):
+                if g.random() < match:
+                    self.draft[self.start[b] + j] = self.argmax[self.start[b] + p[j]]
+        self.req = tv.Requests(row_start=i32(self.start), lens=i32(np.array(lens)), table=i32(self.table), page_size=P,
+                               tree=i32(np.array(tree)))
+        self.results = tv.make_results(B)
+
+    def expected(self, b):
+        lo, hi = self.start[b], self.start[b + 1]
+        return oracle.accept(self.trees[self.tree[b]], self.draft[lo:hi], self.argmax[lo:hi])
+
+    def moved(self, paths):
+        want = [p.clone() for p in self.pools]
+        for b, path in paths.items():
+            L, t = self.lens[b], self.table[b]
+            for new, old in zip(want, self.pools):
+                for j, u in enumerate(path):
+                    new[:, t[(L + j) // self.P], :, (L + j) % self.P] = old[:, t[(L + u) // self.P], :, (L + u) % self.P]
+        return want
+
+
+def same(a, b):
+    return torch.equal(a.contiguous().view(torch.int16), b.contiguous().view(torch.int16))
+
+
+@pytest.mark.parametrize("seed,B,layers,H,d,P,layout,in_place", [
+    (1, 1, 1, 1, 64, 8, "heads", True), (2, 9, 3, 4, 128, 16, "slots", True), (3, 40, 2, 8, 64, 32, "heads", False),
+    (4, 5, 33, 3, 128, 16, "heads", True), (5, 300, 1, 2, 64, 128, "slots", True), (6, 4, 2, 40, 128, 1024, "slots", False)])
+@pytest.mark.parametrize("match", [0.0, 0.7, 1.0])
+def test_accept(bank, seed, B, layers, H, d, P, layout, in_place, match):
+    g = synth.rng(seed + 500)
+    lens = [int(g.integers(0, 200)) for _ in range(B)]
+    tree = [int(g.integers(-1 if B > 1 else 0, 11)) for _ in range(B)]
+    s = Scene(seed, lens, tree, layers, H, d, P, layout, match=match, refused=(2,))
+    paths, results = {}, []
+    for b in range(B):
+        if s.n[b]:
+            k, path, bonus = s.expected(b)
+            paths[b] = path
+            results.append([k, bonus, lens[b] + k, 0] + list(path) + [0] * (64 - k))
+        else:
+            results.append([0, -1, lens[b], 0] + [0] * 64)
+    want = s.moved(paths)
+    out = None if in_place else torch.zeros(B, dtype=torch.int32, device="cuda")
+    tv.paged_accept(bank, s.req, tv.Pages(*s.pools), s.results, draft=i32(s.draft), argmax=i32(s.argmax),
+                    vocab=s.vocab, lens_out=out)
+    torch.cuda.synchronize()
+    assert s.results.tolist() == results
+    assert (s.req.lens if in_place else out).tolist() == [r[2] for r in results]
+    if not in_place:
+        assert s.req.lens.tolist() == lens
+    assert same(s.pools[0], want[0]) and same(s.pools[1], want[1])
+
+
+def test_results_of_another_rule(bank):
+    """accept_len and path given: the rows move, the lengths advance, the results keep their words."""
+    s = Scene(31, [100, 20, 0, 64], [5, 8, -1, 10], 2, 2, 64, 16, "heads")
+    paths = {}
+    res = np.zeros((4, 68), np.int32)
+    for b in (0, 1, 3):
+        parent, u = s.trees[s.tree[b]], len(s.trees[s.tree[b]]) - 1
+        path = []
+        while u >= 0:
+            path.insert(0, int(u))
+            u = parent[u]
+        paths[b] = path
+        res[b, 0], res[b, 1], res[b, 4:4 + len(path)] = len(path), 9, path
+    want = s.moved(paths)
+    s.results.copy_(i32(res))
+    tv.paged_accept(bank, s.req, tv.Pages(*s.pools), s.results)
+    torch.cuda.synchronize()
+    new = [x + len(paths.get(b, ())) for b, x in enumerate(s.lens)]
+    assert s.req.lens.tolist() == new
+    got = s.results.cpu().numpy()
+    assert got[:, 2].tolist() == new
+    got[:, 2] = res[:, 2]
+    assert np.array_equal(got, res)
+    assert same(s.pools[0], want[0]) and same(s.pools[1], want[1])
+
+
+def test_bad_tokens_and_no_pages(bank):
+    s = Scene(41, [10, 30], [3, 3], 1, 1, 64, 16, "heads", match=1.0)
+    s.draft[1] = s.vocab
+    s.draft[8 + 2] = -4
+    before = [p.clone() for p in s.pools]
+    tv.paged_accept(bank, s.req, None, s.results, draft=i32(s.draft), argmax=i32(s.argmax), vocab=s.vocab)
+    torch.cuda.synchronize()
+    for b in range(2):
+        k, path, bonus = s.expected(b)
+        got = s.results[b].tolist()
+        assert got[:4] == [k, bonus, s.lens[b] + k, tv.TB_EINVAL] and got[4:4 + k] == list(path)
+    assert same(before[0], s.pools[0]) and same(before[1], s.pools[1])
