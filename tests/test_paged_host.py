@@ -126,7 +126,7 @@ def test_refusals_of_plan(lib, s):
 def test_refusals_of_store(lib, s):
     refused(tv.TB_EINVAL, s.store, layer=2)
     refused(tv.TB_EINVAL, s.store, layer=-1)
-    refused(tv.TB_EINVAL, s.store, sections=(16, 8))
+    refused(tv.TB_EINVAL, s.store, sections=(16, 8), positions=torch.zeros(2, 9, dtype=torch.int32))
     refused(tv.TB_EINVAL, s.store, sections=(40, -8), positions=torch.zeros(2, 9, dtype=torch.int32))
     refused(tv.TB_EINVAL, s.store, rope_theta=0.5)
     refused(tv.TB_EINVAL, s.store, rope_theta=float("inf"))
