@@ -581,53 +581,58 @@ def verify_step_scheduled(bank: Bank, policy: TbPolicy, state, kv: KvCache, q, h
 # --------------------------------------------------------------------- serving over a paged cache
 
 
-def _dtype(t, *, f32: bool = False) -> int:
+_I32 = _I64 = _F32 = _KINDS = None  # torch's types and the C ABI's numbers for element types
+
+
+def _torch_types():
+    global _I32, _I64, _F32, _KINDS
     import torch
 
-    kinds = {torch.bfloat16: TB_BF16, torch.float16: TB_F16}
-    if f32:
-        kinds[torch.float32] = TB_F32
-    if t.dtype not in kinds:
-        raise TypeError(f"{t.dtype}: {', '.join(map(str, kinds))} expected")
-    return kinds[t.dtype]
+    _I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+    _KINDS = {torch.bfloat16: TB_BF16, torch.float16: TB_F16, torch.float32: TB_F32}
 
 
-def _device_array(t, dtype: str, what: str, shape=None) -> int | None:
-    """The address of a contiguous array of the type that the call reads it as,
-    of at least the given shape's first entries."""
+def _bad_array(t, kind, n: int, what: str):
+    if t.dtype is not kind:
+        raise TypeError(f"{what}: {t.dtype}, {kind} expected")
+    raise ValueError(f"{what}: shape {tuple(t.shape)}, {n} contiguous entries expected")
+
+
+def _arr(t, kind, n: int, what: str) -> int | None:
+    """The address of an array of at least n contiguous entries of the type that the call reads it as."""
     if t is None:
         return None
-    if str(t.dtype) != "torch." + dtype:
-        raise TypeError(f"{what}: {t.dtype}, {dtype} expected")
-    if not t.is_contiguous():
-        raise ValueError(f"{what}: not contiguous")
-    if shape is not None and (t.dim() != len(shape) or any(a < b for a, b in zip(t.shape, shape)) or
-                              tuple(t.shape[1:]) != tuple(shape[1:])):
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, {tuple(shape)} expected")
+    if t.dtype is not kind or t.numel() < n or not t.is_contiguous():
+        _bad_array(t, kind, n, what)
     return t.data_ptr()
 
 
-@dataclass
 class Pages:
     """The paged cache: k and v shaped [n_layers][n_pages][n_kv_heads][page_size][head_dim],
     views of any strides (multiples of 8, elements of a row contiguous), the same for both."""
 
-    k: object
-    v: object
+    def __init__(self, k, v):
+        self.k, self.v = k, v
 
     def as_c(self) -> TbPages:
         k, v = self.k, self.v
-        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(4) != 1:
+        s, shape, dtype = k.stride(), k.shape, k.dtype
+        if len(s) != 5 or s[4] != 1 or v.stride() != s or v.shape != shape or v.dtype is not dtype:
             raise ValueError("pages: k and v of one 5-D shape, type and strides, rows contiguous")
-        n_layers, n_pages, heads, page, d = k.shape
-        s = k.stride()
-        return TbPages(k.data_ptr(), v.data_ptr(), s[0], s[1], s[2], s[3], n_layers, n_pages, heads, page, d, _dtype(k))
+        if _KINDS is None:
+            _torch_types()
+        kind = _KINDS.get(dtype, TB_F32)
+        if kind == TB_F32:
+            raise TypeError(f"pages: {dtype}, bfloat16 or float16 expected")
+        return TbPages(k.data_ptr(), v.data_ptr(), s[0], s[1], s[2], s[3], shape[0], shape[1], shape[2], shape[3],
+                       shape[4], kind)
 
 
-@dataclass
+@dataclass(frozen=True)
 class Requests:
     """A batch of request slots (device int32 tensors): lens [B], table [B][max_pages],
-    row_start [B + 1], and tree [B] (bank ids, -1 for none) or n_new [B]; key_begin [B] or None."""
+    row_start [B + 1], and tree [B] (bank ids, -1 for none) or n_new [B]; key_begin [B] or None.
+    Which tensors they are is fixed; what they hold is read by every call."""
 
     row_start: object
     tree: object = None
@@ -637,15 +642,18 @@ class Requests:
     n_new: object = None
     key_begin: object = None
 
-    def as_c(self) -> TbRequests:
+    def __post_init__(self):
+        if _I32 is None:
+            _torch_types()
         B = self.row_start.shape[0] - 1
-        one = lambda t, what: _device_array(t, "int32", what, (B,))  # noqa: E731
-        return TbRequests(B, 0 if self.table is None else self.table.shape[1], self.page_size, 0,
-                          one(self.tree, "tree"), one(self.n_new, "n_new"), one(self.lens, "lens"),
-                          one(self.key_begin, "key_begin"),
-                          None if self.table is None else _device_array(self.table, "int32", "table",
-                                                                        (B, self.table.shape[1])),
-                          _device_array(self.row_start, "int32", "row_start"))
+        width = 0 if self.table is None else self.table.shape[1]
+        c = TbRequests(B, width, self.page_size, 0, _arr(self.tree, _I32, B, "tree"), _arr(self.n_new, _I32, B, "n_new"),
+                       _arr(self.lens, _I32, B, "lens"), _arr(self.key_begin, _I32, B, "key_begin"),
+                       _arr(self.table, _I32, B * width, "table"), _arr(self.row_start, _I32, B + 1, "row_start"))
+        object.__setattr__(self, "_c", c)
+
+    def as_c(self) -> TbRequests:
+        return self._c
 
 
 @dataclass
@@ -660,13 +668,12 @@ class PagePool:
     held_out: object = None
 
     def as_c(self, batch: int) -> TbPagePool:
-        state_out = self.state if self.state_out is None else self.state_out
-        held_out = self.held if self.held_out is None else self.held_out
-        return TbPagePool(self.ring.shape[0], 0, _device_array(self.ring, "int32", "ring"),
-                          _device_array(self.state, "int32", "state", (2,)),
-                          _device_array(state_out, "int32", "state_out", (2,)),
-                          _device_array(self.held, "int32", "held", (batch,)),
-                          _device_array(held_out, "int32", "held_out", (batch,)))
+        state = _arr(self.state, _I32, 2, "state")
+        held = _arr(self.held, _I32, batch, "held")
+        n = self.ring.numel()
+        return TbPagePool(n, 0, _arr(self.ring, _I32, n, "ring"), state,
+                          state if self.state_out is None else _arr(self.state_out, _I32, 2, "state_out"), held,
+                          held if self.held_out is None else _arr(self.held_out, _I32, batch, "held_out"))
 
 
 def make_page_pool(n_pages: int, batch: int, device="cuda") -> PagePool:
@@ -687,25 +694,31 @@ def make_paged_plan(batch: int, device="cuda"):
     return make_workspace(tb_paged_plan_size(batch), device)
 
 
+def _ref(c):
+    return None if c is None else ctypes.byref(c)
+
+
 def paged_plan(bank, req: Requests, slots, positions, status, plan, pool: PagePool | None = None, n_q_heads: int = 0,
                n_kv_heads: int = 1, window: int = 0, sink: int = 0, stream=None):
     """slots int64, positions int32 [max_rows]; status int32 [B]; bank may be None with n_new."""
-    r = req.as_c()
+    r = req._c
     c = None if pool is None else pool.as_c(r.batch)
     rows = slots.shape[0]
-    _check(load().paged_plan(None if bank is None else bank.handle, ctypes.byref(r),
-                             None if c is None else ctypes.byref(c), _device_array(slots, "int64", "slots"),
-                             _device_array(positions, "int32", "positions", (rows,)), rows,
-                             _device_array(status, "int32", "status", (r.batch,)), n_q_heads, n_kv_heads, window, sink,
-                             _ptr(plan), plan.numel(), _stream(stream)), "paged_plan")
+    rc = load().paged_plan(None if bank is None else bank.handle, ctypes.byref(r), _ref(c),
+                           _arr(slots, _I64, rows, "slots"), _arr(positions, _I32, rows, "positions"), rows,
+                           _arr(status, _I32, r.batch, "status"), n_q_heads, n_kv_heads, window, sink, plan.data_ptr(),
+                           plan.numel(), _stream(stream))
+    if rc:
+        _check(rc, "paged_plan")
 
 
-def _rows_of(t, rows: int, heads: int, pages, what: str) -> TbRows:
-    if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != pages.shape[4] or t.stride(2) != 1:
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, ({rows}, {heads}, {pages.shape[4]}) expected, rows contiguous")
-    if t.dtype != pages.dtype:
-        raise TypeError(f"{what}: {t.dtype}, the pages' {pages.dtype} expected")
-    return TbRows(t.data_ptr(), t.stride(0), t.stride(1))
+def _rows_of(t, rows: int, heads: int, d: int, dtype, what: str) -> TbRows:
+    shape, s = t.shape, t.stride()
+    if len(s) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != d or s[2] != 1:
+        raise ValueError(f"{what}: shape {tuple(shape)}, ({rows}, {heads}, {d}) expected, rows contiguous")
+    if t.dtype is not dtype:
+        raise TypeError(f"{what}: {t.dtype}, the pages' {dtype} expected")
+    return TbRows(t.data_ptr(), s[0], s[1])
 
 
 def paged_kv_store(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None, positions=None, sections=None,
@@ -713,49 +726,44 @@ def paged_kv_store(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None
     """k, v [rows][n_kv_heads][head_dim] and q, q_out [rows][n_q_heads][head_dim] (views of any row
     and head strides); positions int32 [rows] or [axes][rows]; sections: pairs per axis (None: one axis)."""
     c = pages.as_c()
-    rows = slots.shape[0]
-    ck, cv = _rows_of(k, rows, c.n_kv_heads, pages.k, "k"), _rows_of(v, rows, c.n_kv_heads, pages.k, "v")
-    cq = co = None
-    heads = 0
+    rows, heads, H, d, dtype = slots.shape[0], 0, c.n_kv_heads, c.head_dim, pages.k.dtype
+    ck, cv = _rows_of(k, rows, H, d, dtype, "k"), _rows_of(v, rows, H, d, dtype, "v")
+    cq = co = rope = None
     if q is not None:
         heads = q.shape[1]
-        cq = _rows_of(q, rows, heads, pages.k, "q")
-        co = _rows_of(q if q_out is None else q_out, rows, heads, pages.k, "q_out")
-    rope = None
+        cq = _rows_of(q, rows, heads, d, dtype, "q")
+        co = cq if q_out is None else _rows_of(q_out, rows, heads, d, dtype, "q_out")
     if rope_theta:
-        rope = TbRope()
-        sections = (c.head_dim // 2,) if sections is None else tuple(sections)
-        if len(sections) > 4:
-            raise ValueError(f"{len(sections)} position axes: at most 4")
-        pos = positions.view(1, -1) if positions.dim() == 1 else positions
-        rope.theta, rope.n_axes = float(rope_theta), len(sections)
-        for i, n in enumerate(sections):
-            rope.sections[i] = n
-        rope.positions = _device_array(pos, "int32", "positions", (len(sections), pos.shape[1]))
-        if pos.shape[1] < rows:
-            raise ValueError(f"positions: {pos.shape[1]} of {rows} rows")
-        rope.axis_stride = pos.shape[1]
-    ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
-    _check(load().paged_kv_store(ctypes.byref(c), layer, _device_array(slots, "int64", "slots"), rows,
-                                 ctypes.byref(ck), ctypes.byref(cv), ref(cq), ref(co), heads, ref(rope),
-                                 _stream(stream)), "paged_kv_store")
+        sections = (d // 2,) if sections is None else sections
+        axes, stride = len(sections), positions.shape[-1]
+        if axes > 4:
+            raise ValueError(f"{axes} position axes: at most 4")
+        if stride < rows:
+            raise ValueError(f"positions: {stride} of {rows} rows")
+        rope = TbRope(rope_theta, axes, (*sections,), _arr(positions, _I32, axes * stride, "positions"), stride)
+    rc = load().paged_kv_store(ctypes.byref(c), layer, _arr(slots, _I64, rows, "slots"), rows, ctypes.byref(ck),
+                               ctypes.byref(cv), _ref(cq), _ref(co), heads, _ref(rope), _stream(stream))
+    if rc:
+        _check(rc, "paged_kv_store")
 
 
 def paged_tree_attention(bank: Bank, req: Requests, pages: Pages, plan, q, out, ws, layer: int = 0,
                          scale: float | None = None, softcap: float = 0.0, slopes=None, lse=None, stream=None):
     """q, out [rows][n_q_heads][head_dim] of the pages' type; lse float [rows][n_q_heads]; slopes float [n_q_heads];
     scale: 1 / sqrt(head_dim) unless given."""
-    r, c = req.as_c(), pages.as_c()
-    rows, heads, d = q.shape
-    for t, what in ((q, "q"), (out, "out")):
-        if t.dtype != pages.k.dtype or tuple(t.shape) != (rows, heads, c.head_dim) or not t.is_contiguous():
-            raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)}, contiguous {pages.k.dtype} "
-                             f"({rows}, {heads}, {c.head_dim}) expected")
-    _check(load().paged_tree_attention(bank.handle, ctypes.byref(r), ctypes.byref(c), layer, _ptr(plan), plan.numel(),
-                                       _ptr(q), rows, heads, d ** -0.5 if scale is None else float(scale),
-                                       float(softcap), _device_array(slopes, "float32", "slopes", (heads,)), _ptr(out),
-                                       _device_array(lse, "float32", "lse", (rows, heads)), _ptr(ws), ws.numel(),
-                                       _stream(stream)), "paged_tree_attention")
+    c = pages.as_c()
+    shape, dtype = q.shape, pages.k.dtype
+    rows, heads, d = shape
+    if (q.dtype is not dtype or out.dtype is not dtype or out.shape != shape or d != c.head_dim or
+            not q.is_contiguous() or not out.is_contiguous()):
+        raise ValueError(f"q {q.dtype} {tuple(shape)}, out {out.dtype} {tuple(out.shape)}: contiguous {dtype} "
+                         f"(rows, heads, {c.head_dim}) expected for both")
+    rc = load().paged_tree_attention(bank.handle, ctypes.byref(req._c), ctypes.byref(c), layer, plan.data_ptr(),
+                                     plan.numel(), q.data_ptr(), rows, heads, d ** -0.5 if scale is None else scale,
+                                     softcap, _arr(slopes, _F32, heads, "slopes"), out.data_ptr(),
+                                     _arr(lse, _F32, rows * heads, "lse"), ws.data_ptr(), ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "paged_tree_attention")
 
 
 def tb_logits_workspace_size(batch: int, n_rows: int, vocab: int) -> int:
@@ -768,33 +776,37 @@ def logits_process(bank, req: Requests, logits, out, ws, draft=None, history=Non
                    logz_t=None, entropy_t=None, draft_logit=None, stream=None):
     """logits [rows][vocab] (float32, bfloat16 or float16; rows may be strided), out float32 (may be logits);
     history int32 [B][width], mask int32 words [mask rows][width], the rest as the C struct names them."""
-    r = req.as_c()
-    B, (rows, vocab) = r.batch, logits.shape
-    for t, what in ((logits, "logits"), (out, "out")):
-        if tuple(t.shape) != (rows, vocab) or t.stride(1) != 1:
-            raise ValueError(f"{what}: shape {tuple(t.shape)} of strides {t.stride()}, ({rows}, {vocab}) with "
-                             "contiguous rows expected")
-    if _dtype(out, f32=True) != TB_F32:
-        raise TypeError(f"out: {out.dtype}, float32 expected")
-    arr = lambda t, kind, what, n: _device_array(t, kind, what, None if n is None else (n,))  # noqa: E731
-    rules = TbLogitRules(None if history is None else _device_array(history, "int32", "history", (B, history.shape[1])),
-                         0 if history is None else history.shape[1], arr(history_len, "int32", "history_len", B),
-                         arr(prompt_len, "int32", "prompt_len", B), arr(draft, "int32", "draft", rows),
-                         arr(repetition, "float32", "repetition", B), arr(presence, "float32", "presence", B),
-                         arr(frequency, "float32", "frequency", B), arr(bias_start, "int32", "bias_start", B + 1),
-                         arr(bias_token, "int32", "bias_token", None), arr(bias_value, "float32", "bias_value", None),
-                         None if mask is None else _device_array(mask, "int32", "mask"),
-                         0 if mask is None else mask.shape[1], arr(mask_row, "int32", "mask_row", rows))
-    if mask is not None and mask_row is None and mask.shape[0] < rows:
-        raise ValueError(f"mask: {mask.shape[0]} of {rows} rows")
-    st = TbLogitStats(arr(argmax, "int32", "argmax", rows), *(arr(t, "float32", w, rows) for t, w in (
-        (top1, "top1"), (entropy, "entropy"), (logz_t, "logz_t"), (entropy_t, "entropy_t"),
-        (draft_logit, "draft_logit"))))
-    _check(load().logits_process(None if bank is None else bank.handle, ctypes.byref(r), _ptr(logits),
-                                 _dtype(logits, f32=True), logits.stride(0) if rows > 1 else max(vocab, logits.stride(0)),
-                                 rows, vocab, ctypes.byref(rules), float(temperature), _ptr(out),
-                                 out.stride(0) if rows > 1 else max(vocab, out.stride(0)), ctypes.byref(st), _ptr(ws),
-                                 ws.numel(), _stream(stream)), "logits_process")
+    r = req._c
+    B = r.batch
+    shape, s_in, s_out = logits.shape, logits.stride(), out.stride()
+    if len(shape) != 2 or out.shape != shape or (s_in[1] != 1 and shape[1] > 1) or (s_out[1] != 1 and shape[1] > 1):
+        raise ValueError(f"logits {tuple(shape)} of strides {s_in}, out {tuple(out.shape)} of strides {s_out}: two "
+                         "matrices of one shape with contiguous rows expected")
+    kind = _KINDS.get(logits.dtype)
+    if kind is None or out.dtype is not _F32:
+        raise TypeError(f"logits {logits.dtype}, out {out.dtype}: a 32- or 16-bit float type and float32 expected")
+    rows, vocab = shape
+    width = words = 0
+    if history is not None:
+        width = history.shape[-1]
+    if mask is not None:
+        words = mask.shape[-1]
+    rules = TbLogitRules(
+        _arr(history, _I32, B * width, "history"), width, _arr(history_len, _I32, B, "history_len"),
+        _arr(prompt_len, _I32, B, "prompt_len"), _arr(draft, _I32, rows, "draft"), _arr(repetition, _F32, B, "repetition"),
+        _arr(presence, _F32, B, "presence"), _arr(frequency, _F32, B, "frequency"),
+        _arr(bias_start, _I32, B + 1, "bias_start"), _arr(bias_token, _I32, 0, "bias_token"),
+        _arr(bias_value, _F32, 0, "bias_value"), _arr(mask, _I32, 0 if mask_row is not None else rows * words, "mask"),
+        words, _arr(mask_row, _I32, rows, "mask_row"))
+    st = TbLogitStats(_arr(argmax, _I32, rows, "argmax"), _arr(top1, _F32, rows, "top1"),
+                      _arr(entropy, _F32, rows, "entropy"), _arr(logz_t, _F32, rows, "logz_t"),
+                      _arr(entropy_t, _F32, rows, "entropy_t"), _arr(draft_logit, _F32, rows, "draft_logit"))
+    rc = load().logits_process(None if bank is None else bank.handle, ctypes.byref(r), logits.data_ptr(), kind,
+                               s_in[0] if rows > 1 else max(vocab, s_in[0]), rows, vocab, ctypes.byref(rules),
+                               temperature, out.data_ptr(), s_out[0] if rows > 1 else max(vocab, s_out[0]),
+                               ctypes.byref(st), ws.data_ptr(), ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "logits_process")
 
 
 def make_results(batch: int, device="cuda"):
@@ -808,14 +820,16 @@ def paged_accept(bank: Bank, req: Requests, pages, results, draft=None, argmax=N
                  stream=None):
     """results int32 [B][68] (make_results); draft, argmax int32 [rows], or draft None to move by the results given;
     lens_out: None for lens itself; pages None: nothing to move."""
-    r = req.as_c()
+    r = req._c
     c = None if pages is None else pages.as_c()
     rows = 0x7FFFFFFF if draft is None else min(draft.shape[0], argmax.shape[0])
-    _check(load().paged_accept(bank.handle, ctypes.byref(r), None if c is None else ctypes.byref(c),
-                               _device_array(draft, "int32", "draft"), _device_array(argmax, "int32", "argmax"), rows,
-                               vocab, _device_array(results, "int32", "results", (r.batch, RESULT_INTS)),
-                               r.lens if lens_out is None else _device_array(lens_out, "int32", "lens_out", (r.batch,)),
-                               _stream(stream)), "paged_accept")
+    rc = load().paged_accept(bank.handle, ctypes.byref(r), _ref(c), _arr(draft, _I32, 0, "draft"),
+                             _arr(argmax, _I32, 0, "argmax"), rows, vocab,
+                             _arr(results, _I32, r.batch * RESULT_INTS, "results"),
+                             r.lens if lens_out is None else _arr(lens_out, _I32, r.batch, "lens_out"),
+                             _stream(stream))
+    if rc:
+        _check(rc, "paged_accept")
 
 
 # --------------------------------------------------------------------- per-step tree selection
