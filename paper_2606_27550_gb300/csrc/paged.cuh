@@ -30,30 +30,43 @@ struct PlanHeader {
 };
 static_assert(sizeof(PlanHeader) == 64, "");
 
-constexpr int kMaxPlanCtas = 1024;
+// The tiles [t0, t1) of one attention CTA, and the request that t0 lies in.
+struct PlanCta {
+    long long t0, t1, total;
+    int P, idx;  // idx: the request's place among the records
+    PlanReq req;
+};
+static_assert(sizeof(PlanCta) == 88, "eight-byte aligned records");
 
-// header, then the first request of each CTA, then the requests with rows
-// (n_active of them) and one more record whose tile_base is the total
+constexpr int kMaxPlanCtas = 512;
+
+// header, one PlanCta per attention CTA, then the requests with rows (n_active
+// of them) and one more record whose tile_base is the total
 inline size_t plan_bytes_for(int batch)
 {
-    return sizeof(PlanHeader) + kMaxPlanCtas * sizeof(int) + (size_t)(batch + 1) * sizeof(PlanReq);
+    return sizeof(PlanHeader) + kMaxPlanCtas * sizeof(PlanCta) + (size_t)(batch + 1) * sizeof(PlanReq);
 }
-__host__ __device__ inline int *plan_first(void *plan)
+__host__ __device__ inline PlanCta *plan_ctas(void *plan)
 {
-    return reinterpret_cast<int *>(static_cast<unsigned char *>(plan) + sizeof(PlanHeader));
+    return reinterpret_cast<PlanCta *>(static_cast<unsigned char *>(plan) + sizeof(PlanHeader));
 }
 __host__ __device__ inline PlanReq *plan_reqs(void *plan)
 {
     return reinterpret_cast<PlanReq *>(static_cast<unsigned char *>(plan) + sizeof(PlanHeader) +
-                                       kMaxPlanCtas * sizeof(int));
+                                       kMaxPlanCtas * sizeof(PlanCta));
 }
 
-// The first tile of CTA c's range when `total` tiles are split over P CTAs, at
-// least one each where there are so many.
+// The first tile of CTA c's range when `total` tiles are split over P CTAs, and
+// the CTA whose range holds tile t.
 __host__ __device__ inline long long plan_split(long long total, int P, int c)
 {
     const long long q = total / P, r = total % P;
     return q * c + (c < r ? c : r);
+}
+__host__ __device__ inline int plan_cta_of(long long total, int P, long long t)
+{
+    const long long q = total / P, r = total % P, wide = r * (q + 1);
+    return (int)(t < wide ? t / (q + 1) : r + (t - wide) / q);
 }
 
 // argument checks (treeverify.cu); each returns TB_OK or records the error
@@ -62,6 +75,8 @@ tb_status check_requests(const tb_requests *req, bool table, const char *fn);
 tb_status check_pages(const tb_pages *pages, const char *fn);
 tb_status check_workspace(const void *ws, size_t bytes, size_t need, const char *fn);
 tb_status launch_result(cudaError_t e, const char *fn);
+// the attention's partials in a workspace of tb_workspace_size
+float *attention_parts(void *ws);
 int device_sms(int device);  // -1: the current one
 bool ptr_aligned(const void *p, size_t a);
 

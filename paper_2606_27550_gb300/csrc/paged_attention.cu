@@ -1,12 +1,37 @@
 // paged_attention.cu -- tree attention over the pages of one layer: ancestor
 // masks, an optional window with the first tokens kept, capped scores, a bias by
-// distance.
+// distance.  On the 5th-generation tensor cores, as the attention over a
+// contiguous cache (attention_tc.cu) is, with the work split read from the plan
+// of the step.
 //
-// One CTA per (row, query head): its warps share the visible slots, each lane
-// holds d / 32 elements of the query and of the output, and every warp keeps a
-// running maximum m and sum l of its slots (z in units of ln 2),
-//   m' = max(m, z),  l' = l 2^(m - m') + 2^(z - m'),  o' = o 2^(m - m') + 2^(z - m') v,
-// which the first warp joins at the end.
+// A unit is one (request, kv head, block of 128 query rows); its 128-key tiles lie
+// behind one another in a flattened tile space that paged_plan has split evenly
+// over the CTAs.  Per tile
+//   S   = Q K^T   M = 128 rows, N = 128 keys; Q is the TMEM operand, the K tile a
+//                 K-major shared-memory operand
+//   O  += P V     N = head_dim; P = 2^(z - m) is the TMEM operand, the V tile an
+//                 MN-major one
+// with the scores z in units of ln 2 and a reference maximum m that is raised (and
+// O and the sum rescaled) only when the row's maximum has grown past it by 2^8
+// (2^7 in fp16).  A unit split between CTAs leaves one (O, m, l) per CTA, which
+// k_paged_merge joins by log-sum-exp in CTA order: the same sums every time.
+//
+// A tile's 128 slots are 128 / page_size pages (or a part of one): the lanes of a
+// producer warp look their pages up one tile ahead and issue one TMA box each.
+// Pages past the request's end, and ids outside the pool, are addressed past the
+// last page, where TMA fills zeros.  Slots of a landed tile that no row may see (a
+// page's rest behind the last token, before a document's beginning, between the
+// kept first tokens and the window) can hold anything: their scores are replaced
+// (not multiplied) by -inf, and the softmax threads overwrite their V rows with
+// zeros before P V reads them, since 0 * NaN is NaN.
+//
+// One CTA per SM, 12 warps: 0 and 3 load K and V tiles through separate rings, 1
+// issues Q K^T (S double-buffered) and holds the TMEM, 2 issues P V, 4-7 are the
+// softmax (a thread per row), 8-11 stage the next unit's queries and write the
+// finished unit's output.
+// TMEM columns: S0 [0, 128), S1 [128, 256), P0 / P1 on their first halves, O [256,
+// 256 + kD), Q0 [384, 384 + kD / 2), Q1 behind it.  Row r sits in lane 32 (r % 4) +
+// r / 4, so that few rows spread over the four SM sub-partitions.
 #include "paged.cuh"
 
 #include <cuda_fp16.h>
@@ -17,151 +42,835 @@ namespace tv {
 
 namespace {
 
-constexpr int kThreads = 128, kWarps = kThreads / 32;
+constexpr int kBN = kTileKeys;
+constexpr int kAtom = 128 * 128;  // bytes of a 64-column swizzle atom of 128 rows
+constexpr int kThreads = 384;
+constexpr int kKStages = 3, kVStages = 2, kMaxStages = 3;
+constexpr uint32_t kColS = 0, kColO = 256, kColQ = 384;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// score forms
+constexpr int kPlain = 0, kCap = 1, kBias = 2;  // kBias: a bias by distance, capped or not
+
+constexpr int tile_bytes(int d)
+{
+    return d / 64 * kAtom;
+}
+// floats per partial slot: O[128][kD], m[128], l[128]
+constexpr int slot_floats(int d)
+{
+    return 128 * d + 256;
+}
 
 struct PagedArgs {
+    CUtensorMap tk, tv;  // of the layer
     const TreeDesc *trees;
     const int32_t *table;
     int max_pages, page_log2, n_pages, batch;
-    const uint16_t *k, *v;  // of the layer
-    long long page_stride, head_stride, slot_stride;
     const uint16_t *q;
     uint16_t *out;
     float *lse;
     const float *slopes;
-    int n_rows, Hq, Hkv, d;
-    float scale, softcap;
+    int n_rows, Hq, Hkv, group;
+    float scale;      // of the raw scores, times log2(e)
+    float cap, cap_in;  // cap log2(e); 2 scale / cap, times log2(e)
     void *plan;
+    float *part;
     int *status;
 };
-
-template <bool kF16>
-__device__ __forceinline__ float2 unpack(uint32_t w)
-{
-    if constexpr (kF16)
-        return __half22float2(*reinterpret_cast<const __half2 *>(&w));
-    else
-        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-}
 
 template <bool kF16>
 __device__ __forceinline__ uint32_t pack(float lo, float hi)
 {
     if constexpr (kF16) {
-        const __half2 h = __floats2half2_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t *>(&h);
+        uint32_t r;
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
     } else {
         return pack_bf16x2(lo, hi);
     }
 }
 
-// kD / 32 elements of a lane
-template <bool kF16, int kD>
-struct Lane {
-    float v[kD / 32];
-    __device__ __forceinline__ void load(const uint16_t *row, int lane)
+// Instruction descriptor of a kind::f16 MMA with M = 128 and f32 accumulation.
+template <bool kF16>
+__device__ constexpr uint32_t idesc(int N, bool b_mn)
+{
+    const uint32_t bf = idesc_bf16_f32(128, N, false, b_mn);
+    return kF16 ? bf & ~((1u << 7) | (1u << 10)) : bf;  // both operand types: 0 is f16, 1 bf16
+}
+
+__device__ __forceinline__ float rcp_approx(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// cap tanh(scale s / cap) in units of ln 2: tanh y = 1 - 2 / (1 + e^(2y)), with the
+// right limits where the exponential overflows or vanishes
+__device__ __forceinline__ float capped(float s, float cap, float cap_in)
+{
+    return fmaf(-2.f * cap, rcp_approx(1.f + ex2_approx(s * cap_in)), cap);
+}
+
+// The bits of [lo, hi) relative to s0, of 32.
+__device__ __forceinline__ uint32_t range_bits(int s0, int lo, int hi)
+{
+    const int a = max(lo - s0, 0), b = min(hi - s0, 32);
+    if (a >= b)
+        return 0u;
+    return (0xffffffffu >> (32 - (b - a))) << a;
+}
+
+// A CTA's position: the request that its next tile lies in, the one after it
+// fetched ahead.
+struct Cursor {
+    PlanReq r, next;
+    const PlanReq *reqs;
+    int idx;
+    long long end, t1;  // first tile past the request; past the CTA's range
+
+    __device__ __forceinline__ void start(const PlanCta &c, long long past, const PlanReq *all, int Hkv)
     {
-#pragma unroll
-        for (int i = 0; i < kD / 64; ++i) {
-            const float2 x = unpack<kF16>(reinterpret_cast<const uint32_t *>(row)[lane * (kD / 64) + i]);
-            v[2 * i] = x.x, v[2 * i + 1] = x.y;
+        r = c.req;
+        reqs = all;
+        idx = c.idx;
+        t1 = past;
+        set_end(Hkv);
+        if (end < t1)
+            next = reqs[idx + 1];
+    }
+    __device__ __forceinline__ void set_end(int Hkv) { end = r.tile_base + (long long)r.T * Hkv * r.row_blocks; }
+    // moves on to the request of tile t
+    __device__ __forceinline__ void seek(long long t, int Hkv)
+    {
+        while (t >= end) {
+            r = next;
+            ++idx;
+            set_end(Hkv);
+            if (end < t1)
+                next = reqs[idx + 1];
         }
     }
 };
 
-template <bool kF16, int kD>
-__global__ void __launch_bounds__(kThreads) k_paged_attention(const __grid_constant__ PagedArgs p)
+// A run of tiles of one unit.
+struct Seg {
+    int u, j0, n;
+};
+__device__ __forceinline__ Seg seg_at(const Cursor &c, long long t)
 {
-    __shared__ float s_o[kWarps][kD], s_m[kWarps], s_l[kWarps];
+    Seg g;
+    const long long tl = t - c.r.tile_base;
+    g.u = (unsigned long long)tl <= 0xffffffffull ? (int)((uint32_t)tl / (uint32_t)c.r.T) : (int)(tl / c.r.T);
+    g.j0 = (int)(tl - (long long)g.u * c.r.T);
+    const long long left = c.t1 - t;
+    g.n = left < c.r.T - g.j0 ? (int)left : c.r.T - g.j0;
+    return g;
+}
+__device__ __forceinline__ int tile_key(int j, int a0, int n1, int b0)
+{
+    return (j < n1 ? a0 + j : b0 + j - n1) * kBN;
+}
+
+// What the softmax needs of a segment, written with its queries.
+struct SegInfo {
+    int n, j0, a0, n1, b0;
+    int L, end, begin, far, lo_min, lo_max;  // far: end of the kept first tokens within the prefix
+    int lo[128];         // per row: the first prefix slot that its window sees
+    uint64_t anc[128];   // tree nodes that it sees
+    int pos[128];
+    float slope[128];    // times log2(e)
+    float m[128], l[128];  // written back by the softmax
+    int8_t depth[kMaxNodes];
+};
+
+template <int kD, bool kF16, int kForm>
+__global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_constant__ PagedArgs p)
+{
+    constexpr int kTile = tile_bytes(kD), kSlot = slot_floats(kD);
+    // fp16 weights are held 2^8 larger, so that small ones keep their bits above the
+    // subnormals; the largest stays below 2^15
+    constexpr float kShift = kF16 ? 8.f : 0.f, kGrow = kF16 ? 7.f : 8.f;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
+    __shared__ __align__(8) uint64_t s_full[2], p_full[2], pv_done[2], q_full[2], ml_full[2], o_free[2], drain_bar;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag, s_ok;
+    __shared__ __align__(8) PlanCta s_cta;
+    __shared__ SegInfo s_info[2];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *sK = smem, *sV = smem + (size_t)kKStages * kTile;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kMaxStages; ++s) {
+            mbar_init(&k_full[s], 1);
+            mbar_init(&k_empty[s], 1);
+            mbar_init(&v_full[s], 1);
+            mbar_init(&v_empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&s_full[b], 1);
+            mbar_init(&p_full[b], 4);
+            mbar_init(&pv_done[b], 1);
+            mbar_init(&q_full[b], 4);
+            mbar_init(&ml_full[b], 4);
+            mbar_init(&o_free[b], 4);
+        }
+        mbar_init(&drain_bar, 2);
+        abort_flag = 0;
+        fence_mbar_init();
+        prefetch_tmap(&p.tk);
+        prefetch_tmap(&p.tv);
+    }
+    if (warp == 1) {
+        tmem_alloc(&tmem_slot, 512);
+        tmem_relinquish();
+    }
     pdl_wait();
     pdl_trigger();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const PlanHeader *hd = static_cast<const PlanHeader *>(p.plan);
-    if (!hd->valid || hd->batch != p.batch || hd->n_q_heads != p.Hq || hd->n_kv_heads != p.Hkv) {
-        if (threadIdx.x == 0)
-            atomicOr(p.status, kStatusBounds);
-        return;
+    if (warp == 2) {
+        if (lane < (int)(sizeof(PlanCta) / 8))
+            reinterpret_cast<long long *>(&s_cta)[lane] = reinterpret_cast<const long long *>(plan_ctas(p.plan) + c)[lane];
+        if (lane == 31) {
+            const PlanHeader *hd = static_cast<const PlanHeader *>(p.plan);
+            s_ok = hd->valid && hd->batch == p.batch && hd->n_q_heads == p.Hq && hd->n_kv_heads == p.Hkv;
+            if (!s_ok)
+                atomicOr(p.status, kStatusBounds);
+        }
     }
-    const int row = blockIdx.x, h = blockIdx.y;
-    if (row >= hd->rows)
-        return;
-    const PlanReq *reqs = plan_reqs(p.plan);
-    int lo = 0, hi = hd->n_active;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (reqs[mid].row0 <= row)
-            lo = mid;
-        else
-            hi = mid;
-    }
-    const PlanReq rq = reqs[lo];
-    const int i = row - rq.row0, L = rq.L, g = h / (p.Hq / p.Hkv);
-    const TreeDesc &td = p.trees[rq.tree];
-    const uint64_t anc = td.anc[i];
-    const int pos = L + td.depth[i];
-    const float slope = p.slopes ? p.slopes[h] : 0.f;
-    Lane<kF16, kD> q;
-    q.load(p.q + ((size_t)row * p.Hq + h) * kD, lane);
-    float o[kD / 32] = {}, m = -INFINITY, l = 0.f;
-    for (int s = rq.begin + warp; s < L + rq.n; s += kWarps) {
-        const int j = s - L;
-        if (j >= 0 && !((anc >> j) & 1))
-            continue;
-        const int at = j < 0 ? s : L + td.depth[j];
-        if (hd->window > 0 && pos - at >= hd->window && s >= rq.far_end)
-            continue;
-        const int id = p.table[(size_t)rq.b * p.max_pages + (s >> p.page_log2)];
-        if (id < 0 || id >= p.n_pages)
-            continue;
-        const long long off = id * p.page_stride + g * p.head_stride + (s & ((1 << p.page_log2) - 1)) * p.slot_stride;
-        Lane<kF16, kD> k, v;
-        k.load(p.k + off, lane);
-        v.load(p.v + off, lane);
-        float z = 0.f;
-#pragma unroll
-        for (int x = 0; x < kD / 32; ++x)
-            z += q.v[x] * k.v[x];
-#pragma unroll
-        for (int x = 16; x >= 1; x >>= 1)
-            z += __shfl_xor_sync(0xffffffffu, z, x);
-        z *= p.scale;
-        if (p.softcap > 0.f)
-            z = p.softcap * tanhf(z / p.softcap);
-        z = (z - slope * (float)(pos - at)) * kLog2e;
-        const float m2 = fmaxf(m, z), w = exp2f(m - m2), e = exp2f(z - m2);
-        m = m2;
-        l = l * w + e;
-#pragma unroll
-        for (int x = 0; x < kD / 32; ++x)
-            o[x] = o[x] * w + e * v.v[x];
-    }
-#pragma unroll
-    for (int x = 0; x < kD / 32; ++x)
-        s_o[warp][lane * (kD / 32) + x] = o[x];
-    if (lane == 0)
-        s_m[warp] = m, s_l[warp] = l;
+    tc_fence_before();
     __syncthreads();
-    if (warp)
-        return;
-    float M = -INFINITY, sum = 0.f;
-    for (int w = 0; w < kWarps; ++w)
-        M = fmaxf(M, s_m[w]);
-    float acc[kD / 32] = {};
-    for (int w = 0; w < kWarps; ++w) {
-        const float f = s_m[w] == -INFINITY ? 0.f : exp2f(s_m[w] - M);
-        sum += f * s_l[w];
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const long long t0 = s_ok ? s_cta.t0 : 0, t1 = s_ok ? s_cta.t1 : 0;
+    const PlanReq *reqs = plan_reqs(p.plan);
+
+    if (warp < 4) {
+        Cursor cur;  // (a CTA without tiles has an empty one)
+        cur.start(s_cta, t1, reqs, p.Hkv);
+        if (warp == 0 || warp == 3) {
+            // ------------------------------------------------ producers: a page per lane
+            const bool is_v = warp == 3;
+            uint64_t *full = is_v ? v_full : k_full;
+            uint64_t *empty = is_v ? v_empty : k_empty;
+            const int S = is_v ? kVStages : kKStages;
+            uint8_t *ring = is_v ? sV : sK;
+            const CUtensorMap *map = is_v ? &p.tv : &p.tk;
+            const int pages_log2 = p.page_log2 >= 7 ? 0 : 7 - p.page_log2;  // pages of a tile
+            const int a = lane >> pages_log2, pg = lane & ((1 << pages_log2) - 1);
+            const bool box = a < kD / 64;
+            const uint32_t dst_off = (uint32_t)a * kAtom + ((uint32_t)pg << (p.page_log2 + 7));
+            const int page_mask = (1 << p.page_log2) - 1;
+            // this lane's page of tile j of the current request
+            auto page_of = [&](int j) {
+                const int slot = tile_key(j, cur.r.a0, cur.r.n1, cur.r.b0) + (pg << p.page_log2);
+                const int at = slot >> p.page_log2;
+                int id = -1;
+                if (box && slot < cur.r.L + cur.r.n && at < p.max_pages)
+                    id = p.table[(size_t)cur.r.b * p.max_pages + at];
+                return id < 0 || id >= p.n_pages ? p.n_pages : id;  // past the last page: zeros
+            };
+            long long issued = 0;
+            int s = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (long long t = t0; ok && t < t1;) {
+                cur.seek(t, p.Hkv);
+                const Seg g = seg_at(cur, t);
+                const int head = g.u / cur.r.row_blocks;
+                int id = page_of(g.j0);
+                for (int j = 0; j < g.n; ++j) {
+                    const int id_next = j + 1 < g.n ? page_of(g.j0 + j + 1) : 0;
+                    if (lane == 0)
+                        ok = mbar_wait_bounded(&empty[s], ph ^ 1u, &abort_flag, p.status);
+                    ok = __shfl_sync(0xffffffffu, ok, 0);
+                    if (!ok)
+                        break;
+                    if (lane == 0)
+                        mbar_arrive_expect_tx(&full[s], kTile);
+                    __syncwarp();
+                    if (box)
+                        tma_load_4d(ring + (size_t)s * kTile + dst_off, map, &full[s], 64 * a,
+                                    p.page_log2 > 7 ? tile_key(g.j0 + j, cur.r.a0, cur.r.n1, cur.r.b0) & page_mask : 0,
+                                    head, id);
+                    id = id_next;
+                    ++issued;
+                    if (++s == S) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
+                }
+                t += g.n;
+            }
+            if (!ok && lane == 0)
+                for (long long it = (issued > S ? issued - S : 0); it < issued; ++it)
+                    mbar_wait_drain(&full[it % S], (uint32_t)(it / S) & 1u);
+            __syncwarp();
+        } else if (lane == 0 && warp == 1) {
+            // ------------------------------------------------ Q K^T issuer
+            long long it = 0;
+            int s = 0, sg = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (long long t = t0; ok && t < t1; ++sg) {
+                cur.seek(t, p.Hkv);
+                const Seg g = seg_at(cur, t);
+                const uint32_t q_col = tmem + kColQ + (sg & 1) * (kD / 2);
+                for (int j = 0; j < g.n; ++j, ++it) {
+                    const int b = (int)(it & 1);
+                    // K landed; P V(it - 2) has read P_b, whose columns are S_b's; at a segment's
+                    // first tile, its queries are staged
+                    if (!mbar_wait_bounded(&k_full[s], ph, &abort_flag, p.status) ||
+                        (it >= 2 &&
+                         !mbar_wait_bounded(&pv_done[b], (uint32_t)((it - 2) >> 1) & 1u, &abort_flag, p.status)) ||
+                        (j == 0 &&
+                         !mbar_wait_bounded(&q_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status))) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t k_base = smem_u32(sK + (size_t)s * kTile);
 #pragma unroll
-        for (int x = 0; x < kD / 32; ++x)
-            acc[x] += f * s_o[w][lane * (kD / 32) + x];
+                    for (int kk = 0; kk < kD / 16; ++kk) {
+                        const uint32_t off = (uint32_t)(kk >> 2) * kAtom + (uint32_t)(kk & 3) * 32;
+                        tc_mma_f16_ts(tmem + kColS + b * 128, q_col + kk * 8, smem_desc_sw128(k_base + off, 0, 1024),
+                                      idesc<kF16>(kBN, false), kk > 0 ? 1u : 0u);
+                    }
+                    tc_commit(&s_full[b]);
+                    tc_commit(&k_empty[s]);
+                    if (++s == kKStages) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
+                }
+                t += g.n;
+            }
+            tc_commit(&drain_bar);
+        } else if (lane == 0) {
+            // ------------------------------------------------ P V issuer
+            long long it = 0;
+            int s = 0, sg = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (long long t = t0; ok && t < t1; ++sg) {
+                cur.seek(t, p.Hkv);
+                const Seg g = seg_at(cur, t);
+                for (int j = 0; j < g.n; ++j, ++it) {
+                    const int b = (int)(it & 1);
+                    // P written; at a segment's first tile, the previous segment's O has been read
+                    if (!mbar_wait_bounded(&p_full[b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status) ||
+                        (j == 0 && sg > 0 &&
+                         !mbar_wait_bounded(&o_free[(sg - 1) & 1], (uint32_t)((sg - 1) >> 1) & 1u, &abort_flag,
+                                            p.status)) ||
+                        !mbar_wait_bounded(&v_full[s], ph, &abort_flag, p.status)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t v_base = smem_u32(sV + (size_t)s * kTile);
+#pragma unroll
+                    for (int ks = 0; ks < kBN / 16; ++ks)
+                        tc_mma_f16_ts(tmem + kColO, tmem + kColS + b * 128 + ks * 8,
+                                      smem_desc_sw128(v_base + ks * 2048, kAtom, 1024), idesc<kF16>(kD, true),
+                                      (j == 0 && ks == 0) ? 0u : 1u);
+                    tc_commit(&v_empty[s]);
+                    tc_commit(&pv_done[b]);
+                    if (++s == kVStages) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
+                }
+                t += g.n;
+            }
+            tc_commit(&drain_bar);
+        }
+    } else if (warp < 8) {
+        // ---------------------------------------------------- softmax (warps 4-7)
+        const int q4 = warp & 3;
+        const uint32_t lane_addr = tmem + ((uint32_t)(32 * q4) << 16);
+        const int rloc = 4 * lane + q4;
+        long long it = 0;
+        bool aborted = false;
+        int sg = 0;
+        for (long long t = t0; t < t1 && !aborted; ++sg) {
+            SegInfo &si = s_info[sg & 1];
+            if (!mbar_wait_bounded(&q_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status))
+                break;
+            const int n = si.n, L = si.L, end = si.end, lo = si.lo[rloc], pos = si.pos[rloc];
+            const uint64_t anc = si.anc[rloc];
+            const float slope = si.slope[rloc];
+            t += n;
+            float m_ref = -INFINITY, l = 0.f;
+            for (int j = 0; j < n; ++j, ++it) {
+                const int b = (int)(it & 1);
+                const int key0 = tile_key(si.j0 + j, si.a0, si.n1, si.b0);
+                if (!mbar_wait_bounded(&s_full[b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status)) {
+                    aborted = true;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t sa = lane_addr + kColS + b * 128;
+                const bool masked = key0 + kBN > L || key0 < si.lo_max;
+                // scores that are not a multiple of S are written back in units of ln 2
+                const bool final_z = kForm == kBias || (kForm == kCap && masked);
+
+                // pass 1: the row maximum over the allowed keys, 32 columns at a time
+                float mx = -INFINITY;
+#pragma unroll 1
+                for (int c0 = 0; c0 < kBN; c0 += 32) {
+                    uint32_t r[32];
+                    tmem_ld_32x32b_x32(sa + c0, r);
+                    tmem_ld_wait();
+                    const int s0 = key0 + c0;
+                    if constexpr (kForm == kBias) {
+                        if (p.cap > 0.f) {
+#pragma unroll
+                            for (int x = 0; x < 32; ++x)
+                                r[x] = __float_as_uint(capped(__uint_as_float(r[x]), p.cap, p.cap_in));
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 32; ++x)
+                                r[x] = __float_as_uint(__uint_as_float(r[x]) * p.scale);
+                        }
+                        if (s0 + 32 <= L) {
+                            const float d0 = (float)(pos - s0);
+#pragma unroll
+                            for (int x = 0; x < 32; ++x)
+                                r[x] = __float_as_uint(fmaf(-slope, d0 - (float)x, __uint_as_float(r[x])));
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 32; ++x) {
+                                const int node = s0 + x - L;
+                                const int at = node < 0 ? s0 + x : L + si.depth[min(node, kMaxNodes - 1)];
+                                r[x] = __float_as_uint(fmaf(-slope, (float)(pos - at), __uint_as_float(r[x])));
+                            }
+                        }
+                    }
+                    if (masked) {
+                        uint32_t allow = range_bits(s0, lo, L) | range_bits(s0, si.begin, si.far);
+                        if (s0 >= L)
+                            allow |= s0 - L < 64 ? (uint32_t)(anc >> (s0 - L)) : 0u;
+                        else if (s0 + 32 > L)
+                            allow |= (uint32_t)(anc << (L - s0));
+                        if constexpr (kForm == kCap) {
+#pragma unroll
+                            for (int x = 0; x < 32; ++x)
+                                r[x] = __float_as_uint(capped(__uint_as_float(r[x]), p.cap, p.cap_in));
+                        }
+#pragma unroll
+                        for (int x = 0; x < 32; ++x)
+                            r[x] = (allow >> x) & 1u ? r[x] : 0xff800000u;
+                    }
+                    if (masked || kForm == kBias) {
+                        tmem_st_32x32b_x32(sa + c0, r);
+                        tmem_st_wait();
+                    }
+#pragma unroll
+                    for (int x = 0; x < 32; ++x)
+                        mx = fmaxf(mx, __uint_as_float(r[x]));
+                }
+                if (!final_z)
+                    mx = kForm == kCap ? capped(mx, p.cap, p.cap_in) : mx * p.scale;
+
+                // the lazily raised reference
+                float alpha = 1.f;
+                bool rescale = false;
+                if (j == 0) {
+                    m_ref = mx - kShift;
+                } else if (mx > m_ref + kShift + kGrow) {
+                    alpha = m_ref == -INFINITY ? 0.f : ex2_approx(m_ref - (mx - kShift));
+                    m_ref = mx - kShift;
+                    rescale = true;
+                }
+                if (__any_sync(0xffffffffu, rescale)) {
+                    const long long jp = it - 1;
+                    if (!mbar_wait_bounded(&pv_done[jp & 1], (uint32_t)(jp >> 1) & 1u, &abort_flag, p.status)) {
+                        aborted = true;
+                        break;
+                    }
+                    tc_fence_after();
+                    l *= alpha;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kD; c0 += 32) {
+                        uint32_t o[32];
+                        tmem_ld_32x32b_x32(lane_addr + kColO + c0, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int x = 0; x < 32; ++x)
+                            o[x] = __float_as_uint(__uint_as_float(o[x]) * alpha);
+                        tmem_st_32x32b_x32(lane_addr + kColO + c0, o);
+                    }
+                    tmem_st_wait();
+                }
+
+                // pass 2: P in the pages' type, its 32-bit sum into l
+                const float mu = m_ref == -INFINITY ? 0.f : m_ref;
+                float rs = 0.f;
+#pragma unroll 1
+                for (int c0 = 0; c0 < kBN; c0 += 32) {
+                    uint32_t r[32];
+                    tmem_ld_32x32b_x32(sa + c0, r);
+                    tmem_ld_wait();
+                    if (kForm == kCap && !final_z) {
+#pragma unroll
+                        for (int x = 0; x < 32; ++x)
+                            r[x] = __float_as_uint(capped(__uint_as_float(r[x]), p.cap, p.cap_in));
+                    }
+                    const float f = kForm == kPlain ? p.scale : 1.f;
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const float p0 = ex2_approx(fmaf(__uint_as_float(r[2 * x]), f, -mu));
+                        const float p1 = ex2_approx(fmaf(__uint_as_float(r[2 * x + 1]), f, -mu));
+                        rs += p0 + p1;
+                        pk[x] = pack<kF16>(p0, p1);
+                    }
+                    tmem_st_32x32b_x16(sa + c0 / 2, pk);
+                }
+                l += rs;
+                if (key0 + kBN > end || key0 < si.lo_min) {
+                    // V rows that nobody sees may hold anything: zeros, once the tile has landed
+                    const int sv = (int)(it % kVStages);
+                    if (!mbar_wait_bounded(&v_full[sv], (uint32_t)(it / kVStages) & 1u, &abort_flag, p.status)) {
+                        aborted = true;
+                        break;
+                    }
+                    const int slot = key0 + rloc;
+                    if (slot >= end || slot < si.begin || (slot < si.lo_min && slot >= si.far)) {
+                        uint8_t *row = sV + (size_t)sv * kTile + rloc * 128;
+#pragma unroll
+                        for (int x = 0; x < kD / 8; ++x)
+                            *reinterpret_cast<uint4 *>(row + (x >> 3) * kAtom + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(&p_full[b]);
+            }
+            if (aborted)
+                break;
+            if (sg >= 2 && !mbar_wait_bounded(&o_free[sg & 1], (uint32_t)((sg >> 1) - 1) & 1u, &abort_flag, p.status))
+                break;
+            si.m[rloc] = m_ref;
+            si.l[rloc] = l;
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(&ml_full[sg & 1]);
+        }
+    } else if (t0 < t1) {
+        // ---------------------------------------------------- staging and epilogue (warps 8-11)
+        const int q4 = warp & 3;
+        const uint32_t lane_addr = tmem + ((uint32_t)(32 * q4) << 16);
+        const int rloc = 4 * lane + q4;
+        struct Unit {
+            int n, j0, T;
+            bool first, valid;
+            PlanReq r;
+            size_t row;  // (row, query head) of this thread
+            int node, qh;
+        };
+        Cursor cur;
+        cur.start(s_cta, t1, reqs, p.Hkv);
+        const int window = static_cast<const PlanHeader *>(p.plan)->window;
+        auto describe = [&](long long t) {
+            cur.seek(t, p.Hkv);
+            const Seg g = seg_at(cur, t);
+            Unit u;
+            u.n = g.n;
+            u.j0 = g.j0;
+            u.T = cur.r.T;
+            u.first = t == t0;
+            u.r = cur.r;
+            const int rb = g.u % cur.r.row_blocks, head = g.u / cur.r.row_blocks, grow = rb * 128 + rloc;
+            u.node = grow / p.group;
+            u.qh = head * p.group + grow % p.group;
+            u.valid = u.node < cur.r.n && cur.r.row0 + u.node < p.n_rows;
+            if (u.valid)
+                u.valid = in_bounds(u.node < kMaxNodes && u.qh < p.Hq && cur.r.row0 >= 0, p.status);
+            u.row = u.valid ? (size_t)(cur.r.row0 + u.node) * p.Hq + u.qh : 0;
+            return u;
+        };
+        auto stage = [&](const Unit &u, int sg) {
+            SegInfo &si = s_info[sg & 1];
+            const uint32_t col = lane_addr + kColQ + (sg & 1) * (kD / 2);
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.q + u.row * kD);
+            uint4 qv[kD / 8];
+#pragma unroll
+            for (int i = 0; i < kD / 8; ++i)
+                qv[i] = u.valid ? src[i] : make_uint4(0, 0, 0, 0);
+            // what this row sees
+            const TreeDesc &td = p.trees[u.r.tree];
+            const int tid = threadIdx.x - 256, L = u.r.L;
+            const int dep = u.valid ? td.depth[u.node] : 0;
+            uint64_t anc = u.valid ? td.anc[u.node] : 0ull;
+            if (tid < kMaxNodes)
+                si.depth[tid] = td.depth[tid];
+            if (window > 0 && dep >= window) {
+                // ancestors that the window has left behind
+                uint64_t near = 0;
+                for (int node = u.node; node >= 0; node = td.parent[node])
+                    if (dep - td.depth[node] < window || L + node < u.r.far_end)
+                        near |= 1ull << node;
+                anc &= near;
+            }
+            if (u.r.begin > L)
+                anc &= u.r.begin - L < 64 ? ~0ull << (u.r.begin - L) : 0ull;
+            const int lo_min = window > 0 ? max(u.r.begin, L - window + 1) : u.r.begin;
+            si.anc[rloc] = anc;
+            si.lo[rloc] = window > 0 ? max(u.r.begin, L + dep - window + 1) : u.r.begin;
+            si.pos[rloc] = L + dep;
+            si.slope[rloc] = kForm == kBias && u.valid && p.slopes ? p.slopes[u.qh] * kLog2e : 0.f;
+            if (lane == 0) {  // the same words from every warp
+                si.n = u.n;
+                si.j0 = u.j0;
+                si.a0 = u.r.a0;
+                si.n1 = u.r.n1;
+                si.b0 = u.r.b0;
+                si.L = L;
+                si.end = L + u.r.n;
+                si.begin = u.r.begin;
+                si.far = window > 0 ? min(u.r.far_end, L) : u.r.begin;
+                si.lo_min = lo_min;
+                si.lo_max = window > 0 ? max(u.r.begin, L + td.max_depth - window + 1) : u.r.begin;
+            }
+#pragma unroll
+            for (int qc = 0; qc < kD / 32; ++qc) {
+                uint32_t w[16];
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch) {
+                    const uint4 x = qv[qc * 4 + ch];
+                    w[4 * ch] = x.x;
+                    w[4 * ch + 1] = x.y;
+                    w[4 * ch + 2] = x.z;
+                    w[4 * ch + 3] = x.w;
+                }
+                tmem_st_32x32b_x16(col + qc * 16, w);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(&q_full[sg & 1]);
+        };
+        long long t = t0;
+        Unit now = describe(t);
+        stage(now, 0);
+        t += now.n;
+        Unit nxt{};
+        bool has_next = t < t1;
+        if (has_next) {
+            nxt = describe(t);
+            stage(nxt, 1);
+            t += nxt.n;
+        }
+        long long it = 0;
+        for (int sg = 0;; ++sg) {
+            it += now.n;
+            Unit fut{};
+            const bool has_fut = t < t1;
+            if (has_fut) {
+                fut = describe(t);
+                t += fut.n;
+                if (fut.valid) {
+#pragma unroll
+                    for (int off = 0; off < 2 * kD; off += 128)
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char *>(p.q + fut.row * kD) +
+                                                                      off));
+                }
+            }
+            const long long last = it - 1;
+            if (!mbar_wait_bounded(&ml_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status))
+                break;
+            const float m_ref = s_info[sg & 1].m[rloc], l = s_info[sg & 1].l[rloc];
+            if (!mbar_wait_bounded(&pv_done[last & 1], (uint32_t)(last >> 1) & 1u, &abort_flag, p.status))
+                break;
+            tc_fence_after();
+            const bool whole = now.n == now.T;
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            uint4 *dst = reinterpret_cast<uint4 *>(p.out + now.row * kD);
+            float *slot = p.part + ((size_t)c * 2 + (now.first ? 0 : 1)) * kSlot;
+            float4 *pdst = reinterpret_cast<float4 *>(slot + rloc * kD);
+#pragma unroll
+            for (int c0 = 0; c0 < kD; c0 += 64) {
+                uint32_t r[64];
+                tmem_ld_32x32b_x32(lane_addr + kColO + c0, r);
+                tmem_ld_32x32b_x32(lane_addr + kColO + c0 + 32, r + 32);
+                tmem_ld_wait();
+                if (c0 + 64 == kD) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0)
+                        mbar_arrive(&o_free[sg & 1]);
+                }
+                if (!now.valid)
+                    continue;
+                if (whole) {
+#pragma unroll
+                    for (int ch = 0; ch < 8; ++ch) {
+                        uint4 v;
+                        v.x = pack<kF16>(__uint_as_float(r[8 * ch + 0]) * inv, __uint_as_float(r[8 * ch + 1]) * inv);
+                        v.y = pack<kF16>(__uint_as_float(r[8 * ch + 2]) * inv, __uint_as_float(r[8 * ch + 3]) * inv);
+                        v.z = pack<kF16>(__uint_as_float(r[8 * ch + 4]) * inv, __uint_as_float(r[8 * ch + 5]) * inv);
+                        v.w = pack<kF16>(__uint_as_float(r[8 * ch + 6]) * inv, __uint_as_float(r[8 * ch + 7]) * inv);
+                        dst[c0 / 8 + ch] = v;
+                    }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x)
+                        pdst[c0 / 4 + x] = make_float4(__uint_as_float(r[4 * x]), __uint_as_float(r[4 * x + 1]),
+                                                       __uint_as_float(r[4 * x + 2]), __uint_as_float(r[4 * x + 3]));
+                }
+            }
+            if (now.valid && whole) {
+                if (p.lse)
+                    p.lse[now.row] = l > 0.f ? (m_ref + log2f(l)) * kLn2 : -INFINITY;
+            } else if (now.valid) {
+                slot[128 * kD + rloc] = m_ref;
+                slot[128 * kD + 128 + rloc] = l;
+            }
+            if (!has_next)
+                break;
+            if (has_fut)
+                stage(fut, sg + 2);
+            now = nxt;
+            nxt = fut;
+            has_next = has_fut;
+        }
     }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + ((size_t)row * p.Hq + h) * kD) + lane * (kD / 64);
+
+    tc_fence_before();
+    __syncwarp();
+    __syncthreads();
+    if (warp == 1) {
+        if (lane == 0)
+            mbar_wait_drain(&drain_bar, 0);
+        __syncwarp();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Log-sum-exp join of the partials of every unit that CTAs share: block (x, y) takes
+// the unit that CTA x + 1's range starts inside (unless an earlier one does too)
+// and rows y, y + gridDim.y, .. of 8 each, a warp per row.
+template <int kD, bool kF16>
+__global__ void __launch_bounds__(256) k_paged_merge(const __grid_constant__ PagedArgs p)
+{
+    constexpr int kSlot = slot_floats(kD), kCols = kD / 32;
+    pdl_wait();
+    pdl_trigger();
+    const PlanCta *ctas = plan_ctas(p.plan);
+    const int cb = blockIdx.x + 1;
+    const PlanHeader *hd = static_cast<const PlanHeader *>(p.plan);
+    const bool ok = hd->valid && hd->batch == p.batch && hd->n_q_heads == p.Hq && hd->n_kv_heads == p.Hkv;
+    const PlanCta me = ctas[cb];
+    if (!ok || me.t0 >= me.t1)
+        return;
+    const PlanReq &r = me.req;
+    const long long tl = me.t0 - r.tile_base;
+    const int u = (int)(tl / r.T);
+    const long long u_first = r.tile_base + (long long)u * r.T;
+    if (me.t0 == u_first)
+        return;
+    const int c_lo = plan_cta_of(me.total, me.P, u_first), c_hi = plan_cta_of(me.total, me.P, u_first + r.T - 1);
+    if (cb != c_lo + 1)
+        return;
+    const int nseg = c_hi - c_lo + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rb = u % r.row_blocks, head = u / r.row_blocks;
+    const int rows = min(128, r.n * p.group - rb * 128);
+    for (int x = blockIdx.y * 8 + warp; x < rows; x += gridDim.y * 8) {
+        const int grow = rb * 128 + x, node = grow / p.group, qh = head * p.group + grow % p.group;
+        if (r.row0 + node >= p.n_rows || !in_bounds(c_lo >= 0 && c_hi < me.P && qh < p.Hq, p.status))
+            continue;
+        auto slot_of = [&](int k) {
+            const int cc = c_lo + k;
+            return p.part + ((size_t)cc * 2 + (plan_split(me.total, me.P, cc) >= u_first ? 0 : 1)) * kSlot;
+        };
+        // lane k of a group of 32 CTAs has its maximum and sum
+        float M = -INFINITY, sum = 0.f, acc[kCols] = {};
+        for (int k0 = 0; k0 < nseg; k0 += 32) {
+            const bool have = k0 + lane < nseg;
+            const float *sl = slot_of(have ? k0 + lane : 0);
+            const float ms = have ? __ldcg(sl + 128 * kD + x) : -INFINITY;
+            const float ls = have ? __ldcg(sl + 128 * kD + 128 + x) : 0.f;
+            const unsigned long long base = reinterpret_cast<unsigned long long>(sl + x * kD);
+            float m2 = ms;
 #pragma unroll
-    for (int x = 0; x < kD / 64; ++x)
-        dst[x] = pack<kF16>(acc[2 * x] * inv, acc[2 * x + 1] * inv);
-    if (p.lse && lane == 0)
-        p.lse[(size_t)row * p.Hq + h] = sum > 0.f ? M * kLn2 + logf(sum) : -INFINITY;
+            for (int o = 16; o >= 1; o >>= 1)
+                m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, o));
+            m2 = fmaxf(m2, M);
+            const float keep = M == -INFINITY ? 0.f : ex2_approx(M - m2);
+            const float w = ms == -INFINITY ? 0.f : ex2_approx(ms - m2);
+            float ws = w * ls;
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1)
+                ws += __shfl_xor_sync(0xffffffffu, ws, o);
+            M = m2;
+            sum = sum * keep + ws;
+#pragma unroll
+            for (int i = 0; i < kCols; ++i)
+                acc[i] *= keep;
+            const int cnt = min(32, nseg - k0);
+            for (int k = 0; k < cnt; k += 4) {
+                float v[4][kCols], wk[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const unsigned long long b =
+                        __shfl_sync(0xffffffffu, base, (k + y) & 31) + 4ull * kCols * lane;
+                    wk[y] = __shfl_sync(0xffffffffu, w, (k + y) & 31);
+                    if (k + y >= cnt)
+                        continue;
+                    if constexpr (kCols == 4) {
+                        const float4 f = __ldcg(reinterpret_cast<const float4 *>(b));
+                        v[y][0] = f.x, v[y][1] = f.y, v[y][2] = f.z, v[y][3] = f.w;
+                    } else {
+                        const float2 f = __ldcg(reinterpret_cast<const float2 *>(b));
+                        v[y][0] = f.x, v[y][1] = f.y;
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    if (k + y < cnt)
+#pragma unroll
+                        for (int i = 0; i < kCols; ++i)
+                            acc[i] += wk[y] * v[y][i];
+            }
+        }
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        const size_t row = (size_t)(r.row0 + node) * p.Hq + qh;
+        uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + row * kD) + lane * (kCols / 2);
+#pragma unroll
+        for (int i = 0; i < kCols / 2; ++i)
+            dst[i] = pack<kF16>(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+        if (p.lse && lane == 0)
+            p.lse[row] = sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
+    }
+}
+
+template <int kD, bool kF16, int kForm>
+cudaError_t launch(const PagedArgs &a, int n_sm, int max_rows, cudaStream_t stream)
+{
+    cudaError_t e = allow_max_smem((const void *)k_paged_attention<kD, kF16, kForm>);
+    if (e != cudaSuccess)
+        return e;
+    const size_t smem = (size_t)(kKStages + kVStages) * tile_bytes(kD) + 1024;
+    e = launch_kernel(k_paged_attention<kD, kF16, kForm>, dim3(n_sm), dim3(kThreads), smem, stream, true, a);
+    if (e != cudaSuccess || n_sm < 2)
+        return e;
+    // rows of a unit over blocks of 8, at most four blocks
+    const int groups = (max_rows + 7) / 8;
+    return launch_kernel(k_paged_merge<kD, kF16>, dim3(n_sm - 1, groups < 4 ? groups : 4), dim3(256), 0, stream, true, a);
+}
+
+template <int kD, bool kF16>
+cudaError_t launch_form(const PagedArgs &a, int n_sm, int max_rows, cudaStream_t stream)
+{
+    if (a.slopes)
+        return launch<kD, kF16, kBias>(a, n_sm, max_rows, stream);
+    return a.cap > 0.f ? launch<kD, kF16, kCap>(a, n_sm, max_rows, stream)
+                       : launch<kD, kF16, kPlain>(a, n_sm, max_rows, stream);
 }
 
 }  // namespace
@@ -206,17 +915,21 @@ extern "C" tb_status paged_tree_attention(const tb_bank *bank, const tb_requests
         return st;
     if (n_rows == 0)
         return launch_result(cudaSuccess, fn);
+    const int n_sm = device_sms(-1);
+    if (n_sm <= 0 || n_sm > kMaxPlanCtas)
+        return record_error(TB_ECUDA, "%s: no current device, or one of %d SMs", fn, n_sm);
+    const char *err = nullptr;
+    const int box = pages->page_size < kTileKeys ? pages->page_size : kTileKeys;
+    const long long layer_off = (long long)layer * pages->layer_stride;
+    if (!make_tmap_pages(&a.tk, pages, static_cast<uint16_t *>(pages->k) + layer_off, box, &err) ||
+        !make_tmap_pages(&a.tv, pages, static_cast<uint16_t *>(pages->v) + layer_off, box, &err))
+        return record_error(TB_EINVAL, "%s: %s", fn, err);
     a.table = req->table;
     a.max_pages = req->max_pages;
     while ((1 << a.page_log2) < req->page_size)
         ++a.page_log2;
     a.n_pages = pages->n_pages;
     a.batch = req->batch;
-    a.k = static_cast<const uint16_t *>(pages->k) + (long long)layer * pages->layer_stride;
-    a.v = static_cast<const uint16_t *>(pages->v) + (long long)layer * pages->layer_stride;
-    a.page_stride = pages->page_stride;
-    a.head_stride = pages->head_stride;
-    a.slot_stride = pages->slot_stride;
     a.q = static_cast<const uint16_t *>(q);
     a.out = static_cast<uint16_t *>(out);
     a.lse = lse;
@@ -224,15 +937,20 @@ extern "C" tb_status paged_tree_attention(const tb_bank *bank, const tb_requests
     a.n_rows = n_rows;
     a.Hq = n_q_heads;
     a.Hkv = pages->n_kv_heads;
-    a.d = pages->head_dim;
-    a.scale = scale;
-    a.softcap = softcap;
+    a.group = n_q_heads / pages->n_kv_heads;
+    a.scale = scale * kLog2e;
+    a.cap = softcap * kLog2e;
+    a.cap_in = softcap > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)scale / (double)softcap) : 0.f;
     a.plan = const_cast<void *>(plan);
+    a.part = attention_parts(workspace);
     a.status = static_cast<int *>(workspace);
+    const long long most = (long long)(n_rows < kMaxNodes ? n_rows : kMaxNodes) * a.group;
+    const int max_rows = most < 128 ? (int)most : 128;
     const bool f16 = pages->dtype == TB_F16;
-    const auto kernel = pages->head_dim == 64 ? (f16 ? k_paged_attention<true, 64> : k_paged_attention<false, 64>)
-                                              : (f16 ? k_paged_attention<true, 128> : k_paged_attention<false, 128>);
-    return launch_result(launch_kernel(kernel, dim3(n_rows, n_q_heads), dim3(kThreads), 0, (cudaStream_t)stream, true,
-                                       a),
-                         fn);
+    const cudaStream_t s = (cudaStream_t)stream;
+    const cudaError_t e = pages->head_dim == 64 ? (f16 ? launch_form<64, true>(a, n_sm, max_rows, s)
+                                                       : launch_form<64, false>(a, n_sm, max_rows, s))
+                                                : (f16 ? launch_form<128, true>(a, n_sm, max_rows, s)
+                                                       : launch_form<128, false>(a, n_sm, max_rows, s));
+    return launch_result(e, fn);
 }

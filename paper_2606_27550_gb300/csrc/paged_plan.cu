@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kItems = TB_MAX_REQUESTS / kThreads;
+constexpr int kMinTiles = 2;
 
 struct PlanArgs {
     const TreeDesc *trees;
@@ -225,8 +226,9 @@ __global__ void __launch_bounds__(kThreads) k_paged_plan(const __grid_constant__
     PlanHeader *hd = static_cast<PlanHeader *>(p.plan);
     PlanReq *out = plan_reqs(p.plan);
     const bool first = blockIdx.x == 0;
-    // no CTA starts past the last tile
-    const int P = (int)min((long long)p.P, max(total3[2], 1ll));
+    // a CTA has kMinTiles tiles at least: fewer CTAs on a small problem, but whole
+    // units and no partials to merge
+    const int P = (int)min((long long)p.P, max((total3[2] + kMinTiles - 1) / kMinTiles, 1ll));
 #pragma unroll 1
     for (int i = 0; i < items; ++i) {
         const int b = b0 + i;
@@ -277,10 +279,20 @@ __global__ void __launch_bounds__(kThreads) k_paged_plan(const __grid_constant__
         }
     }
     __syncthreads();
-    if (first && n_active > 0) {
-        int *cta_first = plan_first(p.plan);
-        for (int c = threadIdx.x; c < P; c += kThreads)
-            cta_first[c] = owner_of(s_tile, n_active, plan_split(total3[2], P, c));
+    if (first) {
+        PlanCta *ctas = plan_ctas(p.plan);
+        for (int c = threadIdx.x; c < p.P; c += kThreads) {
+            PlanCta x = {};
+            x.total = total3[2];
+            x.P = P;
+            if (c < P && n_active > 0) {
+                x.t0 = plan_split(total3[2], P, c);
+                x.t1 = plan_split(total3[2], P, c + 1);
+                x.idx = owner_of(s_tile, n_active, x.t0);
+                x.req = out[x.idx];
+            }
+            ctas[c] = x;
+        }
     }
 
     // the rows
@@ -425,7 +437,7 @@ extern "C" tb_status paged_plan(const tb_bank *bank, const tb_requests *req, con
     a.Hkv = n_q_heads > 0 ? n_kv_heads : 1;
     a.window = window;
     a.sink = sink;
-    a.P = n_sm < kMaxPlanCtas ? n_sm : kMaxPlanCtas;
+    a.P = n_sm < kMaxPlanCtas ? n_sm : kMaxPlanCtas;  // the grid of the attention
     a.plan = plan;
     // a CTA for every 512 rows: more of them repeat the sums for nothing
     const long long ctas = ((long long)max_rows + 2ll * req->batch + kThreads - 1) / kThreads;

@@ -761,6 +761,11 @@ tb_status tv::launch_result(cudaError_t e, const char *fn)
     return e == cudaSuccess ? ok() : cuda_fail(e, fn);
 }
 
+float *tv::attention_parts(void *ws)
+{
+    return reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + kPartBase);
+}
+
 int tv::device_sms(int device)
 {
     return sm_count(device < 0 ? current_device() : device);
