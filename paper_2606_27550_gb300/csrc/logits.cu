@@ -2,21 +2,31 @@
 // logits of every row, and the statistics that the acceptance rules read, in one
 // pass over the logits.
 //
-// A CTA takes one request and a slice of the vocabulary and builds the slice's
-// rules once in shared memory for all rows of the request: how often each token
-// was generated, whether the prompt has it, its bias, and a bitmap of the tokens
-// that any rule touches (most of a vocabulary is touched by none).  Its warps
-// then take (row, chunk) items: the chunk is read into registers at once, so its
-// maximum is known before the first exponential and nothing is rescaled.  A tree
-// row also counts the tokens on its root path; those inside the chunk (rarely
-// any) go to a small table of the warp.  With x = z - m and m the chunk's
-// maximum each item leaves (m, argmax, sum e^x, sum x e^x, and the two sums at
-// temperature T); items combine to slices in shared memory and slices to rows by
-// the request's last CTA (an arrival ticket), both in index order: outputs do not
-// depend on the placement.
+// A CTA takes one request, a slice of the vocabulary and up to 8 of the request's
+// rows, and builds the slice's rules once in shared memory for all of them: how
+// often each token was generated, whether the prompt has it, its bias, and a
+// bitmap of the tokens that any rule touches.  A warp takes a row's slice (or a
+// part of it where there are few rows) in chunks of 512 tokens through a ring of its
+// own in shared memory, the next two chunks on their way.  Of a chunk's touched
+// tokens (a few percent of a vocabulary, but some lane of nearly every warp has
+// one) up to 32 are handed one to each lane, which applies the rules, counts the
+// token in and writes it; the others pass as if masked.  A chunk with more of them (the frequent words at the
+// front of a vocabulary) goes through the rules as a whole, and so does one with
+// tokens of the row's root path in it.
+//
+// With x = z - m, m the warp's running maximum, each lane keeps s = sum e^x, u = sum
+// x e^x and the two sums at temperature T, rescaled when a chunk has a new maximum;
+// parts and slices join in shared memory and by the last CTA of the rows (an arrival
+// ticket), always in index order: outputs do not depend on the placement.
 //   top1 = 1 / s,  H = ln s - u / s,  ln Z_T = m / T + ln s_T
-// Penalties and biases are exact 32-bit operations in the documented order
-// (nothing is contracted), counts are integers.
+// Penalties and biases are 32-bit operations in the documented order, each rounded
+// to nearest (nothing is contracted).  Where a chunk goes through them as a whole,
+// the division by the repetition penalty is Markstein's correction of a product with
+// its reciprocal y = RN(1/b): q = RN(a y), r = a - b q (exact in an FMA), RN(q + r y),
+// which is the correctly rounded quotient for any b but those whose significand is
+// all ones (P. Markstein, IBM J. Res. Dev. 34, 1990, theorem 8.2), as long as
+// nothing overflows or underflows on the way; such b, and chunks with operands
+// outside 2^-100 .. 2^100, divide plainly.
 #include "paged.cuh"
 
 #include <cuda_fp16.h>
@@ -28,8 +38,11 @@ namespace tv {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMaxChunks = 8;   // chunks per slice
-constexpr int kRowGroup = 64;   // rows whose partials are in shared memory together
+constexpr int kVec = 4, kChunk = 128 * kVec;  // tokens a warp takes at a time: kVec groups of four per lane
+constexpr int kRows = kWarps;   // rows of a CTA
+constexpr int kMaxSlice = 3584;  // three CTAs per SM
+constexpr int kMaxRowsCall = 65536;
+constexpr int kStages = 2;      // chunks of a warp's ring: one in work, the others on their way
 constexpr uint32_t kInPrompt = 0x80000000u;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -42,7 +55,8 @@ struct Part {
 
 struct LogitArgs {
     const TreeDesc *trees;
-    int n_trees, batch, n_rows, V, slices, chunks;  // chunks per slice
+    int n_trees, batch, n_rows, V, slices, size;  // size: tokens per slice
+    int ring_off, mask_off;                       // in the dynamic shared memory
     const int32_t *tree, *row_start;
     const void *in;
     long long in_stride, out_stride;
@@ -50,8 +64,7 @@ struct LogitArgs {
     tb_logit_rules r;
     tb_logit_stats st;
     float temperature, scale_t;  // scale_t = log2(e) / T
-    int want, want_t;            // statistics at temperature 1 (with the argmax), and at T != 1
-    int *ticket;                 // [batch]
+    int *ticket;                 // [pieces of rows]
     Part *parts;                 // [rows][slices]
 };
 
@@ -123,364 +136,645 @@ struct In<TB_F16> {
     }
 };
 
-// The rules of a slice, in shared memory.
-struct Slice {
-    uint32_t *count;    // generated occurrences; kInPrompt: the prompt has the token
-    float *bias;
-    uint32_t *touched;  // bitmap
-    uint8_t *extra;     // this warp's: occurrences on the row's path within its chunk
-    uint32_t *path_bits;
+// The penalties of a request.
+struct Penalty {
+    float rep, inv, freq, pres;  // inv: 1 / rep, rounded
 };
 
-__device__ __forceinline__ float penalise(float z, uint32_t c, int extra, float bias, float rep, float freq, float pres)
+// Loads that are issued where they stand: a CTA's life is short, and as a chain of
+// round trips its parameters, tokens and biases took longer than its logits.
+__device__ __forceinline__ int load_now(const int *p)
 {
-    const int n = (int)(c & ~kInPrompt) + extra;
-    if (n > 0 || (c & kInPrompt))
-        z = z > 0.f ? __fdiv_rn(z, rep) : __fmul_rn(z, rep);
-    if (n > 0)
-        z = __fsub_rn(__fsub_rn(z, __fmul_rn(freq, (float)n)), pres);
+    int v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ float load_now(const float *p)
+{
+    float v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint64_t load_now(const uint64_t *p)
+{
+    uint64_t v;
+    asm volatile("ld.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+    return v;
+}
+
+template <int kBytes>
+__device__ __forceinline__ void copy_async(void *dst, const void *src)
+{
+    if constexpr (kBytes == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(dst)), "l"(src), "n"(kBytes) : "memory");
+}
+
+// The rules on one logit.  n: generated occurrences; seen: they or the prompt have
+// the token.  kShort: the quotient as above.
+template <bool kShort>
+__device__ __forceinline__ float penalise(float z, float n, bool seen, float bias, const Penalty &p)
+{
+    const float b = seen ? p.rep : 1.f;
+    float div;
+    if constexpr (kShort) {
+        const float y = seen ? p.inv : 1.f;
+        const float q = __fmul_rn(z, y);
+        div = __fmaf_rn(__fmaf_rn(-q, b, z), y, q);
+    } else {
+        div = __fdiv_rn(z, b);
+    }
+    z = z > 0.f ? div : __fmul_rn(z, b);
+    z = __fsub_rn(z, __fmul_rn(p.freq, n));
+    z = __fsub_rn(z, n > 0.f ? p.pres : 0.f);
     return __fadd_rn(z, bias);
 }
 
-// kVec: groups of four tokens per lane in a chunk of 128 kVec tokens.
-template <int kType, int kVec>
-__global__ void __launch_bounds__(kThreads) k_logits(const __grid_constant__ LogitArgs p)
+// The largest of the warp's values (NaN only where all are).
+__device__ __forceinline__ float warp_max(float x)
 {
-    constexpr int kChunk = 128 * kVec;
+    float y;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The last request whose rows begin at or before row g, by the whole warp (one round
+// trip to memory for every 32-fold).
+__device__ __forceinline__ int owner_of(const int32_t *row_start, int batch, int g, int lane)
+{
+    int lo = 0, n = batch;  // among requests lo .. lo + n - 1; row_start[lo] <= g
+    while (n > 1) {
+        const int step = (n + 31) / 32, at = lo + lane * step;
+        const bool before = lane * step < n && (lane == 0 || row_start[at] <= g);
+        const int k = __popc(__ballot_sync(0xffffffffu, before)) - 1;
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return lo;
+}
+
+// A row's statistics so far: the warp's maximum and where it is, this lane's sums.
+struct Running {
+    float m, s, u, st, ut;
+    int arg;
+};
+
+// kStats: 0 none, 1 at temperature 1 only, 2 also at T
+template <int kType, int kStats>
+__global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ LogitArgs p)
+{
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ Part s_part[kRowGroup][kMaxChunks];
-    __shared__ uint8_t s_extra[kWarps][kChunk];
-    __shared__ uint32_t s_path[kWarps][kChunk / 32];
+    __shared__ Part s_part[kRows][kWarps];
+    __shared__ uint64_t s_anc[TB_MAX_NODES];
+    __shared__ int s_draft[TB_MAX_NODES];
     __shared__ int s_last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int b = blockIdx.y, slice = blockIdx.x;
-    const int size = p.chunks * kChunk, v0 = slice * size;  // v0 < V (the host's split)
-    Slice sl;
-    sl.count = reinterpret_cast<uint32_t *>(smem);
-    sl.bias = reinterpret_cast<float *>(sl.count + size);
-    sl.touched = reinterpret_cast<uint32_t *>(sl.bias + size);
-    sl.extra = s_extra[warp];
-    sl.path_bits = s_path[warp];
+    const int slice = blockIdx.y, size = p.size, v0 = slice * size;  // v0 < V (the host's split)
+    uint32_t *count = reinterpret_cast<uint32_t *>(smem);  // generated occurrences | kInPrompt; then as floats
+    float *bias = reinterpret_cast<float *>(count + size);
+    uint32_t *touched = reinterpret_cast<uint32_t *>(bias + size);  // bitmap: a rule has the token
+    uint32_t *seen = touched + size / 32;                           // bitmap: the history has it
+    uint16_t *before = reinterpret_cast<uint16_t *>(seen + size / 32);  // touched tokens before a word's
+    uint16_t *list = before + size / 32 + 8;                            // the touched tokens, in order
+    using T = typename In<kType>::T;
+    T *ring = reinterpret_cast<T *>(smem + p.ring_off) + (size_t)warp * kStages * kChunk;
+    uint32_t *mask_ring = reinterpret_cast<uint32_t *>(smem + p.mask_off) + warp * kStages * (kChunk / 32);
     const bool rules = p.r.history || p.r.bias_start;
     if (rules) {
         for (int x = threadIdx.x; x < size / 4; x += kThreads) {
-            reinterpret_cast<uint4 *>(sl.count)[x] = make_uint4(0, 0, 0, 0);
-            reinterpret_cast<uint4 *>(sl.bias)[x] = make_uint4(0, 0, 0, 0);
+            reinterpret_cast<uint4 *>(count)[x] = make_uint4(0, 0, 0, 0);
+            reinterpret_cast<uint4 *>(bias)[x] = make_uint4(0, 0, 0, 0);
         }
         for (int x = threadIdx.x; x < size / 32; x += kThreads)
-            sl.touched[x] = 0;
+            touched[x] = seen[x] = 0;
     }
-    for (int x = lane; x < kChunk / 4; x += 32)
-        reinterpret_cast<uint32_t *>(sl.extra)[x] = 0;
-    for (int x = lane; x < kChunk / 32; x += 32)
-        sl.path_bits[x] = 0;
     pdl_wait();
     pdl_trigger();
-    const int row0 = max(p.row_start[b], 0), row1 = min(p.row_start[b + 1], p.n_rows);
-    if (row0 >= row1)
+    // Rows are grouped in blocks of 8 of the whole batch, cut at the requests' ends.
+    // CTA x < batch takes the first piece of request x, CTA batch + e the block e if
+    // it begins inside a request.
+    int b = blockIdx.x, g0 = 0, g1;
+    const bool head = b < p.batch;
+    if (!head) {
+        g0 = (b - p.batch) * kRows;
+        b = owner_of(p.row_start, p.batch, g0, lane);
+    }
+    // the request's parameters, one round trip
+    const int row0 = load_now(p.row_start + b), row_end = load_now(p.row_start + b + 1);
+    const int t = p.tree ? load_now(p.tree + b) : -1;
+    const int said = p.r.history ? load_now(p.r.history_len + b) : 0;
+    const int asked = p.r.history && p.r.prompt_len ? load_now(p.r.prompt_len + b) : 0;
+    const int bias0 = p.r.bias_start ? load_now(p.r.bias_start + b) : 0;
+    const int bias1 = p.r.bias_start ? load_now(p.r.bias_start + b + 1) : 0;
+    Penalty pen;
+    pen.rep = p.r.repetition ? load_now(p.r.repetition + b) : 1.f;
+    pen.freq = p.r.frequency ? load_now(p.r.frequency + b) : 0.f;
+    pen.pres = p.r.presence ? load_now(p.r.presence + b) : 0.f;
+    const int row1 = min(row_end, p.n_rows);
+    if (head)
+        g0 = row0;
+    if (row0 < 0 || g0 >= row1 || (!head && g0 <= row0))
         return;
-    const int t = p.tree ? p.tree[b] : -1;
-    const TreeDesc *td = t >= 0 && t < p.n_trees ? p.trees + t : nullptr;
-    const float rep = p.r.repetition ? p.r.repetition[b] : 1.f;
-    const float freq = p.r.frequency ? p.r.frequency[b] : 0.f;
-    const float pres = p.r.presence ? p.r.presence[b] : 0.f;
-    __syncthreads();
-    if (p.r.history) {
-        const int32_t *h = p.r.history + b * p.r.history_stride;
-        const int n = (int)min((long long)max(p.r.history_len[b], 0), (long long)p.r.history_stride);
-        const int prompt = p.r.prompt_len ? min(max(p.r.prompt_len[b], 0), n) : 0;
-        auto note = [&](int i, int tok) {
-            const unsigned loc = (unsigned)(tok - v0);
-            if (loc < (unsigned)size && tok < p.V) {
-                if (i < prompt)
-                    atomicOr(&sl.count[loc], kInPrompt);
-                else
-                    atomicAdd(&sl.count[loc], 1u);
-                atomicOr(&sl.touched[loc >> 5], 1u << (loc & 31));
+    g1 = min((g0 / kRows + 1) * kRows, row1);
+    const int here = min(size, p.V - v0);  // tokens of the slice that exist
+    // parts of a row: every warp has work where there are chunks enough
+    const int rows = g1 - g0, parts = kWarps / rows;
+    const int part_size = ((here + kChunk - 1) / kChunk + parts - 1) / parts * kChunk;
+    // the item (row, part) in work
+    const T *src = nullptr;
+    const int32_t *mask = nullptr;
+    int row = 0, c_first = 0, c_end = 0;
+    bool in_vec = false, in_ring = false;  // its chunks go through the ring (16-byte pieces, or 4-byte ones)
+    auto fetch = [&](int c) {  // chunk c on its way; always one group of copies
+        if (c < c_end) {
+            const int st = (c / kChunk) % kStages;
+            T *to = ring + st * kChunk;
+            if (in_vec && c + kChunk <= here) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k)
+                    copy_async<4 * sizeof(T)>(to + k * 128 + lane * 4, src + c + k * 128 + lane * 4);
+            } else if (in_ring) {
+                if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int o = k * 128 + lane * 4 + e;
+                            if (c + o < here)
+                                copy_async<4>(to + o, src + c + o);
+                        }
+                }
             }
-        };
-        constexpr int kAhead = 8;
-        for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kAhead) {
-            int tok[kAhead];
+            if (mask && lane < kChunk / 32 && c + 32 * lane < here)
+                copy_async<4>(mask_ring + st * (kChunk / 32) + lane, mask + (c >> 5) + lane);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    const int gr = warp / parts, part = warp - gr * parts;  // this warp's row and part of it
+    if (gr < rows) {
+        row = g0 + gr;
+        c_first = part * part_size;
+        c_end = min(c_first + part_size, here);
+        src = static_cast<const T *>(p.in) + row * p.in_stride + v0;
+        in_vec = (reinterpret_cast<uintptr_t>(src) & (4 * sizeof(T) - 1)) == 0;
+        in_ring = sizeof(T) == 4;
+        const int mrow = !p.r.mask ? -1 : p.r.mask_row ? p.r.mask_row[row] : row;
+        mask = mrow >= 0 ? p.r.mask + mrow * p.r.mask_stride + (v0 >> 5) : nullptr;
+        // on their way while the rules are built
 #pragma unroll
-            for (int m = 0; m < kAhead; ++m)
-                tok[m] = i0 + m * kThreads < n ? h[i0 + m * kThreads] : -1;
+        for (int k = 0; k < kStages - 1; ++k)
+            fetch(c_first + k * kChunk);
+    }
+
+    const TreeDesc *td = t >= 0 && t < p.n_trees ? p.trees + t : nullptr;
+    const bool paths = td && p.r.draft;
+    // the first tokens of the history, the first biases and the tree, one round trip
+    constexpr int kAhead = 16;
+    const int n_said = (int)min((long long)max(said, 0), (long long)p.r.history_stride);
+    const int n_asked = min(max(asked, 0), n_said);
+    const int32_t *h = p.r.history + (p.r.history ? b * p.r.history_stride : 0);
+    int word_of[kAhead];
 #pragma unroll
-            for (int m = 0; m < kAhead; ++m)
-                if (tok[m] >= 0)
-                    note(i0 + m * kThreads, tok[m]);
+    for (int m = 0; m < kAhead; ++m) {
+        const int i = threadIdx.x + m * kThreads;
+        word_of[m] = i < n_said ? load_now(h + i) : -1;
+    }
+    constexpr int kBiasAhead = 4;
+    int bias_tok[kBiasAhead];
+    float bias_val[kBiasAhead];
+    auto load_biases = [&](int e0) {
+#pragma unroll
+        for (int m = 0; m < kBiasAhead; ++m) {
+            const int e = e0 + 32 * m + lane;
+            bias_tok[m] = e < bias1 ? load_now(p.r.bias_token + e) : -1;
+            bias_val[m] = e < bias1 ? load_now(p.r.bias_value + e) : 0.f;
+        }
+    };
+    if (warp == 0)
+        load_biases(max(bias0, 0));
+    uint64_t node_anc = 0;
+    int node_tok = -1;
+    if (paths && threadIdx.x < TB_MAX_NODES) {
+        const int n = load_now(&td->n);
+        const uint64_t anc = load_now(td->anc + threadIdx.x);
+        if ((int)threadIdx.x < min(n, row1 - row0)) {
+            node_anc = anc & ~1ull;
+            node_tok = load_now(p.r.draft + row0 + threadIdx.x);
         }
     }
-    if (p.r.bias_start && warp == 0) {
-        // in list order: entries of one token add up in a fixed order
-        const int e1 = p.r.bias_start[b + 1];
-        for (int e0 = max(p.r.bias_start[b], 0); e0 < e1; e0 += 32) {
-            const int e = e0 + lane;
-            const int tok = e < e1 ? p.r.bias_token[e] : -1;
-            const unsigned loc = (unsigned)(tok - v0);
-            const bool mine = tok >= 0 && tok < p.V && loc < (unsigned)size;
-            const float val = mine ? p.r.bias_value[e] : 0.f;
+    pen.inv = __fdiv_rn(1.f, pen.rep);
+    // (see above for which divisors and, below, dividends the short quotient is right)
+    const bool short_div = pen.rep > 0x1p-20f && pen.rep < 0x1p20f && (__float_as_uint(pen.rep) & 0x7fffffu) != 0x7fffffu;
+    __shared__ int s_sum[kWarps];
+    if (threadIdx.x < TB_MAX_NODES) {
+        s_anc[threadIdx.x] = node_anc;
+        s_draft[threadIdx.x] = node_tok;
+    }
+    __syncthreads();
+    for (int i0 = threadIdx.x;;) {
+#pragma unroll
+        for (int m = 0; m < kAhead; ++m) {
+            const unsigned loc = (unsigned)(word_of[m] - v0);
+            if (word_of[m] >= 0 && loc < (unsigned)here) {
+                if (i0 + m * kThreads < n_asked)
+                    atomicOr(&count[loc], kInPrompt);
+                else
+                    atomicAdd(&count[loc], 1u);
+            }
+        }
+        i0 += kThreads * kAhead;
+        if (i0 - (int)threadIdx.x >= n_said)
+            break;
+#pragma unroll
+        for (int m = 0; m < kAhead; ++m)
+            word_of[m] = i0 + m * kThreads < n_said ? load_now(h + i0 + m * kThreads) : -1;
+    }
+    // biases by one warp, in list order: entries of one token add up in a fixed order
+    for (int e0 = max(bias0, 0); warp == 0 && e0 < bias1;) {
+#pragma unroll
+        for (int m = 0; m < kBiasAhead; ++m) {
+            const unsigned loc = (unsigned)(bias_tok[m] - v0);
+            const bool mine = bias_tok[m] >= 0 && loc < (unsigned)here;
+            if (!__any_sync(0xffffffffu, mine))
+                continue;
             const unsigned same = __match_any_sync(0xffffffffu, mine ? (int)loc : -1 - lane);
             const bool leader = mine && (same & ((1u << lane) - 1)) == 0;
-            float acc = leader ? sl.bias[loc] : 0.f;
-            for (int k = 0; k < 32; ++k) {
-                const float other = __shfl_sync(0xffffffffu, val, k);
-                if ((same >> k) & 1)
-                    acc += other;
+            float acc = leader ? bias[loc] : 0.f;
+            if (__all_sync(0xffffffffu, __popc(same) == 1)) {
+                acc += bias_val[m];
+            } else {
+                for (int k = 0; k < 32; ++k) {
+                    const float v = __shfl_sync(0xffffffffu, bias_val[m], k);
+                    acc += (same >> k) & 1 ? v : 0.f;
+                }
             }
             if (leader) {
-                sl.bias[loc] = acc;
-                atomicOr(&sl.touched[loc >> 5], 1u << (loc & 31));
+                bias[loc] = acc;
+                atomicOr(&touched[loc >> 5], 1u << (loc & 31));
             }
             __syncwarp();
         }
+        e0 += 32 * kBiasAhead;
+        if (e0 < bias1)
+            load_biases(e0);
     }
     __syncthreads();
 
-    const int n_chunks = min(p.chunks, (p.V - v0 + kChunk - 1) / kChunk);
-    const float inv_t = 1.f / p.temperature;
-    using T = typename In<kType>::T;
-    for (int g0 = row0; g0 < row1; g0 += kRowGroup) {
-        const int rows = min(kRowGroup, row1 - g0);
-        for (int item = warp; item < rows * n_chunks; item += kWarps) {
-            const int gr = item / n_chunks, ch = item - gr * n_chunks, row = g0 + gr;
-            const int c0 = v0 + ch * kChunk, room = p.V - c0;  // tokens of the chunk that exist
-            const T *src = static_cast<const T *>(p.in) + row * p.in_stride + c0;
-            float *dst = p.out + row * p.out_stride + c0;
-            float z[kVec][4];
-            const bool in_vec = (reinterpret_cast<uintptr_t>(src) & (4 * sizeof(T) - 1)) == 0 && room >= kChunk;
-            if (in_vec) {
-#pragma unroll
-                for (int k = 0; k < kVec; ++k) {
-                    const float4 x = In<kType>::four(src + k * 128 + lane * 4);
-                    z[k][0] = x.x, z[k][1] = x.y, z[k][2] = x.z, z[k][3] = x.w;
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int o = k * 128 + lane * 4 + e;
-                        z[k][e] = o < room ? In<kType>::one(src + o) : -INFINITY;
-                    }
-            }
-            // this row's mask words of the chunk: lane's four tokens lie in word 4 k + lane / 8
-            uint32_t allow[kVec];
-            const int mrow = !p.r.mask ? -1 : p.r.mask_row ? p.r.mask_row[row] : row;
-            const int32_t *mask = mrow >= 0 ? p.r.mask + mrow * p.r.mask_stride + (c0 >> 5) : nullptr;
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                const int w = 4 * k + (lane >> 3);
-                allow[k] = 0xfu;
-                if (mask && w * 32 < room)
-                    allow[k] = ((uint32_t)mask[w] >> (4 * (lane & 7))) & 0xfu;
-            }
-            // the draft tokens on this row's root path that fall into the chunk
-            bool on_path = false;
-            int tok[2] = {-1, -1};
-            if (td && p.r.draft && row - row0 < td->n) {
-                const uint64_t anc = td->anc[row - row0] & ~1ull;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int j = lane + 32 * h;
-                    if ((anc >> j) & 1) {
-                        const int x = p.r.draft[row0 + j] - c0;
-                        if (x >= 0 && x < kChunk && x < room)
-                            tok[h] = x;
-                    }
-                }
-                on_path = __any_sync(0xffffffffu, tok[0] >= 0 || tok[1] >= 0);
-            }
-            if (on_path) {
-                for (int h = 0; h < 2; ++h)
-                    for (int k = 0; k < 32; ++k) {
-                        const int x = __shfl_sync(0xffffffffu, tok[h], k);
-                        if (x >= 0 && lane == 0) {
-                            sl.extra[x] += 1;
-                            sl.path_bits[x >> 5] |= 1u << (x & 31);
-                        }
-                    }
-                __syncwarp();
-            }
-            if (rules || on_path) {
-#pragma unroll
-                for (int k = 0; k < kVec; ++k) {
-                    const int o = k * 128 + lane * 4, loc = ch * kChunk + o;
-                    uint32_t bits = rules ? sl.touched[loc >> 5] : 0u;
-                    if (on_path)
-                        bits |= sl.path_bits[o >> 5];
-                    bits = (bits >> (o & 31)) & 0xfu;
-                    if (bits) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if ((bits >> e) & 1)
-                                z[k][e] = penalise(z[k][e], rules ? sl.count[loc + e] : 0u,
-                                                   on_path ? sl.extra[o + e] : 0, rules ? sl.bias[loc + e] : 0.f, rep,
-                                                   freq, pres);
-                    }
+    if (rules) {
+        // counts as floats, who is seen, and the touched tokens as a list
+        const int words = size / 32;
+        static_assert(kMaxSlice / 32 <= kThreads, "a word of the bitmap per thread");
+        for (int x = warp; x < words; x += kWarps) {
+            const uint32_t n = count[32 * x + lane];
+            const uint32_t bits = __ballot_sync(0xffffffffu, n != 0);
+            if (bits) {
+                reinterpret_cast<float *>(count)[32 * x + lane] = (float)(n & ~kInPrompt);
+                if (lane == 0) {
+                    seen[x] = bits;
+                    touched[x] |= bits;
                 }
             }
-            if (on_path) {
-                __syncwarp();
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (tok[h] >= 0) {
-                        sl.extra[tok[h]] = 0;
-                        sl.path_bits[tok[h] >> 5] = 0;
-                    }
-                __syncwarp();
-            }
-#pragma unroll
-            for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (!((allow[k] >> e) & 1))
-                        z[k][e] = -INFINITY;
-            if ((reinterpret_cast<uintptr_t>(dst) & 15) == 0 && room >= kChunk) {
-#pragma unroll
-                for (int k = 0; k < kVec; ++k)
-                    *reinterpret_cast<float4 *>(dst + k * 128 + lane * 4) =
-                        make_float4(z[k][0], z[k][1], z[k][2], z[k][3]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int o = k * 128 + lane * 4 + e;
-                        if (o < room)
-                            dst[o] = z[k][e];
-                    }
-            }
-            if (!p.want)
-                continue;
-            // the chunk's maximum, then its sums
-            Part a = empty_part();
-#pragma unroll
-            for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (z[k][e] > a.m) {
-                        a.m = z[k][e];
-                        a.arg = c0 + k * 128 + lane * 4 + e;
-                    }
-            float m = a.m;
-            int arg = a.arg;
-#pragma unroll
-            for (int o = 16; o >= 1; o >>= 1) {
-                const float om = __shfl_xor_sync(0xffffffffu, m, o);
-                const int oa = __shfl_xor_sync(0xffffffffu, arg, o);
-                if (om > m || (om == m && oa < arg))
-                    m = om, arg = oa;
-            }
-            const float mu = m == -INFINITY ? 0.f : m;
-            float s = 0.f, u = 0.f, st = 0.f, ut = 0.f;
-#pragma unroll
-            for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = z[k][e] - mu;
-                    const float q = ex2_approx(x * kLog2e);
-                    s += q;
-                    u += q > 0.f ? q * x : 0.f;
-                    if (p.want_t) {
-                        const float qt = ex2_approx(x * p.scale_t);
-                        st += qt;
-                        ut += qt > 0.f ? qt * x : 0.f;
-                    }
-                }
-#pragma unroll
-            for (int o = 16; o >= 1; o >>= 1) {
-                s += __shfl_xor_sync(0xffffffffu, s, o);
-                u += __shfl_xor_sync(0xffffffffu, u, o);
-                st += __shfl_xor_sync(0xffffffffu, st, o);
-                ut += __shfl_xor_sync(0xffffffffu, ut, o);
-            }
-            if (lane == 0)
-                s_part[gr][ch] = Part{m, arg, s, u, st, ut * inv_t, {0, 0}};
         }
-        if (!p.want)
-            continue;
         __syncthreads();
-        for (int gr = threadIdx.x; gr < rows; gr += kThreads) {
-            Part a = s_part[gr][0];
-            for (int ch = 1; ch < n_chunks; ++ch)
-                a = combine(a, s_part[gr][ch], inv_t);
-            p.parts[(size_t)(g0 + gr) * p.slices + slice] = a;
+        const uint32_t mine = threadIdx.x < words ? touched[threadIdx.x] : 0u;
+        int at = __popc(mine);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, at, o);
+            at += lane >= o ? y : 0;
+        }
+        if (lane == 31)
+            s_sum[warp] = at;
+        __syncthreads();
+        for (int k = 0; k < warp; ++k)
+            at += s_sum[k];
+        if (threadIdx.x < words) {
+            if (threadIdx.x == words - 1)
+                before[words] = (uint16_t)at;
+            at -= __popc(mine);
+            before[threadIdx.x] = (uint16_t)at;
+            for (uint32_t rest = mine; rest; rest &= rest - 1)
+                list[at++] = (uint16_t)(threadIdx.x * 32 + __ffs(rest) - 1);
         }
         __syncthreads();
     }
-    if (!p.want)
+    const float *generated = reinterpret_cast<const float *>(count);
+
+    const float inv_t = 1.f / p.temperature;
+    if (gr < rows) {
+            float *dst = p.out + row * p.out_stride + v0;
+            const bool out_vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
+            // the draft tokens on this row's root path, relative to the slice
+            int tok[2] = {-1, -1};
+            if (paths && row - row0 < TB_MAX_NODES) {
+                const uint64_t anc = s_anc[row - row0];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int j = lane + 32 * h, x = s_draft[j] - v0;
+                    if (((anc >> j) & 1) && s_draft[j] >= 0 && x >= 0 && x < here)
+                        tok[h] = x;
+                }
+            }
+            Running a{-INFINITY, 0.f, 0.f, 0.f, 0.f, 0x7fffffff};
+            auto add = [&](float v, float mu) {
+                const float x = v - mu;
+                const float q = ex2_approx(x * kLog2e);
+                const float xc = fmaxf(x, -1e4f);  // finite where the weight is 0
+                a.s += q;
+                a.u = fmaf(q, xc, a.u);
+                if constexpr (kStats > 1) {
+                    const float qt = ex2_approx(x * p.scale_t);
+                    a.st += qt;
+                    a.ut = fmaf(qt, xc, a.ut);
+                }
+            };
+#pragma unroll 1
+            for (int c = c_first; c < c_end; c += kChunk) {
+                float z[kVec][4];
+                uint32_t word = 0xffffffffu;  // lane w holds word w of the chunk's mask
+                fetch(c + (kStages - 1) * kChunk);
+                asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+                const int st = (c / kChunk) % kStages;
+                const T *from = ring + st * kChunk;  // every lane reads what it copied
+                if (in_vec && c + kChunk <= here) {
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k) {
+                        const float4 x = In<kType>::four(from + k * 128 + lane * 4);
+                        z[k][0] = x.x, z[k][1] = x.y, z[k][2] = x.z, z[k][3] = x.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int o = k * 128 + lane * 4 + e;
+                            z[k][e] = c + o < here ? In<kType>::one(in_ring ? from + o : src + c + o) : -INFINITY;
+                        }
+                }
+                if (mask && lane < kChunk / 32 && c + 32 * lane < here)
+                    word = mask_ring[st * (kChunk / 32) + lane];
+                int l0 = 0, nl = 0;  // the chunk's touched tokens in the list
+                if (rules) {
+                    l0 = before[c >> 5];
+                    nl = before[min(c + kChunk, size) >> 5] - l0;
+                }
+                const int o0 = tok[0] - c, o1 = tok[1] - c;
+                const bool in0 = (unsigned)o0 < (unsigned)kChunk, in1 = (unsigned)o1 < (unsigned)kChunk;
+                const bool on_path = paths && __any_sync(0xffffffffu, in0 || in1);
+                float mine = -INFINITY;  // this lane's token of the list
+                int mine_at = 0;
+                const bool sparse = nl > 0 && nl <= 32 && !on_path;
+                if (sparse) {
+                    mine_at = lane < nl ? list[l0 + lane] - c : 0;
+                    const int from = (mine_at & 127) >> 2, reg = (mine_at >> 7) * 4 + (mine_at & 3);
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float v = __shfl_sync(0xffffffffu, z[k][e], from);
+                            mine = reg == k * 4 + e ? v : mine;
+                        }
+                    mine = penalise<false>(mine, generated[c + mine_at], (seen[(c + mine_at) >> 5] >> (mine_at & 31)) & 1,
+                                           bias[c + mine_at], pen);
+                    const bool allowed = (__shfl_sync(0xffffffffu, word, mine_at >> 5) >> (mine_at & 31)) & 1;
+                    mine = allowed && lane < nl ? mine : -INFINITY;
+                    // the others go on as if these were masked
+                    if (lane < kChunk / 32)
+                        word &= ~touched[(c >> 5) + lane];
+                } else if (on_path) {
+                    uint32_t extra[kVec] = {};  // path occurrences of this lane's tokens, a byte each
+                    for (int h = 0; h < 2; ++h)
+                        for (unsigned with = __ballot_sync(0xffffffffu, h ? in1 : in0); with; with &= with - 1) {
+                            const int o = __shfl_sync(0xffffffffu, h ? o1 : o0, __ffs(with) - 1);
+#pragma unroll
+                            for (int k = 0; k < kVec; ++k)
+                                if (o >> 7 == k && ((o & 127) >> 2) == lane)
+                                    extra[k] += 1u << (8 * (o & 3));
+                        }
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k) {
+                        const int o = c + k * 128 + lane * 4;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int more = (extra[k] >> (8 * e)) & 0xff;
+                            const bool has = rules && ((seen[o >> 5] >> ((o & 31) + e)) & 1);
+                            const float n = rules ? generated[o + e] : 0.f;
+                            z[k][e] = penalise<false>(z[k][e], n + (float)more, has || more, rules ? bias[o + e] : 0.f, pen);
+                        }
+                    }
+                } else if (nl > 0) {
+                    float big = 0.f, small = 1.f;
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            big = fmaxf(big, fabsf(z[k][e]));
+                            small = fminf(small, z[k][e] == 0.f ? 1.f : fabsf(z[k][e]));
+                        }
+                    const bool plain = !short_div || big > 0x1p100f || small < 0x1p-100f;
+                    if (__any_sync(0xffffffffu, plain)) {
+#pragma unroll
+                        for (int k = 0; k < kVec; ++k) {
+                            const int o = c + k * 128 + lane * 4;
+                            const uint32_t s = seen[o >> 5] >> (o & 31);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                z[k][e] = penalise<false>(z[k][e], generated[o + e], (s >> e) & 1, bias[o + e], pen);
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < kVec; ++k) {
+                            const int o = c + k * 128 + lane * 4;
+                            const uint32_t s = seen[o >> 5] >> (o & 31);
+                            const float4 n = *reinterpret_cast<const float4 *>(generated + o);
+                            const float4 f = *reinterpret_cast<const float4 *>(bias + o);
+                            z[k][0] = penalise<true>(z[k][0], n.x, s & 1, f.x, pen);
+                            z[k][1] = penalise<true>(z[k][1], n.y, s & 2, f.y, pen);
+                            z[k][2] = penalise<true>(z[k][2], n.z, s & 4, f.z, pen);
+                            z[k][3] = penalise<true>(z[k][3], n.w, s & 8, f.w, pen);
+                        }
+                    }
+                }
+                if (mask || sparse) {
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k) {
+                        const uint32_t w = __shfl_sync(0xffffffffu, word, 4 * k + (lane >> 3)) >> (4 * (lane & 7));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            z[k][e] = (w >> e) & 1 ? z[k][e] : -INFINITY;
+                    }
+                }
+                if (out_vec && c + kChunk <= here) {
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k)
+                        *reinterpret_cast<float4 *>(dst + c + k * 128 + lane * 4) =
+                            make_float4(z[k][0], z[k][1], z[k][2], z[k][3]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int o = c + k * 128 + lane * 4 + e;
+                            if (o < here)
+                                dst[o] = z[k][e];
+                        }
+                }
+                if (sparse) {
+                    __syncwarp();
+                    if (lane < nl)
+                        dst[c + mine_at] = mine;
+                }
+                if constexpr (kStats > 0) {
+                    float m = mine;
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            m = fmaxf(m, z[k][e]);
+                    m = warp_max(m);
+                    if (m > a.m) {
+                        // a new maximum: its lowest token, and the sums relative to it
+                        unsigned arg = mine == m ? (unsigned)(v0 + c + mine_at) : 0x7fffffffu;
+#pragma unroll
+                        for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (z[k][e] == m)
+                                    arg = min(arg, (unsigned)(v0 + c + k * 128 + lane * 4 + e));
+                        a.arg = (int)__reduce_min_sync(0xffffffffu, arg);
+                        const float d = a.m == -INFINITY ? 0.f : a.m - m;  // (sums of nothing: 0)
+                        const float w = ex2_approx(d * kLog2e);
+                        a.u = w * (a.u + d * a.s);
+                        a.s *= w;
+                        if constexpr (kStats > 1) {
+                            const float wt = ex2_approx(d * p.scale_t);
+                            a.ut = wt * (a.ut + d * a.st);
+                            a.st *= wt;
+                        }
+                        a.m = m;
+                    }
+                    const float mu = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            add(z[k][e], mu);
+                    if (sparse)
+                        add(mine, mu);
+                }
+            }
+        if constexpr (kStats > 0) {
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) {
+                a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+                a.u += __shfl_xor_sync(0xffffffffu, a.u, o);
+                a.st += __shfl_xor_sync(0xffffffffu, a.st, o);
+                a.ut += __shfl_xor_sync(0xffffffffu, a.ut, o);
+            }
+            if (lane == 0)
+                s_part[gr][part] = Part{a.m, a.arg, a.s, a.u, a.st, a.ut * inv_t, {0, 0}};
+        }
+    }
+    if (kStats == 0)
         return;
 
-    // the request's last CTA combines the slices of its rows
+    __syncthreads();
+    if (threadIdx.x < rows) {
+        Part a = s_part[threadIdx.x][0];
+        for (int k = 1; k < parts; ++k)
+            a = combine(a, s_part[threadIdx.x][k], inv_t);
+        p.parts[(size_t)(g0 + threadIdx.x) * p.slices + slice] = a;
+    }
+    // the last CTA of these rows joins their slices
+    __syncthreads();
     if (threadIdx.x == 0) {
         __threadfence();
-        s_last = atomicAdd(&p.ticket[b], 1) == p.slices - 1;
-        if (s_last) {
-            p.ticket[b] = 0;
-            __threadfence();
-        }
+        int *ticket = &p.ticket[blockIdx.x];
+        s_last = atomicAdd(ticket, 1) == p.slices - 1;
+        if (s_last)
+            *ticket = 0;
+        __threadfence();
     }
     __syncthreads();
     if (!s_last)
         return;
-    for (int row = row0 + warp; row < row1; row += kWarps) {
+    if (warp < rows) {
+        const int row = g0 + warp;
         const Part *parts = p.parts + (size_t)row * p.slices;
         Part a = empty_part();
-        for (int k = lane; k < p.slices; k += 32) {
-            Part x;
-            *reinterpret_cast<float4 *>(&x) = __ldcg(reinterpret_cast<const float4 *>(parts + k));
-            *(reinterpret_cast<float4 *>(&x) + 1) = __ldcg(reinterpret_cast<const float4 *>(parts + k) + 1);
-            a = combine(a, x, inv_t);
-        }
+        for (int k0 = 0; k0 < p.slices; k0 += 64) {
+            Part x[2] = {empty_part(), empty_part()};
 #pragma unroll
-        for (int o = 16; o >= 1; o >>= 1)
-            a = combine(a, shfl_part(a, o), inv_t);
+            for (int y = 0; y < 2; ++y)
+                if (k0 + 32 * y + lane < p.slices) {
+                    const float4 *from = reinterpret_cast<const float4 *>(parts + k0 + 32 * y + lane);
+                    reinterpret_cast<float4 *>(&x[y])[0] = __ldcg(from);
+                    reinterpret_cast<float4 *>(&x[y])[1] = __ldcg(from + 1);
+                }
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+                a = combine(a, x[y], inv_t);
+        }
+        // the lanes' parts relative to the row's maximum, then plain sums
+        const float m = warp_max(a.m);
+        const unsigned arg = __reduce_min_sync(0xffffffffu, a.m == m ? (unsigned)a.arg : 0x7fffffffu);
+        Part top = empty_part();
+        top.m = m;
+        a = combine(a, top, inv_t);
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) {
+            a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+            a.u += __shfl_xor_sync(0xffffffffu, a.u, o);
+            a.st += __shfl_xor_sync(0xffffffffu, a.st, o);
+            a.ut += __shfl_xor_sync(0xffffffffu, a.ut, o);
+        }
         if (lane == 0) {
             // a row without an allowed token: sums 0 (NaN where its allowed logits are)
-            const bool none = a.m == -INFINITY;
+            const bool none = !(m > -INFINITY);
             const bool empty = none && a.s == 0.f;
             if (p.st.argmax)
-                p.st.argmax[row] = none ? -1 : a.arg;
+                p.st.argmax[row] = none ? -1 : (int)arg;
             if (p.st.top1)
                 p.st.top1[row] = empty ? 0.f : 1.f / a.s;
             if (p.st.entropy)
                 p.st.entropy[row] = empty ? 0.f : logf(a.s) - a.u / a.s;
-            const float sT = p.want_t ? a.st : a.s, uT = p.want_t ? a.ut : a.u;
+            const float sT = kStats > 1 ? a.st : a.s, uT = kStats > 1 ? a.ut : a.u;
             if (p.st.logz_t)
-                p.st.logz_t[row] = empty ? -INFINITY : __fdiv_rn(a.m, p.temperature) + logf(sT);
+                p.st.logz_t[row] = empty ? -INFINITY : __fdiv_rn(m, p.temperature) + logf(sT);
             if (p.st.entropy_t)
                 p.st.entropy_t[row] = empty ? 0.f : logf(sT) - uT / sT;
         }
-        const int j = row - row0;
-        if (p.st.draft_logit && lane == 0 && td && j > 0 && j < td->n) {
-            const int tok = p.r.draft[row], par = row0 + td->parent[j];
-            if (tok >= 0 && tok < p.V && par < p.n_rows)
-                p.st.draft_logit[row] = __ldcg(p.out + par * p.out_stride + tok);
-        }
+        // the draft tokens of the row's children
+        if (p.st.draft_logit && td && row - row0 < td->n)
+            for (int j = lane; j < min(td->n, row1 - row0); j += 32)
+                if (j > 0 && td->parent[j] == row - row0) {
+                    const int v = p.r.draft[row0 + j];
+                    if (v >= 0 && v < p.V)
+                        p.st.draft_logit[row0 + j] = __ldcg(p.out + row * p.out_stride + v);
+                }
     }
 }
 
-// Tokens per chunk: large ones where the batch fills the GPU with them, else
-// small ones, so that one request's rows spread over the SMs.
-int chunk_of(int batch, int vocab)
+// The tokens of a slice.
+int slice_of(int batch, int n_rows, int vocab, int n_sm)
 {
-    return (long long)batch * ((vocab + 1023) / 1024) >= 512 ? 1024 : 256;
+    // as many slices as give each SM four CTAs; longer ones scan a history less often
+    const long long rows = (n_rows + batch - 1) / batch, groups = (rows + kRows - 1) / kRows;
+    const long long per_slice = (long long)batch * groups;
+    const long long slices = (4ll * n_sm + per_slice - 1) / per_slice;
+    const long long size = (vocab + slices * kChunk - 1) / (slices * kChunk) * kChunk;
+    return (int)(size > kMaxSlice ? kMaxSlice : size);
 }
 
-constexpr size_t kPartsOff = 256 + (size_t)TB_MAX_REQUESTS * sizeof(int);
-
-template <int kVec>
-cudaError_t launch(const LogitArgs &a, int dtype, cudaStream_t stream)
+template <int kType>
+auto kernel_of(int stats_kind)
 {
-    const int size = a.chunks * 128 * kVec;
-    const size_t smem = (size_t)size * 8 + size / 8;
-    const auto kernel = dtype == TB_F32    ? k_logits<TB_F32, kVec>
-                        : dtype == TB_BF16 ? k_logits<TB_BF16, kVec>
-                                           : k_logits<TB_F16, kVec>;
-    const cudaError_t e = allow_max_smem((const void *)kernel);
-    return e != cudaSuccess ? e : launch_kernel(kernel, dim3(a.slices, a.batch), dim3(kThreads), smem, stream, true, a);
+    return stats_kind == 0 ? k_logits<kType, 0> : stats_kind == 1 ? k_logits<kType, 1> : k_logits<kType, 2>;
 }
+
+// tickets for every piece of rows that a call may have
+constexpr size_t kPartsOff = 256 + (size_t)(TB_MAX_REQUESTS + kMaxRowsCall / kRows) * sizeof(int);
 
 }  // namespace
 
@@ -492,10 +786,9 @@ using namespace tv;
 
 extern "C" size_t tb_logits_workspace_size(int batch, int n_rows, int vocab)
 {
-    if (batch < 1 || batch > TB_MAX_REQUESTS || n_rows < 0 || vocab < 1)
+    if (batch < 1 || batch > TB_MAX_REQUESTS || n_rows < 0 || n_rows > kMaxRowsCall || vocab < 1)
         return 0;
-    const int chunk = chunk_of(batch, vocab);
-    return kPartsOff + (size_t)n_rows * ((vocab + chunk - 1) / chunk) * sizeof(Part);
+    return kPartsOff + (size_t)n_rows * ((vocab + kChunk - 1) / kChunk) * sizeof(Part);  // the shortest slices
 }
 
 extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req, const void *logits, int dtype,
@@ -512,7 +805,7 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
         return st;
     if (dtype != TB_F32 && dtype != TB_BF16 && dtype != TB_F16)
         return record_error(TB_EUNSUPPORTED, "%s: logits of type %d", fn, dtype);
-    if (n_rows < 0 || vocab < 1 || logit_stride < vocab || out_stride < vocab)
+    if (n_rows < 0 || n_rows > kMaxRowsCall || vocab < 1 || logit_stride < vocab || out_stride < vocab)
         return record_error(TB_EINVAL, "%s: n_rows %d, vocab %d, strides %lld, %lld", fn, n_rows, vocab,
                             (long long)logit_stride, (long long)out_stride);
     if (!logits || !out || !ptr_aligned(logits, 16) || !ptr_aligned(out, 16))
@@ -554,17 +847,24 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
     a.out_stride = out_stride;
     a.temperature = temperature;
     a.scale_t = (float)(1.4426950408889634 / (double)temperature);
-    a.want = a.st.argmax || a.st.top1 || a.st.entropy || a.st.logz_t || a.st.entropy_t || a.st.draft_logit;
-    a.want_t = (a.st.logz_t || a.st.entropy_t) && temperature != 1.f;
     a.ticket = reinterpret_cast<int *>(static_cast<uint8_t *>(workspace) + 256);
     a.parts = reinterpret_cast<Part *>(static_cast<uint8_t *>(workspace) + kPartsOff);
-    const int chunk = chunk_of(req->batch, vocab), n_chunks = (vocab + chunk - 1) / chunk;
-    // chunks per slice: about six CTAs for each SM; a longer slice scans a
-    // request's history less often
-    long long per = ((long long)n_chunks * req->batch + 6ll * n_sm - 1) / (6ll * n_sm);
-    a.chunks = (int)(per < 1 ? 1 : per > kMaxChunks ? kMaxChunks : per);
-    a.slices = (n_chunks + a.chunks - 1) / a.chunks;
-    const cudaError_t e = chunk == 1024 ? launch<8>(a, dtype, (cudaStream_t)stream)
-                                        : launch<2>(a, dtype, (cudaStream_t)stream);
+    a.size = slice_of(req->batch, n_rows, vocab, n_sm);
+    a.slices = (vocab + a.size - 1) / a.size;
+    if (a.slices > 65535)
+        return record_error(TB_EUNSUPPORTED, "%s: vocab %d", fn, vocab);
+    // count, bias, two bitmaps, the list and its offsets; then the rings
+    a.ring_off = (a.size * 10 + a.size / 4 + a.size / 16 + 16 + 127) / 128 * 128;
+    a.mask_off = a.ring_off + kWarps * kStages * kChunk * (dtype == TB_F32 ? 4 : 2);
+    const size_t smem = (size_t)a.mask_off + kWarps * kStages * (kChunk / 32) * 4;
+    const bool want = a.st.argmax || a.st.top1 || a.st.entropy || a.st.logz_t || a.st.entropy_t || a.st.draft_logit;
+    const int stats_kind = !want ? 0 : (a.st.logz_t || a.st.entropy_t) && temperature != 1.f ? 2 : 1;
+    const auto kernel = dtype == TB_F32    ? kernel_of<TB_F32>(stats_kind)
+                        : dtype == TB_BF16 ? kernel_of<TB_BF16>(stats_kind)
+                                           : kernel_of<TB_F16>(stats_kind);
+    cudaError_t e = allow_max_smem((const void *)kernel);
+    if (e == cudaSuccess)
+        e = launch_kernel(kernel, dim3(req->batch + (n_rows + kRows - 1) / kRows, a.slices), dim3(kThreads), smem,
+                          (cudaStream_t)stream, true, a);
     return launch_result(e, fn);
 }

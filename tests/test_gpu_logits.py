@@ -216,3 +216,9 @@ def test_temperature_one_and_a_graph(bank):
         graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(s.out, first[0]) and all(torch.equal(s.st[k], v) for k, v in first[1].items())
+
+
+def test_an_empty_list_of_biases(bank):
+    s = Scene(17, [3, 0], 500, biases=0)
+    assert s.btok.size == 0
+    s.run(bank)
