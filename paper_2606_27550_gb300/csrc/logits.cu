@@ -92,18 +92,6 @@ __device__ __forceinline__ Part combine(const Part &a, const Part &b, float inv_
     return o;
 }
 
-__device__ __forceinline__ Part shfl_part(const Part &a, int mask)
-{
-    Part o;
-    o.m = __shfl_xor_sync(0xffffffffu, a.m, mask);
-    o.arg = __shfl_xor_sync(0xffffffffu, a.arg, mask);
-    o.s = __shfl_xor_sync(0xffffffffu, a.s, mask);
-    o.u = __shfl_xor_sync(0xffffffffu, a.u, mask);
-    o.st = __shfl_xor_sync(0xffffffffu, a.st, mask);
-    o.ut = __shfl_xor_sync(0xffffffffu, a.ut, mask);
-    return o;
-}
-
 template <int kType>
 struct In;
 template <>

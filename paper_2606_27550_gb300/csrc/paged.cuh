@@ -26,7 +26,7 @@ struct PlanHeader {
     int batch, n_q_heads, n_kv_heads, window, n_active;
     int P;       // CTAs that the tiles are split over
     long long total;
-    int rows, sink, pad[4];
+    int rows, sink, n_splits, pad[3];
 };
 static_assert(sizeof(PlanHeader) == 64, "");
 
@@ -38,22 +38,34 @@ struct PlanCta {
 };
 static_assert(sizeof(PlanCta) == 88, "eight-byte aligned records");
 
+// A unit that several CTAs share: what joining its partials needs.  rows 0: none.
+struct PlanSplit {
+    int c_lo, nseg;  // its CTAs
+    int lo_slot;     // which of c_lo's two partial slots is the unit's (of the others: their first)
+    int row0, rows;  // the request's first row; rows of the unit
+    int rb, head, pad;
+};
+static_assert(sizeof(PlanSplit) == 32, "");
+
 constexpr int kMaxPlanCtas = 512;
 
-// header, one PlanCta per attention CTA, then the requests with rows (n_active
+// header, one PlanCta per attention CTA, as many PlanSplits, then the requests with rows (n_active
 // of them) and one more record whose tile_base is the total
 inline size_t plan_bytes_for(int batch)
 {
-    return sizeof(PlanHeader) + kMaxPlanCtas * sizeof(PlanCta) + (size_t)(batch + 1) * sizeof(PlanReq);
+    return sizeof(PlanHeader) + kMaxPlanCtas * (sizeof(PlanCta) + sizeof(PlanSplit)) + (size_t)(batch + 1) * sizeof(PlanReq);
 }
 __host__ __device__ inline PlanCta *plan_ctas(void *plan)
 {
     return reinterpret_cast<PlanCta *>(static_cast<unsigned char *>(plan) + sizeof(PlanHeader));
 }
+__host__ __device__ inline PlanSplit *plan_splits(void *plan)
+{
+    return reinterpret_cast<PlanSplit *>(plan_ctas(plan) + kMaxPlanCtas);
+}
 __host__ __device__ inline PlanReq *plan_reqs(void *plan)
 {
-    return reinterpret_cast<PlanReq *>(static_cast<unsigned char *>(plan) + sizeof(PlanHeader) +
-                                       kMaxPlanCtas * sizeof(PlanCta));
+    return reinterpret_cast<PlanReq *>(plan_splits(plan) + kMaxPlanCtas);
 }
 
 // The first tile of CTA c's range when `total` tiles are split over P CTAs, and

@@ -752,98 +752,92 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     }
 }
 
-// Log-sum-exp join of the partials of every unit that CTAs share: block (x, y) takes
-// the unit that CTA x + 1's range starts inside (unless an earlier one does too)
-// and rows y, y + gridDim.y, .. of 8 each, a warp per row.
+// Log-sum-exp join of the partials of the units that CTAs share, in CTA order (the
+// same sums every time), a warp per row: warp w takes row w % 2^rows_log2 of split w
+// / 2^rows_log2, and so on.  Bound by its round trips (the split; the row's maxima,
+// sums and first partials together), so every row has a warp of its own: with two
+// rows per warp, and the splits found here instead of in the plan, it took 6.5 us
+// behind the attention of one 64-node layer at 16384 keys, 8.5 behind the ragged
+// batch's.  (Joined by the last CTA of a unit instead, without this launch, the one
+// SM needed 10 us for 64 rows of six partials.)
 template <int kD, bool kF16>
-__global__ void __launch_bounds__(256) k_paged_merge(const __grid_constant__ PagedArgs p)
+__global__ void __launch_bounds__(256) k_paged_merge(const __grid_constant__ PagedArgs p, int rows_log2)
 {
-    constexpr int kSlot = slot_floats(kD), kCols = kD / 32;
+    constexpr int kSlot = slot_floats(kD), kCols = kD / 32, kAhead = 8;
     pdl_wait();
     pdl_trigger();
-    const PlanCta *ctas = plan_ctas(p.plan);
-    const int cb = blockIdx.x + 1;
+    const int lane = threadIdx.x & 31;
+    int item = (blockIdx.x * 256 + threadIdx.x) >> 5;
     const PlanHeader *hd = static_cast<const PlanHeader *>(p.plan);
-    const bool ok = hd->valid && hd->batch == p.batch && hd->n_q_heads == p.Hq && hd->n_kv_heads == p.Hkv;
-    const PlanCta me = ctas[cb];
-    if (!ok || me.t0 >= me.t1)
+    PlanSplit s = plan_splits(p.plan)[min(item >> rows_log2, kMaxPlanCtas - 1)];
+    const int items = hd->n_splits << rows_log2;
+    if (!hd->valid || hd->batch != p.batch || hd->n_q_heads != p.Hq || hd->n_kv_heads != p.Hkv)
         return;
-    const PlanReq &r = me.req;
-    const long long tl = me.t0 - r.tile_base;
-    const int u = (int)(tl / r.T);
-    const long long u_first = r.tile_base + (long long)u * r.T;
-    if (me.t0 == u_first)
-        return;
-    const int c_lo = plan_cta_of(me.total, me.P, u_first), c_hi = plan_cta_of(me.total, me.P, u_first + r.T - 1);
-    if (cb != c_lo + 1)
-        return;
-    const int nseg = c_hi - c_lo + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rb = u % r.row_blocks, head = u / r.row_blocks;
-    const int rows = min(128, r.n * p.group - rb * 128);
-    for (int x = blockIdx.y * 8 + warp; x < rows; x += gridDim.y * 8) {
-        const int grow = rb * 128 + x, node = grow / p.group, qh = head * p.group + grow % p.group;
-        if (r.row0 + node >= p.n_rows || !in_bounds(c_lo >= 0 && c_hi < me.P && qh < p.Hq, p.status))
+    for (; item < items; item += gridDim.x * 8, s = plan_splits(p.plan)[min(item >> rows_log2, kMaxPlanCtas - 1)]) {
+        const int x = item & ((1 << rows_log2) - 1);
+        const int grow = s.rb * 128 + x, node = grow / p.group, qh = s.head * p.group + grow % p.group;
+        if (x >= s.rows || s.row0 + node >= p.n_rows || !in_bounds(qh < p.Hq && s.c_lo >= 0, p.status))
             continue;
-        auto slot_of = [&](int k) {
-            const int cc = c_lo + k;
-            return p.part + ((size_t)cc * 2 + (plan_split(me.total, me.P, cc) >= u_first ? 0 : 1)) * kSlot;
-        };
-        // lane k of a group of 32 CTAs has its maximum and sum
+        const float *first = p.part + ((size_t)s.c_lo * 2 + s.lo_slot) * kSlot;
+        const float *rest = p.part + (size_t)s.c_lo * 2 * kSlot;  // CTA k > 0: + 2 k slots
         float M = -INFINITY, sum = 0.f, acc[kCols] = {};
-        for (int k0 = 0; k0 < nseg; k0 += 32) {
-            const bool have = k0 + lane < nseg;
-            const float *sl = slot_of(have ? k0 + lane : 0);
+        for (int k0 = 0; k0 < s.nseg; k0 += 32) {
+            // lane k has the k-th CTA's maximum and sum
+            const bool have = k0 + lane < s.nseg;
+            const float *sl = k0 + lane == 0 ? first : rest + (size_t)(have ? k0 + lane : 1) * 2 * kSlot;
             const float ms = have ? __ldcg(sl + 128 * kD + x) : -INFINITY;
             const float ls = have ? __ldcg(sl + 128 * kD + 128 + x) : 0.f;
-            const unsigned long long base = reinterpret_cast<unsigned long long>(sl + x * kD);
-            float m2 = ms;
+            const int cnt = min(32, s.nseg - k0);
+            float w = 0.f;
+            for (int k = 0; k < cnt; k += kAhead) {
+                float v[kAhead][kCols];
 #pragma unroll
-            for (int o = 16; o >= 1; o >>= 1)
-                m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, o));
-            m2 = fmaxf(m2, M);
-            const float keep = M == -INFINITY ? 0.f : ex2_approx(M - m2);
-            const float w = ms == -INFINITY ? 0.f : ex2_approx(ms - m2);
-            float ws = w * ls;
-#pragma unroll
-            for (int o = 16; o >= 1; o >>= 1)
-                ws += __shfl_xor_sync(0xffffffffu, ws, o);
-            M = m2;
-            sum = sum * keep + ws;
-#pragma unroll
-            for (int i = 0; i < kCols; ++i)
-                acc[i] *= keep;
-            const int cnt = min(32, nseg - k0);
-            for (int k = 0; k < cnt; k += 4) {
-                float v[4][kCols], wk[4];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const unsigned long long b =
-                        __shfl_sync(0xffffffffu, base, (k + y) & 31) + 4ull * kCols * lane;
-                    wk[y] = __shfl_sync(0xffffffffu, w, (k + y) & 31);
-                    if (k + y >= cnt)
-                        continue;
+                for (int z = 0; z < kAhead; ++z) {
+                    const int c = k0 + min(k + z, cnt - 1);
+                    const float *from = (c == 0 ? first : rest + (size_t)c * 2 * kSlot) + x * kD;
                     if constexpr (kCols == 4) {
-                        const float4 f = __ldcg(reinterpret_cast<const float4 *>(b));
-                        v[y][0] = f.x, v[y][1] = f.y, v[y][2] = f.z, v[y][3] = f.w;
+                        const float4 f = __ldcg(reinterpret_cast<const float4 *>(from) + lane);
+                        v[z][0] = f.x, v[z][1] = f.y, v[z][2] = f.z, v[z][3] = f.w;
                     } else {
-                        const float2 f = __ldcg(reinterpret_cast<const float2 *>(b));
-                        v[y][0] = f.x, v[y][1] = f.y;
+                        const float2 f = __ldcg(reinterpret_cast<const float2 *>(from) + lane);
+                        v[z][0] = f.x, v[z][1] = f.y;
                     }
                 }
+                if (k == 0) {
+                    float m2 = ms;
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    if (k + y < cnt)
+                    for (int o = 16; o >= 1; o >>= 1)
+                        m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, o));
+                    m2 = fmaxf(m2, M);
+                    const float keep = M == -INFINITY ? 0.f : ex2_approx(M - m2);
+                    w = ms == -INFINITY ? 0.f : ex2_approx(ms - m2);
+                    float ws = w * ls;
 #pragma unroll
-                        for (int i = 0; i < kCols; ++i)
-                            acc[i] += wk[y] * v[y][i];
+                    for (int o = 16; o >= 1; o >>= 1)
+                        ws += __shfl_xor_sync(0xffffffffu, ws, o);
+                    M = m2;
+                    sum = sum * keep + ws;
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i)
+                        acc[i] *= keep;
+                }
+#pragma unroll
+                for (int z = 0; z < kAhead; ++z) {
+                    const float wk = k + z < cnt ? __shfl_sync(0xffffffffu, w, (k + z) & 31) : 0.f;
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i)
+                        acc[i] += k + z < cnt ? wk * v[z][i] : 0.f;
+                }
             }
         }
         const float inv = sum > 0.f ? 1.f / sum : 0.f;
-        const size_t row = (size_t)(r.row0 + node) * p.Hq + qh;
+        const size_t row = (size_t)(s.row0 + node) * p.Hq + qh;
         uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + row * kD) + lane * (kCols / 2);
-#pragma unroll
-        for (int i = 0; i < kCols / 2; ++i)
-            dst[i] = pack<kF16>(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+        if constexpr (kCols == 4)
+            *reinterpret_cast<uint2 *>(dst) =
+                make_uint2(pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv));
+        else
+            *dst = pack<kF16>(acc[0] * inv, acc[1] * inv);
         if (p.lse && lane == 0)
             p.lse[row] = sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
     }
@@ -859,9 +853,13 @@ cudaError_t launch(const PagedArgs &a, int n_sm, int max_rows, cudaStream_t stre
     e = launch_kernel(k_paged_attention<kD, kF16, kForm>, dim3(n_sm), dim3(kThreads), smem, stream, true, a);
     if (e != cudaSuccess || n_sm < 2)
         return e;
-    // rows of a unit over blocks of 8, at most four blocks
-    const int groups = (max_rows + 7) / 8;
-    return launch_kernel(k_paged_merge<kD, kF16>, dim3(n_sm - 1, groups < 4 ? groups : 4), dim3(256), 0, stream, true, a);
+    int rows_log2 = 0;
+    while ((1 << rows_log2) < max_rows)
+        ++rows_log2;
+    const long long warps = (long long)(n_sm - 1) << rows_log2;  // a row of each possible split
+    const int blocks = (int)((warps + 7) / 8);
+    return launch_kernel(k_paged_merge<kD, kF16>, dim3(blocks < 4 * n_sm ? blocks : 4 * n_sm), dim3(256), 0, stream, true,
+                         a, rows_log2);
 }
 
 template <int kD, bool kF16>

@@ -38,6 +38,8 @@ struct PlanArgs {
 };
 
 // Exclusive sums over the block of K values a thread; the totals in `total`.
+static_assert(kMaxPlanCtas <= kThreads, "a split per thread");
+
 template <int K>
 __device__ void block_scan(long long (&v)[K], long long (&total)[K])
 {
@@ -293,6 +295,31 @@ __global__ void __launch_bounds__(kThreads) k_paged_plan(const __grid_constant__
             }
             ctas[c] = x;
         }
+        // the units that a CTA's range starts inside, each once: at its second CTA
+        PlanSplit sp = {};
+        const int c = threadIdx.x;  // P <= kThreads
+        if (c > 0 && c < P && n_active > 0) {
+            const long long t = plan_split(total3[2], P, c);
+            const PlanReq r = out[owner_of(s_tile, n_active, t)];
+            const long long tl = t - r.tile_base;
+            const int u = (int)(tl / r.T);
+            const long long begin = r.tile_base + (long long)u * r.T;
+            if (t > begin && plan_split(total3[2], P, c - 1) <= begin) {
+                sp.c_lo = c - 1;
+                sp.nseg = plan_cta_of(total3[2], P, begin + r.T - 1) - sp.c_lo + 1;
+                sp.lo_slot = plan_split(total3[2], P, c - 1) == begin ? 0 : 1;
+                sp.row0 = r.row0;
+                sp.rb = u % r.row_blocks;
+                sp.head = u / r.row_blocks;
+                sp.rows = min(128, r.n * group - sp.rb * 128);
+            }
+        }
+        long long v1[1] = {sp.rows > 0}, n_splits[1];
+        block_scan<1>(v1, n_splits);
+        if (sp.rows > 0)
+            plan_splits(p.plan)[v1[0]] = sp;
+        if (threadIdx.x == 0)
+            hd->n_splits = (int)n_splits[0];
     }
 
     // the rows
