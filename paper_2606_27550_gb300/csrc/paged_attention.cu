@@ -25,12 +25,12 @@
 // (not multiplied) by -inf, and the softmax threads overwrite their V rows with
 // zeros before P V reads them, since 0 * NaN is NaN.
 //
-// One CTA per SM, 12 warps: 0 and 3 load K and V tiles through separate rings, 1
-// issues Q K^T (S double-buffered) and holds the TMEM, 2 issues P V, 4-7 are the
-// softmax (a thread per row), 8-11 stage the next unit's queries and write the
-// finished unit's output.
-// TMEM columns: S0 [0, 128), S1 [128, 256), P0 / P1 on their first halves, O [256,
-// 256 + kD), Q0 [384, 384 + kD / 2), Q1 behind it.  Row r sits in lane 32 (r % 4) +
+// One CTA per SM, 16 warps: 0 and 3 load K and V tiles through separate rings, 1
+// issues Q K^T (S double-buffered) and holds the TMEM, 2 issues P V, 4-7 and 12-15
+// are the softmax (two threads per row, half of a tile's columns each), 8-11 stage
+// the next unit's queries and write the finished unit's output.
+// TMEM columns: S0 [0, 128), S1 [128, 256), of each the halves' P on their first 32
+// columns, O [256, 256 + kD), Q0 [384, 384 + kD / 2), Q1 behind it.  Row r sits in lane 32 (r % 4) +
 // r / 4, so that few rows spread over the four SM sub-partitions.
 #include "paged.cuh"
 
@@ -44,7 +44,8 @@ namespace {
 
 constexpr int kBN = kTileKeys;
 constexpr int kAtom = 128 * 128;  // bytes of a 64-column swizzle atom of 128 rows
-constexpr int kThreads = 384;
+constexpr int kThreads = 512;
+constexpr int kHalf = kBN / 2;  // columns of a softmax thread
 constexpr int kKStages = 3, kVStages = 2, kMaxStages = 3;
 constexpr uint32_t kColS = 0, kColO = 256, kColQ = 384;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -180,7 +181,7 @@ struct SegInfo {
     uint64_t anc[128];   // tree nodes that it sees
     int pos[128];
     float slope[128];    // times log2(e)
-    float m[128], l[128];  // written back by the softmax
+    float m[128], l[2][128];  // written back by the softmax (a sum of each half)
     int8_t depth[kMaxNodes];
 };
 
@@ -194,6 +195,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
     __shared__ __align__(8) uint64_t s_full[2], p_full[2], pv_done[2], q_full[2], ml_full[2], o_free[2], drain_bar;
+    __shared__ __align__(8) uint64_t mx_full[4][2];  // per lane quadrant: both halves' row maxima are there
+    __shared__ float s_mx[2][2][128];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag, s_ok;
     __shared__ __align__(8) PlanCta s_cta;
@@ -210,11 +213,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&s_full[b], 1);
-            mbar_init(&p_full[b], 4);
+            mbar_init(&p_full[b], 8);
             mbar_init(&pv_done[b], 1);
             mbar_init(&q_full[b], 4);
-            mbar_init(&ml_full[b], 4);
+            mbar_init(&ml_full[b], 8);
             mbar_init(&o_free[b], 4);
+            for (int q = 0; q < 4; ++q)
+                mbar_init(&mx_full[q][b], 2);
         }
         mbar_init(&drain_bar, 2);
         abort_flag = 0;
@@ -370,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     const uint32_t v_base = smem_u32(sV + (size_t)s * kTile);
 #pragma unroll
                     for (int ks = 0; ks < kBN / 16; ++ks)
-                        tc_mma_f16_ts(tmem + kColO, tmem + kColS + b * 128 + ks * 8,
+                        tc_mma_f16_ts(tmem + kColO, tmem + kColS + b * 128 + (ks >> 2) * 64 + (ks & 3) * 8,
                                       smem_desc_sw128(v_base + ks * 2048, kAtom, 1024), idesc<kF16>(kD, true),
                                       (j == 0 && ks == 0) ? 0u : 1u);
                     tc_commit(&v_empty[s]);
@@ -384,9 +389,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             }
             tc_commit(&drain_bar);
         }
-    } else if (warp < 8) {
-        // ---------------------------------------------------- softmax (warps 4-7)
-        const int q4 = warp & 3;
+    } else if (warp < 8 || warp >= 12) {
+        // ---------------------------------------------------- softmax (warps 4-7 and 12-15)
+        // two threads per row: the lower half of a tile's columns and the upper one
+        const int q4 = warp & 3, half = warp >= 12 ? 1 : 0;
         const uint32_t lane_addr = tmem + ((uint32_t)(32 * q4) << 16);
         const int rloc = 4 * lane + q4;
         long long it = 0;
@@ -409,19 +415,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     break;
                 }
                 tc_fence_after();
-                const uint32_t sa = lane_addr + kColS + b * 128;
-                const bool masked = key0 + kBN > L || key0 < si.lo_max;
+                const uint32_t sa = lane_addr + kColS + b * 128 + half * kHalf;
+                const int h0 = key0 + half * kHalf;  // this thread's first slot
+                const bool masked = h0 + kHalf > L || h0 < si.lo_max;
                 // scores that are not a multiple of S are written back in units of ln 2
                 const bool final_z = kForm == kBias || (kForm == kCap && masked);
 
-                // pass 1: the row maximum over the allowed keys, 32 columns at a time
+                // pass 1: the maximum over this half's allowed keys, 32 columns at a time
                 float mx = -INFINITY;
 #pragma unroll 1
-                for (int c0 = 0; c0 < kBN; c0 += 32) {
+                for (int c0 = 0; c0 < kHalf; c0 += 32) {
                     uint32_t r[32];
                     tmem_ld_32x32b_x32(sa + c0, r);
                     tmem_ld_wait();
-                    const int s0 = key0 + c0;
+                    const int s0 = h0 + c0;
                     if constexpr (kForm == kBias) {
                         if (p.cap > 0.f) {
 #pragma unroll
@@ -471,8 +478,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 }
                 if (!final_z)
                     mx = kForm == kCap ? capped(mx, p.cap, p.cap_in) : mx * p.scale;
+                // the other half's
+                s_mx[b][half][rloc] = mx;
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(&mx_full[q4][b]);
+                if (!mbar_wait_bounded(&mx_full[q4][b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status)) {
+                    aborted = true;
+                    break;
+                }
+                mx = fmaxf(mx, s_mx[b][half ^ 1][rloc]);
 
-                // the lazily raised reference
+                // the lazily raised reference, the same in both
                 float alpha = 1.f;
                 bool rescale = false;
                 if (j == 0) {
@@ -483,6 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     rescale = true;
                 }
                 if (__any_sync(0xffffffffu, rescale)) {
+                    // O holds the previous tiles' P V: wait for the last one, then scale in place
                     const long long jp = it - 1;
                     if (!mbar_wait_bounded(&pv_done[jp & 1], (uint32_t)(jp >> 1) & 1u, &abort_flag, p.status)) {
                         aborted = true;
@@ -491,7 +509,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     tc_fence_after();
                     l *= alpha;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < kD; c0 += 32) {
+                    for (int c0 = half * (kD / 2); c0 < (half + 1) * (kD / 2); c0 += 32) {
                         uint32_t o[32];
                         tmem_ld_32x32b_x32(lane_addr + kColO + c0, o);
                         tmem_ld_wait();
@@ -503,11 +521,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     tmem_st_wait();
                 }
 
-                // pass 2: P in the pages' type, its 32-bit sum into l
+                // pass 2: P in the pages' type on the first columns of this half, its 32-bit sum into l
                 const float mu = m_ref == -INFINITY ? 0.f : m_ref;
                 float rs = 0.f;
 #pragma unroll 1
-                for (int c0 = 0; c0 < kBN; c0 += 32) {
+                for (int c0 = 0; c0 < kHalf; c0 += 32) {
                     uint32_t r[32];
                     tmem_ld_32x32b_x32(sa + c0, r);
                     tmem_ld_wait();
@@ -539,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     if (slot >= end || slot < si.begin || (slot < si.lo_min && slot >= si.far)) {
                         uint8_t *row = sV + (size_t)sv * kTile + rloc * 128;
 #pragma unroll
-                        for (int x = 0; x < kD / 8; ++x)
+                        for (int x = half * (kD / 16); x < (half + 1) * (kD / 16); ++x)
                             *reinterpret_cast<uint4 *>(row + (x >> 3) * kAtom + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
                     }
                     fence_proxy_async_smem();
@@ -554,8 +572,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 break;
             if (sg >= 2 && !mbar_wait_bounded(&o_free[sg & 1], (uint32_t)((sg >> 1) - 1) & 1u, &abort_flag, p.status))
                 break;
-            si.m[rloc] = m_ref;
-            si.l[rloc] = l;
+            if (half == 0)
+                si.m[rloc] = m_ref;
+            si.l[half][rloc] = l;
             __syncwarp();
             if (lane == 0)
                 mbar_arrive(&ml_full[sg & 1]);
@@ -684,7 +703,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             const long long last = it - 1;
             if (!mbar_wait_bounded(&ml_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status))
                 break;
-            const float m_ref = s_info[sg & 1].m[rloc], l = s_info[sg & 1].l[rloc];
+            const float m_ref = s_info[sg & 1].m[rloc], l = s_info[sg & 1].l[0][rloc] + s_info[sg & 1].l[1][rloc];
             if (!mbar_wait_bounded(&pv_done[last & 1], (uint32_t)(last >> 1) & 1u, &abort_flag, p.status))
                 break;
             tc_fence_after();
@@ -693,13 +712,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             uint4 *dst = reinterpret_cast<uint4 *>(p.out + now.row * kD);
             float *slot = p.part + ((size_t)c * 2 + (now.first ? 0 : 1)) * kSlot;
             float4 *pdst = reinterpret_cast<float4 *>(slot + rloc * kD);
-#pragma unroll
-            for (int c0 = 0; c0 < kD; c0 += 64) {
-                uint32_t r[64];
+#pragma unroll 1
+            for (int c0 = 0; c0 < kD; c0 += 32) {
+                uint32_t r[32];
                 tmem_ld_32x32b_x32(lane_addr + kColO + c0, r);
-                tmem_ld_32x32b_x32(lane_addr + kColO + c0 + 32, r + 32);
                 tmem_ld_wait();
-                if (c0 + 64 == kD) {
+                if (c0 + 32 == kD) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0)
@@ -709,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     continue;
                 if (whole) {
 #pragma unroll
-                    for (int ch = 0; ch < 8; ++ch) {
+                    for (int ch = 0; ch < 4; ++ch) {
                         uint4 v;
                         v.x = pack<kF16>(__uint_as_float(r[8 * ch + 0]) * inv, __uint_as_float(r[8 * ch + 1]) * inv);
                         v.y = pack<kF16>(__uint_as_float(r[8 * ch + 2]) * inv, __uint_as_float(r[8 * ch + 3]) * inv);
@@ -719,7 +737,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     }
                 } else {
 #pragma unroll
-                    for (int x = 0; x < 16; ++x)
+                    for (int x = 0; x < 8; ++x)
                         pdst[c0 / 4 + x] = make_float4(__uint_as_float(r[4 * x]), __uint_as_float(r[4 * x + 1]),
                                                        __uint_as_float(r[4 * x + 2]), __uint_as_float(r[4 * x + 3]));
                 }
@@ -761,19 +779,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
 // batch's.  (Joined by the last CTA of a unit instead, without this launch, the one
 // SM needed 10 us for 64 rows of six partials.)
 template <int kD, bool kF16>
-__global__ void __launch_bounds__(256) k_paged_merge(const __grid_constant__ PagedArgs p, int rows_log2)
+__global__ void __launch_bounds__(256, 4) k_paged_merge(const __grid_constant__ PagedArgs p, int rows_log2)
 {
-    constexpr int kSlot = slot_floats(kD), kCols = kD / 32, kAhead = 8;
+    constexpr int kSlot = slot_floats(kD), kCols = kD / 32, kAhead = 4;
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
     int item = (blockIdx.x * 256 + threadIdx.x) >> 5;
     const PlanHeader *hd = static_cast<const PlanHeader *>(p.plan);
-    PlanSplit s = plan_splits(p.plan)[min(item >> rows_log2, kMaxPlanCtas - 1)];
-    const int items = hd->n_splits << rows_log2;
+    auto split_at = [&](int i) { return plan_splits(p.plan)[min(i >> rows_log2, kMaxPlanCtas - 1)]; };
+    PlanSplit s, next = split_at(item);
+    const int items = hd->n_splits << rows_log2, stride = gridDim.x * 8;
     if (!hd->valid || hd->batch != p.batch || hd->n_q_heads != p.Hq || hd->n_kv_heads != p.Hkv)
         return;
-    for (; item < items; item += gridDim.x * 8, s = plan_splits(p.plan)[min(item >> rows_log2, kMaxPlanCtas - 1)]) {
+    for (; item < items; item += stride) {
+        s = next;
+        if (item + stride < items)
+            next = split_at(item + stride);
         const int x = item & ((1 << rows_log2) - 1);
         const int grow = s.rb * 128 + x, node = grow / p.group, qh = s.head * p.group + grow % p.group;
         if (x >= s.rows || s.row0 + node >= p.n_rows || !in_bounds(qh < p.Hq && s.c_lo >= 0, p.status))
