@@ -122,6 +122,14 @@ __device__ __forceinline__ uint32_t range_bits(int s0, int lo, int hi)
     return (0xffffffffu >> (32 - (b - a))) << a;
 }
 
+// The bits of a node set of the 32 slots from s0 on (the tree begins at slot L).
+__device__ __forceinline__ uint32_t tree_bits(int s0, int L, uint64_t nodes)
+{
+    if (s0 >= L)
+        return s0 - L < 64 ? (uint32_t)(nodes >> (s0 - L)) : 0u;
+    return s0 + 32 > L ? (uint32_t)(nodes << (L - s0)) : 0u;
+}
+
 // A CTA's position: the request that its next tile lies in, the one after it
 // fetched ahead.
 struct Cursor {
@@ -179,10 +187,10 @@ struct SegInfo {
     int L, end, begin, far, lo_min, lo_max;  // far: end of the kept first tokens within the prefix
     int lo[128];         // per row: the first prefix slot that its window sees
     uint64_t anc[128];   // tree nodes that it sees
+    uint64_t path[128];  // its root path
     int pos[128];
     float slope[128];    // times log2(e)
     float m[128], l[2][128];  // written back by the softmax (a sum of each half)
-    int8_t depth[kMaxNodes];
 };
 
 template <int kD, bool kF16, int kForm>
@@ -403,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             if (!mbar_wait_bounded(&q_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status))
                 break;
             const int n = si.n, L = si.L, end = si.end, lo = si.lo[rloc], pos = si.pos[rloc];
-            const uint64_t anc = si.anc[rloc];
+            const uint64_t anc = si.anc[rloc], path = kForm == kBias ? si.path[rloc] : 0;
             const float slope = si.slope[rloc];
             t += n;
             float m_ref = -INFINITY, l = 0.f;
@@ -418,66 +426,57 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 const uint32_t sa = lane_addr + kColS + b * 128 + half * kHalf;
                 const int h0 = key0 + half * kHalf;  // this thread's first slot
                 const bool masked = h0 + kHalf > L || h0 < si.lo_max;
-                // scores that are not a multiple of S are written back in units of ln 2
-                const bool final_z = kForm == kBias || (kForm == kCap && masked);
-
-                // pass 1: the maximum over this half's allowed keys, 32 columns at a time
-                float mx = -INFINITY;
-#pragma unroll 1
-                for (int c0 = 0; c0 < kHalf; c0 += 32) {
-                    uint32_t r[32];
-                    tmem_ld_32x32b_x32(sa + c0, r);
-                    tmem_ld_wait();
-                    const int s0 = h0 + c0;
-                    if constexpr (kForm == kBias) {
-                        if (p.cap > 0.f) {
+                // this half's scores, held in registers until they are weights
+                uint32_t r[kHalf];
+                tmem_ld_32x32b_x32(sa, r);
+                tmem_ld_32x32b_x32(sa + 32, r + 32);
+                tmem_ld_wait();
+                if constexpr (kForm != kPlain) {
+                    if (kForm == kCap || p.cap > 0.f) {
 #pragma unroll
-                            for (int x = 0; x < 32; ++x)
-                                r[x] = __float_as_uint(capped(__uint_as_float(r[x]), p.cap, p.cap_in));
-                        } else {
+                        for (int x = 0; x < kHalf; ++x)
+                            r[x] = __float_as_uint(capped(__uint_as_float(r[x]), p.cap, p.cap_in));
+                    } else {
 #pragma unroll
-                            for (int x = 0; x < 32; ++x)
-                                r[x] = __float_as_uint(__uint_as_float(r[x]) * p.scale);
-                        }
-                        if (s0 + 32 <= L) {
-                            const float d0 = (float)(pos - s0);
+                        for (int x = 0; x < kHalf; ++x)
+                            r[x] = __float_as_uint(__uint_as_float(r[x]) * p.scale);
+                    }
+                }
+                if (masked) {
 #pragma unroll
-                            for (int x = 0; x < 32; ++x)
-                                r[x] = __float_as_uint(fmaf(-slope, d0 - (float)x, __uint_as_float(r[x])));
-                        } else {
+                    for (int y = 0; y < kHalf; y += 32) {
+                        const int s0 = h0 + y;
+                        if constexpr (kForm == kBias) {
+                            // the distance falls by one from slot to slot of the prefix, and behind
+                            // each node of the row's root path (its nodes are in order of depth)
+                            float dist = (float)(s0 <= L ? pos - s0
+                                                         : pos - L - (s0 - L < 64 ? __popcll(path & ((1ull << (s0 - L)) - 1))
+                                                                                  : __popcll(path)));
+                            const uint32_t fall = range_bits(s0, s0, L) | tree_bits(s0, L, path);
 #pragma unroll
                             for (int x = 0; x < 32; ++x) {
-                                const int node = s0 + x - L;
-                                const int at = node < 0 ? s0 + x : L + si.depth[min(node, kMaxNodes - 1)];
-                                r[x] = __float_as_uint(fmaf(-slope, (float)(pos - at), __uint_as_float(r[x])));
+                                r[y + x] = __float_as_uint(fmaf(-slope, dist, __uint_as_float(r[y + x])));
+                                dist -= (fall >> x) & 1u ? 1.f : 0.f;
                             }
                         }
-                    }
-                    if (masked) {
-                        uint32_t allow = range_bits(s0, lo, L) | range_bits(s0, si.begin, si.far);
-                        if (s0 >= L)
-                            allow |= s0 - L < 64 ? (uint32_t)(anc >> (s0 - L)) : 0u;
-                        else if (s0 + 32 > L)
-                            allow |= (uint32_t)(anc << (L - s0));
-                        if constexpr (kForm == kCap) {
-#pragma unroll
-                            for (int x = 0; x < 32; ++x)
-                                r[x] = __float_as_uint(capped(__uint_as_float(r[x]), p.cap, p.cap_in));
-                        }
+                        const uint32_t allow =
+                            range_bits(s0, lo, L) | range_bits(s0, si.begin, si.far) | tree_bits(s0, L, anc);
 #pragma unroll
                         for (int x = 0; x < 32; ++x)
-                            r[x] = (allow >> x) & 1u ? r[x] : 0xff800000u;
+                            r[y + x] = (allow >> x) & 1u ? r[y + x] : 0xff800000u;
                     }
-                    if (masked || kForm == kBias) {
-                        tmem_st_32x32b_x32(sa + c0, r);
-                        tmem_st_wait();
-                    }
+                } else if constexpr (kForm == kBias) {
+                    const float d0 = (float)(pos - h0);
 #pragma unroll
-                    for (int x = 0; x < 32; ++x)
-                        mx = fmaxf(mx, __uint_as_float(r[x]));
+                    for (int x = 0; x < kHalf; ++x)
+                        r[x] = __float_as_uint(fmaf(-slope, d0 - (float)x, __uint_as_float(r[x])));
                 }
-                if (!final_z)
-                    mx = kForm == kCap ? capped(mx, p.cap, p.cap_in) : mx * p.scale;
+                float mx = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < kHalf; ++x)
+                    mx = fmaxf(mx, __uint_as_float(r[x]));
+                if constexpr (kForm == kPlain)
+                    mx *= p.scale;
                 // the other half's
                 s_mx[b][half][rloc] = mx;
                 __syncwarp();
@@ -489,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 }
                 mx = fmaxf(mx, s_mx[b][half ^ 1][rloc]);
 
-                // the lazily raised reference, the same in both
+                // the lazily raised reference, the same in both halves
                 float alpha = 1.f;
                 bool rescale = false;
                 if (j == 0) {
@@ -521,30 +520,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     tmem_st_wait();
                 }
 
-                // pass 2: P in the pages' type on the first columns of this half, its 32-bit sum into l
+                // P in the pages' type on the first columns of this half, its 32-bit sum into l
                 const float mu = m_ref == -INFINITY ? 0.f : m_ref;
+                const float f = kForm == kPlain ? p.scale : 1.f;
                 float rs = 0.f;
-#pragma unroll 1
-                for (int c0 = 0; c0 < kHalf; c0 += 32) {
-                    uint32_t r[32];
-                    tmem_ld_32x32b_x32(sa + c0, r);
-                    tmem_ld_wait();
-                    if (kForm == kCap && !final_z) {
 #pragma unroll
-                        for (int x = 0; x < 32; ++x)
-                            r[x] = __float_as_uint(capped(__uint_as_float(r[x]), p.cap, p.cap_in));
-                    }
-                    const float f = kForm == kPlain ? p.scale : 1.f;
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const float p0 = ex2_approx(fmaf(__uint_as_float(r[2 * x]), f, -mu));
-                        const float p1 = ex2_approx(fmaf(__uint_as_float(r[2 * x + 1]), f, -mu));
-                        rs += p0 + p1;
-                        pk[x] = pack<kF16>(p0, p1);
-                    }
-                    tmem_st_32x32b_x16(sa + c0 / 2, pk);
+                for (int x = 0; x < kHalf / 2; ++x) {
+                    const float p0 = ex2_approx(fmaf(__uint_as_float(r[2 * x]), f, -mu));
+                    const float p1 = ex2_approx(fmaf(__uint_as_float(r[2 * x + 1]), f, -mu));
+                    rs += p0 + p1;
+                    r[x] = pack<kF16>(p0, p1);
                 }
+                tmem_st_32x32b_x32(sa, r);
                 l += rs;
                 if (key0 + kBN > end || key0 < si.lo_min) {
                     // V rows that nobody sees may hold anything: zeros, once the tile has landed
@@ -622,11 +609,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 qv[i] = u.valid ? src[i] : make_uint4(0, 0, 0, 0);
             // what this row sees
             const TreeDesc &td = p.trees[u.r.tree];
-            const int tid = threadIdx.x - 256, L = u.r.L;
+            const int L = u.r.L;
             const int dep = u.valid ? td.depth[u.node] : 0;
             uint64_t anc = u.valid ? td.anc[u.node] : 0ull;
-            if (tid < kMaxNodes)
-                si.depth[tid] = td.depth[tid];
+            if constexpr (kForm == kBias)
+                si.path[rloc] = anc;
             if (window > 0 && dep >= window) {
                 // ancestors that the window has left behind
                 uint64_t near = 0;
