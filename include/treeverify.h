@@ -605,7 +605,8 @@ TB_API size_t tb_paged_plan_size(int batch, int device);
  *             sink (0, 0: none; see paged_tree_attention), read by
  *             paged_tree_attention calls of this step; a model whose layers
  *             differ in them makes one plan for each kind (pool NULL for the
- *             second).  n_q_heads = 0: no attention follows.
+ *             second).  n_q_heads = 0: no attention follows.  At most 64 query
+ *             heads per kv head (TB_EUNSUPPORTED).
  * One kernel. */
 TB_API tb_status paged_plan(const tb_bank *bank, const tb_requests *req, const tb_page_pool *pool, int64_t *slots,
                             int32_t *positions, int max_rows, int32_t *status, int n_q_heads, int n_kv_heads,

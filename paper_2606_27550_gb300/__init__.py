@@ -786,7 +786,7 @@ def logits_process(bank, req: Requests, logits, out, ws, draft=None, history=Non
     if kind is None or out.dtype is not _F32:
         raise TypeError(f"logits {logits.dtype}, out {out.dtype}: a 32- or 16-bit float type and float32 expected")
     rows, vocab = shape
-    if bias_start is not None and bias_token.numel() == 0:
+    if bias_token is not None and bias_token.numel() == 0:
         bias_start = None  # an empty list has no address
     width = words = 0
     if history is not None:

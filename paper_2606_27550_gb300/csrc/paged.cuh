@@ -9,14 +9,13 @@ namespace tv {
 
 constexpr int kTileKeys = 128;  // keys per tile of the paged attention
 
-// One request of a plan.  A unit is one (kv head, block of 128 query rows); its
-// tiles are key tiles [a0, a0 + n1) (the first tokens that a window keeps) and
-// [b0, b0 + T - n1).
+// One request of a plan.  Its tiles, kv head after kv head, are key tiles [a0, a0 +
+// n1) (the first tokens that a window keeps) and [b0, b0 + T - n1).
 struct PlanReq {
     long long tile_base;  // first of its tiles in the flattened tile space
     int L, n, row0, tree;
     int T, a0, n1, b0;
-    int row_blocks, begin, far_end, b;  // keys before far_end are seen beyond the window
+    int row_blocks, begin, far_end, b;  // blocks of 128 query rows; keys before far_end are seen beyond the window
 };
 static_assert(sizeof(PlanReq) == 56, "eight-byte aligned records");
 
@@ -24,21 +23,21 @@ struct PlanHeader {
     int ticket;  // of paged_plan's CTAs; zero between calls
     int valid;
     int batch, n_q_heads, n_kv_heads, window, n_active;
-    int P;       // CTAs that the tiles are split over
-    long long total;
-    int rows, sink, n_splits, pad[3];
+    int rows, sink, n_splits, pad[6];
 };
 static_assert(sizeof(PlanHeader) == 64, "");
 
-// The tiles [t0, t1) of one attention CTA, and the request that t0 lies in.
+// The tiles [t0, t1) of one attention CTA, for row block rb of the requests that
+// they belong to; req is the one that t0 lies in, idx its place among the records.
 struct PlanCta {
-    long long t0, t1, total;
-    int P, idx;  // idx: the request's place among the records
+    long long t0, t1;
+    int rb, idx;
     PlanReq req;
 };
-static_assert(sizeof(PlanCta) == 88, "eight-byte aligned records");
+static_assert(sizeof(PlanCta) == 80, "eight-byte aligned records");
 
-// A unit that several CTAs share: what joining its partials needs.  rows 0: none.
+// A unit, (request, kv head, row block), that several CTAs share: what joining its
+// partials needs.
 struct PlanSplit {
     int c_lo, nseg;  // its CTAs
     int lo_slot;     // which of c_lo's two partial slots is the unit's (of the others: their first)
@@ -48,9 +47,11 @@ struct PlanSplit {
 static_assert(sizeof(PlanSplit) == 32, "");
 
 constexpr int kMaxPlanCtas = 512;
+constexpr int kMaxGroup = 64;                                   // query heads per kv head
+constexpr int kMaxRowBlocks = kMaxNodes * kMaxGroup / 128;
 
-// header, one PlanCta per attention CTA, as many PlanSplits, then the requests with rows (n_active
-// of them) and one more record whose tile_base is the total
+// header, one PlanCta per attention CTA, as many PlanSplits, then the requests
+// with rows and one more record whose tile_base is the sum of all tiles
 inline size_t plan_bytes_for(int batch)
 {
     return sizeof(PlanHeader) + kMaxPlanCtas * (sizeof(PlanCta) + sizeof(PlanSplit)) + (size_t)(batch + 1) * sizeof(PlanReq);
@@ -66,19 +67,6 @@ __host__ __device__ inline PlanSplit *plan_splits(void *plan)
 __host__ __device__ inline PlanReq *plan_reqs(void *plan)
 {
     return reinterpret_cast<PlanReq *>(plan_splits(plan) + kMaxPlanCtas);
-}
-
-// The first tile of CTA c's range when `total` tiles are split over P CTAs, and
-// the CTA whose range holds tile t.
-__host__ __device__ inline long long plan_split(long long total, int P, int c)
-{
-    const long long q = total / P, r = total % P;
-    return q * c + (c < r ? c : r);
-}
-__host__ __device__ inline int plan_cta_of(long long total, int P, long long t)
-{
-    const long long q = total / P, r = total % P, wide = r * (q + 1);
-    return (int)(t < wide ? t / (q + 1) : r + (t - wide) / q);
 }
 
 // argument checks (treeverify.cu); each returns TB_OK or records the error

@@ -148,7 +148,7 @@ struct Cursor {
         if (end < t1)
             next = reqs[idx + 1];
     }
-    __device__ __forceinline__ void set_end(int Hkv) { end = r.tile_base + (long long)r.T * Hkv * r.row_blocks; }
+    __device__ __forceinline__ void set_end(int Hkv) { end = r.tile_base + (long long)r.T * Hkv; }
     // moves on to the request of tile t
     __device__ __forceinline__ void seek(long long t, int Hkv)
     {
@@ -164,14 +164,14 @@ struct Cursor {
 
 // A run of tiles of one unit.
 struct Seg {
-    int u, j0, n;
+    int head, j0, n;
 };
 __device__ __forceinline__ Seg seg_at(const Cursor &c, long long t)
 {
     Seg g;
     const long long tl = t - c.r.tile_base;
-    g.u = (unsigned long long)tl <= 0xffffffffull ? (int)((uint32_t)tl / (uint32_t)c.r.T) : (int)(tl / c.r.T);
-    g.j0 = (int)(tl - (long long)g.u * c.r.T);
+    g.head = (unsigned long long)tl <= 0xffffffffull ? (int)((uint32_t)tl / (uint32_t)c.r.T) : (int)(tl / c.r.T);
+    g.j0 = (int)(tl - (long long)g.head * c.r.T);
     const long long left = c.t1 - t;
     g.n = left < c.r.T - g.j0 ? (int)left : c.r.T - g.j0;
     return g;
@@ -290,7 +290,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             for (long long t = t0; ok && t < t1;) {
                 cur.seek(t, p.Hkv);
                 const Seg g = seg_at(cur, t);
-                const int head = g.u / cur.r.row_blocks;
                 int id = page_of(g.j0);
                 for (int j = 0; j < g.n; ++j) {
                     const int id_next = j + 1 < g.n ? page_of(g.j0 + j + 1) : 0;
@@ -305,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     if (box)
                         tma_load_4d(ring + (size_t)s * kTile + dst_off, map, &full[s], 64 * a,
                                     p.page_log2 > 7 ? tile_key(g.j0 + j, cur.r.a0, cur.r.n1, cur.r.b0) & page_mask : 0,
-                                    head, id);
+                                    g.head, id);
                     id = id_next;
                     ++issued;
                     if (++s == S) {
@@ -590,9 +589,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             u.T = cur.r.T;
             u.first = t == t0;
             u.r = cur.r;
-            const int rb = g.u % cur.r.row_blocks, head = g.u / cur.r.row_blocks, grow = rb * 128 + rloc;
+            const int grow = s_cta.rb * 128 + rloc;
             u.node = grow / p.group;
-            u.qh = head * p.group + grow % p.group;
+            u.qh = g.head * p.group + grow % p.group;
             u.valid = u.node < cur.r.n && cur.r.row0 + u.node < p.n_rows;
             if (u.valid)
                 u.valid = in_bounds(u.node < kMaxNodes && u.qh < p.Hq && cur.r.row0 >= 0, p.status);
@@ -905,9 +904,12 @@ extern "C" tb_status paged_tree_attention(const tb_bank *bank, const tb_requests
         return record_error(TB_EINVAL, "%s: pages of %d slots, a table of %d", fn, pages->page_size, req->page_size);
     if (layer < 0 || layer >= pages->n_layers)
         return record_error(TB_EINVAL, "%s: layer %d of %d", fn, layer, pages->n_layers);
-    if (n_q_heads < pages->n_kv_heads || n_q_heads % pages->n_kv_heads || n_q_heads > 65535)
+    if (n_q_heads < pages->n_kv_heads || n_q_heads % pages->n_kv_heads)
         return record_error(TB_EINVAL, "%s: n_q_heads %d not a multiple of n_kv_heads %d", fn, n_q_heads,
                             pages->n_kv_heads);
+    if (n_q_heads / pages->n_kv_heads > kMaxGroup)
+        return record_error(TB_EUNSUPPORTED, "%s: %d query heads per kv head (%d supported)", fn,
+                            n_q_heads / pages->n_kv_heads, kMaxGroup);
     if (!(scale > 0.f) || !std::isfinite(scale) || !(softcap >= 0.f) || !std::isfinite(softcap))
         return record_error(TB_EINVAL, "%s: scale %g, softcap %g", fn, scale, softcap);
     if (n_rows < 0)

@@ -8,20 +8,30 @@
 // and the j-th page that b takes is the ring's entry at head + (exclusive sum of
 // take)[b] + j.  Everything follows from exclusive sums over the requests, which
 // each CTA takes for itself (a few thousand values from L2) rather than waiting
-// for another: one launch, no barrier between CTAs.  The rows, the pages that
-// change hands and the records are then shared out over the grid, each by a
-// binary search in the sums.  Taken ids come from the ring's free part and given
-// ones go behind it, so no CTA reads what another writes; `held` and the ring's
-// state, which may be updated in place, are written by the CTA that finishes
-// last (an arrival ticket in the plan).
+// for another: one launch, no barrier between CTAs.  The rows and the pages that
+// change hands are then shared out over the grid, each by a binary search in the
+// sums, while the first CTA makes the attention's split.  Taken ids come from the
+// ring's free part and given ones go behind it, so no CTA reads what another
+// writes; `held` and the ring's state, which may be updated in place, are written by
+// the CTA that finishes last (an arrival ticket in the plan).
+//
+// The attention's split.  Requests are put in order of their row blocks (blocks of
+// 128 query rows per kv head), the most first, and their key tiles behind one
+// another; row block s of all requests that have one is a prefix of that sequence
+// of tiles.  Every CTA takes W tiles of one sequence, so that CTA k of each of
+// them reads the same keys at the same time, once from HBM and then from L2, where
+// row blocks behind one another read them again from HBM.  With one row block
+// (decoding, small trees) the tiles are split evenly.
 #include "paged.cuh"
 
 namespace tv {
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kItems = TB_MAX_REQUESTS / kThreads;
+constexpr int kThreads = 256;
+// Tiles of an attention CTA at least: fewer CTAs on a small problem, but fewer
+// partials to join.  (1: a single request of 64 nodes at 512 keys 14.7 us, with 2
+// 17.2; two kv heads at 4096 keys 18.9 and 17.8.)
 constexpr int kMinTiles = 2;
 
 struct PlanArgs {
@@ -38,8 +48,6 @@ struct PlanArgs {
 };
 
 // Exclusive sums over the block of K values a thread; the totals in `total`.
-static_assert(kMaxPlanCtas <= kThreads, "a split per thread");
-
 template <int K>
 __device__ void block_scan(long long (&v)[K], long long (&total)[K])
 {
@@ -113,258 +121,362 @@ __device__ void tiles_of(PlanReq &q, int window, int sink)
     q.T = q.n1 + (int)((end - 1) / kTileKeys) - q.b0 + 1;
 }
 
-// Bound by latency: 8 requests of 4 to 64 nodes and 1024 requests with 15 000
-// rows differ little, since every chain is a handful of dependent loads (length,
-// tree, page id) and the sums.
+// The first tile of CTA c's range when `total` tiles are split evenly over P CTAs,
+// and the CTA whose range holds tile t.
+__device__ __forceinline__ long long div_up_to(long long a, long long b)
+{
+    return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
+__device__ __forceinline__ long long split_begin(long long total, int P, int c)
+{
+    const long long q = div_up_to(total, P), r = total - q * P;
+    return q * c + (c < r ? c : r);
+}
+__device__ __forceinline__ int split_owner(long long total, int P, long long t)
+{
+    const long long q = div_up_to(total, P), r = total - q * P, wide = r * (q + 1);
+    return (int)(t < wide ? div_up_to(t, q + 1) : r + div_up_to(t - wide, q));
+}
+
+// The requests' sums and sizes in shared memory.
+struct Sums {
+    long long *tile;  // in order of row blocks: tiles before
+    int *row, *take, *give, *need, *held, *len, *n, *tree, *order;
+};
+
+// The attention's work split, by one CTA.
+__device__ void make_split(const PlanArgs &p, const Sums &s, int rows)
+{
+    __shared__ int bins[kMaxRowBlocks + 2], warp_bins[kThreads / 32][kMaxRowBlocks + 2];
+    __shared__ int s_start[kMaxRowBlocks + 1], s_W, s_seqs, s_P;
+    __shared__ long long s_tiles[kMaxRowBlocks];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, B = p.batch, group = p.Hq / p.Hkv;
+    PlanHeader *hd = static_cast<PlanHeader *>(p.plan);
+    PlanReq *out = plan_reqs(p.plan);
+    auto blocks_of = [&](int b) { return (s.n[b] * group + 127) / 128; };
+    // stable counting sort by row blocks, the most first (bin kMaxRowBlocks - blocks; requests
+    // without rows last)
+    for (int x = tid; x < kMaxRowBlocks + 2; x += kThreads)
+        bins[x] = 0;
+    __syncthreads();
+    for (int b = tid; b < B; b += kThreads)
+        atomicAdd(&bins[kMaxRowBlocks - blocks_of(b)], 1);
+    __syncthreads();
+    if (warp == 0) {  // exclusive sums of the bins
+        static_assert(kMaxRowBlocks == 32, "a lane per bin, and the last");
+        const int n = bins[lane];
+        int x = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            x += lane >= o ? y : 0;
+        }
+        bins[lane] = x - n;
+        if (lane == 31)
+            bins[32] = x;
+    }
+    __syncthreads();
+    const int n_active = bins[kMaxRowBlocks];
+    __shared__ int base[kMaxRowBlocks + 1];
+    if (tid <= kMaxRowBlocks)
+        base[tid] = bins[tid];
+    for (int b0 = 0; b0 < B; b0 += kThreads) {
+        for (int x = tid; x < (kThreads / 32) * (kMaxRowBlocks + 2); x += kThreads)
+            (&warp_bins[0][0])[x] = 0;
+        __syncthreads();
+        const int b = b0 + tid, bin = b < B ? kMaxRowBlocks - blocks_of(b) : kMaxRowBlocks + 1;
+        const unsigned same = __match_any_sync(0xffffffffu, bin);
+        const int rank = __popc(same & ((1u << lane) - 1));
+        if (rank == 0)
+            warp_bins[warp][bin] = __popc(same);
+        __syncthreads();
+        if (tid < kMaxRowBlocks) {
+            int at = base[tid];
+            for (int w = 0; w < kThreads / 32; ++w) {
+                const int n = warp_bins[w][tid];
+                warp_bins[w][tid] = at;
+                at += n;
+            }
+            base[tid] = at;
+        }
+        __syncthreads();
+        if (bin < kMaxRowBlocks)
+            s.order[warp_bins[warp][bin] + rank] = b;
+        __syncthreads();
+    }
+
+    // the records in that order, and the tiles before each
+    auto record = [&](int b) {
+        PlanReq q;
+        q.b = b;
+        q.L = s.len[b];
+        q.n = s.n[b];
+        q.tree = s.tree[b];
+        q.row0 = s.row[b];
+        q.row_blocks = blocks_of(b);
+        q.begin = p.key_begin ? min(max(p.key_begin[b], 0), q.L + q.n) : 0;
+        tiles_of(q, p.window, p.sink);
+        return q;
+    };
+    const int items = (n_active + kThreads - 1) / kThreads;
+    long long v[1] = {0}, total[1];
+    for (int i = 0; i < items; ++i)
+        if (tid * items + i < n_active)
+            v[0] += (long long)record(s.order[tid * items + i]).T * p.Hkv;
+    block_scan<1>(v, total);
+    for (int i = 0; i < items; ++i) {
+        const int x = tid * items + i;
+        if (x < n_active) {
+            PlanReq q = record(s.order[x]);
+            q.tile_base = v[0];
+            s.tile[x] = v[0];
+            out[x] = q;
+            v[0] += (long long)q.T * p.Hkv;
+        }
+    }
+    if (tid == 0) {
+        s.tile[n_active] = total[0];
+        PlanReq end = {};
+        end.tile_base = total[0];
+        out[n_active] = end;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        // sequence `lane`: row block `lane` of the requests with more blocks than that
+        const long long mine = s.tile[bins[kMaxRowBlocks - lane]];
+        const int seqs = __popc(__ballot_sync(0xffffffffu, mine > 0));
+        long long all = mine;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1)
+            all += __shfl_xor_sync(0xffffffffu, all, o);
+        // sum over the sequences of ceil(tiles / W) <= all / W + seqs <= P
+        const int W = (int)max((long long)kMinTiles, all > 0 ? div_up_to(all - 1, max(p.P - seqs, 1)) + 1 : 1);
+        const int P1 = (int)min((long long)p.P, max(div_up_to(all + kMinTiles - 1, kMinTiles), 1ll));
+        const int ctas = seqs <= 1 ? (lane == 0 ? P1 : 0) : (int)div_up_to(mine + W - 1, W);
+        int x = ctas;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            x += lane >= o ? y : 0;
+        }
+        s_tiles[lane] = mine;
+        s_start[lane] = x - ctas;
+        if (lane == 31) {
+            s_start[32] = x;
+            s_W = W;
+            s_seqs = seqs;
+            s_P = P1;
+        }
+    }
+    __syncthreads();
+    // the CTAs' ranges, and each unit that a range starts inside, once: at its second CTA
+    PlanCta *ctas = plan_ctas(p.plan);
+    int n_splits = 0;
+    for (int c0 = 0; c0 < p.P; c0 += kThreads) {
+        const int c = c0 + tid;
+        PlanCta x = {};
+        PlanSplit sp = {};
+        if (c < p.P && n_active > 0 && c < s_start[32]) {
+            int q = 0;
+            while (c >= s_start[q + 1])
+                ++q;
+            const bool even = s_seqs <= 1;
+            const long long tiles = s_tiles[q];
+            auto begin_of = [&](int k) { return even ? split_begin(tiles, s_P, k) : min((long long)k * s_W, tiles); };
+            auto owner = [&](long long t) { return even ? split_owner(tiles, s_P, t) : (int)div_up_to(t, s_W); };
+            const int k = c - s_start[q];
+            x.t0 = begin_of(k);
+            x.t1 = begin_of(k + 1);
+            x.rb = q;
+            x.idx = owner_of(s.tile, n_active, x.t0);
+            x.req = out[x.idx];
+            const PlanReq &r = x.req;
+            const int u = (int)div_up_to(x.t0 - r.tile_base, r.T);
+            const long long first = r.tile_base + (long long)u * r.T;
+            if (k > 0 && x.t0 > first && begin_of(k - 1) <= first) {
+                sp.c_lo = c - 1;
+                sp.nseg = owner(first + r.T - 1) - (k - 1) + 1;
+                sp.lo_slot = begin_of(k - 1) == first ? 0 : 1;
+                sp.row0 = r.row0;
+                sp.rb = q;
+                sp.head = u;
+                sp.rows = min(128, r.n * group - q * 128);
+            }
+        }
+        if (c < p.P)
+            ctas[c] = x;
+        long long at[1] = {sp.rows > 0}, n[1];
+        block_scan<1>(at, n);
+        if (sp.rows > 0)
+            plan_splits(p.plan)[n_splits + at[0]] = sp;
+        n_splits += (int)n[0];
+    }
+    if (tid == 0) {
+        hd->valid = 1;
+        hd->batch = B;
+        hd->n_q_heads = p.Hq;
+        hd->n_kv_heads = p.Hkv;
+        hd->window = p.window;
+        hd->sink = p.sink;
+        hd->n_active = n_active;
+        hd->rows = rows;
+        hd->n_splits = n_splits;
+    }
+}
+
+// Bound by latency: every CTA's chain is a handful of dependent loads (length, tree,
+// page id) and the sums; the first CTA's ends with the split.
 __global__ void __launch_bounds__(kThreads) k_paged_plan(const __grid_constant__ PlanArgs p)
 {
     extern __shared__ __align__(16) uint8_t smem[];
-    const int B = p.batch, ld = B + 1;
-    long long *s_tile = reinterpret_cast<long long *>(smem);
-    int *s_row = reinterpret_cast<int *>(s_tile + ld);
-    int *s_take = s_row + ld, *s_give = s_take + ld, *s_need = s_give + ld, *s_held = s_need + ld;
+    const int B = p.batch, ld = B + 1, tid = threadIdx.x;
+    Sums s;
+    s.tile = reinterpret_cast<long long *>(smem);
+    s.row = reinterpret_cast<int *>(s.tile + ld);
+    s.take = s.row + ld;
+    s.give = s.take + ld;
+    s.need = s.give + ld;
+    s.held = s.need + ld;
+    s.len = s.held + ld;
+    s.n = s.len + ld;
+    s.tree = s.n + ld;
+    s.order = s.tree + ld;
     __shared__ int s_last;
     pdl_wait();
     pdl_trigger();
-    const int items = (B + kThreads - 1) / kThreads, b0 = threadIdx.x * items;
-    const bool pool = p.ring != nullptr;
+    const bool pool = p.ring != nullptr, attend = p.Hq > 0, bad_write = blockIdx.x == gridDim.x - 1;
     int head = 0, count = 0;
     if (pool) {
         head = min(max(p.state[0], 0), p.n_pages - 1);
         count = min(max(p.state[1], 0), p.n_pages);
     }
-
-    // the requests of this thread
-    int len[kItems], n[kItems], held[kItems], need[kItems], tree[kItems], bad[kItems];
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        const int b = b0 + i;
-        const bool mine = i < items && b < B;
-        len[i] = mine ? p.lens[b] : 0;
-        tree[i] = mine && p.tree ? p.tree[b] : -1;
-        n[i] = mine && !p.tree ? p.n_new[b] : 0;
-        held[i] = mine && pool ? p.held[b] : 0;
-    }
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        if (tree[i] >= 0 && tree[i] < p.n_trees)
-            n[i] = p.trees[tree[i]].n;
-        const bool ok = len[i] >= 0 && n[i] >= 0 && tree[i] >= -1 && tree[i] < p.n_trees && held[i] >= 0 &&
-                        held[i] <= p.max_pages;
-        const long long want = ok ? ((long long)len[i] + n[i] + (1ll << p.page_log2) - 1) >> p.page_log2 : 0;
-        bad[i] = !ok ? TB_EINVAL : want > p.max_pages ? TB_ECAPACITY : TB_OK;
-        need[i] = (int)want;
-        if (!pool)
-            held[i] = need[i];
-        if (bad[i] != TB_OK) {
-            n[i] = 0;
-            held[i] = min(max(held[i], 0), p.max_pages);
-            need[i] = held[i];
-        }
-    }
-
-    // sums of rows and of pages taken; a request that does not fit gets nothing
-    long long sum[2], total2[2];
-    auto totals = [&] {
-        sum[0] = sum[1] = 0;
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            sum[0] += n[i];
-            sum[1] += max(0, need[i] - held[i]);
-        }
-    };
-    totals();
-    block_scan<2>(sum, total2);
-    if (total2[0] > p.max_rows) {  // the same for every thread
-        long long at = sum[0];
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            at += n[i];
-            if (n[i] > 0 && at > p.max_rows)
-                bad[i] = TB_ECAPACITY, n[i] = 0, need[i] = held[i];
-        }
-        totals();
-        block_scan<2>(sum, total2);
-    }
-    if (total2[1] > count) {
-        long long at = sum[1];
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const int take = max(0, need[i] - held[i]);
-            at += take;
-            if (take > 0 && at > count)
-                bad[i] = TB_ECAPACITY, n[i] = 0, need[i] = held[i];
-        }
-        totals();
-        block_scan<2>(sum, total2);
-    }
-
-    // offsets of rows, pages, records and tiles
-    const int group = p.Hq > 0 ? p.Hq / p.Hkv : 0;
-    auto record = [&](int i) {
-        PlanReq q;
-        q.b = b0 + i;
-        q.L = len[i];
-        q.n = n[i];
-        q.tree = tree[i];
-        q.row_blocks = (n[i] * group + 127) / 128;
-        q.begin = p.key_begin ? min(max(p.key_begin[q.b], 0), len[i] + n[i]) : 0;
-        tiles_of(q, p.window, p.sink);
-        return q;
-    };
-    long long v[3] = {0, 0, 0}, total3[3];
-    const bool attend = group > 0 && p.tree;
-#pragma unroll 1
-    for (int i = 0; i < items; ++i) {
-        v[0] += max(0, held[i] - need[i]);
-        if (n[i] > 0 && attend) {
-            const PlanReq q = record(i);
-            v[1] += 1;
-            v[2] += (long long)q.T * p.Hkv * q.row_blocks;
-        }
-    }
-    block_scan<3>(v, total3);
-    const int rows = (int)total2[0], n_take = (int)total2[1], n_give = (int)total3[0], n_active = (int)total3[1];
-    PlanHeader *hd = static_cast<PlanHeader *>(p.plan);
-    PlanReq *out = plan_reqs(p.plan);
-    const bool first = blockIdx.x == 0;
-    // a CTA has kMinTiles tiles at least: fewer CTAs on a small problem, but whole
-    // units and no partials to merge
-    const int P = (int)min((long long)p.P, max((total3[2] + kMinTiles - 1) / kMinTiles, 1ll));
-#pragma unroll 1
-    for (int i = 0; i < items; ++i) {
-        const int b = b0 + i;
-        if (b >= B)
-            break;
-        s_row[b] = (int)sum[0];
-        s_take[b] = (int)sum[1];
-        s_give[b] = (int)v[0];
-        s_need[b] = need[i];
-        s_held[b] = held[i];
-        if (first) {
-            p.row_start[b] = (int)sum[0];
-            p.status[b] = bad[i];
-            if (n[i] > 0 && attend) {
-                PlanReq q = record(i);
-                q.tile_base = v[2];
-                q.row0 = (int)sum[0];
-                out[v[1]] = q;
-                s_tile[v[1]] = v[2];
-                v[1] += 1;
-                v[2] += (long long)q.T * p.Hkv * q.row_blocks;
-            }
-        }
-        sum[0] += n[i];
-        sum[1] += max(0, need[i] - held[i]);
-        v[0] += max(0, held[i] - need[i]);
-    }
-    if (threadIdx.x == 0) {
-        s_row[B] = rows;
-        s_take[B] = n_take;
-        s_give[B] = n_give;
-        if (first) {
-            s_tile[n_active] = total3[2];
-            p.row_start[B] = rows;
-            PlanReq end = {};
-            end.tile_base = total3[2];
-            out[n_active] = end;
-            hd->valid = attend ? 1 : 0;
-            hd->batch = B;
-            hd->n_q_heads = p.Hq;
-            hd->n_kv_heads = p.Hkv;
-            hd->window = p.window;
-            hd->sink = p.sink;
-            hd->n_active = n_active;
-            hd->P = P;
-            hd->total = total3[2];
-            hd->rows = rows;
-        }
+    for (int b = tid; b < B; b += kThreads) {
+        const int len = p.lens[b], tree = p.tree ? p.tree[b] : -1;
+        int n = p.tree ? 0 : p.n_new[b], held = pool ? p.held[b] : 0;
+        if (tree >= 0 && tree < p.n_trees)
+            n = p.trees[tree].n;
+        const bool ok = len >= 0 && n >= 0 && tree >= -1 && tree < p.n_trees && held >= 0 && held <= p.max_pages;
+        const long long want = ok ? ((long long)len + n + (1ll << p.page_log2) - 1) >> p.page_log2 : 0;
+        const int bad = !ok ? TB_EINVAL : want > p.max_pages ? TB_ECAPACITY : TB_OK;
+        held = pool ? min(max(held, 0), p.max_pages) : bad ? 0 : (int)want;
+        s.len[b] = len;
+        s.tree[b] = tree;
+        s.n[b] = bad ? 0 : n;
+        s.held[b] = held;
+        s.need[b] = bad ? held : (int)want;
+        s.order[b] = bad;  // the status, until the split sorts
     }
     __syncthreads();
-    if (first) {
-        PlanCta *ctas = plan_ctas(p.plan);
-        for (int c = threadIdx.x; c < p.P; c += kThreads) {
-            PlanCta x = {};
-            x.total = total3[2];
-            x.P = P;
-            if (c < P && n_active > 0) {
-                x.t0 = plan_split(total3[2], P, c);
-                x.t1 = plan_split(total3[2], P, c + 1);
-                x.idx = owner_of(s_tile, n_active, x.t0);
-                x.req = out[x.idx];
-            }
-            ctas[c] = x;
-        }
-        // the units that a CTA's range starts inside, each once: at its second CTA
-        PlanSplit sp = {};
-        const int c = threadIdx.x;  // P <= kThreads
-        if (c > 0 && c < P && n_active > 0) {
-            const long long t = plan_split(total3[2], P, c);
-            const PlanReq r = out[owner_of(s_tile, n_active, t)];
-            const long long tl = t - r.tile_base;
-            const int u = (int)(tl / r.T);
-            const long long begin = r.tile_base + (long long)u * r.T;
-            if (t > begin && plan_split(total3[2], P, c - 1) <= begin) {
-                sp.c_lo = c - 1;
-                sp.nseg = plan_cta_of(total3[2], P, begin + r.T - 1) - sp.c_lo + 1;
-                sp.lo_slot = plan_split(total3[2], P, c - 1) == begin ? 0 : 1;
-                sp.row0 = r.row0;
-                sp.rb = u % r.row_blocks;
-                sp.head = u / r.row_blocks;
-                sp.rows = min(128, r.n * group - sp.rb * 128);
-            }
-        }
-        long long v1[1] = {sp.rows > 0}, n_splits[1];
-        block_scan<1>(v1, n_splits);
-        if (sp.rows > 0)
-            plan_splits(p.plan)[v1[0]] = sp;
-        if (threadIdx.x == 0)
-            hd->n_splits = (int)n_splits[0];
-    }
 
-    // the rows
-    const int stride = gridDim.x * kThreads, tid = blockIdx.x * kThreads + threadIdx.x;
-    const int ring_n = p.n_pages;
-    for (int r = tid; r < p.max_rows; r += stride) {
-        int64_t slot = -1;
-        int pos = 0;
-        if (r < rows) {
-            const int b = owner_of(s_row, B, r), i = r - s_row[b];
-            const int L = p.lens[b], s = L + i, pg = s >> p.page_log2;
-            int id;
-            if (pg < s_held[b]) {
-                id = p.table[(size_t)b * p.max_pages + pg];
-            } else {
-                int at = head + s_take[b] + pg - s_held[b];
-                at -= at >= ring_n ? ring_n : 0;
-                id = p.ring[at];
-            }
-            if (id >= 0)
-                slot = ((int64_t)id << p.page_log2) + (s & ((1 << p.page_log2) - 1));
-            pos = L + (p.tree ? p.trees[p.tree[b]].depth[i] : i);
+    // sums of rows, of pages taken and given; a request that does not fit gets nothing
+    const int items = (B + kThreads - 1) / kThreads, b0 = min(tid * items, B), b1 = min(b0 + items, B);
+    long long v[3], total[3];
+    auto sum = [&] {
+        v[0] = v[1] = v[2] = 0;
+        for (int b = b0; b < b1; ++b) {
+            v[0] += s.n[b];
+            v[1] += max(0, s.need[b] - s.held[b]);
+            v[2] += max(0, s.held[b] - s.need[b]);
         }
-        p.slots[r] = slot;
-        p.positions[r] = pos;
+        block_scan<3>(v, total);
+    };
+    auto refuse = [&](int b) {
+        s.order[b] = TB_ECAPACITY;
+        s.n[b] = 0;
+        s.need[b] = s.held[b];
+    };
+    sum();
+    if (total[0] > p.max_rows) {  // the same for every thread
+        long long at = v[0];
+        for (int b = b0; b < b1; ++b) {
+            at += s.n[b];
+            if (s.n[b] > 0 && at > p.max_rows)
+                refuse(b);
+        }
+        sum();
     }
-    // the pages that change hands
-    for (int x = tid; x < n_take; x += stride) {
-        const int b = owner_of(s_take, B, x);
-        int at = head + x;
-        at -= at >= ring_n ? ring_n : 0;
-        const int pg = s_held[b] + x - s_take[b];
-        if (in_bounds(pg < p.max_pages && at < ring_n, nullptr))
-            p.table[(size_t)b * p.max_pages + pg] = p.ring[at];
+    if (total[1] > count) {
+        long long at = v[1];
+        for (int b = b0; b < b1; ++b) {
+            const int take = max(0, s.need[b] - s.held[b]);
+            at += take;
+            if (take > 0 && at > count)
+                refuse(b);
+        }
+        sum();
     }
-    for (int x = tid; x < n_give; x += stride) {
-        const int b = owner_of(s_give, B, x);
-        const int at = (int)(((long long)head + count + x) % ring_n);
-        p.ring[at] = p.table[(size_t)b * p.max_pages + s_need[b] + x - s_give[b]];
+    const int rows = (int)total[0], n_take = (int)total[1], n_give = (int)total[2];
+    for (int b = b0; b < b1; ++b) {
+        s.row[b] = (int)v[0];
+        s.take[b] = (int)v[1];
+        s.give[b] = (int)v[2];
+        v[0] += s.n[b];
+        v[1] += max(0, s.need[b] - s.held[b]);
+        v[2] += max(0, s.held[b] - s.need[b]);
+        if (bad_write)
+            p.status[b] = s.order[b];
+    }
+    if (tid == 0) {
+        s.row[B] = rows;
+        s.take[B] = n_take;
+        s.give[B] = n_give;
+    }
+    __syncthreads();
+    PlanHeader *hd = static_cast<PlanHeader *>(p.plan);
+    if (bad_write) {
+        for (int b = tid; b <= B; b += kThreads)
+            p.row_start[b] = s.row[b];
+        if (!attend && tid == 0)
+            hd->valid = 0;
+    }
+    if (attend && blockIdx.x == 0) {
+        make_split(p, s, rows);
+    } else {
+        // the rows
+        const int ctas = gridDim.x - (attend ? 1 : 0), stride = ctas * kThreads;
+        const int from = (blockIdx.x - (attend ? 1 : 0)) * kThreads + tid;
+        const int ring_n = p.n_pages;
+        for (int r = from; r < p.max_rows; r += stride) {
+            int64_t slot = -1;
+            int pos = 0;
+            if (r < rows) {
+                const int b = owner_of(s.row, B, r), i = r - s.row[b];
+                const int at = s.len[b] + i, pg = at >> p.page_log2;
+                int id;
+                if (pg < s.held[b]) {
+                    id = p.table[(size_t)b * p.max_pages + pg];
+                } else {
+                    int x = head + s.take[b] + pg - s.held[b];
+                    x -= x >= ring_n ? ring_n : 0;
+                    id = p.ring[x];
+                }
+                if (id >= 0)
+                    slot = ((int64_t)id << p.page_log2) + (at & ((1 << p.page_log2) - 1));
+                pos = s.len[b] + (p.tree ? p.trees[s.tree[b]].depth[i] : i);
+            }
+            p.slots[r] = slot;
+            p.positions[r] = pos;
+        }
+        // the pages that change hands
+        for (int x = from; x < n_take; x += stride) {
+            const int b = owner_of(s.take, B, x);
+            int at = head + x;
+            at -= at >= ring_n ? ring_n : 0;
+            const int pg = s.held[b] + x - s.take[b];
+            if (in_bounds(pg < p.max_pages && at < ring_n, nullptr))
+                p.table[(size_t)b * p.max_pages + pg] = p.ring[at];
+        }
+        for (int x = from; x < n_give; x += stride) {
+            const int b = owner_of(s.give, B, x);
+            const int at = (int)(((long long)head + count + x) % ring_n);
+            p.ring[at] = p.table[(size_t)b * p.max_pages + s.need[b] + x - s.give[b]];
+        }
     }
     if (!pool)
         return;
     // every CTA has read `held` and the state by the time the last one arrives
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (tid == 0) {
         bool last = true;
         if (gridDim.x > 1) {
             __threadfence();
@@ -377,10 +489,10 @@ __global__ void __launch_bounds__(kThreads) k_paged_plan(const __grid_constant__
     __syncthreads();
     if (!s_last)
         return;
-    for (int b = threadIdx.x; b < B; b += kThreads)
-        p.held_out[b] = s_need[b];
-    if (threadIdx.x == 0) {
-        p.state_out[0] = (int)(((long long)head + n_take) % ring_n);
+    for (int b = tid; b < B; b += kThreads)
+        p.held_out[b] = s.need[b];
+    if (tid == 0) {
+        p.state_out[0] = (int)(((long long)head + n_take) % p.n_pages);
         p.state_out[1] = count - n_take + n_give;
     }
 }
@@ -425,8 +537,11 @@ extern "C" tb_status paged_plan(const tb_bank *bank, const tb_requests *req, con
     }
     if (!slots || !positions || !status || max_rows < 1)
         return record_error(TB_EINVAL, "%s: slots, positions or status is NULL, or max_rows %d < 1", fn, max_rows);
-    if (n_q_heads < 0 || (n_q_heads > 0 && (n_kv_heads < 1 || n_q_heads % n_kv_heads || n_q_heads > 65536)))
+    if (n_q_heads < 0 || (n_q_heads > 0 && (n_kv_heads < 1 || n_q_heads % n_kv_heads)))
         return record_error(TB_EINVAL, "%s: n_q_heads %d not a multiple of n_kv_heads %d", fn, n_q_heads, n_kv_heads);
+    if (n_q_heads > 0 && n_q_heads / n_kv_heads > kMaxGroup)
+        return record_error(TB_EUNSUPPORTED, "%s: %d query heads per kv head (%d supported)", fn,
+                            n_q_heads / n_kv_heads, kMaxGroup);
     if (n_q_heads > 0 && !req->tree)
         return record_error(TB_EINVAL, "%s: an attention plan is for trees", fn);
     if (window < 0 || sink < 0)
@@ -466,10 +581,10 @@ extern "C" tb_status paged_plan(const tb_bank *bank, const tb_requests *req, con
     a.sink = sink;
     a.P = n_sm < kMaxPlanCtas ? n_sm : kMaxPlanCtas;  // the grid of the attention
     a.plan = plan;
-    // a CTA for every 512 rows: more of them repeat the sums for nothing
-    const long long ctas = ((long long)max_rows + 2ll * req->batch + kThreads - 1) / kThreads;
-    const int grid = (int)(ctas < 1 ? 1 : ctas > n_sm ? n_sm : ctas);
-    const size_t smem = (size_t)(req->batch + 1) * (sizeof(long long) + 5 * sizeof(int));
+    // a CTA for every 512 rows (more of them repeat the sums for nothing), and one for the split
+    const long long ctas = ((long long)max_rows + 2ll * req->batch + 511) / 512;
+    const int grid = (int)(ctas < 1 ? 1 : ctas > n_sm ? n_sm : ctas) + (n_q_heads > 0 ? 1 : 0);
+    const size_t smem = (size_t)(req->batch + 1) * (sizeof(long long) + 9 * sizeof(int));
     cudaError_t e = allow_max_smem((const void *)k_paged_plan);
     if (e == cudaSuccess)
         e = launch_kernel(k_paged_plan, dim3(grid), dim3(kThreads), smem, (cudaStream_t)stream, true, a);
