@@ -106,11 +106,47 @@ __device__ __forceinline__ float rcp_approx(float x)
     return y;
 }
 
-// cap tanh(scale s / cap) in units of ln 2: tanh y = 1 - 2 / (1 + e^(2y)), with the
-// right limits where the exponential overflows or vanishes
-__device__ __forceinline__ float capped(float s, float cap, float cap_in)
+// Two 32-bit floats in one instruction (the softmax is bound by its issue slots).
+__device__ __forceinline__ uint64_t two(float lo, float hi)
 {
-    return fmaf(-2.f * cap, rcp_approx(1.f + ex2_approx(s * cap_in)), cap);
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 halves(uint64_t v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul_two(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// cap tanh(scale s / cap) of two scores in units of ln 2: tanh y = 1 - 2 / (1 + e^(2y)),
+// with the right limits where the exponential overflows or vanishes.  (An odd
+// polynomial for small arguments in place of the two special functions took longer:
+// 128 us for 111, two row blocks over 65536 keys.)
+__device__ __forceinline__ float2 capped(float s0, float s1, float cap, float cap_in)
+{
+    const float2 e = halves(mul_two(two(s0, s1), two(cap_in, cap_in)));
+    const float2 d = halves(add_two(two(ex2_approx(e.x), ex2_approx(e.y)), two(1.f, 1.f)));
+    return halves(fma_two(two(rcp_approx(d.x), rcp_approx(d.y)), two(-2.f * cap, -2.f * cap), two(cap, cap)));
 }
 
 // The bits of [lo, hi) relative to s0, of 32.
@@ -433,8 +469,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 if constexpr (kForm != kPlain) {
                     if (kForm == kCap || p.cap > 0.f) {
 #pragma unroll
-                        for (int x = 0; x < kHalf; ++x)
-                            r[x] = __float_as_uint(capped(__uint_as_float(r[x]), p.cap, p.cap_in));
+                        for (int x = 0; x < kHalf; x += 2) {
+                            const float2 z = capped(__uint_as_float(r[x]), __uint_as_float(r[x + 1]), p.cap, p.cap_in);
+                            r[x] = __float_as_uint(z.x), r[x + 1] = __float_as_uint(z.y);
+                        }
                     } else {
 #pragma unroll
                         for (int x = 0; x < kHalf; ++x)
@@ -466,9 +504,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     }
                 } else if constexpr (kForm == kBias) {
                     const float d0 = (float)(pos - h0);
+                    uint64_t dist = two(d0, d0 - 1.f);
 #pragma unroll
-                    for (int x = 0; x < kHalf; ++x)
-                        r[x] = __float_as_uint(fmaf(-slope, d0 - (float)x, __uint_as_float(r[x])));
+                    for (int x = 0; x < kHalf; x += 2) {
+                        const float2 z = halves(fma_two(two(-slope, -slope), dist,
+                                                        two(__uint_as_float(r[x]), __uint_as_float(r[x + 1]))));
+                        r[x] = __float_as_uint(z.x), r[x + 1] = __float_as_uint(z.y);
+                        dist = add_two(dist, two(-2.f, -2.f));
+                    }
                 }
                 float mx = -INFINITY;
 #pragma unroll
@@ -522,16 +565,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 // P in the pages' type on the first columns of this half, its 32-bit sum into l
                 const float mu = m_ref == -INFINITY ? 0.f : m_ref;
                 const float f = kForm == kPlain ? p.scale : 1.f;
-                float rs = 0.f;
+                uint64_t rs = two(0.f, 0.f);
 #pragma unroll
                 for (int x = 0; x < kHalf / 2; ++x) {
-                    const float p0 = ex2_approx(fmaf(__uint_as_float(r[2 * x]), f, -mu));
-                    const float p1 = ex2_approx(fmaf(__uint_as_float(r[2 * x + 1]), f, -mu));
-                    rs += p0 + p1;
+                    const float2 z = halves(fma_two(two(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), two(f, f),
+                                                    two(-mu, -mu)));
+                    const float p0 = ex2_approx(z.x), p1 = ex2_approx(z.y);
+                    rs = add_two(rs, two(p0, p1));
                     r[x] = pack<kF16>(p0, p1);
                 }
                 tmem_st_32x32b_x32(sa, r);
-                l += rs;
+                l += halves(rs).x + halves(rs).y;
                 if (key0 + kBN > end || key0 < si.lo_min) {
                     // V rows that nobody sees may hold anything: zeros, once the tile has landed
                     const int sv = (int)(it % kVStages);
@@ -757,96 +801,98 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
 }
 
 // Log-sum-exp join of the partials of the units that CTAs share, in CTA order (the
-// same sums every time), a warp per row: warp w takes row w % 2^rows_log2 of split w
-// / 2^rows_log2, and so on.  Bound by its round trips (the split; the row's maxima,
-// sums and first partials together), so every row has a warp of its own: with two
-// rows per warp, and the splits found here instead of in the plan, it took 6.5 us
-// behind the attention of one 64-node layer at 16384 keys, 8.5 behind the ragged
-// batch's.  (Joined by the last CTA of a unit instead, without this launch, the one
-// SM needed 10 us for 64 rows of six partials.)
+// same sums every time).  A group of 8 lanes takes a row, kD / 8 columns each:
+// group w row w % 2^rows_log2 of split w / 2^rows_log2, and so on.  Bound by its round
+// trips (the split; the row's maxima, sums and first four partials together), so
+// all rows are under way at once.  Joined by the last CTA of a unit instead,
+// without this launch, the one SM needed 10 us for 64 rows of six partials.
 template <int kD, bool kF16>
-__global__ void __launch_bounds__(256, 4) k_paged_merge(const __grid_constant__ PagedArgs p, int rows_log2)
+__global__ void __launch_bounds__(256, 2) k_paged_merge(const __grid_constant__ PagedArgs p, int rows_log2)
 {
-    constexpr int kSlot = slot_floats(kD), kCols = kD / 32, kAhead = 4;
+    constexpr int kSlot = slot_floats(kD), kVec = kD / 32, kAhead = 4;  // kVec: float4s of a lane
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31;
-    int item = (blockIdx.x * 256 + threadIdx.x) >> 5;
+    const int lane = threadIdx.x & 31, sub = lane & 7;
     const PlanHeader *hd = static_cast<const PlanHeader *>(p.plan);
+    int item = (blockIdx.x * 256 + threadIdx.x) >> 3;
     auto split_at = [&](int i) { return plan_splits(p.plan)[min(i >> rows_log2, kMaxPlanCtas - 1)]; };
     PlanSplit s, next = split_at(item);
-    const int items = hd->n_splits << rows_log2, stride = gridDim.x * 8;
+    const int items = hd->n_splits << rows_log2, stride = gridDim.x * 32;
     if (!hd->valid || hd->batch != p.batch || hd->n_q_heads != p.Hq || hd->n_kv_heads != p.Hkv)
         return;
-    for (; item < items; item += stride) {
+    for (; __any_sync(0xffffffffu, item < items); item += stride) {
         s = next;
         if (item + stride < items)
             next = split_at(item + stride);
-        const int x = item & ((1 << rows_log2) - 1);
+        int x = item & ((1 << rows_log2) - 1);
         const int grow = s.rb * 128 + x, node = grow / p.group, qh = s.head * p.group + grow % p.group;
-        if (x >= s.rows || s.row0 + node >= p.n_rows || !in_bounds(qh < p.Hq && s.c_lo >= 0, p.status))
+        const bool live = item < items && x < s.rows && s.row0 + node < p.n_rows && in_bounds(qh < p.Hq && s.c_lo >= 0, p.status);
+        if (!__any_sync(0xffffffffu, live))
             continue;
-        const float *first = p.part + ((size_t)s.c_lo * 2 + s.lo_slot) * kSlot;
-        const float *rest = p.part + (size_t)s.c_lo * 2 * kSlot;  // CTA k > 0: + 2 k slots
-        float M = -INFINITY, sum = 0.f, acc[kCols] = {};
-        for (int k0 = 0; k0 < s.nseg; k0 += 32) {
-            // lane k has the k-th CTA's maximum and sum
-            const bool have = k0 + lane < s.nseg;
-            const float *sl = k0 + lane == 0 ? first : rest + (size_t)(have ? k0 + lane : 1) * 2 * kSlot;
-            const float ms = have ? __ldcg(sl + 128 * kD + x) : -INFINITY;
-            const float ls = have ? __ldcg(sl + 128 * kD + 128 + x) : 0.f;
-            const int cnt = min(32, s.nseg - k0);
+        const int nseg = live ? s.nseg : 0;
+        const float *rest = p.part + (live ? (size_t)s.c_lo * 2 * kSlot : 0);  // CTA k > 0: + 2 k slots
+        const float *first = rest + (live ? s.lo_slot * kSlot : 0);
+        float M = -INFINITY, sum = 0.f;
+        float4 acc[kVec] = {};
+        for (int k0 = 0; __any_sync(0xffffffffu, k0 < nseg); k0 += 8) {
+            // lane k of the group has the (k0 + k)-th CTA's maximum and sum
+            const int k = k0 + sub;
+            const float *sl = k == 0 ? first : rest + (size_t)(k < nseg ? k : 0) * 2 * kSlot;
+            const float ms = k < nseg ? __ldcg(sl + 128 * kD + x) : -INFINITY;
+            const float ls = k < nseg ? __ldcg(sl + 128 * kD + 128 + x) : 0.f;
             float w = 0.f;
-            for (int k = 0; k < cnt; k += kAhead) {
-                float v[kAhead][kCols];
+            for (int z = 0; z < 8; z += kAhead) {
+                if (!__any_sync(0xffffffffu, k0 + z < nseg))
+                    break;
+                float4 v[kAhead][kVec];
 #pragma unroll
-                for (int z = 0; z < kAhead; ++z) {
-                    const int c = k0 + min(k + z, cnt - 1);
-                    const float *from = (c == 0 ? first : rest + (size_t)c * 2 * kSlot) + x * kD;
-                    if constexpr (kCols == 4) {
-                        const float4 f = __ldcg(reinterpret_cast<const float4 *>(from) + lane);
-                        v[z][0] = f.x, v[z][1] = f.y, v[z][2] = f.z, v[z][3] = f.w;
-                    } else {
-                        const float2 f = __ldcg(reinterpret_cast<const float2 *>(from) + lane);
-                        v[z][0] = f.x, v[z][1] = f.y;
-                    }
+                for (int y = 0; y < kAhead; ++y) {
+                    const int c = k0 + z + y;
+                    const float4 *from = reinterpret_cast<const float4 *>((c == 0 ? first : rest + (size_t)c * 2 * kSlot) + x * kD);
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i)
+                        v[y][i] = c < nseg ? __ldcg(from + sub + 8 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
-                if (k == 0) {
+                if (z == 0) {
                     float m2 = ms;
 #pragma unroll
-                    for (int o = 16; o >= 1; o >>= 1)
+                    for (int o = 4; o >= 1; o >>= 1)
                         m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, o));
                     m2 = fmaxf(m2, M);
                     const float keep = M == -INFINITY ? 0.f : ex2_approx(M - m2);
                     w = ms == -INFINITY ? 0.f : ex2_approx(ms - m2);
                     float ws = w * ls;
 #pragma unroll
-                    for (int o = 16; o >= 1; o >>= 1)
+                    for (int o = 4; o >= 1; o >>= 1)
                         ws += __shfl_xor_sync(0xffffffffu, ws, o);
                     M = m2;
                     sum = sum * keep + ws;
 #pragma unroll
-                    for (int i = 0; i < kCols; ++i)
-                        acc[i] *= keep;
+                    for (int i = 0; i < kVec; ++i)
+                        acc[i].x *= keep, acc[i].y *= keep, acc[i].z *= keep, acc[i].w *= keep;
                 }
 #pragma unroll
-                for (int z = 0; z < kAhead; ++z) {
-                    const float wk = k + z < cnt ? __shfl_sync(0xffffffffu, w, (k + z) & 31) : 0.f;
+                for (int y = 0; y < kAhead; ++y) {
+                    const float f = __shfl_sync(0xffffffffu, w, z + y, 8);
 #pragma unroll
-                    for (int i = 0; i < kCols; ++i)
-                        acc[i] += k + z < cnt ? wk * v[z][i] : 0.f;
+                    for (int i = 0; i < kVec; ++i) {
+                        acc[i].x = fmaf(f, v[y][i].x, acc[i].x);
+                        acc[i].y = fmaf(f, v[y][i].y, acc[i].y);
+                        acc[i].z = fmaf(f, v[y][i].z, acc[i].z);
+                        acc[i].w = fmaf(f, v[y][i].w, acc[i].w);
+                    }
                 }
             }
         }
+        if (!live)
+            continue;
         const float inv = sum > 0.f ? 1.f / sum : 0.f;
         const size_t row = (size_t)(s.row0 + node) * p.Hq + qh;
-        uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + row * kD) + lane * (kCols / 2);
-        if constexpr (kCols == 4)
-            *reinterpret_cast<uint2 *>(dst) =
-                make_uint2(pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv));
-        else
-            *dst = pack<kF16>(acc[0] * inv, acc[1] * inv);
-        if (p.lse && lane == 0)
+        uint2 *dst = reinterpret_cast<uint2 *>(p.out + row * kD) + sub;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            dst[8 * i] = make_uint2(pack<kF16>(acc[i].x * inv, acc[i].y * inv), pack<kF16>(acc[i].z * inv, acc[i].w * inv));
+        if (p.lse && sub == 0)
             p.lse[row] = sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
     }
 }
@@ -864,9 +910,9 @@ cudaError_t launch(const PagedArgs &a, int n_sm, int max_rows, cudaStream_t stre
     int rows_log2 = 0;
     while ((1 << rows_log2) < max_rows)
         ++rows_log2;
-    const long long warps = (long long)(n_sm - 1) << rows_log2;  // a row of each possible split
-    const int blocks = (int)((warps + 7) / 8);
-    return launch_kernel(k_paged_merge<kD, kF16>, dim3(blocks < 4 * n_sm ? blocks : 4 * n_sm), dim3(256), 0, stream, true,
+    const long long rows = (long long)(n_sm - 1) << rows_log2;  // of every possible split
+    const int blocks = (int)((rows + 31) / 32);
+    return launch_kernel(k_paged_merge<kD, kF16>, dim3(blocks < 2 * n_sm ? blocks : 2 * n_sm), dim3(256), 0, stream, true,
                          a, rows_log2);
 }
 
