@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kCluster = 8;
-constexpr int kAhead = 4;  // moves in flight per thread
+constexpr int kAhead = 2, kPieces = 4;  // moves in flight per thread: kAhead of each of kPieces
 
 struct AcceptArgs {
     const TreeDesc *trees;
@@ -152,29 +152,40 @@ __global__ void __launch_bounds__(kThreads) k_paged_accept(const __grid_constant
     }
     if (!p.k || a.len < 2)
         return;
-    // pieces: 16 bytes of one (layer, kv head, K or V)
-    const int per_head = p.d >> 3;
-    const long long pieces = 2ll * p.n_layers * p.Hkv * per_head;
-    for (long long x = rank * kThreads + threadIdx.x; x < pieces; x += kCluster * kThreads) {
-        const int c = (int)(x % per_head);
-        const long long y = x / per_head;
-        const int g = (int)(y % p.Hkv);
-        const int lv = (int)(y / p.Hkv);
-        uint16_t *base = ((lv & 1) ? p.v : p.k) + (lv >> 1) * p.layer_stride + g * p.head_stride + 8 * c;
+    // pieces: 16 bytes of one (layer, kv head, K or V), several per thread in flight
+    const int per_head_log2 = p.d == 64 ? 3 : 4;
+    const unsigned pieces = 2u * p.n_layers * p.Hkv << per_head_log2;  // < 2^30 (the host's check)
+    constexpr unsigned kStride = kCluster * kThreads;
+    for (unsigned x0 = rank * kThreads + threadIdx.x; x0 < pieces; x0 += kPieces * kStride) {
+        uint16_t *base[kPieces];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const unsigned x = x0 + i * kStride, c = x & ((1u << per_head_log2) - 1), y = x >> per_head_log2;
+            const unsigned lv = y / (unsigned)p.Hkv, g = y - lv * (unsigned)p.Hkv;
+            base[i] = x < pieces ? ((lv & 1) ? p.v : p.k) + (lv >> 1) * p.layer_stride + g * p.head_stride + 8 * c : nullptr;
+        }
         for (int j0 = 1; j0 < a.len; j0 += kAhead) {
-            uint4 buf[kAhead];
-            bool move[kAhead];
+            uint4 buf[kPieces][kAhead];
+            long long src[kAhead], at[kAhead];
 #pragma unroll
             for (int m = 0; m < kAhead; ++m) {
                 const int j = j0 + m;
-                move[m] = j < a.len && a.src[j] >= 0 && a.at[j] >= 0;
-                if (move[m])
-                    buf[m] = *reinterpret_cast<const uint4 *>(base + a.src[j]);
+                const bool move = j < a.len && a.src[j] >= 0 && a.at[j] >= 0;
+                src[m] = move ? a.src[j] : -1;
+                at[m] = move ? a.at[j] : -1;
             }
 #pragma unroll
-            for (int m = 0; m < kAhead; ++m)
-                if (move[m])
-                    *reinterpret_cast<uint4 *>(base + a.at[j0 + m]) = buf[m];
+            for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                for (int m = 0; m < kAhead; ++m)
+                    if (src[m] >= 0 && base[i])
+                        buf[i][m] = *reinterpret_cast<const uint4 *>(base[i] + src[m]);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                for (int m = 0; m < kAhead; ++m)
+                    if (at[m] >= 0 && base[i])
+                        *reinterpret_cast<uint4 *>(base[i] + at[m]) = buf[i][m];
         }
     }
 }
@@ -210,6 +221,8 @@ extern "C" tb_status paged_accept(const tb_bank *bank, const tb_requests *req, c
         if (pages->page_size != req->page_size)
             return record_error(TB_EINVAL, "%s: pages of %d slots, a table of %d", fn, pages->page_size,
                                 req->page_size);
+        if ((long long)pages->n_layers * pages->n_kv_heads > 1 << 24)
+            return record_error(TB_EUNSUPPORTED, "%s: %d layers of %d kv heads", fn, pages->n_layers, pages->n_kv_heads);
         a.k = static_cast<uint16_t *>(pages->k);
         a.v = static_cast<uint16_t *>(pages->v);
         a.layer_stride = pages->layer_stride;
