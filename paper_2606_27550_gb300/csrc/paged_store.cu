@@ -93,48 +93,65 @@ __global__ void __launch_bounds__(kThreads) k_paged_store(const __grid_constant_
         }
     }
     __syncthreads();
-    // items: a 16-byte piece of the lower half of a head and its partner; queries, keys, values
+    // items: a 16-byte piece of the lower half of a head and its partner; queries, keys,
+    // values; kAhead of them in flight per thread
+    constexpr int kAhead = 2;
     const int pc_log2 = half_log2 - 3, heads = p.Hq + 2 * p.Hkv;
-    const int per_row = heads << pc_log2;
-    for (int x = threadIdx.x; x < n_rows * per_row; x += kThreads) {
-        const int r = x / per_row, y = x - r * per_row;
-        int h = y >> pc_log2;
-        const int c = (y & ((1 << pc_log2) - 1)) * 8;
-        const long long row = r0 + r;
-        const uint16_t *src;
-        uint16_t *dst;
-        bool turn = kRope;
-        if (h < p.Hq) {
-            src = p.q.p + row * p.q.row_stride + h * p.q.head_stride;
-            dst = p.q_out.p + row * p.q_out.row_stride + h * p.q_out.head_stride;
-        } else {
-            h -= p.Hq;
-            const bool is_v = h >= p.Hkv;
-            h -= is_v ? p.Hkv : 0;
-            const long long slot = s_slot[r], page = slot >> p.page_log2;
-            if (slot < 0 || page >= p.n_pages)
-                continue;  // padding
-            const Rows &in = is_v ? p.v : p.k;
-            src = in.p + row * in.row_stride + h * in.head_stride;
-            dst = (is_v ? p.v_pages : p.k_pages) + page * p.page_stride + h * p.head_stride +
-                  (slot & ((1 << p.page_log2) - 1)) * p.slot_stride;
-            turn = kRope && !is_v;
-        }
-        uint4 lo = *reinterpret_cast<const uint4 *>(src + c);
-        uint4 hi = *reinterpret_cast<const uint4 *>(src + c + half);
-        if (turn) {
-            uint32_t *a = &lo.x, *b = &hi.x;
-            const float2 *cs = &s_cs[r][c];
+    const unsigned per_row = (unsigned)heads << pc_log2, items = n_rows * per_row;
+    for (unsigned x0 = threadIdx.x; x0 < items; x0 += kAhead * kThreads) {
+        uint4 lo[kAhead], hi[kAhead];
+        uint16_t *dst[kAhead];
+        const float2 *turn[kAhead];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 t0 = cs[2 * e], t1 = cs[2 * e + 1];
-                const float2 u = unpack<kF16>(a[e]), w = unpack<kF16>(b[e]);
-                a[e] = pack<kF16>(u.x * t0.x - w.x * t0.y, u.y * t1.x - w.y * t1.y);
-                b[e] = pack<kF16>(w.x * t0.x + u.x * t0.y, w.y * t1.x + u.y * t1.y);
+        for (int m = 0; m < kAhead; ++m) {
+            const unsigned x = x0 + m * kThreads;
+            dst[m] = nullptr;
+            turn[m] = nullptr;
+            if (x >= items)
+                continue;
+            const unsigned r = x / per_row, y = x - r * per_row;
+            int h = (int)(y >> pc_log2);
+            const int c = (int)(y & ((1u << pc_log2) - 1)) * 8;
+            const long long row = r0 + r;
+            const uint16_t *src;
+            if (h < p.Hq) {
+                src = p.q.p + row * p.q.row_stride + h * p.q.head_stride;
+                dst[m] = p.q_out.p + row * p.q_out.row_stride + h * p.q_out.head_stride + c;
+                turn[m] = &s_cs[r][c];
+            } else {
+                h -= p.Hq;
+                const bool is_v = h >= p.Hkv;
+                h -= is_v ? p.Hkv : 0;
+                const long long slot = s_slot[r], page = slot >> p.page_log2;
+                if (slot < 0 || page >= p.n_pages)
+                    continue;  // padding
+                const Rows &in = is_v ? p.v : p.k;
+                src = in.p + row * in.row_stride + h * in.head_stride;
+                dst[m] = (is_v ? p.v_pages : p.k_pages) + page * p.page_stride + h * p.head_stride +
+                         (slot & ((1 << p.page_log2) - 1)) * p.slot_stride + c;
+                turn[m] = is_v ? nullptr : &s_cs[r][c];
             }
+            lo[m] = *reinterpret_cast<const uint4 *>(src + c);
+            hi[m] = *reinterpret_cast<const uint4 *>(src + c + half);
         }
-        *reinterpret_cast<uint4 *>(dst + c) = lo;
-        *reinterpret_cast<uint4 *>(dst + c + half) = hi;
+#pragma unroll
+        for (int m = 0; m < kAhead; ++m) {
+            if (!dst[m])
+                continue;
+            if (kRope && turn[m]) {
+                uint32_t *a = &lo[m].x, *b = &hi[m].x;
+                const float2 *cs = turn[m];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 t0 = cs[2 * e], t1 = cs[2 * e + 1];
+                    const float2 u = unpack<kF16>(a[e]), w = unpack<kF16>(b[e]);
+                    a[e] = pack<kF16>(u.x * t0.x - w.x * t0.y, u.y * t1.x - w.y * t1.y);
+                    b[e] = pack<kF16>(w.x * t0.x + u.x * t0.y, w.y * t1.x + u.y * t1.y);
+                }
+            }
+            *reinterpret_cast<uint4 *>(dst[m]) = lo[m];
+            *reinterpret_cast<uint4 *>(dst[m] + half) = hi[m];
+        }
     }
 }
 
