@@ -1,0 +1,168 @@
+"""The example's decode loop over a paged cache, step by step against the
+contiguous calls of the library and the 64-bit references."""
+import os
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paged_reference as ref
+import paper_2606_27550_gb300 as tv
+from paper_2606_27550_gb300 import synth
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+
+pytestmark = pytest.mark.gpu
+
+
+def cached(server, layer, b, n):
+    """K and V of the first n slots of request b, [n][heads][d], as stored."""
+    slot = torch.arange(n, device="cuda")
+    page = server.req.table[b].long()[slot // server.req.page_size]
+    at = slot % server.req.page_size
+    return [p[layer].transpose(1, 2)[page, at] for p in (server.pages.k, server.pages.v)]
+
+
+def test_decode_loop():
+    import paged_serving as ex
+
+    server = ex.Server(ex.Model())
+    m = server.m
+    server.admit({b: list(range(5 * b + 2, 5 * b + 2 + n)) for b, n in enumerate((5, 40, 17, 100))})
+    assert server.req.lens.tolist() == [4, 39, 16, 99] and server.status.tolist() == [0] * 4
+    accepted = 0
+    for step in range(6):
+        trees = [(b + step) % 3 for b in range(server.B)]
+        if step >= 3:
+            trees[2] = -1
+        if step == 3:
+            server.finish(2)
+        draft = ex.drafts(server, trees)
+        before, said = server.req.lens.tolist(), server.said.tolist()
+        old = {b: [cached(server, layer, b, before[b]) for layer in range(m.layers)] for b in range(server.B)}
+        # what the layers' attention was given and gave
+        seen = []
+        real = tv.paged_tree_attention
+
+        def spy(bank, req, pages, plan, q, out, w, **kw):
+            real(bank, req, pages, plan, q, out, w, **kw)
+            seen.append((q.clone(), out.clone(), [cached(server, kw["layer"], b, before[b] + (len(server.parents[t]) if t >= 0 else 0))
+                                                  for b, t in enumerate(trees)]))
+
+        tv.paged_tree_attention = spy
+        try:
+            logits, argmax = server.step(torch.tensor(trees, dtype=torch.int32), draft)
+        finally:
+            tv.paged_tree_attention = real
+        torch.cuda.synchronize()
+        assert server.status.tolist() == [0] * 4 and tv.tb_workspace_status(server.ws) == 0
+        start = server.req.row_start.tolist()
+        d = draft.cpu().numpy()
+        for b, t in enumerate(trees):
+            if t < 0:
+                assert start[b] == start[b + 1] and server.results[b, 0] == 0
+                continue
+            parent, lo = server.parents[t], start[b]
+            n = len(parent)
+            assert start[b + 1] - lo == n
+            for layer, (q, out, kv) in enumerate(seen):
+                k, v = kv[b]
+                # the prefix as it was, and the formula in 64 bits on the cache as stored
+                assert torch.equal(k[:before[b]], old[b][layer][0]) and torch.equal(v[:before[b]], old[b][layer][1])
+                o, _, absv, big = ref.attend(q[lo:lo + n].double().cpu().numpy(), k.double().cpu().numpy(),
+                                             v.double().cpu().numpy(), parent, before[b], m.d ** -0.5, server.softcap)
+                bound = 2.0 ** -8 * np.abs(o) + (2.0 ** -8 + 2.0 ** -12 + 2.0 ** -21 * big[..., None]) * absv + 1e-7
+                assert (np.abs(out[lo:lo + n].double().cpu().numpy() - o) <= bound).all()
+            a = argmax[lo:lo + n].cpu().numpy()
+            assert np.array_equal(a, logits[lo:lo + n].argmax(1).cpu().numpy())
+            k_len, path, bonus = oracle.accept(parent, d[lo:lo + n], a)
+            accepted += k_len - 1
+            got = server.results[b].tolist()
+            assert got[:4] == [k_len, bonus, before[b] + k_len, 0] and got[4:4 + k_len] == list(path)
+            assert server.history[b, said[b]:said[b] + k_len].tolist() == [int(d[lo + u]) for u in path[1:]] + [bonus]
+            for layer, (q, out, kv) in enumerate(seen):
+                after = cached(server, layer, b, before[b] + k_len)
+                for x, y in zip(after, kv[b]):
+                    assert torch.equal(x[:before[b]], y[:before[b]])
+                    assert torch.equal(x[before[b]:], y[before[b]:][torch.tensor(path, device="cuda", dtype=torch.long)])
+        assert server.req.lens.tolist() == server.results[:, 2].tolist()
+    head, free = server.pool.state.tolist()
+    held, table = server.pool.held.tolist(), server.req.table.cpu().numpy()
+    ring = server.pool.ring.cpu().numpy()
+    everything = np.concatenate([*[table[b, :h] for b, h in enumerate(held)], ring[(head + np.arange(free)) % len(ring)]])
+    assert sorted(everything.tolist()) == list(range(len(ring)))
+    assert held[2] == 0
+    assert accepted > 0  # the guesses are good enough that paths longer than the root come up
+
+
+@pytest.mark.parametrize("Hq,H,d,L,nodes", [(8, 8, 64, 500, 26), (8, 2, 128, 1300, 40)])
+def test_paged_and_contiguous_attention_agree(Hq, H, d, L, nodes):
+    """The same cache in pages and in one slab: both kernels within their common bound of each other."""
+    torch.manual_seed(L)
+    parent = synth.rank_product_tree((4, 3, 2, 2, 2), nodes)
+    bank = tv.Bank(2, 0)
+    bid, _ = bank.add(parent)
+    N, P = len(parent), 16
+    k, v = (torch.randn(1, H, L + N, d, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn(N, Hq, d, device="cuda").bfloat16()
+    want = torch.empty((1, N, Hq, d), dtype=torch.bfloat16, device="cuda")
+    ws = tv.make_workspace(tv.tb_workspace_size(64, 1, H, Hq, d, 1, 0))
+    tv.tree_attention(bank, bid, tv.KvCache(k, v, L), q[None].contiguous(), want, ws)
+    n = -(-(L + N) // P)
+    ids = torch.randperm(n + 3, device="cuda")[:n]
+    pages = [torch.zeros(1, n + 3, H, P, d, device="cuda").bfloat16() for _ in range(2)]
+    slot = torch.arange(L + N, device="cuda")
+    for pool, x in zip(pages, (k, v)):
+        pool[0].transpose(1, 2)[ids[slot // P], slot % P] = x[0].transpose(0, 1)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    req = tv.Requests(row_start=i32([0, 0]), tree=i32([bid]), lens=i32([L]), table=ids.int()[None].contiguous(), page_size=P)
+    plan = tv.make_paged_plan(1)
+    tv.paged_plan(bank, req, torch.empty(N, dtype=torch.int64, device="cuda"), i32([0] * N), i32([0]), plan, n_q_heads=Hq,
+                  n_kv_heads=H)
+    out = torch.empty_like(q)
+    tv.paged_tree_attention(bank, req, tv.Pages(*pages), plan, q, out, ws)
+    # each within 2^-8 |o| + (2^-8 + 2^-12) A of the exact output, A <= max |v|
+    err = (out.float() - want[0].float()).abs()
+    lim = 2 * (2.0 ** -8 * want[0].float().abs() + (2.0 ** -8 + 2.0 ** -12) * v.float().abs().max())
+    assert bool((err <= lim * 1.01).all())
+    # and the same workspace serves both again
+    again = torch.empty_like(want)
+    tv.tree_attention(bank, bid, tv.KvCache(k, v, L), q[None].contiguous(), again, ws)
+    assert torch.equal(again, want)
+    bank.close()
+
+
+def test_sampled_and_typical_rules_take_processed_logits():
+    """logits_process feeds the other acceptance rules: its statistics are theirs."""
+    torch.manual_seed(5)
+    parent = synth.rank_product_tree((3, 2, 1), 8)
+    bank = tv.Bank(2, 0)
+    bid, _ = bank.add(parent)
+    N, V, L, T = len(parent), 700, 33, 0.7
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    req = tv.Requests(row_start=i32([0, N]), tree=i32([bid]))
+    logits = 2 * torch.randn(N, V, device="cuda")
+    draft = torch.randint(0, V, (N,), device="cuda", dtype=torch.int32)
+    logits[torch.tensor(parent[1:], device="cuda").long(), draft[1:].long()] += 6.0
+    ws = tv.make_workspace(tv.tb_logits_workspace_size(1, N, V))
+    st = {k: torch.zeros(N, device="cuda") for k in ("top1", "entropy", "logz_t", "entropy_t", "draft_logit")}
+    argmax = torch.zeros(N, dtype=torch.int32, device="cuda")
+    mask = torch.full((N, -(-V // 32)), -1, dtype=torch.int32, device="cuda")
+    mask[:, 3] = 0  # tokens 96 .. 127 are not allowed
+    out = torch.empty_like(logits)
+    tv.logits_process(bank, req, logits, out, ws, draft=draft, mask=mask, temperature=T, argmax=argmax, **st)
+    z = out.double().cpu().numpy()
+    res = tv.make_result()
+    tv.typical_accept(bank, bid, draft, argmax, st["logz_t"], st["entropy_t"], st["draft_logit"], V, L, res, T, 0.09, 0.3)
+    k, path, bonus = oracle.typical_accept(parent, draft.cpu().numpy(), z, T, 0.09, 0.3)
+    r = tv.parse_result(res)
+    assert (r["accept_len"], r["path"], r["bonus_token"]) == (k, list(path), bonus)
+    q = torch.softmax(torch.randn(N, V, device="cuda"), 1)
+    u = torch.rand(2 * N, device="cuda")
+    tv.spec_sample_accept(bank, bid, draft, out, st["logz_t"], q, u, L, T, torch.empty(V, device="cuda"), res)
+    r = tv.parse_result(res)
+    assert not 96 <= r["bonus_token"] < 128
+    assert all(not 96 <= int(draft[j]) < 128 for j in r["path"][1:])
+    bank.close()
