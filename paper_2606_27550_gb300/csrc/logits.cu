@@ -451,207 +451,207 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
 
     const float inv_t = 1.f / p.temperature;
     if (gr < rows) {
-            float *dst = p.out + row * p.out_stride + v0;
-            const bool out_vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
-            // the draft tokens on this row's root path, relative to the slice
-            int tok[2] = {-1, -1};
-            if (paths && row - row0 < TB_MAX_NODES) {
-                const uint64_t anc = s_anc[row - row0];
+        float *dst = p.out + row * p.out_stride + v0;
+        const bool out_vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
+        // the draft tokens on this row's root path, relative to the slice
+        int tok[2] = {-1, -1};
+        if (paths && row - row0 < TB_MAX_NODES) {
+            const uint64_t anc = s_anc[row - row0];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int j = lane + 32 * h, x = s_draft[j] - v0;
-                    if (((anc >> j) & 1) && s_draft[j] >= 0 && x >= 0 && x < here)
-                        tok[h] = x;
-                }
+            for (int h = 0; h < 2; ++h) {
+                const int j = lane + 32 * h, x = s_draft[j] - v0;
+                if (((anc >> j) & 1) && s_draft[j] >= 0 && x >= 0 && x < here)
+                    tok[h] = x;
             }
-            Running a{-INFINITY, 0.f, 0.f, 0.f, 0.f, 0x7fffffff};
-            auto add = [&](float v, float mu) {
-                const float x = v - mu;
-                const float q = ex2_approx(x * kLog2e);
-                const float xc = fmaxf(x, -1e4f);  // finite where the weight is 0
-                a.s += q;
-                a.u = fmaf(q, xc, a.u);
-                if constexpr (kStats > 1) {
-                    const float qt = ex2_approx(x * p.scale_t);
-                    a.st += qt;
-                    a.ut = fmaf(qt, xc, a.ut);
-                }
-            };
+        }
+        Running a{-INFINITY, 0.f, 0.f, 0.f, 0.f, 0x7fffffff};
+        auto add = [&](float v, float mu) {
+            const float x = v - mu;
+            const float q = ex2_approx(x * kLog2e);
+            const float xc = fmaxf(x, -1e4f);  // finite where the weight is 0
+            a.s += q;
+            a.u = fmaf(q, xc, a.u);
+            if constexpr (kStats > 1) {
+                const float qt = ex2_approx(x * p.scale_t);
+                a.st += qt;
+                a.ut = fmaf(qt, xc, a.ut);
+            }
+        };
 #pragma unroll 1
-            for (int c = c_first; c < c_end; c += kChunk) {
-                float z[kVec][4];
-                uint32_t word = 0xffffffffu;  // lane w holds word w of the chunk's mask
-                fetch(c + (kStages - 1) * kChunk);
-                asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-                const int st = (c / kChunk) % kStages;
-                const T *from = ring + st * kChunk;  // every lane reads what it copied
-                if (in_vec && c + kChunk <= here) {
+        for (int c = c_first; c < c_end; c += kChunk) {
+            float z[kVec][4];
+            uint32_t word = 0xffffffffu;  // lane w holds word w of the chunk's mask
+            fetch(c + (kStages - 1) * kChunk);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            const int st = (c / kChunk) % kStages;
+            const T *from = ring + st * kChunk;  // every lane reads what it copied
+            if (in_vec && c + kChunk <= here) {
 #pragma unroll
-                    for (int k = 0; k < kVec; ++k) {
-                        const float4 x = In<kType>::four(from + k * 128 + lane * 4);
-                        z[k][0] = x.x, z[k][1] = x.y, z[k][2] = x.z, z[k][3] = x.w;
+                for (int k = 0; k < kVec; ++k) {
+                    const float4 x = In<kType>::four(from + k * 128 + lane * 4);
+                    z[k][0] = x.x, z[k][1] = x.y, z[k][2] = x.z, z[k][3] = x.w;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int o = k * 128 + lane * 4 + e;
+                        z[k][e] = c + o < here ? In<kType>::one(in_ring ? from + o : src + c + o) : -INFINITY;
                     }
-                } else {
+            }
+            if (mask && lane < kChunk / 32 && c + 32 * lane < here)
+                word = mask_ring[st * (kChunk / 32) + lane];
+            int l0 = 0, nl = 0;  // the chunk's touched tokens in the list
+            if (rules) {
+                l0 = before[c >> 5];
+                nl = before[min(c + kChunk, size) >> 5] - l0;
+            }
+            const int o0 = tok[0] - c, o1 = tok[1] - c;
+            const bool in0 = (unsigned)o0 < (unsigned)kChunk, in1 = (unsigned)o1 < (unsigned)kChunk;
+            const bool on_path = paths && __any_sync(0xffffffffu, in0 || in1);
+            float mine = -INFINITY;  // this lane's token of the list
+            int mine_at = 0;
+            const bool sparse = nl > 0 && nl <= 32 && !on_path;
+            if (sparse) {
+                mine_at = lane < nl ? list[l0 + lane] - c : 0;
+                const int from = (mine_at & 127) >> 2, reg = (mine_at >> 7) * 4 + (mine_at & 3);
 #pragma unroll
-                    for (int k = 0; k < kVec; ++k)
+                for (int k = 0; k < kVec; ++k)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int o = k * 128 + lane * 4 + e;
-                            z[k][e] = c + o < here ? In<kType>::one(in_ring ? from + o : src + c + o) : -INFINITY;
-                        }
+                    for (int e = 0; e < 4; ++e) {
+                        const float v = __shfl_sync(0xffffffffu, z[k][e], from);
+                        mine = reg == k * 4 + e ? v : mine;
+                    }
+                mine = penalise<false>(mine, generated[c + mine_at], (seen[(c + mine_at) >> 5] >> (mine_at & 31)) & 1,
+                                       bias[c + mine_at], pen);
+                const bool allowed = (__shfl_sync(0xffffffffu, word, mine_at >> 5) >> (mine_at & 31)) & 1;
+                mine = allowed && lane < nl ? mine : -INFINITY;
+                // the others go on as if these were masked
+                if (lane < kChunk / 32)
+                    word &= ~touched[(c >> 5) + lane];
+            } else if (on_path) {
+                uint32_t extra[kVec] = {};  // path occurrences of this lane's tokens, a byte each
+                for (int h = 0; h < 2; ++h)
+                    for (unsigned with = __ballot_sync(0xffffffffu, h ? in1 : in0); with; with &= with - 1) {
+                        const int o = __shfl_sync(0xffffffffu, h ? o1 : o0, __ffs(with) - 1);
+#pragma unroll
+                        for (int k = 0; k < kVec; ++k)
+                            if (o >> 7 == k && ((o & 127) >> 2) == lane)
+                                extra[k] += 1u << (8 * (o & 3));
+                    }
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    const int o = c + k * 128 + lane * 4;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int more = (extra[k] >> (8 * e)) & 0xff;
+                        const bool has = rules && ((seen[o >> 5] >> ((o & 31) + e)) & 1);
+                        const float n = rules ? generated[o + e] : 0.f;
+                        z[k][e] = penalise<false>(z[k][e], n + (float)more, has || more, rules ? bias[o + e] : 0.f, pen);
+                    }
                 }
-                if (mask && lane < kChunk / 32 && c + 32 * lane < here)
-                    word = mask_ring[st * (kChunk / 32) + lane];
-                int l0 = 0, nl = 0;  // the chunk's touched tokens in the list
-                if (rules) {
-                    l0 = before[c >> 5];
-                    nl = before[min(c + kChunk, size) >> 5] - l0;
-                }
-                const int o0 = tok[0] - c, o1 = tok[1] - c;
-                const bool in0 = (unsigned)o0 < (unsigned)kChunk, in1 = (unsigned)o1 < (unsigned)kChunk;
-                const bool on_path = paths && __any_sync(0xffffffffu, in0 || in1);
-                float mine = -INFINITY;  // this lane's token of the list
-                int mine_at = 0;
-                const bool sparse = nl > 0 && nl <= 32 && !on_path;
-                if (sparse) {
-                    mine_at = lane < nl ? list[l0 + lane] - c : 0;
-                    const int from = (mine_at & 127) >> 2, reg = (mine_at >> 7) * 4 + (mine_at & 3);
+            } else if (nl > 0) {
+                float big = 0.f, small = 1.f;
 #pragma unroll
-                    for (int k = 0; k < kVec; ++k)
+                for (int k = 0; k < kVec; ++k)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float v = __shfl_sync(0xffffffffu, z[k][e], from);
-                            mine = reg == k * 4 + e ? v : mine;
-                        }
-                    mine = penalise<false>(mine, generated[c + mine_at], (seen[(c + mine_at) >> 5] >> (mine_at & 31)) & 1,
-                                           bias[c + mine_at], pen);
-                    const bool allowed = (__shfl_sync(0xffffffffu, word, mine_at >> 5) >> (mine_at & 31)) & 1;
-                    mine = allowed && lane < nl ? mine : -INFINITY;
-                    // the others go on as if these were masked
-                    if (lane < kChunk / 32)
-                        word &= ~touched[(c >> 5) + lane];
-                } else if (on_path) {
-                    uint32_t extra[kVec] = {};  // path occurrences of this lane's tokens, a byte each
-                    for (int h = 0; h < 2; ++h)
-                        for (unsigned with = __ballot_sync(0xffffffffu, h ? in1 : in0); with; with &= with - 1) {
-                            const int o = __shfl_sync(0xffffffffu, h ? o1 : o0, __ffs(with) - 1);
-#pragma unroll
-                            for (int k = 0; k < kVec; ++k)
-                                if (o >> 7 == k && ((o & 127) >> 2) == lane)
-                                    extra[k] += 1u << (8 * (o & 3));
-                        }
+                    for (int e = 0; e < 4; ++e) {
+                        big = fmaxf(big, fabsf(z[k][e]));
+                        small = fminf(small, z[k][e] == 0.f ? 1.f : fabsf(z[k][e]));
+                    }
+                const bool plain = !short_div || big > 0x1p100f || small < 0x1p-100f;
+                if (__any_sync(0xffffffffu, plain)) {
 #pragma unroll
                     for (int k = 0; k < kVec; ++k) {
                         const int o = c + k * 128 + lane * 4;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int more = (extra[k] >> (8 * e)) & 0xff;
-                            const bool has = rules && ((seen[o >> 5] >> ((o & 31) + e)) & 1);
-                            const float n = rules ? generated[o + e] : 0.f;
-                            z[k][e] = penalise<false>(z[k][e], n + (float)more, has || more, rules ? bias[o + e] : 0.f, pen);
-                        }
-                    }
-                } else if (nl > 0) {
-                    float big = 0.f, small = 1.f;
-#pragma unroll
-                    for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            big = fmaxf(big, fabsf(z[k][e]));
-                            small = fminf(small, z[k][e] == 0.f ? 1.f : fabsf(z[k][e]));
-                        }
-                    const bool plain = !short_div || big > 0x1p100f || small < 0x1p-100f;
-                    if (__any_sync(0xffffffffu, plain)) {
-#pragma unroll
-                        for (int k = 0; k < kVec; ++k) {
-                            const int o = c + k * 128 + lane * 4;
-                            const uint32_t s = seen[o >> 5] >> (o & 31);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                z[k][e] = penalise<false>(z[k][e], generated[o + e], (s >> e) & 1, bias[o + e], pen);
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < kVec; ++k) {
-                            const int o = c + k * 128 + lane * 4;
-                            const uint32_t s = seen[o >> 5] >> (o & 31);
-                            const float4 n = *reinterpret_cast<const float4 *>(generated + o);
-                            const float4 f = *reinterpret_cast<const float4 *>(bias + o);
-                            z[k][0] = penalise<true>(z[k][0], n.x, s & 1, f.x, pen);
-                            z[k][1] = penalise<true>(z[k][1], n.y, s & 2, f.y, pen);
-                            z[k][2] = penalise<true>(z[k][2], n.z, s & 4, f.z, pen);
-                            z[k][3] = penalise<true>(z[k][3], n.w, s & 8, f.w, pen);
-                        }
-                    }
-                }
-                if (mask || sparse) {
-#pragma unroll
-                    for (int k = 0; k < kVec; ++k) {
-                        const uint32_t w = __shfl_sync(0xffffffffu, word, 4 * k + (lane >> 3)) >> (4 * (lane & 7));
+                        const uint32_t s = seen[o >> 5] >> (o & 31);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            z[k][e] = (w >> e) & 1 ? z[k][e] : -INFINITY;
+                            z[k][e] = penalise<false>(z[k][e], generated[o + e], (s >> e) & 1, bias[o + e], pen);
                     }
-                }
-                if (out_vec && c + kChunk <= here) {
-#pragma unroll
-                    for (int k = 0; k < kVec; ++k)
-                        *reinterpret_cast<float4 *>(dst + c + k * 128 + lane * 4) =
-                            make_float4(z[k][0], z[k][1], z[k][2], z[k][3]);
                 } else {
 #pragma unroll
-                    for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int o = c + k * 128 + lane * 4 + e;
-                            if (o < here)
-                                dst[o] = z[k][e];
-                        }
-                }
-                if (sparse) {
-                    __syncwarp();
-                    if (lane < nl)
-                        dst[c + mine_at] = mine;
-                }
-                if constexpr (kStats > 0) {
-                    float m = mine;
-#pragma unroll
-                    for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            m = fmaxf(m, z[k][e]);
-                    m = warp_max(m);
-                    if (m > a.m) {
-                        // a new maximum: its lowest token, and the sums relative to it
-                        unsigned arg = mine == m ? (unsigned)(v0 + c + mine_at) : 0x7fffffffu;
-#pragma unroll
-                        for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (z[k][e] == m)
-                                    arg = min(arg, (unsigned)(v0 + c + k * 128 + lane * 4 + e));
-                        a.arg = (int)__reduce_min_sync(0xffffffffu, arg);
-                        const float d = a.m == -INFINITY ? 0.f : a.m - m;  // (sums of nothing: 0)
-                        const float w = ex2_approx(d * kLog2e);
-                        a.u = w * (a.u + d * a.s);
-                        a.s *= w;
-                        if constexpr (kStats > 1) {
-                            const float wt = ex2_approx(d * p.scale_t);
-                            a.ut = wt * (a.ut + d * a.st);
-                            a.st *= wt;
-                        }
-                        a.m = m;
+                    for (int k = 0; k < kVec; ++k) {
+                        const int o = c + k * 128 + lane * 4;
+                        const uint32_t s = seen[o >> 5] >> (o & 31);
+                        const float4 n = *reinterpret_cast<const float4 *>(generated + o);
+                        const float4 f = *reinterpret_cast<const float4 *>(bias + o);
+                        z[k][0] = penalise<true>(z[k][0], n.x, s & 1, f.x, pen);
+                        z[k][1] = penalise<true>(z[k][1], n.y, s & 2, f.y, pen);
+                        z[k][2] = penalise<true>(z[k][2], n.z, s & 4, f.z, pen);
+                        z[k][3] = penalise<true>(z[k][3], n.w, s & 8, f.w, pen);
                     }
-                    const float mu = a.m == -INFINITY ? 0.f : a.m;
-#pragma unroll
-                    for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            add(z[k][e], mu);
-                    if (sparse)
-                        add(mine, mu);
                 }
             }
+            if (mask || sparse) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    const uint32_t w = __shfl_sync(0xffffffffu, word, 4 * k + (lane >> 3)) >> (4 * (lane & 7));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        z[k][e] = (w >> e) & 1 ? z[k][e] : -INFINITY;
+                }
+            }
+            if (out_vec && c + kChunk <= here) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k)
+                    *reinterpret_cast<float4 *>(dst + c + k * 128 + lane * 4) =
+                        make_float4(z[k][0], z[k][1], z[k][2], z[k][3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int o = c + k * 128 + lane * 4 + e;
+                        if (o < here)
+                            dst[o] = z[k][e];
+                    }
+            }
+            if (sparse) {
+                __syncwarp();
+                if (lane < nl)
+                    dst[c + mine_at] = mine;
+            }
+            if constexpr (kStats > 0) {
+                float m = mine;
+#pragma unroll
+                for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        m = fmaxf(m, z[k][e]);
+                m = warp_max(m);
+                if (m > a.m) {
+                    // a new maximum: its lowest token, and the sums relative to it
+                    unsigned arg = mine == m ? (unsigned)(v0 + c + mine_at) : 0x7fffffffu;
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (z[k][e] == m)
+                                arg = min(arg, (unsigned)(v0 + c + k * 128 + lane * 4 + e));
+                    a.arg = (int)__reduce_min_sync(0xffffffffu, arg);
+                    const float d = a.m == -INFINITY ? 0.f : a.m - m;  // (sums of nothing: 0)
+                    const float w = ex2_approx(d * kLog2e);
+                    a.u = w * (a.u + d * a.s);
+                    a.s *= w;
+                    if constexpr (kStats > 1) {
+                        const float wt = ex2_approx(d * p.scale_t);
+                        a.ut = wt * (a.ut + d * a.st);
+                        a.st *= wt;
+                    }
+                    a.m = m;
+                }
+                const float mu = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+                for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        add(z[k][e], mu);
+                if (sparse)
+                    add(mine, mu);
+            }
+        }
         if constexpr (kStats > 0) {
 #pragma unroll
             for (int o = 16; o >= 1; o >>= 1) {
