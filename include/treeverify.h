@@ -652,7 +652,8 @@ TB_API tb_status paged_kv_store(const tb_pages *pages, int layer, const int64_t 
  * (softcap 0: no cap; slopes NULL: no bias).  A row that sees nothing gets out
  * 0 and lse -inf.  Keys that no row of a request may see do not reach its
  * outputs, whatever their pages hold (NaN and infinities included); the values
- * of slots that some rows see and others do not have to be finite.
+ * of slots that some rows see and others do not have to be finite.  A capped
+ * score is right to softcap 2^-20, so that softcap may be 1024 at most.
  *   q, out [n_rows][n_q_heads][head_dim] of the pages' type, rows as row_start
  *          numbers them (rows of the plan past n_rows are left out)
  *   lse    NULL, or float [n_rows][n_q_heads]; slopes: NULL or device float [n_q_heads]

@@ -56,6 +56,15 @@ constexpr int tile_bytes(int d)
 {
     return d / 64 * kAtom;
 }
+// A capped score carries an error of up to cap 2^-20 from the 32-bit tanh: 2^-10 at this cap, where
+// rounding a weight costs 2^-8 (bf16) or 2^-11 (fp16).
+constexpr float kMaxCap = 1024.f;
+
+float cap_in(float scale, float softcap)
+{
+    return (float)(2.0 * 1.4426950408889634 * (double)scale / (double)softcap);
+}
+
 // floats per partial slot: O[128][kD], m[128], l[128]
 constexpr int slot_floats(int d)
 {
@@ -138,15 +147,35 @@ __device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b)
     return r;
 }
 
-// cap tanh(scale s / cap) of two scores in units of ln 2: tanh y = 1 - 2 / (1 + e^(2y)),
-// with the right limits where the exponential overflows or vanishes.  (An odd
-// polynomial for small arguments in place of the two special functions took longer:
-// 128 us for 111, two row blocks over 65536 keys.)
-__device__ __forceinline__ float2 capped(float s0, float s1, float cap, float cap_in)
+__device__ __forceinline__ float min_or_nan(float a, float b)
 {
-    const float2 e = halves(mul_two(two(s0, s1), two(cap_in, cap_in)));
-    const float2 d = halves(add_two(two(ex2_approx(e.x), ex2_approx(e.y)), two(1.f, 1.f)));
-    return halves(fma_two(two(rcp_approx(d.x), rcp_approx(d.y)), two(-2.f * cap, -2.f * cap), two(cap, cap)));
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
+// A capped score is cap tanh y = cap - 2 cap w with w = 1 / (1 + e^(2y)), y = scale s / cap.
+// w of four scores in their place: from e^(2y) = 2^30 on, 2 w is below half a unit in the
+// last place of 1, so that the exponent stops there and one reciprocal, of the product of
+// all four denominators (at most 2^120), serves them: 1/a = b (cd / abcd).  The special
+// functions bound a capped tile: two row blocks over 65536 keys (8 kv heads) take 98 us
+// with this, 107 us with a reciprocal each, 113 us with an odd polynomial for small
+// arguments, and 75 us without a cap.
+__device__ __forceinline__ void cap_four(uint32_t *r, float cap_in)
+{
+    float e[4];
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const float2 y = halves(mul_two(two(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), two(cap_in, cap_in)));
+        e[i] = ex2_approx(min_or_nan(y.x, 30.f)), e[i + 1] = ex2_approx(min_or_nan(y.y, 30.f));
+    }
+    const uint64_t ac = add_two(two(e[0], e[2]), two(1.f, 1.f)), bd = add_two(two(e[1], e[3]), two(1.f, 1.f));
+    const float2 ab_cd = halves(mul_two(ac, bd));
+    const float y = rcp_approx(ab_cd.x * ab_cd.y);
+    const uint64_t inv = mul_two(two(ab_cd.y, ab_cd.x), two(y, y));  // 1 / ab, 1 / cd
+    const float2 w02 = halves(mul_two(bd, inv)), w13 = halves(mul_two(ac, inv));
+    r[0] = __float_as_uint(w02.x), r[2] = __float_as_uint(w02.y);
+    r[1] = __float_as_uint(w13.x), r[3] = __float_as_uint(w13.y);
 }
 
 // The bits of [lo, hi) relative to s0, of 32.
@@ -461,17 +490,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 const uint32_t sa = lane_addr + kColS + b * 128 + half * kHalf;
                 const int h0 = key0 + half * kHalf;  // this thread's first slot
                 const bool masked = h0 + kHalf > L || h0 < si.lo_max;
-                // this half's scores, held in registers until they are weights
+                const auto visible = [&](int s0) {  // which of the 32 slots from s0 on this row sees
+                    return range_bits(s0, lo, L) | range_bits(s0, si.begin, si.far) | tree_bits(s0, L, anc);
+                };
+                // this half's scores (kCap: their w), held in registers until they are weights
+                constexpr uint32_t kHidden = kForm == kCap ? 0x7f800000u : 0xff800000u;  // z = -inf
                 uint32_t r[kHalf];
                 tmem_ld_32x32b_x32(sa, r);
                 tmem_ld_32x32b_x32(sa + 32, r + 32);
                 tmem_ld_wait();
                 if constexpr (kForm != kPlain) {
                     if (kForm == kCap || p.cap > 0.f) {
+                        // a NaN in a hidden slot must not reach its neighbours through the common reciprocal
+                        if (masked) {
 #pragma unroll
-                        for (int x = 0; x < kHalf; x += 2) {
-                            const float2 z = capped(__uint_as_float(r[x]), __uint_as_float(r[x + 1]), p.cap, p.cap_in);
-                            r[x] = __float_as_uint(z.x), r[x + 1] = __float_as_uint(z.y);
+                            for (int y = 0; y < kHalf; y += 32) {
+                                const uint32_t allow = visible(h0 + y);
+#pragma unroll
+                                for (int x = 0; x < 32; ++x)
+                                    r[y + x] = (allow >> x) & 1u ? r[y + x] : 0xff800000u;
+                            }
+                        }
+#pragma unroll
+                        for (int x = 0; x < kHalf; x += 4)
+                            cap_four(r + x, p.cap_in);
+                        if constexpr (kForm == kBias) {
+#pragma unroll
+                            for (int x = 0; x < kHalf; x += 2) {
+                                const float2 z = halves(fma_two(two(__uint_as_float(r[x]), __uint_as_float(r[x + 1])),
+                                                                two(-2.f * p.cap, -2.f * p.cap), two(p.cap, p.cap)));
+                                r[x] = __float_as_uint(z.x), r[x + 1] = __float_as_uint(z.y);
+                            }
                         }
                     } else {
 #pragma unroll
@@ -496,11 +545,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                                 dist -= (fall >> x) & 1u ? 1.f : 0.f;
                             }
                         }
-                        const uint32_t allow =
-                            range_bits(s0, lo, L) | range_bits(s0, si.begin, si.far) | tree_bits(s0, L, anc);
+                        const uint32_t allow = visible(s0);
 #pragma unroll
                         for (int x = 0; x < 32; ++x)
-                            r[y + x] = (allow >> x) & 1u ? r[y + x] : 0xff800000u;
+                            r[y + x] = (allow >> x) & 1u ? r[y + x] : kHidden;
                     }
                 } else if constexpr (kForm == kBias) {
                     const float d0 = (float)(pos - h0);
@@ -513,12 +561,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                         dist = add_two(dist, two(-2.f, -2.f));
                     }
                 }
-                float mx = -INFINITY;
+                // z = f r + f0; f < 0 where r is a capped score's w
+                float mx = kForm == kCap ? INFINITY : -INFINITY;
 #pragma unroll
                 for (int x = 0; x < kHalf; ++x)
-                    mx = fmaxf(mx, __uint_as_float(r[x]));
-                if constexpr (kForm == kPlain)
-                    mx *= p.scale;
+                    mx = kForm == kCap ? fminf(mx, __uint_as_float(r[x])) : fmaxf(mx, __uint_as_float(r[x]));
+                const float f = kForm == kCap ? -2.f * p.cap : kForm == kPlain ? p.scale : 1.f;
+                const float f0 = kForm == kCap ? p.cap : 0.f;
+                mx = fmaf(f, mx, f0);
                 // the other half's
                 s_mx[b][half][rloc] = mx;
                 __syncwarp();
@@ -564,12 +614,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
 
                 // P in the pages' type on the first columns of this half, its 32-bit sum into l
                 const float mu = m_ref == -INFINITY ? 0.f : m_ref;
-                const float f = kForm == kPlain ? p.scale : 1.f;
                 uint64_t rs = two(0.f, 0.f);
 #pragma unroll
                 for (int x = 0; x < kHalf / 2; ++x) {
                     const float2 z = halves(fma_two(two(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), two(f, f),
-                                                    two(-mu, -mu)));
+                                                    two(f0 - mu, f0 - mu)));
                     const float p0 = ex2_approx(z.x), p1 = ex2_approx(z.y);
                     rs = add_two(rs, two(p0, p1));
                     r[x] = pack<kF16>(p0, p1);
@@ -958,6 +1007,8 @@ extern "C" tb_status paged_tree_attention(const tb_bank *bank, const tb_requests
                             n_q_heads / pages->n_kv_heads, kMaxGroup);
     if (!(scale > 0.f) || !std::isfinite(scale) || !(softcap >= 0.f) || !std::isfinite(softcap))
         return record_error(TB_EINVAL, "%s: scale %g, softcap %g", fn, scale, softcap);
+    if (softcap > kMaxCap || (softcap > 0.f && !std::isfinite(cap_in(scale, softcap))))
+        return record_error(TB_EUNSUPPORTED, "%s: scale %g with softcap %g (%g at most)", fn, scale, softcap, kMaxCap);
     if (n_rows < 0)
         return record_error(TB_EINVAL, "%s: n_rows %d", fn, n_rows);
     if (!q || !out || !ptr_aligned(q, 16) || !ptr_aligned(out, 16))
@@ -995,7 +1046,7 @@ extern "C" tb_status paged_tree_attention(const tb_bank *bank, const tb_requests
     a.group = n_q_heads / pages->n_kv_heads;
     a.scale = scale * kLog2e;
     a.cap = softcap * kLog2e;
-    a.cap_in = softcap > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)scale / (double)softcap) : 0.f;
+    a.cap_in = softcap > 0.f ? cap_in(scale, softcap) : 0.f;
     a.plan = const_cast<void *>(plan);
     a.part = attention_parts(workspace);
     a.status = static_cast<int *>(workspace);

@@ -262,3 +262,34 @@ def test_random_batches(bank, seed):
     slopes = torch.rand(H * group, device="cuda") if g.random() < 0.3 else None
     s.check(bank, window=window, sink=int(g.integers(0, 200)) if window else 0,
             cap=float(g.choice([0.0, 0.0, 5.0, 50.0])), slopes=slopes)
+
+
+@pytest.mark.parametrize("cap", [0.01, 0.5, 50.0, 1024.0])
+@pytest.mark.parametrize("biased", [False, True])
+def test_caps_from_saturated_to_hardly_bent(bank, cap, biased):
+    """Scores far past the cap in both directions, and caps far past the scores; hidden slots hold NaN."""
+    s = Scene(int(cap) + 3, [130, 5, 0, 260], [7, 5, 8, 0], 6, 3, 64, 16, q_std=20.0 if cap < 100 else 2.0)
+    slopes = torch.full((6,), 0.05, device="cuda") if biased else None
+    out, lse = s.run(bank, cap=cap, slopes=slopes)
+    q, at = s.q.double().cpu().numpy(), 0
+    s64 = None if slopes is None else slopes.double().cpu().numpy()
+    for b, n in enumerate(s.n):
+        k, v = s.dense[b]
+        o, ls, absv, big = ref.attend(q[at:at + n], k, v, s.trees[s.tree[b]], s.lens[b], s.d ** -0.5, cap, s64)
+        # as for the others, and the documented cap 2^-20 of every score (once in the weight, once in the sum)
+        z = 2.0 ** -21 * big + 2.0 ** -20 * cap
+        bound = 2.0 ** -8 * np.abs(o) + (2.0 ** -8 + 2.0 ** -12 + 2 * z[..., None]) * absv + 1e-7
+        assert (np.abs(out[at:at + n] - o) <= bound).all()
+        assert (np.abs(lse[at:at + n] - ls) <= 1e-5 + 2.0 ** -21 * np.abs(ls) + z).all()
+        at += n
+
+
+def test_a_query_that_is_not_a_number_shows(bank):
+    """With a cap, NaN in one row's query makes that row NaN and leaves the others as they were."""
+    s = Scene(4, [70], [5], 2, 2, 64, 16)
+    want, _ = s.run(bank, cap=30.0)
+    s.q[3, 1, 5] = float("nan")
+    got, _ = s.run(bank, cap=30.0)
+    assert np.isnan(got[3, 1]).all()
+    got[3, 1] = want[3, 1]
+    assert np.array_equal(got, want)

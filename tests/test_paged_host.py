@@ -157,6 +157,8 @@ def test_refusals_of_attention(lib, s):
     refused(tv.TB_EINVAL, s.attend, scale=0.0)
     refused(tv.TB_EINVAL, s.attend, scale=float("nan"))
     refused(tv.TB_EINVAL, s.attend, softcap=-1.0)
+    refused(tv.TB_EUNSUPPORTED, s.attend, softcap=1025.0)
+    refused(tv.TB_EUNSUPPORTED, s.attend, softcap=1e-40)
     refused(tv.TB_EINVAL, s.attend, q=torch.zeros(9, 3, 64, dtype=BF), out=torch.zeros(9, 3, 64, dtype=BF))
     refused(tv.TB_EINVAL, s.attend, req=_other(s.req, page_size=32))
     refused(tv.TB_EINVAL, s.attend, req=_other(s.req, tree=None))
