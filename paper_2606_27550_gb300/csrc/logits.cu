@@ -43,7 +43,6 @@ constexpr int kRows = kWarps;   // rows of a CTA
 constexpr int kMaxSlice = 3584;  // three CTAs per SM
 constexpr int kMaxRowsCall = 65536;
 constexpr int kStages = 2;      // chunks of a warp's ring: one in work, the others on their way
-constexpr uint32_t kInPrompt = 0x80000000u;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Part {
@@ -179,6 +178,24 @@ __device__ __forceinline__ float penalise(float z, float n, bool seen, float bia
     return __fadd_rn(z, bias);
 }
 
+// Notes an occurrence of the slice's token `loc`, if it is below `here`: the history has
+// it, and if it was generated, once more.  Predicated: one lane in 36 has a token of the
+// slice, some lane of most warps, and as a branch per token this took longer than the
+// tokens' way from memory.
+__device__ __forceinline__ void note_token(uint32_t *count, uint32_t *seen, unsigned loc, unsigned here, bool generated)
+{
+    asm volatile("{\n\t"
+                 ".reg .pred p, q;\n\t"
+                 "setp.ne.s32 q, %4, 0;\n\t"
+                 "setp.lt.u32 p, %2, %3;\n\t"
+                 "setp.lt.and.u32 q, %2, %3, q;\n\t"
+                 "@p red.shared.or.b32 [%1], %5;\n\t"
+                 "@q red.shared.add.u32 [%0], 1;\n\t"
+                 "}" ::"r"(smem_u32(count) + 4 * loc), "r"(smem_u32(seen) + 4 * (loc >> 5)), "r"(loc), "r"(here),
+                 "r"((int)generated), "r"(1u << (loc & 31))
+                 : "memory");
+}
+
 // The largest of the warp's values (NaN only where all are).
 __device__ __forceinline__ float warp_max(float x)
 {
@@ -219,14 +236,18 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
     __shared__ int s_last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int slice = blockIdx.y, size = p.size, v0 = slice * size;  // v0 < V (the host's split)
-    uint32_t *count = reinterpret_cast<uint32_t *>(smem);  // generated occurrences | kInPrompt; then as floats
+    uint32_t *count = reinterpret_cast<uint32_t *>(smem);  // generated occurrences; then as floats
     float *bias = reinterpret_cast<float *>(count + size);
     uint32_t *touched = reinterpret_cast<uint32_t *>(bias + size);  // bitmap: a rule has the token
     uint32_t *seen = touched + size / 32;                           // bitmap: the history has it
     uint16_t *before = reinterpret_cast<uint16_t *>(seen + size / 32);  // touched tokens before a word's
     uint16_t *list = before + size / 32 + 8;                            // the touched tokens, in order
     using T = typename In<kType>::T;
-    T *ring = reinterpret_cast<T *>(smem + p.ring_off) + (size_t)warp * kStages * kChunk;
+    T *ring = reinterpret_cast<T *>(smem + p.ring_off) + warp * kChunk;  // a stage of all warps behind another
+    // the second stage holds tokens of the history until the rules are built
+    int *early = reinterpret_cast<int *>(smem + p.ring_off + kWarps * kChunk * sizeof(T));
+    constexpr int kEarly = kWarps * kChunk * sizeof(T) / 4;
+    static_assert(kStages >= 2, "tokens of the history in the second stage");
     uint32_t *mask_ring = reinterpret_cast<uint32_t *>(smem + p.mask_off) + warp * kStages * (kChunk / 32);
     const bool rules = p.r.history || p.r.bias_start;
     if (rules) {
@@ -276,8 +297,8 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
     bool in_vec = false, in_ring = false;  // its chunks go through the ring (16-byte pieces, or 4-byte ones)
     auto fetch = [&](int c) {  // chunk c on its way; always one group of copies
         if (c < c_end) {
-            const int st = (c / kChunk) % kStages;
-            T *to = ring + st * kChunk;
+            const int st = ((c - c_first) / kChunk) % kStages;
+            T *to = ring + st * (kWarps * kChunk);
             if (in_vec && c + kChunk <= here) {
 #pragma unroll
                 for (int k = 0; k < kVec; ++k)
@@ -299,6 +320,31 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    // The first tokens of the history (some in registers, others by way of shared
+    // memory) and the first biases, then the logits and the tree: one round trip.
+    constexpr int kAhead = 16, kInRegs = kAhead * kThreads, kBiasAhead = 2;
+    const int n_said = (int)min((long long)max(said, 0), (long long)p.r.history_stride);
+    const int n_asked = min(max(asked, 0), n_said);
+    const int32_t *h = p.r.history + (p.r.history ? b * p.r.history_stride : 0);
+    const int bias_end = bias1;
+    int word_of[kAhead], bias_tok[kBiasAhead];
+    float bias_val[kBiasAhead];
+#pragma unroll
+    for (int m = 0; m < kAhead; ++m) {
+        const int i = threadIdx.x + m * kThreads;
+        word_of[m] = i < n_said ? load_now(h + i) : -1;
+    }
+    const auto load_biases = [&](int e) {
+#pragma unroll
+        for (int m = 0; m < kBiasAhead; ++m) {
+            bias_tok[m] = e + m * kThreads < bias_end ? load_now(p.r.bias_token + e + m * kThreads) : -1;
+            bias_val[m] = e + m * kThreads < bias_end ? load_now(p.r.bias_value + e + m * kThreads) : 0.f;
+        }
+    };
+    load_biases(max(bias0, 0) + threadIdx.x);
+    for (int i = threadIdx.x; i < min(n_said - kInRegs, kEarly); i += kThreads)
+        copy_async<4>(early + i, h + kInRegs + i);
+    asm volatile("cp.async.commit_group;" ::: "memory");
     const int gr = warp / parts, part = warp - gr * parts;  // this warp's row and part of it
     if (gr < rows) {
         row = g0 + gr;
@@ -313,119 +359,95 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
 #pragma unroll
         for (int k = 0; k < kStages - 1; ++k)
             fetch(c_first + k * kChunk);
+    } else {
+#pragma unroll
+        for (int k = 0; k < kStages - 1; ++k)
+            asm volatile("cp.async.commit_group;" ::: "memory");
     }
 
     const TreeDesc *td = t >= 0 && t < p.n_trees ? p.trees + t : nullptr;
     const bool paths = td && p.r.draft;
-    // the first tokens of the history, the first biases and the tree, one round trip
-    constexpr int kAhead = 16;
-    const int n_said = (int)min((long long)max(said, 0), (long long)p.r.history_stride);
-    const int n_asked = min(max(asked, 0), n_said);
-    const int32_t *h = p.r.history + (p.r.history ? b * p.r.history_stride : 0);
-    int word_of[kAhead];
-#pragma unroll
-    for (int m = 0; m < kAhead; ++m) {
-        const int i = threadIdx.x + m * kThreads;
-        word_of[m] = i < n_said ? load_now(h + i) : -1;
-    }
-    constexpr int kBiasAhead = 4;
-    int bias_tok[kBiasAhead];
-    float bias_val[kBiasAhead];
-    auto load_biases = [&](int e0) {
-#pragma unroll
-        for (int m = 0; m < kBiasAhead; ++m) {
-            const int e = e0 + 32 * m + lane;
-            bias_tok[m] = e < bias1 ? load_now(p.r.bias_token + e) : -1;
-            bias_val[m] = e < bias1 ? load_now(p.r.bias_value + e) : 0.f;
-        }
-    };
-    if (warp == 0)
-        load_biases(max(bias0, 0));
     uint64_t node_anc = 0;
     int node_tok = -1;
     if (paths && threadIdx.x < TB_MAX_NODES) {
-        const int n = load_now(&td->n);
+        const int n = load_now(&td->n), here_rows = row1 - row0;
         const uint64_t anc = load_now(td->anc + threadIdx.x);
-        if ((int)threadIdx.x < min(n, row1 - row0)) {
+        const int token = (int)threadIdx.x < here_rows ? load_now(p.r.draft + row0 + threadIdx.x) : -1;
+        if ((int)threadIdx.x < min(n, here_rows)) {
             node_anc = anc & ~1ull;
-            node_tok = load_now(p.r.draft + row0 + threadIdx.x);
+            node_tok = token;
         }
     }
     pen.inv = __fdiv_rn(1.f, pen.rep);
     // (see above for which divisors and, below, dividends the short quotient is right)
     const bool short_div = pen.rep > 0x1p-20f && pen.rep < 0x1p20f && (__float_as_uint(pen.rep) & 0x7fffffu) != 0x7fffffu;
-    __shared__ int s_sum[kWarps];
+    __shared__ int s_sum[kWarps], s_again;
     if (threadIdx.x < TB_MAX_NODES) {
         s_anc[threadIdx.x] = node_anc;
         s_draft[threadIdx.x] = node_tok;
     }
+    if (threadIdx.x == 0)
+        s_again = 0;
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");  // all but the logits
     __syncthreads();
-    for (int i0 = threadIdx.x;;) {
 #pragma unroll
-        for (int m = 0; m < kAhead; ++m) {
-            const unsigned loc = (unsigned)(word_of[m] - v0);
-            if (word_of[m] >= 0 && loc < (unsigned)here) {
-                if (i0 + m * kThreads < n_asked)
-                    atomicOr(&count[loc], kInPrompt);
-                else
-                    atomicAdd(&count[loc], 1u);
-            }
-        }
-        i0 += kThreads * kAhead;
-        if (i0 - (int)threadIdx.x >= n_said)
-            break;
+    for (int m = 0; m < kAhead; ++m)
+        note_token(count, seen, (unsigned)(word_of[m] - v0), (unsigned)here, (int)threadIdx.x + m * kThreads >= n_asked);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < min(n_said - kInRegs, kEarly); i += kThreads)
+        note_token(count, seen, (unsigned)(early[i] - v0), (unsigned)here, kInRegs + i >= n_asked);
+    for (int i0 = kInRegs + kEarly + threadIdx.x; i0 < n_said; i0 += kInRegs) {
 #pragma unroll
         for (int m = 0; m < kAhead; ++m)
             word_of[m] = i0 + m * kThreads < n_said ? load_now(h + i0 + m * kThreads) : -1;
+#pragma unroll
+        for (int m = 0; m < kAhead; ++m)
+            note_token(count, seen, (unsigned)(word_of[m] - v0), (unsigned)here, i0 + m * kThreads >= n_asked);
     }
-    // biases by one warp, in list order: entries of one token add up in a fixed order
-    for (int e0 = max(bias0, 0); warp == 0 && e0 < bias1;) {
+    // Biases, in any order as long as no token comes up twice; where one does, all again
+    // by one warp in list order, so that its entries add up in a fixed order.
+    for (int e = max(bias0, 0) + threadIdx.x; e < bias_end;) {
 #pragma unroll
         for (int m = 0; m < kBiasAhead; ++m) {
             const unsigned loc = (unsigned)(bias_tok[m] - v0);
-            const bool mine = bias_tok[m] >= 0 && loc < (unsigned)here;
-            if (!__any_sync(0xffffffffu, mine))
-                continue;
+            if (loc < (unsigned)here) {
+                if ((atomicOr(&touched[loc >> 5], 1u << (loc & 31)) >> (loc & 31)) & 1)
+                    s_again = 1;
+                else
+                    bias[loc] = bias_val[m];
+            }
+        }
+        e += kThreads * kBiasAhead;
+        load_biases(e);
+    }
+    __syncthreads();
+    if (s_again) {
+        for (int x = threadIdx.x; x < size; x += kThreads)
+            bias[x] = 0.f;
+        __syncthreads();
+        for (int e0 = max(bias0, 0); warp == 0 && e0 < bias_end; e0 += 32) {
+            const int e = e0 + lane;
+            const unsigned loc = e < bias_end ? (unsigned)(load_now(p.r.bias_token + e) - v0) : 0xffffffffu;
+            const float value = e < bias_end ? load_now(p.r.bias_value + e) : 0.f;
+            const bool mine = loc < (unsigned)here;
             const unsigned same = __match_any_sync(0xffffffffu, mine ? (int)loc : -1 - lane);
             const bool leader = mine && (same & ((1u << lane) - 1)) == 0;
             float acc = leader ? bias[loc] : 0.f;
-            if (__all_sync(0xffffffffu, __popc(same) == 1)) {
-                acc += bias_val[m];
-            } else {
-                for (int k = 0; k < 32; ++k) {
-                    const float v = __shfl_sync(0xffffffffu, bias_val[m], k);
-                    acc += (same >> k) & 1 ? v : 0.f;
-                }
+            for (int k = 0; k < 32; ++k) {
+                const float v = __shfl_sync(0xffffffffu, value, k);
+                acc += (same >> k) & 1 ? v : 0.f;
             }
-            if (leader) {
+            if (leader)
                 bias[loc] = acc;
-                atomicOr(&touched[loc >> 5], 1u << (loc & 31));
-            }
             __syncwarp();
         }
-        e0 += 32 * kBiasAhead;
-        if (e0 < bias1)
-            load_biases(e0);
     }
-    __syncthreads();
 
     if (rules) {
-        // counts as floats, who is seen, and the touched tokens as a list
+        // the touched tokens as a list, their counts as floats
         const int words = size / 32;
         static_assert(kMaxSlice / 32 <= kThreads, "a word of the bitmap per thread");
-        for (int x = warp; x < words; x += kWarps) {
-            const uint32_t n = count[32 * x + lane];
-            const uint32_t bits = __ballot_sync(0xffffffffu, n != 0);
-            if (bits) {
-                reinterpret_cast<float *>(count)[32 * x + lane] = (float)(n & ~kInPrompt);
-                if (lane == 0) {
-                    seen[x] = bits;
-                    touched[x] |= bits;
-                }
-            }
-        }
-        __syncthreads();
-        const uint32_t mine = threadIdx.x < words ? touched[threadIdx.x] : 0u;
+        const uint32_t mine = threadIdx.x < words ? touched[threadIdx.x] | seen[threadIdx.x] : 0u;
         int at = __popc(mine);
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -442,8 +464,12 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
                 before[words] = (uint16_t)at;
             at -= __popc(mine);
             before[threadIdx.x] = (uint16_t)at;
-            for (uint32_t rest = mine; rest; rest &= rest - 1)
-                list[at++] = (uint16_t)(threadIdx.x * 32 + __ffs(rest) - 1);
+            touched[threadIdx.x] = mine;
+            for (uint32_t rest = mine; rest; rest &= rest - 1) {
+                const int x = threadIdx.x * 32 + __ffs(rest) - 1;
+                list[at++] = (uint16_t)x;
+                reinterpret_cast<float *>(count)[x] = (float)count[x];
+            }
         }
         __syncthreads();
     }
@@ -483,8 +509,8 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
             uint32_t word = 0xffffffffu;  // lane w holds word w of the chunk's mask
             fetch(c + (kStages - 1) * kChunk);
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-            const int st = (c / kChunk) % kStages;
-            const T *from = ring + st * kChunk;  // every lane reads what it copied
+            const int st = ((c - c_first) / kChunk) % kStages;
+            const T *from = ring + st * (kWarps * kChunk);  // every lane reads what it copied
             if (in_vec && c + kChunk <= here) {
 #pragma unroll
                 for (int k = 0; k < kVec; ++k) {
