@@ -711,8 +711,9 @@ typedef struct tb_logit_stats {
  * row without an allowed token has argmax -1, top1 0, entropy 0 and logz_t
  * -inf; a NaN among the allowed logits makes the row's statistics NaN.
  * Requests and rows are req's (batch, row_start, tree; tree NULL: rows without
- * root paths); rows past n_rows (at most 65536) are left out.  One kernel; results
- * do not depend on the launch's placement. */
+ * root paths); rows past n_rows (at most 65536) are left out.  One kernel, or two where
+ * the call has more work than the SMs hold at once; results do not depend on the
+ * launch's placement. */
 TB_API tb_status logits_process(const tb_bank *bank, const tb_requests *req, const void *logits, int dtype,
                                 int64_t logit_stride, int n_rows, int vocab, const tb_logit_rules *rules,
                                 float temperature, float *out, int64_t out_stride, const tb_logit_stats *stats,

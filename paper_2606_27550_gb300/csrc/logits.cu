@@ -7,17 +7,22 @@
 // often each token was generated, whether the prompt has it, its bias, and a
 // bitmap of the tokens that any rule touches.  A warp takes a row's slice (or a
 // part of it where there are few rows) in chunks of 512 tokens through a ring of its
-// own in shared memory, the next two chunks on their way.  Of a chunk's touched
-// tokens (a few percent of a vocabulary, but some lane of nearly every warp has
-// one) up to 32 are handed one to each lane, which applies the rules, counts the
-// token in and writes it; the others pass as if masked.  A chunk with more of them (the frequent words at the
-// front of a vocabulary) goes through the rules as a whole, and so does one with
-// tokens of the row's root path in it.
+// own in shared memory, the next chunk on its way.  Of a chunk's touched tokens (a few
+// percent of a vocabulary, but some lane of nearly every warp has one) up to 32 are
+// handed one to each lane, which takes the logit from the ring, applies the rules,
+// counts the token in and writes it; the others pass as if masked.  A chunk with more
+// of them (the frequent words at the front of a vocabulary) goes through the rules as a
+// whole, and so does one with tokens of the row's root path in it.
+//
+// Bound by HBM while the logits stream (at that pace three CTAs of an SM together would
+// take 9 TB/s), but half of a CTA's life goes into its rules, where it waits for memory
+// in turn: parameters, history and tree, the rows' first chunks.  Eight trees (358 rows)
+// at 128256 tokens 82 us, 4.55 TB/s; 71 without rules; 256 requests of one row 159 us.
 //
 // With x = z - m, m the warp's running maximum, each lane keeps s = sum e^x, u = sum
 // x e^x and the two sums at temperature T, rescaled when a chunk has a new maximum;
-// parts and slices join in shared memory and by the last CTA of the rows (an arrival
-// ticket), always in index order: outputs do not depend on the placement.
+// parts join in shared memory, slices by the last CTA of the rows (an arrival ticket) or
+// by k_logits_join, always in index order: outputs do not depend on the placement.
 //   top1 = 1 / s,  H = ln s - u / s,  ln Z_T = m / T + ln s_T
 // Penalties and biases are 32-bit operations in the documented order, each rounded
 // to nearest (nothing is contracted).  Where a chunk goes through them as a whole,
@@ -40,10 +45,11 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kVec = 4, kChunk = 128 * kVec;  // tokens a warp takes at a time: kVec groups of four per lane
 constexpr int kRows = kWarps;   // rows of a CTA
-constexpr int kMaxSlice = 3584;  // three CTAs per SM
+constexpr int kPerSm = 3;        // CTAs of an SM
+constexpr int kMaxSlice = 3584;  // kPerSm of them fit its shared memory
 constexpr int kMaxRowsCall = 65536;
 constexpr int kStages = 2;      // chunks of a warp's ring: one in work, the others on their way
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Part {
     float m;
@@ -62,7 +68,8 @@ struct LogitArgs {
     float *out;
     tb_logit_rules r;
     tb_logit_stats st;
-    float temperature, scale_t;  // scale_t = log2(e) / T
+    float temperature, inv_t;
+    bool join;  // by the last CTA of a piece's rows, else by k_logits_join
     int *ticket;                 // [pieces of rows]
     Part *parts;                 // [rows][slices]
 };
@@ -219,15 +226,77 @@ __device__ __forceinline__ int owner_of(const int32_t *row_start, int batch, int
     return lo;
 }
 
-// A row's statistics so far: the warp's maximum and where it is, this lane's sums.
+// A row's statistics so far: the warp's maximum and where it is, and this lane's sums over
+// the tokens of even and odd index, x in units of ln 2.
 struct Running {
-    float m, s, u, st, ut;
+    float m;
     int arg;
+    uint64_t s, u, st, ut;
 };
+
+// One warp joins the slices of a row and writes its statistics, and the draft tokens'
+// logits of its children.  The request's rows are row0 .. row1 - 1.
+template <int kStats>
+__device__ __forceinline__ void join_row(const LogitArgs &p, int row, int row0, int row1, const TreeDesc *td, int lane)
+{
+    const float inv_t = p.inv_t;
+    const Part *parts = p.parts + (size_t)row * p.slices;
+    Part a = empty_part();
+    for (int k0 = 0; k0 < p.slices; k0 += 64) {
+        Part x[2] = {empty_part(), empty_part()};
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+            if (k0 + 32 * y + lane < p.slices) {
+                const float4 *from = reinterpret_cast<const float4 *>(parts + k0 + 32 * y + lane);
+                reinterpret_cast<float4 *>(&x[y])[0] = __ldcg(from);
+                reinterpret_cast<float4 *>(&x[y])[1] = __ldcg(from + 1);
+            }
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+            a = combine(a, x[y], inv_t);
+    }
+    // the lanes' parts relative to the row's maximum, then plain sums
+    const float m = warp_max(a.m);
+    const unsigned arg = __reduce_min_sync(0xffffffffu, a.m == m ? (unsigned)a.arg : 0x7fffffffu);
+    Part top = empty_part();
+    top.m = m;
+    a = combine(a, top, inv_t);
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) {
+        a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+        a.u += __shfl_xor_sync(0xffffffffu, a.u, o);
+        a.st += __shfl_xor_sync(0xffffffffu, a.st, o);
+        a.ut += __shfl_xor_sync(0xffffffffu, a.ut, o);
+    }
+    if (lane == 0) {
+        // a row without an allowed token: sums 0 (NaN where its allowed logits are)
+        const bool none = !(m > -INFINITY);
+        const bool empty = none && a.s == 0.f;
+        if (p.st.argmax)
+            p.st.argmax[row] = none ? -1 : (int)arg;
+        if (p.st.top1)
+            p.st.top1[row] = empty ? 0.f : 1.f / a.s;
+        if (p.st.entropy)
+            p.st.entropy[row] = empty ? 0.f : logf(a.s) - a.u / a.s;
+        const float sT = kStats > 1 ? a.st : a.s, uT = kStats > 1 ? a.ut : a.u;
+        if (p.st.logz_t)
+            p.st.logz_t[row] = empty ? -INFINITY : __fdiv_rn(m, p.temperature) + logf(sT);
+        if (p.st.entropy_t)
+            p.st.entropy_t[row] = empty ? 0.f : logf(sT) - uT / sT;
+    }
+    // the draft tokens of the row's children
+    if (p.st.draft_logit && td && row - row0 < td->n)
+        for (int j = lane; j < min(td->n, row1 - row0); j += 32)
+            if (j > 0 && td->parent[j] == row - row0) {
+                const int v = p.r.draft[row0 + j];
+                if (v >= 0 && v < p.V)
+                    p.st.draft_logit[row0 + j] = __ldcg(p.out + row * p.out_stride + v);
+            }
+}
 
 // kStats: 0 none, 1 at temperature 1 only, 2 also at T
 template <int kType, int kStats>
-__global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ LogitArgs p)
+__global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_constant__ LogitArgs p)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Part s_part[kRows][kWarps];
@@ -288,8 +357,9 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
     g1 = min((g0 / kRows + 1) * kRows, row1);
     const int here = min(size, p.V - v0);  // tokens of the slice that exist
     // parts of a row: every warp has work where there are chunks enough
-    const int rows = g1 - g0, parts = kWarps / rows;
-    const int part_size = ((here + kChunk - 1) / kChunk + parts - 1) / parts * kChunk;
+    static_assert(kWarps == 8 && kRows == 8, "warps per row as powers of two");
+    const int rows = g1 - g0, parts_log2 = rows == 1 ? 3 : rows == 2 ? 2 : rows <= 4 ? 1 : 0, parts = 1 << parts_log2;
+    const int part_size = (((here + kChunk - 1) / kChunk + parts - 1) >> parts_log2) * kChunk;
     // the item (row, part) in work
     const T *src = nullptr;
     const int32_t *mask = nullptr;
@@ -345,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
     for (int i = threadIdx.x; i < min(n_said - kInRegs, kEarly); i += kThreads)
         copy_async<4>(early + i, h + kInRegs + i);
     asm volatile("cp.async.commit_group;" ::: "memory");
-    const int gr = warp / parts, part = warp - gr * parts;  // this warp's row and part of it
+    const int gr = warp >> parts_log2, part = warp & (parts - 1);  // this warp's row and part of it
     if (gr < rows) {
         row = g0 + gr;
         c_first = part * part_size;
@@ -391,8 +461,11 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");  // all but the logits
     __syncthreads();
 #pragma unroll
-    for (int m = 0; m < kAhead; ++m)
+    for (int m = 0; m < kAhead; ++m) {
+        if (m * kThreads >= n_said)
+            break;
         note_token(count, seen, (unsigned)(word_of[m] - v0), (unsigned)here, (int)threadIdx.x + m * kThreads >= n_asked);
+    }
 #pragma unroll 4
     for (int i = threadIdx.x; i < min(n_said - kInRegs, kEarly); i += kThreads)
         note_token(count, seen, (unsigned)(early[i] - v0), (unsigned)here, kInRegs + i >= n_asked);
@@ -475,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
     }
     const float *generated = reinterpret_cast<const float *>(count);
 
-    const float inv_t = 1.f / p.temperature;
+    const float inv_t = p.inv_t;
     if (gr < rows) {
         float *dst = p.out + row * p.out_stride + v0;
         const bool out_vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
@@ -490,17 +563,19 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
                     tok[h] = x;
             }
         }
-        Running a{-INFINITY, 0.f, 0.f, 0.f, 0.f, 0x7fffffff};
-        auto add = [&](float v, float mu) {
-            const float x = v - mu;
-            const float q = ex2_approx(x * kLog2e);
-            const float xc = fmaxf(x, -1e4f);  // finite where the weight is 0
-            a.s += q;
-            a.u = fmaf(q, xc, a.u);
+        Running a{-INFINITY, 0x7fffffff, 0, 0, 0, 0};
+        auto add = [&](float v0, float v1, float mu) {
+            const uint64_t y = mul_two(add_two(two(v0, v1), two(-mu, -mu)), two(kLog2e, kLog2e));
+            const float2 x = halves(y);
+            const uint64_t yc = two(fmaxf(x.x, -3e38f), fmaxf(x.y, -3e38f));  // finite where the weight is 0
+            const uint64_t q = two(ex2_approx(x.x), ex2_approx(x.y));
+            a.s = add_two(a.s, q);
+            a.u = fma_two(q, yc, a.u);
             if constexpr (kStats > 1) {
-                const float qt = ex2_approx(x * p.scale_t);
-                a.st += qt;
-                a.ut = fmaf(qt, xc, a.ut);
+                const float2 t = halves(mul_two(y, two(inv_t, inv_t)));
+                const uint64_t qt = two(ex2_approx(t.x), ex2_approx(t.y));
+                a.st = add_two(a.st, qt);
+                a.ut = fma_two(qt, yc, a.ut);
             }
         };
 #pragma unroll 1
@@ -541,14 +616,8 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
             const bool sparse = nl > 0 && nl <= 32 && !on_path;
             if (sparse) {
                 mine_at = lane < nl ? list[l0 + lane] - c : 0;
-                const int from = (mine_at & 127) >> 2, reg = (mine_at >> 7) * 4 + (mine_at & 3);
-#pragma unroll
-                for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float v = __shfl_sync(0xffffffffu, z[k][e], from);
-                        mine = reg == k * 4 + e ? v : mine;
-                    }
+                __syncwarp();  // the other lanes' copies have landed too
+                mine = In<kType>::one(in_ring || (in_vec && c + kChunk <= here) ? from + mine_at : src + c + mine_at);
                 mine = penalise<false>(mine, generated[c + mine_at], (seen[(c + mine_at) >> 5] >> (mine_at & 31)) & 1,
                                        bias[c + mine_at], pen);
                 const bool allowed = (__shfl_sync(0xffffffffu, word, mine_at >> 5) >> (mine_at & 31)) & 1;
@@ -658,13 +727,13 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
                                 arg = min(arg, (unsigned)(v0 + c + k * 128 + lane * 4 + e));
                     a.arg = (int)__reduce_min_sync(0xffffffffu, arg);
                     const float d = a.m == -INFINITY ? 0.f : a.m - m;  // (sums of nothing: 0)
-                    const float w = ex2_approx(d * kLog2e);
-                    a.u = w * (a.u + d * a.s);
-                    a.s *= w;
+                    const float dy = d * kLog2e, w = ex2_approx(dy);
+                    a.u = mul_two(two(w, w), fma_two(two(dy, dy), a.s, a.u));
+                    a.s = mul_two(two(w, w), a.s);
                     if constexpr (kStats > 1) {
-                        const float wt = ex2_approx(d * p.scale_t);
-                        a.ut = wt * (a.ut + d * a.st);
-                        a.st *= wt;
+                        const float wt = ex2_approx(dy * inv_t);
+                        a.ut = mul_two(two(wt, wt), fma_two(two(dy, dy), a.st, a.ut));
+                        a.st = mul_two(two(wt, wt), a.st);
                     }
                     a.m = m;
                 }
@@ -672,22 +741,22 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
 #pragma unroll
                 for (int k = 0; k < kVec; ++k)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        add(z[k][e], mu);
+                    for (int e = 0; e < 4; e += 2)
+                        add(z[k][e], z[k][e + 1], mu);
                 if (sparse)
-                    add(mine, mu);
+                    add(mine, -INFINITY, mu);
             }
         }
         if constexpr (kStats > 0) {
+            float sum[4] = {halves(a.s).x + halves(a.s).y, (halves(a.u).x + halves(a.u).y) * kLn2,
+                            halves(a.st).x + halves(a.st).y, (halves(a.ut).x + halves(a.ut).y) * kLn2};
 #pragma unroll
-            for (int o = 16; o >= 1; o >>= 1) {
-                a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
-                a.u += __shfl_xor_sync(0xffffffffu, a.u, o);
-                a.st += __shfl_xor_sync(0xffffffffu, a.st, o);
-                a.ut += __shfl_xor_sync(0xffffffffu, a.ut, o);
-            }
+            for (int o = 16; o >= 1; o >>= 1)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
             if (lane == 0)
-                s_part[gr][part] = Part{a.m, a.arg, a.s, a.u, a.st, a.ut * inv_t, {0, 0}};
+                s_part[gr][part] = Part{a.m, a.arg, sum[0], sum[1], sum[2], sum[3] * inv_t, {0, 0}};
         }
     }
     if (kStats == 0)
@@ -700,6 +769,8 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
             a = combine(a, s_part[threadIdx.x][k], inv_t);
         p.parts[(size_t)(g0 + threadIdx.x) * p.slices + slice] = a;
     }
+    if (!p.join)
+        return;
     // the last CTA of these rows joins their slices
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -713,70 +784,39 @@ __global__ void __launch_bounds__(kThreads, 3) k_logits(const __grid_constant__ 
     __syncthreads();
     if (!s_last)
         return;
-    if (warp < rows) {
-        const int row = g0 + warp;
-        const Part *parts = p.parts + (size_t)row * p.slices;
-        Part a = empty_part();
-        for (int k0 = 0; k0 < p.slices; k0 += 64) {
-            Part x[2] = {empty_part(), empty_part()};
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-                if (k0 + 32 * y + lane < p.slices) {
-                    const float4 *from = reinterpret_cast<const float4 *>(parts + k0 + 32 * y + lane);
-                    reinterpret_cast<float4 *>(&x[y])[0] = __ldcg(from);
-                    reinterpret_cast<float4 *>(&x[y])[1] = __ldcg(from + 1);
-                }
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-                a = combine(a, x[y], inv_t);
-        }
-        // the lanes' parts relative to the row's maximum, then plain sums
-        const float m = warp_max(a.m);
-        const unsigned arg = __reduce_min_sync(0xffffffffu, a.m == m ? (unsigned)a.arg : 0x7fffffffu);
-        Part top = empty_part();
-        top.m = m;
-        a = combine(a, top, inv_t);
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) {
-            a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
-            a.u += __shfl_xor_sync(0xffffffffu, a.u, o);
-            a.st += __shfl_xor_sync(0xffffffffu, a.st, o);
-            a.ut += __shfl_xor_sync(0xffffffffu, a.ut, o);
-        }
-        if (lane == 0) {
-            // a row without an allowed token: sums 0 (NaN where its allowed logits are)
-            const bool none = !(m > -INFINITY);
-            const bool empty = none && a.s == 0.f;
-            if (p.st.argmax)
-                p.st.argmax[row] = none ? -1 : (int)arg;
-            if (p.st.top1)
-                p.st.top1[row] = empty ? 0.f : 1.f / a.s;
-            if (p.st.entropy)
-                p.st.entropy[row] = empty ? 0.f : logf(a.s) - a.u / a.s;
-            const float sT = kStats > 1 ? a.st : a.s, uT = kStats > 1 ? a.ut : a.u;
-            if (p.st.logz_t)
-                p.st.logz_t[row] = empty ? -INFINITY : __fdiv_rn(m, p.temperature) + logf(sT);
-            if (p.st.entropy_t)
-                p.st.entropy_t[row] = empty ? 0.f : logf(sT) - uT / sT;
-        }
-        // the draft tokens of the row's children
-        if (p.st.draft_logit && td && row - row0 < td->n)
-            for (int j = lane; j < min(td->n, row1 - row0); j += 32)
-                if (j > 0 && td->parent[j] == row - row0) {
-                    const int v = p.r.draft[row0 + j];
-                    if (v >= 0 && v < p.V)
-                        p.st.draft_logit[row0 + j] = __ldcg(p.out + row * p.out_stride + v);
-                }
-    }
+    if (warp < rows)
+        join_row<kStats>(p, g0 + warp, row0, row1, td, lane);
+}
+
+// Where CTAs follow one another on an SM, each one's way to the ticket and back (its
+// stores have to land first) costs more than another launch: 256 requests of one row of
+// 128256 tokens 162 us with this kernel and 189 with the last CTA's join, 16 of them
+// 17.2 and 18.3.  Below that it is one launch less at the same time (10.4 us for a tree
+// of 26 nodes at 32000 tokens).
+template <int kStats>
+__global__ void __launch_bounds__(kThreads) k_logits_join(const __grid_constant__ LogitArgs p)
+{
+    const int lane = threadIdx.x & 31, row = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    pdl_wait();
+    pdl_trigger();
+    if (row >= p.n_rows)
+        return;
+    const int b = owner_of(p.row_start, p.batch, row, lane);
+    const int row0 = p.row_start[b], row1 = min(p.row_start[b + 1], p.n_rows);
+    if (row0 < 0 || row < row0 || row >= row1)  // nobody's row
+        return;
+    const int t = p.tree ? p.tree[b] : -1;
+    join_row<kStats>(p, row, row0, row1, t >= 0 && t < p.n_trees ? p.trees + t : nullptr, lane);
 }
 
 // The tokens of a slice.
 int slice_of(int batch, int n_rows, int vocab, int n_sm)
 {
-    // as many slices as give each SM four CTAs; longer ones scan a history less often
+    // as many slices as fill every SM once; longer ones scan a history less often
+    // (4 requests of one row of 128256 tokens: 11.6 us, 14.6 with a third more CTAs)
     const long long rows = (n_rows + batch - 1) / batch, groups = (rows + kRows - 1) / kRows;
     const long long per_slice = (long long)batch * groups;
-    const long long slices = (4ll * n_sm + per_slice - 1) / per_slice;
+    const long long slices = ((long long)kPerSm * n_sm + per_slice - 1) / per_slice;
     const long long size = (vocab + slices * kChunk - 1) / (slices * kChunk) * kChunk;
     return (int)(size > kMaxSlice ? kMaxSlice : size);
 }
@@ -826,7 +866,7 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
         return record_error(TB_EINVAL, "%s: logits / out NULL or not 16-byte aligned", fn);
     if ((const void *)out == logits && (dtype != TB_F32 || logit_stride != out_stride))
         return record_error(TB_EINVAL, "%s: in place with another type or stride", fn);
-    if (!(temperature > 0.f) || !std::isfinite(temperature))
+    if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature))
         return record_error(TB_EINVAL, "%s: temperature %g", fn, temperature);
     if (rules)
         a.r = *rules;
@@ -860,7 +900,7 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
     a.out = out;
     a.out_stride = out_stride;
     a.temperature = temperature;
-    a.scale_t = (float)(1.4426950408889634 / (double)temperature);
+    a.inv_t = 1.f / temperature;
     a.ticket = reinterpret_cast<int *>(static_cast<uint8_t *>(workspace) + 256);
     a.parts = reinterpret_cast<Part *>(static_cast<uint8_t *>(workspace) + kPartsOff);
     a.size = slice_of(req->batch, n_rows, vocab, n_sm);
@@ -876,9 +916,13 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
     const auto kernel = dtype == TB_F32    ? kernel_of<TB_F32>(stats_kind)
                         : dtype == TB_BF16 ? kernel_of<TB_BF16>(stats_kind)
                                            : kernel_of<TB_F16>(stats_kind);
+    const long long pieces = req->batch + (n_rows + kRows - 1) / kRows;
+    a.join = pieces * a.slices <= (long long)kPerSm * n_sm;
     cudaError_t e = allow_max_smem((const void *)kernel);
     if (e == cudaSuccess)
-        e = launch_kernel(kernel, dim3(req->batch + (n_rows + kRows - 1) / kRows, a.slices), dim3(kThreads), smem,
-                          (cudaStream_t)stream, true, a);
+        e = launch_kernel(kernel, dim3((unsigned)pieces, a.slices), dim3(kThreads), smem, (cudaStream_t)stream, true, a);
+    if (e == cudaSuccess && want && !a.join)
+        e = launch_kernel(stats_kind == 1 ? k_logits_join<1> : k_logits_join<2>, dim3((n_rows + kWarps - 1) / kWarps),
+                          dim3(kThreads), 0, (cudaStream_t)stream, true, a);
     return launch_result(e, fn);
 }

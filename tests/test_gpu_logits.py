@@ -222,3 +222,50 @@ def test_an_empty_list_of_biases(bank):
     s = Scene(17, [3, 0], 500, biases=0)
     assert s.btok.size == 0
     s.run(bank)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("hist_max", [4096, 4097, 6145, 8193, 21000])
+def test_long_histories_and_many_biases(bank, dtype, hist_max):
+    """Histories past what is fetched at once, prompts that end anywhere in them, hundreds of biases; ids at
+    the ends of their type."""
+    s = Scene(hist_max, [3, 0, 4], 1500, dtype, hist_max=hist_max, biases=900)
+    s.hist_len[:] = hist_max, hist_max - 1, hist_max
+    s.prompt[:] = hist_max // 3, hist_max - 2, 0
+    s.hist[:, ::97] = 2 ** 31 - 1
+    s.hist[:, ::89] = -2 ** 31
+    s.btok[::50] = 2 ** 31 - 1
+    s.btok[::61] = -2 ** 31
+    s.run(bank)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_more_work_than_the_gpu_holds(bank, dtype):
+    """Several CTAs per SM one after the other; the statistics as of the same rows alone."""
+    g = synth.rng(40)
+    s = Scene(41, [int(g.integers(-1, 4)) for _ in range(70)], 50001, dtype, hist_max=200)
+    s.run(bank)
+    whole = {k: v.clone() for k, v in s.st.items()}
+    one = Scene(41, s.tree, 50001, dtype, hist_max=200)
+    lo, hi = int(one.start[5]), int(one.start[8])
+    keep = [None] * 3
+    for i, b in enumerate((5, 6, 7)):
+        keep[i] = slice(one.bstart[b], one.bstart[b + 1])
+    one.tree, one.n, one.R = one.tree[5:8], one.n[5:8], hi - lo
+    one.start = one.start[5:9] - lo
+    one.logits, one.z, one.allowed, one.draft = one.logits[lo:hi], one.z[lo:hi], one.allowed[lo:hi], one.draft[lo:hi]
+    for k in ("hist", "hist_len", "prompt", "rep", "pres", "freq"):
+        setattr(one, k, getattr(one, k)[5:8])
+    one.btok, one.bval = (np.concatenate([x[k] for k in keep]) for x in (one.btok, one.bval))
+    one.bstart = one.bstart[5:9] - one.bstart[5]
+    one.logits = one.logits.clone(memory_format=torch.contiguous_format)
+    one.run(bank)
+    # other slices, other sums: the outputs are the same, the statistics within their own bounds
+    assert torch.equal(one.out, s.out[lo:hi]) and torch.equal(one.st["argmax"], whole["argmax"][lo:hi])
+
+
+@pytest.mark.parametrize("T", [0.01, 0.3, 50.0])
+def test_temperatures(bank, T):
+    s = Scene(18, [4, 2], 2500)
+    s.T = T
+    s.run(bank)

@@ -178,6 +178,7 @@ def test_refusals_of_attention(lib, s):
 def test_refusals_of_logits(lib, s):
     for T in (0.0, -1.0, float("nan"), float("inf")):
         refused(tv.TB_EINVAL, s.process, temperature=T)
+    refused(tv.TB_EINVAL, s.process, temperature=1e-39)  # 1 / T is no number
     refused(tv.TB_ECAPACITY, s.process, ws=s.lws[:-16])
     refused(tv.TB_EINVAL, s.process, history=torch.zeros(3, 4, dtype=torch.int32))
     refused(tv.TB_EINVAL, s.process, bias_start=torch.zeros(4, dtype=torch.int32))
