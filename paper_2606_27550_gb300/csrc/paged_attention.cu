@@ -30,8 +30,19 @@
 // are the softmax (two threads per row, half of a tile's columns each), 8-11 stage
 // the next unit's queries and write the finished unit's output.
 // TMEM columns: S0 [0, 128), S1 [128, 256), of each the halves' P on their first 32
-// columns, O [256, 256 + kD), Q0 [384, 384 + kD / 2), Q1 behind it.  Row r sits in lane 32 (r % 4) +
-// r / 4, so that few rows spread over the four SM sub-partitions.
+// columns, O [256, 256 + kD), Q0 [384, 384 + kD / 2), Q1 behind it.  Row
+// r sits in lane 32 (r % 4) + r / 4, so that few rows spread over the four SM
+// sub-partitions.
+//
+// Bound by HBM where rows are few (64 requests of one token, 8 kv heads of 128, prefixes
+// of 512 to 8192: 182 us, 6.37 TB/s, 94 % of a copy's bandwidth; 32 kv heads at 65536
+// keys 166 us, 95 %), by the softmax's chain per tile with 128 rows per kv head (two row
+// blocks of 64 nodes at 65536 keys: 75 us, 0.91 PFLOP/s; 2060 cycles a tile, 700 of them
+// for the weights, 260 for the exchange between the halves, 340 waiting for S), and by
+// the way to the first tile, unit boundaries and the join in short calls (9.3 us for a
+// tree of 7 nodes at 128 keys, 52 us for 32 heads at 16384 keys).  Eight ragged trees with capped scores
+// took 51.7 us with one softmax thread per row, 47.9 with two, 43.7 with packed pairs and
+// one reciprocal for four caps.
 #include "paged.cuh"
 
 #include <cuda_fp16.h>

@@ -325,7 +325,8 @@ __device__ void make_split(const PlanArgs &p, const Sums &s, int rows)
 }
 
 // Bound by latency: every CTA's chain is a handful of dependent loads (length, tree,
-// page id) and the sums; the first CTA's ends with the split.
+// page id) and the sums; the first CTA's ends with the split.  8 requests 6.9 us,
+// 1024 requests with 31000 rows 12.5 us.
 __global__ void __launch_bounds__(kThreads) k_paged_plan(const __grid_constant__ PlanArgs p)
 {
     extern __shared__ __align__(16) uint8_t smem[];
