@@ -17,7 +17,7 @@
 // Bound by HBM while the logits stream (at that pace three CTAs of an SM together would
 // take 9 TB/s), but half of a CTA's life goes into its rules, where it waits for memory
 // in turn: parameters, history and tree, the rows' first chunks.  Eight trees (358 rows)
-// at 128256 tokens 82 us, 4.55 TB/s; 71 without rules; 256 requests of one row 159 us.
+// at 128256 tokens 81 us, 4.6 TB/s; 71 without rules; 256 requests of one row 159 us.
 //
 // With x = z - m, m the warp's running maximum, each lane keeps s = sum e^x, u = sum
 // x e^x and the two sums at temperature T, rescaled when a chunk has a new maximum;
@@ -234,26 +234,53 @@ struct Running {
     uint64_t s, u, st, ut;
 };
 
+// The lane's parts k and k + 32 of a row, on their way.
+struct TwoParts {
+    Part x[2];
+};
+__device__ __forceinline__ TwoParts load_parts(const LogitArgs &p, int row, int k)
+{
+    TwoParts t{{empty_part(), empty_part()}};
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+        if (k + 32 * y < p.slices) {
+            const Part *from = p.parts + (size_t)row * p.slices + k + 32 * y;
+            float4 *to = reinterpret_cast<float4 *>(&t.x[y]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(to[h].x), "=f"(to[h].y), "=f"(to[h].z), "=f"(to[h].w)
+                             : "l"(reinterpret_cast<const float4 *>(from) + h)
+                             : "memory");
+        }
+    return t;
+}
+
 // One warp joins the slices of a row and writes its statistics, and the draft tokens'
-// logits of its children.  The request's rows are row0 .. row1 - 1.
+// logits of its children.  The request's rows are row0 .. row1 - 1; first: the lane's
+// parts from `lane` on.
 template <int kStats>
-__device__ __forceinline__ void join_row(const LogitArgs &p, int row, int row0, int row1, const TreeDesc *td, int lane)
+__device__ __forceinline__ void join_row(const LogitArgs &p, int row, int row0, int row1, const TreeDesc *td, int lane,
+                                         const TwoParts &first)
 {
     const float inv_t = p.inv_t;
-    const Part *parts = p.parts + (size_t)row * p.slices;
-    Part a = empty_part();
-    for (int k0 = 0; k0 < p.slices; k0 += 64) {
-        Part x[2] = {empty_part(), empty_part()};
+    // the draft tokens of the row's children
+    float draft_logit[2];
+    bool child[2] = {};
+    if (p.st.draft_logit && td) {
+        const int nodes = min(load_now(&td->n), row1 - row0);
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
-            if (k0 + 32 * y + lane < p.slices) {
-                const float4 *from = reinterpret_cast<const float4 *>(parts + k0 + 32 * y + lane);
-                reinterpret_cast<float4 *>(&x[y])[0] = __ldcg(from);
-                reinterpret_cast<float4 *>(&x[y])[1] = __ldcg(from + 1);
-            }
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-            a = combine(a, x[y], inv_t);
+        for (int h = 0; h < 2; ++h) {
+            const int j = lane + 32 * h, v = row0 + j < row1 ? load_now(p.r.draft + row0 + j) : -1;
+            const int8_t parent = td->parent[j];
+            child[h] = j > 0 && j < nodes && row - row0 < nodes && parent == row - row0 && v >= 0 && v < p.V;
+            draft_logit[h] = child[h] ? __ldcg(p.out + row * p.out_stride + v) : 0.f;
+        }
+    }
+    Part a = combine(first.x[0], first.x[1], inv_t);
+    for (int k = 64 + lane; k - lane < p.slices; k += 64) {
+        const TwoParts t = load_parts(p, row, k);
+        a = combine(combine(a, t.x[0], inv_t), t.x[1], inv_t);
     }
     // the lanes' parts relative to the row's maximum, then plain sums
     const float m = warp_max(a.m);
@@ -284,14 +311,10 @@ __device__ __forceinline__ void join_row(const LogitArgs &p, int row, int row0, 
         if (p.st.entropy_t)
             p.st.entropy_t[row] = empty ? 0.f : logf(sT) - uT / sT;
     }
-    // the draft tokens of the row's children
-    if (p.st.draft_logit && td && row - row0 < td->n)
-        for (int j = lane; j < min(td->n, row1 - row0); j += 32)
-            if (j > 0 && td->parent[j] == row - row0) {
-                const int v = p.r.draft[row0 + j];
-                if (v >= 0 && v < p.V)
-                    p.st.draft_logit[row0 + j] = __ldcg(p.out + row * p.out_stride + v);
-            }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (child[h])
+            p.st.draft_logit[row0 + lane + 32 * h] = draft_logit[h];
 }
 
 // kStats: 0 none, 1 at temperature 1 only, 2 also at T
@@ -785,13 +808,13 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
     if (!s_last)
         return;
     if (warp < rows)
-        join_row<kStats>(p, g0 + warp, row0, row1, td, lane);
+        join_row<kStats>(p, g0 + warp, row0, row1, td, lane, load_parts(p, g0 + warp, lane));
 }
 
 // Where CTAs follow one another on an SM, each one's way to the ticket and back (its
 // stores have to land first) costs more than another launch: 256 requests of one row of
 // 128256 tokens 162 us with this kernel and 189 with the last CTA's join, 16 of them
-// 17.2 and 18.3.  Below that it is one launch less at the same time (10.4 us for a tree
+// 17.2 and 18.3.  Below that it is one launch less at the same time (10.2 us for a tree
 // of 26 nodes at 32000 tokens).
 template <int kStats>
 __global__ void __launch_bounds__(kThreads) k_logits_join(const __grid_constant__ LogitArgs p)
@@ -801,12 +824,13 @@ __global__ void __launch_bounds__(kThreads) k_logits_join(const __grid_constant_
     pdl_trigger();
     if (row >= p.n_rows)
         return;
+    const TwoParts first = load_parts(p, row, lane);
     const int b = owner_of(p.row_start, p.batch, row, lane);
-    const int row0 = p.row_start[b], row1 = min(p.row_start[b + 1], p.n_rows);
+    const int row0 = load_now(p.row_start + b), row1 = min(load_now(p.row_start + b + 1), p.n_rows);
+    const int t = p.tree ? load_now(p.tree + b) : -1;
     if (row0 < 0 || row < row0 || row >= row1)  // nobody's row
         return;
-    const int t = p.tree ? p.tree[b] : -1;
-    join_row<kStats>(p, row, row0, row1, t >= 0 && t < p.n_trees ? p.trees + t : nullptr, lane);
+    join_row<kStats>(p, row, row0, row1, t >= 0 && t < p.n_trees ? p.trees + t : nullptr, lane, first);
 }
 
 // The tokens of a slice.
