@@ -7,17 +7,17 @@
 // often each token was generated, whether the prompt has it, its bias, and a
 // bitmap of the tokens that any rule touches.  A warp takes a row's slice (or a
 // part of it where there are few rows) in chunks of 512 tokens through a ring of its
-// own in shared memory, the next chunk on its way.  Of a chunk's touched tokens (a few
-// percent of a vocabulary, but some lane of nearly every warp has one) up to 32 are
-// handed one to each lane, which takes the logit from the ring, applies the rules,
-// counts the token in and writes it; the others pass as if masked.  A chunk with more
-// of them (the frequent words at the front of a vocabulary) goes through the rules as a
-// whole, and so does one with tokens of the row's root path in it.
+// own in shared memory, the next chunk on its way.  A chunk's touched tokens (a few
+// percent of a vocabulary, but some lane of nearly every warp has one) take the rules one
+// per lane, in shared memory, and so do the draft tokens on the row's root path that
+// lie in it; then every lane takes its sixteen logits.  (With the rules on all of a
+// chunk's logits wherever more than 32 were touched, eight trees at 128256 tokens took
+// 81 us.)
 //
 // Bound by HBM while the logits stream (at that pace three CTAs of an SM together would
 // take 9 TB/s), but half of a CTA's life goes into its rules, where it waits for memory
 // in turn: parameters, history and tree, the rows' first chunks.  Eight trees (358 rows)
-// at 128256 tokens 81 us, 4.6 TB/s; 71 without rules; 256 requests of one row 159 us.
+// at 128256 tokens 76 us, 4.9 TB/s; 68 without rules; 256 requests of one row 153 us.
 //
 // With x = z - m, m the warp's running maximum, each lane keeps s = sum e^x, u = sum
 // x e^x and the two sums at temperature T, rescaled when a chunk has a new maximum;
@@ -25,13 +25,7 @@
 // by k_logits_join, always in index order: outputs do not depend on the placement.
 //   top1 = 1 / s,  H = ln s - u / s,  ln Z_T = m / T + ln s_T
 // Penalties and biases are 32-bit operations in the documented order, each rounded
-// to nearest (nothing is contracted).  Where a chunk goes through them as a whole,
-// the division by the repetition penalty is Markstein's correction of a product with
-// its reciprocal y = RN(1/b): q = RN(a y), r = a - b q (exact in an FMA), RN(q + r y),
-// which is the correctly rounded quotient for any b but those whose significand is
-// all ones (P. Markstein, IBM J. Res. Dev. 34, 1990, theorem 8.2), as long as
-// nothing overflows or underflows on the way; such b, and chunks with operands
-// outside 2^-100 .. 2^100, divide plainly.
+// to nearest (nothing is contracted).
 #include "paged.cuh"
 
 #include <cuda_fp16.h>
@@ -61,7 +55,7 @@ struct Part {
 struct LogitArgs {
     const TreeDesc *trees;
     int n_trees, batch, n_rows, V, slices, size;  // size: tokens per slice
-    int ring_off, mask_off;                       // in the dynamic shared memory
+    int ring_off, mask_off, copy_off;             // in the dynamic shared memory
     const int32_t *tree, *row_start;
     const void *in;
     long long in_stride, out_stride;
@@ -132,7 +126,7 @@ struct In<TB_F16> {
 
 // The penalties of a request.
 struct Penalty {
-    float rep, inv, freq, pres;  // inv: 1 / rep, rounded
+    float rep, freq, pres;
 };
 
 // Loads that are issued where they stand: a CTA's life is short, and as a chain of
@@ -166,20 +160,11 @@ __device__ __forceinline__ void copy_async(void *dst, const void *src)
 }
 
 // The rules on one logit.  n: generated occurrences; seen: they or the prompt have
-// the token.  kShort: the quotient as above.
-template <bool kShort>
+// the token.
 __device__ __forceinline__ float penalise(float z, float n, bool seen, float bias, const Penalty &p)
 {
     const float b = seen ? p.rep : 1.f;
-    float div;
-    if constexpr (kShort) {
-        const float y = seen ? p.inv : 1.f;
-        const float q = __fmul_rn(z, y);
-        div = __fmaf_rn(__fmaf_rn(-q, b, z), y, q);
-    } else {
-        div = __fdiv_rn(z, b);
-    }
-    z = z > 0.f ? div : __fmul_rn(z, b);
+    z = z > 0.f ? __fdiv_rn(z, b) : __fmul_rn(z, b);
     z = __fsub_rn(z, __fmul_rn(p.freq, n));
     z = __fsub_rn(z, n > 0.f ? p.pres : 0.f);
     return __fadd_rn(z, bias);
@@ -341,6 +326,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
     constexpr int kEarly = kWarps * kChunk * sizeof(T) / 4;
     static_assert(kStages >= 2, "tokens of the history in the second stage");
     uint32_t *mask_ring = reinterpret_cast<uint32_t *>(smem + p.mask_off) + warp * kStages * (kChunk / 32);
+    float *copy = reinterpret_cast<float *>(smem + p.copy_off) + warp * kChunk;  // (16-bit logits only)
     const bool rules = p.r.history || p.r.bias_start;
     if (rules) {
         for (int x = threadIdx.x; x < size / 4; x += kThreads) {
@@ -471,9 +457,6 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
             node_tok = token;
         }
     }
-    pen.inv = __fdiv_rn(1.f, pen.rep);
-    // (see above for which divisors and, below, dividends the short quotient is right)
-    const bool short_div = pen.rep > 0x1p-20f && pen.rep < 0x1p20f && (__float_as_uint(pen.rep) & 0x7fffffu) != 0x7fffffu;
     __shared__ int s_sum[kWarps], s_again;
     if (threadIdx.x < TB_MAX_NODES) {
         s_anc[threadIdx.x] = node_anc;
@@ -560,7 +543,6 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
                 before[words] = (uint16_t)at;
             at -= __popc(mine);
             before[threadIdx.x] = (uint16_t)at;
-            touched[threadIdx.x] = mine;
             for (uint32_t rest = mine; rest; rest &= rest - 1) {
                 const int x = threadIdx.x * 32 + __ffs(rest) - 1;
                 list[at++] = (uint16_t)x;
@@ -608,7 +590,62 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
             fetch(c + (kStages - 1) * kChunk);
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
             const int st = ((c - c_first) / kChunk) % kStages;
-            const T *from = ring + st * (kWarps * kChunk);  // every lane reads what it copied
+            T *from = ring + st * (kWarps * kChunk);  // every lane reads what it copied
+            int l0 = 0, nl = 0;  // the chunk's touched tokens in the list
+            if (rules) {
+                l0 = before[c >> 5];
+                nl = before[(c + kChunk) >> 5] - l0;
+            }
+            const int o0 = tok[0] - c, o1 = tok[1] - c;
+            const bool in0 = (unsigned)o0 < (unsigned)kChunk, in1 = (unsigned)o1 < (unsigned)kChunk;
+            const bool on_path = paths && __any_sync(0xffffffffu, in0 || in1);
+            const bool touched_here = nl > 0 || on_path;
+            // the rules on the chunk's touched tokens, one per lane, in a 32-bit copy of it
+            const auto touch = [&](float *copy) {
+                __syncwarp();  // the other lanes' copies have landed
+                // tokens of the root path: up to two per lane, each once, with how often it comes up
+                int at[2] = {-1, -1}, more[2] = {0, 0}, n = 0;
+                float value[2];
+                if (on_path) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        for (unsigned with = __ballot_sync(0xffffffffu, h ? in1 : in0); with; with &= with - 1) {
+                            const int o = __shfl_sync(0xffffffffu, h ? o1 : o0, __ffs(with) - 1);
+                            const bool known = __any_sync(0xffffffffu, at[0] == o || at[1] == o);
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                if (!known && lane + 32 * y == n)
+                                    at[y] = o;
+                                more[y] += at[y] == o;
+                            }
+                            n += !known;
+                        }
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        if (at[y] >= 0) {
+                            const int x = c + at[y];
+                            value[y] = penalise(copy[at[y]], (rules ? generated[x] : 0.f) + (float)more[y], true,
+                                                rules ? bias[x] : 0.f, pen);
+                        }
+                    __syncwarp();
+                }
+                for (int i = lane; i < nl; i += 32) {
+                    const int x = list[l0 + i];
+                    copy[x - c] = penalise(copy[x - c], generated[x], (seen[x >> 5] >> (x & 31)) & 1, bias[x], pen);
+                }
+                __syncwarp();
+                if (on_path) {
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        if (at[y] >= 0)
+                            copy[at[y]] = value[y];
+                    __syncwarp();
+                }
+            };
+            if constexpr (sizeof(T) == 4) {
+                if (touched_here)
+                    touch(from);
+            }
             if (in_vec && c + kChunk <= here) {
 #pragma unroll
                 for (int k = 0; k < kVec; ++k) {
@@ -626,83 +663,21 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
             }
             if (mask && lane < kChunk / 32 && c + 32 * lane < here)
                 word = mask_ring[st * (kChunk / 32) + lane];
-            int l0 = 0, nl = 0;  // the chunk's touched tokens in the list
-            if (rules) {
-                l0 = before[c >> 5];
-                nl = before[min(c + kChunk, size) >> 5] - l0;
-            }
-            const int o0 = tok[0] - c, o1 = tok[1] - c;
-            const bool in0 = (unsigned)o0 < (unsigned)kChunk, in1 = (unsigned)o1 < (unsigned)kChunk;
-            const bool on_path = paths && __any_sync(0xffffffffu, in0 || in1);
-            float mine = -INFINITY;  // this lane's token of the list
-            int mine_at = 0;
-            const bool sparse = nl > 0 && nl <= 32 && !on_path;
-            if (sparse) {
-                mine_at = lane < nl ? list[l0 + lane] - c : 0;
-                __syncwarp();  // the other lanes' copies have landed too
-                mine = In<kType>::one(in_ring || (in_vec && c + kChunk <= here) ? from + mine_at : src + c + mine_at);
-                mine = penalise<false>(mine, generated[c + mine_at], (seen[(c + mine_at) >> 5] >> (mine_at & 31)) & 1,
-                                       bias[c + mine_at], pen);
-                const bool allowed = (__shfl_sync(0xffffffffu, word, mine_at >> 5) >> (mine_at & 31)) & 1;
-                mine = allowed && lane < nl ? mine : -INFINITY;
-                // the others go on as if these were masked
-                if (lane < kChunk / 32)
-                    word &= ~touched[(c >> 5) + lane];
-            } else if (on_path) {
-                uint32_t extra[kVec] = {};  // path occurrences of this lane's tokens, a byte each
-                for (int h = 0; h < 2; ++h)
-                    for (unsigned with = __ballot_sync(0xffffffffu, h ? in1 : in0); with; with &= with - 1) {
-                        const int o = __shfl_sync(0xffffffffu, h ? o1 : o0, __ffs(with) - 1);
+            if constexpr (sizeof(T) != 4) {
+                if (touched_here) {
+                    float4 *own = reinterpret_cast<float4 *>(copy) + lane;
 #pragma unroll
-                        for (int k = 0; k < kVec; ++k)
-                            if (o >> 7 == k && ((o & 127) >> 2) == lane)
-                                extra[k] += 1u << (8 * (o & 3));
-                    }
-#pragma unroll
-                for (int k = 0; k < kVec; ++k) {
-                    const int o = c + k * 128 + lane * 4;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int more = (extra[k] >> (8 * e)) & 0xff;
-                        const bool has = rules && ((seen[o >> 5] >> ((o & 31) + e)) & 1);
-                        const float n = rules ? generated[o + e] : 0.f;
-                        z[k][e] = penalise<false>(z[k][e], n + (float)more, has || more, rules ? bias[o + e] : 0.f, pen);
-                    }
-                }
-            } else if (nl > 0) {
-                float big = 0.f, small = 1.f;
-#pragma unroll
-                for (int k = 0; k < kVec; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        big = fmaxf(big, fabsf(z[k][e]));
-                        small = fminf(small, z[k][e] == 0.f ? 1.f : fabsf(z[k][e]));
-                    }
-                const bool plain = !short_div || big > 0x1p100f || small < 0x1p-100f;
-                if (__any_sync(0xffffffffu, plain)) {
+                    for (int k = 0; k < kVec; ++k)
+                        own[32 * k] = make_float4(z[k][0], z[k][1], z[k][2], z[k][3]);
+                    touch(copy);
 #pragma unroll
                     for (int k = 0; k < kVec; ++k) {
-                        const int o = c + k * 128 + lane * 4;
-                        const uint32_t s = seen[o >> 5] >> (o & 31);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            z[k][e] = penalise<false>(z[k][e], generated[o + e], (s >> e) & 1, bias[o + e], pen);
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < kVec; ++k) {
-                        const int o = c + k * 128 + lane * 4;
-                        const uint32_t s = seen[o >> 5] >> (o & 31);
-                        const float4 n = *reinterpret_cast<const float4 *>(generated + o);
-                        const float4 f = *reinterpret_cast<const float4 *>(bias + o);
-                        z[k][0] = penalise<true>(z[k][0], n.x, s & 1, f.x, pen);
-                        z[k][1] = penalise<true>(z[k][1], n.y, s & 2, f.y, pen);
-                        z[k][2] = penalise<true>(z[k][2], n.z, s & 4, f.z, pen);
-                        z[k][3] = penalise<true>(z[k][3], n.w, s & 8, f.w, pen);
+                        const float4 x = own[32 * k];
+                        z[k][0] = x.x, z[k][1] = x.y, z[k][2] = x.z, z[k][3] = x.w;
                     }
                 }
             }
-            if (mask || sparse) {
+            if (mask) {
 #pragma unroll
                 for (int k = 0; k < kVec; ++k) {
                     const uint32_t w = __shfl_sync(0xffffffffu, word, 4 * k + (lane >> 3)) >> (4 * (lane & 7));
@@ -726,13 +701,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
                             dst[o] = z[k][e];
                     }
             }
-            if (sparse) {
-                __syncwarp();
-                if (lane < nl)
-                    dst[c + mine_at] = mine;
-            }
             if constexpr (kStats > 0) {
-                float m = mine;
+                float m = -INFINITY;
 #pragma unroll
                 for (int k = 0; k < kVec; ++k)
 #pragma unroll
@@ -741,7 +711,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
                 m = warp_max(m);
                 if (m > a.m) {
                     // a new maximum: its lowest token, and the sums relative to it
-                    unsigned arg = mine == m ? (unsigned)(v0 + c + mine_at) : 0x7fffffffu;
+                    unsigned arg = 0x7fffffffu;
 #pragma unroll
                     for (int k = 0; k < kVec; ++k)
 #pragma unroll
@@ -766,8 +736,6 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
 #pragma unroll
                     for (int e = 0; e < 4; e += 2)
                         add(z[k][e], z[k][e + 1], mu);
-                if (sparse)
-                    add(mine, -INFINITY, mu);
             }
         }
         if constexpr (kStats > 0) {
@@ -814,7 +782,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
 // Where CTAs follow one another on an SM, each one's way to the ticket and back (its
 // stores have to land first) costs more than another launch: 256 requests of one row of
 // 128256 tokens 162 us with this kernel and 189 with the last CTA's join, 16 of them
-// 17.2 and 18.3.  Below that it is one launch less at the same time (10.2 us for a tree
+// 17.2 and 18.3.  Below that it is one launch less at the same time (9.7 us for a tree
 // of 26 nodes at 32000 tokens).
 template <int kStats>
 __global__ void __launch_bounds__(kThreads) k_logits_join(const __grid_constant__ LogitArgs p)
@@ -934,7 +902,8 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
     // count, bias, two bitmaps, the list and its offsets; then the rings
     a.ring_off = (a.size * 10 + a.size / 4 + a.size / 16 + 16 + 127) / 128 * 128;
     a.mask_off = a.ring_off + kWarps * kStages * kChunk * (dtype == TB_F32 ? 4 : 2);
-    const size_t smem = (size_t)a.mask_off + kWarps * kStages * (kChunk / 32) * 4;
+    a.copy_off = a.mask_off + kWarps * kStages * (kChunk / 32) * 4;
+    const size_t smem = (size_t)a.copy_off + (dtype == TB_F32 ? 0 : kWarps * kChunk * 4);
     const bool want = a.st.argmax || a.st.top1 || a.st.entropy || a.st.logz_t || a.st.entropy_t || a.st.draft_logit;
     const int stats_kind = !want ? 0 : (a.st.logz_t || a.st.entropy_t) && temperature != 1.f ? 2 : 1;
     const auto kernel = dtype == TB_F32    ? kernel_of<TB_F32>(stats_kind)

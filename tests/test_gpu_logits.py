@@ -269,3 +269,17 @@ def test_temperatures(bank, T):
     s = Scene(18, [4, 2], 2500)
     s.T = T
     s.run(bank)
+
+
+def test_a_long_root_path(bank, monkeypatch):
+    """64 nodes in a chain: more draft tokens in one chunk than a warp has lanes, some of them twice."""
+    trees = ref.trees() + [synth.chain(64)]
+    monkeypatch.setattr(ref, "trees", lambda: trees)
+    bid, _ = bank.add(trees[-1])
+    assert bid == len(trees) - 1
+    for dtype in (torch.float32, torch.bfloat16):
+        for V, rules in ((500, ("draft", "penalty")), (500, ("history", "penalty", "bias", "mask", "draft")),
+                         (60, ("history", "penalty", "draft")), (1300, ("bias", "draft", "penalty"))):
+            s = Scene(V, [bid, 5], V, dtype, hist_max=40)
+            s.draft = s.g.integers(-1, V + 1, s.R).astype(np.int32)
+            s.run(bank, rules)
