@@ -45,6 +45,12 @@ constexpr int kMaxRowsCall = 65536;
 constexpr int kStages = 2;      // chunks of a warp's ring: one in work, the others on their way
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// logits that a chunk's stage of the ring holds: 16-bit ones may begin and end in the middle of a word
+__host__ __device__ constexpr int stage_elems(int bytes)
+{
+    return bytes == 4 ? kChunk : kChunk + 8;
+}
+
 struct Part {
     float m;
     int arg;
@@ -320,10 +326,11 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
     uint16_t *before = reinterpret_cast<uint16_t *>(seen + size / 32);  // touched tokens before a word's
     uint16_t *list = before + size / 32 + 8;                            // the touched tokens, in order
     using T = typename In<kType>::T;
-    T *ring = reinterpret_cast<T *>(smem + p.ring_off) + warp * kChunk;  // a stage of all warps behind another
+    constexpr int kStage = stage_elems(sizeof(T));
+    T *ring = reinterpret_cast<T *>(smem + p.ring_off) + warp * kStage;  // a stage of all warps behind another
     // the second stage holds tokens of the history until the rules are built
-    int *early = reinterpret_cast<int *>(smem + p.ring_off + kWarps * kChunk * sizeof(T));
-    constexpr int kEarly = kWarps * kChunk * sizeof(T) / 4;
+    int *early = reinterpret_cast<int *>(smem + p.ring_off + kWarps * kStage * sizeof(T));
+    constexpr int kEarly = kWarps * kStage * sizeof(T) / 4;
     static_assert(kStages >= 2, "tokens of the history in the second stage");
     uint32_t *mask_ring = reinterpret_cast<uint32_t *>(smem + p.mask_off) + warp * kStages * (kChunk / 32);
     float *copy = reinterpret_cast<float *>(smem + p.copy_off) + warp * kChunk;  // (16-bit logits only)
@@ -373,25 +380,30 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
     const T *src = nullptr;
     const int32_t *mask = nullptr;
     int row = 0, c_first = 0, c_end = 0;
-    bool in_vec = false, in_ring = false;  // its chunks go through the ring (16-byte pieces, or 4-byte ones)
+    float *dst = nullptr;
+    bool vec = false;  // four logits at a time, in and out
+    int odd = 0;       // 16-bit logits from between two 32-bit words on
     auto fetch = [&](int c) {  // chunk c on its way; always one group of copies
         if (c < c_end) {
             const int st = ((c - c_first) / kChunk) % kStages;
-            T *to = ring + st * (kWarps * kChunk);
-            if (in_vec && c + kChunk <= here) {
+            T *to = ring + st * (kWarps * kStage);
+            if (vec && c + kChunk <= here) {
 #pragma unroll
                 for (int k = 0; k < kVec; ++k)
                     copy_async<4 * sizeof(T)>(to + k * 128 + lane * 4, src + c + k * 128 + lane * 4);
-            } else if (in_ring) {
-                if constexpr (sizeof(T) == 4) {
+            } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                    for (int k = 0; k < kVec; ++k)
+                for (int k = 0; k < 4 * kVec; ++k)
+                    if (c + 32 * k + lane < here)
+                        copy_async<4>(to + 32 * k + lane, src + c + 32 * k + lane);
+            } else {
+                // pairs of 16-bit logits, from the element before where the row begins between two
+                // (the tensor begins on 16 bytes); those that would end past the slice stay out
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int o = k * 128 + lane * 4 + e;
-                            if (c + o < here)
-                                copy_async<4>(to + o, src + c + o);
-                        }
+                for (int k = 0; k <= 2 * kVec; ++k) {
+                    const int o = 64 * k + 2 * lane - odd;
+                    if ((k < 2 * kVec || (lane == 0 && odd)) && c + o + 1 < here)
+                        copy_async<4>(to + o + odd, src + c + o);
                 }
             }
             if (mask && lane < kChunk / 32 && c + 32 * lane < here)
@@ -430,8 +442,9 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
         c_first = part * part_size;
         c_end = min(c_first + part_size, here);
         src = static_cast<const T *>(p.in) + row * p.in_stride + v0;
-        in_vec = (reinterpret_cast<uintptr_t>(src) & (4 * sizeof(T) - 1)) == 0;
-        in_ring = sizeof(T) == 4;
+        dst = p.out + row * p.out_stride + v0;
+        odd = sizeof(T) == 2 ? (int)(reinterpret_cast<uintptr_t>(src) >> 1) & 1 : 0;
+        vec = (reinterpret_cast<uintptr_t>(src) & (4 * sizeof(T) - 1)) == 0 && (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
         const int mrow = !p.r.mask ? -1 : p.r.mask_row ? p.r.mask_row[row] : row;
         mask = mrow >= 0 ? p.r.mask + mrow * p.r.mask_stride + (v0 >> 5) : nullptr;
         // on their way while the rules are built
@@ -555,8 +568,6 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
 
     const float inv_t = p.inv_t;
     if (gr < rows) {
-        float *dst = p.out + row * p.out_stride + v0;
-        const bool out_vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
         // the draft tokens on this row's root path, relative to the slice
         int tok[2] = {-1, -1};
         if (paths && row - row0 < TB_MAX_NODES) {
@@ -590,7 +601,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
             fetch(c + (kStages - 1) * kChunk);
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
             const int st = ((c - c_first) / kChunk) % kStages;
-            T *from = ring + st * (kWarps * kChunk);  // every lane reads what it copied
+            T *from = ring + st * (kWarps * kStage);  // 32-bit logits: every lane reads what it copied
             int l0 = 0, nl = 0;  // the chunk's touched tokens in the list
             if (rules) {
                 l0 = before[c >> 5];
@@ -646,38 +657,64 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
                 if (touched_here)
                     touch(from);
             }
-            if (in_vec && c + kChunk <= here) {
+            // a lane's logits: four in a row of each 128, or where that is not aligned (and at a slice's
+            // end) one of each 32: eight trees at 128255 tokens 87 us, 98 with four in a row one by one;
+            // bf16 107 us, 150 without the ring
+            const bool four = vec && c + kChunk <= here;
+            const int mine = four ? 4 * lane : lane, next = four ? 1 : 32;
+            if (four) {
 #pragma unroll
                 for (int k = 0; k < kVec; ++k) {
-                    const float4 x = In<kType>::four(from + k * 128 + lane * 4);
+                    const float4 x = In<kType>::four(from + k * 128 + mine);
                     z[k][0] = x.x, z[k][1] = x.y, z[k][2] = x.z, z[k][3] = x.w;
                 }
             } else {
+                if constexpr (sizeof(T) != 4)
+                    __syncwarp();  // other lanes' copies
 #pragma unroll
                 for (int k = 0; k < kVec; ++k)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int o = k * 128 + lane * 4 + e;
-                        z[k][e] = c + o < here ? In<kType>::one(in_ring ? from + o : src + c + o) : -INFINITY;
+                        const int o = k * 128 + e * 32 + lane;
+                        const bool landed = sizeof(T) == 4 || c + ((o + odd) | 1) - odd < here;
+                        z[k][e] = c + o < here ? In<kType>::one(landed ? from + o + odd : src + c + o) : -INFINITY;
                     }
+                if constexpr (sizeof(T) != 4)
+                    __syncwarp();
             }
             if (mask && lane < kChunk / 32 && c + 32 * lane < here)
                 word = mask_ring[st * (kChunk / 32) + lane];
             if constexpr (sizeof(T) != 4) {
                 if (touched_here) {
-                    float4 *own = reinterpret_cast<float4 *>(copy) + lane;
+                    if (four) {
 #pragma unroll
-                    for (int k = 0; k < kVec; ++k)
-                        own[32 * k] = make_float4(z[k][0], z[k][1], z[k][2], z[k][3]);
+                        for (int k = 0; k < kVec; ++k)
+                            *reinterpret_cast<float4 *>(copy + k * 128 + mine) =
+                                make_float4(z[k][0], z[k][1], z[k][2], z[k][3]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                copy[k * 128 + e * 32 + lane] = z[k][e];
+                    }
                     touch(copy);
+                    if (four) {
 #pragma unroll
-                    for (int k = 0; k < kVec; ++k) {
-                        const float4 x = own[32 * k];
-                        z[k][0] = x.x, z[k][1] = x.y, z[k][2] = x.z, z[k][3] = x.w;
+                        for (int k = 0; k < kVec; ++k) {
+                            const float4 x = *reinterpret_cast<const float4 *>(copy + k * 128 + mine);
+                            z[k][0] = x.x, z[k][1] = x.y, z[k][2] = x.z, z[k][3] = x.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < kVec; ++k)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                z[k][e] = copy[k * 128 + e * 32 + lane];
                     }
                 }
             }
-            if (mask) {
+            if (mask && four) {
 #pragma unroll
                 for (int k = 0; k < kVec; ++k) {
                     const uint32_t w = __shfl_sync(0xffffffffu, word, 4 * k + (lane >> 3)) >> (4 * (lane & 7));
@@ -685,18 +722,23 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
                     for (int e = 0; e < 4; ++e)
                         z[k][e] = (w >> e) & 1 ? z[k][e] : -INFINITY;
                 }
-            }
-            if (out_vec && c + kChunk <= here) {
+            } else if (mask) {
 #pragma unroll
                 for (int k = 0; k < kVec; ++k)
-                    *reinterpret_cast<float4 *>(dst + c + k * 128 + lane * 4) =
-                        make_float4(z[k][0], z[k][1], z[k][2], z[k][3]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        z[k][e] = (__shfl_sync(0xffffffffu, word, 4 * k + e) >> lane) & 1 ? z[k][e] : -INFINITY;
+            }
+            if (four) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k)
+                    *reinterpret_cast<float4 *>(dst + c + k * 128 + mine) = make_float4(z[k][0], z[k][1], z[k][2], z[k][3]);
             } else {
 #pragma unroll
                 for (int k = 0; k < kVec; ++k)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int o = c + k * 128 + lane * 4 + e;
+                        const int o = c + k * 128 + e * 32 + lane;
                         if (o < here)
                             dst[o] = z[k][e];
                     }
@@ -717,7 +759,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             if (z[k][e] == m)
-                                arg = min(arg, (unsigned)(v0 + c + k * 128 + lane * 4 + e));
+                                arg = min(arg, (unsigned)(v0 + c + k * 128 + mine + e * next));
                     a.arg = (int)__reduce_min_sync(0xffffffffu, arg);
                     const float d = a.m == -INFINITY ? 0.f : a.m - m;  // (sums of nothing: 0)
                     const float dy = d * kLog2e, w = ex2_approx(dy);
@@ -901,7 +943,8 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
         return record_error(TB_EUNSUPPORTED, "%s: vocab %d", fn, vocab);
     // count, bias, two bitmaps, the list and its offsets; then the rings
     a.ring_off = (a.size * 10 + a.size / 4 + a.size / 16 + 16 + 127) / 128 * 128;
-    a.mask_off = a.ring_off + kWarps * kStages * kChunk * (dtype == TB_F32 ? 4 : 2);
+    const int elem = dtype == TB_F32 ? 4 : 2;
+    a.mask_off = a.ring_off + kWarps * kStages * stage_elems(elem) * elem;
     a.copy_off = a.mask_off + kWarps * kStages * (kChunk / 32) * 4;
     const size_t smem = (size_t)a.copy_off + (dtype == TB_F32 ? 0 : kWarps * kChunk * 4);
     const bool want = a.st.argmax || a.st.top1 || a.st.entropy || a.st.logz_t || a.st.entropy_t || a.st.draft_logit;

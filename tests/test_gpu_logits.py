@@ -283,3 +283,13 @@ def test_a_long_root_path(bank, monkeypatch):
             s = Scene(V, [bid, 5], V, dtype, hist_max=40)
             s.draft = s.g.integers(-1, V + 1, s.R).astype(np.int32)
             s.run(bank, rules)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("V,pad,out_pad", [(5001, 0, 0), (5002, 0, 0), (5000, 1, 0), (5003, 4, 1), (4096, 2, 2), (513, 0, 3),
+                                           (511, 1, 1), (3585, 0, 0), (7170, 1, 0)])
+def test_rows_of_any_alignment(bank, dtype, V, pad, out_pad):
+    s = Scene(V + pad, [5, 3], V, dtype, pad=pad)
+    s.run(bank, out_pad=out_pad)
+    s.run(bank, ("mask",), out_pad=out_pad)
+    s.run(bank, (), out_pad=out_pad)
