@@ -135,27 +135,6 @@ struct Penalty {
     float rep, freq, pres;
 };
 
-// Loads that are issued where they stand: a CTA's life is short, and as a chain of
-// round trips its parameters, tokens and biases took longer than its logits.
-__device__ __forceinline__ int load_now(const int *p)
-{
-    int v;
-    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ float load_now(const float *p)
-{
-    float v;
-    asm volatile("ld.global.b32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint64_t load_now(const uint64_t *p)
-{
-    uint64_t v;
-    asm volatile("ld.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
-    return v;
-}
-
 template <int kBytes>
 __device__ __forceinline__ void copy_async(void *dst, const void *src)
 {

@@ -89,6 +89,27 @@ unsigned int bounds_violations_paged_attention();
 unsigned int bounds_violations_logits();
 unsigned int bounds_violations_paged_accept();
 
+// Loads that are issued where they stand: a short CTA's life is its round trips to
+// memory, and a compiler that moves a load behind the branch that uses it adds one.
+__device__ __forceinline__ int load_now(const int *p)
+{
+    int v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ float load_now(const float *p)
+{
+    float v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint64_t load_now(const uint64_t *p)
+{
+    uint64_t v;
+    asm volatile("ld.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+    return v;
+}
+
 // Two 32-bit floats in one instruction (softmax loops are bound by their issue slots).
 __device__ __forceinline__ uint64_t two(float lo, float hi)
 {

@@ -13,7 +13,8 @@
 //
 // A cluster of CTAs shares a request: each repeats the (tiny) acceptance, moves
 // its share of the pieces, and the first writes the length after all have read
-// it (one cluster barrier), so that the lengths may be advanced in place.
+// it (a cluster barrier whose halves lie before and behind the moves), so that the
+// lengths may be advanced in place.
 #include "paged.cuh"
 
 namespace tv {
@@ -21,7 +22,7 @@ namespace tv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCluster = 8;
+constexpr int kMaxCluster = 8;  // CTAs of a request
 constexpr int kAhead = 2, kPieces = 4;  // moves in flight per thread: kAhead of each of kPieces
 
 struct AcceptArgs {
@@ -32,7 +33,7 @@ struct AcceptArgs {
     int32_t *lens_out;
     uint16_t *k, *v;
     long long layer_stride, page_stride, head_stride, slot_stride;
-    int n_layers, n_pages, Hkv, d;
+    int n_layers, n_pages, Hkv, d, cluster_log2;
 };
 
 // What one request accepts; warp 0 of each CTA fills it in.
@@ -43,39 +44,53 @@ struct Accepted {
     long long src[TB_MAX_NODES];  // the same for slot L + path[j]
 };
 
-__device__ __forceinline__ long long slot_offset(const AcceptArgs &p, const int32_t *table, int slot)
-{
-    const int pg = slot >> p.page_log2;
-    if (pg >= p.max_pages)
-        return -1;
-    const int id = table[pg];
-    if (id < 0 || id >= p.n_pages)
-        return -1;
-    return id * p.page_stride + (slot & ((1 << p.page_log2) - 1)) * p.slot_stride;
-}
-
+// Two round trips: the request's lengths, then its tree, tokens and block table together.
 __device__ void accept_one(const AcceptArgs &p, int b, Accepted &a)
 {
     const int lane = threadIdx.x;
-    const int t = p.tree[b], L = p.lens[b], row0 = p.row_start[b], n_here = p.row_start[b + 1] - row0;
+    const int t = load_now(p.tree + b), L = load_now(p.lens + b);
+    const int row0 = load_now(p.row_start + b), n_here = load_now(p.row_start + b + 1) - row0;
     const bool tree_ok = t >= 0 && t < p.n_trees;
     const TreeDesc *td = p.trees + (tree_ok ? t : 0);
-    const int n = td->n;
+    const int n = load_now(&td->n);
+    const tb_result &r = p.results[b];
+    const int given = p.draft ? 0 : load_now(&r.accept_len);
+    uint64_t anc[2];
+    int par[2], dep[2], tok[2], best_tok[2], path[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = lane + 32 * h;
+        anc[h] = load_now(td->anc + i);
+        par[h] = td->parent[i];
+        dep[h] = td->depth[i];
+        const bool row = p.draft && row0 >= 0 && i < n_here && i < p.n_rows - row0;
+        tok[h] = row ? load_now(p.draft + row0 + i) : 0;
+        best_tok[h] = row ? load_now(p.argmax + row0 + i) : 0;
+        path[h] = p.draft ? 0 : load_now(r.path + i);
+    }
+    // the pages of slots L .. L + 63, one per lane
+    const int mask = (1 << p.page_log2) - 1, first = L >= 0 ? L >> p.page_log2 : 0, in_page = L & mask;
+    const int spanned = ((TB_MAX_NODES - 1) >> p.page_log2) + 2;
+    const int id = p.k && L >= 0 && lane < spanned && first + lane < p.max_pages
+                       ? load_now(p.table + (size_t)b * p.max_pages + first + lane)
+                       : -1;
+    const auto slot_offset = [&](int j) {  // by the whole warp
+        const int x = in_page + j, page = __shfl_sync(0xffffffffu, id, x >> p.page_log2);
+        return page < 0 || page >= p.n_pages ? -1ll : page * p.page_stride + (x & mask) * p.slot_stride;
+    };
+
     // a request that paged_plan gave no rows takes no part in the step
     const bool live = tree_ok && L >= 0 && row0 >= 0 && n_here == n && row0 + n <= p.n_rows;
     int len = 0, bonus = -1, status = t >= p.n_trees ? TB_EINVAL : TB_OK;
     if (live && p.draft) {
         bool match[2], badtok[2];
-        uint64_t anc[2];
-        int dep[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int i = lane + 32 * h, par = td->parent[i];
-            anc[h] = td->anc[i];
-            dep[h] = td->depth[i];
-            const int tok = i < n ? p.draft[row0 + i] : 0;
-            badtok[h] = i > 0 && i < n && (tok < 0 || tok >= p.vocab);
-            match[h] = i < n && (i == 0 || (!badtok[h] && tok == p.argmax[row0 + par]));
+            const int i = lane + 32 * h;
+            const int of_parent[2] = {__shfl_sync(0xffffffffu, best_tok[0], par[h] & 31),
+                                      __shfl_sync(0xffffffffu, best_tok[1], par[h] & 31)};
+            badtok[h] = i > 0 && i < n && (tok[h] < 0 || tok[h] >= p.vocab);
+            match[h] = i < n && (i == 0 || (!badtok[h] && tok[h] == (par[h] < 32 ? of_parent[0] : of_parent[1])));
         }
         const uint64_t m = (uint64_t)__ballot_sync(0xffffffffu, match[0]) |
                            ((uint64_t)__ballot_sync(0xffffffffu, match[1]) << 32);
@@ -99,19 +114,24 @@ __device__ void accept_one(const AcceptArgs &p, int b, Accepted &a)
             if ((on >> i) & 1)
                 a.path[__popcll(on & ((1ull << i) - 1))] = i;
         }
-        bonus = p.argmax[row0 + j];
+        bonus = __shfl_sync(0xffffffffu, j < 32 ? best_tok[0] : best_tok[1], j & 31);
     } else if (live) {
-        const tb_result &r = p.results[b];
-        len = min(max(r.accept_len, 0), n);
-        for (int j = lane; j < len; j += 32)
-            a.path[j] = min(max(r.path[j], j), n - 1);
+        len = min(max(given, 0), n);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (lane + 32 * h < len)
+                a.path[lane + 32 * h] = min(max(path[h], lane + 32 * h), n - 1);
     }
     __syncwarp();
     if (p.k && live) {
-        const int32_t *table = p.table + (size_t)b * p.max_pages;
-        for (int j = lane; j < len; j += 32) {
-            a.at[j] = slot_offset(p, table, L + j);
-            a.src[j] = a.path[j] == j ? -1 : slot_offset(p, table, L + a.path[j]);  // in place already: nothing moves
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = lane + 32 * h, from = j < len ? a.path[j] : j;
+            const long long at = slot_offset(j), src = slot_offset(from);
+            if (j < len) {
+                a.at[j] = at;
+                a.src[j] = from == j ? -1 : src;  // in place already: nothing moves
+            }
         }
     }
     if (lane == 0) {
@@ -122,47 +142,20 @@ __device__ void accept_one(const AcceptArgs &p, int b, Accepted &a)
     }
 }
 
-// Bound by the latency of the chain length, tree, tokens, block table, rows (one
-// request of two layers: 3.6 us); with many requests by the scattered 128- or
-// 256-byte rows, read and written (64 requests of 32 layers and 8 heads, 36 MB:
-// 10.3 us, 3.5 TB/s; 12.8 with a piece at a time per thread).
-__global__ void __launch_bounds__(kThreads) k_paged_accept(const __grid_constant__ AcceptArgs p)
+// This CTA's share of the accepted rows.
+__device__ __forceinline__ void move_rows(const AcceptArgs &p, const Accepted &a, int rank)
 {
-    __shared__ Accepted a;
-    pdl_wait();
-    pdl_trigger();
-    const int b = blockIdx.x / kCluster, rank = blockIdx.x % kCluster;
-    if (threadIdx.x < 32)
-        accept_one(p, b, a);
-    __syncthreads();
-    cluster_barrier();  // every CTA of the request has read its length and result
-    if (rank == 0) {
-        tb_result &r = p.results[b];
-        if (p.draft) {
-            if (threadIdx.x < TB_MAX_NODES)
-                r.path[threadIdx.x] = threadIdx.x < a.len ? a.path[threadIdx.x] : 0;
-            if (threadIdx.x == 0) {
-                r.accept_len = a.len;
-                r.bonus_token = a.bonus;
-                r.status = a.status;
-            }
-        }
-        if (threadIdx.x == 0) {
-            r.new_L = a.L + a.len;
-            p.lens_out[b] = a.L + a.len;
-        }
-    }
     if (!p.k || a.len < 2)
         return;
     // pieces: 16 bytes of one (layer, kv head, K or V), several per thread in flight
     const int per_head_log2 = p.d == 64 ? 3 : 4;
     const unsigned pieces = 2u * p.n_layers * p.Hkv << per_head_log2;  // < 2^30 (the host's check)
-    constexpr unsigned kStride = kCluster * kThreads;
-    for (unsigned x0 = rank * kThreads + threadIdx.x; x0 < pieces; x0 += kPieces * kStride) {
+    const unsigned stride = (unsigned)kThreads << p.cluster_log2;
+    for (unsigned x0 = rank * kThreads + threadIdx.x; x0 < pieces; x0 += kPieces * stride) {
         uint16_t *base[kPieces];
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const unsigned x = x0 + i * kStride, c = x & ((1u << per_head_log2) - 1), y = x >> per_head_log2;
+            const unsigned x = x0 + i * stride, c = x & ((1u << per_head_log2) - 1), y = x >> per_head_log2;
             const unsigned lv = y / (unsigned)p.Hkv, g = y - lv * (unsigned)p.Hkv;
             base[i] = x < pieces ? ((lv & 1) ? p.v : p.k) + (lv >> 1) * p.layer_stride + g * p.head_stride + 8 * c : nullptr;
         }
@@ -188,6 +181,40 @@ __global__ void __launch_bounds__(kThreads) k_paged_accept(const __grid_constant
                 for (int m = 0; m < kAhead; ++m)
                     if (at[m] >= 0 && base[i])
                         *reinterpret_cast<uint4 *>(base[i] + at[m]) = buf[i][m];
+        }
+    }
+}
+
+// Bound by the latency of the chain lengths, tree and tokens and table, rows (one
+// request of two layers: 2.75 us; 3.6 with each of these loads behind the one before);
+// with many requests by the scattered 128- or 256-byte rows, read and written (64
+// requests of 32 layers and 8 heads, 36 MB: 9.4 us, 3.8 TB/s; 512 of them 50 us, 5.0).
+__global__ void __launch_bounds__(kThreads) k_paged_accept(const __grid_constant__ AcceptArgs p)
+{
+    __shared__ Accepted a;
+    pdl_wait();
+    pdl_trigger();
+    const int b = blockIdx.x >> p.cluster_log2, rank = blockIdx.x & ((1 << p.cluster_log2) - 1);
+    if (threadIdx.x < 32)
+        accept_one(p, b, a);
+    __syncthreads();
+    cluster_arrive();  // this CTA has read the request's length and result
+    move_rows(p, a, rank);
+    cluster_wait();  // and so have the others, which frees them to be written
+    if (rank == 0) {
+        tb_result &r = p.results[b];
+        if (p.draft) {
+            if (threadIdx.x < TB_MAX_NODES)
+                r.path[threadIdx.x] = threadIdx.x < a.len ? a.path[threadIdx.x] : 0;
+            if (threadIdx.x == 0) {
+                r.accept_len = a.len;
+                r.bonus_token = a.bonus;
+                r.status = a.status;
+            }
+        }
+        if (threadIdx.x == 0) {
+            r.new_L = a.L + a.len;
+            p.lens_out[b] = a.L + a.len;
         }
     }
 }
@@ -250,7 +277,18 @@ extern "C" tb_status paged_accept(const tb_bank *bank, const tb_requests *req, c
     a.argmax = argmax;
     a.results = results;
     a.lens_out = lens_out;
-    return launch_result(launch_kernel_cluster(k_paged_accept, dim3(req->batch * kCluster), dim3(kThreads), 0,
-                                               (cudaStream_t)stream, true, kCluster, a),
+    // as many CTAs per request as it has rounds of pieces, or while there are SMs for them one piece per
+    // thread (512 requests of 8 layers: 16.6 us, 33 with 8 CTAs each; 8 of them 3.5 us, 4.3 with 2)
+    const int n_sm = device_sms(-1);
+    if (n_sm <= 0)
+        return record_error(TB_ECUDA, "%s: no current device", fn);
+    const long long pieces = a.k ? 2ll * a.n_layers * a.Hkv * (a.d / 8) : 0;
+    int cluster = 1;
+    while (cluster < kMaxCluster && cluster * kThreads * (req->batch * cluster < n_sm / 2 ? 1 : kPieces) < pieces)
+        cluster *= 2;
+    while ((1 << a.cluster_log2) < cluster)
+        ++a.cluster_log2;
+    return launch_result(launch_kernel_cluster(k_paged_accept, dim3(req->batch * cluster), dim3(kThreads), 0,
+                                               (cudaStream_t)stream, true, cluster, a),
                          fn);
 }

@@ -143,3 +143,18 @@ def test_bad_tokens_and_no_pages(bank):
         got = s.results[b].tolist()
         assert got[:4] == [k, bonus, s.lens[b] + k, tv.TB_EINVAL] and got[4:4 + k] == list(path)
     assert same(before[0], s.pools[0]) and same(before[1], s.pools[1])
+
+
+@pytest.mark.parametrize("layers,H", [(4, 4), (12, 4), (12, 8), (20, 8)])
+def test_requests_of_one_and_more_ctas(bank, layers, H):
+    """From one CTA per request to a cluster of eight; lengths in place."""
+    g = synth.rng(layers)
+    B = 90
+    lens, tree = [int(g.integers(0, 60)) for _ in range(B)], [int(g.integers(0, 11)) for _ in range(B)]
+    s = Scene(layers + H, lens, tree, layers, H, 128, 16, "heads", match=0.9)
+    paths = {b: s.expected(b)[1] for b in range(B)}
+    want = s.moved(paths)
+    tv.paged_accept(bank, s.req, tv.Pages(*s.pools), s.results, draft=i32(s.draft), argmax=i32(s.argmax), vocab=s.vocab)
+    torch.cuda.synchronize()
+    assert s.req.lens.tolist() == [L + len(paths[b]) for b, L in enumerate(lens)]
+    assert same(s.pools[0], want[0]) and same(s.pools[1], want[1])
