@@ -609,13 +609,14 @@ def _arr(t, kind, n: int, what: str) -> int | None:
 
 class Pages:
     """The paged cache: k and v shaped [n_layers][n_pages][n_kv_heads][page_size][head_dim],
-    views of any strides (multiples of 8, elements of a row contiguous), the same for both."""
+    views of any strides (multiples of 8, elements of a row contiguous), the same for both.
+    Which tensors they are is fixed; what they hold is read and written by every call."""
+
+    __slots__ = ("_k", "_v", "_c", "dtype")
+    k = property(lambda self: self._k)
+    v = property(lambda self: self._v)
 
     def __init__(self, k, v):
-        self.k, self.v = k, v
-
-    def as_c(self) -> TbPages:
-        k, v = self.k, self.v
         s, shape, dtype = k.stride(), k.shape, k.dtype
         if len(s) != 5 or s[4] != 1 or v.stride() != s or v.shape != shape or v.dtype is not dtype:
             raise ValueError("pages: k and v of one 5-D shape, type and strides, rows contiguous")
@@ -624,8 +625,11 @@ class Pages:
         kind = _KINDS.get(dtype, TB_F32)
         if kind == TB_F32:
             raise TypeError(f"pages: {dtype}, bfloat16 or float16 expected")
-        return TbPages(k.data_ptr(), v.data_ptr(), s[0], s[1], s[2], s[3], shape[0], shape[1], shape[2], shape[3],
-                       shape[4], kind)
+        self._k, self._v, self.dtype = k, v, dtype
+        self._c = TbPages(k.data_ptr(), v.data_ptr(), *s[:4], *shape, kind)
+
+    def as_c(self) -> TbPages:
+        return self._c
 
 
 @dataclass(frozen=True)
@@ -714,7 +718,7 @@ def paged_plan(bank, req: Requests, slots, positions, status, plan, pool: PagePo
 
 def _rows_of(t, rows: int, heads: int, d: int, dtype, what: str) -> TbRows:
     shape, s = t.shape, t.stride()
-    if len(s) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != d or s[2] != 1:
+    if len(s) != 3 or s[2] != 1 or shape[0] < rows or shape[1] != heads or shape[2] != d:
         raise ValueError(f"{what}: shape {tuple(shape)}, ({rows}, {heads}, {d}) expected, rows contiguous")
     if t.dtype is not dtype:
         raise TypeError(f"{what}: {t.dtype}, the pages' {dtype} expected")
@@ -725,8 +729,8 @@ def paged_kv_store(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None
                    rope_theta: float = 0.0, stream=None):
     """k, v [rows][n_kv_heads][head_dim] and q, q_out [rows][n_q_heads][head_dim] (views of any row
     and head strides); positions int32 [rows] or [axes][rows]; sections: pairs per axis (None: one axis)."""
-    c = pages.as_c()
-    rows, heads, H, d, dtype = slots.shape[0], 0, c.n_kv_heads, c.head_dim, pages.k.dtype
+    c, dtype = pages._c, pages.dtype
+    rows, heads, H, d = slots.shape[0], 0, c.n_kv_heads, c.head_dim
     ck, cv = _rows_of(k, rows, H, d, dtype, "k"), _rows_of(v, rows, H, d, dtype, "v")
     cq = co = rope = None
     if q is not None:
@@ -751,8 +755,8 @@ def paged_tree_attention(bank: Bank, req: Requests, pages: Pages, plan, q, out, 
                          scale: float | None = None, softcap: float = 0.0, slopes=None, lse=None, stream=None):
     """q, out [rows][n_q_heads][head_dim] of the pages' type; lse float [rows][n_q_heads]; slopes float [n_q_heads];
     scale: 1 / sqrt(head_dim) unless given."""
-    c = pages.as_c()
-    shape, dtype = q.shape, pages.k.dtype
+    c, dtype = pages._c, pages.dtype
+    shape = q.shape
     rows, heads, d = shape
     if (q.dtype is not dtype or out.dtype is not dtype or out.shape != shape or d != c.head_dim or
             not q.is_contiguous() or not out.is_contiguous()):
@@ -823,7 +827,7 @@ def paged_accept(bank: Bank, req: Requests, pages, results, draft=None, argmax=N
     """results int32 [B][68] (make_results); draft, argmax int32 [rows], or draft None to move by the results given;
     lens_out: None for lens itself; pages None: nothing to move."""
     r = req._c
-    c = None if pages is None else pages.as_c()
+    c = None if pages is None else pages._c
     rows = 0x7FFFFFFF if draft is None else min(draft.shape[0], argmax.shape[0])
     rc = load().paged_accept(bank.handle, ctypes.byref(r), _ref(c), _arr(draft, _I32, 0, "draft"),
                              _arr(argmax, _I32, 0, "argmax"), rows, vocab,
