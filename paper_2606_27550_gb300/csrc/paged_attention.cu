@@ -38,7 +38,8 @@
 // of 512 to 8192: 182 us, 6.37 TB/s, 94 % of a copy's bandwidth; 32 kv heads at 65536
 // keys 166 us, 95 %), by the softmax's chain per tile with 128 rows per kv head (two row
 // blocks of 64 nodes at 65536 keys: 75 us, 0.91 PFLOP/s; 2060 cycles a tile, 700 of them
-// for the weights, 260 for the exchange between the halves, 340 waiting for S), and by
+// for the weights, 260 for the exchange between the halves, 340 waiting for S, whose
+// 16 MMAs with P V take over 100 cycles each), and by
 // the way to the first tile, unit boundaries and the join in short calls (9.3 us for a
 // tree of 7 nodes at 128 keys, 52 us for 32 heads at 16384 keys).  Eight ragged trees with capped scores
 // took 51.7 us with one softmax thread per row, 47.9 with two, 43.7 with packed pairs and
