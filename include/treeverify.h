@@ -572,7 +572,9 @@ typedef struct tb_requests {
 /* The free pages: a ring of n_pages page ids in device memory, of which the
  * state[1] ids from position state[0] on (cyclically) are free; held[b] is the
  * number of pages that request b holds.  state_out / held_out receive the
- * values after the call; each may be the input array itself. */
+ * values after the call; each may be the input array itself.  With ring, state,
+ * state_out and held_out all NULL (n_pages is then not read) no page changes
+ * hands: the form for a step's further plans, see paged_plan. */
 typedef struct tb_page_pool {
     int32_t n_pages;
     int32_t reserved;          /* 0 */
@@ -592,7 +594,8 @@ TB_API size_t tb_paged_plan_size(int batch, int device);
  * Requests with need > held take pages off the front of the ring, in request
  * order; those with need < held give the last ones back to its end, in
  * (request, page) order.  pool == NULL: the table is the caller's and already
- * complete.  Written:
+ * complete for every request.  A pool of `held` alone: no page is taken or given
+ * back, and a request with need > held gets nothing.  Written:
  *   row_start [batch + 1]; per row (max_rows entries, -1 / 0 past the last row):
  *   slots     int64  page * page_size + slot in the page
  *   positions int32  lens[b] + depth(node) (lens[b] + i without trees)
@@ -600,13 +603,18 @@ TB_API size_t tb_paged_plan_size(int batch, int device);
  *             (no rows, no pages taken or given): TB_EINVAL for an unknown
  *             tree or a negative length, TB_ECAPACITY when it needs more than
  *             max_pages, its rows do not fit max_rows, or the ring has run out
- *             (then later requests that need pages get none either)
+ *             (then later requests that need pages get none either; without a
+ *             ring, those that need more than they hold)
  *   plan      the attention's work split for n_q_heads / n_kv_heads, window and
  *             sink (0, 0: none; see paged_tree_attention), read by
  *             paged_tree_attention calls of this step; a model whose layers
- *             differ in them makes one plan for each kind (pool NULL for the
- *             second).  n_q_heads = 0: no attention follows.  At most 64 query
- *             heads per kv head (TB_EUNSUPPORTED).
+ *             differ in them makes one plan for each kind, the first with the
+ *             pool and the others with what the first left in held_out as `held`
+ *             alone: they then refuse the requests that the first refused and
+ *             write the same row_start, slots and positions.  (With pool NULL
+ *             they would give rows to a request that got no pages.)  n_q_heads =
+ *             0: no attention follows.  At most 64 query heads per kv head
+ *             (TB_EUNSUPPORTED).
  * One kernel. */
 TB_API tb_status paged_plan(const tb_bank *bank, const tb_requests *req, const tb_page_pool *pool, int64_t *slots,
                             int32_t *positions, int max_rows, int32_t *status, int n_q_heads, int n_kv_heads,

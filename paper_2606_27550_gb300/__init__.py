@@ -663,7 +663,8 @@ class Requests:
 @dataclass
 class PagePool:
     """The free pages (device int32 tensors): ring [n_pages], state [2] = (first, free), held [B];
-    state_out / held_out receive the new values (None: in place)."""
+    state_out / held_out receive the new values (None: in place).  ring and state None: no page
+    changes hands (see held_only)."""
 
     ring: object
     state: object
@@ -671,9 +672,17 @@ class PagePool:
     state_out: object = None
     held_out: object = None
 
+    def held_only(self) -> PagePool:
+        """The pool for the further plans of a step: what the first one left with every request.  They
+        refuse what the first refused, and write the same rows."""
+        return PagePool(None, None, self.held if self.held_out is None else self.held_out)
+
     def as_c(self, batch: int) -> TbPagePool:
         state = _arr(self.state, _I32, 2, "state")
         held = _arr(self.held, _I32, batch, "held")
+        if self.ring is None:
+            return TbPagePool(0, 0, None, state, _arr(self.state_out, _I32, 2, "state_out"), held,
+                              _arr(self.held_out, _I32, batch, "held_out"))
         n = self.ring.numel()
         return TbPagePool(n, 0, _arr(self.ring, _I32, n, "ring"), state,
                           state if self.state_out is None else _arr(self.state_out, _I32, 2, "state_out"), held,

@@ -353,18 +353,20 @@ __global__ void __launch_bounds__(kThreads) k_paged_plan(const __grid_constant__
     }
     for (int b = tid; b < B; b += kThreads) {
         const int len = p.lens[b], tree = p.tree ? p.tree[b] : -1;
-        int n = p.tree ? 0 : p.n_new[b], held = pool ? p.held[b] : 0;
+        int n = p.tree ? 0 : p.n_new[b], held = p.held ? p.held[b] : 0;
         if (tree >= 0 && tree < p.n_trees)
             n = p.trees[tree].n;
         const bool ok = len >= 0 && n >= 0 && tree >= -1 && tree < p.n_trees && held >= 0 && held <= p.max_pages;
         const long long want = ok ? ((long long)len + n + (1ll << p.page_log2) - 1) >> p.page_log2 : 0;
         const int bad = !ok ? TB_EINVAL : want > p.max_pages ? TB_ECAPACITY : TB_OK;
-        held = pool ? min(max(held, 0), p.max_pages) : bad ? 0 : (int)want;
+        // without `held` every page is there; with it but no ring, no page changes hands, so that a request
+        // which needs more than it holds is refused as one that the ring has nothing left for
+        held = p.held ? min(max(held, 0), p.max_pages) : bad ? 0 : (int)want;
         s.len[b] = len;
         s.tree[b] = tree;
         s.n[b] = bad ? 0 : n;
         s.held[b] = held;
-        s.need[b] = bad ? held : (int)want;
+        s.need[b] = bad ? held : pool ? (int)want : max((int)want, held);
         s.order[b] = bad;  // the status, until the split sorts
     }
     __syncthreads();
@@ -550,8 +552,9 @@ extern "C" tb_status paged_plan(const tb_bank *bank, const tb_requests *req, con
     if ((st = check_workspace(plan, plan_bytes, plan_bytes_for(req->batch), fn)) != TB_OK)
         return st;
     if (pool) {
-        if (pool->n_pages < 1 || pool->n_pages > 1 << 30 || !pool->ring || !pool->state || !pool->state_out ||
-            !pool->held || !pool->held_out)
+        const bool held_only = !pool->ring && !pool->state && !pool->state_out && !pool->held_out;
+        if (!pool->held || (!held_only && (pool->n_pages < 1 || pool->n_pages > 1 << 30 || !pool->ring ||
+                                           !pool->state || !pool->state_out || !pool->held_out)))
             return record_error(TB_EINVAL, "%s: pool of %d pages or with a NULL pointer", fn, pool->n_pages);
         a.n_pages = pool->n_pages;
         a.ring = pool->ring;

@@ -181,3 +181,34 @@ def test_on_another_stream_and_in_a_graph(bank):
     graph.replay()
     torch.cuda.synchronize()
     check(s, got, max_rows, False, False)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("free,rows_share", [(None, 1.0), (5, 1.0), (0, 1.0), (5, 0.5), (None, 0.3)])
+def test_a_further_plan_of_a_step_serves_the_same_requests(bank, in_place, free, rows_share):
+    """Two plans of one step, the ring or the rows running out in the first: the second refuses the same requests,
+    takes and gives nothing, and lays the same rows out."""
+    s = scene(70, 40, 16)
+    s["tree"][3], s["n"][3], s["lens"][17] = 99, 0, -1
+    if free is not None:
+        s["state"] = (s["state"][0], free)
+    max_rows = max(1, int(sum(s["n"]) * rows_share))
+    got = run(s, max_rows, False, in_place, bank)
+    check(s, got, max_rows, False, in_place, bad=(3,))
+    req, p, slots, positions, status, plan = got
+    first = [t.clone() for t in (req.row_start, slots, positions, status, req.table, p.ring)]
+    held = (p.held if in_place else p.held_out).clone()
+    # the reference, with what the requests hold by now and nothing in the ring
+    want = ref.plan(s["lens"], s["n"], held.tolist(), (0, 0), p.ring.cpu().numpy(), req.table.cpu().numpy(), 16, max_rows,
+                    (3,))
+    for t in (req.row_start, slots, positions, status):
+        t.fill_(-77)
+    other = tv.make_paged_plan(len(s["lens"]))
+    tv.paged_plan(bank, req, slots, positions, status, other, pool=p.held_only(), n_q_heads=8, n_kv_heads=4, window=50)
+    assert status.tolist() == want[0] and req.row_start.tolist() == want[1].tolist()
+    assert slots.tolist() == want[2].tolist()
+    for t, was in zip((req.row_start, slots, positions, status, req.table, p.ring), first):
+        assert torch.equal(t, was)
+    assert torch.equal(p.held if in_place else p.held_out, held) and want[4] == held.tolist()
+    if free == 0:
+        assert tv.TB_ECAPACITY in status.tolist()

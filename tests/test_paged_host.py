@@ -226,3 +226,14 @@ def test_another_devices_bank_is_refused(lib, s):
     finally:
         lib.fake_set_device(0)
     assert fake_cuda.launches(lib) == []
+
+
+def test_a_pool_of_what_is_held_alone(lib, s):
+    """The form of a step's further plans launches; any other pool without a ring, or without `held`, is refused."""
+    s.do_plan(pool=s.pool.held_only())
+    assert len(fake_cuda.launches(lib)) == 1
+    z = torch.zeros(3, dtype=torch.int32)
+    for bad in (tv.PagePool(None, z, z), tv.PagePool(None, None, z, state_out=z), tv.PagePool(None, None, z, held_out=z),
+                tv.PagePool(None, None, None), tv.PagePool(z, None, z), tv.PagePool(z, z, None)):
+        refused(tv.TB_EINVAL, s.do_plan, pool=bad)
+    assert fake_cuda.launches(lib) == []
