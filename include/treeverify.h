@@ -658,7 +658,7 @@ TB_API tb_status paged_kv_store(const tb_pages *pages, int layer, const int64_t 
  *   z = cap(scale q.k) - slopes[h] (pos(i) - pos(s)),  cap(x) = softcap tanh(x / softcap)
  *   out[r, h] = sum_s softmax_s(z) v[s],  lse[r, h] = ln sum_s e^z
  * (softcap 0: no cap; slopes NULL: no bias).  A row that sees nothing gets out
- * 0 and lse -inf.  Keys that no row of a request may see do not reach its
+ * 0 and lse -inf; one with a visible score of NaN or +inf gets NaN in both.  Keys that no row of a request may see do not reach its
  * outputs, whatever their pages hold (NaN and infinities included); the values
  * of slots that some rows see and others do not have to be finite.  A capped
  * score is right to softcap 2^-20, so that softcap may be 1024 at most.

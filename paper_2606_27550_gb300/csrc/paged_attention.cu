@@ -767,7 +767,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 break;
             tc_fence_after();
             const bool whole = now.n == now.T;
-            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const float inv = l == 0.f ? 0.f : 1.f / l;  // a NaN stays one
             uint4 *dst = reinterpret_cast<uint4 *>(p.out + now.row * kD);
             float *slot = p.part + ((size_t)c * 2 + (now.first ? 0 : 1)) * kSlot;
             float4 *pdst = reinterpret_cast<float4 *>(slot + rloc * kD);
@@ -803,7 +803,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             }
             if (now.valid && whole) {
                 if (p.lse)
-                    p.lse[now.row] = l > 0.f ? (m_ref + log2f(l)) * kLn2 : -INFINITY;
+                    p.lse[now.row] = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * kLn2;
             } else if (now.valid) {
                 slot[128 * kD + rloc] = m_ref;
                 slot[128 * kD + 128 + rloc] = l;
@@ -915,14 +915,14 @@ __global__ void __launch_bounds__(256, 2) k_paged_merge(const __grid_constant__ 
         }
         if (!live)
             continue;
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const size_t row = (size_t)(s.row0 + node) * p.Hq + qh;
         uint2 *dst = reinterpret_cast<uint2 *>(p.out + row * kD) + sub;
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
             dst[8 * i] = make_uint2(pack<kF16>(acc[i].x * inv, acc[i].y * inv), pack<kF16>(acc[i].z * inv, acc[i].w * inv));
         if (p.lse && sub == 0)
-            p.lse[row] = sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
+            p.lse[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
     }
 }
 

@@ -293,3 +293,32 @@ def test_a_query_that_is_not_a_number_shows(bank):
     assert np.isnan(got[3, 1]).all()
     got[3, 1] = want[3, 1]
     assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("form", ["plain", "cap", "bias"])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("L", [70, 9000])
+def test_a_score_that_is_not_finite_shows_in_the_log_sum_exp(bank, form, dtype, L):
+    """NaN in a query, NaN in one visible key, a score of +inf: output and log-sum-exp of those rows are NaN, in units
+    of one CTA and of several, and all others are as they were."""
+    s = Scene(L, [L], [3], 4, 2, 64, 16, dtype=dtype)
+    kw = dict(cap=30.0 if form == "cap" else 0.0, slopes=torch.full((4,), 0.02, device="cuda") if form == "bias" else None)
+    want, want_lse = s.run(bank, **kw)
+    assert np.isfinite(want).all() and np.isfinite(want_lse).all()
+    kept = s.q.clone()
+    for value in (float("nan"), float("inf")):
+        if value == float("inf") and form == "cap":
+            continue  # capped: a finite score
+        s.q.copy_(kept)
+        s.q[2, 1, 5] = value  # +inf times a key of either sign: +inf, -inf and so NaN among the scores
+        got, lse = s.run(bank, **kw)
+        assert np.isnan(got[2, 1]).all() and np.isnan(lse[2, 1])
+        got[2, 1], lse[2, 1] = want[2, 1], want_lse[2, 1]
+        assert np.array_equal(got, want) and np.array_equal(lse, want_lse)
+    # one key of head 0, in the prefix: every row of its two query heads
+    s.q.copy_(kept)
+    slot = L // 2
+    s.pages.k[0, int(s.table[0, slot // 16]), 0, slot % 16, 9] = float("nan")
+    got, lse = s.run(bank, **kw)
+    assert np.isnan(got[:, :2]).all() and np.isnan(lse[:, :2]).all()
+    assert np.array_equal(got[:, 2:], want[:, 2:]) and np.array_equal(lse[:, 2:], want_lse[:, 2:])
