@@ -44,6 +44,10 @@ constexpr int kMaxSlice = 3584;  // kPerSm of them fit its shared memory
 constexpr int kMaxRowsCall = 65536;
 constexpr int kStages = 2;      // chunks of a warp's ring: one in work, the others on their way
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// How far below a row's maximum a part's maximum counts as: its weight is 0 long before, but a
+// difference that overflows (a part of nothing but the type's lowest value, which stands for "masked"
+// in many models' logits, or a temperature near 0) would make 0 x inf of it.
+constexpr float kFar = -1e30f;
 
 // logits that a chunk's stage of the ring holds: 16-bit ones may begin and end in the middle of a word
 __host__ __device__ constexpr int stage_elems(int bytes)
@@ -87,11 +91,12 @@ __device__ __forceinline__ Part combine(const Part &a, const Part &b, float inv_
     o.m = take_b ? b.m : a.m;
     o.arg = take_b ? b.arg : a.arg;
     // the sums of an empty part are 0 (or NaN), whatever its weight
-    const float da = a.m == -INFINITY ? 0.f : a.m - o.m, db = b.m == -INFINITY ? 0.f : b.m - o.m;
+    const float da = a.m == -INFINITY ? 0.f : fmaxf(a.m - o.m, kFar);
+    const float db = b.m == -INFINITY ? 0.f : fmaxf(b.m - o.m, kFar);
     const float wa = ex2_approx(da * kLog2e), wb = ex2_approx(db * kLog2e);
     o.s = wa * a.s + wb * b.s;
     o.u = wa * (a.u + da * a.s) + wb * (b.u + db * b.s);
-    const float ta = da * inv_t, tb = db * inv_t;
+    const float ta = fmaxf(da * inv_t, kFar), tb = fmaxf(db * inv_t, kFar);
     const float va = ex2_approx(ta * kLog2e), vb = ex2_approx(tb * kLog2e);
     o.st = va * a.st + vb * b.st;
     o.ut = va * (a.ut + ta * a.st) + vb * (b.ut + tb * b.st);
@@ -741,7 +746,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
                                 arg = min(arg, (unsigned)(v0 + c + k * 128 + mine + e * next));
                     a.arg = (int)__reduce_min_sync(0xffffffffu, arg);
                     const float d = a.m == -INFINITY ? 0.f : a.m - m;  // (sums of nothing: 0)
-                    const float dy = d * kLog2e, w = ex2_approx(dy);
+                    const float dy = fmaxf(d * kLog2e, kFar), w = ex2_approx(dy);
                     a.u = mul_two(two(w, w), fma_two(two(dy, dy), a.s, a.u));
                     a.s = mul_two(two(w, w), a.s);
                     if constexpr (kStats > 1) {

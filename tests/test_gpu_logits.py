@@ -293,3 +293,34 @@ def test_rows_of_any_alignment(bank, dtype, V, pad, out_pad):
     s.run(bank, out_pad=out_pad)
     s.run(bank, ("mask",), out_pad=out_pad)
     s.run(bank, (), out_pad=out_pad)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("V,lo,hi", [(513, 0, 512), (700, 512, 700), (6000, 0, 3600), (6000, 4000, 6000), (5001, 0, 5000),
+                                     (128256, 128000, 128256), (131072, 128256, 131072), (50001, 1024, 50000)])
+def test_logits_of_the_types_lowest_value(bank, dtype, V, lo, hi):
+    """The lowest value of a type in place of -inf, over whole chunks, parts and slices: it weighs nothing, and the
+    entropies stay numbers."""
+    s = Scene(V + lo, [2, -1, 1], V, dtype, biases=3)
+    low = torch.finfo(dtype).min
+    s.z[:, lo:hi] = low
+    s.z[3] = low  # a row of nothing else: all tokens alike
+    s.logits.copy_(dev(s.z))
+    s.T = 2.0
+    s.run(bank, ())
+    s.run(bank, ("mask", "draft"))
+    s.z[3] = s.z[0]
+    s.logits.copy_(dev(s.z))
+    s.T = 1.7  # (below 1, ln Z of a row whose mask leaves only the lowest value is past 32 bits)
+    s.run(bank)
+
+
+@pytest.mark.parametrize("T", [1e-30, 4e-38])
+def test_temperatures_next_to_zero(bank, T):
+    """1 / T is a number, a difference of two logits over T need not be: the largest logit has all the weight."""
+    s = Scene(19, [2, 1], 6000)
+    s.z[:] = s.z - 50
+    s.z[:, 2500] = 0.5
+    s.logits.copy_(dev(s.z))
+    s.T = T
+    s.run(bank, ())
