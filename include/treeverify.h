@@ -735,8 +735,11 @@ TB_API size_t tb_logits_workspace_size(int batch, int n_rows, int vocab);
  * tree's slots in every layer and kv head of the pages, and the length
  * advanced: lens_out[b] = lens[b] + accept_len (lens_out may be lens itself).
  * draft_tokens == NULL: results[b] already holds accept_len and path (another
- * rule's), which are only moved by.  Requests without a tree keep their length,
- * and their results get accept_len 0.  results: device tb_result [batch].  A draft
+ * rule's), which are only moved by; an accept_len outside 0 .. n is clamped, in
+ * the result too.  Requests that take no part in the step (without a tree, or
+ * refused by paged_plan) keep their length, and their results get accept_len 0;
+ * where a given result said otherwise, also bonus token -1 and an empty path.
+ * results: device tb_result [batch].  A draft
  * token outside [0, vocab) never matches and sets TB_EINVAL in the request's
  * result.  pages NULL: nothing to move.  One kernel. */
 TB_API tb_status paged_accept(const tb_bank *bank, const tb_requests *req, const tb_pages *pages,

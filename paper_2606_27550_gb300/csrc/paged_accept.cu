@@ -39,6 +39,8 @@ struct AcceptArgs {
 // What one request accepts; warp 0 of each CTA fills it in.
 struct Accepted {
     int len, bonus, status, L;
+    int given;  // the accept_len that a given result says
+    bool live;  // the request takes part in the step
     int path[TB_MAX_NODES];
     long long at[TB_MAX_NODES];   // elements from the layer's first head to slot L + j, -1: no such slot
     long long src[TB_MAX_NODES];  // the same for slot L + path[j]
@@ -139,6 +141,8 @@ __device__ void accept_one(const AcceptArgs &p, int b, Accepted &a)
         a.bonus = bonus;
         a.status = status;
         a.L = L;
+        a.given = given;
+        a.live = live;
     }
 }
 
@@ -210,6 +214,15 @@ __global__ void __launch_bounds__(kThreads) k_paged_accept(const __grid_constant
                 r.accept_len = a.len;
                 r.bonus_token = a.bonus;
                 r.status = a.status;
+            }
+        } else if (a.given != a.len) {
+            // cut off, or left there by an earlier step for a request that takes no part in this one
+            if (threadIdx.x < TB_MAX_NODES && !a.live)
+                r.path[threadIdx.x] = 0;
+            if (threadIdx.x == 0) {
+                r.accept_len = a.len;
+                if (!a.live)
+                    r.bonus_token = -1;
             }
         }
         if (threadIdx.x == 0) {

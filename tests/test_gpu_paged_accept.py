@@ -158,3 +158,30 @@ def test_requests_of_one_and_more_ctas(bank, layers, H):
     torch.cuda.synchronize()
     assert s.req.lens.tolist() == [L + len(paths[b]) for b, L in enumerate(lens)]
     assert same(s.pools[0], want[0]) and same(s.pools[1], want[1])
+
+
+@pytest.mark.parametrize("layers,H", [(1, 1), (8, 8)])
+def test_results_left_by_an_earlier_step(bank, layers, H):
+    """Given results: a waiting and a refused request get accept_len 0 whatever their results held, and an accept_len
+    above the tree's nodes or below 0 is clamped in the result as in the length."""
+    s = Scene(51, [100, 20, 30, 64, 7], [3, -1, 5, 8, 2], layers, H, 64, 16, "heads", refused=(2,))
+    res = np.zeros((5, 68), np.int32)
+    res[:, 0], res[:, 1], res[:, 2], res[:, 3] = (99, 3, 4, 20, -6), 9, 1234, 0
+    res[:, 4:] = 1
+    n = [8, 0, 0, 20, 4]
+    paths = {0: [0, 1, 2, 3, 4, 5, 6, 7], 3: list(range(20))}
+    for b, path in paths.items():
+        res[b, 4:4 + len(path)] = path
+    res[3, 4:24] = range(20)
+    s.results.copy_(i32(res))
+    before = [p.clone() for p in s.pools]
+    tv.paged_accept(bank, s.req, tv.Pages(*s.pools), s.results)
+    torch.cuda.synchronize()
+    want = res.copy()
+    want[:, 0] = n[0], 0, 0, 20, 0
+    want[:, 2] = 108, 20, 30, 84, 7
+    for b in (1, 2):
+        want[b, 1], want[b, 4:] = -1, 0
+    assert s.results.tolist() == want.tolist()
+    assert s.req.lens.tolist() == want[:, 2].tolist()
+    assert same(before[0], s.pools[0]) and same(before[1], s.pools[1])  # every path is in place already
