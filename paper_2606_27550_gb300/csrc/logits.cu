@@ -582,6 +582,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
         for (int c = c_first; c < c_end; c += kChunk) {
             float z[kVec][4];
             uint32_t word = 0xffffffffu;  // lane w holds word w of the chunk's mask
+            __syncwarp();  // a chunk of another order (a slice's end) takes the place of what other lanes read
             fetch(c + (kStages - 1) * kChunk);
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
             const int st = ((c - c_first) / kChunk) % kStages;

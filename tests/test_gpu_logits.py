@@ -324,3 +324,25 @@ def test_temperatures_next_to_zero(bank, T):
     s.logits.copy_(dev(s.z))
     s.T = T
     s.run(bank, ())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("V", [5932, 5931, 3584 + 513])
+@pytest.mark.parametrize("rules", [(), ("mask",), ("bias",), ("history", "penalty", "bias", "mask", "draft")])
+def test_without_statistics(bank, dtype, V, rules):
+    """Logits alone, in slices of several whole chunks and the rest of one: the same bits as with statistics."""
+    s = Scene(V, [3] * 300, V, dtype, hist_max=30)
+    s.run(bank, rules)
+    kw = dict(history=dev(s.hist), history_len=dev(s.hist_len), prompt_len=dev(s.prompt)) if "history" in rules else {}
+    if "penalty" in rules:
+        kw.update(repetition=dev(s.rep), presence=dev(s.pres), frequency=dev(s.freq), draft=dev(s.draft))
+    if "bias" in rules:
+        kw.update(bias_start=dev(s.bstart), bias_token=dev(s.btok), bias_value=dev(s.bval))
+    if "mask" in rules:
+        kw.update(mask=dev(pack_bits(s.allowed)))
+    req = tv.Requests(row_start=dev(s.start), tree=dev(np.array(s.tree, np.int32)))
+    ws = tv.make_workspace(tv.tb_logits_workspace_size(len(s.tree), s.R, V))
+    for _ in range(3):
+        out = torch.full((s.R, V), 3.0, device="cuda")
+        tv.logits_process(bank, req, s.logits, out, ws, **kw)
+        assert torch.equal(out, s.out)
