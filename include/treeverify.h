@@ -669,7 +669,9 @@ TB_API tb_status paged_kv_store(const tb_pages *pages, int layer, const int64_t 
  * and the output are accumulated in 32 bits; the weights enter the second
  * product in the pages' type.  The workspace needs tb_workspace_size for
  * head_dim; a plan of other heads or another batch size sets TB_EINVAL in its
- * status word and leaves out and lse unwritten. */
+ * status word and leaves out and lse unwritten, and so does, for its own rows, a
+ * request of the plan whose tree `bank` lacks or has with another number of
+ * nodes. */
 TB_API tb_status paged_tree_attention(const tb_bank *bank, const tb_requests *req, const tb_pages *pages, int layer,
                                       const void *plan, size_t plan_bytes, const void *q, int n_rows, int n_q_heads,
                                       float scale, float softcap, const float *slopes, void *out, float *lse,

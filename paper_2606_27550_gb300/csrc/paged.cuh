@@ -41,8 +41,9 @@ static_assert(sizeof(PlanCta) == 80, "eight-byte aligned records");
 struct PlanSplit {
     int c_lo, nseg;  // its CTAs
     int lo_slot;     // which of c_lo's two partial slots is the unit's (of the others: their first)
-    int row0, rows;  // the request's first row; rows of the unit
-    int rb, head, pad;
+    int row0;        // the request's first row
+    int16_t rows, rb;  // of the unit
+    int head, tree, n;
 };
 static_assert(sizeof(PlanSplit) == 32, "");
 

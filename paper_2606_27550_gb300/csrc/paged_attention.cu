@@ -86,6 +86,7 @@ constexpr int slot_floats(int d)
 struct PagedArgs {
     CUtensorMap tk, tv;  // of the layer
     const TreeDesc *trees;
+    int n_trees;
     const int32_t *table;
     int max_pages, page_log2, n_pages, batch;
     const uint16_t *q;
@@ -666,12 +667,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             u.node = grow / p.group;
             u.qh = g.head * p.group + grow % p.group;
             u.valid = u.node < cur.r.n && cur.r.row0 + u.node < p.n_rows;
+            if (u.valid && (unsigned)cur.r.tree >= (unsigned)p.n_trees) {  // a plan of another bank
+                atomicOr(p.status, kStatusBounds);
+                u.valid = false;
+            }
             if (u.valid)
                 u.valid = in_bounds(u.node < kMaxNodes && u.qh < p.Hq && cur.r.row0 >= 0, p.status);
             u.row = u.valid ? (size_t)(cur.r.row0 + u.node) * p.Hq + u.qh : 0;
             return u;
         };
-        auto stage = [&](const Unit &u, int sg) {
+        auto stage = [&](Unit &u, int sg) {
             SegInfo &si = s_info[sg & 1];
             const uint32_t col = lane_addr + kColQ + (sg & 1) * (kD / 2);
             const uint4 *src = reinterpret_cast<const uint4 *>(p.q + u.row * kD);
@@ -680,10 +685,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             for (int i = 0; i < kD / 8; ++i)
                 qv[i] = u.valid ? src[i] : make_uint4(0, 0, 0, 0);
             // what this row sees
-            const TreeDesc &td = p.trees[u.r.tree];
-            const int L = u.r.L;
-            const int dep = u.valid ? td.depth[u.node] : 0;
-            uint64_t anc = u.valid ? td.anc[u.node] : 0ull;
+            const TreeDesc &td = p.trees[(unsigned)u.r.tree < (unsigned)p.n_trees ? u.r.tree : 0];
+            const int L = u.r.L, node = u.valid ? u.node : 0;
+            int dep = td.depth[node];
+            uint64_t anc = td.anc[node];
+            if (u.valid && td.n != u.r.n) {
+                atomicOr(p.status, kStatusBounds);
+                u.valid = false;
+            }
+            dep = u.valid ? dep : 0;
+            anc = u.valid ? anc : 0ull;
             if constexpr (kForm == kBias)
                 si.path[rloc] = anc;
             if (window > 0 && dep >= window) {
@@ -855,9 +866,11 @@ __global__ void __launch_bounds__(256, 2) k_paged_merge(const __grid_constant__ 
             next = split_at(item + stride);
         int x = item & ((1 << rows_log2) - 1);
         const int grow = s.rb * 128 + x, node = grow / p.group, qh = s.head * p.group + grow % p.group;
-        const bool live = item < items && x < s.rows && s.row0 + node < p.n_rows && in_bounds(qh < p.Hq && s.c_lo >= 0, p.status);
+        const bool live = item < items && x < s.rows && s.row0 + node < p.n_rows &&
+                          (unsigned)s.tree < (unsigned)p.n_trees && in_bounds(qh < p.Hq && s.c_lo >= 0, p.status);
         if (!__any_sync(0xffffffffu, live))
             continue;
+        const int tree_n = live ? load_now(&p.trees[s.tree].n) : 0;  // (read at the end)
         const int nseg = live ? s.nseg : 0;
         const float *rest = p.part + (live ? (size_t)s.c_lo * 2 * kSlot : 0);  // CTA k > 0: + 2 k slots
         const float *first = rest + (live ? s.lo_slot * kSlot : 0);
@@ -913,7 +926,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_merge(const __grid_constant__ 
                 }
             }
         }
-        if (!live)
+        if (!live || tree_n != s.n)  // its CTAs have reported it
             continue;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const size_t row = (size_t)(s.row0 + node) * p.Hq + qh;
@@ -969,8 +982,7 @@ extern "C" tb_status paged_tree_attention(const tb_bank *bank, const tb_requests
 {
     const char *fn = "paged_tree_attention";
     PagedArgs a{};
-    int n_trees = 0;
-    tb_status st = check_device_bank(bank, fn, &a.trees, &n_trees);
+    tb_status st = check_device_bank(bank, fn, &a.trees, &a.n_trees);
     if (st != TB_OK || (st = check_requests(req, true, fn)) != TB_OK || (st = check_pages(pages, fn)) != TB_OK)
         return st;
     if (!req->tree)

@@ -298,9 +298,11 @@ __device__ void make_split(const PlanArgs &p, const Sums &s, int rows)
                 sp.nseg = owner(first + r.T - 1) - (k - 1) + 1;
                 sp.lo_slot = begin_of(k - 1) == first ? 0 : 1;
                 sp.row0 = r.row0;
-                sp.rb = q;
+                sp.rb = (int16_t)q;
                 sp.head = u;
-                sp.rows = min(128, r.n * group - q * 128);
+                sp.rows = (int16_t)min(128, r.n * group - q * 128);
+                sp.tree = r.tree;
+                sp.n = r.n;
             }
         }
         if (c < p.P)

@@ -322,3 +322,33 @@ def test_a_score_that_is_not_finite_shows_in_the_log_sum_exp(bank, form, dtype, 
     got, lse = s.run(bank, **kw)
     assert np.isnan(got[:, :2]).all() and np.isnan(lse[:, :2]).all()
     assert np.array_equal(got[:, 2:], want[:, 2:]) and np.array_equal(lse[:, 2:], want_lse[:, 2:])
+
+
+@pytest.mark.parametrize("L", [90, 6000])
+@pytest.mark.parametrize("window", [0, 3])
+def test_a_plan_of_another_bank(bank, L, window):
+    """Requests whose tree the call's bank lacks, or has with other nodes, are reported and left out, whether one CTA
+    has their unit or several; the others are served."""
+    s = Scene(L, [L, 40, L, 70, 9], [0, 9, 7, 3, 1], 4, 2, 64, 16)
+    s.run(bank, window=window)
+    at = np.concatenate([[0], np.cumsum(s.n)])
+
+    def left_out(trees, served):
+        other = tv.Bank(len(trees), 0)
+        for t in trees:
+            other.add(s.trees[t])
+        ws = tv.make_workspace(tv.tb_workspace_size(0, 1, s.H, s.Hq, s.d, 0, 0))
+        out, lse = torch.full_like(s.out, 5.0), torch.full_like(s.lse, 5.0)
+        tv.paged_tree_attention(other, s.req, s.pages, s.plan, s.q, out, ws, lse=lse)
+        torch.cuda.synchronize()
+        assert tv.tb_workspace_status(ws) == (tv.TB_OK if all(served) else tv.TB_EINVAL)
+        for b, known in enumerate(served):
+            rows = slice(at[b], at[b + 1])
+            for got, was in ((out, s.out), (lse, s.lse)):
+                assert torch.equal(got[rows], was[rows] if known else torch.full_like(was[rows], 5.0))
+        other.close()
+
+    left_out((0, 1, 5, 3), (True, False, False, True, True))
+    left_out((0,), (True, False, False, False, False))
+    left_out((0, 1, 2, 4, 4, 5, 6, 7, 8, 9), (True, True, True, False, True))
+    left_out(range(10), (True,) * 5)
