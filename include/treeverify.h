@@ -695,6 +695,8 @@ typedef struct tb_logit_rules {
     const int32_t *mask;         /* bit v % 32 of word v / 32: token v is allowed */
     int64_t mask_stride;         /* words per mask row, >= ceil(vocab / 32) */
     const int32_t *mask_row;     /* [rows]: a row's mask row, -1 for none (NULL: row r has mask row r) */
+    int64_t mask_rows;           /* with mask_row: rows of mask; a row that names one past them is allowed no
+                                    token, and TB_EINVAL is set in the workspace's status word */
 } tb_logit_rules;
 
 /* Statistics of the processed rows, as lm_head_stats and lm_head_stats_typical

@@ -74,6 +74,8 @@ struct LogitArgs {
     tb_logit_stats st;
     float temperature, inv_t;
     bool join;  // by the last CTA of a piece's rows, else by k_logits_join
+    int mask_rows;               // that mask_row may name
+    int *status;
     int *ticket;                 // [pieces of rows]
     Part *parts;                 // [rows][slices]
 };
@@ -363,6 +365,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
     // the item (row, part) in work
     const T *src = nullptr;
     const int32_t *mask = nullptr;
+    bool unknown = false;  // the row names a mask that there is not: no token is allowed
     int row = 0, c_first = 0, c_end = 0;
     float *dst = nullptr;
     bool vec = false;  // four logits at a time, in and out
@@ -430,7 +433,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
         odd = sizeof(T) == 2 ? (int)(reinterpret_cast<uintptr_t>(src) >> 1) & 1 : 0;
         vec = (reinterpret_cast<uintptr_t>(src) & (4 * sizeof(T) - 1)) == 0 && (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
         const int mrow = !p.r.mask ? -1 : p.r.mask_row ? p.r.mask_row[row] : row;
-        mask = mrow >= 0 ? p.r.mask + mrow * p.r.mask_stride + (v0 >> 5) : nullptr;
+        unknown = mrow >= p.mask_rows;
+        mask = mrow >= 0 ? p.r.mask + (unknown ? 0 : mrow) * p.r.mask_stride + (v0 >> 5) : nullptr;
         // on their way while the rules are built
 #pragma unroll
         for (int k = 0; k < kStages - 1; ++k)
@@ -668,7 +672,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
                     __syncwarp();
             }
             if (mask && lane < kChunk / 32 && c + 32 * lane < here)
-                word = mask_ring[st * (kChunk / 32) + lane];
+                word = unknown ? 0u : mask_ring[st * (kChunk / 32) + lane];
             if constexpr (sizeof(T) != 4) {
                 if (touched_here) {
                     if (four) {
@@ -765,6 +769,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
                         add(z[k][e], z[k][e + 1], mu);
             }
         }
+        if (unknown && lane == 0)
+            atomicOr(p.status, kStatusBounds);
         if constexpr (kStats > 0) {
             float sum[4] = {halves(a.s).x + halves(a.s).y, (halves(a.u).x + halves(a.u).y) * kLn2,
                             halves(a.st).x + halves(a.st).y, (halves(a.ut).x + halves(a.ut).y) * kLn2};
@@ -899,6 +905,8 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
     if (a.r.mask && a.r.mask_stride < (vocab + 31) / 32)
         return record_error(TB_EINVAL, "%s: mask_stride %lld below %d words", fn, (long long)a.r.mask_stride,
                             (vocab + 31) / 32);
+    if (a.r.mask && a.r.mask_row && a.r.mask_rows < 1)
+        return record_error(TB_EINVAL, "%s: mask_row into %lld mask rows", fn, (long long)a.r.mask_rows);
     if (a.st.draft_logit && (!a.r.draft || !req->tree))
         return record_error(TB_EINVAL, "%s: draft_logit without draft tokens or trees", fn);
     if ((st = check_workspace(workspace, workspace_bytes, tb_logits_workspace_size(req->batch, n_rows, vocab), fn)) !=
@@ -920,6 +928,8 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
     a.out_stride = out_stride;
     a.temperature = temperature;
     a.inv_t = 1.f / temperature;
+    a.mask_rows = a.r.mask_row && a.r.mask_rows < 0x7fffffff ? (int)a.r.mask_rows : 0x7fffffff;
+    a.status = static_cast<int *>(workspace);
     a.ticket = reinterpret_cast<int *>(static_cast<uint8_t *>(workspace) + 256);
     a.parts = reinterpret_cast<Part *>(static_cast<uint8_t *>(workspace) + kPartsOff);
     a.size = slice_of(req->batch, n_rows, vocab, n_sm);

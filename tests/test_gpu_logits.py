@@ -346,3 +346,28 @@ def test_without_statistics(bank, dtype, V, rules):
         out = torch.full((s.R, V), 3.0, device="cuda")
         tv.logits_process(bank, req, s.logits, out, ws, **kw)
         assert torch.equal(out, s.out)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [700, 5001])
+def test_mask_rows_that_there_are_not(bank, dtype, V):
+    """A row that names a mask past the last is allowed nothing and reported; -1 stands for no mask as before."""
+    s = Scene(V, [5, -1, 2], V, dtype)
+    known = s.g.integers(-1, s.R, s.R).astype(np.int32)
+    assert tv.tb_workspace_status(s.run(bank, mask_row=known)) == tv.TB_OK
+    first, st = s.out.clone(), {k: v.clone() for k, v in s.st.items()}
+    rows = known.copy()
+    rows[4], rows[7], rows[-1] = s.R, 2 ** 31 - 1, s.R + 3
+    req = tv.Requests(row_start=dev(s.start), tree=dev(np.array(s.tree, np.int32)))
+    ws = tv.make_workspace(tv.tb_logits_workspace_size(3, s.R, V))
+    tv.logits_process(bank, req, s.logits, s.out, ws, temperature=s.T, draft=dev(s.draft), history=dev(s.hist),
+                      history_len=dev(s.hist_len), prompt_len=dev(s.prompt), repetition=dev(s.rep), presence=dev(s.pres),
+                      frequency=dev(s.freq), bias_start=dev(s.bstart), bias_token=dev(s.btok), bias_value=dev(s.bval),
+                      mask=dev(pack_bits(s.allowed)), mask_row=dev(rows), **s.st)
+    torch.cuda.synchronize()
+    assert tv.tb_workspace_status(ws) == tv.TB_EINVAL
+    bad = [4, 7, s.R - 1]
+    assert bool((s.out[bad] == -np.inf).all()) and s.st["argmax"][bad].tolist() == [-1] * 3
+    assert s.st["entropy"][bad].tolist() == [0.0] * 3 and s.st["logz_t"][bad].tolist() == [-np.inf] * 3
+    good = [i for i in range(s.R) if i not in bad]
+    assert torch.equal(s.out[good], first[good]) and all(torch.equal(s.st[k][good], st[k][good]) for k in ("argmax", "entropy"))

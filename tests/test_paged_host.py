@@ -237,3 +237,21 @@ def test_a_pool_of_what_is_held_alone(lib, s):
                 tv.PagePool(None, None, None), tv.PagePool(z, None, z), tv.PagePool(z, z, None)):
         refused(tv.TB_EINVAL, s.do_plan, pool=bad)
     assert fake_cuda.launches(lib) == []
+
+
+def test_mask_rows_need_their_number(lib, s):
+    """mask_row indexes the mask's rows on the device: the C call wants to know how many there are."""
+    words, rows = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(9, dtype=torch.int32)
+    rules = tv.TbLogitRules()
+    rules.mask, rules.mask_stride, rules.mask_row = words.data_ptr(), 4, rows.data_ptr()
+    out = torch.zeros(9, 100)
+
+    def call():
+        return lib.logits_process(s.bank.handle, ctypes.byref(s.req.as_c()), s.logits.data_ptr(), tv.TB_F32, 100, 9, 100,
+                                  ctypes.byref(rules), 1.0, out.data_ptr(), 100, None, s.lws.data_ptr(), s.lws.numel(), STREAM)
+
+    assert call() == tv.TB_EINVAL and fake_cuda.launches(lib) == []
+    rules.mask_rows = 2
+    assert call() == tv.TB_OK and len(fake_cuda.launches(lib)) == 1
+    s.process(mask=words, mask_row=rows)
+    assert len(fake_cuda.launches(lib)) == 1
