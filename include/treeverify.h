@@ -524,7 +524,9 @@ TB_API tb_status verify_step_scheduled(const tb_bank *bank, const tb_policy *pol
  * (the paper decodes one sequence over one contiguous cache; these calls have
  * no counterpart in it).  None needs a host read of the lengths, so the calls
  * of a step can be captured into one CUDA graph; all of them are asynchronous
- * on `stream`.
+ * on `stream`.  A step may have no rows (max_rows or n_rows 0): the pointers to
+ * per-row arrays are then not read and may be NULL.  Pages, queries, keys,
+ * values, outputs of the attention and logits begin on 16 bytes.
  * ---------------------------------------------------------------------- */
 
 #define TB_MAX_REQUESTS 4096 /* request slots of one batch */

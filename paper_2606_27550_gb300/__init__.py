@@ -839,9 +839,11 @@ def paged_accept(bank: Bank, req: Requests, pages, results, draft=None, argmax=N
     r = req._c
     c = None if pages is None else pages._c
     rows = 0x7FFFFFFF if draft is None else min(draft.shape[0], argmax.shape[0])
-    rc = load().paged_accept(bank.handle, ctypes.byref(r), _ref(c), _arr(draft, _I32, 0, "draft"),
-                             _arr(argmax, _I32, 0, "argmax"), rows, vocab,
-                             _arr(results, _I32, r.batch * RESULT_INTS, "results"),
+    block = _arr(results, _I32, r.batch * RESULT_INTS, "results")
+    tokens, greedy = _arr(draft, _I32, 0, "draft"), _arr(argmax, _I32, 0, "argmax")
+    if rows == 0:
+        tokens = greedy = block  # a step without rows: no address, and none is read, but not "results given" either
+    rc = load().paged_accept(bank.handle, ctypes.byref(r), _ref(c), tokens, greedy, rows, vocab, block,
                              r.lens if lens_out is None else _arr(lens_out, _I32, r.batch, "lens_out"),
                              _stream(stream))
     if rc:

@@ -887,9 +887,9 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
     if (n_rows < 0 || n_rows > kMaxRowsCall || vocab < 1 || logit_stride < vocab || out_stride < vocab)
         return record_error(TB_EINVAL, "%s: n_rows %d, vocab %d, strides %lld, %lld", fn, n_rows, vocab,
                             (long long)logit_stride, (long long)out_stride);
-    if (!logits || !out || !ptr_aligned(logits, 16) || !ptr_aligned(out, 16))
+    if (n_rows > 0 && (!logits || !out || !ptr_aligned(logits, 16) || !ptr_aligned(out, 16)))
         return record_error(TB_EINVAL, "%s: logits / out NULL or not 16-byte aligned", fn);
-    if ((const void *)out == logits && (dtype != TB_F32 || logit_stride != out_stride))
+    if (n_rows > 0 && (const void *)out == logits && (dtype != TB_F32 || logit_stride != out_stride))
         return record_error(TB_EINVAL, "%s: in place with another type or stride", fn);
     if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature))
         return record_error(TB_EINVAL, "%s: temperature %g", fn, temperature);

@@ -1003,7 +1003,7 @@ extern "C" tb_status paged_tree_attention(const tb_bank *bank, const tb_requests
         return record_error(TB_EUNSUPPORTED, "%s: scale %g with softcap %g (%g at most)", fn, scale, softcap, kMaxCap);
     if (n_rows < 0)
         return record_error(TB_EINVAL, "%s: n_rows %d", fn, n_rows);
-    if (!q || !out || !ptr_aligned(q, 16) || !ptr_aligned(out, 16))
+    if (n_rows > 0 && (!q || !out || !ptr_aligned(q, 16) || !ptr_aligned(out, 16)))
         return record_error(TB_EINVAL, "%s: q / out NULL or not 16-byte aligned", fn);
     if ((st = check_workspace(plan, plan_bytes, plan_bytes_for(req->batch), fn)) != TB_OK)
         return st;

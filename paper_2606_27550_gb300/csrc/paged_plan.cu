@@ -540,8 +540,8 @@ extern "C" tb_status paged_plan(const tb_bank *bank, const tb_requests *req, con
     } else if (!req->n_new) {
         return record_error(TB_EINVAL, "%s: neither tree nor n_new", fn);
     }
-    if (!slots || !positions || !status || max_rows < 1)
-        return record_error(TB_EINVAL, "%s: slots, positions or status is NULL, or max_rows %d < 1", fn, max_rows);
+    if (!status || max_rows < 0 || (max_rows > 0 && (!slots || !positions)))
+        return record_error(TB_EINVAL, "%s: slots, positions or status is NULL, or max_rows %d < 0", fn, max_rows);
     if (n_q_heads < 0 || (n_q_heads > 0 && (n_kv_heads < 1 || n_q_heads % n_kv_heads)))
         return record_error(TB_EINVAL, "%s: n_q_heads %d not a multiple of n_kv_heads %d", fn, n_q_heads, n_kv_heads);
     if (n_q_heads > 0 && n_q_heads / n_kv_heads > kMaxGroup)

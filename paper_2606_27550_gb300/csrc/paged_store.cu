@@ -229,9 +229,9 @@ extern "C" tb_status paged_kv_store(const tb_pages *pages, int layer, const int6
     if (n_rows < 0 || (n_rows > 0 && !slots))
         return record_error(TB_EINVAL, "%s: n_rows %d, or slots is NULL", fn, n_rows);
     const bool has_q = q && q->ptr;
-    if ((st = check_rows(k, "k", fn)) != TB_OK || (st = check_rows(v, "v", fn)) != TB_OK)
+    if (n_rows > 0 && ((st = check_rows(k, "k", fn)) != TB_OK || (st = check_rows(v, "v", fn)) != TB_OK))
         return st;
-    if (has_q && ((st = check_rows(q, "q", fn)) != TB_OK || (st = check_rows(q_out, "q_out", fn)) != TB_OK))
+    if (n_rows > 0 && has_q && ((st = check_rows(q, "q", fn)) != TB_OK || (st = check_rows(q_out, "q_out", fn)) != TB_OK))
         return st;
     if (has_q && (n_q_heads < 1 || n_q_heads > 65536))
         return record_error(TB_EINVAL, "%s: n_q_heads %d", fn, n_q_heads);
@@ -241,8 +241,8 @@ extern "C" tb_status paged_kv_store(const tb_pages *pages, int layer, const int6
     if (turn) {
         if (!(rope->theta >= 1.f) || !std::isfinite(rope->theta))
             return record_error(TB_EINVAL, "%s: rope theta %g (1 or more)", fn, rope->theta);
-        if (rope->n_axes < 1 || rope->n_axes > kMaxAxes || !rope->positions || rope->axis_stride < 0 ||
-            (rope->n_axes > 1 && rope->axis_stride < n_rows))
+        if (rope->n_axes < 1 || rope->n_axes > kMaxAxes || (n_rows > 0 && !rope->positions) ||
+            rope->axis_stride < 0 || (rope->n_axes > 1 && rope->axis_stride < n_rows))
             return record_error(TB_EINVAL, "%s: %d axes, positions NULL or axis_stride %lld below n_rows", fn,
                                 rope->n_axes, (long long)rope->axis_stride);
         int end = 0;

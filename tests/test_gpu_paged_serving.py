@@ -166,3 +166,51 @@ def test_sampled_and_typical_rules_take_processed_logits():
     assert not 96 <= r["bonus_token"] < 128
     assert all(not 96 <= int(draft[j]) < 128 for j in r["path"][1:])
     bank.close()
+
+
+def test_a_step_without_rows():
+    """Requests that all wait or have ended: pages go back, nothing else moves, and no result says "accepted"."""
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    torch.manual_seed(8)
+    B, H, Hq, d, P, V = 3, 2, 4, 64, 16, 100
+    bank = tv.Bank(2, 0)
+    bank.add(synth.chain(3))
+    pool = tv.make_page_pool(9, B)
+    pages = tv.Pages(torch.randn(2, 9, H, P, d, device="cuda").bfloat16(), torch.randn(2, 9, H, P, d, device="cuda").bfloat16())
+    req = tv.Requests(row_start=i32([7] * (B + 1)), tree=i32([0, 0, 0]), lens=i32([20, 30, 5]), table=i32([[-1] * 4] * B),
+                      page_size=P)
+    status, plan = i32([9] * B), tv.make_paged_plan(B)
+
+    def lay(rows):
+        slots, pos = torch.empty(rows, dtype=torch.int64, device="cuda"), torch.empty(rows, dtype=torch.int32, device="cuda")
+        tv.paged_plan(bank, req, slots, pos, status, plan, pool=pool, n_q_heads=Hq, n_kv_heads=H)
+        return slots, pos
+
+    lay(9)
+    assert status.tolist() == [0] * 3 and pool.held.tolist() == [2, 3, 1] and pool.state.tolist() == [6, 3]
+    req.tree.fill_(-1)
+    req.lens[2] = 0
+    slots, pos = lay(0)
+    assert status.tolist() == [0] * 3 and req.row_start.tolist() == [0] * 4
+    assert pool.held.tolist() == [2, 2, 0] and pool.state.tolist() == [6, 5]
+    before = [pages.k.clone(), pages.v.clone()]
+    kv, q = (torch.empty(0, h, d, dtype=torch.bfloat16, device="cuda") for h in (H, Hq))
+    ws = tv.make_workspace(tv.tb_workspace_size(0, 1, H, Hq, d, 0, 0))
+    tv.paged_kv_store(pages, slots, kv, kv, layer=1, q=q, q_out=torch.empty_like(q), positions=pos, rope_theta=1e4)
+    tv.paged_tree_attention(bank, req, pages, plan, q, torch.empty_like(q), ws, layer=1,
+                            lse=torch.empty(0, Hq, device="cuda"))
+    z = torch.empty(0, V, device="cuda")
+    tv.logits_process(bank, req, z, z, tv.make_workspace(tv.tb_logits_workspace_size(B, 0, V)), draft=pos, argmax=pos)
+    results = tv.make_results(B)
+    results.fill_(4)
+    tv.paged_accept(bank, req, pages, results, draft=pos, argmax=pos, vocab=V)
+    torch.cuda.synchronize()
+    assert results.tolist() == [[0, -1, L, 0] + [0] * 64 for L in (20, 30, 0)] and req.lens.tolist() == [20, 30, 0]
+    assert torch.equal(pages.k, before[0]) and torch.equal(pages.v, before[1])
+    assert tv.tb_workspace_status(ws) == tv.TB_OK
+    # rows that no request may have, none given room for: refused one by one
+    req.tree.fill_(0)
+    lay(0)
+    assert status.tolist() == [tv.TB_ECAPACITY] * 3 and req.row_start.tolist() == [0] * 4
+    assert pool.held.tolist() == [2, 2, 0] and pool.state.tolist() == [6, 5]
+    bank.close()

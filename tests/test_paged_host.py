@@ -255,3 +255,22 @@ def test_mask_rows_need_their_number(lib, s):
     assert call() == tv.TB_OK and len(fake_cuda.launches(lib)) == 1
     s.process(mask=words, mask_row=rows)
     assert len(fake_cuda.launches(lib)) == 1
+
+
+def test_steps_without_rows(lib, s):
+    """Empty tensors have no address: no call refuses them, and those that have only rows to work on launch nothing."""
+    none = torch.zeros(0, 2, 64, dtype=BF)
+    s.slots, s.positions = s.slots[:0], s.positions[:0]
+    s.do_plan()
+    assert len(fake_cuda.launches(lib)) == 1
+    s.kv = none
+    s.store(k=none, q=torch.zeros(0, 4, 64, dtype=BF), q_out=torch.zeros(0, 4, 64, dtype=BF))
+    s.store(k=none, q=None, positions=torch.zeros(3, 0, dtype=torch.int32), sections=(8, 12, 12))
+    s.store(k=none, q=None, rope_theta=0.0)
+    s.attend(q=s.q[:0], out=s.out[:0], lse=torch.zeros(0, 4))
+    s.process(logits=s.logits[:0], out=torch.zeros(0, 100), draft=s.positions, argmax=s.positions, top1=torch.zeros(0),
+              draft_logit=torch.zeros(0), mask=torch.zeros(0, 4, dtype=torch.int32))
+    assert fake_cuda.launches(lib) == []
+    s.accept(draft=s.positions, argmax=s.positions)
+    assert len(fake_cuda.launches(lib)) == 1
+    refused(tv.TB_EINVAL, s.accept, draft=s.positions, argmax=s.positions, vocab=0)  # greedy, not results given
