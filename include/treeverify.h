@@ -673,7 +673,10 @@ TB_API tb_status paged_kv_store(const tb_pages *pages, int layer, const int64_t 
  * head_dim; a plan of other heads or another batch size sets TB_EINVAL in its
  * status word and leaves out and lse unwritten, and so does, for its own rows, a
  * request of the plan whose tree `bank` lacks or has with another number of
- * nodes. */
+ * nodes.  `layer` or'ed with TB_DEBUG_EXPIRE_WAIT is a test hook, as for
+ * verify_step: a bounded wait inside the kernel runs out, the status word says
+ * TB_ETIMEOUT, out and lse stay unwritten, and the workspace has to be
+ * re-initialised. */
 TB_API tb_status paged_tree_attention(const tb_bank *bank, const tb_requests *req, const tb_pages *pages, int layer,
                                       const void *plan, size_t plan_bytes, const void *q, int n_rows, int n_q_heads,
                                       float scale, float softcap, const float *slopes, void *out, float *lse,

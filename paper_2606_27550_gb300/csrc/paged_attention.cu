@@ -99,6 +99,7 @@ struct PagedArgs {
     void *plan;
     float *part;
     int *status;
+    int expire_wait;  // test hook: P V waits on a barrier that nothing arrives on
 };
 
 template <bool kF16>
@@ -157,6 +158,13 @@ __device__ __forceinline__ void cap_four(uint32_t *r, float cap_in)
     const float2 w02 = halves(mul_two(bd, inv)), w13 = halves(mul_two(ac, inv));
     r[0] = __float_as_uint(w02.x), r[2] = __float_as_uint(w02.y);
     r[1] = __float_as_uint(w13.x), r[3] = __float_as_uint(w13.y);
+}
+
+// The verdict of a wait by a whole warp.  Its lanes may see a barrier complete and the time run out
+// in one instant, and leave the kernel's loops together or not at all.
+__device__ __forceinline__ bool warp_agrees(bool ok)
+{
+    return __all_sync(0xffffffffu, ok);
 }
 
 // The bits of [lo, hi) relative to s0, of 32.
@@ -249,6 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
     __shared__ __align__(8) uint64_t s_full[2], p_full[2], pv_done[2], q_full[2], ml_full[2], o_free[2], drain_bar;
+    __shared__ __align__(8) uint64_t never_bar[2];
     __shared__ __align__(8) uint64_t mx_full[4][2];  // per lane quadrant: both halves' row maxima are there
     __shared__ float s_mx[2][2][128];
     __shared__ uint32_t tmem_slot;
@@ -272,6 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             mbar_init(&q_full[b], 4);
             mbar_init(&ml_full[b], 8);
             mbar_init(&o_free[b], 4);
+            mbar_init(&never_bar[b], 1);
             for (int q = 0; q < 4; ++q)
                 mbar_init(&mx_full[q][b], 2);
         }
@@ -406,6 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             tc_commit(&drain_bar);
         } else if (lane == 0) {
             // ------------------------------------------------ P V issuer
+            uint64_t *const p_ready = p.expire_wait ? never_bar : p_full;
             long long it = 0;
             int s = 0, sg = 0;
             uint32_t ph = 0;
@@ -416,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 for (int j = 0; j < g.n; ++j, ++it) {
                     const int b = (int)(it & 1);
                     // P written; at a segment's first tile, the previous segment's O has been read
-                    if (!mbar_wait_bounded(&p_full[b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status) ||
+                    if (!mbar_wait_bounded(&p_ready[b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status) ||
                         (j == 0 && sg > 0 &&
                          !mbar_wait_bounded(&o_free[(sg - 1) & 1], (uint32_t)((sg - 1) >> 1) & 1u, &abort_flag,
                                             p.status)) ||
@@ -453,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         int sg = 0;
         for (long long t = t0; t < t1 && !aborted; ++sg) {
             SegInfo &si = s_info[sg & 1];
-            if (!mbar_wait_bounded(&q_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status))
+            if (!warp_agrees(mbar_wait_bounded(&q_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status)))
                 break;
             const int n = si.n, L = si.L, end = si.end, lo = si.lo[rloc], pos = si.pos[rloc];
             const uint64_t anc = si.anc[rloc], path = kForm == kBias ? si.path[rloc] : 0;
@@ -463,10 +474,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             for (int j = 0; j < n; ++j, ++it) {
                 const int b = (int)(it & 1);
                 const int key0 = tile_key(si.j0 + j, si.a0, si.n1, si.b0);
-                if (!mbar_wait_bounded(&s_full[b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status)) {
-                    aborted = true;
-                    break;
-                }
+                // (a wait that ran out is looked at where the warp votes anyway, below; until then it
+                // goes on with whatever S holds)
+                bool ok = mbar_wait_bounded(&s_full[b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status);
                 tc_fence_after();
                 const uint32_t sa = lane_addr + kColS + b * 128 + half * kHalf;
                 const int h0 = key0 + half * kHalf;  // this thread's first slot
@@ -555,10 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 __syncwarp();
                 if (lane == 0)
                     mbar_arrive(&mx_full[q4][b]);
-                if (!mbar_wait_bounded(&mx_full[q4][b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status)) {
-                    aborted = true;
-                    break;
-                }
+                ok = mbar_wait_bounded(&mx_full[q4][b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status) && ok;
                 mx = fmaxf(mx, s_mx[b][half ^ 1][rloc]);
 
                 // the lazily raised reference, the same in both halves
@@ -571,10 +578,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     m_ref = mx - kShift;
                     rescale = true;
                 }
-                if (__any_sync(0xffffffffu, rescale)) {
+                if (__any_sync(0xffffffffu, rescale || !ok)) {
                     // O holds the previous tiles' P V: wait for the last one, then scale in place
                     const long long jp = it - 1;
-                    if (!mbar_wait_bounded(&pv_done[jp & 1], (uint32_t)(jp >> 1) & 1u, &abort_flag, p.status)) {
+                    if (!warp_agrees(ok) ||
+                        !warp_agrees(mbar_wait_bounded(&pv_done[jp & 1], (uint32_t)(jp >> 1) & 1u, &abort_flag, p.status))) {
                         aborted = true;
                         break;
                     }
@@ -609,7 +617,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 if (key0 + kBN > end || key0 < si.lo_min) {
                     // V rows that nobody sees may hold anything: zeros, once the tile has landed
                     const int sv = (int)(it % kVStages);
-                    if (!mbar_wait_bounded(&v_full[sv], (uint32_t)(it / kVStages) & 1u, &abort_flag, p.status)) {
+                    if (!warp_agrees(
+                            mbar_wait_bounded(&v_full[sv], (uint32_t)(it / kVStages) & 1u, &abort_flag, p.status))) {
                         aborted = true;
                         break;
                     }
@@ -630,7 +639,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             }
             if (aborted)
                 break;
-            if (sg >= 2 && !mbar_wait_bounded(&o_free[sg & 1], (uint32_t)((sg >> 1) - 1) & 1u, &abort_flag, p.status))
+            if (sg >= 2 &&
+                !warp_agrees(mbar_wait_bounded(&o_free[sg & 1], (uint32_t)((sg >> 1) - 1) & 1u, &abort_flag, p.status)))
                 break;
             if (half == 0)
                 si.m[rloc] = m_ref;
@@ -771,10 +781,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 }
             }
             const long long last = it - 1;
-            if (!mbar_wait_bounded(&ml_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status))
+            if (!warp_agrees(mbar_wait_bounded(&ml_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status)))
                 break;
             const float m_ref = s_info[sg & 1].m[rloc], l = s_info[sg & 1].l[0][rloc] + s_info[sg & 1].l[1][rloc];
-            if (!mbar_wait_bounded(&pv_done[last & 1], (uint32_t)(last >> 1) & 1u, &abort_flag, p.status))
+            if (!warp_agrees(mbar_wait_bounded(&pv_done[last & 1], (uint32_t)(last >> 1) & 1u, &abort_flag, p.status)))
                 break;
             tc_fence_after();
             const bool whole = now.n == now.T;
@@ -857,6 +867,12 @@ __global__ void __launch_bounds__(256, 2) k_paged_merge(const __grid_constant__ 
     int item = (blockIdx.x * 256 + threadIdx.x) >> 3;
     auto split_at = [&](int i) { return plan_splits(p.plan)[min(i >> rows_log2, kMaxPlanCtas - 1)]; };
     PlanSplit s, next = split_at(item);
+    // What the CTAs have reported, looked at before the first write: a wait that ran out, or a request
+    // whose tree is another here (a load per row for that would be one more on every call's way).
+    const int reported = load_now(p.status);
+    const auto left_out = [&](const PlanSplit &s) {
+        return (reported & kStatusTimeout) || (unsigned)s.tree >= (unsigned)p.n_trees || p.trees[s.tree].n != s.n;
+    };
     const int items = hd->n_splits << rows_log2, stride = gridDim.x * 32;
     if (!hd->valid || hd->batch != p.batch || hd->n_q_heads != p.Hq || hd->n_kv_heads != p.Hkv)
         return;
@@ -867,10 +883,9 @@ __global__ void __launch_bounds__(256, 2) k_paged_merge(const __grid_constant__ 
         int x = item & ((1 << rows_log2) - 1);
         const int grow = s.rb * 128 + x, node = grow / p.group, qh = s.head * p.group + grow % p.group;
         const bool live = item < items && x < s.rows && s.row0 + node < p.n_rows &&
-                          (unsigned)s.tree < (unsigned)p.n_trees && in_bounds(qh < p.Hq && s.c_lo >= 0, p.status);
+                          in_bounds(qh < p.Hq && s.c_lo >= 0, p.status);
         if (!__any_sync(0xffffffffu, live))
             continue;
-        const int tree_n = live ? load_now(&p.trees[s.tree].n) : 0;  // (read at the end)
         const int nseg = live ? s.nseg : 0;
         const float *rest = p.part + (live ? (size_t)s.c_lo * 2 * kSlot : 0);  // CTA k > 0: + 2 k slots
         const float *first = rest + (live ? s.lo_slot * kSlot : 0);
@@ -926,7 +941,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_merge(const __grid_constant__ 
                 }
             }
         }
-        if (!live || tree_n != s.n)  // its CTAs have reported it
+        if (!live || (reported && left_out(s)))
             continue;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const size_t row = (size_t)(s.row0 + node) * p.Hq + qh;
@@ -989,6 +1004,8 @@ extern "C" tb_status paged_tree_attention(const tb_bank *bank, const tb_requests
         return record_error(TB_EINVAL, "%s: req->tree is NULL", fn);
     if (pages->page_size != req->page_size)
         return record_error(TB_EINVAL, "%s: pages of %d slots, a table of %d", fn, pages->page_size, req->page_size);
+    a.expire_wait = (layer & TB_DEBUG_EXPIRE_WAIT) ? 1 : 0;
+    layer &= ~TB_DEBUG_EXPIRE_WAIT;
     if (layer < 0 || layer >= pages->n_layers)
         return record_error(TB_EINVAL, "%s: layer %d of %d", fn, layer, pages->n_layers);
     if (n_q_heads < pages->n_kv_heads || n_q_heads % pages->n_kv_heads)
