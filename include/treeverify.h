@@ -555,7 +555,9 @@ typedef struct tb_pages {
  * request).  With tree == NULL it brings n_new[b] tokens of a prompt instead
  * (paged_plan and paged_kv_store only).  Token s of request b lives in page
  * table[b * max_pages + s / page_size] at s % page_size; table entries past the
- * request's pages are never read.  The rows of all requests (node order within
+ * request's pages are never read, and entries that are not page ids (-1) may
+ * stand where no row looks: before key_begin, and between the first tokens that
+ * a window keeps and the window.  The rows of all requests (node order within
  * a request) lie behind one another: request b's are row_start[b] ..
  * row_start[b + 1] - 1 of every per-row array. */
 typedef struct tb_requests {
@@ -599,7 +601,8 @@ TB_API size_t tb_paged_plan_size(int batch, int device);
  * complete for every request.  A pool of `held` alone: no page is taken or given
  * back, and a request with need > held gets nothing.  Written:
  *   row_start [batch + 1]; per row (max_rows entries, -1 / 0 past the last row):
- *   slots     int64  page * page_size + slot in the page
+ *   slots     int64  page * page_size + slot in the page (-1 where the table's
+ *             entry is negative: paged_kv_store skips it)
  *   positions int32  lens[b] + depth(node) (lens[b] + i without trees)
  *   status    int32 [batch]: TB_OK, or why the request got nothing in this step
  *             (no rows, no pages taken or given): TB_EINVAL for an unknown
@@ -673,7 +676,8 @@ TB_API tb_status paged_kv_store(const tb_pages *pages, int layer, const int64_t 
  * head_dim; a plan of other heads or another batch size sets TB_EINVAL in its
  * status word and leaves out and lse unwritten, and so does, for its own rows, a
  * request of the plan whose tree `bank` lacks or has with another number of
- * nodes.  `layer` or'ed with TB_DEBUG_EXPIRE_WAIT is a test hook, as for
+ * nodes.  A table entry outside the pool whose page holds slots that some row
+ * sees sets TB_EINVAL there too; its keys and values count as zeros.  `layer` or'ed with TB_DEBUG_EXPIRE_WAIT is a test hook, as for
  * verify_step: a bounded wait inside the kernel runs out, the status word says
  * TB_ETIMEOUT, out and lse stay unwritten, and the workspace has to be
  * re-initialised. */

@@ -330,14 +330,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             const bool box = a < kD / 64;
             const uint32_t dst_off = (uint32_t)a * kAtom + ((uint32_t)pg << (p.page_log2 + 7));
             const int page_mask = (1 << p.page_log2) - 1;
-            // this lane's page of tile j of the current request
+            // this lane's page of tile j of the current request; nothing is asked of it before its tile's turn
+            struct Page {
+                int id;
+                bool inside;  // the request has slots in it
+            };
+            auto first_slot = [&](int j) { return tile_key(j, cur.r.a0, cur.r.n1, cur.r.b0) + (pg << p.page_log2); };
             auto page_of = [&](int j) {
-                const int slot = tile_key(j, cur.r.a0, cur.r.n1, cur.r.b0) + (pg << p.page_log2);
-                const int at = slot >> p.page_log2;
-                int id = -1;
-                if (box && slot < cur.r.L + cur.r.n && at < p.max_pages)
-                    id = p.table[(size_t)cur.r.b * p.max_pages + at];
-                return id < 0 || id >= p.n_pages ? p.n_pages : id;  // past the last page: zeros
+                const int slot = first_slot(j), at = slot >> p.page_log2;
+                Page x{-1, box && slot < cur.r.L + cur.r.n};
+                if (x.inside && at < p.max_pages)
+                    x.id = p.table[(size_t)cur.r.b * p.max_pages + at];
+                return x;
+            };
+            // a hole in the table: reported, if some row may see one of the slots
+            auto report_hole = [&](int slot) {
+                const int window = static_cast<const PlanHeader *>(p.plan)->window, past = slot + min(1 << p.page_log2, kBN);
+                const int lo_min = window > 0 ? max(cur.r.begin, cur.r.L - window + 1) : cur.r.begin;
+                if (past > lo_min || (window > 0 && past > cur.r.begin && slot < min(cur.r.far_end, cur.r.L)))
+                    atomicOr(p.status, kStatusBounds);
             };
             long long issued = 0;
             int s = 0;
@@ -346,9 +357,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             for (long long t = t0; ok && t < t1;) {
                 cur.seek(t, p.Hkv);
                 const Seg g = seg_at(cur, t);
-                int id = page_of(g.j0);
+                Page page = page_of(g.j0);
                 for (int j = 0; j < g.n; ++j) {
-                    const int id_next = j + 1 < g.n ? page_of(g.j0 + j + 1) : 0;
+                    const Page next = j + 1 < g.n ? page_of(g.j0 + j + 1) : Page{-1, false};
                     if (lane == 0)
                         ok = mbar_wait_bounded(&empty[s], ph ^ 1u, &abort_flag, p.status);
                     ok = __shfl_sync(0xffffffffu, ok, 0);
@@ -357,11 +368,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     if (lane == 0)
                         mbar_arrive_expect_tx(&full[s], kTile);
                     __syncwarp();
-                    if (box)
+                    const bool there = page.id >= 0 && page.id < p.n_pages;
+                    if (box)  // past the last page: zeros
                         tma_load_4d(ring + (size_t)s * kTile + dst_off, map, &full[s], 64 * a,
                                     p.page_log2 > 7 ? tile_key(g.j0 + j, cur.r.a0, cur.r.n1, cur.r.b0) & page_mask : 0,
-                                    g.head, id);
-                    id = id_next;
+                                    g.head, there ? page.id : p.n_pages);
+                    if (page.inside && !there && !is_v)
+                        report_hole(first_slot(g.j0 + j));
+                    page = next;
                     ++issued;
                     if (++s == S) {
                         s = 0;

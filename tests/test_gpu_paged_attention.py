@@ -352,3 +352,38 @@ def test_a_plan_of_another_bank(bank, L, window):
     left_out((0,), (True, False, False, False, False))
     left_out((0, 1, 2, 4, 4, 5, 6, 7, 8, 9), (True, True, True, False, True))
     left_out(range(10), (True,) * 5)
+
+
+@pytest.mark.parametrize("P", [16, 128, 512])
+@pytest.mark.parametrize("entry", [-1, -2 ** 31, "past", 2 ** 31 - 1])
+def test_holes_in_the_table(bank, P, entry):
+    """A page that is not there, where rows look: reported, its keys and values zeros.  Where none looks: nothing."""
+    def scene(**kw):
+        s = Scene(P, [1700, 300], [5, 3], 4, 2, 64, P, **kw)
+        return s, s.pages.k.shape[1] if entry == "past" else entry
+
+    def run(s, reported, **kw):
+        real = tv.tb_workspace_status
+        tv.tb_workspace_status = lambda ws: 0  # (the scene's own check)
+        try:
+            s.check(bank, **kw)
+        finally:
+            tv.tb_workspace_status = real
+        assert tv.tb_workspace_status(s.ws) == (tv.TB_EINVAL if reported else tv.TB_OK)
+
+    for page in (0, 1024 // P, 1699 // P):  # the first page, one in the middle, the last prefix slot's
+        s, e = scene()
+        s.table[0, page] = e
+        for x in s.dense[0]:
+            x[page * P:(page + 1) * P] = 0
+        run(s, True)
+        # with a window of 100 the pages before slot 1601 are looked at by the first tokens' rule alone
+        run(s, page * P + P > 1601, window=100)
+        run(s, page * P + P > 1601 or page * P < 20, window=100, sink=20)
+    # documents that begin behind the hole, at its end, inside it
+    for begin, reported in ((1024 + P, False), (1023 + P, True), (1024, True)):
+        s, e = scene(begin=[begin, 0])
+        s.table[0, 1024 // P] = e
+        for x in s.dense[0]:
+            x[1024:1024 + P] = 0
+        run(s, reported)
