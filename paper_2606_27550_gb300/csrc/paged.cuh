@@ -15,15 +15,15 @@ struct PlanReq {
     long long tile_base;  // first of its tiles in the flattened tile space
     int L, n, row0, tree;
     int T, a0, n1, b0;
-    int row_blocks, begin, far_end, b;  // blocks of 128 query rows; keys before far_end are seen beyond the window
+    int begin, far_end, b;  // keys before far_end are seen beyond the window
 };
 static_assert(sizeof(PlanReq) == 56, "eight-byte aligned records");
 
 struct PlanHeader {
     int ticket;  // of paged_plan's CTAs; zero between calls
     int valid;
-    int batch, n_q_heads, n_kv_heads, window, n_active;
-    int rows, sink, n_splits, pad[6];
+    int batch, n_q_heads, n_kv_heads, window, n_splits;
+    int pad[9];
 };
 static_assert(sizeof(PlanHeader) == 64, "");
 

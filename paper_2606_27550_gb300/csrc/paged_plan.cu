@@ -145,7 +145,7 @@ struct Sums {
 };
 
 // The attention's work split, by one CTA.
-__device__ void make_split(const PlanArgs &p, const Sums &s, int rows)
+__device__ void make_split(const PlanArgs &p, const Sums &s)
 {
     __shared__ int bins[kMaxRowBlocks + 2], warp_bins[kThreads / 32][kMaxRowBlocks + 2];
     __shared__ int s_start[kMaxRowBlocks + 1], s_W, s_seqs, s_P;
@@ -213,7 +213,6 @@ __device__ void make_split(const PlanArgs &p, const Sums &s, int rows)
         q.n = s.n[b];
         q.tree = s.tree[b];
         q.row0 = s.row[b];
-        q.row_blocks = blocks_of(b);
         q.begin = p.key_begin ? min(max(p.key_begin[b], 0), q.L + q.n) : 0;
         tiles_of(q, p.window, p.sink);
         return q;
@@ -319,9 +318,6 @@ __device__ void make_split(const PlanArgs &p, const Sums &s, int rows)
         hd->n_q_heads = p.Hq;
         hd->n_kv_heads = p.Hkv;
         hd->window = p.window;
-        hd->sink = p.sink;
-        hd->n_active = n_active;
-        hd->rows = rows;
         hd->n_splits = n_splits;
     }
 }
@@ -435,7 +431,7 @@ __global__ void __launch_bounds__(kThreads) k_paged_plan(const __grid_constant__
             hd->valid = 0;
     }
     if (attend && blockIdx.x == 0) {
-        make_split(p, s, rows);
+        make_split(p, s);
     } else {
         // the rows
         const int ctas = gridDim.x - (attend ? 1 : 0), stride = ctas * kThreads;
