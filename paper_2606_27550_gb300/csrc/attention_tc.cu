@@ -87,11 +87,6 @@ constexpr int attn_ring_bytes(int d)
 {
     return (kKStages + kVStages) * tile_bytes(d);
 }
-// floats per partial slot: O[128][kD], m[128], l[128]
-constexpr int slot_floats(int d)
-{
-    return 128 * d + 256;
-}
 // TMEM columns.  P_b (bf16 pairs) overwrites the first half of S_b once the
 // softmax has read S_b into registers; Q (bf16 pairs) is the A operand of QK^T.
 constexpr uint32_t kColS0 = 0, kColS1 = 128, kColP0 = 0, kColP1 = 128, kColO = 256, kColQ = 384;
@@ -1450,11 +1445,6 @@ bool attn_tc_clustered(const tb_kv *kv, int N, int Hq, int n_layers, int n_sm)
     bool fused;
     return alone_cluster(attn_tc_plan(kv->L, N, Hq, kv->n_kv_heads, n_layers, n_sm), kv->head_dim, n_sm,
                          kv->rope_theta != 0.f, &fused) > 0;
-}
-
-size_t attn_tc_slot_floats(int d)
-{
-    return (size_t)slot_floats(d);
 }
 
 int attn_tc_units(const AttnSeq *seqs, int n_seq, int Hq, int Hkv, int n_layers)

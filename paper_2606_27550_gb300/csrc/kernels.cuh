@@ -199,7 +199,12 @@ bool attn_tc_fuses_rope(const tb_kv *kv, int N, int Hq, int n_layers, int n_sm);
 // whether its launch leaves no partials to merge (clusters share its units)
 bool attn_tc_clustered(const tb_kv *kv, int N, int Hq, int n_layers, int n_sm);
 AttnPlan attn_tc_plan(int L, int N, int Hq, int Hkv, int n_layers, int n_sm);
-size_t attn_tc_slot_floats(int d);  // floats per partial slot (two slots per CTA)
+// Floats per partial slot of the attention over a slab and over pages (two slots per
+// CTA in a workspace): O[128][d], m[128], l[128].
+constexpr int slot_floats(int d)
+{
+    return 128 * d + 256;
+}
 // scheduled mode: the tree (rung_tree[sched[0]]) and L (sched[1]) are read on
 // the device; q / out hold N_max nodes per layer; all kv->n_layers layers
 struct AttnSched {

@@ -77,12 +77,6 @@ float cap_in(float scale, float softcap)
     return (float)(2.0 * 1.4426950408889634 * (double)scale / (double)softcap);
 }
 
-// floats per partial slot: O[128][kD], m[128], l[128]
-constexpr int slot_floats(int d)
-{
-    return 128 * d + 256;
-}
-
 struct PagedArgs {
     CUtensorMap tk, tv;  // of the layer
     const TreeDesc *trees;

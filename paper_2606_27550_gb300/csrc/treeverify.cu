@@ -230,7 +230,7 @@ static size_t align256(size_t x)
 // Partial slots of the split-L merge: two per CTA of the attention kernel.
 static size_t attn_part_bytes(int n_sm, int d)
 {
-    return align256((size_t)n_sm * 2 * attn_tc_slot_floats(d) * 4);
+    return align256((size_t)n_sm * 2 * slot_floats(d) * sizeof(float));
 }
 
 static int sm_count(int device)
