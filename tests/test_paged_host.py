@@ -274,3 +274,13 @@ def test_steps_without_rows(lib, s):
     s.accept(draft=s.positions, argmax=s.positions)
     assert len(fake_cuda.launches(lib)) == 1
     refused(tv.TB_EINVAL, s.accept, draft=s.positions, argmax=s.positions, vocab=0)  # greedy, not results given
+
+
+def test_the_attention_and_its_join(lib, s):
+    """Exactly two launches, on the call's stream, the join behind the attention as its dependent."""
+    s.attend()
+    first, second = fake_cuda.launches(lib)
+    assert "k_paged_attention" in first.name and "k_paged_merge" in second.name
+    for launch in (first, second):
+        assert launch.stream == STREAM and launch.pdl and launch.cluster == 1 and launch.device == 0
+    assert first.grid == (152, 1, 1) and first.block == 512 and second.block == 256
