@@ -752,9 +752,10 @@ TB_API size_t tb_logits_workspace_size(int batch, int n_rows, int vocab);
  * the result too.  Requests that take no part in the step (without a tree, or
  * refused by paged_plan) keep their length, and their results get accept_len 0;
  * where a given result said otherwise, also bonus token -1 and an empty path.
- * results: device tb_result [batch].  A draft
- * token outside [0, vocab) never matches and sets TB_EINVAL in the request's
- * result.  pages NULL: nothing to move.  One kernel. */
+ * results: device tb_result [batch].  Its status is set to TB_EINVAL for an
+ * unknown tree, a draft token outside [0, vocab) (which never matches), and a
+ * table entry outside the pool where a row had to move from or to (that row
+ * stays where it was).  pages NULL: nothing to move.  One kernel. */
 TB_API tb_status paged_accept(const tb_bank *bank, const tb_requests *req, const tb_pages *pages,
                               const int32_t *draft_tokens, const int32_t *argmax, int n_rows, int vocab,
                               tb_result *results, int32_t *lens_out, tb_stream stream);

@@ -126,6 +126,7 @@ __device__ void accept_one(const AcceptArgs &p, int b, Accepted &a)
     }
     __syncwarp();
     if (p.k && live) {
+        bool hole = false;  // in the table, where a row should move from or to
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int j = lane + 32 * h, from = j < len ? a.path[j] : j;
@@ -133,8 +134,11 @@ __device__ void accept_one(const AcceptArgs &p, int b, Accepted &a)
             if (j < len) {
                 a.at[j] = at;
                 a.src[j] = from == j ? -1 : src;  // in place already: nothing moves
+                hole |= from != j && (at < 0 || src < 0);
             }
         }
+        if (__any_sync(0xffffffffu, hole))
+            status = TB_EINVAL;
     }
     if (lane == 0) {
         a.len = len;
@@ -215,15 +219,19 @@ __global__ void __launch_bounds__(kThreads) k_paged_accept(const __grid_constant
                 r.bonus_token = a.bonus;
                 r.status = a.status;
             }
-        } else if (a.given != a.len) {
-            // cut off, or left there by an earlier step for a request that takes no part in this one
-            if (threadIdx.x < TB_MAX_NODES && !a.live)
-                r.path[threadIdx.x] = 0;
-            if (threadIdx.x == 0) {
-                r.accept_len = a.len;
-                if (!a.live)
-                    r.bonus_token = -1;
+        } else {
+            if (a.given != a.len) {
+                // cut off, or left there by an earlier step for a request that takes no part in this one
+                if (threadIdx.x < TB_MAX_NODES && !a.live)
+                    r.path[threadIdx.x] = 0;
+                if (threadIdx.x == 0) {
+                    r.accept_len = a.len;
+                    if (!a.live)
+                        r.bonus_token = -1;
+                }
             }
+            if (threadIdx.x == 0 && a.status != TB_OK)
+                r.status = a.status;
         }
         if (threadIdx.x == 0) {
             r.new_L = a.L + a.len;

@@ -185,3 +185,30 @@ def test_results_left_by_an_earlier_step(bank, layers, H):
     assert s.results.tolist() == want.tolist()
     assert s.req.lens.tolist() == want[:, 2].tolist()
     assert same(before[0], s.pools[0]) and same(before[1], s.pools[1])  # every path is in place already
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("entry", [-1, 10 ** 6])
+def test_rows_that_cannot_move_are_reported(bank, given, entry):
+    """A hole in the table under the last accepted node: that row stays, the others move, the request says so."""
+    s = Scene(61, [5, 40], [7, 7], 3, 2, 64, 8, "heads", match=1.0)
+    paths = {b: list(s.expected(b)[1]) for b in range(2)}
+    assert paths[0][-1] > 20
+    hole = (5 + paths[0][-1]) // 8
+    s.req.table[0, hole] = entry
+    stays = [j for j, u in enumerate(paths[0]) if hole in ((5 + u) // 8, (5 + j) // 8)]
+    assert len(paths[0]) - 1 in stays and len(stays) < len(paths[0])
+    kept = {0: [j if j in stays else u for j, u in enumerate(paths[0])], 1: paths[1]}
+    want = s.moved(kept)
+    kw = dict(draft=i32(s.draft), argmax=i32(s.argmax), vocab=s.vocab)
+    if given:
+        kw = {}
+        for b, path in paths.items():
+            s.results[b, 0] = len(path)
+            s.results[b, 4:4 + len(path)] = i32(np.array(path))
+    tv.paged_accept(bank, s.req, tv.Pages(*s.pools), s.results, **kw)
+    torch.cuda.synchronize()
+    assert s.results[:, 3].tolist() == [tv.TB_EINVAL, 0]
+    assert s.results[:, 0].tolist() == [len(paths[0]), len(paths[1])]
+    assert s.req.lens.tolist() == [5 + len(paths[0]), 40 + len(paths[1])]
+    assert same(s.pools[0], want[0]) and same(s.pools[1], want[1])
