@@ -706,6 +706,8 @@ typedef struct tb_logit_rules {
     const int32_t *mask_row;     /* [rows]: a row's mask row, -1 for none (NULL: row r has mask row r) */
     int64_t mask_rows;           /* with mask_row: rows of mask; a row that names one past them is allowed no
                                     token, and TB_EINVAL is set in the workspace's status word */
+    int64_t n_bias;              /* with bias_start: entries of bias_token and bias_value, 1 or more; a bias_start
+                                    that names some past them sets TB_EINVAL there, and those are left out */
 } tb_logit_rules;
 
 /* Statistics of the processed rows, as lm_head_stats and lm_head_stats_typical

@@ -114,7 +114,8 @@ class TbLogitRules(ctypes.Structure):
                 ("prompt_len", ctypes.c_void_p), ("draft", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
                 ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("bias_start", ctypes.c_void_p),
                 ("bias_token", ctypes.c_void_p), ("bias_value", ctypes.c_void_p), ("mask", ctypes.c_void_p),
-                ("mask_stride", ctypes.c_int64), ("mask_row", ctypes.c_void_p), ("mask_rows", ctypes.c_int64)]
+                ("mask_stride", ctypes.c_int64), ("mask_row", ctypes.c_void_p), ("mask_rows", ctypes.c_int64),
+                ("n_bias", ctypes.c_int64)]
 
 
 class TbLogitStats(ctypes.Structure):
@@ -799,8 +800,11 @@ def logits_process(bank, req: Requests, logits, out, ws, draft=None, history=Non
     if kind is None or out.dtype is not _F32:
         raise TypeError(f"logits {logits.dtype}, out {out.dtype}: a 32- or 16-bit float type and float32 expected")
     rows, vocab = shape
-    if bias_token is not None and bias_token.numel() == 0:
-        bias_start = None  # an empty list has no address
+    n_bias = 0
+    if bias_token is not None:
+        n_bias = bias_token.numel()
+        if n_bias == 0:
+            bias_start = None  # an empty list has no address
     width = words = mask_rows = 0
     if history is not None:
         width = history.shape[-1]
@@ -812,8 +816,8 @@ def logits_process(bank, req: Requests, logits, out, ws, draft=None, history=Non
         _arr(prompt_len, _I32, B, "prompt_len"), _arr(draft, _I32, rows, "draft"), _arr(repetition, _F32, B, "repetition"),
         _arr(presence, _F32, B, "presence"), _arr(frequency, _F32, B, "frequency"),
         _arr(bias_start, _I32, B + 1, "bias_start"), _arr(bias_token, _I32, 0, "bias_token"),
-        _arr(bias_value, _F32, 0, "bias_value"), _arr(mask, _I32, 0 if mask_row is not None else rows * words, "mask"),
-        words, _arr(mask_row, _I32, rows, "mask_row"), mask_rows)
+        _arr(bias_value, _F32, n_bias, "bias_value"), _arr(mask, _I32, 0 if mask_row is not None else rows * words, "mask"),
+        words, _arr(mask_row, _I32, rows, "mask_row"), mask_rows, n_bias)
     st = TbLogitStats(_arr(argmax, _I32, rows, "argmax"), _arr(top1, _F32, rows, "top1"),
                       _arr(entropy, _F32, rows, "entropy"), _arr(logz_t, _F32, rows, "logz_t"),
                       _arr(entropy_t, _F32, rows, "entropy_t"), _arr(draft_logit, _F32, rows, "draft_logit"))

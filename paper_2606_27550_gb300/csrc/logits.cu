@@ -74,7 +74,7 @@ struct LogitArgs {
     tb_logit_stats st;
     float temperature, inv_t;
     bool join;  // by the last CTA of a piece's rows, else by k_logits_join
-    int mask_rows;               // that mask_row may name
+    int mask_rows, n_bias;       // that mask_row may name; entries of all biases
     int *status;
     int *ticket;                 // [pieces of rows]
     Part *parts;                 // [rows][slices]
@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
     const int said = p.r.history ? load_now(p.r.history_len + b) : 0;
     const int asked = p.r.history && p.r.prompt_len ? load_now(p.r.prompt_len + b) : 0;
     const int bias0 = p.r.bias_start ? load_now(p.r.bias_start + b) : 0;
-    const int bias1 = p.r.bias_start ? load_now(p.r.bias_start + b + 1) : 0;
+    const int bias_said = p.r.bias_start ? load_now(p.r.bias_start + b + 1) : 0;
     Penalty pen;
     pen.rep = p.r.repetition ? load_now(p.r.repetition + b) : 1.f;
     pen.freq = p.r.frequency ? load_now(p.r.frequency + b) : 0.f;
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
     const int n_said = (int)min((long long)max(said, 0), (long long)p.r.history_stride);
     const int n_asked = min(max(asked, 0), n_said);
     const int32_t *h = p.r.history + (p.r.history ? b * p.r.history_stride : 0);
-    const int bias_end = bias1;
+    const int bias_end = min(bias_said, p.n_bias);
     int word_of[kAhead], bias_tok[kBiasAhead];
     float bias_val[kBiasAhead];
 #pragma unroll
@@ -484,6 +484,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
         for (int m = 0; m < kAhead; ++m)
             note_token(count, seen, (unsigned)(word_of[m] - v0), (unsigned)here, i0 + m * kThreads >= n_asked);
     }
+    if (bias_said > p.n_bias && threadIdx.x == 0)
+        atomicOr(p.status, kStatusBounds);
     // Biases, in any order as long as no token comes up twice; where one does, all again
     // by one warp in list order, so that its entries add up in a fixed order.
     for (int e = max(bias0, 0) + threadIdx.x; e < bias_end;) {
@@ -902,6 +904,8 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
                             (long long)a.r.history_stride);
     if (a.r.bias_start && (!a.r.bias_token || !a.r.bias_value))
         return record_error(TB_EINVAL, "%s: bias_start without bias_token or bias_value", fn);
+    if (a.r.bias_start && (a.r.n_bias < 1 || a.r.n_bias > 0x7fffffff))
+        return record_error(TB_EINVAL, "%s: bias_start into %lld entries", fn, (long long)a.r.n_bias);
     if (a.r.mask && a.r.mask_stride < (vocab + 31) / 32)
         return record_error(TB_EINVAL, "%s: mask_stride %lld below %d words", fn, (long long)a.r.mask_stride,
                             (vocab + 31) / 32);
@@ -928,6 +932,7 @@ extern "C" tb_status logits_process(const tb_bank *bank, const tb_requests *req,
     a.out_stride = out_stride;
     a.temperature = temperature;
     a.inv_t = 1.f / temperature;
+    a.n_bias = (int)a.r.n_bias;
     a.mask_rows = a.r.mask_row && a.r.mask_rows < 0x7fffffff ? (int)a.r.mask_rows : 0x7fffffff;
     a.status = static_cast<int *>(workspace);
     a.ticket = reinterpret_cast<int *>(static_cast<uint8_t *>(workspace) + 256);

@@ -371,3 +371,23 @@ def test_mask_rows_that_there_are_not(bank, dtype, V):
     assert s.st["entropy"][bad].tolist() == [0.0] * 3 and s.st["logz_t"][bad].tolist() == [-np.inf] * 3
     good = [i for i in range(s.R) if i not in bad]
     assert torch.equal(s.out[good], first[good]) and all(torch.equal(s.st[k][good], st[k][good]) for k in ("argmax", "entropy"))
+
+
+def test_bias_offsets_past_the_list(bank):
+    """Offsets that name entries past the last: those are left out and the call says so; the others count."""
+    s = Scene(71, [5, 2, 3], 1500, biases=30)
+    assert tv.tb_workspace_status(s.run(bank)) == tv.TB_OK
+    n = s.btok.size
+    assert s.bstart[1] < n
+    want = s.out.clone()
+    req = tv.Requests(row_start=dev(s.start), tree=dev(np.array(s.tree, np.int32)))
+    for end in (n + 1, n + 5000, 2 ** 31 - 1):
+        start = s.bstart.copy()
+        start[-1] = end  # of the last request
+        ws = tv.make_workspace(tv.tb_logits_workspace_size(3, s.R, s.V))
+        tv.logits_process(bank, req, s.logits, s.out, ws, temperature=s.T, draft=dev(s.draft), history=dev(s.hist),
+                          history_len=dev(s.hist_len), prompt_len=dev(s.prompt), repetition=dev(s.rep), presence=dev(s.pres),
+                          frequency=dev(s.freq), bias_start=dev(start), bias_token=dev(s.btok), bias_value=dev(s.bval),
+                          mask=dev(pack_bits(s.allowed)), **s.st)
+        torch.cuda.synchronize()
+        assert tv.tb_workspace_status(ws) == tv.TB_EINVAL and torch.equal(s.out, want)

@@ -284,3 +284,26 @@ def test_the_attention_and_its_join(lib, s):
     for launch in (first, second):
         assert launch.stream == STREAM and launch.pdl and launch.cluster == 1 and launch.device == 0
     assert first.grid == (152, 1, 1) and first.block == 512 and second.block == 256
+
+
+def test_bias_offsets_need_the_lists_length(lib, s):
+    """bias_start indexes the bias lists on the device: the C call wants to know how long they are."""
+    start, token, value = torch.zeros(4, dtype=torch.int32), torch.zeros(5, dtype=torch.int32), torch.zeros(5)
+    rules = tv.TbLogitRules()
+    rules.bias_start, rules.bias_token, rules.bias_value = start.data_ptr(), token.data_ptr(), value.data_ptr()
+    out = torch.zeros(9, 100)
+
+    def call():
+        return lib.logits_process(s.bank.handle, ctypes.byref(s.req.as_c()), s.logits.data_ptr(), tv.TB_F32, 100, 9, 100,
+                                  ctypes.byref(rules), 1.0, out.data_ptr(), 100, None, s.lws.data_ptr(), s.lws.numel(), STREAM)
+
+    for n in (0, -1, 2 ** 31):
+        rules.n_bias = n
+        assert call() == tv.TB_EINVAL and fake_cuda.launches(lib) == []
+    rules.n_bias = 5
+    assert call() == tv.TB_OK and len(fake_cuda.launches(lib)) == 1
+    s.process(bias_start=start, bias_token=token, bias_value=value)
+    s.process(bias_start=start, bias_token=token[:0], bias_value=value[:0])
+    assert len(fake_cuda.launches(lib)) == 2
+    with pytest.raises(ValueError):
+        s.process(bias_start=start, bias_token=token, bias_value=value[:4])
