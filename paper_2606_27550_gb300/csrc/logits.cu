@@ -17,7 +17,8 @@
 // Bound by HBM while the logits stream (at that pace three CTAs of an SM together would
 // take 9 TB/s), but half of a CTA's life goes into its rules, where it waits for memory
 // in turn: parameters, history and tree, the rows' first chunks.  Eight trees (358 rows)
-// at 128256 tokens 76 us, 4.9 TB/s; 68 without rules; 256 requests of one row 153 us.
+// at 128256 tokens 77 us, 4.9 TB/s; 68 without rules; 256 requests of one row 154 us.
+// 16-bit logits take as long (76 us, a quarter fewer bytes): instructions bound them.
 //
 // With x = z - m, m the warp's running maximum, each lane keeps s = sum e^x, u = sum
 // x e^x and the two sums at temperature T, rescaled when a chunk has a new maximum;
@@ -649,7 +650,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
                     touch(from);
             }
             // a lane's logits: four in a row of each 128, or where that is not aligned (and at a slice's
-            // end) one of each 32: eight trees at 128255 tokens 87 us, 98 with four in a row one by one;
+            // end) one of each 32: eight trees at 128255 tokens 88 us, 98 with four in a row one by one;
             // bf16 107 us, 150 without the ring
             const bool four = vec && c + kChunk <= here;
             const int mine = four ? 4 * lane : lane, next = four ? 1 : 32;
@@ -816,8 +817,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logits(const __grid_consta
 
 // Where CTAs follow one another on an SM, each one's way to the ticket and back (its
 // stores have to land first) costs more than another launch: 256 requests of one row of
-// 128256 tokens 162 us with this kernel and 189 with the last CTA's join, 16 of them
-// 17.2 and 18.3.  Below that it is one launch less at the same time (9.7 us for a tree
+// 128256 tokens took 162 us with this kernel and 189 with the last CTA's join when it was
+// chosen (154 now), 16 of them 17.2 and 18.3 (16.3 now).  Below that it is one launch less at the same time (9.7 us for a tree
 // of 26 nodes at 32000 tokens).
 template <int kStats>
 __global__ void __launch_bounds__(kThreads) k_logits_join(const __grid_constant__ LogitArgs p)

@@ -194,7 +194,7 @@ __device__ __forceinline__ void move_rows(const AcceptArgs &p, const Accepted &a
 }
 
 // Bound by the latency of the chain lengths, tree and tokens and table, rows (one
-// request of two layers: 2.75 us; 3.6 with each of these loads behind the one before);
+// request of two layers: 2.8 us; 3.6 with each of these loads behind the one before);
 // with many requests by the scattered 128- or 256-byte rows, read and written (64
 // requests of 32 layers and 8 heads, 36 MB: 9.4 us, 3.8 TB/s; 512 of them 50 us, 5.0).
 __global__ void __launch_bounds__(kThreads) k_paged_accept(const __grid_constant__ AcceptArgs p)

@@ -19,7 +19,7 @@
 // A tile's 128 slots are 128 / page_size pages (or a part of one): the lanes of a
 // producer warp look their pages up one tile ahead and issue one TMA box each.
 // Pages past the request's end, and ids outside the pool, are addressed past the
-// last page, where TMA fills zeros.  Slots of a landed tile that no row may see (a
+// last page, where TMA fills zeros; such an id where some row looks is reported.  Slots of a landed tile that no row may see (a
 // page's rest behind the last token, before a document's beginning, between the
 // kept first tokens and the window) can hold anything: their scores are replaced
 // (not multiplied) by -inf, and the softmax threads overwrite their V rows with
@@ -35,15 +35,17 @@
 // sub-partitions.
 //
 // Bound by HBM where rows are few (64 requests of one token, 8 kv heads of 128, prefixes
-// of 512 to 8192: 182 us, 6.37 TB/s, 94 % of a copy's bandwidth; 32 kv heads at 65536
-// keys 166 us, 95 %), by the softmax's chain per tile with 128 rows per kv head (two row
-// blocks of 64 nodes at 65536 keys: 75 us, 0.91 PFLOP/s; 2060 cycles a tile, 700 of them
+// of 512 to 8192: 182 us, 6.37 TB/s, 94 % of a copy's bandwidth, 206 us with a cap and 201
+// with a bias, whose special functions run for 128 rows where 4 are there; 32 kv heads at
+// 65536 keys 166 us, 95 %), by the softmax's chain per tile with 128 rows per kv head (two row
+// blocks of 64 nodes at 65536 keys: 76 us, 0.91 PFLOP/s; 2060 cycles a tile, 700 of them
 // for the weights, 260 for the exchange between the halves, 340 waiting for S, whose
 // 16 MMAs with P V take over 100 cycles each), and by
-// the way to the first tile, unit boundaries and the join in short calls (9.3 us for a
-// tree of 7 nodes at 128 keys, 52 us for 32 heads at 16384 keys).  Eight ragged trees with capped scores
-// took 51.7 us with one softmax thread per row, 47.9 with two, 43.7 with packed pairs and
-// one reciprocal for four caps.
+// the way to the first tile, unit boundaries and the join in short calls (9.1 us for a
+// tree of 7 nodes at 128 keys, 52 us for 32 heads at 16384 keys).  Eight ragged trees with
+// capped scores take 44.5 us; they took 51.7 with one softmax thread per row, 47.9 with two,
+// and 43.6 with packed pairs and one reciprocal for four caps, before holes in the table
+// were reported.
 #include "paged.cuh"
 
 #include <cuda_fp16.h>

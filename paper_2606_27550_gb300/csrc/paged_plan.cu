@@ -13,7 +13,8 @@
 // sums, while the first CTA makes the attention's split.  Taken ids come from the
 // ring's free part and given ones go behind it, so no CTA reads what another
 // writes; `held` and the ring's state, which may be updated in place, are written by
-// the CTA that finishes last (an arrival ticket in the plan).
+// the CTA that finishes last (an arrival ticket in the plan).  A further plan of the
+// same step has `held` but no ring: it refuses what the first one refused.
 //
 // The attention's split.  Requests are put in order of their row blocks (blocks of
 // 128 query rows per kv head), the most first, and their key tiles behind one
@@ -30,8 +31,10 @@ namespace {
 
 constexpr int kThreads = 256;
 // Tiles of an attention CTA at least: fewer CTAs on a small problem, but fewer
-// partials to join.  (1: a single request of 64 nodes at 512 keys 14.7 us, with 2
-// 17.2; two kv heads at 4096 keys 18.9 and 17.8.)
+// partials to join.  Neither 1 nor 2 is better throughout.  In us with 1 and with 2:
+// 64 nodes over 512 keys, 32 / 8 heads 13.7 and 16.2, 32 / 32 heads 14.7 and 13.8,
+// 2 / 2 heads 11.2 and 12.7; over 4096 keys, 2 / 2 heads 18.1 and 16.4, 8 / 2 heads
+// 20.3 and 19.8; one ragged capped tree 15.9 and 14.9; one token 12.6 with either.
 constexpr int kMinTiles = 2;
 
 struct PlanArgs {
@@ -323,8 +326,8 @@ __device__ void make_split(const PlanArgs &p, const Sums &s)
 }
 
 // Bound by latency: every CTA's chain is a handful of dependent loads (length, tree,
-// page id) and the sums; the first CTA's ends with the split.  8 requests 6.9 us,
-// 1024 requests with 31000 rows 12.5 us.
+// page id) and the sums; the first CTA's ends with the split.  8 requests 7.0 us,
+// 1024 requests with 31000 rows 12.8 us.
 __global__ void __launch_bounds__(kThreads) k_paged_plan(const __grid_constant__ PlanArgs p)
 {
     extern __shared__ __align__(16) uint8_t smem[];

@@ -5,9 +5,10 @@
 // pos taken from the axis that owns pair i.  Only the fraction of a turn
 // matters, so the frequency in turns, theta^(-2i/d) / (2 pi) < 1, is held as a
 // 64-bit fixed-point fraction and pos * frequency is one 64-bit integer product,
-// whose overflow is the whole turns: the fraction is right to pos * 2^-65 of a
-// turn at any position, where a 32-bit float product loses it after a few
-// thousand turns.
+// whose overflow is the whole turns: the fraction is as right as the frequency,
+// to pos * 2^-65 of a turn where the host's long double has 113 bits (Arm), and
+// to pos * 2^-62 where it has 64 (2^-64 for theta of 100 and more), where a
+// 32-bit float product loses it after a few thousand turns.
 //
 // A CTA takes a few rows: their (cos, sin) once into shared memory (they serve
 // all heads), then every (row, head, 16-byte piece of the lower half of the head
@@ -65,9 +66,9 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi)
 }
 
 // kRope: queries and keys turn.  Bound by HBM: each element is read once and
-// written once.  8191 rows of a prompt, 32 heads of 128 (403 MB): 65.4 us, 6.16 TB/s,
-// 91 % of a copy's bandwidth, with two items per thread in flight (69.4 with one); a
-// step's few hundred rows (8.9 MB): 3.45 us, a launch and one round trip.
+// written once.  8191 rows of a prompt, 32 heads of 128 (403 MB): 65.7 us, 6.13 TB/s,
+// 90 % of a copy's bandwidth, with two items per thread in flight (69.4 with one); a
+// step's few hundred rows (8.9 MB): 3.4 us, a launch and one round trip.
 template <bool kF16, bool kRope>
 __global__ void __launch_bounds__(kThreads) k_paged_store(const __grid_constant__ StoreArgs p)
 {
@@ -192,7 +193,9 @@ u128 fraction_of(long double x)  // 0 <= x < 1
 
 // freq[i] = theta^(-2i/d) / (2 pi) as a fraction of 2^64, a geometric series in
 // 128 bits whose ratio r = theta^(-2/d) is Newton's step on r^(d/2) = 1 / theta
-// from its double value (64 calls of a long-double pow took 90 us a call on the
+// from its double value, in long double: half a unit of 2^-64 off where that has
+// 113 bits; with 64 bits up to 0.8 units for theta of 100 and more, 3.1 at theta 2,
+// since the ratio's error grows with i (64 calls of a long-double pow took 90 us a call on the
 // GB300's host).
 void turns(double theta, int d, uint64_t *freq)
 {
