@@ -48,6 +48,7 @@ class Server:
         self.parents = [synth.chain(1), synth.rank_product_tree((3, 2, 1), 8), synth.rank_product_tree((4, 3, 2, 1), 26)]
         for p in self.parents:
             self.bank.add(p)
+        self.nodes = torch.tensor([len(p) for p in self.parents], dtype=i32, device=dev)
         self.rows = 64 * batch
         self.pool = tv.make_page_pool(n_pages, batch)
         shape = (model.layers, n_pages, model.H, page_size, model.d)
@@ -89,22 +90,27 @@ class Server:
 
     def admit(self, prompts):
         """Prompts (token lists, by slot): their keys and values into pages.  (The toy model's layers see
-        a prompt's embeddings; a real one attends among the prompt's own tokens here.)"""
+        a prompt's embeddings; a real one attends among the prompt's own tokens here.)  Returns the slots
+        whose prompt found no room: nothing of them was stored."""
         m = self.m
         n_new = [len(prompts.get(b, ())) for b in range(self.B)]
         self.fill.n_new.copy_(torch.tensor(n_new, dtype=torch.int32))
         rows = sum(n_new)
         slots, positions = self._slots(rows)
         tv.paged_plan(None, self.fill, slots, positions, self.status, self.plan, pool=self.pool)
-        x = m.embed[torch.tensor([t for b in range(self.B) for t in prompts.get(b, ())], device="cuda")]
+        refused = [b for b, why in enumerate(self.status.tolist()) if why and b in prompts]
+        prompts = {b: tokens for b, tokens in prompts.items() if b not in refused}
+        tokens = [t for b in range(self.B) for t in prompts.get(b, ())]
+        x = m.embed[torch.tensor(tokens, dtype=torch.int64, device="cuda")]
         for layer in range(m.layers):
-            self._layer(layer, x, slots, positions, attend=False)
-        self.req.lens.add_(self.fill.n_new)
+            self._layer(layer, x, slots[:len(tokens)], positions[:len(tokens)], attend=False)
+        self.req.lens.add_(self.fill.n_new * (self.status == 0))
         for b, tokens in prompts.items():
             # the last prompt token is the root of the first tree: its keys come with that
             self.req.lens[b] -= 1
             self.history[b, :len(tokens)] = torch.tensor(tokens, dtype=torch.int32)
             self.said[b] = self.asked[b] = len(tokens)
+        return refused
 
     def finish(self, slot):
         """Ends a request: its pages go back with the next plan."""
@@ -112,12 +118,14 @@ class Server:
         self.req.tree[slot] = -1
 
     def step(self, trees, draft):
-        """One step: trees int32 [B] (bank ids, -1: none), draft int32 [rows] (roots: the last token)."""
+        """One step: trees int32 [B] (bank ids, -1: none), draft int32 [rows] (roots: the last token), the
+        trees' nodes one after the other.  A request that finds no room waits: its length stays."""
         m = self.m
         self.req.tree.copy_(trees)
         slots, positions = self._slots(self.rows)
         tv.paged_plan(self.bank, self.req, slots, positions, self.status, self.plan, pool=self.pool, n_q_heads=m.Hq,
                       n_kv_heads=m.H)
+        draft = self._drafted_rows(draft)
         x = m.embed[draft.long()]
         for layer in range(m.layers):
             x = self._layer(layer, x, slots, positions, attend=True)
@@ -129,6 +137,15 @@ class Server:
         tv.paged_accept(self.bank, self.req, self.pages, self.results, draft=draft, argmax=argmax, vocab=m.vocab)
         self._note(draft)
         return logits, argmax
+
+    def _drafted_rows(self, draft):
+        """The draft tokens in the plan's rows, which leave out the requests that it refused (on the GPU)."""
+        drafted = torch.where(self.req.tree < 0, 0, self.nodes[self.req.tree.long()])
+        first = drafted.cumsum(0) - drafted
+        row = torch.arange(self.rows, dtype=torch.int32, device="cuda")
+        b = torch.searchsorted(self.req.row_start[1:], row, right=True).clamp(max=self.B - 1)
+        at = first[b] + row - self.req.row_start[b]
+        return torch.where(row < self.req.row_start[-1], draft[at.clamp(0, self.rows - 1)], 0)
 
     def _note(self, draft):
         """Appends the accepted drafts and the bonus token of every request to its history (on the GPU)."""

@@ -609,7 +609,9 @@ TB_API size_t tb_paged_plan_size(int batch, int device);
  *             tree or a negative length, TB_ECAPACITY when it needs more than
  *             max_pages, its rows do not fit max_rows, or the ring has run out
  *             (then later requests that need pages get none either; without a
- *             ring, those that need more than they hold)
+ *             ring, those that need more than they hold).  The rows of those
+ *             behind it move up: per-row inputs that were made before the call
+ *             (draft tokens) have to be laid out by row_start
  *   plan      the attention's work split for n_q_heads / n_kv_heads, window and
  *             sink (0, 0: none; see paged_tree_attention), read by
  *             paged_tree_attention calls of this step; a model whose layers

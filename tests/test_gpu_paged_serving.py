@@ -214,3 +214,39 @@ def test_a_step_without_rows():
     assert status.tolist() == [tv.TB_ECAPACITY] * 3 and req.row_start.tolist() == [0] * 4
     assert pool.held.tolist() == [2, 2, 0] and pool.state.tolist() == [6, 5]
     bank.close()
+
+
+def test_the_example_when_the_pages_run_out():
+    """A prompt and a tree that find no room: their requests wait, and the others go on as they would alone."""
+    import paged_serving as ex
+
+    model = ex.Model()
+    prompts = {b: list(range(5 * b + 2, 5 * b + 2 + n)) for b, n in enumerate((5, 16, 6, 7))}
+    small, large = ex.Server(model, n_pages=4), ex.Server(model)
+    for server in (small, large):
+        assert not server.admit(prompts)
+    assert small.pool.state.tolist()[1] == 0
+    # request 1 needs two more pages for its tree and there is none; in the other server it waits by itself
+    small.step(torch.tensor([1, 2, 1, 0], dtype=torch.int32), ex.drafts(small, [1, 2, 1, 0]))
+    large.step(torch.tensor([1, -1, 1, 0], dtype=torch.int32), ex.drafts(large, [1, -1, 1, 0]))
+    assert small.status.tolist() == [0, tv.TB_ECAPACITY, 0, 0] and large.status.tolist() == [0] * 4
+    assert tv.tb_workspace_status(small.ws) == 0
+    for name in ("results", "said", "history"):
+        assert torch.equal(getattr(small, name), getattr(large, name)), name
+    assert torch.equal(small.req.lens, large.req.lens) and small.req.lens.tolist()[1] == 15
+    for layer in range(model.layers):
+        for b in (0, 2, 3):
+            for x, y in zip(cached(small, layer, b, 8), cached(large, layer, b, 8)):
+                assert torch.equal(x[:int(small.req.lens[b])], y[:int(small.req.lens[b])])
+    # a prompt that finds no room, and with it the one behind it, which does the next time
+    server = ex.Server(model, n_pages=3)
+    assert server.admit({0: prompts[0]}) == []
+    kept = [cached(server, layer, 0, 5) for layer in range(model.layers)]
+    assert server.admit({1: list(range(40)), 2: [9, 3]}) == [1, 2]
+    assert server.req.lens.tolist() == [4, 0, 0, 0] and server.pool.held.tolist() == [1, 0, 0, 0]
+    assert server.admit({2: [9, 3]}) == []
+    assert server.req.lens.tolist() == [4, 0, 1, 0] and server.pool.held.tolist() == [1, 0, 1, 0]
+    assert server.said.tolist() == [5, 0, 2, 0]
+    for layer in range(model.layers):
+        for x, y in zip(cached(server, layer, 0, 5), kept[layer]):
+            assert torch.equal(x, y)
