@@ -764,6 +764,80 @@ TB_API tb_status paged_accept(const tb_bank *bank, const tb_requests *req, const
                               const int32_t *draft_tokens, const int32_t *argmax, int n_rows, int vocab,
                               tb_result *results, int32_t *lens_out, tb_stream stream);
 
+/* ------------------------------------------------------------------------
+ * Norms of queries and keys for each head before the rotation, and the paged
+ * cache in 4 bits: calls that stand beside those above and take the same
+ * requests, plans, pools and results (paged_plan and logits_process serve
+ * both).
+ * ---------------------------------------------------------------------- */
+
+/* Norms of the heads (a head's row x, weight w [head_dim] of the rows' type):
+ *   r = 1 / sqrt(mean(x^2) + eps),   y = (x r) (weight_offset + w)
+ * r rounded once to 32 bits, each product too.  A NULL weight leaves that operand
+ * as it is.  eps >= 0; weight_offset is 0, or 1 where a model holds w - 1. */
+typedef struct tb_head_norm {
+    const void *q_weight; /* device, 16-byte aligned */
+    const void *k_weight;
+    float eps;
+    float weight_offset;
+} tb_head_norm;
+
+/* paged_kv_store with norms: q and k are normed, then turned, then rounded to
+ * their type, in one pass; v is stored as it is.  norm NULL: none.  The angles'
+ * sines and cosines are right to half a unit in the last place of 32 bits (but
+ * for about one in a thousand), and the rotation is taken as
+ *   a' = fl(fl(a c) - fl(b s)),   b' = fl(fl(b c) + fl(a s))
+ * so that its results are those of the same formulas in any 32-bit arithmetic
+ * (paged_kv_store's may differ from them in the last bit).  One kernel. */
+TB_API tb_status paged_kv_store_norm(const tb_pages *pages, int layer, const int64_t *slots, int n_rows,
+                                     const tb_rows *k, const tb_rows *v, const tb_rows *q, const tb_rows *q_out,
+                                     int n_q_heads, const tb_head_norm *norm, const tb_rope *rope, tb_stream stream);
+
+/* Pages that hold K and V in 4 bits.  32 consecutive elements of a head's row
+ * share a scale s: one byte, bits 7 to 14 of the fp16 number s (5 exponent bits,
+ * 3 mantissa bits, no sign).  An element is (c - 8) s with a code c of 4 bits.
+ * The page of one (layer, page, kv head) is a block of
+ *   page_size rows of head_dim / 2 bytes: element e in byte e / 2, the even one
+ *   in its low half, then page_size rows of head_dim / 32 bytes: the scales
+ * at k + layer * layer_stride + page * page_stride + head * head_stride, likewise
+ * V; strides in bytes, multiples of 16, so that any order of layers, pages and
+ * heads, and pools that hold K and V side by side, will do.  (c - 8) s has at most
+ * 7 significant bits: it is exact in bf16 and fp16.  dtype (TB_BF16 or TB_F16) is
+ * the type of the queries, keys, values and outputs of the calls; page_size
+ * and head_dim as for tb_pages. */
+typedef struct tb_pages_q4 {
+    void *k;
+    void *v;
+    int64_t layer_stride, page_stride, head_stride;
+    int32_t n_layers, n_pages, n_kv_heads, page_size, head_dim;
+    int32_t dtype;
+} tb_pages_q4;
+
+/* paged_kv_store_norm into 4-bit pages: keys as they are after norm and rotation,
+ * in 32 bits, and values take per 32 elements x
+ *   t = fl(max |x| / 7);  s = t rounded up to 4 significant bits (below 2^-14: to a
+ *   multiple of 2^-17), 9216 at most;  c = 8 + clamp(rint(fl(x / s)), -7, 7)
+ * (s = 0: c = 8).  A group with a NaN or an infinity gets the scale NaN (byte 255)
+ * and c = 15.  Rows, slots, queries and padding as for paged_kv_store.  One kernel. */
+TB_API tb_status paged_kv_store_q4(const tb_pages_q4 *pages, int layer, const int64_t *slots, int n_rows,
+                                   const tb_rows *k, const tb_rows *v, const tb_rows *q, const tb_rows *q_out,
+                                   int n_q_heads, const tb_head_norm *norm, const tb_rope *rope, tb_stream stream);
+
+/* Reads rows back in 16 bits (a cached prefix for its prompt's attention, a
+ * request that moves elsewhere): row r of layer `layer` + i, 0 <= i < n_layers, at
+ * k->ptr + i * row_layer_stride + r * row_stride + head * head_stride (strides in
+ * elements of pages->dtype, multiples of 8), likewise v; exact.  A slot outside
+ * the pool (-1: padding) leaves its rows as they were; a slot may be named more
+ * than once.  n_rows >= 0, n_layers >= 1; one kernel. */
+TB_API tb_status paged_kv_load_q4(const tb_pages_q4 *pages, int layer, int n_layers, const int64_t *slots, int n_rows,
+                                  const tb_rows *k, const tb_rows *v, int64_t row_layer_stride, tb_stream stream);
+
+/* paged_accept over 4-bit pages: the accepted rows' codes and scales move as they
+ * lie; everything else is paged_accept's.  One kernel. */
+TB_API tb_status paged_accept_q4(const tb_bank *bank, const tb_requests *req, const tb_pages_q4 *pages,
+                                 const int32_t *draft_tokens, const int32_t *argmax, int n_rows, int vocab,
+                                 tb_result *results, int32_t *lens_out, tb_stream stream);
+
 /* Message for the last failing call on this thread ("" if none). */
 TB_API const char *tb_last_error(void);
 

@@ -38,7 +38,8 @@ API = ("tb_canonicalize", "tb_create", "tb_add_topology", "tb_get_topology", "tb
        "lm_head_stats_typical", "typical_accept", "verify_step_typical", "verify_step_batched_typical",
        "verify_step_scheduled", "spec_sample_accept", "verify_step_sampled", "tb_debug_bounds_violations",
        "tb_debug_bounds_build", "tb_launch_count", "tb_paged_plan_size", "paged_plan", "paged_kv_store",
-       "paged_tree_attention", "logits_process", "tb_logits_workspace_size", "paged_accept")
+       "paged_tree_attention", "logits_process", "tb_logits_workspace_size", "paged_accept", "paged_kv_store_norm",
+       "paged_kv_store_q4", "paged_kv_load_q4", "paged_accept_q4")
 
 
 class TreeVerifyError(RuntimeError):
@@ -87,6 +88,13 @@ class TbPages(ctypes.Structure):
                 ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
+class TbPagesQ4(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("layer_stride", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("n_layers", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
 class TbRequests(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("tree", ctypes.c_void_p), ("n_new", ctypes.c_void_p),
@@ -107,6 +115,11 @@ class TbRope(ctypes.Structure):
 
 class TbRows(ctypes.Structure):
     _fields_ = [("ptr", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class TbHeadNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("weight_offset", ctypes.c_float)]
 
 
 class TbLogitRules(ctypes.Structure):
@@ -176,6 +189,10 @@ def load(path: str = LIB_PATH):
         "tb_logits_workspace_size": [i32, i32, i32],
         "logits_process": [P, P, P, i32, i64, i32, i32, P, ctypes.c_float, P, i64, P, P, sz, P],
         "paged_accept": [P, P, P, P, P, i32, i32, P, P, P],
+        "paged_kv_store_norm": [P, i32, P, i32, P, P, P, P, i32, P, P, P],
+        "paged_kv_store_q4": [P, i32, P, i32, P, P, P, P, i32, P, P, P],
+        "paged_kv_load_q4": [P, i32, i32, P, i32, P, P, i64, P],
+        "paged_accept_q4": [P, P, P, P, P, i32, i32, P, P, P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -735,14 +752,9 @@ def _rows_of(t, rows: int, heads: int, d: int, dtype, what: str) -> TbRows:
     return TbRows(t.data_ptr(), s[0], s[1])
 
 
-def paged_kv_store(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None, positions=None, sections=None,
-                   rope_theta: float = 0.0, stream=None):
-    """k, v [rows][n_kv_heads][head_dim] and q, q_out [rows][n_q_heads][head_dim] (views of any row
-    and head strides); positions int32 [rows] or [axes][rows]; sections: pairs per axis (None: one axis)."""
-    c, dtype = pages._c, pages.dtype
-    rows, heads, H, d = slots.shape[0], 0, c.n_kv_heads, c.head_dim
-    ck, cv = _rows_of(k, rows, H, d, dtype, "k"), _rows_of(v, rows, H, d, dtype, "v")
-    cq = co = rope = None
+def _queries_and_rope(q, q_out, rows: int, d: int, dtype, positions, sections, rope_theta: float):
+    """(heads, q, q_out, rope) of a store's arguments, None for what is not there."""
+    heads, cq, co, rope = 0, None, None, None
     if q is not None:
         heads = q.shape[1]
         cq = _rows_of(q, rows, heads, d, dtype, "q")
@@ -755,29 +767,151 @@ def paged_kv_store(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None
         if stride < rows:
             raise ValueError(f"positions: {stride} of {rows} rows")
         rope = TbRope(rope_theta, axes, (*sections,), _arr(positions, _I32, axes * stride, "positions"), stride)
+    return heads, cq, co, rope
+
+
+def paged_kv_store(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None, positions=None, sections=None,
+                   rope_theta: float = 0.0, stream=None):
+    """k, v [rows][n_kv_heads][head_dim] and q, q_out [rows][n_q_heads][head_dim] (views of any row
+    and head strides); positions int32 [rows] or [axes][rows]; sections: pairs per axis (None: one axis)."""
+    c, dtype = _page_kind(pages, Pages), pages.dtype
+    rows, H, d = slots.shape[0], c.n_kv_heads, c.head_dim
+    ck, cv = _rows_of(k, rows, H, d, dtype, "k"), _rows_of(v, rows, H, d, dtype, "v")
+    heads, cq, co, rope = _queries_and_rope(q, q_out, rows, d, dtype, positions, sections, rope_theta)
     rc = load().paged_kv_store(ctypes.byref(c), layer, _arr(slots, _I64, rows, "slots"), rows, ctypes.byref(ck),
                                ctypes.byref(cv), _ref(cq), _ref(co), heads, _ref(rope), _stream(stream))
     if rc:
         _check(rc, "paged_kv_store")
 
 
+def _norm_of(q_norm, k_norm, eps: float, weight_offset: float, d: int, dtype):
+    if q_norm is None and k_norm is None:
+        return None
+    return TbHeadNorm(_arr(q_norm, dtype, d, "q_norm"), _arr(k_norm, dtype, d, "k_norm"), eps, weight_offset)
+
+
+def _page_kind(pages, kind):
+    """The C struct of pages, which have to be of the kind that the call reads them as."""
+    if type(pages) is not kind:
+        raise TypeError(f"pages: {type(pages).__name__}, {kind.__name__} expected")
+    return pages._c
+
+
+def _store_rows(name: str, kind, pages, layer: int, slots, k, v, q, q_out, q_norm, k_norm, eps, weight_offset,
+                positions, sections, rope_theta, stream):
+    c, dtype = _page_kind(pages, kind), pages.dtype
+    rows, H, d = slots.shape[0], c.n_kv_heads, c.head_dim
+    ck, cv = _rows_of(k, rows, H, d, dtype, "k"), _rows_of(v, rows, H, d, dtype, "v")
+    heads, cq, co, rope = _queries_and_rope(q, q_out, rows, d, dtype, positions, sections, rope_theta)
+    norm = _norm_of(q_norm, k_norm, eps, weight_offset, d, dtype)
+    rc = getattr(load(), name)(ctypes.byref(c), layer, _arr(slots, _I64, rows, "slots"), rows, ctypes.byref(ck),
+                               ctypes.byref(cv), _ref(cq), _ref(co), heads, _ref(norm), _ref(rope), _stream(stream))
+    if rc:
+        _check(rc, name)
+
+
+def paged_kv_store_norm(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None, q_norm=None, k_norm=None,
+                        eps: float = 1e-6, weight_offset: float = 0.0, positions=None, sections=None,
+                        rope_theta: float = 0.0, stream=None):
+    """paged_kv_store with norms of the heads before the rotation: q_norm, k_norm [head_dim] of the pages'
+    type, None where that operand is left as it is."""
+    _store_rows("paged_kv_store_norm", Pages, pages, layer, slots, k, v, q, q_out, q_norm, k_norm, eps,
+                weight_offset, positions, sections, rope_theta, stream)
+
+
+class PagesQ4:
+    """The paged cache in 4 bits: k and v uint8 [n_layers][n_pages][n_kv_heads][q4_page_bytes], views of any strides
+    (multiples of 16, a page's bytes contiguous), the same for both; dtype: the type of the rows that go in and out.
+    Which tensors they are is fixed; what they hold is read and written by every call."""
+
+    __slots__ = ("_k", "_v", "_c", "dtype")
+    k = property(lambda self: self._k)
+    v = property(lambda self: self._v)
+
+    def __init__(self, k, v, page_size: int, head_dim: int, dtype):
+        import torch
+
+        s, shape = k.stride(), k.shape
+        n = q4_page_bytes(page_size, head_dim)
+        if len(s) != 4 or s[3] != 1 or shape[3] != n or v.stride() != s or v.shape != shape:
+            raise ValueError(f"4-bit pages: k and v of one 4-D shape and strides, {n} contiguous bytes per page and head")
+        if k.dtype is not torch.uint8 or v.dtype is not torch.uint8:
+            raise TypeError(f"4-bit pages: {k.dtype}, {v.dtype}, uint8 expected")
+        if _KINDS is None:
+            _torch_types()
+        kind = _KINDS.get(dtype, TB_F32)
+        if kind == TB_F32:
+            raise TypeError(f"4-bit pages: rows of {dtype}, bfloat16 or float16 expected")
+        self._k, self._v, self.dtype = k, v, dtype
+        self._c = TbPagesQ4(k.data_ptr(), v.data_ptr(), *s[:3], *shape[:3], page_size, head_dim, kind)
+
+    def as_c(self) -> TbPagesQ4:
+        return self._c
+
+
+def q4_page_bytes(page_size: int, head_dim: int) -> int:
+    """Bytes of one head's block of a 4-bit page: codes, then a scale byte per 32 elements."""
+    return page_size * (head_dim // 2 + head_dim // 32)
+
+
+def make_pages_q4(n_layers: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, dtype,
+                  device="cuda") -> PagesQ4:
+    """Zero-filled 4-bit pages (every element 0)."""
+    import torch
+
+    shape = (n_layers, n_pages, n_kv_heads, q4_page_bytes(page_size, head_dim))
+    return PagesQ4(*(torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2)), page_size, head_dim, dtype)
+
+
+def paged_kv_store_q4(pages: PagesQ4, slots, k, v, layer: int = 0, q=None, q_out=None, q_norm=None, k_norm=None,
+                      eps: float = 1e-6, weight_offset: float = 0.0, positions=None, sections=None,
+                      rope_theta: float = 0.0, stream=None):
+    """paged_kv_store_norm into 4-bit pages; the operands have the pages' row type."""
+    _store_rows("paged_kv_store_q4", PagesQ4, pages, layer, slots, k, v, q, q_out, q_norm, k_norm, eps,
+                weight_offset, positions, sections, rope_theta, stream)
+
+
+def paged_kv_load_q4(pages: PagesQ4, slots, k, v, layer: int = 0, stream=None):
+    """Rows of 4-bit pages in 16 bits: k, v [rows][n_kv_heads][head_dim] of one layer, or [n_layers][rows][n_kv_heads]
+    [head_dim] of `layer` and the ones behind it (views of any layer, row and head strides, the same layer stride)."""
+    c, dtype = _page_kind(pages, PagesQ4), pages.dtype
+    rows, layers, stride = slots.shape[0], 1, 0
+    if len(k.shape) == 4:
+        layers, stride = k.shape[0], k.stride(0)
+        if len(v.shape) != 4 or v.shape[0] != layers or (v.stride(0) != stride and layers > 1):
+            raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}: one number of layers and one layer stride expected")
+        if layers < 1:
+            raise ValueError("no layers")
+        k, v = k[0], v[0]
+    ck = _rows_of(k, rows, c.n_kv_heads, c.head_dim, dtype, "k")
+    cv = _rows_of(v, rows, c.n_kv_heads, c.head_dim, dtype, "v")
+    rc = load().paged_kv_load_q4(ctypes.byref(c), layer, layers, _arr(slots, _I64, rows, "slots"), rows,
+                                 ctypes.byref(ck), ctypes.byref(cv), stride, _stream(stream))
+    if rc:
+        _check(rc, "paged_kv_load_q4")
+
+
 def paged_tree_attention(bank: Bank, req: Requests, pages: Pages, plan, q, out, ws, layer: int = 0,
                          scale: float | None = None, softcap: float = 0.0, slopes=None, lse=None, stream=None):
     """q, out [rows][n_q_heads][head_dim] of the pages' type; lse float [rows][n_q_heads]; slopes float [n_q_heads];
     scale: 1 / sqrt(head_dim) unless given."""
-    c, dtype = pages._c, pages.dtype
+    _attend("paged_tree_attention", Pages, bank, req, pages, plan, q, out, ws, layer, scale, softcap, slopes, lse, stream)
+
+
+def _attend(name: str, kind, bank, req, pages, plan, q, out, ws, layer, scale, softcap, slopes, lse, stream):
+    c, dtype = _page_kind(pages, kind), pages.dtype
     shape = q.shape
     rows, heads, d = shape
     if (q.dtype is not dtype or out.dtype is not dtype or out.shape != shape or d != c.head_dim or
             not q.is_contiguous() or not out.is_contiguous()):
         raise ValueError(f"q {q.dtype} {tuple(shape)}, out {out.dtype} {tuple(out.shape)}: contiguous {dtype} "
                          f"(rows, heads, {c.head_dim}) expected for both")
-    rc = load().paged_tree_attention(bank.handle, ctypes.byref(req._c), ctypes.byref(c), layer, plan.data_ptr(),
-                                     plan.numel(), q.data_ptr(), rows, heads, d ** -0.5 if scale is None else scale,
-                                     softcap, _arr(slopes, _F32, heads, "slopes"), out.data_ptr(),
-                                     _arr(lse, _F32, rows * heads, "lse"), ws.data_ptr(), ws.numel(), _stream(stream))
+    rc = getattr(load(), name)(bank.handle, ctypes.byref(req._c), ctypes.byref(c), layer, plan.data_ptr(),
+                               plan.numel(), q.data_ptr(), rows, heads, d ** -0.5 if scale is None else scale,
+                               softcap, _arr(slopes, _F32, heads, "slopes"), out.data_ptr(),
+                               _arr(lse, _F32, rows * heads, "lse"), ws.data_ptr(), ws.numel(), _stream(stream))
     if rc:
-        _check(rc, "paged_tree_attention")
+        _check(rc, name)
 
 
 def tb_logits_workspace_size(batch: int, n_rows: int, vocab: int) -> int:
@@ -840,18 +974,28 @@ def paged_accept(bank: Bank, req: Requests, pages, results, draft=None, argmax=N
                  stream=None):
     """results int32 [B][68] (make_results); draft, argmax int32 [rows], or draft None to move by the results given;
     lens_out: None for lens itself; pages None: nothing to move."""
+    _accept("paged_accept", Pages, bank, req, pages, results, draft, argmax, vocab, lens_out, stream)
+
+
+def paged_accept_q4(bank: Bank, req: Requests, pages, results, draft=None, argmax=None, vocab: int = 0, lens_out=None,
+                    stream=None):
+    """paged_accept over 4-bit pages (PagesQ4, or None: nothing to move)."""
+    _accept("paged_accept_q4", PagesQ4, bank, req, pages, results, draft, argmax, vocab, lens_out, stream)
+
+
+def _accept(name: str, kind, bank, req, pages, results, draft, argmax, vocab, lens_out, stream):
     r = req._c
-    c = None if pages is None else pages._c
+    c = None if pages is None else _page_kind(pages, kind)
     rows = 0x7FFFFFFF if draft is None else min(draft.shape[0], argmax.shape[0])
     block = _arr(results, _I32, r.batch * RESULT_INTS, "results")
     tokens, greedy = _arr(draft, _I32, 0, "draft"), _arr(argmax, _I32, 0, "argmax")
     if rows == 0:
         tokens = greedy = block  # a step without rows: no address, and none is read, but not "results given" either
-    rc = load().paged_accept(bank.handle, ctypes.byref(r), _ref(c), tokens, greedy, rows, vocab, block,
-                             r.lens if lens_out is None else _arr(lens_out, _I32, r.batch, "lens_out"),
-                             _stream(stream))
+    rc = getattr(load(), name)(bank.handle, ctypes.byref(r), _ref(c), tokens, greedy, rows, vocab, block,
+                               r.lens if lens_out is None else _arr(lens_out, _I32, r.batch, "lens_out"),
+                               _stream(stream))
     if rc:
-        _check(rc, "paged_accept")
+        _check(rc, name)
 
 
 # --------------------------------------------------------------------- per-step tree selection

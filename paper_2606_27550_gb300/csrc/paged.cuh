@@ -5,6 +5,8 @@
 
 #include "kernels.cuh"
 
+#include <cuda_fp16.h>
+
 namespace tv {
 
 constexpr int kTileKeys = 128;  // keys per tile of the paged attention
@@ -82,11 +84,36 @@ float *attention_parts(void *ws);
 int device_sms(int device);  // -1: the current one
 bool ptr_aligned(const void *p, size_t a);
 
+// What the stores share (paged_store.cu).
+constexpr int kMaxAxes = 4;
+
+struct Rows {
+    uint16_t *p;
+    long long row_stride, head_stride;
+};
+inline Rows rows_of(const tb_rows *r)
+{
+    return Rows{static_cast<uint16_t *>(r->ptr), r->row_stride, r->head_stride};
+}
+
+struct RopeAxes {
+    const int32_t *pos;
+    long long axis_stride;
+    int axis_end[kMaxAxes];       // first pair past the axis
+    uint64_t freq[kRopeMaxHalf];  // turns per position, times 2^64
+};
+tb_status check_rows(const tb_rows *r, const char *what, const char *fn);
+tb_status check_store(int layer, int n_layers, const int64_t *slots, int n_rows, const tb_rows *k, const tb_rows *v,
+                      const tb_rows *q, const tb_rows *q_out, int n_q_heads, const char *fn);
+tb_status rope_axes(const tb_rope *rope, int d, int n_rows, RopeAxes *a, const char *fn);
+tb_status check_pages_q4(const tb_pages_q4 *pages, const char *fn);
+
 // K or V of one layer's pages: (d, slots of a page, kv heads, pages), box (64, box_slots, 1, 1)
 bool make_tmap_pages(CUtensorMap *map, const tb_pages *pages, const void *base, int box_slots, const char **err);
 
 unsigned int bounds_violations_paged_plan();
 unsigned int bounds_violations_paged_store();
+unsigned int bounds_violations_paged_rows();
 unsigned int bounds_violations_paged_attention();
 unsigned int bounds_violations_logits();
 unsigned int bounds_violations_paged_accept();
@@ -110,6 +137,38 @@ __device__ __forceinline__ uint64_t load_now(const uint64_t *p)
     uint64_t v;
     asm volatile("ld.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
     return v;
+}
+
+// The angle of pair i of a row, in 2^-64 of a turn (whole turns overflow).
+__device__ __forceinline__ uint64_t turn_of(const RopeAxes &rope, int row, int i)
+{
+    int axis = 0;
+#pragma unroll
+    for (int a = 0; a < kMaxAxes - 1; ++a)
+        axis += i >= rope.axis_end[a];
+    const long long pos = rope.pos[axis * rope.axis_stride + row];
+    return (uint64_t)pos * rope.freq[i];
+}
+
+// Two 16-bit elements of a word.
+template <bool kF16>
+__device__ __forceinline__ float2 unpack_pair(uint32_t w)
+{
+    if constexpr (kF16) {
+        return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    } else {
+        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
+}
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack_pair(float lo, float hi)
+{
+    if constexpr (kF16) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    } else {
+        return pack_bf16x2(lo, hi);
+    }
 }
 
 // Two 32-bit floats in one instruction (softmax loops are bound by their issue slots).

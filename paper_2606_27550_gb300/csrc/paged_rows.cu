@@ -1,0 +1,560 @@
+// paged_rows.cu -- the store with norms of the heads before the rotation, into
+// pages of 16 bits or of 4, and the way back from 4 bits to rows of 16.
+//
+// What follows the rotation may be a rounding to 4 bits, where the last bit of a
+// 32-bit number decides between two values a seventh of the largest apart.  So
+// the steps before it are those of the documented formulas, each rounded once,
+// and what goes into them is right to the last bit but for rare near-ties: sines,
+// cosines and the norm's reciprocal root are computed with a second float that
+// holds what the first leaves (a sum's or product's rounding error is a float
+// itself: Dekker 1971, Knuth's two-sum).  Another program that follows the formulas
+// gets the same codes.
+//
+// A CTA takes a few rows: their (cos, sin) once into shared memory (they serve
+// all heads), then every (row, head, 16-byte piece of the lower half of the head
+// and its partner in the upper half).  A head's pieces lie in 4 or 8 neighbouring
+// lanes, which add up its squares; four of them hold a scale's 32 elements.
+#include "paged_q4.cuh"
+
+#include <cmath>
+
+namespace tv {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxRows = 8;  // rows per CTA
+
+struct RowsArgs {
+    uint8_t *k_pages, *v_pages;  // of the layer
+    long long page_stride, head_stride, slot_stride;  // bytes; 4-bit pages have no slot stride
+    int n_pages, page_log2, Hkv, Hq, n_rows, rows_per_cta;
+    const int64_t *slots;
+    Rows k, v, q, q_out;
+    const uint16_t *q_weight, *k_weight;  // NULL: not normed
+    float eps, weight_offset;
+    int turn;
+    RopeAxes rope;
+};
+
+// A number as the sum of two floats, the second below half a unit in the last place of the first.
+struct Two {
+    float hi, lo;
+};
+__device__ __forceinline__ Two sum_of(float a, float b)
+{
+    const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+    return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+}
+__device__ __forceinline__ Two near_sum(float a, float b)  // |a| >= |b|
+{
+    const float s = __fadd_rn(a, b);
+    return {s, __fsub_rn(b, __fsub_rn(s, a))};
+}
+__device__ __forceinline__ Two product(Two a, Two b)
+{
+    const float p = __fmul_rn(a.hi, b.hi);
+    float e = __fmaf_rn(a.hi, b.hi, -p);
+    e = __fmaf_rn(a.hi, b.lo, e);
+    e = __fmaf_rn(a.lo, b.hi, e);
+    return {p, e};
+}
+__device__ __forceinline__ Two plus(Two c, Two x)  // |c| >= |x|
+{
+    const Two s = near_sum(c.hi, x.hi);
+    return {s.hi, __fadd_rn(s.lo, __fadd_rn(c.lo, x.lo))};
+}
+
+// Cosine and sine of an angle in 2^-64 of a turn: the nearest quarter turn, and the Taylor series of
+// the rest, at most pi / 4, its first terms in two floats.  Off by 2^-40 before the one rounding.
+__device__ float2 cos_sin(uint64_t turn)
+{
+    const int quarter = (int)((turn + (1ull << 61)) >> 62);
+    const int64_t r = (int64_t)(turn - ((uint64_t)quarter << 62));  // in [-2^61, 2^61)
+    const int r_hi = (int)(r >> 32);
+    const float h = __int2float_rn(r_hi);
+    const float l = __fadd_rn(__int2float_rn(r_hi - __float2int_rn(h)), __fmul_rn(__uint2float_rn((uint32_t)r), 0x1p-32f));
+    // times 2 pi / 2^32
+    Two y = product(near_sum(h, l), Two{6.28318548202514648f * 0x1p-32f, -1.74845553146951715e-07f * 0x1p-32f});
+    y = near_sum(y.hi, y.lo);
+    const Two z = product(y, y);
+    // sin y = y + y z S(z), cos y = 1 + z C(z)
+    float f = __fmaf_rn(z.hi, __fmaf_rn(z.hi, -1.f / 39916800.f, 1.f / 362880.f), -1.f / 5040.f);
+    Two s = plus(Two{8.33333376795053482e-03f, -4.34617203337595e-10f}, Two{__fmul_rn(z.hi, f), 0.f});  // 1 / 120
+    s = plus(Two{-1.66666671633720398e-01f, 4.96705373128283e-09f}, product(z, s));                     // -1 / 6
+    s = product(y, product(z, s));
+    Two e = near_sum(y.hi, s.hi);
+    const float sine = __fadd_rn(e.hi, __fadd_rn(e.lo, __fadd_rn(y.lo, s.lo)));
+    f = __fmaf_rn(z.hi, __fmaf_rn(z.hi, __fmaf_rn(z.hi, 1.f / 479001600.f, -1.f / 3628800.f), 1.f / 40320.f), -1.f / 720.f);
+    Two c = plus(Two{4.16666679084300995e-02f, -1.24176343282071e-09f}, Two{__fmul_rn(z.hi, f), 0.f});  // 1 / 24
+    c = plus(Two{-0.5f, 0.f}, product(z, c));
+    c = product(z, c);
+    e = near_sum(1.f, c.hi);
+    const float cosine = __fadd_rn(e.hi, __fadd_rn(e.lo, c.lo));
+    switch (quarter & 3) {
+    case 0:
+        return make_float2(cosine, sine);
+    case 1:
+        return make_float2(-sine, cosine);
+    case 2:
+        return make_float2(-cosine, -sine);
+    default:
+        return make_float2(sine, -cosine);
+    }
+}
+
+// 1 / sqrt(mean of squares + eps) of the head whose 16 elements each are held by kLanes neighbouring
+// lanes.  By the whole warp; what it returns where `normed` is false is not read.
+template <int kLanes>
+__device__ __forceinline__ float inverse_norm(const float (&lo)[8], const float (&hi)[8], float eps, bool normed)
+{
+    Two s{0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float x = i < 8 ? lo[i & 7] : hi[i & 7];  // 11 bits at most: the square is exact
+        const Two t = sum_of(s.hi, __fmul_rn(x, x));
+        s = {t.hi, __fadd_rn(s.lo, t.lo)};
+    }
+#pragma unroll
+    for (int m = 1; m < kLanes; m *= 2) {
+        const float h = __shfl_xor_sync(0xffffffffu, s.hi, m), l = __shfl_xor_sync(0xffffffffu, s.lo, m);
+        const Two t = sum_of(s.hi, h);
+        s = {t.hi, __fadd_rn(__fadd_rn(s.lo, l), t.lo)};
+    }
+    constexpr float kMean = 1.f / (16 * kLanes);
+    const bool fits = !normed || (s.hi > 0x1p-60f && s.hi < 0x1p120f);
+    if (__any_sync(0xffffffffu, !fits)) {
+        // squares that leave the range of 32 bits (all zeros among them): in 64
+        double t = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            t += (double)lo[i] * lo[i] + (double)hi[i] * hi[i];
+#pragma unroll
+        for (int m = 1; m < kLanes; m *= 2)
+            t += __shfl_xor_sync(0xffffffffu, t, m);
+        if (!fits)
+            return (float)(1.0 / sqrt(t * kMean + eps));
+    }
+    Two v = sum_of(s.hi * kMean, eps);
+    v = near_sum(v.hi, __fadd_rn(v.lo, s.lo * kMean));
+    // one Newton step from the 32-bit root, its residual 1 - v y^2 with y^2 in two floats
+    const float y = rsqrtf(v.hi);
+    const float a = __fmul_rn(y, y), b = __fmaf_rn(y, y, -a);
+    float t = __fmaf_rn(-v.hi, a, 1.f);
+    t = __fmaf_rn(-v.hi, b, t);
+    t = __fmaf_rn(-v.lo, a, t);
+    return __fmaf_rn(0.5f * y, t, y);
+}
+
+template <bool kF16>
+__device__ __forceinline__ void widen(const uint4 &w, float (&x)[8])
+{
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack_pair<kF16>(u[i]);
+        x[2 * i] = f.x, x[2 * i + 1] = f.y;
+    }
+}
+template <bool kF16>
+__device__ __forceinline__ uint4 narrow(const float (&x)[8])
+{
+    return make_uint4(pack_pair<kF16>(x[0], x[1]), pack_pair<kF16>(x[2], x[3]), pack_pair<kF16>(x[4], x[5]),
+                      pack_pair<kF16>(x[6], x[7]));
+}
+
+// Bound by HBM: each element is read once and written once.
+template <int kD, bool kF16, bool kQ4>
+__global__ void __launch_bounds__(kThreads) k_paged_rows(const __grid_constant__ RowsArgs p)
+{
+    constexpr int kHalf = kD / 2, kLanes = kHalf / 8;  // lanes of a head
+    __shared__ float2 s_cs[kMaxRows][kHalf];
+    __shared__ float s_weight[2][kD];
+    __shared__ long long s_slot[kMaxRows];
+    pdl_wait();
+    pdl_trigger();
+    const int r0 = blockIdx.x * p.rows_per_cta, n_rows = min(p.rows_per_cta, p.n_rows - r0);
+    const bool norms = p.q_weight || p.k_weight;
+    for (int x = threadIdx.x; x < n_rows; x += kThreads)
+        s_slot[x] = p.slots[r0 + x];
+    if (norms && threadIdx.x < kD) {
+        const int x = threadIdx.x;
+        const uint16_t *w[2] = {p.q_weight, p.k_weight};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (w[i])
+                s_weight[i][x] = p.weight_offset + unpack_pair<kF16>(w[i][x]).x;
+    }
+    if (p.turn)
+        for (int x = threadIdx.x; x < n_rows * kHalf; x += kThreads)
+            s_cs[x / kHalf][x % kHalf] = cos_sin(turn_of(p.rope, r0 + x / kHalf, x % kHalf));
+    __syncthreads();
+    const unsigned per_row = (unsigned)(p.Hq + 2 * p.Hkv) * kLanes, items = n_rows * per_row;
+    constexpr int kAhead = 2;  // items per thread in flight
+    // whole warps go through the loop: a head's lanes add up together
+    for (unsigned x0 = threadIdx.x; (x0 & ~31u) < items; x0 += kAhead * kThreads) {
+        uint4 in[kAhead][2];
+        uint8_t *dst[kAhead];
+        int row[kAhead], kind[kAhead];  // 0: a query, 1: a key, 2: a value, 3: nothing
+#pragma unroll
+        for (int m = 0; m < kAhead; ++m) {
+            const unsigned x = x0 + m * kThreads;
+            const unsigned r = x / per_row, y = x - r * per_row;
+            int h = (int)(y / kLanes);
+            const int c = (int)(y % kLanes) * 8;
+            in[m][0] = in[m][1] = make_uint4(0, 0, 0, 0);
+            dst[m] = nullptr;
+            kind[m] = 3;
+            row[m] = (int)r;
+            if (x >= items)
+                continue;
+            const long long at = r0 + r;
+            const uint16_t *src;
+            if (h < p.Hq) {
+                src = p.q.p + at * p.q.row_stride + h * p.q.head_stride;
+                dst[m] = reinterpret_cast<uint8_t *>(p.q_out.p + at * p.q_out.row_stride + h * p.q_out.head_stride + c);
+                kind[m] = 0;
+            } else {
+                h -= p.Hq;
+                const bool is_v = h >= p.Hkv;
+                h -= is_v ? p.Hkv : 0;
+                const long long slot = s_slot[r], page = slot >> p.page_log2;
+                if (slot < 0 || page >= p.n_pages)
+                    continue;  // padding
+                const int in_page = (int)(slot & ((1 << p.page_log2) - 1));
+                const Rows &rows = is_v ? p.v : p.k;
+                src = rows.p + at * rows.row_stride + h * rows.head_stride;
+                dst[m] = (is_v ? p.v_pages : p.k_pages) + page * p.page_stride + h * p.head_stride;
+                dst[m] += kQ4 ? in_page * code_bytes(kD) + c / 2 : in_page * p.slot_stride + 2 * c;
+                kind[m] = is_v ? 2 : 1;
+            }
+            in[m][0] = *reinterpret_cast<const uint4 *>(src + c);
+            in[m][1] = *reinterpret_cast<const uint4 *>(src + c + kHalf);
+        }
+#pragma unroll
+        for (int m = 0; m < kAhead; ++m) {
+            const unsigned x = x0 + m * kThreads;
+            if ((x & ~31u) >= items)
+                break;
+            const int c = (int)(x % kLanes) * 8;
+            const bool turns = kind[m] < 2;
+            float lo[8], hi[8];
+            widen<kF16>(in[m][0], lo);
+            widen<kF16>(in[m][1], hi);
+            const bool normed = kind[m] == 0 ? p.q_weight != nullptr : kind[m] == 1 && p.k_weight != nullptr;
+            if (__any_sync(0xffffffffu, normed)) {
+                const float r = inverse_norm<kLanes>(lo, hi, p.eps, normed);
+                if (normed) {
+                    const float *w = s_weight[kind[m]];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        lo[i] = __fmul_rn(__fmul_rn(lo[i], r), w[c + i]);
+                        hi[i] = __fmul_rn(__fmul_rn(hi[i], r), w[c + kHalf + i]);
+                    }
+                }
+            }
+            if (p.turn && turns) {
+                const float2 *cs = &s_cs[row[m]][c];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float2 t = cs[i];
+                    const float a = lo[i], b = hi[i];
+                    lo[i] = __fsub_rn(__fmul_rn(a, t.x), __fmul_rn(b, t.y));
+                    hi[i] = __fadd_rn(__fmul_rn(b, t.x), __fmul_rn(a, t.y));
+                }
+            }
+            if (!kQ4 || kind[m] == 0) {
+                if (dst[m]) {
+                    *reinterpret_cast<uint4 *>(dst[m]) = narrow<kF16>(lo);
+                    *reinterpret_cast<uint4 *>(dst[m] + 2 * kHalf) = narrow<kF16>(hi);
+                }
+            }
+            if (kQ4 && __any_sync(0xffffffffu, kind[m] == 1 || kind[m] == 2)) {
+                uint32_t top[2] = {0, 0};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    top[0] = max(top[0], __float_as_uint(lo[i]) & 0x7fffffffu);
+                    top[1] = max(top[1], __float_as_uint(hi[i]) & 0x7fffffffu);
+                }
+                uint32_t sb[2], word[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+                    top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+                    sb[i] = scale_byte(top[i]);
+                    const float s = scale_of(sb[i]);
+                    word[i] = quantize8(i == 0 ? lo : hi, s, s == 0.f ? 0.f : __frcp_rn(s));
+                }
+                // the head's scales from its lanes 0 and 4 (kD = 64: lane 0)
+                uint32_t scales = sb[0] | sb[1] << (8 * kD / (2 * kGroup));
+                if constexpr (kLanes == 8) {
+                    const uint32_t more = __shfl_xor_sync(0xffffffffu, scales, 4);
+                    scales |= more << 8;
+                }
+                if (kind[m] == 1 || kind[m] == 2) {
+                    *reinterpret_cast<uint32_t *>(dst[m]) = word[0];
+                    *reinterpret_cast<uint32_t *>(dst[m] + kHalf / 2) = word[1];
+                    if (c == 0) {
+                        const int in_page = (int)(s_slot[row[m]] & ((1 << p.page_log2) - 1));
+                        uint8_t *to = dst[m] + ((long long)code_bytes(kD) << p.page_log2) +
+                                      in_page * (scale_bytes(kD) - code_bytes(kD));
+                        if constexpr (kD == 128)
+                            *reinterpret_cast<uint32_t *>(to) = scales;
+                        else
+                            *reinterpret_cast<uint16_t *>(to) = (uint16_t)scales;
+                    }
+                }
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ back to 16 bits
+
+struct LoadArgs {
+    const uint8_t *k_pages, *v_pages;  // of the first layer
+    long long layer_stride, page_stride, head_stride;
+    int n_pages, page_log2, Hkv, n_rows, n_layers;
+    const int64_t *slots;
+    Rows k, v;
+    long long row_layer_stride;
+};
+
+// A lane takes 8 codes of a (row, layer, K or V, head), neighbouring lanes its neighbours.  Bound by HBM:
+// 0.53 bytes read and 2 written per element.
+template <int kD, bool kF16>
+__global__ void __launch_bounds__(kThreads) k_paged_load(const __grid_constant__ LoadArgs p)
+{
+    constexpr int kWords = kD / 8, kAhead = 4;
+    pdl_wait();
+    pdl_trigger();
+    const unsigned per_row = (unsigned)(2 * p.Hkv) * kWords;
+    const int layer = blockIdx.y;
+    const unsigned items = p.n_rows * per_row, stride = gridDim.x * kThreads;  // below 2^31 (the host's check)
+    for (unsigned x0 = blockIdx.x * kThreads + threadIdx.x; x0 < items; x0 += kAhead * stride) {
+        uint32_t code[kAhead], scale[kAhead];
+        uint16_t *dst[kAhead];
+#pragma unroll
+        for (int m = 0; m < kAhead; ++m) {
+            const unsigned x = x0 + m * stride;
+            dst[m] = nullptr;
+            if (x >= items)
+                continue;
+            const unsigned r = x / per_row, y = x - r * per_row;
+            int h = (int)(y / kWords);
+            const int w = (int)(y % kWords);
+            const bool is_v = h >= p.Hkv;
+            h -= is_v ? p.Hkv : 0;
+            const long long slot = p.slots[r], page = slot >> p.page_log2;
+            if (slot < 0 || page >= p.n_pages)
+                continue;  // padding
+            const int in_page = (int)(slot & ((1 << p.page_log2) - 1));
+            const uint8_t *src = (is_v ? p.v_pages : p.k_pages) + layer * p.layer_stride + page * p.page_stride +
+                                 h * p.head_stride;
+            code[m] = *reinterpret_cast<const uint32_t *>(src + in_page * code_bytes(kD) + 4 * w);
+            scale[m] = src[((long long)code_bytes(kD) << p.page_log2) + in_page * scale_bytes(kD) + w / 4];
+            const Rows &to = is_v ? p.v : p.k;
+            dst[m] = to.p + layer * p.row_layer_stride + r * to.row_stride + h * to.head_stride + 8 * w;
+        }
+#pragma unroll
+        for (int m = 0; m < kAhead; ++m) {
+            if (!dst[m])
+                continue;
+            const float f = scale_of(scale[m]);
+            const Scale<kF16> s = scale_pair<kF16>(f, f);
+            uint32_t a[4];  // elements j and j + 4
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                a[j] = dequant_pair<kF16>(code[m] >> (4 * j), s);
+            *reinterpret_cast<uint4 *>(dst[m]) =
+                make_uint4(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410),
+                           __byte_perm(a[0], a[1], 0x7632), __byte_perm(a[2], a[3], 0x7632));
+        }
+    }
+}
+
+tb_status check_norm(const tb_head_norm *norm, const char *fn)
+{
+    if (!norm)
+        return TB_OK;
+    if (!ptr_aligned(norm->q_weight, 16) || !ptr_aligned(norm->k_weight, 16))
+        return record_error(TB_EINVAL, "%s: norm weights must be 16-byte aligned", fn);
+    if (!(norm->eps >= 0.f) || !std::isfinite(norm->eps) || !std::isfinite(norm->weight_offset))
+        return record_error(TB_EINVAL, "%s: norm eps %g, weight_offset %g", fn, norm->eps, norm->weight_offset);
+    return TB_OK;
+}
+
+// What both stores do once their pages are checked and put into `a`.
+tb_status store_rows(RowsArgs &a, bool q4, int layer, int n_layers, int n_kv_heads, int page_size, int d, int dtype,
+                     const int64_t *slots, int n_rows, const tb_rows *k, const tb_rows *v, const tb_rows *q,
+                     const tb_rows *q_out, int n_q_heads, const tb_head_norm *norm, const tb_rope *rope,
+                     cudaStream_t stream, const char *fn)
+{
+    tb_status st = check_store(layer, n_layers, slots, n_rows, k, v, q, q_out, n_q_heads, fn);
+    if (st != TB_OK || (st = check_norm(norm, fn)) != TB_OK)
+        return st;
+    const bool has_q = q && q->ptr;
+    a.turn = rope && rope->theta != 0.f;
+    if (a.turn && (st = rope_axes(rope, d, n_rows, &a.rope, fn)) != TB_OK)
+        return st;
+    if (n_rows == 0)
+        return launch_result(cudaSuccess, fn);
+    const int n_sm = device_sms(-1);
+    if (n_sm <= 0)
+        return record_error(TB_ECUDA, "%s: no current device", fn);
+    while ((1 << a.page_log2) < page_size)
+        ++a.page_log2;
+    a.Hkv = n_kv_heads;
+    a.Hq = has_q ? n_q_heads : 0;
+    a.n_rows = n_rows;
+    a.slots = slots;
+    a.k = rows_of(k);
+    a.v = rows_of(v);
+    if (has_q) {
+        a.q = rows_of(q);
+        a.q_out = rows_of(q_out);
+    }
+    if (norm) {
+        a.q_weight = has_q ? static_cast<const uint16_t *>(norm->q_weight) : nullptr;
+        a.k_weight = static_cast<const uint16_t *>(norm->k_weight);
+        a.eps = norm->eps;
+        a.weight_offset = norm->weight_offset;
+    }
+    // one row per CTA while there are SMs for more, up to kMaxRows of them otherwise
+    const int per = n_rows / (8 * n_sm);
+    a.rows_per_cta = per < 1 ? 1 : per > kMaxRows ? kMaxRows : per;
+    using Kernel = void (*)(RowsArgs);
+    static const Kernel kernels[2][2][2] = {
+        {{k_paged_rows<64, false, false>, k_paged_rows<64, false, true>},
+         {k_paged_rows<64, true, false>, k_paged_rows<64, true, true>}},
+        {{k_paged_rows<128, false, false>, k_paged_rows<128, false, true>},
+         {k_paged_rows<128, true, false>, k_paged_rows<128, true, true>}}};
+    const int grid = (n_rows + a.rows_per_cta - 1) / a.rows_per_cta;
+    return launch_result(launch_kernel(kernels[d == 128][dtype == TB_F16][q4], dim3(grid), dim3(kThreads), 0, stream,
+                                       true, a),
+                         fn);
+}
+
+}  // namespace
+
+TB_BOUNDS_COUNTER(bounds_violations_paged_rows)
+
+tb_status check_pages_q4(const tb_pages_q4 *pages, const char *fn)
+{
+    if (!pages || !pages->k || !pages->v)
+        return record_error(TB_EINVAL, "%s: pages, pages->k or pages->v is NULL", fn);
+    if (!ptr_aligned(pages->k, 16) || !ptr_aligned(pages->v, 16))
+        return record_error(TB_EINVAL, "%s: pages->k / pages->v must be 16-byte aligned", fn);
+    if (pages->dtype != TB_BF16 && pages->dtype != TB_F16)
+        return record_error(TB_EUNSUPPORTED, "%s: rows of type %d (TB_BF16 or TB_F16)", fn, pages->dtype);
+    if (pages->head_dim != 64 && pages->head_dim != 128)
+        return record_error(TB_EUNSUPPORTED, "%s: head_dim %d (64 or 128 supported)", fn, pages->head_dim);
+    if (pages->n_layers < 1 || pages->n_pages < 1 || pages->n_kv_heads < 1)
+        return record_error(TB_EINVAL, "%s: n_layers=%d n_pages=%d n_kv_heads=%d", fn, pages->n_layers, pages->n_pages,
+                            pages->n_kv_heads);
+    if (pages->page_size < 8 || pages->page_size > 1024 || (pages->page_size & (pages->page_size - 1)))
+        return record_error(TB_EINVAL, "%s: page_size %d (a power of two from 8 to 1024)", fn, pages->page_size);
+    const int64_t block = (int64_t)pages->page_size * row_bytes(pages->head_dim);
+    for (int64_t s : {pages->layer_stride, pages->page_stride, pages->head_stride})
+        if (s < 0 || s % 16)
+            return record_error(TB_EINVAL, "%s: strides must be multiples of 16 bytes, none negative", fn);
+    if ((pages->n_kv_heads > 1 && pages->head_stride < block) || (pages->n_pages > 1 && pages->page_stride < block) ||
+        (pages->n_layers > 1 && pages->layer_stride < block))
+        return record_error(TB_EINVAL, "%s: layer, page or head stride below a page's %lld bytes", fn, (long long)block);
+    return TB_OK;
+}
+
+}  // namespace tv
+
+using namespace tv;
+
+extern "C" tb_status paged_kv_store_norm(const tb_pages *pages, int layer, const int64_t *slots, int n_rows,
+                                         const tb_rows *k, const tb_rows *v, const tb_rows *q, const tb_rows *q_out,
+                                         int n_q_heads, const tb_head_norm *norm, const tb_rope *rope, tb_stream stream)
+{
+    const char *fn = "paged_kv_store_norm";
+    const tb_status st = check_pages(pages, fn);
+    if (st != TB_OK)
+        return st;
+    RowsArgs a{};
+    const long long off = 2ll * layer * pages->layer_stride;
+    a.k_pages = static_cast<uint8_t *>(pages->k) + off;
+    a.v_pages = static_cast<uint8_t *>(pages->v) + off;
+    a.page_stride = 2 * pages->page_stride;
+    a.head_stride = 2 * pages->head_stride;
+    a.slot_stride = 2 * pages->slot_stride;
+    a.n_pages = pages->n_pages;
+    return store_rows(a, false, layer, pages->n_layers, pages->n_kv_heads, pages->page_size, pages->head_dim,
+                      pages->dtype, slots, n_rows, k, v, q, q_out, n_q_heads, norm, rope, (cudaStream_t)stream, fn);
+}
+
+extern "C" tb_status paged_kv_store_q4(const tb_pages_q4 *pages, int layer, const int64_t *slots, int n_rows,
+                                       const tb_rows *k, const tb_rows *v, const tb_rows *q, const tb_rows *q_out,
+                                       int n_q_heads, const tb_head_norm *norm, const tb_rope *rope, tb_stream stream)
+{
+    const char *fn = "paged_kv_store_q4";
+    const tb_status st = check_pages_q4(pages, fn);
+    if (st != TB_OK)
+        return st;
+    RowsArgs a{};
+    const long long off = (long long)layer * pages->layer_stride;
+    a.k_pages = static_cast<uint8_t *>(pages->k) + off;
+    a.v_pages = static_cast<uint8_t *>(pages->v) + off;
+    a.page_stride = pages->page_stride;
+    a.head_stride = pages->head_stride;
+    a.n_pages = pages->n_pages;
+    return store_rows(a, true, layer, pages->n_layers, pages->n_kv_heads, pages->page_size, pages->head_dim,
+                      pages->dtype, slots, n_rows, k, v, q, q_out, n_q_heads, norm, rope, (cudaStream_t)stream, fn);
+}
+
+extern "C" tb_status paged_kv_load_q4(const tb_pages_q4 *pages, int layer, int n_layers, const int64_t *slots,
+                                      int n_rows, const tb_rows *k, const tb_rows *v, int64_t row_layer_stride,
+                                      tb_stream stream)
+{
+    const char *fn = "paged_kv_load_q4";
+    tb_status st = check_pages_q4(pages, fn);
+    if (st != TB_OK)
+        return st;
+    if (layer < 0 || n_layers < 1 || n_layers > pages->n_layers - layer)
+        return record_error(TB_EINVAL, "%s: layers %d to %d of %d", fn, layer, layer + n_layers, pages->n_layers);
+    if (n_layers > 65535)
+        return record_error(TB_EUNSUPPORTED, "%s: %d layers", fn, n_layers);
+    if (n_rows < 0 || (n_rows > 0 && !slots))
+        return record_error(TB_EINVAL, "%s: n_rows %d, or slots is NULL", fn, n_rows);
+    if (n_rows > 0 && ((st = check_rows(k, "k", fn)) != TB_OK || (st = check_rows(v, "v", fn)) != TB_OK))
+        return st;
+    if ((long long)n_rows * 2 * pages->n_kv_heads * (pages->head_dim / 8) >= 1ll << 31)
+        return record_error(TB_EUNSUPPORTED, "%s: %d rows of %d heads in one call", fn, n_rows, pages->n_kv_heads);
+    if (row_layer_stride % 8)
+        return record_error(TB_EINVAL, "%s: row_layer_stride must be a multiple of 8 elements", fn);
+    if (n_rows == 0)
+        return launch_result(cudaSuccess, fn);
+    const int n_sm = device_sms(-1);
+    if (n_sm <= 0)
+        return record_error(TB_ECUDA, "%s: no current device", fn);
+    LoadArgs a{};
+    const long long off = (long long)layer * pages->layer_stride;
+    a.k_pages = static_cast<const uint8_t *>(pages->k) + off;
+    a.v_pages = static_cast<const uint8_t *>(pages->v) + off;
+    a.layer_stride = pages->layer_stride;
+    a.page_stride = pages->page_stride;
+    a.head_stride = pages->head_stride;
+    a.n_pages = pages->n_pages;
+    while ((1 << a.page_log2) < pages->page_size)
+        ++a.page_log2;
+    a.Hkv = pages->n_kv_heads;
+    a.n_rows = n_rows;
+    a.n_layers = n_layers;
+    a.slots = slots;
+    a.k = rows_of(k);
+    a.v = rows_of(v);
+    a.row_layer_stride = row_layer_stride;
+    // a thread has 4 items in flight; CTAs for all of a layer's, as many as the SMs hold a few times over
+    const long long ctas = ((long long)n_rows * 2 * a.Hkv * (pages->head_dim / 8) + 4 * kThreads - 1) / (4 * kThreads);
+    const long long most = (64ll * n_sm + n_layers - 1) / n_layers;
+    const dim3 grid((unsigned)(ctas < most ? ctas : most), n_layers);
+    const bool f16 = pages->dtype == TB_F16;
+    const auto kernel = pages->head_dim == 64 ? (f16 ? k_paged_load<64, true> : k_paged_load<64, false>)
+                                              : (f16 ? k_paged_load<128, true> : k_paged_load<128, false>);
+    return launch_result(launch_kernel(kernel, grid, dim3(kThreads), 0, (cudaStream_t)stream, true, a), fn);
+}

@@ -25,12 +25,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxRows = 8;  // rows per CTA
-constexpr int kMaxAxes = 4;
-
-struct Rows {
-    uint16_t *p;
-    long long row_stride, head_stride;
-};
 
 struct StoreArgs {
     uint16_t *k_pages, *v_pages;  // of the layer
@@ -38,32 +32,8 @@ struct StoreArgs {
     int n_pages, page_log2, Hkv, Hq, n_rows, d_log2, rows_per_cta;
     const int64_t *slots;
     Rows k, v, q, q_out;
-    const int32_t *pos;
-    long long axis_stride;
-    int axis_end[kMaxAxes];  // first pair past the axis
-    uint64_t freq[kRopeMaxHalf];  // turns per position, times 2^64
+    RopeAxes rope;
 };
-
-template <bool kF16>
-__device__ __forceinline__ float2 unpack(uint32_t w)
-{
-    if constexpr (kF16) {
-        return __half22float2(*reinterpret_cast<const __half2 *>(&w));
-    } else {
-        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-    }
-}
-
-template <bool kF16>
-__device__ __forceinline__ uint32_t pack(float lo, float hi)
-{
-    if constexpr (kF16) {
-        const __half2 h = __floats2half2_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t *>(&h);
-    } else {
-        return pack_bf16x2(lo, hi);
-    }
-}
 
 // kRope: queries and keys turn.  Bound by HBM: each element is read once and
 // written once.  8191 rows of a prompt, 32 heads of 128 (403 MB): 65.7 us, 6.13 TB/s,
@@ -83,13 +53,8 @@ __global__ void __launch_bounds__(kThreads) k_paged_store(const __grid_constant_
     if constexpr (kRope) {
         for (int x = threadIdx.x; x < n_rows << half_log2; x += kThreads) {
             const int r = x >> half_log2, i = x & (half - 1);
-            int axis = 0;
-#pragma unroll
-            for (int a = 0; a < kMaxAxes - 1; ++a)
-                axis += i >= p.axis_end[a];
-            const long long pos = p.pos[axis * p.axis_stride + r0 + r];
             // the fraction of a turn in [-1/2, 1/2), as an angle in units of pi
-            const int turn = (int)(((uint64_t)pos * p.freq[i]) >> 32);
+            const int turn = (int)(turn_of(p.rope, r0 + r, i) >> 32);
             float2 cs;
             sincospif((float)turn * 0x1p-31f, &cs.y, &cs.x);
             s_cs[r][i] = cs;
@@ -147,29 +112,15 @@ __global__ void __launch_bounds__(kThreads) k_paged_store(const __grid_constant_
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float2 t0 = cs[2 * e], t1 = cs[2 * e + 1];
-                    const float2 u = unpack<kF16>(a[e]), w = unpack<kF16>(b[e]);
-                    a[e] = pack<kF16>(u.x * t0.x - w.x * t0.y, u.y * t1.x - w.y * t1.y);
-                    b[e] = pack<kF16>(w.x * t0.x + u.x * t0.y, w.y * t1.x + u.y * t1.y);
+                    const float2 u = unpack_pair<kF16>(a[e]), w = unpack_pair<kF16>(b[e]);
+                    a[e] = pack_pair<kF16>(u.x * t0.x - w.x * t0.y, u.y * t1.x - w.y * t1.y);
+                    b[e] = pack_pair<kF16>(w.x * t0.x + u.x * t0.y, w.y * t1.x + u.y * t1.y);
                 }
             }
             *reinterpret_cast<uint4 *>(dst[m]) = lo[m];
             *reinterpret_cast<uint4 *>(dst[m] + half) = hi[m];
         }
     }
-}
-
-tb_status check_rows(const tb_rows *r, const char *what, const char *fn)
-{
-    if (!r || !r->ptr || !ptr_aligned(r->ptr, 16))
-        return record_error(TB_EINVAL, "%s: %s NULL or not 16-byte aligned", fn, what);
-    if (r->row_stride % 8 || r->head_stride % 8)
-        return record_error(TB_EINVAL, "%s: strides of %s must be multiples of 8 elements", fn, what);
-    return TB_OK;
-}
-
-Rows rows_of(const tb_rows *r)
-{
-    return Rows{static_cast<uint16_t *>(r->ptr), r->row_stride, r->head_stride};
 }
 
 using u128 = unsigned __int128;
@@ -213,6 +164,56 @@ void turns(double theta, int d, uint64_t *freq)
 
 }  // namespace
 
+tb_status check_rows(const tb_rows *r, const char *what, const char *fn)
+{
+    if (!r || !r->ptr || !ptr_aligned(r->ptr, 16))
+        return record_error(TB_EINVAL, "%s: %s NULL or not 16-byte aligned", fn, what);
+    if (r->row_stride % 8 || r->head_stride % 8)
+        return record_error(TB_EINVAL, "%s: strides of %s must be multiples of 8 elements", fn, what);
+    return TB_OK;
+}
+
+tb_status check_store(int layer, int n_layers, const int64_t *slots, int n_rows, const tb_rows *k, const tb_rows *v,
+                      const tb_rows *q, const tb_rows *q_out, int n_q_heads, const char *fn)
+{
+    if (layer < 0 || layer >= n_layers)
+        return record_error(TB_EINVAL, "%s: layer %d of %d", fn, layer, n_layers);
+    if (n_rows < 0 || (n_rows > 0 && !slots))
+        return record_error(TB_EINVAL, "%s: n_rows %d, or slots is NULL", fn, n_rows);
+    const bool has_q = q && q->ptr;
+    tb_status st;
+    if (n_rows > 0 && ((st = check_rows(k, "k", fn)) != TB_OK || (st = check_rows(v, "v", fn)) != TB_OK))
+        return st;
+    if (n_rows > 0 && has_q && ((st = check_rows(q, "q", fn)) != TB_OK || (st = check_rows(q_out, "q_out", fn)) != TB_OK))
+        return st;
+    if (has_q && (n_q_heads < 1 || n_q_heads > 65536))
+        return record_error(TB_EINVAL, "%s: n_q_heads %d", fn, n_q_heads);
+    return TB_OK;
+}
+
+tb_status rope_axes(const tb_rope *rope, int d, int n_rows, RopeAxes *a, const char *fn)
+{
+    if (!(rope->theta >= 1.f) || !std::isfinite(rope->theta))
+        return record_error(TB_EINVAL, "%s: rope theta %g (1 or more)", fn, rope->theta);
+    if (rope->n_axes < 1 || rope->n_axes > kMaxAxes || (n_rows > 0 && !rope->positions) || rope->axis_stride < 0 ||
+        (rope->n_axes > 1 && rope->axis_stride < n_rows))
+        return record_error(TB_EINVAL, "%s: %d axes, positions NULL or axis_stride %lld below n_rows", fn, rope->n_axes,
+                            (long long)rope->axis_stride);
+    int end = 0;
+    for (int x = 0; x < kMaxAxes; ++x) {
+        if (x < rope->n_axes && (rope->sections[x] < 0 || rope->sections[x] > d / 2))
+            return record_error(TB_EINVAL, "%s: section %d of %d pairs", fn, x, rope->sections[x]);
+        end += x < rope->n_axes ? rope->sections[x] : 0;
+        a->axis_end[x] = x < rope->n_axes - 1 ? end : d;
+    }
+    if (end != d / 2)
+        return record_error(TB_EINVAL, "%s: the sections have %d pairs, a head %d", fn, end, d / 2);
+    turns((double)rope->theta, d, a->freq);
+    a->pos = rope->positions;
+    a->axis_stride = rope->axis_stride;
+    return TB_OK;
+}
+
 TB_BOUNDS_COUNTER(bounds_violations_paged_store)
 
 }  // namespace tv
@@ -227,40 +228,14 @@ extern "C" tb_status paged_kv_store(const tb_pages *pages, int layer, const int6
     tb_status st = check_pages(pages, fn);
     if (st != TB_OK)
         return st;
-    if (layer < 0 || layer >= pages->n_layers)
-        return record_error(TB_EINVAL, "%s: layer %d of %d", fn, layer, pages->n_layers);
-    if (n_rows < 0 || (n_rows > 0 && !slots))
-        return record_error(TB_EINVAL, "%s: n_rows %d, or slots is NULL", fn, n_rows);
+    if ((st = check_store(layer, pages->n_layers, slots, n_rows, k, v, q, q_out, n_q_heads, fn)) != TB_OK)
+        return st;
     const bool has_q = q && q->ptr;
-    if (n_rows > 0 && ((st = check_rows(k, "k", fn)) != TB_OK || (st = check_rows(v, "v", fn)) != TB_OK))
-        return st;
-    if (n_rows > 0 && has_q && ((st = check_rows(q, "q", fn)) != TB_OK || (st = check_rows(q_out, "q_out", fn)) != TB_OK))
-        return st;
-    if (has_q && (n_q_heads < 1 || n_q_heads > 65536))
-        return record_error(TB_EINVAL, "%s: n_q_heads %d", fn, n_q_heads);
     StoreArgs a{};
     const bool turn = rope && rope->theta != 0.f;
     const int d = pages->head_dim;
-    if (turn) {
-        if (!(rope->theta >= 1.f) || !std::isfinite(rope->theta))
-            return record_error(TB_EINVAL, "%s: rope theta %g (1 or more)", fn, rope->theta);
-        if (rope->n_axes < 1 || rope->n_axes > kMaxAxes || (n_rows > 0 && !rope->positions) ||
-            rope->axis_stride < 0 || (rope->n_axes > 1 && rope->axis_stride < n_rows))
-            return record_error(TB_EINVAL, "%s: %d axes, positions NULL or axis_stride %lld below n_rows", fn,
-                                rope->n_axes, (long long)rope->axis_stride);
-        int end = 0;
-        for (int x = 0; x < kMaxAxes; ++x) {
-            if (x < rope->n_axes && (rope->sections[x] < 0 || rope->sections[x] > d / 2))
-                return record_error(TB_EINVAL, "%s: section %d of %d pairs", fn, x, rope->sections[x]);
-            end += x < rope->n_axes ? rope->sections[x] : 0;
-            a.axis_end[x] = x < rope->n_axes - 1 ? end : d;
-        }
-        if (end != d / 2)
-            return record_error(TB_EINVAL, "%s: the sections have %d pairs, a head %d", fn, end, d / 2);
-        turns((double)rope->theta, d, a.freq);
-        a.pos = rope->positions;
-        a.axis_stride = rope->axis_stride;
-    }
+    if (turn && (st = rope_axes(rope, d, n_rows, &a.rope, fn)) != TB_OK)
+        return st;
     if (n_rows == 0)
         return launch_result(cudaSuccess, fn);
     const int n_sm = device_sms(-1);
