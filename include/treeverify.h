@@ -768,7 +768,8 @@ TB_API tb_status paged_accept(const tb_bank *bank, const tb_requests *req, const
  * Norms of queries and keys for each head before the rotation, and the paged
  * cache in 4 bits: calls that stand beside those above and take the same
  * requests, plans, pools and results (paged_plan and logits_process serve
- * both).
+ * both).  A step over a 4-bit cache is paged_plan, per layer paged_kv_store_q4
+ * and paged_tree_attention_q4, then paged_accept_q4.
  * ---------------------------------------------------------------------- */
 
 /* Norms of the heads (a head's row x, weight w [head_dim] of the rows' type):
@@ -831,6 +832,14 @@ TB_API tb_status paged_kv_store_q4(const tb_pages_q4 *pages, int layer, const in
  * than once.  n_rows >= 0, n_layers >= 1; one kernel. */
 TB_API tb_status paged_kv_load_q4(const tb_pages_q4 *pages, int layer, int n_layers, const int64_t *slots, int n_rows,
                                   const tb_rows *k, const tb_rows *v, int64_t row_layer_stride, tb_stream stream);
+
+/* paged_tree_attention over 4-bit pages: the same formulas, arguments, plan,
+ * workspace and status word.  The elements enter the products exactly; a scale
+ * of NaN in a slot that a row sees makes that row NaN. */
+TB_API tb_status paged_tree_attention_q4(const tb_bank *bank, const tb_requests *req, const tb_pages_q4 *pages,
+                                         int layer, const void *plan, size_t plan_bytes, const void *q, int n_rows,
+                                         int n_q_heads, float scale, float softcap, const float *slopes, void *out,
+                                         float *lse, void *workspace, size_t workspace_bytes, tb_stream stream);
 
 /* paged_accept over 4-bit pages: the accepted rows' codes and scales move as they
  * lie; everything else is paged_accept's.  One kernel. */

@@ -39,7 +39,7 @@ API = ("tb_canonicalize", "tb_create", "tb_add_topology", "tb_get_topology", "tb
        "verify_step_scheduled", "spec_sample_accept", "verify_step_sampled", "tb_debug_bounds_violations",
        "tb_debug_bounds_build", "tb_launch_count", "tb_paged_plan_size", "paged_plan", "paged_kv_store",
        "paged_tree_attention", "logits_process", "tb_logits_workspace_size", "paged_accept", "paged_kv_store_norm",
-       "paged_kv_store_q4", "paged_kv_load_q4", "paged_accept_q4")
+       "paged_kv_store_q4", "paged_kv_load_q4", "paged_tree_attention_q4", "paged_accept_q4")
 
 
 class TreeVerifyError(RuntimeError):
@@ -192,6 +192,7 @@ def load(path: str = LIB_PATH):
         "paged_kv_store_norm": [P, i32, P, i32, P, P, P, P, i32, P, P, P],
         "paged_kv_store_q4": [P, i32, P, i32, P, P, P, P, i32, P, P, P],
         "paged_kv_load_q4": [P, i32, i32, P, i32, P, P, i64, P],
+        "paged_tree_attention_q4": [P, P, P, i32, P, sz, P, i32, i32, ctypes.c_float, ctypes.c_float, P, P, P, P, sz, P],
         "paged_accept_q4": [P, P, P, P, P, i32, i32, P, P, P],
     }
     for name, args in sig.items():
@@ -896,6 +897,12 @@ def paged_tree_attention(bank: Bank, req: Requests, pages: Pages, plan, q, out, 
     """q, out [rows][n_q_heads][head_dim] of the pages' type; lse float [rows][n_q_heads]; slopes float [n_q_heads];
     scale: 1 / sqrt(head_dim) unless given."""
     _attend("paged_tree_attention", Pages, bank, req, pages, plan, q, out, ws, layer, scale, softcap, slopes, lse, stream)
+
+
+def paged_tree_attention_q4(bank: Bank, req: Requests, pages: PagesQ4, plan, q, out, ws, layer: int = 0,
+                            scale: float | None = None, softcap: float = 0.0, slopes=None, lse=None, stream=None):
+    """paged_tree_attention over 4-bit pages; q and out have the pages' row type."""
+    _attend("paged_tree_attention_q4", PagesQ4, bank, req, pages, plan, q, out, ws, layer, scale, softcap, slopes, lse, stream)
 
 
 def _attend(name: str, kind, bank, req, pages, plan, q, out, ws, layer, scale, softcap, slopes, lse, stream):

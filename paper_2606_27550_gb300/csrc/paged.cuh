@@ -115,6 +115,7 @@ unsigned int bounds_violations_paged_plan();
 unsigned int bounds_violations_paged_store();
 unsigned int bounds_violations_paged_rows();
 unsigned int bounds_violations_paged_attention();
+unsigned int bounds_violations_paged_attention_q4();
 unsigned int bounds_violations_logits();
 unsigned int bounds_violations_paged_accept();
 

@@ -625,7 +625,7 @@ extern "C" tb_status tb_debug_bounds_violations(uint32_t *count)
     for (unsigned int (*f)() : {bounds_violations_attention_tc, bounds_violations_lm_head, bounds_violations_accept,
                                 bounds_violations_rope, bounds_violations_sample, bounds_violations_paged_plan,
                                 bounds_violations_paged_store, bounds_violations_paged_rows,
-                                bounds_violations_paged_attention,
+                                bounds_violations_paged_attention, bounds_violations_paged_attention_q4,
                                 bounds_violations_logits, bounds_violations_paged_accept}) {
         const unsigned int x = f();
         if (x == 0xffffffffu)
