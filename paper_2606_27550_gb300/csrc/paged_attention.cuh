@@ -58,6 +58,7 @@
 #include "paged_q4.cuh"
 
 #include <cmath>
+#include <type_traits>
 
 namespace tv {
 
@@ -86,10 +87,6 @@ constexpr int kVStages = 2;
 constexpr int packed_bytes(int d)
 {
     return kBN * row_bytes(d);
-}
-constexpr int smem_bytes(int d, bool q4)
-{
-    return (k_stages(q4) + kVStages) * tile_bytes(d) + (q4 ? 2 * kPackedStages * packed_bytes(d) : 0) + 1024;
 }
 // A capped score carries an error of up to cap 2^-20 from the 32-bit tanh: 2^-10 at this cap, where
 // rounding a weight costs 2^-8 (bf16) or 2^-11 (fp16).
@@ -328,6 +325,27 @@ __device__ __forceinline__ void unpack_tile(const uint8_t *packed, uint8_t *tile
     }
 }
 
+}  // namespace
+
+}  // namespace tv
+
+#include "paged_attention_few.cuh"
+
+namespace tv {
+
+namespace {
+
+// What the kernel keeps in dynamic shared memory: the tiles of K and V; for 4-bit pages also the packed
+// tiles and the segments' records, or all that few rows take.
+template <int kD, bool kQ4>
+constexpr int smem_bytes()
+{
+    const int tiles = (k_stages(kQ4) + kVStages) * tile_bytes(kD);
+    const int many = tiles + (kQ4 ? 2 * kPackedStages * packed_bytes(kD) + 2 * (int)sizeof(SegInfo) : 0);
+    const int few = kQ4 ? (int)sizeof(FewSmem<kD>) : 0;
+    return (many > few ? many : few) + 1024;
+}
+
 template <int kD, bool kF16, int kForm, bool kQ4>
 __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_constant__ PagedArgs p)
 {
@@ -345,13 +363,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag, s_ok;
     __shared__ __align__(8) PlanCta s_cta;
-    __shared__ SegInfo s_info[2];
+    struct None {
+    };
+    __shared__ std::conditional_t<kQ4, None, SegInfo[2]> info;
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *sK = smem, *sV = smem + (size_t)kKStages * kTile;
     // 4-bit pages: the packed tiles of K and V, filled by the producers and emptied by warps 8-11
     uint8_t *const packed = sV + (size_t)kVStages * kTile;
     __shared__ __align__(8) uint64_t packed_full[kQ4 ? 2 : 1][kPackedStages], packed_empty[kQ4 ? 2 : 1][kPackedStages];
     __shared__ uint32_t packed_holes[kQ4 ? 2 : 1][kPackedStages];
+    __shared__ int s_rows;  // 4-bit pages: of the CTA's largest unit
+    SegInfo *const s_info = [&] {
+        if constexpr (kQ4)
+            return reinterpret_cast<SegInfo *>(packed + 2 * kPackedStages * kPacked);
+        else
+            return info;
+    }();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) {
@@ -400,15 +427,44 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             if (!s_ok)
                 atomicOr(p.status, kStatusBounds);
         }
+        if constexpr (kQ4) {
+            // the requests of this CTA's range follow one another
+            __syncwarp();
+            const PlanReq *all = plan_reqs(p.plan);
+            int rows = 0;
+            for (int i0 = s_cta.idx; s_cta.t0 < s_cta.t1; i0 += 32) {
+                const int i = i0 + lane;
+                const bool in = i < p.batch && all[i].tile_base < s_cta.t1;
+                const uint32_t run = __ballot_sync(0xffffffffu, in);
+                const int n = run == 0xffffffffu ? 32 : __ffs((int)~run) - 1;
+                rows = max(rows, lane < n ? all[i].n * p.group - s_cta.rb * 128 : 0);
+                if (n < 32)
+                    break;
+            }
+            rows = __reduce_max_sync(0xffffffffu, rows);
+            if (lane == 0)
+                s_rows = rows;
+        }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    const bool few = kQ4 && s_rows <= kFewRows;  // (all threads of the CTA alike)
     const uint32_t tmem = tmem_slot;
     const long long t0 = s_ok ? s_cta.t0 : 0, t1 = s_ok ? s_cta.t1 : 0;
     const PlanReq *reqs = plan_reqs(p.plan);
 
-    if (warp < 4) {
+    if (kQ4 && few) {
+        if constexpr (kQ4) {
+            FewSmem<kD> &sm = *reinterpret_cast<FewSmem<kD> *>(smem);
+            if (s_ok && t0 < t1) {
+                if (s_rows <= 8)
+                    few_rows<kD, kF16, kForm, 1>(p, s_cta, sm, &abort_flag, &never_bar[0]);
+                else
+                    few_rows<kD, kF16, kForm, 2>(p, s_cta, sm, &abort_flag, &never_bar[0]);
+            }
+        }
+    } else if (warp < 4) {
         Cursor cur;  // (a CTA without tiles has an empty one)
         cur.start(s_cta, t1, reqs, p.Hkv);
         if (warp == 0 || warp == 3) {
@@ -1025,7 +1081,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     __syncwarp();
     __syncthreads();
     if (warp == 1) {
-        if (lane == 0)
+        if (lane == 0 && !few)
             mbar_wait_drain(&drain_bar, 0);
         __syncwarp();
         tmem_dealloc(tmem, 512);
@@ -1142,8 +1198,8 @@ cudaError_t launch(const PagedArgs &a, int n_sm, int max_rows, cudaStream_t stre
     cudaError_t e = allow_max_smem((const void *)k_paged_attention<kD, kF16, kForm, kQ4>);
     if (e != cudaSuccess)
         return e;
-    e = launch_kernel(k_paged_attention<kD, kF16, kForm, kQ4>, dim3(n_sm), dim3(kThreads), (size_t)smem_bytes(kD, kQ4),
-                      stream, true, a);
+    e = launch_kernel(k_paged_attention<kD, kF16, kForm, kQ4>, dim3(n_sm), dim3(kThreads),
+                      (size_t)smem_bytes<kD, kQ4>(), stream, true, a);
     if (e != cudaSuccess || n_sm < 2)
         return e;
     int rows_log2 = 0;
