@@ -14,9 +14,12 @@
 // shared memory.  P moves from the layout of a result (keys by queries) to that of an
 // operand by an 8 x 8 transpose in the warp.
 //
-// Each warp walks its own pieces of 32 keys (every 16th of the CTA's), copied whole
-// from the pages into a ring of its own, with its own maxima, sums and output;
-// at a unit's end the CTA adds the 16 of them up, in a fixed order.
+// The CTA's tiles, as pieces of 32 keys, are split evenly over its 16 warps, a run
+// each, and a warp walks its run alone: its own ring of copied pieces, its own maxima,
+// sums and output, nothing to wait for.  A unit that lies within a run is written out
+// by its warp.  Of those that do not, the warps leave their parts (the first of a run
+// in the CTA's slots of the workspace, the last in shared memory once all rings are
+// done with), and the CTA joins them in order.
 #pragma once
 
 namespace tv {
@@ -25,7 +28,7 @@ namespace {
 
 constexpr int kFewRows = 16;
 constexpr int kFewKeys = 32;  // of a piece
-constexpr int kFewSegs = 64;  // units laid out at a time
+constexpr int kFewSegs = 16;  // units that a warp lays out at a time
 constexpr int kFewWarps = kThreads / 32;
 
 constexpr int few_stages(int d)
@@ -33,36 +36,83 @@ constexpr int few_stages(int d)
     return d == 64 ? 4 : 2;
 }
 
-// A run of tiles of one unit.
+// The pieces of one unit in a warp's run.
 struct FewSeg {
-    int first, end;  // its pieces, from the CTA's first tile on
-    int head, j0, whole;
+    int first, from, to;  // the unit's first piece, the run's own: pieces of the CTA's tiles, counted from t0
+    int head;
     PlanReq r;
 };
 
 // A query row of a unit.
 struct FewRow {
     uint64_t anc, path;
-    long long out;  // (row, query head); -1: none
     int lo, pos;
     float slope;
     int pad;
 };
 
+// A warp's part of a unit that others have parts of too.
+struct FewPart {
+    int unit;  // its first piece; parts of one unit follow one another
+    int begins, ends, valid;  // whether the unit does, in this part; one that was computed
+    int head;
+    int row0, n;  // the request's rows; n 0: none to write
+};
+constexpr int kNoUnit = 0x7fffffff;
+
 template <int kD>
 struct FewSmem {
     static constexpr int kStage = 2 * kFewKeys * row_bytes(kD), kRing = few_stages(kD) * kStage;
-    static constexpr int kQueryRow = 2 * kD + 16;  // bytes: rows begin in different banks
-    uint8_t ring[kFewWarps][kRing];
-    float4 sum[8][2 * kD / 16][32];       // O^T of 8 warps, fragment by fragment
-    uint8_t query[2][kFewRows * kQueryRow];  // of this unit and of the next
-    FewRow row[2][kFewRows];
-    float m[kFewWarps][kFewRows], l[kFewWarps][kFewRows];
-    FewSeg seg[kFewSegs];
-    uint32_t holes[kFewWarps][few_stages(kD)];
-    uint64_t full[kFewWarps][few_stages(kD)];
-    int n_segs;
+    union {
+        uint8_t ring[kFewWarps][kRing];
+        float4 last[kFewWarps][2 * kD / 16][32];  // O^T of the runs' last parts, fragment by fragment
+    };
+    FewRow row[kFewWarps][kFewRows];
+    FewSeg seg[kFewWarps][kFewSegs];
+    FewPart part[kFewWarps][2];
+    float m[kFewWarps][2][kFewRows], l[kFewWarps][2][kFewRows];
 };
+
+// Shared memory by its 32-bit address.
+__device__ __forceinline__ uint32_t lds8(uint32_t a)
+{
+    uint32_t x;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(a));
+    return x;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a)
+{
+    uint32_t x;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(a));
+    return x;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a)
+{
+    uint2 x;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(a));
+    return x;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a)
+{
+    uint4 x;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(a));
+    return x;
+}
+
+// 16 bytes into shared memory, behind this thread's back.
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_end()  // of a group
+{
+    asm volatile("cp.async.commit_group;" ::: "memory");
+}
+template <int kLeft>
+__device__ __forceinline__ void copies_wait()  // for all groups but the last kLeft
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
 
 template <bool kF16>
 __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -97,71 +147,87 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const PlanReq *reqs = plan_reqs(p.plan);
     const int window = static_cast<const PlanHeader *>(p.plan)->window;
-    const long long t0 = cta.t0, t1 = cta.t1;
+    const long long t0 = cta.t0;
+    const int pieces = 4 * (int)(cta.t1 - t0);
+    const int run0 = (int)((long long)pieces * warp / kFewWarps), run1 = (int)((long long)pieces * (warp + 1) / kFewWarps);
     uint8_t *ring = sm.ring[warp];
+    FewSeg *segs = sm.seg[warp];
+    FewRow *rows = sm.row[warp];
 
-    // ---- a warp's copies: lane (kind, piece) copies K's or V's part of a piece of min(page_size, 32) keys, with
-    // larger pages its codes or its scales
+    // ---- a warp's copies.  A piece's blocks are parts of min(page_size, 32) keys, first K's, then V's, each as it
+    // lies in its page (of a larger page: its codes, then its scales); 32, 16, 8 or 4 lanes copy a block.
     const int part_log2 = min(p.page_log2, 5);
-    const bool split = p.page_log2 > 5;
-    const int parts = split ? 2 : kFewKeys >> part_log2;
-    const bool copies = lane < 2 * parts, copies_v = lane >= parts;
-    const int part = copies_v ? lane - parts : lane, part_key = split ? 0 : part << part_log2;
+    const int block_log2 = 1 + 5 - part_log2;  // blocks of a piece
+    const int lanes_log2 = 5 - block_log2;     // lanes of a block
+    const int block = lane >> lanes_log2, in_block = lane & ((1 << lanes_log2) - 1);
+    const bool copies_v = block >> (block_log2 - 1);
+    const int part_key = (block & ((1 << (block_log2 - 1)) - 1)) << part_log2;
+    const uint32_t ring_a = smem_u32(ring);
+    const uint32_t copy_to = ring_a + (copies_v ? kFewKeys * row_bytes(kD) : 0) + part_key * row_bytes(kD) + 16 * in_block;
+    // its last round, of half or a quarter as many lanes; in a large page the scales
+    constexpr int kRounds = kD / 16, kTail = kD / 128 ? 2 : 4;
+    const bool in_tail = in_block < (1 << lanes_log2) / kTail;
     struct Fetch {
         int id, key0, head;
         bool inside;
     };
     auto seg_key = [&](const FewSeg &s, int piece) {
-        return tile_key(s.j0 + ((piece - s.first) >> 2), s.r.a0, s.r.n1, s.r.b0) + ((piece & 3) * kFewKeys);
+        return tile_key((piece - s.first) >> 2, s.r.a0, s.r.n1, s.r.b0) + ((piece & 3) * kFewKeys);
     };
-    int ahead_seg = 0, issued = 0, taken = 0;
+    int ahead_seg = 0, issue_at = 0, take_at = 0;
+    uint32_t hole_ring = 0;  // four bits per stage: parts that are not there
     auto fetch = [&](int piece) {
-        while (piece >= sm.seg[ahead_seg].end)
+        while (piece >= segs[ahead_seg].to)
             ++ahead_seg;
-        const FewSeg &s = sm.seg[ahead_seg];
+        const FewSeg &s = segs[ahead_seg];
         Fetch f{-1, seg_key(s, piece), s.head, false};
         const int slot = f.key0 + part_key, at = slot >> p.page_log2;
-        f.inside = copies && slot < s.r.L + s.r.n;
+        f.inside = slot < s.r.L + s.r.n;
         if (f.inside && at < p.max_pages)
             f.id = p.table[(size_t)s.r.b * p.max_pages + at];
         return f;
     };
     auto report_hole = [&](int slot) {
-        const PlanReq &r = sm.seg[ahead_seg].r;
+        const PlanReq &r = segs[ahead_seg].r;
         const int past = slot + (1 << part_log2);
         const int lo_min = window > 0 ? max(r.begin, r.L - window + 1) : r.begin;
         if (past > lo_min || (window > 0 && past > r.begin && slot < min(r.far_end, r.L)))
             atomicOr(p.status, kStatusBounds);
     };
+    auto copy_block = [&](auto log2, uint32_t to, const uint8_t *src, const uint8_t *tail) {
+        constexpr int kStep = 16 << decltype(log2)::value;
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i)
+            copy16(to + i * kStep, src + i * kStep);
+        if (in_tail)
+            copy16(to + kRounds * kStep, tail);
+    };
     auto issue = [&](const Fetch &f) {
-        const int s = issued % kStages;
         const bool there = f.inside && f.id >= 0 && f.id < p.n_pages;
-        const uint32_t holes = __ballot_sync(0xffffffffu, f.inside && !there);
-        const uint32_t found = __ballot_sync(0xffffffffu, there);
-        if (lane == 0) {
-            sm.holes[warp][s] = holes & ((1u << parts) - 1);
-            mbar_arrive_expect_tx(&sm.full[warp][s], split ? (found ? 2 * kFewKeys * row_bytes(kD) : 0)
-                                                           : (__popc(found) << part_log2) * row_bytes(kD));
-        }
-        __syncwarp();
         if (there) {
-            const uint8_t *src = (copies_v ? p.v_pages : p.k_pages) + f.id * p.page_stride + f.head * p.head_stride;
-            uint8_t *dst = ring + s * FewSmem<kD>::kStage + (copies_v ? kFewKeys * row_bytes(kD) : 0);
-            if (!split) {
-                bulk_load(dst + part_key * row_bytes(kD), src, row_bytes(kD) << part_log2, &sm.full[warp][s]);
+            const uint8_t *src = (copies_v ? p.v_pages : p.k_pages) + f.id * p.page_stride + f.head * p.head_stride +
+                                 16 * in_block;
+            const uint32_t to = copy_to + issue_at * FewSmem<kD>::kStage;
+            if (part_log2 == 4) {
+                copy_block(std::integral_constant<int, 3>{}, to, src, src + kRounds * 128);
+            } else if (part_log2 == 3) {
+                copy_block(std::integral_constant<int, 2>{}, to, src, src + kRounds * 64);
             } else {
                 const int at = f.key0 & ((1 << p.page_log2) - 1);
-                if (part == 0)
-                    bulk_load(dst, src + at * code_bytes(kD), kFewKeys * code_bytes(kD), &sm.full[warp][s]);
-                else
-                    bulk_load(dst + kFewKeys * code_bytes(kD),
-                              src + ((long long)code_bytes(kD) << p.page_log2) + at * scale_bytes(kD),
-                              kFewKeys * scale_bytes(kD), &sm.full[warp][s]);
+                const uint8_t *tail = src + ((long long)code_bytes(kD) << p.page_log2) + at * scale_bytes(kD);
+                copy_block(std::integral_constant<int, 4>{}, to, src + at * code_bytes(kD), tail);
             }
         }
-        if (f.inside && !there && !copies_v && (!split || part == 0))
-            report_hole(f.key0 + part_key);
-        ++issued;
+        copies_end();
+        const uint32_t missing = __ballot_sync(0xffffffffu, f.inside && !there && !copies_v);
+        hole_ring &= ~(15u << (4 * issue_at));
+        if (missing) {
+            for (int x = 0; x < kFewKeys >> part_log2; ++x)
+                hole_ring |= ((missing >> (x << lanes_log2)) & 1u) << (4 * issue_at + x);
+            if (f.inside && !there && !copies_v && in_block == 0)
+                report_hole(f.key0 + part_key);
+        }
+        issue_at = issue_at + 1 == kStages ? 0 : issue_at + 1;
     };
 
     // ---- where this thread's keys and values lie in a piece.  Row i of a product's 16 keys is key i with its
@@ -178,34 +244,24 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
     const int v_scale = kFewKeys * row_bytes(kD) + per_part * code_bytes(kD) + key_v * scale_bytes(kD) +
                         g * (kD / 8) / kGroup;
 
-    if (lane == 0)
-        for (int s = 0; s < kStages; ++s)
-            mbar_init(&sm.full[warp][s], 1);
-    fence_mbar_init();
-    __syncwarp();
-
-    // ---- a unit's rows: warp w takes row w, its query and what it sees
-    auto stage = [&](const FewSeg &s, int buf) {
-        const int row = cta.rb * 128 + warp, node = row / p.group, qh = s.head * p.group + row % p.group;
-        bool valid = node < s.r.n && s.r.row0 + node < p.n_rows;
+    // where row r of a unit goes, (row, query head); -1: no such row
+    auto row_at = [&](const FewSeg &s, int r) {
+        const int row = cta.rb * 128 + r, node = row / p.group, qh = s.head * p.group + row % p.group;
+        const bool valid = node < s.r.n && s.r.row0 + node < p.n_rows &&
+                           in_bounds(node < kMaxNodes && qh < p.Hq && s.r.row0 >= 0, p.status);
+        return valid ? (long long)(s.r.row0 + node) * p.Hq + qh : -1ll;
+    };
+    // what the rows see: a lane each; false if the call's bank has not the plan's tree
+    auto stage = [&](const FewSeg &s) {
         const bool known = (unsigned)s.r.tree < (unsigned)p.n_trees;
-        if (valid && !known)
-            atomicOr(p.status, kStatusBounds);
         const TreeDesc &td = p.trees[known ? s.r.tree : 0];
-        if (valid && known && td.n != s.r.n)
-            atomicOr(p.status, kStatusBounds);
-        valid = valid && known && td.n == s.r.n;
-        valid = valid && in_bounds(node < kMaxNodes && qh < p.Hq && s.r.row0 >= 0, p.status);
-        const size_t at = valid ? (size_t)(s.r.row0 + node) * p.Hq + qh : 0;
-        uint32_t *dst = reinterpret_cast<uint32_t *>(sm.query[buf] + warp * FewSmem<kD>::kQueryRow);
-        const uint32_t *src = reinterpret_cast<const uint32_t *>(p.q + at * kD);
-#pragma unroll
-        for (int i = 0; i < kD / 64; ++i)
-            dst[lane + 32 * i] = valid ? src[lane + 32 * i] : 0u;
-        if (lane == 0) {
+        const bool same = known && td.n == s.r.n;
+        if (lane < kFewRows) {
+            const int row = cta.rb * 128 + lane, node = row / p.group, qh = s.head * p.group + row % p.group;
+            const bool valid = same && node < s.r.n && node < kMaxNodes;
             const int L = s.r.L, dep = valid ? td.depth[node] : 0;
             uint64_t anc = valid ? td.anc[node] : 0;
-            FewRow &r = sm.row[buf][warp];
+            FewRow &r = rows[lane];
             r.path = anc;
             if (window > 0 && dep >= window) {
                 // ancestors that the window has left behind
@@ -218,112 +274,123 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
             if (s.r.begin > L)
                 anc &= s.r.begin - L < 64 ? ~0ull << (s.r.begin - L) : 0ull;
             r.anc = anc;
-            r.out = valid ? (long long)at : -1;
             r.lo = window > 0 ? max(s.r.begin, L + dep - window + 1) : s.r.begin;
             r.pos = L + dep;
-            r.slope = kForm == kBias && valid && p.slopes ? p.slopes[qh] * kLog2e : 0.f;
+            r.slope = kForm == kBias && valid && qh < p.Hq && p.slopes ? p.slopes[qh] * kLog2e : 0.f;
         }
+        if (!same && lane == 0)
+            atomicOr(p.status, kStatusBounds);
+        __syncwarp();
+        return same;
     };
 
+    // ---- the run's first unit
     bool ok = true;
-    int unit0 = 0;  // units before this round's
-    const int head0 = (int)((t0 - cta.req.tile_base) / cta.req.T);
-    for (bool more = true; more; unit0 += kFewSegs) {
-        // ---- the next units: those whose tiles begin before t1, in order
-        __syncthreads();
-        if (threadIdx.x < kFewSegs) {
-            const int u = head0 + unit0 + threadIdx.x, i = cta.idx + u / p.Hkv;
+    int request = cta.idx, head0 = 0;
+    if (run0 < run1) {
+        const long long tile = t0 + (run0 >> 2);
+        for (int i0 = cta.idx;; i0 += 32) {
+            const int i = i0 + lane;
+            const uint32_t before = __ballot_sync(0xffffffffu, i < p.batch && reqs[i].tile_base <= tile);
+            const int n = before == 0xffffffffu ? 32 : __ffs((int)~before) - 1;
+            request = i0 + n - 1;
+            if (n < 32)
+                break;
+        }
+        head0 = (int)((tile - reqs[request].tile_base) / reqs[request].T);
+    }
+    if (lane < 2)
+        sm.part[warp][lane] = FewPart{kNoUnit, 0, 0, 0, 0, 0, 0};
+    float o[kTilesD][kN][4];
+    float m[kN][2], l[kN][2];  // of columns 8 n + 2 t and the one after it; l: this thread's keys
+    bool last_here = false;    // o, m and l are the run's last part
+    int n_parts = 0;
+    for (int piece = run0; piece < run1; head0 += kFewSegs) {
+        // ---- the next units
+        int n_segs;
+        {
+            const int u = head0 + lane, i = request + u / p.Hkv;
             FewSeg s{};
-            bool in = i < p.batch;
+            bool in = lane < kFewSegs && i < p.batch;
             if (in) {
                 s.r = reqs[i];
                 s.head = u % p.Hkv;
-                const long long first = s.r.tile_base + (long long)s.head * s.r.T;
-                in = first < t1 && s.r.T > 0;
-                const long long from = max(first, t0), to = min(first + s.r.T, t1);
-                s.j0 = (int)(from - first);
-                s.first = 4 * (int)(from - t0);
-                s.end = 4 * (int)(to - t0);
-                s.whole = to - from == s.r.T;
+                const long long first = s.r.tile_base + (long long)s.head * s.r.T - t0;
+                in = first < (run1 + 3) / 4;
+                s.first = in ? 4 * (int)first : 0;
+                s.from = max(s.first, run0);
+                s.to = min(s.first + 4 * s.r.T, run1);
+                in = in && s.from < s.to;
             }
             // records behind the last request hold anything: only what follows without a gap counts
             const uint32_t all = __ballot_sync(0xffffffffu, in);
-            const int n = all == 0xffffffffu ? 32 : __ffs((int)~all) - 1;
-            if (lane < n)
-                sm.seg[threadIdx.x] = s;
-            if (threadIdx.x == 0)
-                sm.n_segs = n;
-            asm volatile("bar.sync 1, 64;" ::: "memory");
-            if (threadIdx.x == 32 && sm.n_segs == 32)
-                sm.n_segs = 32 + n;
+            n_segs = __ffs((int)~all) - 1;  // (at most kFewSegs lanes)
+            __syncwarp();
+            if (lane < n_segs)
+                segs[lane] = s;
+            __syncwarp();
         }
-        __syncthreads();
-        const int n_segs = sm.n_segs;
         if (n_segs == 0)
             break;
-        const int last = sm.seg[n_segs - 1].end;
-        more = last < 4 * (int)(t1 - t0);
-        // this warp's pieces of the round: the ring filled, the next page looked up
-        int next = sm.seg[0].first + ((warp - sm.seg[0].first) & (kFewWarps - 1));
-        int piece = next;
+        const int last = segs[n_segs - 1].to;
+        // the ring filled, the next page looked up
+        issue_at = take_at = 0;
         ahead_seg = 0;
-        Fetch ahead{};
-        bool has_ahead = next < last;
-        if (has_ahead)
-            ahead = fetch(next);
-        auto refill = [&] {
+        int next = piece;
+        Fetch ahead = fetch(next);
+        auto refill = [&] {  // one group of copies each time, an empty one at the end
+            if (next >= last) {
+                copies_end();
+                return;
+            }
             issue(ahead);
-            next += kFewWarps;
-            has_ahead = next < last;
-            if (has_ahead)
+            if (++next < last)
                 ahead = fetch(next);
         };
-        for (int s = 0; s < kStages && has_ahead && ok; ++s)
+        for (int s = 0; s < kStages; ++s)
             refill();
-        stage(sm.seg[0], 0);
-        __syncthreads();
 
         for (int si = 0; si < n_segs; ++si) {
-            const FewSeg &seg = sm.seg[si];
-            const int buf = si & 1, L = seg.r.L, end = L + seg.r.n, begin = seg.r.begin;
+            const FewSeg &seg = segs[si];
+            const int L = seg.r.L, end = L + seg.r.n, begin = seg.r.begin;
             const int far = window > 0 ? min(seg.r.far_end, L) : begin;
             const int lo_min = window > 0 ? max(begin, L - window + 1) : begin;
             const int lo_max = window > 0 ? lo_min + kMaxNodes : begin;  // past any row's
-            const FewRow *rows = sm.row[buf];
             // queries of columns g (and 8 + g) in the order of the keys' elements
             uint32_t q[kD / 16][kN][2];
 #pragma unroll
-            for (int n = 0; n < kN; ++n)
+            for (int n = 0; n < kN; ++n) {
+                const long long at = row_at(seg, 8 * n + g);
+                const uint4 *src = reinterpret_cast<const uint4 *>(p.q + max(at, 0ll) * kD + t * (kD / 4));
 #pragma unroll
                 for (int i = 0; i < kD / 32; ++i) {
-                    const uint4 x = code_order(*reinterpret_cast<const uint4 *>(
-                        sm.query[buf] + (8 * n + g) * FewSmem<kD>::kQueryRow + t * (kD / 2) + 16 * i));
+                    const uint4 x = code_order(at >= 0 ? src[i] : make_uint4(0, 0, 0, 0));
                     q[2 * i][n][0] = x.x, q[2 * i][n][1] = x.y;
                     q[2 * i + 1][n][0] = x.z, q[2 * i + 1][n][1] = x.w;
                 }
-            if (si + 1 < n_segs)
-                stage(sm.seg[si + 1], buf ^ 1);
-            float o[kTilesD][kN][4] = {};
-            float m[kN][2], l[kN][2];  // of columns 8 n + 2 t and the one after it; l: this thread's keys
+            }
+            const bool known = stage(seg);
 #pragma unroll
-            for (int n = 0; n < kN; ++n)
+            for (int n = 0; n < kN; ++n) {
                 m[n][0] = m[n][1] = -INFINITY, l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+                for (int j = 0; j < kTilesD; ++j)
+                    o[j][n][0] = o[j][n][1] = o[j][n][2] = o[j][n][3] = 0.f;
+            }
 
-            for (; piece < seg.end; piece += kFewWarps) {
-                const int st = taken % kStages;
-                ok = ok && warp_agrees(mbar_wait_bounded(p.expire_wait ? never_bar : &sm.full[warp][st],
-                                                         p.expire_wait ? 0u : (uint32_t)(taken / kStages) & 1u, abort_flag,
-                                                         p.status));
-                if (!ok)
-                    continue;
-                ++taken;
+            for (; piece < seg.to; ++piece) {
+                if (p.expire_wait)
+                    ok = ok && warp_agrees(mbar_wait_bounded(never_bar, 0, abort_flag, p.status));
+                copies_wait<kStages - 1>();
+                __syncwarp();
                 const int key0 = seg_key(seg, piece);
-                const uint8_t *base = ring + st * FewSmem<kD>::kStage;
-                const uint32_t holes = sm.holes[warp][st];
-                if (key0 < end) {
-                    const bool masked = key0 + kFewKeys > L || key0 < lo_max || holes;
+                const uint32_t base = ring_a + take_at * FewSmem<kD>::kStage;
+                const uint32_t holes = (hole_ring >> (4 * take_at)) & 15u;
+                take_at = take_at + 1 == kStages ? 0 : take_at + 1;
+                const auto work = [&](auto is_masked) {
+                    constexpr bool masked = decltype(is_masked)::value;
                     // a key's or value's scale: 0 in a hole, of a value also where no row looks
-                    auto there = [&](int key) { return !((holes >> (split ? 0 : key >> part_log2)) & 1u); };
+                    auto there = [&](int key) { return !((holes >> (key >> part_log2)) & 1u); };
                     auto looked_at = [&](int key) {
                         const int slot = key0 + key;
                         return there(key) && slot < end && slot >= begin && (slot >= lo_min || slot < far);
@@ -335,16 +402,16 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                         Scale<kF16> sc[2];
 #pragma unroll
                         for (int a = 0; a < 2; ++a) {
-                            const uint8_t *c = base + k_code + a * code8 + b * code16;
+                            const uint32_t c = base + k_code + a * code8 + b * code16;
                             if constexpr (kD == 128) {
-                                const uint4 x = *reinterpret_cast<const uint4 *>(c);
+                                const uint4 x = lds128(c);
                                 w[a][0] = x.x, w[a][1] = x.y, w[a][2] = x.z, w[a][3] = x.w;
                             } else {
-                                const uint2 x = *reinterpret_cast<const uint2 *>(c);
+                                const uint2 x = lds64(c);
                                 w[a][0] = x.x, w[a][1] = x.y;
                             }
-                            float f = scale_of(base[k_scale + a * scale8 + b * scale16]);
-                            if (masked)
+                            float f = scale_of(lds8(base + k_scale + a * scale8 + b * scale16));
+                            if constexpr (masked)
                                 f = there(key_k + 8 * a + 16 * b) ? f : 0.f;
                             sc[a] = scale_pair<kF16>(f, f);
                         }
@@ -369,7 +436,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                     };
                     constexpr float kHidden = kForm == kCap ? INFINITY : -INFINITY;  // z = -inf
                     uint32_t sees = 0xffffffffu;  // bit 8 n + 4 b + c... of this thread's scores
-                    if (masked) {
+                    if constexpr (masked) {
                         sees = 0;
 #pragma unroll
                         for (int n = 0; n < kN; ++n)
@@ -392,7 +459,8 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
 #pragma unroll
                                     for (int i = 0; i < 4; ++i) {
                                         const int b = i >> 1, e = c + 2 * (i & 1);
-                                        r[i] = (sees >> (8 * n + 4 * b + e)) & 1u ? __float_as_uint(s[b][n][e]) : 0xff800000u;
+                                        r[i] = !masked || ((sees >> (8 * n + 4 * b + e)) & 1u) ? __float_as_uint(s[b][n][e])
+                                                                                               : 0xff800000u;
                                     }
                                     cap_four(r, p.cap_in);
 #pragma unroll
@@ -427,7 +495,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                                     z[c] = fmaf(-r.slope, (float)dist, z[c]);
                                 }
                             }
-                            if (masked) {
+                            if constexpr (masked) {
 #pragma unroll
                                 for (int c = 0; c < 4; ++c)
                                     z[c] = (sees >> (8 * n + 4 * b + c)) & 1u ? z[c] : kHidden;
@@ -497,15 +565,15 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                             float f[2];
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
-                                const uint8_t *c = base + v_code + 2 * x * code_bytes(kD) + a * code8 + b * code16;
+                                const uint32_t c = base + v_code + 2 * x * code_bytes(kD) + a * code8 + b * code16;
                                 if constexpr (kD == 128) {
-                                    const uint2 y = *reinterpret_cast<const uint2 *>(c);
+                                    const uint2 y = lds64(c);
                                     v[a][x][0] = y.x, v[a][x][1] = y.y;
                                 } else {
-                                    v[a][x][0] = *reinterpret_cast<const uint32_t *>(c);
+                                    v[a][x][0] = lds32(c);
                                 }
-                                f[x] = scale_of(base[v_scale + 2 * x * scale_bytes(kD) + a * scale8 + b * scale16]);
-                                if (masked)
+                                f[x] = scale_of(lds8(base + v_scale + 2 * x * scale_bytes(kD) + a * scale8 + b * scale16));
+                                if constexpr (masked)
                                     f[x] = looked_at(key_v + 2 * x + 8 * a + 16 * b) ? f[x] : 0.f;
                             }
                             sc[a] = scale_pair<kF16>(f[0], f[1]);
@@ -530,112 +598,174 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                                 }
                             }
                     }
+                };
+                if (key0 + kFewKeys > L || key0 < lo_max || holes) {
+                    if (key0 < end)
+                        work(std::true_type{});
+                } else {
+                    work(std::false_type{});
                 }
                 __syncwarp();
-                if (has_ahead)
-                    refill();
+                refill();
             }
 
-            // ---- the unit's end: 16 warps' maxima, sums and outputs, added up in their order
+            // ---- the unit's end here
 #pragma unroll
             for (int n = 0; n < kN; ++n)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int x = 4; x < 32; x *= 2)
                         l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], x);
-                    if (g == 0) {
-                        sm.m[warp][8 * n + 2 * t + c] = m[n][c];
-                        sm.l[warp][8 * n + 2 * t + c] = l[n][c];
+            const bool begins = seg.from == seg.first, ends = seg.to == seg.first + 4 * seg.r.T;
+            if (begins && ends) {
+                // columns 8 n + 2 t and the next: kD / 8 elements from (kD / 8) g on
+#pragma unroll
+                for (int n = 0; n < kN; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const long long at = row_at(seg, 8 * n + 2 * t + c);
+                        if (at < 0 || !known || !ok)
+                            continue;
+                        const float lc = l[n][c], inv = lc == 0.f ? 0.f : 1.f / lc;  // a NaN stays one
+                        uint32_t w[kTilesD];
+#pragma unroll
+                        for (int j = 0; j < kTilesD; ++j)
+                            w[j] = pack<kF16>(o[j][n][c] * inv, o[j][n][c + 2] * inv);
+                        uint4 *dst = reinterpret_cast<uint4 *>(p.out + at * kD + g * (kD / 8));
+#pragma unroll
+                        for (int j = 0; j < kTilesD / 4; ++j)
+                            dst[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+                        if (p.lse && g == 0)
+                            p.lse[at] = lc == 0.f ? -INFINITY : (m[n][c] + log2f(lc)) * kLn2;
                     }
-                }
-            __syncthreads();
-            const bool stop = *const_cast<volatile int *>(abort_flag) != 0;  // (nobody waits until the next unit)
-            float M[kN][2], sum[kN][2];
+                continue;
+            }
+            // a part: at most two of a run, the second at its end
+            if (lane == 0)
+                sm.part[warp][n_parts] =
+                    FewPart{seg.first, begins, ends, ok, seg.head, seg.r.row0, known ? seg.r.n : 0};
+            if (g == 0) {
 #pragma unroll
-            for (int n = 0; n < kN; ++n)
+                for (int n = 0; n < kN; ++n)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int col = 8 * n + 2 * t + c;
-                    float x = -INFINITY, y = 0.f;
-#pragma unroll
-                    for (int k = 0; k < kFewWarps; ++k)
-                        x = fmaxf(x, sm.m[k][col]);
-#pragma unroll
-                    for (int k = 0; k < kFewWarps; ++k)
-                        y += (sm.m[k][col] == -INFINITY ? 0.f : ex2_approx(sm.m[k][col] - x)) * sm.l[k][col];
-                    const float scale = m[n][c] == -INFINITY ? 0.f : ex2_approx(m[n][c] - x);
-                    M[n][c] = x;
-                    sum[n][c] = y;
-#pragma unroll
-                    for (int j = 0; j < kTilesD; ++j)
-                        o[j][n][c] *= scale, o[j][n][c + 2] *= scale;
-                }
-            // fragment (j, n) is written by warp j kN + n: elements (kD / 8) g + 2 j and the next of columns
-            // 8 n + 2 t and the next.  (Where to is read here: the next unit's rows may be staged from the last
-            // barrier on.)
-            const int write_j = warp / kN, write_n = warp % kN;
-            long long write_at[2];
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-                write_at[c] = rows[8 * write_n + 2 * t + c].out;
-            float4(*part)[32] = sm.sum[warp & 7];
-            if (warp >= 8) {
+                    for (int c = 0; c < 2; ++c) {
+                        sm.m[warp][n_parts][8 * n + 2 * t + c] = m[n][c];
+                        sm.l[warp][n_parts][8 * n + 2 * t + c] = l[n][c];
+                    }
+            }
+            if (n_parts == 0) {
+                float4 *to = reinterpret_cast<float4 *>(p.part + (size_t)blockIdx.x * 2 * kSlot) + warp * kTilesD * kN * 32;
 #pragma unroll
                 for (int j = 0; j < kTilesD; ++j)
 #pragma unroll
                     for (int n = 0; n < kN; ++n)
-                        part[j * kN + n][lane] = make_float4(o[j][n][0], o[j][n][1], o[j][n][2], o[j][n][3]);
+                        to[(j * kN + n) * 32 + lane] = make_float4(o[j][n][0], o[j][n][1], o[j][n][2], o[j][n][3]);
+            } else {
+                last_here = true;
             }
-            __syncthreads();
-            if (warp < 8) {
+            ++n_parts;
+        }
+    }
+    copies_wait<0>();
+
+    // ---- the units that runs share
+    __syncthreads();  // all rings are done with
+    if (last_here) {
 #pragma unroll
-                for (int j = 0; j < kTilesD; ++j)
+        for (int j = 0; j < kTilesD; ++j)
 #pragma unroll
-                    for (int n = 0; n < kN; ++n) {
-                        const float4 x = part[j * kN + n][lane];
-                        part[j * kN + n][lane] =
-                            make_float4(o[j][n][0] + x.x, o[j][n][1] + x.y, o[j][n][2] + x.z, o[j][n][3] + x.w);
-                    }
-            }
-            __syncthreads();
-            if (warp < kTilesD * kN && !stop) {
-                float4 a = sm.sum[0][warp][lane];
+            for (int n = 0; n < kN; ++n)
+                sm.last[warp][j * kN + n][lane] = make_float4(o[j][n][0], o[j][n][1], o[j][n][2], o[j][n][3]);
+    }
+    __syncthreads();
+    // thread f of kTilesD kN 32 takes fragment f of every unit; at most two of them are also other CTAs', and go to
+    // the slots that the first parts lie in: once all have read those
+    const int frag = threadIdx.x, fj = frag / 32 / kN, fn = frag / 32 % kN;
+    const bool mine = frag < kTilesD * kN * 32;
+    const bool stop = *const_cast<volatile int *>(abort_flag) != 0;  // (nobody waits any more)
+    const float4 *firsts = reinterpret_cast<const float4 *>(p.part + (size_t)blockIdx.x * 2 * kSlot);
+    float4 kept[2];
+    float kept_m[2][2], kept_l[2][2];
+    int kept_slot[2] = {-1, -1}, n_kept = 0;
+    for (int x = 0; x < 2 * kFewWarps;) {
+        const FewPart head = sm.part[x >> 1][x & 1];
+        int y = x + 1;
+        if (head.unit == kNoUnit) {
+            x = y;
+            continue;
+        }
+        while (y < 2 * kFewWarps && (sm.part[y >> 1][y & 1].unit == head.unit || sm.part[y >> 1][y & 1].unit == kNoUnit))
+            ++y;
+        bool ends = false;
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        float M[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+        if (mine) {
+            for (int z = x; z < y; ++z)
+                if (sm.part[z >> 1][z & 1].unit == head.unit)
 #pragma unroll
-                for (int k = 1; k < 8; ++k) {
-                    const float4 x = sm.sum[k][warp][lane];
-                    a.x += x.x, a.y += x.y, a.z += x.z, a.w += x.w;
-                }
+                    for (int c = 0; c < 2; ++c)
+                        M[c] = fmaxf(M[c], sm.m[z >> 1][z & 1][8 * fn + 2 * t + c]);
+            for (int z = x; z < y; ++z) {
+                const FewPart &part = sm.part[z >> 1][z & 1];
+                if (part.unit != head.unit)
+                    continue;
+                ends = part.ends;
+                const float4 v = z & 1 ? sm.last[z >> 1][frag / 32][lane]
+                                       : __ldcg(firsts + (z >> 1) * kTilesD * kN * 32 + frag);
+                float f[2];
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const int col = 8 * write_n + 2 * t + c, e = (kD / 8) * g + 2 * write_j;
-                    const long long at = write_at[c];
-                    if (at < 0)
-                        continue;
-                    const float Mc = write_n == 0 ? M[0][c] : M[kN - 1][c];
-                    const float lc = write_n == 0 ? sum[0][c] : sum[kN - 1][c];
-                    const float x = c ? a.y : a.x, y = c ? a.w : a.z;
-                    if (seg.whole) {
-                        const float inv = lc == 0.f ? 0.f : 1.f / lc;  // a NaN stays one
-                        *reinterpret_cast<uint32_t *>(p.out + at * kD + e) = pack<kF16>(x * inv, y * inv);
-                        if (p.lse && write_j == 0 && g == 0)
-                            p.lse[at] = lc == 0.f ? -INFINITY : (Mc + log2f(lc)) * kLn2;
-                    } else {
-                        float *slot = p.part + ((size_t)blockIdx.x * 2 + (seg.first == 0 ? 0 : 1)) * kSlot;
-                        *reinterpret_cast<float2 *>(slot + col * kD + e) = make_float2(x, y);
-                        if (write_j == 0 && g == 0) {
-                            slot[128 * kD + col] = Mc;
-                            slot[128 * kD + 128 + col] = lc;
-                        }
-                    }
+                    const float mz = sm.m[z >> 1][z & 1][8 * fn + 2 * t + c];
+                    f[c] = mz == -INFINITY ? 0.f : ex2_approx(mz - M[c]);
+                    sum[c] = fmaf(f[c], sm.l[z >> 1][z & 1][8 * fn + 2 * t + c], sum[c]);
                 }
+                a.x = fmaf(f[0], v.x, a.x), a.y = fmaf(f[1], v.y, a.y);
+                a.z = fmaf(f[0], v.z, a.z), a.w = fmaf(f[1], v.w, a.w);
+            }
+        }
+        if (mine && head.begins && ends) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                FewSeg s{};
+                s.head = head.head, s.r.n = head.n, s.r.row0 = head.row0;
+                const long long at = row_at(s, 8 * fn + 2 * t + c);
+                if (at < 0 || stop)
+                    continue;
+                const float inv = sum[c] == 0.f ? 0.f : 1.f / sum[c];
+                *reinterpret_cast<uint32_t *>(p.out + at * kD + g * (kD / 8) + 2 * fj) =
+                    pack<kF16>((c ? a.y : a.x) * inv, (c ? a.w : a.z) * inv);
+                if (p.lse && fj == 0 && g == 0)
+                    p.lse[at] = sum[c] == 0.f ? -INFINITY : (M[c] + log2f(sum[c])) * kLn2;
+            }
+        } else if (mine && n_kept < 2) {
+            // of the CTA's first tile on: slot 0, as for many rows
+            kept_slot[n_kept] = head.unit <= 0 ? 0 : 1;
+            kept[n_kept] = a;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                kept_m[n_kept][c] = M[c], kept_l[n_kept][c] = sum[c];
+            ++n_kept;
+        }
+        x = y;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (!mine || kept_slot[i] < 0)
+            continue;
+        float *slot = p.part + ((size_t)blockIdx.x * 2 + kept_slot[i]) * kSlot;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int col = 8 * fn + 2 * t + c;
+            *reinterpret_cast<float2 *>(slot + col * kD + g * (kD / 8) + 2 * fj) =
+                c ? make_float2(kept[i].y, kept[i].w) : make_float2(kept[i].x, kept[i].z);
+            if (fj == 0 && g == 0) {
+                slot[128 * kD + col] = kept_m[i][c];
+                slot[128 * kD + 128 + col] = kept_l[i][c];
             }
         }
     }
-    if (!ok && lane == 0)
-        for (; taken < issued; ++taken)
-            mbar_wait_drain(&sm.full[warp][taken % kStages], (uint32_t)(taken / kStages) & 1u);
-    __syncwarp();
 }
 
 }  // namespace
