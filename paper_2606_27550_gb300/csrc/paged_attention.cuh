@@ -100,7 +100,8 @@ float cap_in(float scale, float softcap)
 struct PagedArgs {
     CUtensorMap tk, tv;  // of the layer
     const uint8_t *k_pages, *v_pages;  // 4-bit pages: the layer's, strides in bytes
-    long long page_stride, head_stride;
+    long long head_stride;
+    uint32_t page_units;  // 16 bytes each
     const TreeDesc *trees;
     int n_trees;
     const int32_t *table;
@@ -275,6 +276,38 @@ __device__ constexpr int code_place(int e)
     return e < 4 ? 2 * e : 2 * (e - 4) + 1;
 }
 
+// Shared memory by its 32-bit address.
+__device__ __forceinline__ uint32_t lds8(uint32_t a)
+{
+    uint32_t x;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(a));
+    return x;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a)
+{
+    uint32_t x;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(a));
+    return x;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a)
+{
+    uint2 x;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(a));
+    return x;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a)
+{
+    uint4 x;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(a));
+    return x;
+}
+
+__device__ __forceinline__ void sts128(uint32_t a, const uint32_t (&x)[4])
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3])
+                 : "memory");
+}
+
 // The packed tile of 128 keys: pieces of min(page_size, 128) keys, each as it lies in its page.
 struct PackedTile {
     int log2;  // keys of a piece
@@ -295,32 +328,35 @@ struct PackedTile {
 // A packed tile into one of 16-bit elements, by 128 threads (tid): 32 elements of a key each.  holes: the
 // pieces that are not there, whose elements count as zeros.
 template <int kD, bool kF16>
-__device__ __forceinline__ void unpack_tile(const uint8_t *packed, uint8_t *tile, const PackedTile &pt, uint32_t holes,
-                                            int tid)
+__device__ __forceinline__ void unpack_tile(uint32_t packed, uint32_t tile, const PackedTile &pt, uint32_t holes, int tid)
 {
     constexpr int kChunks = kD / kGroup;  // of a key
     constexpr int kKeys = 128 / kChunks;  // per round
+    const int key0 = tid / kChunks, chunk = tid % kChunks;
+    // eight neighbouring lanes write eight different 16-byte columns: those of the second atom in another order
+    const int flip = kD == 128 ? (chunk >> 1) * 2 : 0;
+    uint4 w[kChunks];
+    float f[kChunks];
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-        const int key = tid / kChunks + i * kKeys, chunk = tid % kChunks;
-        uint4 w = *reinterpret_cast<const uint4 *>(packed + pt.codes<kD>(key) + 16 * chunk);
-        const uint32_t byte = packed[pt.scales<kD>(key) + chunk];
-        const float f = (holes >> (key >> pt.log2)) & 1u ? 0.f : scale_of(byte);
-        const Scale<kF16> s = scale_pair<kF16>(f, f);
-        // eight neighbouring lanes write eight different 16-byte columns: those of the second atom in another order
-        const int flip = kD == 128 ? (chunk >> 1) * 2 : 0;
-        if (flip)
-            w = make_uint4(w.z, w.w, w.x, w.y);
-        uint8_t *row = tile + (kD == 128 ? (chunk >> 1) * kAtom : 0) + key * 128;
-        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+        const int key = key0 + i * kKeys;
+        w[i] = lds128(packed + pt.codes<kD>(key) + 16 * chunk);
+        f[i] = scale_of(lds8(packed + pt.scales<kD>(key) + chunk));
+        if (holes)
+            f[i] = (holes >> (key >> pt.log2)) & 1u ? 0.f : f[i];
+    }
+    const uint32_t to = tile + (kD == 128 ? (chunk >> 1) * kAtom : 0) + key0 * 128;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const OperandScale<kF16> s = operand_scale<kF16>(f[i], f[i]);
+        const uint32_t words[4] = {flip ? w[i].z : w[i].x, flip ? w[i].w : w[i].y, flip ? w[i].x : w[i].z,
+                                   flip ? w[i].y : w[i].w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             uint32_t e[4];
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-                e[n] = dequant_pair<kF16>(words[j] >> (4 * n), s);
-            const int col = (chunk & 1) * 4 + (j ^ flip);
-            *reinterpret_cast<uint4 *>(row + ((col ^ (key & 7)) * 16)) = make_uint4(e[0], e[1], e[2], e[3]);
+            dequant_four<kF16>(words[j], s, e);
+            // (kKeys is a multiple of 8: key & 7 is key0 & 7)
+            sts128(to + i * kKeys * 128 + ((((chunk & 1) * 4 + (j ^ flip)) ^ (key0 & 7)) * 16), e);
         }
     }
 }
@@ -527,7 +563,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                         }
                         __syncwarp();
                         if (page.inside && there) {
-                            const uint8_t *src = (is_v ? p.v_pages : p.k_pages) + page.id * p.page_stride +
+                            const uint8_t *src = (is_v ? p.v_pages : p.k_pages) +
+                                                 ((unsigned long long)(unsigned)page.id * p.page_units << 4) +
                                                  g.head * p.head_stride;
                             uint8_t *dst = ring + (size_t)s * kPacked + pg * keys * row_bytes(kD);
                             if (p.page_log2 <= 7) {
@@ -955,8 +992,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 !warp_agrees(mbar_wait_bounded(is_v ? &v_empty[s] : &k_empty[s], ((uint32_t)(n / S) & 1u) ^ 1u, &abort_flag,
                                                p.status)))
                 return false;
-            unpack_tile<kD, kF16>(packed + (size_t)((is_v ? kPackedStages : 0) + ps) * kPacked,
-                                  (is_v ? sV : sK) + (size_t)s * kTile, pt, packed_holes[is_v][ps], threadIdx.x & 127);
+            unpack_tile<kD, kF16>(smem_u32(packed) + ((is_v ? kPackedStages : 0) + ps) * kPacked,
+                                  smem_u32(is_v ? sV : sK) + s * kTile, pt, packed_holes[is_v][ps], threadIdx.x & 127);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
@@ -1017,7 +1054,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 break;
             tc_fence_after();
             const bool whole = now.n == now.T;
-            const float inv = l == 0.f ? 0.f : 1.f / l;  // a NaN stays one
+            // of 4-bit pages, the elements entered times a power of two
+            constexpr float kBack = kQ4 ? 1.f / kOperandScale<kF16> : 1.f;
+            const float inv = l == 0.f ? 0.f : kBack / l;  // a NaN stays one
             uint4 *dst = reinterpret_cast<uint4 *>(p.out + now.row * kD);
             float *slot = p.part + ((size_t)c * 2 + (now.first ? 0 : 1)) * kSlot;
             float4 *pdst = reinterpret_cast<float4 *>(slot + rloc * kD);
@@ -1056,8 +1095,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 } else {
 #pragma unroll
                     for (int x = 0; x < 8; ++x)
-                        pdst[c0 / 4 + x] = make_float4(__uint_as_float(r[4 * x]), __uint_as_float(r[4 * x + 1]),
-                                                       __uint_as_float(r[4 * x + 2]), __uint_as_float(r[4 * x + 3]));
+                        pdst[c0 / 4 + x] =
+                            make_float4(__uint_as_float(r[4 * x]) * kBack, __uint_as_float(r[4 * x + 1]) * kBack,
+                                        __uint_as_float(r[4 * x + 2]) * kBack, __uint_as_float(r[4 * x + 3]) * kBack);
                 }
             }
             if (now.valid && whole) {
@@ -1285,8 +1325,14 @@ tb_status attend(const tb_bank *bank, const tb_requests *req, const Pages *pages
     a.plan = const_cast<void *>(plan);
     a.part = attention_parts(workspace);
     a.status = static_cast<int *>(workspace);
+    if (kQ4 && pages->dtype == TB_BF16) {
+        a.scale *= 1.f / kOperandScale<false>;
+        a.cap_in *= 1.f / kOperandScale<false>;
+        if (!std::isfinite(a.scale) || !std::isfinite(a.cap_in))
+            return record_error(TB_EUNSUPPORTED, "%s: scale %g with softcap %g", fn, scale, softcap);
+    }
     if (const char *err = fill(a, layer))
-        return record_error(TB_EINVAL, "%s: %s", fn, err);
+        return record_error(kQ4 ? TB_EUNSUPPORTED : TB_EINVAL, "%s: %s", fn, err);
     const long long most = (long long)(n_rows < kMaxNodes ? n_rows : kMaxNodes) * a.group;
     const int max_rows = most < 128 ? (int)most : 128;
     const bool f16 = pages->dtype == TB_F16;

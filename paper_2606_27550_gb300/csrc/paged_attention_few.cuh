@@ -54,7 +54,7 @@ struct FewRow {
 // A warp's part of a unit that others have parts of too.
 struct FewPart {
     int unit;  // its first piece; parts of one unit follow one another
-    int begins, ends, valid;  // whether the unit does, in this part; one that was computed
+    int begins, ends;  // whether the unit does, in this part
     int head;
     int row0, n;  // the request's rows; n 0: none to write
 };
@@ -72,32 +72,6 @@ struct FewSmem {
     FewPart part[kFewWarps][2];
     float m[kFewWarps][2][kFewRows], l[kFewWarps][2][kFewRows];
 };
-
-// Shared memory by its 32-bit address.
-__device__ __forceinline__ uint32_t lds8(uint32_t a)
-{
-    uint32_t x;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(a));
-    return x;
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a)
-{
-    uint32_t x;
-    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(a));
-    return x;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a)
-{
-    uint2 x;
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(a));
-    return x;
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a)
-{
-    uint4 x;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(a));
-    return x;
-}
 
 // 16 bytes into shared memory, behind this thread's back.
 __device__ __forceinline__ void copy16(uint32_t dst, const uint8_t *src)
@@ -144,6 +118,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
 {
     constexpr int kStages = few_stages(kD), kSlot = slot_floats(kD), kTilesD = kD / 16;
     constexpr float kShift = kF16 ? 8.f : 0.f, kGrow = kF16 ? 7.f : 8.f;  // as for many rows
+    constexpr float kBack = 1.f / kOperandScale<kF16>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const PlanReq *reqs = plan_reqs(p.plan);
     const int window = static_cast<const PlanHeader *>(p.plan)->window;
@@ -168,27 +143,38 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
     constexpr int kRounds = kD / 16, kTail = kD / 128 ? 2 : 4;
     const bool in_tail = in_block < (1 << lanes_log2) / kTail;
     struct Fetch {
-        int id, key0, head;
+        int id, key0, seg;
         bool inside;
-    };
-    auto seg_key = [&](const FewSeg &s, int piece) {
-        return tile_key((piece - s.first) >> 2, s.r.a0, s.r.n1, s.r.b0) + ((piece & 3) * kFewKeys);
     };
     int ahead_seg = 0, issue_at = 0, take_at = 0;
     uint32_t hole_ring = 0;  // four bits per stage: parts that are not there
+    // of the unit that is being fetched: its first piece not fetched, where its window's gap is, the key of piece
+    // 0 before and behind that, its last token, its pages' ids and where this lane's blocks of them begin
+    int a_to = run0, a_gap = 0, a_key = 0, a_key2 = 0, a_end = 0;
+    const int32_t *a_table = nullptr;
+    const uint8_t *a_pages = nullptr, *f_pages = nullptr;
     auto fetch = [&](int piece) {
-        while (piece >= segs[ahead_seg].to)
-            ++ahead_seg;
-        const FewSeg &s = segs[ahead_seg];
-        Fetch f{-1, seg_key(s, piece), s.head, false};
+        if (piece >= a_to) {
+            while (piece >= segs[ahead_seg].to)
+                ++ahead_seg;
+            const FewSeg &s = segs[ahead_seg];
+            a_to = s.to;
+            a_gap = s.first + 4 * s.r.n1;
+            a_key = s.r.a0 * kBN - kFewKeys * s.first;
+            a_key2 = (s.r.b0 - s.r.n1) * kBN - kFewKeys * s.first;
+            a_end = s.r.L + s.r.n;
+            a_table = p.table + (size_t)s.r.b * p.max_pages;
+            a_pages = (copies_v ? p.v_pages : p.k_pages) + s.head * p.head_stride + 16 * in_block;
+        }
+        Fetch f{-1, (piece < a_gap ? a_key : a_key2) + kFewKeys * piece, ahead_seg, false};
         const int slot = f.key0 + part_key, at = slot >> p.page_log2;
-        f.inside = slot < s.r.L + s.r.n;
+        f.inside = slot < a_end;
         if (f.inside && at < p.max_pages)
-            f.id = p.table[(size_t)s.r.b * p.max_pages + at];
+            f.id = a_table[at];
+        f_pages = a_pages;
         return f;
     };
-    auto report_hole = [&](int slot) {
-        const PlanReq &r = segs[ahead_seg].r;
+    auto report_hole = [&](int slot, const PlanReq &r) {
         const int past = slot + (1 << part_log2);
         const int lo_min = window > 0 ? max(r.begin, r.L - window + 1) : r.begin;
         if (past > lo_min || (window > 0 && past > r.begin && slot < min(r.far_end, r.L)))
@@ -205,8 +191,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
     auto issue = [&](const Fetch &f) {
         const bool there = f.inside && f.id >= 0 && f.id < p.n_pages;
         if (there) {
-            const uint8_t *src = (copies_v ? p.v_pages : p.k_pages) + f.id * p.page_stride + f.head * p.head_stride +
-                                 16 * in_block;
+            const uint8_t *src = f_pages + ((unsigned long long)(unsigned)f.id * p.page_units << 4);
             const uint32_t to = copy_to + issue_at * FewSmem<kD>::kStage;
             if (part_log2 == 4) {
                 copy_block(std::integral_constant<int, 3>{}, to, src, src + kRounds * 128);
@@ -225,7 +210,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
             for (int x = 0; x < kFewKeys >> part_log2; ++x)
                 hole_ring |= ((missing >> (x << lanes_log2)) & 1u) << (4 * issue_at + x);
             if (f.inside && !there && !copies_v && in_block == 0)
-                report_hole(f.key0 + part_key);
+                report_hole(f.key0 + part_key, segs[f.seg].r);
         }
         issue_at = issue_at + 1 == kStages ? 0 : issue_at + 1;
     };
@@ -300,7 +285,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
         head0 = (int)((tile - reqs[request].tile_base) / reqs[request].T);
     }
     if (lane < 2)
-        sm.part[warp][lane] = FewPart{kNoUnit, 0, 0, 0, 0, 0, 0};
+        sm.part[warp][lane] = FewPart{kNoUnit, 0, 0, 0, 0, 0};
     float o[kTilesD][kN][4];
     float m[kN][2], l[kN][2];  // of columns 8 n + 2 t and the one after it; l: this thread's keys
     bool last_here = false;    // o, m and l are the run's last part
@@ -336,6 +321,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
         // the ring filled, the next page looked up
         issue_at = take_at = 0;
         ahead_seg = 0;
+        a_to = piece;
         int next = piece;
         Fetch ahead = fetch(next);
         auto refill = [&] {  // one group of copies each time, an empty one at the end
@@ -356,6 +342,9 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
             const int far = window > 0 ? min(seg.r.far_end, L) : begin;
             const int lo_min = window > 0 ? max(begin, L - window + 1) : begin;
             const int lo_max = window > 0 ? lo_min + kMaxNodes : begin;  // past any row's
+            const int gap = seg.first + 4 * seg.r.n1, to = seg.to;
+            const int key_a = seg.r.a0 * kBN - kFewKeys * seg.first;
+            const int key_b = (seg.r.b0 - seg.r.n1) * kBN - kFewKeys * seg.first;
             // queries of columns g (and 8 + g) in the order of the keys' elements
             uint32_t q[kD / 16][kN][2];
 #pragma unroll
@@ -378,12 +367,12 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                     o[j][n][0] = o[j][n][1] = o[j][n][2] = o[j][n][3] = 0.f;
             }
 
-            for (; piece < seg.to; ++piece) {
+            for (; piece < to; ++piece) {
                 if (p.expire_wait)
                     ok = ok && warp_agrees(mbar_wait_bounded(never_bar, 0, abort_flag, p.status));
                 copies_wait<kStages - 1>();
                 __syncwarp();
-                const int key0 = seg_key(seg, piece);
+                const int key0 = (piece < gap ? key_a : key_b) + kFewKeys * piece;
                 const uint32_t base = ring_a + take_at * FewSmem<kD>::kStage;
                 const uint32_t holes = (hole_ring >> (4 * take_at)) & 15u;
                 take_at = take_at + 1 == kStages ? 0 : take_at + 1;
@@ -399,7 +388,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         uint32_t w[2][kD / 32];
-                        Scale<kF16> sc[2];
+                        OperandScale<kF16> sc[2];
 #pragma unroll
                         for (int a = 0; a < 2; ++a) {
                             const uint32_t c = base + k_code + a * code8 + b * code16;
@@ -413,20 +402,20 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                             float f = scale_of(lds8(base + k_scale + a * scale8 + b * scale16));
                             if constexpr (masked)
                                 f = there(key_k + 8 * a + 16 * b) ? f : 0.f;
-                            sc[a] = scale_pair<kF16>(f, f);
+                            sc[a] = operand_scale<kF16>(f, f);
                         }
 #pragma unroll
-                        for (int i = 0; i < kD / 32; ++i)
+                        for (int i = 0; i < kD / 32; ++i) {
+                            uint32_t x[4], y[4];
+                            dequant_four<kF16>(w[0][i], sc[0], x);
+                            dequant_four<kF16>(w[1][i], sc[1], y);
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const uint32_t a0 = dequant_pair<kF16>(w[0][i] >> (8 * h), sc[0]);
-                                const uint32_t a1 = dequant_pair<kF16>(w[1][i] >> (8 * h), sc[1]);
-                                const uint32_t a2 = dequant_pair<kF16>(w[0][i] >> (8 * h + 4), sc[0]);
-                                const uint32_t a3 = dequant_pair<kF16>(w[1][i] >> (8 * h + 4), sc[1]);
+                            for (int h = 0; h < 2; ++h)
 #pragma unroll
                                 for (int n = 0; n < kN; ++n)
-                                    mma_16x8x16<kF16>(s[b][n], a0, a1, a2, a3, q[2 * i + h][n][0], q[2 * i + h][n][1]);
-                            }
+                                    mma_16x8x16<kF16>(s[b][n], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1],
+                                                      q[2 * i + h][n][0], q[2 * i + h][n][1]);
+                        }
                     }
                     // scores: element c of s[b][n] is key 16 b + 8 (c / 2) + key_k, column 8 n + 2 t + c % 2
                     auto visible = [&](int slot, const FewRow &r) {
@@ -559,7 +548,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         uint32_t v[2][2][kD / 64];  // [keys 0-7, 8-15][first key, second][8 codes each]
-                        Scale<kF16> sc[2];
+                        OperandScale<kF16> sc[2];
 #pragma unroll
                         for (int a = 0; a < 2; ++a) {
                             float f[2];
@@ -576,7 +565,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                                 if constexpr (masked)
                                     f[x] = looked_at(key_v + 2 * x + 8 * a + 16 * b) ? f[x] : 0.f;
                             }
-                            sc[a] = scale_pair<kF16>(f[0], f[1]);
+                            sc[a] = operand_scale<kF16>(f[0], f[1]);
                         }
 #pragma unroll
                         for (int i = 0; i < kD / 64; ++i)
@@ -584,18 +573,15 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                             for (int h = 0; h < 2; ++h) {
                                 // four elements of two keys
                                 const uint32_t sel = h ? 0x7632 : 0x5410;
-                                const uint32_t u0 = __byte_perm(v[0][0][i], v[0][1][i], sel);
-                                const uint32_t u1 = __byte_perm(v[1][0][i], v[1][1][i], sel);
+                                uint32_t x[4], y[4];
+                                dequant_four<kF16>(__byte_perm(v[0][0][i], v[0][1][i], sel), sc[0], x);
+                                dequant_four<kF16>(__byte_perm(v[1][0][i], v[1][1][i], sel), sc[1], y);
 #pragma unroll
-                                for (int x = 0; x < 2; ++x) {
-                                    const uint32_t a0 = dequant_pair<kF16>(u0 >> (8 * x), sc[0]);
-                                    const uint32_t a1 = dequant_pair<kF16>(u0 >> (8 * x + 4), sc[0]);
-                                    const uint32_t a2 = dequant_pair<kF16>(u1 >> (8 * x), sc[1]);
-                                    const uint32_t a3 = dequant_pair<kF16>(u1 >> (8 * x + 4), sc[1]);
+                                for (int e = 0; e < 2; ++e)
 #pragma unroll
                                     for (int n = 0; n < kN; ++n)
-                                        mma_16x8x16<kF16>(o[4 * i + 2 * h + x][n], a0, a1, a2, a3, w[b][n][0], w[b][n][1]);
-                                }
+                                        mma_16x8x16<kF16>(o[4 * i + 2 * h + e][n], x[2 * e], x[2 * e + 1], y[2 * e],
+                                                          y[2 * e + 1], w[b][n][0], w[b][n][1]);
                             }
                     }
                 };
@@ -627,7 +613,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                         const long long at = row_at(seg, 8 * n + 2 * t + c);
                         if (at < 0 || !known || !ok)
                             continue;
-                        const float lc = l[n][c], inv = lc == 0.f ? 0.f : 1.f / lc;  // a NaN stays one
+                        const float lc = l[n][c], inv = lc == 0.f ? 0.f : kBack / lc;  // a NaN stays one
                         uint32_t w[kTilesD];
 #pragma unroll
                         for (int j = 0; j < kTilesD; ++j)
@@ -643,8 +629,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
             }
             // a part: at most two of a run, the second at its end
             if (lane == 0)
-                sm.part[warp][n_parts] =
-                    FewPart{seg.first, begins, ends, ok, seg.head, seg.r.row0, known ? seg.r.n : 0};
+                sm.part[warp][n_parts] = FewPart{seg.first, begins, ends, seg.head, seg.r.row0, known ? seg.r.n : 0};
             if (g == 0) {
 #pragma unroll
                 for (int n = 0; n < kN; ++n)
@@ -732,7 +717,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                 const long long at = row_at(s, 8 * fn + 2 * t + c);
                 if (at < 0 || stop)
                     continue;
-                const float inv = sum[c] == 0.f ? 0.f : 1.f / sum[c];
+                const float inv = sum[c] == 0.f ? 0.f : kBack / sum[c];
                 *reinterpret_cast<uint32_t *>(p.out + at * kD + g * (kD / 8) + 2 * fj) =
                     pack<kF16>((c ? a.y : a.x) * inv, (c ? a.w : a.z) * inv);
                 if (p.lse && fj == 0 && g == 0)
@@ -759,7 +744,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
         for (int c = 0; c < 2; ++c) {
             const int col = 8 * fn + 2 * t + c;
             *reinterpret_cast<float2 *>(slot + col * kD + g * (kD / 8) + 2 * fj) =
-                c ? make_float2(kept[i].y, kept[i].w) : make_float2(kept[i].x, kept[i].z);
+                c ? make_float2(kept[i].y * kBack, kept[i].w * kBack) : make_float2(kept[i].x * kBack, kept[i].z * kBack);
             if (fj == 0 && g == 0) {
                 slot[128 * kD + col] = kept_m[i][c];
                 slot[128 * kD + 128 + col] = kept_l[i][c];

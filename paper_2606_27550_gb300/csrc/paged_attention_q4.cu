@@ -18,9 +18,9 @@ extern "C" tb_status paged_tree_attention_q4(const tb_bank *bank, const tb_reque
         const long long off = (long long)layer * pages->layer_stride;
         a.k_pages = static_cast<const uint8_t *>(pages->k) + off;
         a.v_pages = static_cast<const uint8_t *>(pages->v) + off;
-        a.page_stride = pages->page_stride;
+        a.page_units = (uint32_t)(pages->page_stride / 16);
         a.head_stride = pages->head_stride;
-        return nullptr;
+        return pages->page_stride / 16 <= 0xffffffffll ? nullptr : "a page stride of 2^36 bytes or more";
     };
     return attend<true>(bank, req, pages, layer, plan, plan_bytes, q, n_rows, n_q_heads, scale, softcap, slopes, out,
                         lse, workspace, workspace_bytes, stream, "paged_tree_attention_q4", check_pages_q4, fill);

@@ -103,4 +103,62 @@ __device__ __forceinline__ uint32_t dequant_pair(uint32_t w, const Scale<kF16> &
     }
 }
 
+// ---- for the products of the attention: all the elements times one power of two
+//
+// In bf16 the numbers with bits 0 to 7 are k 2^-133, below the smallest normal number and
+// one binade above it.  So the code in bits 0 to 3 is c 2^-133 and the one in bits 4 to 7
+// 16 c 2^-133 as they stand, and an fma with s 2^113 (s 2^109) and -8 s 2^-20 makes
+// (c - 8) s 2^-20 of them, exactly: one shift for four codes.  fp16 has no room for that:
+// c - 8 first, then s.
+template <bool kF16>
+constexpr float kOperandScale = kF16 ? 1.f : 0x1p-20f;
+
+template <bool kF16>
+struct OperandScale {
+    uint32_t low, high, bias;  // fp16: low alone, s
+};
+
+template <bool kF16>
+__device__ __forceinline__ OperandScale<kF16> operand_scale(float lo, float hi)
+{
+    OperandScale<kF16> r;
+    if constexpr (kF16) {
+        r.low = pack_pair<true>(lo, hi);
+        r.high = r.bias = 0;
+    } else {
+        const uint32_t s = pack_pair<false>(lo, hi);
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r.low) : "r"(s), "r"(0x78007800u));   // 2^113
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r.high) : "r"(s), "r"(0x76007600u));  // 2^109
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r.bias) : "r"(s), "r"(0xb700b700u));  // -2^-17
+    }
+    return r;
+}
+
+// The elements whose codes stand at bits 0, 4, 8 and 12 of both halves of w.
+template <bool kF16>
+__device__ __forceinline__ void dequant_four(uint32_t w, const OperandScale<kF16> &s, uint32_t (&e)[4])
+{
+    const uint32_t v = w >> 8;
+    if constexpr (kF16) {
+        uint32_t x[4];
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[0]) : "r"(w), "r"(0x000f000fu), "r"(0x64006400u));
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[1]) : "r"(w), "r"(0x00f000f0u), "r"(0x64006400u));
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[2]) : "r"(v), "r"(0x000f000fu), "r"(0x64006400u));
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x[3]) : "r"(v), "r"(0x00f000f0u), "r"(0x64006400u));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i % 2 == 0)
+                asm("add.rn.f16x2 %0, %1, %2;" : "=r"(x[i]) : "r"(x[i]), "r"(0xe408e408u));  // 1024 + c - 1032
+            else
+                asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[i]) : "r"(x[i]), "r"(0x2c002c00u), "r"(0xd480d480u));  // / 16 - 72
+            asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(e[i]) : "r"(x[i]), "r"(s.low));
+        }
+    } else {
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(e[0]) : "r"(w & 0x000f000fu), "r"(s.low), "r"(s.bias));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(e[1]) : "r"(w & 0x00f000f0u), "r"(s.high), "r"(s.bias));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(e[2]) : "r"(v & 0x000f000fu), "r"(s.low), "r"(s.bias));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(e[3]) : "r"(v & 0x00f000f0u), "r"(s.high), "r"(s.bias));
+    }
+}
+
 }  // namespace tv
