@@ -73,10 +73,10 @@ struct FewSmem {
     float m[kFewWarps][2][kFewRows], l[kFewWarps][2][kFewRows];
 };
 
-// 16 bytes into shared memory, behind this thread's back.
-__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t *src)
+// 16 bytes into shared memory, behind this thread's back: n of them (0 or 16) from src, else zeros.
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t *src, uint32_t n)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
 __device__ __forceinline__ void copies_end()  // of a group
 {
@@ -129,8 +129,8 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
     FewSeg *segs = sm.seg[warp];
     FewRow *rows = sm.row[warp];
 
-    // ---- a warp's copies.  A piece's blocks are parts of min(page_size, 32) keys, first K's, then V's, each as it
-    // lies in its page (of a larger page: its codes, then its scales); 32, 16, 8 or 4 lanes copy a block.
+    // ---- a warp's copies.  A piece's blocks are parts of min(page_size, 32) keys, first K's, then V's; 16, 8 or 4
+    // lanes copy a block, its codes in kD / 16 rounds and its scales in one more, to where those of all 32 keys lie.
     const int part_log2 = min(p.page_log2, 5);
     const int block_log2 = 1 + 5 - part_log2;  // blocks of a piece
     const int lanes_log2 = 5 - block_log2;     // lanes of a block
@@ -138,16 +138,18 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
     const bool copies_v = block >> (block_log2 - 1);
     const int part_key = (block & ((1 << (block_log2 - 1)) - 1)) << part_log2;
     const uint32_t ring_a = smem_u32(ring);
-    const uint32_t copy_to = ring_a + (copies_v ? kFewKeys * row_bytes(kD) : 0) + part_key * row_bytes(kD) + 16 * in_block;
-    // its last round, of half or a quarter as many lanes; in a large page the scales
-    constexpr int kRounds = kD / 16, kTail = kD / 128 ? 2 : 4;
-    const bool in_tail = in_block < (1 << lanes_log2) / kTail;
+    constexpr int kScales = kFewKeys * code_bytes(kD), kV = kFewKeys * row_bytes(kD);  // in a stage
+    const uint32_t copy_to = ring_a + (copies_v ? kV : 0) + part_key * code_bytes(kD) + 16 * in_block;
+    const uint32_t scales_to = ring_a + (copies_v ? kV : 0) + kScales + part_key * scale_bytes(kD) + 16 * in_block;
+    constexpr int kRounds = kD / 16;
+    const bool in_scales = in_block < (scale_bytes(kD) << part_log2) / 16;
+    const int in_page = p.page_log2 > 5 ? (1 << p.page_log2) - 1 : 0;
+    const long long scales_from = (long long)code_bytes(kD) << p.page_log2;
     struct Fetch {
         int id, key0, seg;
         bool inside;
     };
     int ahead_seg = 0, issue_at = 0, take_at = 0;
-    uint32_t hole_ring = 0;  // four bits per stage: parts that are not there
     // of the unit that is being fetched: its first piece not fetched, where its window's gap is, the key of piece
     // 0 before and behind that, its last token, its pages' ids and where this lane's blocks of them begin
     int a_to = run0, a_gap = 0, a_key = 0, a_key2 = 0, a_end = 0;
@@ -170,7 +172,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
         const int slot = f.key0 + part_key, at = slot >> p.page_log2;
         f.inside = slot < a_end;
         if (f.inside && at < p.max_pages)
-            f.id = a_table[at];
+            f.id = a_table[at];  // (looked up here, used a piece later)
         f_pages = a_pages;
         return f;
     };
@@ -180,54 +182,41 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
         if (past > lo_min || (window > 0 && past > r.begin && slot < min(r.far_end, r.L)))
             atomicOr(p.status, kStatusBounds);
     };
-    auto copy_block = [&](auto log2, uint32_t to, const uint8_t *src, const uint8_t *tail) {
+    auto copy_codes = [&](auto log2, uint32_t to, const uint8_t *src, uint32_t n) {
         constexpr int kStep = 16 << decltype(log2)::value;
 #pragma unroll
         for (int i = 0; i < kRounds; ++i)
-            copy16(to + i * kStep, src + i * kStep);
-        if (in_tail)
-            copy16(to + kRounds * kStep, tail);
+            copy16(to + i * kStep, src + i * kStep, n);
     };
+    // Past the request's end and where a page is not there: zeros, whose scales make every element 0.
     auto issue = [&](const Fetch &f) {
-        const bool there = f.inside && f.id >= 0 && f.id < p.n_pages;
-        if (there) {
-            const uint8_t *src = f_pages + ((unsigned long long)(unsigned)f.id * p.page_units << 4);
-            const uint32_t to = copy_to + issue_at * FewSmem<kD>::kStage;
-            if (part_log2 == 4) {
-                copy_block(std::integral_constant<int, 3>{}, to, src, src + kRounds * 128);
-            } else if (part_log2 == 3) {
-                copy_block(std::integral_constant<int, 2>{}, to, src, src + kRounds * 64);
-            } else {
-                const int at = f.key0 & ((1 << p.page_log2) - 1);
-                const uint8_t *tail = src + ((long long)code_bytes(kD) << p.page_log2) + at * scale_bytes(kD);
-                copy_block(std::integral_constant<int, 4>{}, to, src + at * code_bytes(kD), tail);
-            }
-        }
+        const bool there = f.inside && (unsigned)f.id < (unsigned)p.n_pages;
+        const uint32_t n = there ? 16 : 0;
+        const uint8_t *src = f_pages + ((unsigned long long)(there ? (unsigned)f.id : 0u) * p.page_units << 4);
+        const int at = f.key0 & in_page;  // in a page of more than 32 slots
+        const uint8_t *codes = src + at * code_bytes(kD);
+        const uint32_t stage = issue_at * FewSmem<kD>::kStage;
+        if (in_scales)
+            copy16(scales_to + stage, src + scales_from + at * scale_bytes(kD), n);
+        if (part_log2 == 4)
+            copy_codes(std::integral_constant<int, 3>{}, copy_to + stage, codes, n);
+        else if (part_log2 == 3)
+            copy_codes(std::integral_constant<int, 2>{}, copy_to + stage, codes, n);
+        else
+            copy_codes(std::integral_constant<int, 4>{}, copy_to + stage, codes, n);
         copies_end();
-        const uint32_t missing = __ballot_sync(0xffffffffu, f.inside && !there && !copies_v);
-        hole_ring &= ~(15u << (4 * issue_at));
-        if (missing) {
-            for (int x = 0; x < kFewKeys >> part_log2; ++x)
-                hole_ring |= ((missing >> (x << lanes_log2)) & 1u) << (4 * issue_at + x);
-            if (f.inside && !there && !copies_v && in_block == 0)
-                report_hole(f.key0 + part_key, segs[f.seg].r);
-        }
+        if (f.inside && !there && !copies_v && in_block == 0)
+            report_hole(f.key0 + part_key, segs[f.seg].r);
         issue_at = issue_at + 1 == kStages ? 0 : issue_at + 1;
     };
 
     // ---- where this thread's keys and values lie in a piece.  Row i of a product's 16 keys is key i with its
     // lowest two bits swapped, so that the four keys which V's loads take at once lie in different banks.
     const int key_k = (g & 4) | ((g & 1) << 1) | ((g >> 1) & 1), key_v = (t >> 1) * 4 + (t & 1);
-    const int per_part = 1 << part_log2;
-    const int code8 = part_log2 == 3 ? 8 * row_bytes(kD) : 8 * code_bytes(kD);
-    const int code16 = part_log2 == 5 ? 16 * code_bytes(kD) : 16 * row_bytes(kD);
-    const int scale8 = part_log2 == 3 ? 8 * row_bytes(kD) : 8 * scale_bytes(kD);
-    const int scale16 = part_log2 == 5 ? 16 * scale_bytes(kD) : 16 * row_bytes(kD);
     const int k_code = key_k * code_bytes(kD) + t * (kD / 8);
-    const int k_scale = per_part * code_bytes(kD) + key_k * scale_bytes(kD) + t * (kD / 4) / kGroup;
-    const int v_code = kFewKeys * row_bytes(kD) + key_v * code_bytes(kD) + g * (kD / 16);
-    const int v_scale = kFewKeys * row_bytes(kD) + per_part * code_bytes(kD) + key_v * scale_bytes(kD) +
-                        g * (kD / 8) / kGroup;
+    const int k_scale = kScales + key_k * scale_bytes(kD) + t * (kD / 4) / kGroup;
+    const int v_code = kV + key_v * code_bytes(kD) + g * (kD / 16);
+    const int v_scale = kV + kScales + key_v * scale_bytes(kD) + g * (kD / 8) / kGroup;
 
     // where row r of a unit goes, (row, query head); -1: no such row
     auto row_at = [&](const FewSeg &s, int r) {
@@ -374,15 +363,13 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                 __syncwarp();
                 const int key0 = (piece < gap ? key_a : key_b) + kFewKeys * piece;
                 const uint32_t base = ring_a + take_at * FewSmem<kD>::kStage;
-                const uint32_t holes = (hole_ring >> (4 * take_at)) & 15u;
                 take_at = take_at + 1 == kStages ? 0 : take_at + 1;
                 const auto work = [&](auto is_masked) {
                     constexpr bool masked = decltype(is_masked)::value;
-                    // a key's or value's scale: 0 in a hole, of a value also where no row looks
-                    auto there = [&](int key) { return !((holes >> (key >> part_log2)) & 1u); };
+                    // whether some row looks at a value: the others may be anything
                     auto looked_at = [&](int key) {
                         const int slot = key0 + key;
-                        return there(key) && slot < end && slot >= begin && (slot >= lo_min || slot < far);
+                        return slot < end && slot >= begin && (slot >= lo_min || slot < far);
                     };
                     float s[2][kN][4] = {};
 #pragma unroll
@@ -391,7 +378,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                         OperandScale<kF16> sc[2];
 #pragma unroll
                         for (int a = 0; a < 2; ++a) {
-                            const uint32_t c = base + k_code + a * code8 + b * code16;
+                            const uint32_t c = base + k_code + (8 * a + 16 * b) * code_bytes(kD);
                             if constexpr (kD == 128) {
                                 const uint4 x = lds128(c);
                                 w[a][0] = x.x, w[a][1] = x.y, w[a][2] = x.z, w[a][3] = x.w;
@@ -399,9 +386,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                                 const uint2 x = lds64(c);
                                 w[a][0] = x.x, w[a][1] = x.y;
                             }
-                            float f = scale_of(lds8(base + k_scale + a * scale8 + b * scale16));
-                            if constexpr (masked)
-                                f = there(key_k + 8 * a + 16 * b) ? f : 0.f;
+                            const float f = scale_of(lds8(base + k_scale + (8 * a + 16 * b) * scale_bytes(kD)));
                             sc[a] = operand_scale<kF16>(f, f);
                         }
 #pragma unroll
@@ -554,14 +539,14 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                             float f[2];
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
-                                const uint32_t c = base + v_code + 2 * x * code_bytes(kD) + a * code8 + b * code16;
+                                const uint32_t c = base + v_code + (2 * x + 8 * a + 16 * b) * code_bytes(kD);
                                 if constexpr (kD == 128) {
                                     const uint2 y = lds64(c);
                                     v[a][x][0] = y.x, v[a][x][1] = y.y;
                                 } else {
                                     v[a][x][0] = lds32(c);
                                 }
-                                f[x] = scale_of(lds8(base + v_scale + 2 * x * scale_bytes(kD) + a * scale8 + b * scale16));
+                                f[x] = scale_of(lds8(base + v_scale + (2 * x + 8 * a + 16 * b) * scale_bytes(kD)));
                                 if constexpr (masked)
                                     f[x] = looked_at(key_v + 2 * x + 8 * a + 16 * b) ? f[x] : 0.f;
                             }
@@ -585,7 +570,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                             }
                     }
                 };
-                if (key0 + kFewKeys > L || key0 < lo_max || holes) {
+                if (key0 + kFewKeys > L || key0 < lo_max) {
                     if (key0 < end)
                         work(std::true_type{});
                 } else {
