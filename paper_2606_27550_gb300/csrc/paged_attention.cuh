@@ -467,8 +467,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             // the requests of this CTA's range follow one another
             __syncwarp();
             const PlanReq *all = plan_reqs(p.plan);
-            int rows = 0;
-            for (int i0 = s_cta.idx; s_cta.t0 < s_cta.t1; i0 += 32) {
+            int rows = s_cta.req.n * p.group - s_cta.rb * 128;
+            const bool several = s_cta.req.tile_base + (long long)s_cta.req.T * p.Hkv < s_cta.t1;
+            for (int i0 = s_cta.idx; several; i0 += 32) {
                 const int i = i0 + lane;
                 const bool in = i < p.batch && all[i].tile_base < s_cta.t1;
                 const uint32_t run = __ballot_sync(0xffffffffu, in);

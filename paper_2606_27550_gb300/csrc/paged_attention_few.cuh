@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kFewRows = 16;
 constexpr int kFewKeys = 32;  // of a piece
-constexpr int kFewSegs = 16;  // units that a warp lays out at a time
+constexpr int kFewSegs = 8;  // units that a warp lays out at a time
 constexpr int kFewWarps = kThreads / 32;
 
 constexpr int few_stages(int d)
@@ -55,6 +55,7 @@ struct FewRow {
 struct FewPart {
     int unit;  // its first piece; parts of one unit follow one another
     int begins, ends;  // whether the unit does, in this part
+    int last;          // of its run: in shared memory
     int head;
     int row0, n;  // the request's rows; n 0: none to write
 };
@@ -67,6 +68,7 @@ struct FewSmem {
         uint8_t ring[kFewWarps][kRing];
         float4 last[kFewWarps][2 * kD / 16][32];  // O^T of the runs' last parts, fragment by fragment
     };
+    uint2 query[kFewWarps][kD / 8][32];  // with 16 columns: the queries as operands (8 stay in registers)
     FewRow row[kFewWarps][kFewRows];
     FewSeg seg[kFewWarps][kFewSegs];
     FewPart part[kFewWarps][2];
@@ -263,18 +265,25 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
     int request = cta.idx, head0 = 0;
     if (run0 < run1) {
         const long long tile = t0 + (run0 >> 2);
-        for (int i0 = cta.idx;; i0 += 32) {
-            const int i = i0 + lane;
-            const uint32_t before = __ballot_sync(0xffffffffu, i < p.batch && reqs[i].tile_base <= tile);
-            const int n = before == 0xffffffffu ? 32 : __ffs((int)~before) - 1;
-            request = i0 + n - 1;
-            if (n < 32)
-                break;
+        long long base = cta.req.tile_base;
+        int T = cta.req.T;
+        if (tile >= base + (long long)T * p.Hkv) {  // not of the request that the CTA begins in
+            for (int i0 = cta.idx;; i0 += 32) {
+                const int i = i0 + lane;
+                const uint32_t before = __ballot_sync(0xffffffffu, i < p.batch && reqs[i].tile_base <= tile);
+                const int n = before == 0xffffffffu ? 32 : __ffs((int)~before) - 1;
+                request = i0 + n - 1;
+                if (n < 32)
+                    break;
+            }
+            base = reqs[request].tile_base;
+            T = reqs[request].T;
         }
-        head0 = (int)((tile - reqs[request].tile_base) / reqs[request].T);
+        const long long in = tile - base;
+        head0 = (unsigned long long)in <= 0xffffffffull ? (int)((uint32_t)in / (uint32_t)T) : (int)(in / T);
     }
     if (lane < 2)
-        sm.part[warp][lane] = FewPart{kNoUnit, 0, 0, 0, 0, 0};
+        sm.part[warp][lane] = FewPart{kNoUnit, 0, 0, 0, 0, 0, 0};
     float o[kTilesD][kN][4];
     float m[kN][2], l[kN][2];  // of columns 8 n + 2 t and the one after it; l: this thread's keys
     bool last_here = false;    // o, m and l are the run's last part
@@ -287,7 +296,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
             FewSeg s{};
             bool in = lane < kFewSegs && i < p.batch;
             if (in) {
-                s.r = reqs[i];
+                s.r = i == cta.idx ? cta.req : reqs[i];
                 s.head = u % p.Hkv;
                 const long long first = s.r.tile_base + (long long)s.head * s.r.T - t0;
                 in = first < (run1 + 3) / 4;
@@ -335,7 +344,9 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
             const int key_a = seg.r.a0 * kBN - kFewKeys * seg.first;
             const int key_b = (seg.r.b0 - seg.r.n1) * kBN - kFewKeys * seg.first;
             // queries of columns g (and 8 + g) in the order of the keys' elements
-            uint32_t q[kD / 16][kN][2];
+            constexpr bool kKept = kN == 1;  // 16 columns: 32 registers that the output needs
+            uint32_t q[kKept ? kD / 16 : 1][2];
+            const uint32_t q_at = smem_u32(sm.query[warp]) + 8 * lane;
 #pragma unroll
             for (int n = 0; n < kN; ++n) {
                 const long long at = row_at(seg, 8 * n + g);
@@ -343,10 +354,21 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
 #pragma unroll
                 for (int i = 0; i < kD / 32; ++i) {
                     const uint4 x = code_order(at >= 0 ? src[i] : make_uint4(0, 0, 0, 0));
-                    q[2 * i][n][0] = x.x, q[2 * i][n][1] = x.y;
-                    q[2 * i + 1][n][0] = x.z, q[2 * i + 1][n][1] = x.w;
+                    if constexpr (kKept) {
+                        q[2 * i][0] = x.x, q[2 * i][1] = x.y;
+                        q[2 * i + 1][0] = x.z, q[2 * i + 1][1] = x.w;
+                    } else {
+                        sm.query[warp][4 * i + n][lane] = make_uint2(x.x, x.y);
+                        sm.query[warp][4 * i + 2 + n][lane] = make_uint2(x.z, x.w);
+                    }
                 }
             }
+            const auto query = [&](int step, int n) {
+                if constexpr (kKept)
+                    return make_uint2(q[step][0], q[step][1]);
+                else
+                    return lds64(q_at + (2 * step + n) * 256);
+            };
             const bool known = stage(seg);
 #pragma unroll
             for (int n = 0; n < kN; ++n) {
@@ -397,9 +419,10 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
 #pragma unroll
                             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                                for (int n = 0; n < kN; ++n)
-                                    mma_16x8x16<kF16>(s[b][n], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1],
-                                                      q[2 * i + h][n][0], q[2 * i + h][n][1]);
+                                for (int n = 0; n < kN; ++n) {
+                                    const uint2 z = query(2 * i + h, n);
+                                    mma_16x8x16<kF16>(s[b][n], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1], z.x, z.y);
+                                }
                         }
                     }
                     // scores: element c of s[b][n] is key 16 b + 8 (c / 2) + key_k, column 8 n + 2 t + c % 2
@@ -614,7 +637,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
             }
             // a part: at most two of a run, the second at its end
             if (lane == 0)
-                sm.part[warp][n_parts] = FewPart{seg.first, begins, ends, seg.head, seg.r.row0, known ? seg.r.n : 0};
+                sm.part[warp][n_parts] = FewPart{seg.first, begins, ends, seg.to == run1, seg.head, seg.r.row0, known ? seg.r.n : 0};
             if (g == 0) {
 #pragma unroll
                 for (int n = 0; n < kN; ++n)
@@ -624,7 +647,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                         sm.l[warp][n_parts][8 * n + 2 * t + c] = l[n][c];
                     }
             }
-            if (n_parts == 0) {
+            if (seg.to < run1) {
                 float4 *to = reinterpret_cast<float4 *>(p.part + (size_t)blockIdx.x * 2 * kSlot) + warp * kTilesD * kN * 32;
 #pragma unroll
                 for (int j = 0; j < kTilesD; ++j)
@@ -632,7 +655,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                     for (int n = 0; n < kN; ++n)
                         to[(j * kN + n) * 32 + lane] = make_float4(o[j][n][0], o[j][n][1], o[j][n][2], o[j][n][3]);
             } else {
-                last_here = true;
+                last_here = true;  // the last of the run
             }
             ++n_parts;
         }
@@ -657,7 +680,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
     const float4 *firsts = reinterpret_cast<const float4 *>(p.part + (size_t)blockIdx.x * 2 * kSlot);
     float4 kept[2];
     float kept_m[2][2], kept_l[2][2];
-    int kept_slot[2] = {-1, -1}, n_kept = 0;
+    bool keep[2] = {false, false};
     for (int x = 0; x < 2 * kFewWarps;) {
         const FewPart head = sm.part[x >> 1][x & 1];
         int y = x + 1;
@@ -667,64 +690,69 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
         }
         while (y < 2 * kFewWarps && (sm.part[y >> 1][y & 1].unit == head.unit || sm.part[y >> 1][y & 1].unit == kNoUnit))
             ++y;
-        bool ends = false;
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        float M[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
         if (mine) {
+            bool ends = false;
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+            float M[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+            const int col0 = 8 * fn + 2 * t;
             for (int z = x; z < y; ++z)
                 if (sm.part[z >> 1][z & 1].unit == head.unit)
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
-                        M[c] = fmaxf(M[c], sm.m[z >> 1][z & 1][8 * fn + 2 * t + c]);
+                        M[c] = fmaxf(M[c], sm.m[z >> 1][z & 1][col0 + c]);
+#pragma unroll 4
             for (int z = x; z < y; ++z) {
                 const FewPart &part = sm.part[z >> 1][z & 1];
                 if (part.unit != head.unit)
                     continue;
                 ends = part.ends;
-                const float4 v = z & 1 ? sm.last[z >> 1][frag / 32][lane]
-                                       : __ldcg(firsts + (z >> 1) * kTilesD * kN * 32 + frag);
+                const float4 v = part.last ? sm.last[z >> 1][frag / 32][lane]
+                                           : __ldcg(firsts + (z >> 1) * kTilesD * kN * 32 + frag);
                 float f[2];
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const float mz = sm.m[z >> 1][z & 1][8 * fn + 2 * t + c];
+                    const float mz = sm.m[z >> 1][z & 1][col0 + c];
                     f[c] = mz == -INFINITY ? 0.f : ex2_approx(mz - M[c]);
-                    sum[c] = fmaf(f[c], sm.l[z >> 1][z & 1][8 * fn + 2 * t + c], sum[c]);
+                    sum[c] = fmaf(f[c], sm.l[z >> 1][z & 1][col0 + c], sum[c]);
                 }
                 a.x = fmaf(f[0], v.x, a.x), a.y = fmaf(f[1], v.y, a.y);
                 a.z = fmaf(f[0], v.z, a.z), a.w = fmaf(f[1], v.w, a.w);
             }
-        }
-        if (mine && head.begins && ends) {
+            if (head.begins && ends) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                FewSeg s{};
-                s.head = head.head, s.r.n = head.n, s.r.row0 = head.row0;
-                const long long at = row_at(s, 8 * fn + 2 * t + c);
-                if (at < 0 || stop)
-                    continue;
-                const float inv = sum[c] == 0.f ? 0.f : kBack / sum[c];
-                *reinterpret_cast<uint32_t *>(p.out + at * kD + g * (kD / 8) + 2 * fj) =
-                    pack<kF16>((c ? a.y : a.x) * inv, (c ? a.w : a.z) * inv);
-                if (p.lse && fj == 0 && g == 0)
-                    p.lse[at] = sum[c] == 0.f ? -INFINITY : (M[c] + log2f(sum[c])) * kLn2;
+                for (int c = 0; c < 2; ++c) {
+                    FewSeg s{};
+                    s.head = head.head, s.r.n = head.n, s.r.row0 = head.row0;
+                    const long long at = row_at(s, col0 + c);
+                    if (at < 0 || stop)
+                        continue;
+                    const float inv = sum[c] == 0.f ? 0.f : kBack / sum[c];
+                    *reinterpret_cast<uint32_t *>(p.out + at * kD + g * (kD / 8) + 2 * fj) =
+                        pack<kF16>((c ? a.y : a.x) * inv, (c ? a.w : a.z) * inv);
+                    if (p.lse && fj == 0 && g == 0)
+                        p.lse[at] = sum[c] == 0.f ? -INFINITY : (M[c] + log2f(sum[c])) * kLn2;
+                }
+            } else {
+                // of the CTA's first tile on: slot 0, as for many rows
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (i == (head.unit <= 0 ? 0 : 1)) {
+                        keep[i] = true;
+                        kept[i] = a;
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+                            kept_m[i][c] = M[c], kept_l[i][c] = sum[c];
+                    }
             }
-        } else if (mine && n_kept < 2) {
-            // of the CTA's first tile on: slot 0, as for many rows
-            kept_slot[n_kept] = head.unit <= 0 ? 0 : 1;
-            kept[n_kept] = a;
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-                kept_m[n_kept][c] = M[c], kept_l[n_kept][c] = sum[c];
-            ++n_kept;
         }
         x = y;
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        if (!mine || kept_slot[i] < 0)
+        if (!keep[i])
             continue;
-        float *slot = p.part + ((size_t)blockIdx.x * 2 + kept_slot[i]) * kSlot;
+        float *slot = p.part + ((size_t)blockIdx.x * 2 + i) * kSlot;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int col = 8 * fn + 2 * t + c;
