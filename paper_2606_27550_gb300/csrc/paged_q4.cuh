@@ -34,36 +34,46 @@ __device__ __forceinline__ float scale_of(uint32_t byte)
     return __half2float(__ushort_as_half((unsigned short)(byte << 7)));
 }
 
-// The scale byte of a group whose largest magnitude has the bits `top`.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t top)
+// fl(x / n) for a number n of at most 4 significant bits and its rounded reciprocal: a product and one
+// correction.  y = fl(x inv) is x / n (1 + e) with |e| <= 2^-23, its remainder x - y n is a float, and y plus
+// remainder times inv is x / n but for e^2, 2^-46 of it, before the one rounding.  That cannot round
+// otherwise than x / n does: a midpoint between two floats has 25 bits, times n 29, so that x (24 bits) is
+// never n times a midpoint, and never nearer to one than 2^-29.
+__device__ __forceinline__ uint64_t quotient_two(uint64_t x, uint64_t minus_n, uint64_t inv)
 {
-    if (top >= 0x7f800000u)
-        return kNanScaleByte;
-    const float t = __fdiv_rn(__uint_as_float(top), 7.f);
-    // up to 4 significant bits; below 2^-14 (byte 8) up to a multiple of 2^-17
-    const uint32_t normal = ((__float_as_uint(t) + 0xfffffu) >> 20) - ((127 - 15) << 3);
-    const uint32_t b = t > 0x1p-14f ? normal : (uint32_t)ceilf(t * 0x1p17f);
-    return min(b, (uint32_t)kMaxScaleByte);
+    const uint64_t y = mul_two(x, inv);
+    return fma_two(fma_two(y, minus_n, x), inv, y);
 }
 
-// Codes of 8 elements, the first in the lowest 4 bits; inv = 1 / s rounded (0 where s is 0).
-__device__ __forceinline__ uint32_t quantize8(const float (&x)[8], float s, float inv)
+// The scale byte of a group whose largest magnitude is `top` (NaN if one of it is none).
+__device__ __forceinline__ uint32_t scale_byte(float top)
 {
-    // adding 1.5 * 2^23 + 8 leaves rint(y) + 8 in the low bits, ties to even
+    constexpr float kInv = 1.f / 7.f;
+    const float y = __fmul_rn(top, kInv), t = __fmaf_rn(__fmaf_rn(y, -7.f, top), kInv, y);  // as above
+    // up to 4 significant bits; below 2^-14 (byte 8) up to a multiple of 2^-17
+    uint32_t b = ((__float_as_uint(t) + 0xfffffu) >> 20) - ((127 - 15) << 3);
+    if (!(t > 0x1p-14f))
+        b = (uint32_t)ceilf(t * 0x1p17f);
+    return top < INFINITY ? min(b, (uint32_t)kMaxScaleByte) : (uint32_t)kNanScaleByte;
+}
+
+// Codes of 8 elements (pairs), the first in the lowest 4 bits; inv = 1 / s rounded (0 where s is 0).
+__device__ __forceinline__ uint32_t quantize8(const uint64_t (&x)[4], float s, float inv, bool clamp)
+{
+    // adding 1.5 * 2^23 + 8 leaves rint(y) + 8 in the low bits, ties to even; of a NaN, 15
     constexpr float kRound = 12582912.f + 8.f;
-    uint32_t w = 0;
+    uint32_t b[4];  // two codes each
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float y = fmaxf(fminf(x[i] * inv, 7.f), -7.f);
-        float f = __fadd_rn(y, kRound);
-        // x * inv is x / s but for its last bits: where those decide, the quotient itself
-        if (fabsf(fabsf(__fsub_rn(y, __fsub_rn(f, kRound))) - 0.5f) < 1e-5f && s > 0.f) {
-            y = fmaxf(fminf(__fdiv_rn(x[i], s), 7.f), -7.f);
-            f = __fadd_rn(y, kRound);
+    for (int i = 0; i < 4; ++i) {
+        uint64_t y = quotient_two(x[i], two(-s, -s), two(inv, inv));
+        if (clamp) {  // the scale is the largest one (or NaN, which gives 7)
+            const float2 f = halves(y);
+            y = two(fmaxf(fminf(f.x, 7.f), -7.f), fmaxf(fminf(f.y, 7.f), -7.f));
         }
-        w |= (__float_as_uint(f) & 15u) << (4 * i);
+        const float2 f = halves(add_two(y, two(kRound, kRound)));
+        b[i] = (__float_as_uint(f.y) << 4) + (__float_as_uint(f.x) & 15u);
     }
-    return w;
+    return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
 }
 
 // 16-bit pairs.  In bf16 128 + c is 0x4300 | c, and (128 + c) s - 136 s is (c - 8) s,

@@ -103,18 +103,27 @@ __device__ float2 cos_sin(uint64_t turn)
     }
 }
 
+__device__ __forceinline__ uint64_t minus(uint64_t a, uint64_t b)  // of two numbers each
+{
+    return fma_two(b, two(-1.f, -1.f), a);
+}
+
 // 1 / sqrt(mean of squares + eps) of the head whose 16 elements each are held by kLanes neighbouring
 // lanes.  By the whole warp; what it returns where `normed` is false is not read.
 template <int kLanes>
-__device__ __forceinline__ float inverse_norm(const float (&lo)[8], const float (&hi)[8], float eps, bool normed)
+__device__ __forceinline__ float inverse_norm(const uint64_t (&x)[8], float eps, bool normed)
 {
-    Two s{0.f, 0.f};
+    // two sums, each with what its roundings left
+    uint64_t hi = two(0.f, 0.f), lo = hi;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float x = i < 8 ? lo[i & 7] : hi[i & 7];  // 11 bits at most: the square is exact
-        const Two t = sum_of(s.hi, __fmul_rn(x, x));
-        s = {t.hi, __fadd_rn(s.lo, t.lo)};
+    for (int i = 0; i < 8; ++i) {
+        const uint64_t b = mul_two(x[i], x[i]);  // 11 bits at most: the squares are exact
+        const uint64_t s = add_two(hi, b), t = minus(s, hi);
+        lo = add_two(lo, add_two(minus(hi, minus(s, t)), minus(b, t)));
+        hi = s;
     }
+    Two s = sum_of(halves(hi).x, halves(hi).y);
+    s.lo = __fadd_rn(s.lo, __fadd_rn(halves(lo).x, halves(lo).y));
 #pragma unroll
     for (int m = 1; m < kLanes; m *= 2) {
         const float h = __shfl_xor_sync(0xffffffffu, s.hi, m), l = __shfl_xor_sync(0xffffffffu, s.lo, m);
@@ -127,8 +136,10 @@ __device__ __forceinline__ float inverse_norm(const float (&lo)[8], const float 
         // squares that leave the range of 32 bits (all zeros among them): in 64
         double t = 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            t += (double)lo[i] * lo[i] + (double)hi[i] * hi[i];
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = halves(x[i]);
+            t += (double)f.x * f.x + (double)f.y * f.y;
+        }
 #pragma unroll
         for (int m = 1; m < kLanes; m *= 2)
             t += __shfl_xor_sync(0xffffffffu, t, m);
@@ -147,20 +158,35 @@ __device__ __forceinline__ float inverse_norm(const float (&lo)[8], const float 
 }
 
 template <bool kF16>
-__device__ __forceinline__ void widen(const uint4 &w, float (&x)[8])
+__device__ __forceinline__ void widen(const uint4 &w, uint64_t *x)
 {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 f = unpack_pair<kF16>(u[i]);
-        x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        x[i] = two(f.x, f.y);
     }
 }
 template <bool kF16>
-__device__ __forceinline__ uint4 narrow(const float (&x)[8])
+__device__ __forceinline__ uint4 narrow(const uint64_t *x)
 {
-    return make_uint4(pack_pair<kF16>(x[0], x[1]), pack_pair<kF16>(x[2], x[3]), pack_pair<kF16>(x[4], x[5]),
-                      pack_pair<kF16>(x[6], x[7]));
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        u[i] = pack_pair<kF16>(halves(x[i]).x, halves(x[i]).y);
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+// 8 floats of shared memory
+__device__ __forceinline__ void four_pairs(const float *from, uint64_t (&x)[4])
+{
+    const float4 a = *reinterpret_cast<const float4 *>(from), b = *reinterpret_cast<const float4 *>(from + 4);
+    x[0] = two(a.x, a.y), x[1] = two(a.z, a.w), x[2] = two(b.x, b.y), x[3] = two(b.z, b.w);
+}
+__device__ __forceinline__ float max_or_nan(float a, float b)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
 }
 
 // Bound by HBM: each element is read once and written once.
@@ -168,8 +194,8 @@ template <int kD, bool kF16, bool kQ4>
 __global__ void __launch_bounds__(kThreads) k_paged_rows(const __grid_constant__ RowsArgs p)
 {
     constexpr int kHalf = kD / 2, kLanes = kHalf / 8;  // lanes of a head
-    __shared__ float2 s_cs[kMaxRows][kHalf];
-    __shared__ float s_weight[2][kD];
+    __shared__ __align__(16) float s_cos[kMaxRows][kHalf], s_sin[kMaxRows][kHalf];
+    __shared__ __align__(16) float s_weight[2][kD];
     __shared__ long long s_slot[kMaxRows];
     pdl_wait();
     pdl_trigger();
@@ -186,104 +212,124 @@ __global__ void __launch_bounds__(kThreads) k_paged_rows(const __grid_constant__
                 s_weight[i][x] = p.weight_offset + unpack_pair<kF16>(w[i][x]).x;
     }
     if (p.turn)
-        for (int x = threadIdx.x; x < n_rows * kHalf; x += kThreads)
-            s_cs[x / kHalf][x % kHalf] = cos_sin(turn_of(p.rope, r0 + x / kHalf, x % kHalf));
+        for (int x = threadIdx.x; x < n_rows * kHalf; x += kThreads) {
+            const float2 cs = cos_sin(turn_of(p.rope, r0 + x / kHalf, x % kHalf));
+            s_cos[x / kHalf][x % kHalf] = cs.x;
+            s_sin[x / kHalf][x % kHalf] = cs.y;
+        }
     __syncthreads();
-    const unsigned per_row = (unsigned)(p.Hq + 2 * p.Hkv) * kLanes, items = n_rows * per_row;
+    const int per_row = (p.Hq + 2 * p.Hkv) * kLanes, items = n_rows * per_row;
     constexpr int kAhead = 2;  // items per thread in flight
+    const int c = (int)(threadIdx.x % kLanes) * 8;  // (kThreads is a multiple of a head's lanes)
+    int r = (int)threadIdx.x / per_row, y = (int)threadIdx.x % per_row;
+    const int step_r = kThreads / per_row, step_y = kThreads % per_row;
     // whole warps go through the loop: a head's lanes add up together
-    for (unsigned x0 = threadIdx.x; (x0 & ~31u) < items; x0 += kAhead * kThreads) {
+    for (int x0 = threadIdx.x; (x0 & ~31) < items; x0 += kAhead * kThreads) {
         uint4 in[kAhead][2];
-        uint8_t *dst[kAhead];
+        uint8_t *dst[kAhead], *scales_to[kAhead];
         int row[kAhead], kind[kAhead];  // 0: a query, 1: a key, 2: a value, 3: nothing
 #pragma unroll
         for (int m = 0; m < kAhead; ++m) {
-            const unsigned x = x0 + m * kThreads;
-            const unsigned r = x / per_row, y = x - r * per_row;
-            int h = (int)(y / kLanes);
-            const int c = (int)(y % kLanes) * 8;
             in[m][0] = in[m][1] = make_uint4(0, 0, 0, 0);
-            dst[m] = nullptr;
+            dst[m] = scales_to[m] = nullptr;
             kind[m] = 3;
-            row[m] = (int)r;
-            if (x >= items)
-                continue;
-            const long long at = r0 + r;
-            const uint16_t *src;
-            if (h < p.Hq) {
-                src = p.q.p + at * p.q.row_stride + h * p.q.head_stride;
-                dst[m] = reinterpret_cast<uint8_t *>(p.q_out.p + at * p.q_out.row_stride + h * p.q_out.head_stride + c);
-                kind[m] = 0;
-            } else {
-                h -= p.Hq;
-                const bool is_v = h >= p.Hkv;
-                h -= is_v ? p.Hkv : 0;
-                const long long slot = s_slot[r], page = slot >> p.page_log2;
-                if (slot < 0 || page >= p.n_pages)
-                    continue;  // padding
-                const int in_page = (int)(slot & ((1 << p.page_log2) - 1));
-                const Rows &rows = is_v ? p.v : p.k;
-                src = rows.p + at * rows.row_stride + h * rows.head_stride;
-                dst[m] = (is_v ? p.v_pages : p.k_pages) + page * p.page_stride + h * p.head_stride;
-                dst[m] += kQ4 ? in_page * code_bytes(kD) + c / 2 : in_page * p.slot_stride + 2 * c;
-                kind[m] = is_v ? 2 : 1;
+            row[m] = r;
+            if (x0 + m * kThreads < items) {
+                const long long at = r0 + r;
+                int h = y / kLanes;
+                const uint16_t *src = nullptr;
+                if (h < p.Hq) {
+                    src = p.q.p + at * p.q.row_stride + h * p.q.head_stride;
+                    dst[m] = reinterpret_cast<uint8_t *>(p.q_out.p + at * p.q_out.row_stride + h * p.q_out.head_stride + c);
+                    kind[m] = 0;
+                } else {
+                    h -= p.Hq;
+                    const bool is_v = h >= p.Hkv;
+                    h -= is_v ? p.Hkv : 0;
+                    const long long slot = s_slot[r], page = slot >> p.page_log2;
+                    if (slot >= 0 && page < p.n_pages) {  // else padding
+                        const int in_page = (int)slot & ((1 << p.page_log2) - 1);
+                        const Rows &rows = is_v ? p.v : p.k;
+                        src = rows.p + at * rows.row_stride + h * rows.head_stride;
+                        dst[m] = (is_v ? p.v_pages : p.k_pages) + page * p.page_stride + h * p.head_stride;
+                        if constexpr (kQ4) {
+                            scales_to[m] = dst[m] + ((long long)code_bytes(kD) << p.page_log2) + in_page * scale_bytes(kD);
+                            dst[m] += in_page * code_bytes(kD) + c / 2;
+                        } else {
+                            dst[m] += in_page * p.slot_stride + 2 * c;
+                        }
+                        kind[m] = is_v ? 2 : 1;
+                    }
+                }
+                if (src) {
+                    in[m][0] = *reinterpret_cast<const uint4 *>(src + c);
+                    in[m][1] = *reinterpret_cast<const uint4 *>(src + c + kHalf);
+                }
             }
-            in[m][0] = *reinterpret_cast<const uint4 *>(src + c);
-            in[m][1] = *reinterpret_cast<const uint4 *>(src + c + kHalf);
+            y += step_y, r += step_r;
+            if (y >= per_row)
+                y -= per_row, ++r;
         }
 #pragma unroll
         for (int m = 0; m < kAhead; ++m) {
-            const unsigned x = x0 + m * kThreads;
-            if ((x & ~31u) >= items)
+            if (((x0 + m * kThreads) & ~31) >= items)
                 break;
-            const int c = (int)(x % kLanes) * 8;
-            const bool turns = kind[m] < 2;
-            float lo[8], hi[8];
-            widen<kF16>(in[m][0], lo);
-            widen<kF16>(in[m][1], hi);
+            if (!kQ4 && __all_sync(0xffffffffu, kind[m] >= 2)) {  // values stay as they are
+                if (dst[m]) {
+                    *reinterpret_cast<uint4 *>(dst[m]) = in[m][0];
+                    *reinterpret_cast<uint4 *>(dst[m] + 2 * kHalf) = in[m][1];
+                }
+                continue;
+            }
+            uint64_t v[8];  // the lower half's 8 elements, the upper half's
+            widen<kF16>(in[m][0], v);
+            widen<kF16>(in[m][1], v + 4);
             const bool normed = kind[m] == 0 ? p.q_weight != nullptr : kind[m] == 1 && p.k_weight != nullptr;
             if (__any_sync(0xffffffffu, normed)) {
-                const float r = inverse_norm<kLanes>(lo, hi, p.eps, normed);
+                const float inv = inverse_norm<kLanes>(v, p.eps, normed);
                 if (normed) {
-                    const float *w = s_weight[kind[m]];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        lo[i] = __fmul_rn(__fmul_rn(lo[i], r), w[c + i]);
-                        hi[i] = __fmul_rn(__fmul_rn(hi[i], r), w[c + kHalf + i]);
+                    for (int h = 0; h < 2; ++h) {
+                        uint64_t w[4];
+                        four_pairs(s_weight[kind[m]] + c + h * kHalf, w);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            v[4 * h + i] = mul_two(mul_two(v[4 * h + i], two(inv, inv)), w[i]);
                     }
                 }
             }
-            if (p.turn && turns) {
-                const float2 *cs = &s_cs[row[m]][c];
+            if (p.turn && kind[m] < 2) {
+                uint64_t co[4], si[4];
+                four_pairs(s_cos[row[m]] + c, co);
+                four_pairs(s_sin[row[m]] + c, si);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 t = cs[i];
-                    const float a = lo[i], b = hi[i];
-                    lo[i] = __fsub_rn(__fmul_rn(a, t.x), __fmul_rn(b, t.y));
-                    hi[i] = __fadd_rn(__fmul_rn(b, t.x), __fmul_rn(a, t.y));
+                for (int i = 0; i < 4; ++i) {
+                    const uint64_t a = v[i], b = v[4 + i];
+                    const float2 ac = halves(mul_two(a, co[i])), bs = halves(mul_two(b, si[i]));
+                    const float2 bc = halves(mul_two(b, co[i])), as = halves(mul_two(a, si[i]));
+                    // (one by one: the assembler makes one fma of a product and a sum of pairs)
+                    v[i] = two(__fsub_rn(ac.x, bs.x), __fsub_rn(ac.y, bs.y));
+                    v[4 + i] = two(__fadd_rn(bc.x, as.x), __fadd_rn(bc.y, as.y));
                 }
             }
-            if (!kQ4 || kind[m] == 0) {
-                if (dst[m]) {
-                    *reinterpret_cast<uint4 *>(dst[m]) = narrow<kF16>(lo);
-                    *reinterpret_cast<uint4 *>(dst[m] + 2 * kHalf) = narrow<kF16>(hi);
-                }
+            if ((!kQ4 || kind[m] == 0) && dst[m]) {
+                *reinterpret_cast<uint4 *>(dst[m]) = narrow<kF16>(v);
+                *reinterpret_cast<uint4 *>(dst[m] + 2 * kHalf) = narrow<kF16>(v + 4);
             }
             if (kQ4 && __any_sync(0xffffffffu, kind[m] == 1 || kind[m] == 2)) {
-                uint32_t top[2] = {0, 0};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    top[0] = max(top[0], __float_as_uint(lo[i]) & 0x7fffffffu);
-                    top[1] = max(top[1], __float_as_uint(hi[i]) & 0x7fffffffu);
-                }
                 uint32_t sb[2], word[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-                    top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-                    sb[i] = scale_byte(top[i]);
-                    const float s = scale_of(sb[i]);
-                    word[i] = quantize8(i == 0 ? lo : hi, s, s == 0.f ? 0.f : __frcp_rn(s));
+                for (int h = 0; h < 2; ++h) {
+                    const uint64_t x[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+                    float top = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        top = max_or_nan(max_or_nan(top, fabsf(halves(x[i]).x)), fabsf(halves(x[i]).y));
+                    top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    sb[h] = scale_byte(top);
+                    const float s = scale_of(sb[h]);
+                    word[h] = quantize8(x, s, s == 0.f ? 0.f : __frcp_rn(s), sb[h] >= kMaxScaleByte);
                 }
                 // the head's scales from its lanes 0 and 4 (kD = 64: lane 0)
                 uint32_t scales = sb[0] | sb[1] << (8 * kD / (2 * kGroup));
@@ -295,13 +341,10 @@ __global__ void __launch_bounds__(kThreads) k_paged_rows(const __grid_constant__
                     *reinterpret_cast<uint32_t *>(dst[m]) = word[0];
                     *reinterpret_cast<uint32_t *>(dst[m] + kHalf / 2) = word[1];
                     if (c == 0) {
-                        const int in_page = (int)(s_slot[row[m]] & ((1 << p.page_log2) - 1));
-                        uint8_t *to = dst[m] + ((long long)code_bytes(kD) << p.page_log2) +
-                                      in_page * (scale_bytes(kD) - code_bytes(kD));
                         if constexpr (kD == 128)
-                            *reinterpret_cast<uint32_t *>(to) = scales;
+                            *reinterpret_cast<uint32_t *>(scales_to[m]) = scales;
                         else
-                            *reinterpret_cast<uint16_t *>(to) = (uint16_t)scales;
+                            *reinterpret_cast<uint16_t *>(scales_to[m]) = (uint16_t)scales;
                     }
                 }
             }
@@ -320,55 +363,75 @@ struct LoadArgs {
     long long row_layer_stride;
 };
 
-// A lane takes 8 codes of a (row, layer, K or V, head), neighbouring lanes its neighbours.  Bound by HBM:
-// 0.53 bytes read and 2 written per element.
+// 16 codes (8 bytes, half a scale's) become 32 bytes, a sector, written at once.
+constexpr int kLoadCodes = 16, kLoadAhead = 4;
+
+// A thread keeps its place in a row, (K or V, head, 16 elements), and takes a few rows.  Bound by HBM: 0.53
+// bytes read and 2 written per element.
 template <int kD, bool kF16>
-__global__ void __launch_bounds__(kThreads) k_paged_load(const __grid_constant__ LoadArgs p)
+__global__ void __launch_bounds__(kThreads) k_paged_load(const __grid_constant__ LoadArgs p, int rows_per_cta)
 {
-    constexpr int kWords = kD / 8, kAhead = 4;
+    constexpr int kPieces = kD / kLoadCodes;
     pdl_wait();
     pdl_trigger();
-    const unsigned per_row = (unsigned)(2 * p.Hkv) * kWords;
-    const int layer = blockIdx.y;
-    const unsigned items = p.n_rows * per_row, stride = gridDim.x * kThreads;  // below 2^31 (the host's check)
-    for (unsigned x0 = blockIdx.x * kThreads + threadIdx.x; x0 < items; x0 += kAhead * stride) {
-        uint32_t code[kAhead], scale[kAhead];
-        uint16_t *dst[kAhead];
+    const int per_row = 2 * p.Hkv * kPieces, layer = blockIdx.y;
+    // rows at a time: as many as the CTA's threads cover
+    const int abreast = per_row < kThreads ? kThreads / per_row : 1;
+    const int first = (int)blockIdx.x * rows_per_cta, end = min(first + rows_per_cta, p.n_rows);
+    const int sub = per_row < kThreads ? (int)threadIdx.x / per_row : 0;
+    if (sub >= abreast)
+        return;
+    for (int y = (int)threadIdx.x - sub * per_row; y < per_row; y += kThreads) {
+        int h = y / kPieces;
+        const int w = y % kPieces;
+        const bool is_v = h >= p.Hkv;
+        h -= is_v ? p.Hkv : 0;
+        const uint8_t *codes = (is_v ? p.v_pages : p.k_pages) + layer * p.layer_stride + h * p.head_stride + 8 * w;
+        const uint8_t *scales = codes - 8 * w + ((long long)code_bytes(kD) << p.page_log2) + w / 2;
+        const Rows &to = is_v ? p.v : p.k;
+        uint16_t *out = to.p + layer * p.row_layer_stride + h * to.head_stride + kLoadCodes * w;
+        for (int r0 = first + sub; r0 < end; r0 += kLoadAhead * abreast) {
+            uint2 code[kLoadAhead];
+            uint32_t scale[kLoadAhead];
+            bool there[kLoadAhead];
 #pragma unroll
-        for (int m = 0; m < kAhead; ++m) {
-            const unsigned x = x0 + m * stride;
-            dst[m] = nullptr;
-            if (x >= items)
-                continue;
-            const unsigned r = x / per_row, y = x - r * per_row;
-            int h = (int)(y / kWords);
-            const int w = (int)(y % kWords);
-            const bool is_v = h >= p.Hkv;
-            h -= is_v ? p.Hkv : 0;
-            const long long slot = p.slots[r], page = slot >> p.page_log2;
-            if (slot < 0 || page >= p.n_pages)
-                continue;  // padding
-            const int in_page = (int)(slot & ((1 << p.page_log2) - 1));
-            const uint8_t *src = (is_v ? p.v_pages : p.k_pages) + layer * p.layer_stride + page * p.page_stride +
-                                 h * p.head_stride;
-            code[m] = *reinterpret_cast<const uint32_t *>(src + in_page * code_bytes(kD) + 4 * w);
-            scale[m] = src[((long long)code_bytes(kD) << p.page_log2) + in_page * scale_bytes(kD) + w / 4];
-            const Rows &to = is_v ? p.v : p.k;
-            dst[m] = to.p + layer * p.row_layer_stride + r * to.row_stride + h * to.head_stride + 8 * w;
-        }
+            for (int m = 0; m < kLoadAhead; ++m) {
+                const int r = r0 + m * abreast;
+                const long long slot = r < end ? p.slots[r] : -1, page = slot >> p.page_log2;
+                there[m] = slot >= 0 && page < p.n_pages;  // else padding
+                if (!there[m])
+                    continue;
+                const int in_page = (int)slot & ((1 << p.page_log2) - 1);
+                code[m] = *reinterpret_cast<const uint2 *>(codes + page * p.page_stride + in_page * code_bytes(kD));
+                scale[m] = scales[page * p.page_stride + in_page * scale_bytes(kD)];
+            }
 #pragma unroll
-        for (int m = 0; m < kAhead; ++m) {
-            if (!dst[m])
-                continue;
-            const float f = scale_of(scale[m]);
-            const Scale<kF16> s = scale_pair<kF16>(f, f);
-            uint32_t a[4];  // elements j and j + 4
+            for (int m = 0; m < kLoadAhead; ++m) {
+                if (!there[m])
+                    continue;
+                const float f = scale_of(scale[m]);
+                const Scale<kF16> s = scale_pair<kF16>(f, f);
+                uint32_t e[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                a[j] = dequant_pair<kF16>(code[m] >> (4 * j), s);
-            *reinterpret_cast<uint4 *>(dst[m]) =
-                make_uint4(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410),
-                           __byte_perm(a[0], a[1], 0x7632), __byte_perm(a[2], a[3], 0x7632));
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t x = i ? code[m].y : code[m].x;
+                    uint32_t a[4];  // elements j and j + 4
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        a[j] = dequant_pair<kF16>(x >> (4 * j), s);
+                    e[4 * i] = __byte_perm(a[0], a[1], 0x5410), e[4 * i + 1] = __byte_perm(a[2], a[3], 0x5410);
+                    e[4 * i + 2] = __byte_perm(a[0], a[1], 0x7632), e[4 * i + 3] = __byte_perm(a[2], a[3], 0x7632);
+                }
+                uint16_t *dst = out + (long long)(r0 + m * abreast) * to.row_stride;
+                if ((reinterpret_cast<uintptr_t>(dst) & 31) == 0) {
+                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(e[0]), "r"(e[1]),
+                                 "r"(e[2]), "r"(e[3]), "r"(e[4]), "r"(e[5]), "r"(e[6]), "r"(e[7])
+                                 : "memory");
+                } else {
+                    reinterpret_cast<uint4 *>(dst)[0] = make_uint4(e[0], e[1], e[2], e[3]);
+                    reinterpret_cast<uint4 *>(dst)[1] = make_uint4(e[4], e[5], e[6], e[7]);
+                }
+            }
         }
     }
 }
@@ -523,8 +586,8 @@ extern "C" tb_status paged_kv_load_q4(const tb_pages_q4 *pages, int layer, int n
         return record_error(TB_EINVAL, "%s: n_rows %d, or slots is NULL", fn, n_rows);
     if (n_rows > 0 && ((st = check_rows(k, "k", fn)) != TB_OK || (st = check_rows(v, "v", fn)) != TB_OK))
         return st;
-    if ((long long)n_rows * 2 * pages->n_kv_heads * (pages->head_dim / 8) >= 1ll << 31)
-        return record_error(TB_EUNSUPPORTED, "%s: %d rows of %d heads in one call", fn, n_rows, pages->n_kv_heads);
+    if (n_rows > 1 << 30 || pages->n_kv_heads > 1 << 20)
+        return record_error(TB_EUNSUPPORTED, "%s: %d rows of %d kv heads", fn, n_rows, pages->n_kv_heads);
     if (row_layer_stride % 8)
         return record_error(TB_EINVAL, "%s: row_layer_stride must be a multiple of 8 elements", fn);
     if (n_rows == 0)
@@ -549,12 +612,18 @@ extern "C" tb_status paged_kv_load_q4(const tb_pages_q4 *pages, int layer, int n
     a.k = rows_of(k);
     a.v = rows_of(v);
     a.row_layer_stride = row_layer_stride;
-    // a thread has 4 items in flight; CTAs for all of a layer's, as many as the SMs hold a few times over
-    const long long ctas = ((long long)n_rows * 2 * a.Hkv * (pages->head_dim / 8) + 4 * kThreads - 1) / (4 * kThreads);
-    const long long most = (64ll * n_sm + n_layers - 1) / n_layers;
-    const dim3 grid((unsigned)(ctas < most ? ctas : most), n_layers);
+    // kLoadAhead rows per thread, fewer rows per CTA where that would leave SMs without one, more where it would
+    // make more than 64 CTAs for each
+    const long long per_row = 2ll * a.Hkv * (pages->head_dim / kLoadCodes), abreast = per_row < kThreads ? kThreads / per_row : 1;
+    long long rows = kLoadAhead * abreast;
+    while (rows > abreast && (n_rows + rows - 1) / rows * n_layers < 2 * n_sm)
+        rows -= abreast;
+    while ((n_rows + rows - 1) / rows * n_layers > 64ll * n_sm && rows < n_rows)
+        rows *= 2;
+    const dim3 grid((unsigned)((n_rows + rows - 1) / rows), n_layers);
     const bool f16 = pages->dtype == TB_F16;
     const auto kernel = pages->head_dim == 64 ? (f16 ? k_paged_load<64, true> : k_paged_load<64, false>)
                                               : (f16 ? k_paged_load<128, true> : k_paged_load<128, false>);
-    return launch_result(launch_kernel(kernel, grid, dim3(kThreads), 0, (cudaStream_t)stream, true, a), fn);
+    return launch_result(launch_kernel(kernel, grid, dim3(kThreads), 0, (cudaStream_t)stream, true, a, (int)rows),
+                         fn);
 }
