@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t quantize8(const uint64_t (&x)[4], float s, f
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint64_t y = quotient_two(x[i], two(-s, -s), two(inv, inv));
-        if (clamp) {  // the scale is the largest one (or NaN, which gives 7)
+        if (clamp) {  // some scale is the largest one, or NaN (which gives 7)
             const float2 f = halves(y);
             y = two(fmaxf(fminf(f.x, 7.f), -7.f), fmaxf(fminf(f.y, 7.f), -7.f));
         }

@@ -191,7 +191,7 @@ __device__ __forceinline__ float max_or_nan(float a, float b)
 
 // Bound by HBM: each element is read once and written once.
 template <int kD, bool kF16, bool kQ4>
-__global__ void __launch_bounds__(kThreads) k_paged_rows(const __grid_constant__ RowsArgs p)
+__global__ void __launch_bounds__(kThreads, 4) k_paged_rows(const __grid_constant__ RowsArgs p)
 {
     constexpr int kHalf = kD / 2, kLanes = kHalf / 8;  // lanes of a head
     __shared__ __align__(16) float s_cos[kMaxRows][kHalf], s_sin[kMaxRows][kHalf];
@@ -218,133 +218,127 @@ __global__ void __launch_bounds__(kThreads) k_paged_rows(const __grid_constant__
             s_sin[x / kHalf][x % kHalf] = cs.y;
         }
     __syncthreads();
-    const int per_row = (p.Hq + 2 * p.Hkv) * kLanes, items = n_rows * per_row;
-    constexpr int kAhead = 2;  // items per thread in flight
+    // A thread keeps its place in a row, (head, 16 bytes of either half), and takes row after row; where a row
+    // has fewer places than the CTA threads, several rows stand abreast.  Whole warps go through the loops: a
+    // head's lanes add up together, and what lies outside does a valid row's work and writes nothing.
+    const int per_row = (p.Hq + 2 * p.Hkv) * kLanes, abreast = per_row < kThreads ? kThreads / per_row : 1;
+    const int sub = per_row < kThreads ? (int)threadIdx.x / per_row : 0;
+    constexpr int kAhead = 2;  // rows per thread in flight
     const int c = (int)(threadIdx.x % kLanes) * 8;  // (kThreads is a multiple of a head's lanes)
-    int r = (int)threadIdx.x / per_row, y = (int)threadIdx.x % per_row;
-    const int step_r = kThreads / per_row, step_y = kThreads % per_row;
-    // whole warps go through the loop: a head's lanes add up together
-    for (int x0 = threadIdx.x; (x0 & ~31) < items; x0 += kAhead * kThreads) {
-        uint4 in[kAhead][2];
-        uint8_t *dst[kAhead], *scales_to[kAhead];
-        int row[kAhead], kind[kAhead];  // 0: a query, 1: a key, 2: a value, 3: nothing
+    for (int y0 = 0; y0 < per_row; y0 += kThreads) {
+        const int y = y0 + (int)threadIdx.x - sub * per_row;
+        const bool live = y < per_row && sub < abreast;
+        int h = live ? y / kLanes : 0;
+        const int kind = h < p.Hq ? 0 : h < p.Hq + p.Hkv ? 1 : 2;  // a query, a key, a value
+        h -= kind == 0 ? 0 : kind == 1 ? p.Hq : p.Hq + p.Hkv;
+        const Rows &rows = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
+        const uint16_t *src = rows.p + r0 * rows.row_stride + h * rows.head_stride + c;
+        const long long src_stride = rows.row_stride;
+        uint16_t *const q_out = p.q_out.p + r0 * p.q_out.row_stride + h * p.q_out.head_stride + c;
+        uint8_t *const pages = (kind == 2 ? p.v_pages : p.k_pages) + h * p.head_stride;
+        const bool normed = live && (kind == 0 ? p.q_weight != nullptr : kind == 1 && p.k_weight != nullptr);
+        const bool any_normed = __any_sync(0xffffffffu, normed), turns = p.turn && kind < 2;
+        const bool any_key = __any_sync(0xffffffffu, live && kind > 0);
+        const bool as_is = !kQ4 && __all_sync(0xffffffffu, kind == 2 || !live);  // values stay as they are
+        for (int rr = 0; rr < n_rows; rr += kAhead * abreast) {
+            uint4 in[kAhead][2];
 #pragma unroll
-        for (int m = 0; m < kAhead; ++m) {
-            in[m][0] = in[m][1] = make_uint4(0, 0, 0, 0);
-            dst[m] = scales_to[m] = nullptr;
-            kind[m] = 3;
-            row[m] = r;
-            if (x0 + m * kThreads < items) {
-                const long long at = r0 + r;
-                int h = y / kLanes;
-                const uint16_t *src = nullptr;
-                if (h < p.Hq) {
-                    src = p.q.p + at * p.q.row_stride + h * p.q.head_stride;
-                    dst[m] = reinterpret_cast<uint8_t *>(p.q_out.p + at * p.q_out.row_stride + h * p.q_out.head_stride + c);
-                    kind[m] = 0;
+            for (int m = 0; m < kAhead; ++m) {
+                const uint16_t *from = src + min(rr + m * abreast + sub, n_rows - 1) * src_stride;
+                in[m][0] = *reinterpret_cast<const uint4 *>(from);
+                in[m][1] = *reinterpret_cast<const uint4 *>(from + kHalf);
+            }
+#pragma unroll
+            for (int m = 0; m < kAhead; ++m) {
+                if (rr + m * abreast >= n_rows)
+                    break;
+                const int r = min(rr + m * abreast + sub, n_rows - 1);
+                bool there = live && rr + m * abreast + sub < n_rows;
+                uint8_t *dst, *scales_to = nullptr;
+                if (kind == 0) {
+                    dst = reinterpret_cast<uint8_t *>(q_out + r * p.q_out.row_stride);
                 } else {
-                    h -= p.Hq;
-                    const bool is_v = h >= p.Hkv;
-                    h -= is_v ? p.Hkv : 0;
                     const long long slot = s_slot[r], page = slot >> p.page_log2;
-                    if (slot >= 0 && page < p.n_pages) {  // else padding
-                        const int in_page = (int)slot & ((1 << p.page_log2) - 1);
-                        const Rows &rows = is_v ? p.v : p.k;
-                        src = rows.p + at * rows.row_stride + h * rows.head_stride;
-                        dst[m] = (is_v ? p.v_pages : p.k_pages) + page * p.page_stride + h * p.head_stride;
-                        if constexpr (kQ4) {
-                            scales_to[m] = dst[m] + ((long long)code_bytes(kD) << p.page_log2) + in_page * scale_bytes(kD);
-                            dst[m] += in_page * code_bytes(kD) + c / 2;
-                        } else {
-                            dst[m] += in_page * p.slot_stride + 2 * c;
+                    there = there && slot >= 0 && page < p.n_pages;  // else padding
+                    const int in_page = (int)slot & ((1 << p.page_log2) - 1);
+                    dst = pages + page * p.page_stride;
+                    if constexpr (kQ4) {
+                        scales_to = dst + ((long long)code_bytes(kD) << p.page_log2) + in_page * scale_bytes(kD);
+                        dst += in_page * code_bytes(kD) + c / 2;
+                    } else {
+                        dst += in_page * p.slot_stride + 2 * c;
+                    }
+                }
+                if (as_is) {
+                    if (there) {
+                        *reinterpret_cast<uint4 *>(dst) = in[m][0];
+                        *reinterpret_cast<uint4 *>(dst + 2 * kHalf) = in[m][1];
+                    }
+                    continue;
+                }
+                uint64_t v[8];  // the lower half's 8 elements, the upper half's
+                widen<kF16>(in[m][0], v);
+                widen<kF16>(in[m][1], v + 4);
+                if (any_normed) {
+                    const float inv = inverse_norm<kLanes>(v, p.eps, normed);
+                    if (normed) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            uint64_t w[4];
+                            four_pairs(s_weight[kind] + c + i * kHalf, w);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                v[4 * i + j] = mul_two(mul_two(v[4 * i + j], two(inv, inv)), w[j]);
                         }
-                        kind[m] = is_v ? 2 : 1;
                     }
                 }
-                if (src) {
-                    in[m][0] = *reinterpret_cast<const uint4 *>(src + c);
-                    in[m][1] = *reinterpret_cast<const uint4 *>(src + c + kHalf);
-                }
-            }
-            y += step_y, r += step_r;
-            if (y >= per_row)
-                y -= per_row, ++r;
-        }
+                if (turns) {
+                    uint64_t co[4], si[4];
+                    four_pairs(s_cos[r] + c, co);
+                    four_pairs(s_sin[r] + c, si);
 #pragma unroll
-        for (int m = 0; m < kAhead; ++m) {
-            if (((x0 + m * kThreads) & ~31) >= items)
-                break;
-            if (!kQ4 && __all_sync(0xffffffffu, kind[m] >= 2)) {  // values stay as they are
-                if (dst[m]) {
-                    *reinterpret_cast<uint4 *>(dst[m]) = in[m][0];
-                    *reinterpret_cast<uint4 *>(dst[m] + 2 * kHalf) = in[m][1];
-                }
-                continue;
-            }
-            uint64_t v[8];  // the lower half's 8 elements, the upper half's
-            widen<kF16>(in[m][0], v);
-            widen<kF16>(in[m][1], v + 4);
-            const bool normed = kind[m] == 0 ? p.q_weight != nullptr : kind[m] == 1 && p.k_weight != nullptr;
-            if (__any_sync(0xffffffffu, normed)) {
-                const float inv = inverse_norm<kLanes>(v, p.eps, normed);
-                if (normed) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint64_t w[4];
-                        four_pairs(s_weight[kind[m]] + c + h * kHalf, w);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            v[4 * h + i] = mul_two(mul_two(v[4 * h + i], two(inv, inv)), w[i]);
+                    for (int i = 0; i < 4; ++i) {
+                        const uint64_t a = v[i], b = v[4 + i];
+                        const float2 ac = halves(mul_two(a, co[i])), bs = halves(mul_two(b, si[i]));
+                        const float2 bc = halves(mul_two(b, co[i])), as = halves(mul_two(a, si[i]));
+                        // (one by one: the assembler makes one fma of a product and a sum of pairs)
+                        v[i] = two(__fsub_rn(ac.x, bs.x), __fsub_rn(ac.y, bs.y));
+                        v[4 + i] = two(__fadd_rn(bc.x, as.x), __fadd_rn(bc.y, as.y));
                     }
                 }
-            }
-            if (p.turn && kind[m] < 2) {
-                uint64_t co[4], si[4];
-                four_pairs(s_cos[row[m]] + c, co);
-                four_pairs(s_sin[row[m]] + c, si);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint64_t a = v[i], b = v[4 + i];
-                    const float2 ac = halves(mul_two(a, co[i])), bs = halves(mul_two(b, si[i]));
-                    const float2 bc = halves(mul_two(b, co[i])), as = halves(mul_two(a, si[i]));
-                    // (one by one: the assembler makes one fma of a product and a sum of pairs)
-                    v[i] = two(__fsub_rn(ac.x, bs.x), __fsub_rn(ac.y, bs.y));
-                    v[4 + i] = two(__fadd_rn(bc.x, as.x), __fadd_rn(bc.y, as.y));
+                if ((!kQ4 || kind == 0) && there) {
+                    *reinterpret_cast<uint4 *>(dst) = narrow<kF16>(v);
+                    *reinterpret_cast<uint4 *>(dst + 2 * kHalf) = narrow<kF16>(v + 4);
                 }
-            }
-            if ((!kQ4 || kind[m] == 0) && dst[m]) {
-                *reinterpret_cast<uint4 *>(dst[m]) = narrow<kF16>(v);
-                *reinterpret_cast<uint4 *>(dst[m] + 2 * kHalf) = narrow<kF16>(v + 4);
-            }
-            if (kQ4 && __any_sync(0xffffffffu, kind[m] == 1 || kind[m] == 2)) {
-                uint32_t sb[2], word[2];
+                if (kQ4 && any_key) {
+                    uint32_t sb[2], word[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint64_t x[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-                    float top = 0.f;
+                    for (int i = 0; i < 2; ++i) {
+                        const uint64_t x[4] = {v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+                        float top = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        top = max_or_nan(max_or_nan(top, fabsf(halves(x[i]).x)), fabsf(halves(x[i]).y));
-                    top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    sb[h] = scale_byte(top);
-                    const float s = scale_of(sb[h]);
-                    word[h] = quantize8(x, s, s == 0.f ? 0.f : __frcp_rn(s), sb[h] >= kMaxScaleByte);
-                }
-                // the head's scales from its lanes 0 and 4 (kD = 64: lane 0)
-                uint32_t scales = sb[0] | sb[1] << (8 * kD / (2 * kGroup));
-                if constexpr (kLanes == 8) {
-                    const uint32_t more = __shfl_xor_sync(0xffffffffu, scales, 4);
-                    scales |= more << 8;
-                }
-                if (kind[m] == 1 || kind[m] == 2) {
-                    *reinterpret_cast<uint32_t *>(dst[m]) = word[0];
-                    *reinterpret_cast<uint32_t *>(dst[m] + kHalf / 2) = word[1];
-                    if (c == 0) {
-                        if constexpr (kD == 128)
-                            *reinterpret_cast<uint32_t *>(scales_to[m]) = scales;
-                        else
-                            *reinterpret_cast<uint16_t *>(scales_to[m]) = (uint16_t)scales;
+                        for (int j = 0; j < 4; ++j)
+                            top = max_or_nan(max_or_nan(top, fabsf(halves(x[j]).x)), fabsf(halves(x[j]).y));
+                        top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                        top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                        sb[i] = scale_byte(top);
+                        const float s = scale_of(sb[i]);
+                        word[i] = quantize8(x, s, s == 0.f ? 0.f : __frcp_rn(s),
+                                             __any_sync(0xffffffffu, sb[i] >= kMaxScaleByte));
+                    }
+                    // the head's scales from its lanes 0 and 4 (kD = 64: lane 0)
+                    uint32_t scales = sb[0] | sb[1] << (8 * kD / (2 * kGroup));
+                    if constexpr (kLanes == 8)
+                        scales |= __shfl_xor_sync(0xffffffffu, scales, 4) << 8;
+                    if (kind > 0 && there) {
+                        *reinterpret_cast<uint32_t *>(dst) = word[0];
+                        *reinterpret_cast<uint32_t *>(dst + kHalf / 2) = word[1];
+                        if (c == 0) {
+                            if constexpr (kD == 128)
+                                *reinterpret_cast<uint32_t *>(scales_to) = scales;
+                            else
+                                *reinterpret_cast<uint16_t *>(scales_to) = (uint16_t)scales;
+                        }
                     }
                 }
             }
