@@ -47,9 +47,10 @@
 // and 43.6 with packed pairs and one reciprocal for four caps, before holes in the table
 // were reported.
 //
-// 4-bit pages (kQ4): the producers copy pages as they lie into rings of packed
-// tiles, and warps 8-11 turn them into the tiles above, each element exactly: 32
-// codes and their scale per thread, eight 16-byte pieces into the swizzled rows.
+// 4-bit pages (kQ4): warps 0 and 1 copy pages as they lie into rings of packed
+// tiles of K and V, and warps 8-11 (K, some of V) and 0-2 (the rest) turn them into
+// the tiles above, each element exactly: 32 codes and their scale per
+// thread, eight 16-byte pieces into the swizzled rows.  Warp 3 issues both products.
 // Within 8 elements those stand in the order 0 4 1 5 2 6 3 7, in which two are
 // unpacked at a time; the queries are staged in that order too, and the output's
 // columns put back.
@@ -308,56 +309,71 @@ __device__ __forceinline__ void sts128(uint32_t a, const uint32_t (&x)[4])
                  : "memory");
 }
 
-// The packed tile of 128 keys: pieces of min(page_size, 128) keys, each as it lies in its page.
+// The packed tile of 128 keys: pieces of min(page_size, 128) keys, each as it lies in its page: its keys'
+// codes, then their scales.
 struct PackedTile {
     int log2;  // keys of a piece
     __device__ __forceinline__ explicit PackedTile(int page_log2) : log2(min(page_log2, 7)) {}
     template <int kD>
     __device__ __forceinline__ int codes(int key) const
     {
-        return (key >> log2 << log2) * row_bytes(kD) + (key & ((1 << log2) - 1)) * code_bytes(kD);
+        return key * code_bytes(kD) + (key & -(1 << log2)) * scale_bytes(kD);
     }
     template <int kD>
     __device__ __forceinline__ int scales(int key) const
     {
-        return (key >> log2 << log2) * row_bytes(kD) + (code_bytes(kD) << log2) +
-               (key & ((1 << log2) - 1)) * scale_bytes(kD);
+        return (key & -(1 << log2)) * code_bytes(kD) + key * scale_bytes(kD) + (code_bytes(kD) << log2);
     }
 };
 
-// A packed tile into one of 16-bit elements, by 128 threads (tid): 32 elements of a key each.  holes: the
-// pieces that are not there, whose elements count as zeros.
+// Part of a packed tile into one of 16-bit elements, by a warp: 32 elements of a key per lane and block, 8 keys
+// of 128 elements or 16 of 64; blocks first to first + n - 1.  holes: the pieces that are not there, whose
+// elements count as zeros.
+template <int kD>
+constexpr int kTileBlocks = kBN * kD / kGroup / 32;
+
 template <int kD, bool kF16>
-__device__ __forceinline__ void unpack_tile(uint32_t packed, uint32_t tile, const PackedTile &pt, uint32_t holes, int tid)
+__device__ __forceinline__ void unpack_blocks(uint32_t packed, uint32_t tile, const PackedTile &pt, uint32_t holes, int first,
+                                              int n)
 {
-    constexpr int kChunks = kD / kGroup;  // of a key
-    constexpr int kKeys = 128 / kChunks;  // per round
-    const int key0 = tid / kChunks, chunk = tid % kChunks;
+    constexpr int kChunks = kD / kGroup, kKeys = 32 / kChunks;
+    const int lane = threadIdx.x & 31, chunk = lane % kChunks;
     // eight neighbouring lanes write eight different 16-byte columns: those of the second atom in another order
-    const int flip = kD == 128 ? (chunk >> 1) * 2 : 0;
-    uint4 w[kChunks];
-    float f[kChunks];
-#pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        const int key = key0 + i * kKeys;
-        w[i] = lds128(packed + pt.codes<kD>(key) + 16 * chunk);
-        f[i] = scale_of(lds8(packed + pt.scales<kD>(key) + chunk));
+    const bool flip = kD == 128 && chunk >= 2;
+    int key = first * kKeys + lane / kChunks;
+    const auto load = [&](uint4 &w, float &f) {
+        const uint32_t at = packed + pt.codes<kD>(key) + 16 * chunk;
+        const uint2 a = lds64(at + (flip ? 8 : 0)), b = lds64(at + (flip ? 0 : 8));
+        w = make_uint4(a.x, a.y, b.x, b.y);
+        f = scale_of(lds8(packed + pt.scales<kD>(key) + chunk));
         if (holes)
-            f[i] = (holes >> (key >> pt.log2)) & 1u ? 0.f : f[i];
-    }
-    const uint32_t to = tile + (kD == 128 ? (chunk >> 1) * kAtom : 0) + key0 * 128;
+            f = (holes >> (key >> pt.log2)) & 1u ? 0.f : f;
+    };
+    uint32_t to = tile + (flip ? kAtom : 0) + key * 128;
+    uint32_t column[4];  // (a block's keys are a multiple of 8: key & 7 stays)
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        const OperandScale<kF16> s = operand_scale<kF16>(f[i], f[i]);
-        const uint32_t words[4] = {flip ? w[i].z : w[i].x, flip ? w[i].w : w[i].y, flip ? w[i].x : w[i].z,
-                                   flip ? w[i].y : w[i].w};
+    for (int j = 0; j < 4; ++j)
+        column[j] = (((chunk & 1) * 4 + (flip ? j ^ 2 : j)) ^ (key & 7)) * 16;
+    uint4 w, next{};
+    float f, next_f = 0.f;
+    load(w, f);
+    // (a short loop: four roles' unrolled code does not fit the instruction caches)
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        key += kKeys;
+        if (i + 1 < n)
+            load(next, next_f);
+        const OperandScale<kF16> s = operand_scale<kF16>(f, f);
+        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             uint32_t e[4];
             dequant_four<kF16>(words[j], s, e);
-            // (kKeys is a multiple of 8: key & 7 is key0 & 7)
-            sts128(to + i * kKeys * 128 + ((((chunk & 1) * 4 + (j ^ flip)) ^ (key0 & 7)) * 16), e);
+            sts128(to + column[j], e);
         }
+        to += kKeys * 128;
+        w = next;
+        f = next_f;
     }
 }
 
@@ -420,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         for (int s = 0; s < kMaxStages; ++s) {
             mbar_init(&k_full[s], kQ4 ? 4 : 1);
             mbar_init(&k_empty[s], 1);
-            mbar_init(&v_full[s], kQ4 ? 4 : 1);
+            mbar_init(&v_full[s], kQ4 ? 7 : 1);
             mbar_init(&v_empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -437,10 +453,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         if constexpr (kQ4) {
             for (int s = 0; s < 2 * kPackedStages; ++s) {
                 mbar_init(&packed_full[s / kPackedStages][s % kPackedStages], 1);
-                mbar_init(&packed_empty[s / kPackedStages][s % kPackedStages], 4);
+                mbar_init(&packed_empty[s / kPackedStages][s % kPackedStages], s < kPackedStages ? 4 : 7);
             }
         }
-        mbar_init(&drain_bar, 2);
+        mbar_init(&drain_bar, kQ4 ? 1 : 2);  // issuing threads
         abort_flag = 0;
         fence_mbar_init();
         if constexpr (!kQ4) {
@@ -491,6 +507,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     const long long t0 = s_ok ? s_cta.t0 : 0, t1 = s_ok ? s_cta.t1 : 0;
     const PlanReq *reqs = plan_reqs(p.plan);
 
+    // 4-bit pages: this warp's blocks of tile i (of K or V)
+    [[maybe_unused]] const auto unpack = [&](bool is_v, int i, int first, int n) {
+        const int ps = i % kPackedStages, S = is_v ? kVStages : kKStages, s = i % S;
+        if (!warp_agrees(mbar_wait_bounded(&packed_full[is_v][ps], (uint32_t)(i / kPackedStages) & 1u, &abort_flag,
+                                           p.status)) ||
+            !warp_agrees(mbar_wait_bounded(is_v ? &v_empty[s] : &k_empty[s], ((uint32_t)(i / S) & 1u) ^ 1u, &abort_flag,
+                                           p.status)))
+            return false;
+        unpack_blocks<kD, kF16>(smem_u32(packed) + ((is_v ? kPackedStages : 0) + ps) * kPacked,
+                                smem_u32(is_v ? sV : sK) + s * kTile, PackedTile(p.page_log2), packed_holes[is_v][ps], first,
+                                n);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            mbar_arrive(&packed_empty[is_v][ps]);
+            mbar_arrive(is_v ? &v_full[s] : &k_full[s]);
+        }
+        return true;
+    };
+    // K's blocks lie with warps 8-11, V's with all seven so that none takes much longer than the others: copying
+    // costs warps 0 and 1 about as much as three blocks
+    constexpr int kBlocks = kTileBlocks<kD>, kShare = kBlocks == 16 ? 3 : 1;
+    static_assert(kBlocks == 4 * kShare + 4, "of warps 0 and 1, twice it of warp 2, one each of warps 8-11");
     if (kQ4 && few) {
         if constexpr (kQ4) {
             FewSmem<kD> &sm = *reinterpret_cast<FewSmem<kD> *>(smem);
@@ -501,20 +540,186 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     few_rows<kD, kF16, kForm, 2>(p, s_cta, sm, &abort_flag, &never_bar[0]);
             }
         }
+    } else if (kQ4 && warp < 4) {
+        if constexpr (kQ4) {
+            const int all = (int)(t1 - t0);
+            if (warp == 3) {
+                if (lane == 0) {
+                    // -------------------------------------------- both products: Q K^T a tile ahead of P V
+                    struct Walk {
+                        Cursor cur;
+                        Seg g{0, 0, 0};
+                        long long t;
+                        int j = 0, sg = -1;
+                    } wq, wp;
+                    wq.cur.start(s_cta, t1, reqs, p.Hkv);
+                    wp.cur.start(s_cta, t1, reqs, p.Hkv);
+                    wq.t = wp.t = t0;
+                    const auto step = [&](Walk &w) {  // to the next tile; true if it begins a segment
+                        if (w.j < w.g.n)
+                            return false;
+                        w.t += w.g.n;
+                        w.cur.seek(w.t, p.Hkv);
+                        w.g = seg_at(w.cur, w.t);
+                        w.j = 0;
+                        ++w.sg;
+                        return true;
+                    };
+                    const auto scores = [&](int it) {
+                        const bool first = step(wq);
+                        const int b = it & 1, s = it % kKStages;
+                        if (!mbar_wait_bounded(&k_full[s], (uint32_t)(it / kKStages) & 1u, &abort_flag, p.status) ||
+                            (it >= 2 &&
+                             !mbar_wait_bounded(&pv_done[b], (uint32_t)((it - 2) >> 1) & 1u, &abort_flag, p.status)) ||
+                            (first &&
+                             !mbar_wait_bounded(&q_full[wq.sg & 1], (uint32_t)(wq.sg >> 1) & 1u, &abort_flag, p.status)))
+                            return false;
+                        tc_fence_after();
+                        const uint32_t k_base = smem_u32(sK + (size_t)s * kTile);
+                        const uint32_t q_col = tmem + kColQ + (wq.sg & 1) * (kD / 2);
+#pragma unroll
+                        for (int kk = 0; kk < kD / 16; ++kk) {
+                            const uint32_t off = (uint32_t)(kk >> 2) * kAtom + (uint32_t)(kk & 3) * 32;
+                            tc_mma_f16_ts(tmem + kColS + b * 128, q_col + kk * 8, smem_desc_sw128(k_base + off, 0, 1024),
+                                          idesc<kF16>(kBN, false), kk > 0 ? 1u : 0u);
+                        }
+                        tc_commit(&s_full[b]);
+                        tc_commit(&k_empty[s]);
+                        ++wq.j;
+                        return true;
+                    };
+                    uint64_t *const p_ready = p.expire_wait ? never_bar : p_full;
+                    const auto outputs = [&](int it) {
+                        const bool first = step(wp);
+                        const int b = it & 1, s = it % kVStages;
+                        if (!mbar_wait_bounded(&p_ready[b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status) ||
+                            (first && wp.sg > 0 &&
+                             !mbar_wait_bounded(&o_free[(wp.sg - 1) & 1], (uint32_t)((wp.sg - 1) >> 1) & 1u, &abort_flag,
+                                                p.status)) ||
+                            !mbar_wait_bounded(&v_full[s], (uint32_t)(it / kVStages) & 1u, &abort_flag, p.status))
+                            return false;
+                        tc_fence_after();
+                        const uint32_t v_base = smem_u32(sV + (size_t)s * kTile);
+#pragma unroll
+                        for (int ks = 0; ks < kBN / 16; ++ks)
+                            tc_mma_f16_ts(tmem + kColO, tmem + kColS + b * 128 + (ks >> 2) * 64 + (ks & 3) * 8,
+                                          smem_desc_sw128(v_base + ks * 2048, kAtom, 1024), idesc<kF16>(kD, true),
+                                          (first && ks == 0) ? 0u : 1u);
+                        tc_commit(&v_empty[s]);
+                        tc_commit(&pv_done[b]);
+                        ++wp.j;
+                        return true;
+                    };
+                    bool ok = all == 0 || scores(0);
+                    for (int it = 0; ok && it < all; ++it)
+                        ok = (it + 1 == all || scores(it + 1)) && outputs(it);
+                    tc_commit(&drain_bar);
+                }
+            } else {
+                // ------------------------------------------------ most of V; warp 0 copies K's tiles, warp 1 V's
+                const bool is_v = warp == 1;
+                uint64_t *full = packed_full[is_v], *empty = packed_empty[is_v];
+                uint8_t *ring = packed + (is_v ? kPackedStages * kPacked : 0);
+                const int pages_log2 = p.page_log2 >= 7 ? 0 : 7 - p.page_log2;  // pages of a tile: one per lane
+                const int keys = min(1 << p.page_log2, kBN);
+                const bool box = lane < 1 << pages_log2;
+                Cursor cur;
+                cur.start(s_cta, t1, reqs, p.Hkv);
+                struct Page {
+                    int id;
+                    bool inside;  // the request has slots in it
+                };
+                const auto first_slot = [&](int j) {
+                    return tile_key(j, cur.r.a0, cur.r.n1, cur.r.b0) + (lane << p.page_log2);
+                };
+                const auto page_of = [&](int j) {
+                    const int slot = first_slot(j), at = slot >> p.page_log2;
+                    Page x{-1, box && slot < cur.r.L + cur.r.n};
+                    if (x.inside && at < p.max_pages)
+                        x.id = p.table[(size_t)cur.r.b * p.max_pages + at];
+                    return x;
+                };
+                const auto report_hole = [&](int slot) {
+                    const int window = static_cast<const PlanHeader *>(p.plan)->window, past = slot + keys;
+                    const int lo_min = window > 0 ? max(cur.r.begin, cur.r.L - window + 1) : cur.r.begin;
+                    if (past > lo_min ||
+                        (window > 0 && past > cur.r.begin && slot < min(cur.r.far_end, cur.r.L)))
+                        atomicOr(p.status, kStatusBounds);
+                };
+                Seg g{0, 0, 0};
+                long long t = t0;
+                int j = 0, copied = 0;
+                Page page{-1, false};
+                const auto copy_tile = [&] {  // the next one, once its stage is free
+                    if (j == g.n) {
+                        t += g.n;
+                        cur.seek(t, p.Hkv);
+                        g = seg_at(cur, t);
+                        j = 0;
+                        page = page_of(g.j0);
+                    }
+                    const Page next = j + 1 < g.n ? page_of(g.j0 + j + 1) : Page{-1, false};
+                    const int s = copied % kPackedStages;
+                    if (!warp_agrees(mbar_wait_bounded(&empty[s], ((uint32_t)(copied / kPackedStages) & 1u) ^ 1u,
+                                                       &abort_flag, p.status)))
+                        return false;
+                    // a page's block, or a tile's part of its codes and of its scales; nothing for holes
+                    const bool there = page.inside && (unsigned)page.id < (unsigned)p.n_pages;
+                    const uint32_t holes = __ballot_sync(0xffffffffu, page.inside && !there);
+                    const int pieces = __popc(__ballot_sync(0xffffffffu, there));
+                    if (lane == 0) {
+                        packed_holes[is_v][s] = holes;
+                        mbar_arrive_expect_tx(&full[s], pieces * keys * row_bytes(kD));
+                    }
+                    __syncwarp();
+                    if (there) {
+                        const uint8_t *src = (is_v ? p.v_pages : p.k_pages) +
+                                             ((unsigned long long)(unsigned)page.id * p.page_units << 4) +
+                                             g.head * p.head_stride;
+                        uint8_t *dst = ring + (size_t)s * kPacked + lane * keys * row_bytes(kD);
+                        if (p.page_log2 <= 7) {
+                            bulk_load(dst, src, keys * row_bytes(kD), &full[s]);
+                        } else {
+                            const int at = first_slot(g.j0 + j) & ((1 << p.page_log2) - 1);
+                            bulk_load(dst, src + at * code_bytes(kD), kBN * code_bytes(kD), &full[s]);
+                            bulk_load(dst + kBN * code_bytes(kD),
+                                      src + ((long long)code_bytes(kD) << p.page_log2) + at * scale_bytes(kD),
+                                      kBN * scale_bytes(kD), &full[s]);
+                        }
+                    }
+                    if (page.inside && !there && !is_v)
+                        report_hole(first_slot(g.j0 + j));
+                    page = next;
+                    ++j;
+                    ++copied;
+                    return true;
+                };
+                bool ok = true;
+                for (int it = 0; ok && it < all; ++it) {
+                    while (ok && warp < 2 && copied < min(all, it + kPackedStages))
+                        ok = copy_tile();
+                    ok = ok && unpack(true, it, warp * kShare, warp < 2 ? kShare : 2 * kShare);
+                }
+                if (!ok && lane == 0 && warp < 2)
+                    for (int x = max(copied - kPackedStages, 0); x < copied; ++x)
+                        mbar_wait_drain(&full[x % kPackedStages], (uint32_t)(x / kPackedStages) & 1u);
+                __syncwarp();
+            }
+        }
     } else if (warp < 4) {
         Cursor cur;  // (a CTA without tiles has an empty one)
         cur.start(s_cta, t1, reqs, p.Hkv);
         if (warp == 0 || warp == 3) {
             // ------------------------------------------------ producers: a page per lane
             const bool is_v = warp == 3;
-            uint64_t *full = kQ4 ? packed_full[kQ4 && is_v] : is_v ? v_full : k_full;
-            uint64_t *empty = kQ4 ? packed_empty[kQ4 && is_v] : is_v ? v_empty : k_empty;
-            const int S = kQ4 ? kPackedStages : is_v ? kVStages : kKStages;
-            uint8_t *ring = kQ4 ? packed + (is_v ? kPackedStages * kPacked : 0) : is_v ? sV : sK;
+            uint64_t *full = is_v ? v_full : k_full;
+            uint64_t *empty = is_v ? v_empty : k_empty;
+            const int S = is_v ? kVStages : kKStages;
+            uint8_t *ring = is_v ? sV : sK;
             const CUtensorMap *map = is_v ? &p.tv : &p.tk;
             const int pages_log2 = p.page_log2 >= 7 ? 0 : 7 - p.page_log2;  // pages of a tile
             const int a = lane >> pages_log2, pg = lane & ((1 << pages_log2) - 1);
-            const bool box = a < (kQ4 ? 1 : kD / 64);
+            const bool box = a < kD / 64;
             const uint32_t dst_off = (uint32_t)a * kAtom + ((uint32_t)pg << (p.page_log2 + 7));
             const int page_mask = (1 << p.page_log2) - 1;
             // this lane's page of tile j of the current request; nothing is asked of it before its tile's turn
@@ -552,42 +757,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                     ok = __shfl_sync(0xffffffffu, ok, 0);
                     if (!ok)
                         break;
+                    if (lane == 0)
+                        mbar_arrive_expect_tx(&full[s], kTile);
+                    __syncwarp();
                     const bool there = page.id >= 0 && page.id < p.n_pages;
-                    if constexpr (kQ4) {
-                        // a page's block, or a tile's part of its codes and of its scales; nothing for holes
-                        const uint32_t holes = __ballot_sync(0xffffffffu, page.inside && !there);
-                        const int pieces = __popc(__ballot_sync(0xffffffffu, page.inside && there));
-                        const int keys = min(1 << p.page_log2, kBN);
-                        if (lane == 0) {
-                            packed_holes[is_v][s] = holes;
-                            mbar_arrive_expect_tx(&full[s], pieces * keys * row_bytes(kD));
-                        }
-                        __syncwarp();
-                        if (page.inside && there) {
-                            const uint8_t *src = (is_v ? p.v_pages : p.k_pages) +
-                                                 ((unsigned long long)(unsigned)page.id * p.page_units << 4) +
-                                                 g.head * p.head_stride;
-                            uint8_t *dst = ring + (size_t)s * kPacked + pg * keys * row_bytes(kD);
-                            if (p.page_log2 <= 7) {
-                                bulk_load(dst, src, keys * row_bytes(kD), &full[s]);
-                            } else {
-                                const int at = first_slot(g.j0 + j) & page_mask;
-                                bulk_load(dst, src + at * code_bytes(kD), kBN * code_bytes(kD), &full[s]);
-                                bulk_load(dst + kBN * code_bytes(kD),
-                                          src + ((long long)code_bytes(kD) << p.page_log2) + at * scale_bytes(kD),
-                                          kBN * scale_bytes(kD), &full[s]);
-                            }
-                        }
-                    } else {
-                        if (lane == 0)
-                            mbar_arrive_expect_tx(&full[s], kTile);
-                        __syncwarp();
-                        if (box)  // past the last page: zeros
-                            tma_load_4d(ring + (size_t)s * kTile + dst_off, map, &full[s], 64 * a,
-                                        p.page_log2 > 7 ? tile_key(g.j0 + j, cur.r.a0, cur.r.n1, cur.r.b0) & page_mask
-                                                        : 0,
-                                        g.head, there ? page.id : p.n_pages);
-                    }
+                    if (box)  // past the last page: zeros
+                        tma_load_4d(ring + (size_t)s * kTile + dst_off, map, &full[s], 64 * a,
+                                    p.page_log2 > 7 ? tile_key(g.j0 + j, cur.r.a0, cur.r.n1, cur.r.b0) & page_mask : 0,
+                                    g.head, there ? page.id : p.n_pages);
                     if (page.inside && !there && !is_v)
                         report_hole(first_slot(g.j0 + j));
                     page = next;
@@ -983,35 +1160,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             if (lane == 0)
                 mbar_arrive(&q_full[sg & 1]);
         };
-        // 4-bit pages: tiles unpacked so far; a tile's K before the previous tile's V
-        [[maybe_unused]] long long k_done = 0, v_done = 0;
-        [[maybe_unused]] const PackedTile pt(p.page_log2);
-        [[maybe_unused]] const auto unpack = [&](bool is_v, long long n) {
-            const int ps = (int)(n % kPackedStages), S = is_v ? kVStages : kKStages, s = (int)(n % S);
-            if (!warp_agrees(mbar_wait_bounded(&packed_full[is_v][ps], (uint32_t)(n / kPackedStages) & 1u, &abort_flag,
-                                               p.status)) ||
-                !warp_agrees(mbar_wait_bounded(is_v ? &v_empty[s] : &k_empty[s], ((uint32_t)(n / S) & 1u) ^ 1u, &abort_flag,
-                                               p.status)))
-                return false;
-            unpack_tile<kD, kF16>(smem_u32(packed) + ((is_v ? kPackedStages : 0) + ps) * kPacked,
-                                  smem_u32(is_v ? sV : sK) + s * kTile, pt, packed_holes[is_v][ps], threadIdx.x & 127);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&packed_empty[is_v][ps]);
-                mbar_arrive(is_v ? &v_full[s] : &k_full[s]);
-            }
-            return true;
-        };
-        // V up to tile n (not n itself), K up to the one after it
-        [[maybe_unused]] const auto unpack_to = [&](long long n) {
-            const long long all = t1 - t0;
-            for (; v_done < min(n, all); ++v_done) {
-                for (; k_done < min(v_done + 2, all); ++k_done)
-                    if (!unpack(false, k_done))
-                        return false;
-                if (!unpack(true, v_done))
+        // 4-bit pages: tiles unpacked so far
+        [[maybe_unused]] int k_done = 0, v_done = 0;
+        // V up to tile n (not n itself), K up to the one after it: a tile's K before the previous tile's V
+        [[maybe_unused]] const auto unpack_to = [&](int n) {
+            const int all = (int)(t1 - t0);
+            n = min(n, all);
+            while (v_done < n) {
+                const bool is_v = k_done >= min(v_done + 2, all);
+                if (!unpack(is_v, is_v ? v_done : k_done, is_v ? kBlocks - 4 + q4 : q4 * (kBlocks / 4),
+                            is_v ? 1 : kBlocks / 4))
                     return false;
+                v_done += is_v;
+                k_done += !is_v;
             }
             return true;
         };
@@ -1045,7 +1206,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             if constexpr (kQ4) {
                 // through the next unit's first tile: its products wait for this unit's output to be read, its
                 // scores do not
-                if (!unpack_to(it + 1))
+                if (!unpack_to((int)it + 1))
                     break;
             }
             if (!warp_agrees(mbar_wait_bounded(&ml_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status)))
