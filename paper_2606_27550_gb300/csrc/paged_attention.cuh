@@ -48,8 +48,7 @@
 // were reported.
 //
 // 4-bit pages (kQ4): warps 0 and 1 copy pages as they lie into rings of packed
-// tiles of K and V, and warps 8-11 (K, some of V) and 0-2 (the rest) turn them into
-// the tiles above, each element exactly: 32 codes and their scale per
+// tiles of K and V, and warps 8-11 (K) and 0-2 (V) turn them into the tiles above, each element exactly: 32 codes and their scale per
 // thread, eight 16-byte pieces into the swizzled rows.  Warp 3 issues both products.
 // Within 8 elements those stand in the order 0 4 1 5 2 6 3 7, in which two are
 // unpacked at a time; the queries are staged in that order too, and the output's
@@ -436,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         for (int s = 0; s < kMaxStages; ++s) {
             mbar_init(&k_full[s], kQ4 ? 4 : 1);
             mbar_init(&k_empty[s], 1);
-            mbar_init(&v_full[s], kQ4 ? 7 : 1);
+            mbar_init(&v_full[s], kQ4 ? 3 : 1);
             mbar_init(&v_empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -453,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         if constexpr (kQ4) {
             for (int s = 0; s < 2 * kPackedStages; ++s) {
                 mbar_init(&packed_full[s / kPackedStages][s % kPackedStages], 1);
-                mbar_init(&packed_empty[s / kPackedStages][s % kPackedStages], s < kPackedStages ? 4 : 7);
+                mbar_init(&packed_empty[s / kPackedStages][s % kPackedStages], s < kPackedStages ? 4 : 3);
             }
         }
         mbar_init(&drain_bar, kQ4 ? 1 : 2);  // issuing threads
@@ -526,10 +525,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         }
         return true;
     };
-    // K's blocks lie with warps 8-11, V's with all seven so that none takes much longer than the others: copying
-    // costs warps 0 and 1 about as much as three blocks
-    constexpr int kBlocks = kTileBlocks<kD>, kShare = kBlocks == 16 ? 3 : 1;
-    static_assert(kBlocks == 4 * kShare + 4, "of warps 0 and 1, twice it of warp 2, one each of warps 8-11");
+    // K's blocks lie with warps 8-11, V's with 0-2 so that none takes much longer than the others: copying a tile
+    // costs warps 0 and 1 as much as four blocks or so
+    constexpr int kBlocks = kTileBlocks<kD>, kShare = kBlocks == 16 ? 3 : 1;  // of V, for warps 0 and 1
     if (kQ4 && few) {
         if constexpr (kQ4) {
             FewSmem<kD> &sm = *reinterpret_cast<FewSmem<kD> *>(smem);
@@ -545,35 +543,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             const int all = (int)(t1 - t0);
             if (warp == 3) {
                 if (lane == 0) {
-                    // -------------------------------------------- both products: Q K^T a tile ahead of P V
+                    // -------------------------------------------- both products, whichever is ready
                     struct Walk {
                         Cursor cur;
                         Seg g{0, 0, 0};
                         long long t;
-                        int j = 0, sg = -1;
+                        int it = 0, j = 0, sg = -1;
+                        bool first = false;  // tile `it` begins a segment
                     } wq, wp;
                     wq.cur.start(s_cta, t1, reqs, p.Hkv);
                     wp.cur.start(s_cta, t1, reqs, p.Hkv);
                     wq.t = wp.t = t0;
-                    const auto step = [&](Walk &w) {  // to the next tile; true if it begins a segment
-                        if (w.j < w.g.n)
-                            return false;
+                    const auto next = [&](Walk &w) {
+                        w.first = w.j == w.g.n;
+                        if (!w.first)
+                            return;
                         w.t += w.g.n;
                         w.cur.seek(w.t, p.Hkv);
                         w.g = seg_at(w.cur, w.t);
                         w.j = 0;
                         ++w.sg;
-                        return true;
                     };
-                    const auto scores = [&](int it) {
-                        const bool first = step(wq);
-                        const int b = it & 1, s = it % kKStages;
-                        if (!mbar_wait_bounded(&k_full[s], (uint32_t)(it / kKStages) & 1u, &abort_flag, p.status) ||
-                            (it >= 2 &&
-                             !mbar_wait_bounded(&pv_done[b], (uint32_t)((it - 2) >> 1) & 1u, &abort_flag, p.status)) ||
-                            (first &&
-                             !mbar_wait_bounded(&q_full[wq.sg & 1], (uint32_t)(wq.sg >> 1) & 1u, &abort_flag, p.status)))
-                            return false;
+                    const auto scores_ready = [&] {
+                        const int it = wq.it;
+                        return mbar_test(&k_full[it % kKStages], (uint32_t)(it / kKStages) & 1u) &&
+                               (it < 2 || mbar_test(&pv_done[it & 1], (uint32_t)((it - 2) >> 1) & 1u)) &&
+                               (!wq.first || mbar_test(&q_full[wq.sg & 1], (uint32_t)(wq.sg >> 1) & 1u));
+                    };
+                    const auto scores = [&] {
+                        const int b = wq.it & 1, s = wq.it % kKStages;
                         tc_fence_after();
                         const uint32_t k_base = smem_u32(sK + (size_t)s * kTile);
                         const uint32_t q_col = tmem + kColQ + (wq.sg & 1) * (kD / 2);
@@ -586,37 +584,56 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                         tc_commit(&s_full[b]);
                         tc_commit(&k_empty[s]);
                         ++wq.j;
-                        return true;
+                        if (++wq.it < all)
+                            next(wq);
                     };
                     uint64_t *const p_ready = p.expire_wait ? never_bar : p_full;
-                    const auto outputs = [&](int it) {
-                        const bool first = step(wp);
-                        const int b = it & 1, s = it % kVStages;
-                        if (!mbar_wait_bounded(&p_ready[b], (uint32_t)(it >> 1) & 1u, &abort_flag, p.status) ||
-                            (first && wp.sg > 0 &&
-                             !mbar_wait_bounded(&o_free[(wp.sg - 1) & 1], (uint32_t)((wp.sg - 1) >> 1) & 1u, &abort_flag,
-                                                p.status)) ||
-                            !mbar_wait_bounded(&v_full[s], (uint32_t)(it / kVStages) & 1u, &abort_flag, p.status))
-                            return false;
+                    const auto outputs_ready = [&] {
+                        const int it = wp.it;
+                        return mbar_test(&p_ready[it & 1], (uint32_t)(it >> 1) & 1u) &&
+                               (!wp.first || wp.sg == 0 ||
+                                mbar_test(&o_free[(wp.sg - 1) & 1], (uint32_t)((wp.sg - 1) >> 1) & 1u)) &&
+                               mbar_test(&v_full[it % kVStages], (uint32_t)(it / kVStages) & 1u);
+                    };
+                    const auto outputs = [&] {
+                        const int b = wp.it & 1, s = wp.it % kVStages;
                         tc_fence_after();
                         const uint32_t v_base = smem_u32(sV + (size_t)s * kTile);
 #pragma unroll
                         for (int ks = 0; ks < kBN / 16; ++ks)
                             tc_mma_f16_ts(tmem + kColO, tmem + kColS + b * 128 + (ks >> 2) * 64 + (ks & 3) * 8,
                                           smem_desc_sw128(v_base + ks * 2048, kAtom, 1024), idesc<kF16>(kD, true),
-                                          (first && ks == 0) ? 0u : 1u);
+                                          (wp.first && ks == 0) ? 0u : 1u);
                         tc_commit(&v_empty[s]);
                         tc_commit(&pv_done[b]);
                         ++wp.j;
-                        return true;
+                        if (++wp.it < all)
+                            next(wp);
                     };
-                    bool ok = all == 0 || scores(0);
-                    for (int it = 0; ok && it < all; ++it)
-                        ok = (it + 1 == all || scores(it + 1)) && outputs(it);
+                    if (all > 0)
+                        next(wq), next(wp);
+                    long long idle = cycles();
+                    while (wp.it < all) {
+                        if (outputs_ready()) {  // (tile `it`'s weights are there, so its scores have been issued)
+                            outputs();
+                        } else if (wq.it < all && scores_ready()) {
+                            scores();
+                        } else {
+                            if (*const_cast<volatile int *>(&abort_flag))
+                                break;
+                            if (cycles() - idle > kWaitLimitCycles) {
+                                *const_cast<volatile int *>(&abort_flag) = 1;
+                                atomicOr(p.status, kStatusTimeout);
+                                break;
+                            }
+                            continue;
+                        }
+                        idle = cycles();
+                    }
                     tc_commit(&drain_bar);
                 }
             } else {
-                // ------------------------------------------------ most of V; warp 0 copies K's tiles, warp 1 V's
+                // ------------------------------------------------ V; warp 0 copies K's tiles, warp 1 V's
                 const bool is_v = warp == 1;
                 uint64_t *full = packed_full[is_v], *empty = packed_empty[is_v];
                 uint8_t *ring = packed + (is_v ? kPackedStages * kPacked : 0);
@@ -625,20 +642,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                 const bool box = lane < 1 << pages_log2;
                 Cursor cur;
                 cur.start(s_cta, t1, reqs, p.Hkv);
-                struct Page {
-                    int id;
-                    bool inside;  // the request has slots in it
-                };
-                const auto first_slot = [&](int j) {
-                    return tile_key(j, cur.r.a0, cur.r.n1, cur.r.b0) + (lane << p.page_log2);
-                };
-                const auto page_of = [&](int j) {
-                    const int slot = first_slot(j), at = slot >> p.page_log2;
-                    Page x{-1, box && slot < cur.r.L + cur.r.n};
-                    if (x.inside && at < p.max_pages)
-                        x.id = p.table[(size_t)cur.r.b * p.max_pages + at];
-                    return x;
-                };
                 const auto report_hole = [&](int slot) {
                     const int window = static_cast<const PlanHeader *>(p.plan)->window, past = slot + keys;
                     const int lo_min = window > 0 ? max(cur.r.begin, cur.r.L - window + 1) : cur.r.begin;
@@ -646,59 +649,68 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                         (window > 0 && past > cur.r.begin && slot < min(cur.r.far_end, cur.r.L)))
                         atomicOr(p.status, kStatusBounds);
                 };
+                // of the segment that is being copied: where its pages lie, its tile and past its last one; this
+                // lane's page of the next tile, looked up a tile ahead
+                const int32_t *table = nullptr;
+                const uint8_t *pages = nullptr;
                 Seg g{0, 0, 0};
-                long long t = t0;
-                int j = 0, copied = 0;
-                Page page{-1, false};
+                int j = 0, past = 0, copied = 0, id = -1, slot = 0;
+                const auto look_up = [&] {
+                    slot = tile_key(j, cur.r.a0, cur.r.n1, cur.r.b0) + (lane << p.page_log2);
+                    const int at = slot >> p.page_log2;
+                    id = -1;
+                    if (box && slot < past && at < p.max_pages)
+                        id = table[at];
+                };
                 const auto copy_tile = [&] {  // the next one, once its stage is free
-                    if (j == g.n) {
-                        t += g.n;
+                    if (copied == 0 || j == g.j0 + g.n) {
+                        const long long t = t0 + copied;
                         cur.seek(t, p.Hkv);
                         g = seg_at(cur, t);
-                        j = 0;
-                        page = page_of(g.j0);
+                        j = g.j0;
+                        past = cur.r.L + cur.r.n;
+                        table = p.table + (size_t)cur.r.b * p.max_pages;
+                        pages = (is_v ? p.v_pages : p.k_pages) + g.head * p.head_stride;
+                        look_up();
                     }
-                    const Page next = j + 1 < g.n ? page_of(g.j0 + j + 1) : Page{-1, false};
                     const int s = copied % kPackedStages;
                     if (!warp_agrees(mbar_wait_bounded(&empty[s], ((uint32_t)(copied / kPackedStages) & 1u) ^ 1u,
                                                        &abort_flag, p.status)))
                         return false;
                     // a page's block, or a tile's part of its codes and of its scales; nothing for holes
-                    const bool there = page.inside && (unsigned)page.id < (unsigned)p.n_pages;
-                    const uint32_t holes = __ballot_sync(0xffffffffu, page.inside && !there);
-                    const int pieces = __popc(__ballot_sync(0xffffffffu, there));
+                    const bool inside = box && slot < past, there = inside && (unsigned)id < (unsigned)p.n_pages;
+                    const uint32_t found = __ballot_sync(0xffffffffu, there);
+                    const uint32_t holes = __ballot_sync(0xffffffffu, inside) & ~found;
                     if (lane == 0) {
                         packed_holes[is_v][s] = holes;
-                        mbar_arrive_expect_tx(&full[s], pieces * keys * row_bytes(kD));
+                        mbar_arrive_expect_tx(&full[s], __popc(found) * keys * row_bytes(kD));
                     }
                     __syncwarp();
                     if (there) {
-                        const uint8_t *src = (is_v ? p.v_pages : p.k_pages) +
-                                             ((unsigned long long)(unsigned)page.id * p.page_units << 4) +
-                                             g.head * p.head_stride;
-                        uint8_t *dst = ring + (size_t)s * kPacked + lane * keys * row_bytes(kD);
+                        const uint8_t *src = pages + ((unsigned long long)(unsigned)id * p.page_units << 4);
+                        uint8_t *dst = ring + s * kPacked + lane * keys * row_bytes(kD);
                         if (p.page_log2 <= 7) {
                             bulk_load(dst, src, keys * row_bytes(kD), &full[s]);
                         } else {
-                            const int at = first_slot(g.j0 + j) & ((1 << p.page_log2) - 1);
+                            const int at = slot & ((1 << p.page_log2) - 1);
                             bulk_load(dst, src + at * code_bytes(kD), kBN * code_bytes(kD), &full[s]);
                             bulk_load(dst + kBN * code_bytes(kD),
                                       src + ((long long)code_bytes(kD) << p.page_log2) + at * scale_bytes(kD),
                                       kBN * scale_bytes(kD), &full[s]);
                         }
                     }
-                    if (page.inside && !there && !is_v)
-                        report_hole(first_slot(g.j0 + j));
-                    page = next;
-                    ++j;
+                    if (holes && inside && !there && !is_v)
+                        report_hole(slot);
                     ++copied;
+                    if (++j < g.j0 + g.n)
+                        look_up();
                     return true;
                 };
                 bool ok = true;
                 for (int it = 0; ok && it < all; ++it) {
                     while (ok && warp < 2 && copied < min(all, it + kPackedStages))
                         ok = copy_tile();
-                    ok = ok && unpack(true, it, warp * kShare, warp < 2 ? kShare : 2 * kShare);
+                    ok = ok && unpack(true, it, warp * kShare, warp < 2 ? kShare : kBlocks - 2 * kShare);
                 }
                 if (!ok && lane == 0 && warp < 2)
                     for (int x = max(copied - kPackedStages, 0); x < copied; ++x)
@@ -1160,20 +1172,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             if (lane == 0)
                 mbar_arrive(&q_full[sg & 1]);
         };
-        // 4-bit pages: tiles unpacked so far
-        [[maybe_unused]] int k_done = 0, v_done = 0;
-        // V up to tile n (not n itself), K up to the one after it: a tile's K before the previous tile's V
+        // 4-bit pages: K's tiles unpacked so far
+        [[maybe_unused]] int k_done = 0;
         [[maybe_unused]] const auto unpack_to = [&](int n) {
-            const int all = (int)(t1 - t0);
-            n = min(n, all);
-            while (v_done < n) {
-                const bool is_v = k_done >= min(v_done + 2, all);
-                if (!unpack(is_v, is_v ? v_done : k_done, is_v ? kBlocks - 4 + q4 : q4 * (kBlocks / 4),
-                            is_v ? 1 : kBlocks / 4))
+            for (n = min(n, (int)(t1 - t0)); k_done < n; ++k_done)
+                if (!unpack(false, k_done, q4 * (kBlocks / 4), kBlocks / 4))
                     return false;
-                v_done += is_v;
-                k_done += !is_v;
-            }
             return true;
         };
         long long t = t0;
@@ -1204,9 +1208,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
             }
             const long long last = it - 1;
             if constexpr (kQ4) {
-                // through the next unit's first tile: its products wait for this unit's output to be read, its
-                // scores do not
-                if (!unpack_to((int)it + 1))
+                // through the next unit's first two tiles: their scores do not wait for this unit's output to be read
+                if (!unpack_to((int)it + 2))
                     break;
             }
             if (!warp_agrees(mbar_wait_bounded(&ml_full[sg & 1], (uint32_t)(sg >> 1) & 1u, &abort_flag, p.status)))
