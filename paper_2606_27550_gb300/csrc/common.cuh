@@ -132,6 +132,18 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t *bar, uint32_t parity)
     return ok != 0;
 }
 
+// One lane of a whole warp.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(one)::"memory");
+    return one != 0;
+}
+
 // Whether it has completed, without a wait.
 __device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity)
 {

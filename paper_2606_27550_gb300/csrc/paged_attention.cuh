@@ -542,96 +542,107 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
         if constexpr (kQ4) {
             const int all = (int)(t1 - t0);
             if (warp == 3) {
-                if (lane == 0) {
-                    // -------------------------------------------- both products, whichever is ready
-                    struct Walk {
-                        Cursor cur;
-                        Seg g{0, 0, 0};
-                        long long t;
-                        int it = 0, j = 0, sg = -1;
-                        bool first = false;  // tile `it` begins a segment
-                    } wq, wp;
-                    wq.cur.start(s_cta, t1, reqs, p.Hkv);
-                    wp.cur.start(s_cta, t1, reqs, p.Hkv);
-                    wq.t = wp.t = t0;
-                    const auto next = [&](Walk &w) {
-                        w.first = w.j == w.g.n;
-                        if (!w.first)
-                            return;
-                        w.t += w.g.n;
-                        w.cur.seek(w.t, p.Hkv);
-                        w.g = seg_at(w.cur, w.t);
-                        w.j = 0;
-                        ++w.sg;
-                    };
-                    const auto scores_ready = [&] {
-                        const int it = wq.it;
-                        return mbar_test(&k_full[it % kKStages], (uint32_t)(it / kKStages) & 1u) &&
-                               (it < 2 || mbar_test(&pv_done[it & 1], (uint32_t)((it - 2) >> 1) & 1u)) &&
-                               (!wq.first || mbar_test(&q_full[wq.sg & 1], (uint32_t)(wq.sg >> 1) & 1u));
-                    };
-                    const auto scores = [&] {
-                        const int b = wq.it & 1, s = wq.it % kKStages;
-                        tc_fence_after();
-                        const uint32_t k_base = smem_u32(sK + (size_t)s * kTile);
-                        const uint32_t q_col = tmem + kColQ + (wq.sg & 1) * (kD / 2);
+                // ------------------------------------------------ both products, whichever is ready.  The whole warp
+                // goes through this (what it decides by is voted on) and one lane issues: addresses and descriptors
+                // then stay in uniform registers
+                struct Walk {
+                    Cursor cur;
+                    Seg g{0, 0, 0};
+                    long long t;
+                    int it = 0, j = 0, sg = -1;
+                    bool first = false;  // tile `it` begins a segment
+                } wq, wp;
+                wq.cur.start(s_cta, t1, reqs, p.Hkv);
+                wp.cur.start(s_cta, t1, reqs, p.Hkv);
+                wq.t = wp.t = t0;
+                const auto next = [&](Walk &w) {
+                    w.first = w.j == w.g.n;
+                    if (!w.first)
+                        return;
+                    w.t += w.g.n;
+                    w.cur.seek(w.t, p.Hkv);
+                    w.g = seg_at(w.cur, w.t);
+                    w.g.n = __shfl_sync(0xffffffffu, w.g.n, 0);
+                    w.j = 0;
+                    ++w.sg;
+                };
+                const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+                const uint64_t k_desc = smem_desc_sw128(smem_u32(sK), 0, 1024), v_desc = smem_desc_sw128(smem_u32(sV), kAtom, 1024);
+                const auto scores_ready = [&] {
+                    const int it = wq.it;
+                    return warp_agrees(mbar_test(&k_full[it % kKStages], (uint32_t)(it / kKStages) & 1u) &&
+                                       (it < 2 || mbar_test(&pv_done[it & 1], (uint32_t)((it - 2) >> 1) & 1u)) &&
+                                       (!wq.first || mbar_test(&q_full[wq.sg & 1], (uint32_t)(wq.sg >> 1) & 1u)));
+                };
+                const auto scores = [&] {
+                    const int b = wq.it & 1, s = wq.it % kKStages;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t q_col = tm + kColQ + (wq.sg & 1) * (kD / 2);
+                        const uint64_t desc = k_desc + (uint32_t)(s * (kTile >> 4));
 #pragma unroll
-                        for (int kk = 0; kk < kD / 16; ++kk) {
-                            const uint32_t off = (uint32_t)(kk >> 2) * kAtom + (uint32_t)(kk & 3) * 32;
-                            tc_mma_f16_ts(tmem + kColS + b * 128, q_col + kk * 8, smem_desc_sw128(k_base + off, 0, 1024),
-                                          idesc<kF16>(kBN, false), kk > 0 ? 1u : 0u);
-                        }
+                        for (int kk = 0; kk < kD / 16; ++kk)
+                            tc_mma_f16_ts(tm + kColS + b * 128, q_col + kk * 8,
+                                          desc + (((kk >> 2) * kAtom + (kk & 3) * 32) >> 4), idesc<kF16>(kBN, false),
+                                          kk > 0 ? 1u : 0u);
                         tc_commit(&s_full[b]);
                         tc_commit(&k_empty[s]);
-                        ++wq.j;
-                        if (++wq.it < all)
-                            next(wq);
-                    };
-                    uint64_t *const p_ready = p.expire_wait ? never_bar : p_full;
-                    const auto outputs_ready = [&] {
-                        const int it = wp.it;
-                        return mbar_test(&p_ready[it & 1], (uint32_t)(it >> 1) & 1u) &&
-                               (!wp.first || wp.sg == 0 ||
-                                mbar_test(&o_free[(wp.sg - 1) & 1], (uint32_t)((wp.sg - 1) >> 1) & 1u)) &&
-                               mbar_test(&v_full[it % kVStages], (uint32_t)(it / kVStages) & 1u);
-                    };
-                    const auto outputs = [&] {
-                        const int b = wp.it & 1, s = wp.it % kVStages;
-                        tc_fence_after();
-                        const uint32_t v_base = smem_u32(sV + (size_t)s * kTile);
+                    }
+                    __syncwarp();
+                    ++wq.j;
+                    if (++wq.it < all)
+                        next(wq);
+                };
+                uint64_t *const p_ready = p.expire_wait ? never_bar : p_full;
+                const auto outputs_ready = [&] {
+                    const int it = wp.it;
+                    return warp_agrees(mbar_test(&p_ready[it & 1], (uint32_t)(it >> 1) & 1u) &&
+                                       (!wp.first || wp.sg == 0 ||
+                                        mbar_test(&o_free[(wp.sg - 1) & 1], (uint32_t)((wp.sg - 1) >> 1) & 1u)) &&
+                                       mbar_test(&v_full[it % kVStages], (uint32_t)(it / kVStages) & 1u));
+                };
+                const auto outputs = [&] {
+                    const int b = wp.it & 1, s = wp.it % kVStages;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t desc = v_desc + (uint32_t)(s * (kTile >> 4));
+                        const uint32_t fresh = wp.first ? 0u : 1u;
 #pragma unroll
                         for (int ks = 0; ks < kBN / 16; ++ks)
-                            tc_mma_f16_ts(tmem + kColO, tmem + kColS + b * 128 + (ks >> 2) * 64 + (ks & 3) * 8,
-                                          smem_desc_sw128(v_base + ks * 2048, kAtom, 1024), idesc<kF16>(kD, true),
-                                          (wp.first && ks == 0) ? 0u : 1u);
+                            tc_mma_f16_ts(tm + kColO, tm + kColS + b * 128 + (ks >> 2) * 64 + (ks & 3) * 8,
+                                          desc + ((ks * 2048) >> 4), idesc<kF16>(kD, true), ks == 0 ? fresh : 1u);
                         tc_commit(&v_empty[s]);
                         tc_commit(&pv_done[b]);
-                        ++wp.j;
-                        if (++wp.it < all)
-                            next(wp);
-                    };
-                    if (all > 0)
-                        next(wq), next(wp);
-                    long long idle = cycles();
-                    while (wp.it < all) {
-                        if (outputs_ready()) {  // (tile `it`'s weights are there, so its scores have been issued)
-                            outputs();
-                        } else if (wq.it < all && scores_ready()) {
-                            scores();
-                        } else {
-                            if (*const_cast<volatile int *>(&abort_flag))
-                                break;
-                            if (cycles() - idle > kWaitLimitCycles) {
-                                *const_cast<volatile int *>(&abort_flag) = 1;
-                                atomicOr(p.status, kStatusTimeout);
-                                break;
-                            }
-                            continue;
-                        }
-                        idle = cycles();
                     }
-                    tc_commit(&drain_bar);
+                    __syncwarp();
+                    ++wp.j;
+                    if (++wp.it < all)
+                        next(wp);
+                };
+                if (all > 0)
+                    next(wq), next(wp);
+                long long idle = cycles();
+                while (wp.it < all) {
+                    if (outputs_ready()) {  // (tile `it`'s weights are there, so its scores have been issued)
+                        outputs();
+                    } else if (wq.it < all && scores_ready()) {
+                        scores();
+                    } else {
+                        if (!warp_agrees(*const_cast<volatile int *>(&abort_flag) == 0))
+                            break;
+                        if (!warp_agrees(cycles() - idle <= kWaitLimitCycles)) {
+                            *const_cast<volatile int *>(&abort_flag) = 1;
+                            if (lane == 0)
+                                atomicOr(p.status, kStatusTimeout);
+                            break;
+                        }
+                        continue;
+                    }
+                    idle = cycles();
                 }
+                if (elect_one())
+                    tc_commit(&drain_bar);
+                __syncwarp();
             } else {
                 // ------------------------------------------------ V; warp 0 copies K's tiles, warp 1 V's
                 const bool is_v = warp == 1;
