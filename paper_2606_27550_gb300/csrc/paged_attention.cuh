@@ -501,10 +501,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const bool few = kQ4 && s_rows <= kFewRows;  // (all threads of the CTA alike)
     const uint32_t tmem = tmem_slot;
     const long long t0 = s_ok ? s_cta.t0 : 0, t1 = s_ok ? s_cta.t1 : 0;
     const PlanReq *reqs = plan_reqs(p.plan);
+    // Few rows, unless the CTA's share is short: their way there and the join of 16 runs cost 7 us more than a tile's
+    // way through the tensor cores (4 rows of 8 kv heads at 2000 keys: 18.2 and 16.8 us, at 8000 keys 23.7 and
+    // 26.6, at 131000 keys 55 and 107).  All threads of the CTA alike.
+    const bool few = kQ4 && s_rows <= kFewRows && t1 - t0 > kFewTiles;
 
     // 4-bit pages: this warp's blocks of tile i (of K or V)
     [[maybe_unused]] const auto unpack = [&](bool is_v, int i, int first, int n) {
@@ -527,16 +530,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     };
     // K's blocks lie with warps 8-11, V's with 0-2 so that none takes much longer than the others: copying a tile
     // costs warps 0 and 1 as much as four blocks or so
-    constexpr int kBlocks = kTileBlocks<kD>, kShare = kBlocks == 16 ? 3 : 1;  // of V, for warps 0 and 1
+    constexpr int kBlocks = kTileBlocks<kD>, kShare = kBlocks / 4;  // of V, for warps 0 and 1
     if (kQ4 && few) {
         if constexpr (kQ4) {
             FewSmem<kD> &sm = *reinterpret_cast<FewSmem<kD> *>(smem);
-            if (s_ok && t0 < t1) {
-                if (s_rows <= 8)
-                    few_rows<kD, kF16, kForm, 1>(p, s_cta, sm, &abort_flag, &never_bar[0]);
-                else
-                    few_rows<kD, kF16, kForm, 2>(p, s_cta, sm, &abort_flag, &never_bar[0]);
-            }
+            few_rows<kD, kF16, kForm>(p, s_cta, sm, &abort_flag, &never_bar[0]);
         }
     } else if (kQ4 && warp < 4) {
         if constexpr (kQ4) {

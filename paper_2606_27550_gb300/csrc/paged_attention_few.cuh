@@ -1,9 +1,9 @@
-// paged_attention_few.cuh -- the attention over 4-bit pages for units of up to 16
-// query rows per kv head: single tokens, chains and small trees of drafts.
+// paged_attention_few.cuh -- the attention over 4-bit pages for units of up to 8
+// query rows per kv head: single tokens and the shortest chains of drafts.
 //
 // With so few rows the bytes bound, and a score tile of 128 rows would be work for
 // rows that are not there.  So keys lie on the rows of the products here and
-// queries on their columns (8 or 16), in registers:
+// queries on their 8 columns, in registers:
 //   S^T = K Q^T   16 keys x 8 queries x 16 elements per mma
 //   O^T += V^T P^T   16 elements x 8 queries x 16 keys
 // Any order of the summed index will do, as long as both operands have it.  For
@@ -26,14 +26,15 @@ namespace tv {
 
 namespace {
 
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 8;
+constexpr int kFewTiles = 2;  // of a CTA: with so many or fewer, as for many rows
 constexpr int kFewKeys = 32;  // of a piece
 constexpr int kFewSegs = 8;  // units that a warp lays out at a time
 constexpr int kFewWarps = kThreads / 32;
 
 constexpr int few_stages(int d)
 {
-    return d == 64 ? 4 : 2;
+    return d == 64 ? 6 : 3;
 }
 
 // The pieces of one unit in a warp's run.
@@ -66,9 +67,8 @@ struct FewSmem {
     static constexpr int kStage = 2 * kFewKeys * row_bytes(kD), kRing = few_stages(kD) * kStage;
     union {
         uint8_t ring[kFewWarps][kRing];
-        float4 last[kFewWarps][2 * kD / 16][32];  // O^T of the runs' last parts, fragment by fragment
+        float4 last[kFewWarps][kD / 16][32];  // O^T of the runs' last parts, fragment by fragment
     };
-    uint2 query[kFewWarps][kD / 8][32];  // with 16 columns: the queries as operands (8 stay in registers)
     FewRow row[kFewWarps][kFewRows];
     FewSeg seg[kFewWarps][kFewSegs];
     FewPart part[kFewWarps][2];
@@ -113,8 +113,7 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x)
     return y;
 }
 
-// kN: columns of 8 queries.
-template <int kD, bool kF16, int kForm, int kN>
+template <int kD, bool kF16, int kForm>
 __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta, FewSmem<kD> &sm, int *abort_flag,
                                          uint64_t *never_bar)
 {
@@ -284,8 +283,8 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
     }
     if (lane < 2)
         sm.part[warp][lane] = FewPart{kNoUnit, 0, 0, 0, 0, 0, 0};
-    float o[kTilesD][kN][4];
-    float m[kN][2], l[kN][2];  // of columns 8 n + 2 t and the one after it; l: this thread's keys
+    float o[kTilesD][4];
+    float m[2], l[2];          // of columns 2 t and 2 t + 1; l: this thread's keys
     bool last_here = false;    // o, m and l are the run's last part
     int n_parts = 0;
     for (int piece = run0; piece < run1; head0 += kFewSegs) {
@@ -343,40 +342,23 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
             const int gap = seg.first + 4 * seg.r.n1, to = seg.to;
             const int key_a = seg.r.a0 * kBN - kFewKeys * seg.first;
             const int key_b = (seg.r.b0 - seg.r.n1) * kBN - kFewKeys * seg.first;
-            // queries of columns g (and 8 + g) in the order of the keys' elements
-            constexpr bool kKept = kN == 1;  // 16 columns: 32 registers that the output needs
-            uint32_t q[kKept ? kD / 16 : 1][2];
-            const uint32_t q_at = smem_u32(sm.query[warp]) + 8 * lane;
-#pragma unroll
-            for (int n = 0; n < kN; ++n) {
-                const long long at = row_at(seg, 8 * n + g);
+            // the query of column g in the order of the keys' elements
+            uint32_t q[kD / 16][2];
+            {
+                const long long at = row_at(seg, g);
                 const uint4 *src = reinterpret_cast<const uint4 *>(p.q + max(at, 0ll) * kD + t * (kD / 4));
 #pragma unroll
                 for (int i = 0; i < kD / 32; ++i) {
                     const uint4 x = code_order(at >= 0 ? src[i] : make_uint4(0, 0, 0, 0));
-                    if constexpr (kKept) {
-                        q[2 * i][0] = x.x, q[2 * i][1] = x.y;
-                        q[2 * i + 1][0] = x.z, q[2 * i + 1][1] = x.w;
-                    } else {
-                        sm.query[warp][4 * i + n][lane] = make_uint2(x.x, x.y);
-                        sm.query[warp][4 * i + 2 + n][lane] = make_uint2(x.z, x.w);
-                    }
+                    q[2 * i][0] = x.x, q[2 * i][1] = x.y;
+                    q[2 * i + 1][0] = x.z, q[2 * i + 1][1] = x.w;
                 }
             }
-            const auto query = [&](int step, int n) {
-                if constexpr (kKept)
-                    return make_uint2(q[step][0], q[step][1]);
-                else
-                    return lds64(q_at + (2 * step + n) * 256);
-            };
             const bool known = stage(seg);
+            m[0] = m[1] = -INFINITY, l[0] = l[1] = 0.f;
 #pragma unroll
-            for (int n = 0; n < kN; ++n) {
-                m[n][0] = m[n][1] = -INFINITY, l[n][0] = l[n][1] = 0.f;
-#pragma unroll
-                for (int j = 0; j < kTilesD; ++j)
-                    o[j][n][0] = o[j][n][1] = o[j][n][2] = o[j][n][3] = 0.f;
-            }
+            for (int j = 0; j < kTilesD; ++j)
+                o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
 
             for (; piece < to; ++piece) {
                 if (p.expire_wait)
@@ -393,7 +375,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                         const int slot = key0 + key;
                         return slot < end && slot >= begin && (slot >= lo_min || slot < far);
                     };
-                    float s[2][kN][4] = {};
+                    float s[2][4] = {};
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         uint32_t w[2][kD / 32];
@@ -418,141 +400,111 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                             dequant_four<kF16>(w[1][i], sc[1], y);
 #pragma unroll
                             for (int h = 0; h < 2; ++h)
-#pragma unroll
-                                for (int n = 0; n < kN; ++n) {
-                                    const uint2 z = query(2 * i + h, n);
-                                    mma_16x8x16<kF16>(s[b][n], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1], z.x, z.y);
-                                }
+                                mma_16x8x16<kF16>(s[b], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1], q[2 * i + h][0],
+                                                  q[2 * i + h][1]);
                         }
                     }
-                    // scores: element c of s[b][n] is key 16 b + 8 (c / 2) + key_k, column 8 n + 2 t + c % 2
-                    auto visible = [&](int slot, const FewRow &r) {
-                        if (slot < L)
-                            return slot >= r.lo || (slot >= begin && slot < far);
-                        return slot - L < 64 && ((r.anc >> (slot - L)) & 1);
-                    };
+                    // scores: element c of s[b] is key 16 b + 8 (c / 2) + key_k, column 2 t + c % 2
                     constexpr float kHidden = kForm == kCap ? INFINITY : -INFINITY;  // z = -inf
-                    uint32_t sees = 0xffffffffu;  // bit 8 n + 4 b + c... of this thread's scores
+                    uint32_t sees = 0xffu;  // bit 4 b + c of this thread's scores
                     if constexpr (masked) {
                         sees = 0;
 #pragma unroll
-                        for (int n = 0; n < kN; ++n)
-#pragma unroll
-                            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                                for (int c = 0; c < 4; ++c)
-                                    if (visible(key0 + 16 * b + 8 * (c >> 1) + key_k, rows[8 * n + 2 * t + (c & 1)]))
-                                        sees |= 1u << (8 * n + 4 * b + c);
+                        for (int x = 0; x < 8; ++x) {
+                            const FewRow &r = rows[2 * t + (x & 1)];
+                            const int slot = key0 + 8 * (x >> 1) + key_k;
+                            const bool see = slot < L ? slot >= r.lo || (slot >= begin && slot < far)
+                                                      : slot - L < 64 && ((r.anc >> (slot - L)) & 1);
+                            sees |= see ? 1u << x : 0u;
+                        }
                     }
                     if constexpr (kForm != kPlain) {
                         if (kForm == kCap || p.cap > 0.f) {
                             // four of one row together: what is not a number there makes that row none anyway,
                             // unless it is hidden
 #pragma unroll
-                            for (int n = 0; n < kN; ++n)
+                            for (int c = 0; c < 2; ++c) {
+                                uint32_t r[4];
 #pragma unroll
-                                for (int c = 0; c < 2; ++c) {
-                                    uint32_t r[4];
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i) {
-                                        const int b = i >> 1, e = c + 2 * (i & 1);
-                                        r[i] = !masked || ((sees >> (8 * n + 4 * b + e)) & 1u) ? __float_as_uint(s[b][n][e])
-                                                                                               : 0xff800000u;
-                                    }
-                                    cap_four(r, p.cap_in);
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i)
-                                        s[i >> 1][n][c + 2 * (i & 1)] =
-                                            kForm == kCap ? __uint_as_float(r[i])
-                                                          : fmaf(-2.f * p.cap, __uint_as_float(r[i]), p.cap);
+                                for (int i = 0; i < 4; ++i) {
+                                    const int b = i >> 1, e = c + 2 * (i & 1);
+                                    r[i] = !masked || ((sees >> (4 * b + e)) & 1u) ? __float_as_uint(s[b][e]) : 0xff800000u;
                                 }
+                                cap_four(r, p.cap_in);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+                                    s[i >> 1][c + 2 * (i & 1)] = kForm == kCap
+                                                                     ? __uint_as_float(r[i])
+                                                                     : fmaf(-2.f * p.cap, __uint_as_float(r[i]), p.cap);
+                            }
                         } else {
 #pragma unroll
-                            for (int n = 0; n < kN; ++n)
-#pragma unroll
-                                for (int c = 0; c < 8; ++c)
-                                    s[c >> 2][n][c & 3] *= p.scale;
+                            for (int x = 0; x < 8; ++x)
+                                s[x >> 2][x & 3] *= p.scale;
                         }
                     }
 #pragma unroll
-                    for (int n = 0; n < kN; ++n)
-#pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            float(&z)[4] = s[b][n];
-                            if constexpr (kForm == kBias) {
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    const FewRow &r = rows[8 * n + 2 * t + (c & 1)];
-                                    const int slot = key0 + 16 * b + 8 * (c >> 1) + key_k;
-                                    // in the tree: one step for each node of the row's root path before this one
-                                    const int dist =
-                                        slot <= L ? r.pos - slot
-                                                  : r.pos - L - (slot - L < 64 ? __popcll(r.path & ((1ull << (slot - L)) - 1))
-                                                                               : __popcll(r.path));
-                                    z[c] = fmaf(-r.slope, (float)dist, z[c]);
-                                }
-                            }
-                            if constexpr (masked) {
-#pragma unroll
-                                for (int c = 0; c < 4; ++c)
-                                    z[c] = (sees >> (8 * n + 4 * b + c)) & 1u ? z[c] : kHidden;
-                            }
+                    for (int x = 0; x < 8; ++x) {
+                        float &z = s[x >> 2][x & 3];
+                        if constexpr (kForm == kBias) {
+                            const FewRow &r = rows[2 * t + (x & 1)];
+                            const int slot = key0 + 8 * (x >> 1) + key_k;
+                            // in the tree: one step for each node of the row's root path before this one
+                            const int dist = slot <= L ? r.pos - slot
+                                                       : r.pos - L - (slot - L < 64
+                                                                          ? __popcll(r.path & ((1ull << (slot - L)) - 1))
+                                                                          : __popcll(r.path));
+                            z = fmaf(-r.slope, (float)dist, z);
                         }
+                        if constexpr (masked)
+                            z = (sees >> x) & 1u ? z : kHidden;
+                    }
                     // z = f s + f0; f < 0 where s is a capped score's w
                     const float f = kForm == kCap ? -2.f * p.cap : kForm == kPlain ? p.scale : 1.f;
                     const float f0 = kForm == kCap ? p.cap : 0.f;
-                    float alpha[kN][2];
+                    float alpha[2];
                     bool raise = false;
 #pragma unroll
-                    for (int n = 0; n < kN; ++n)
+                    for (int c = 0; c < 2; ++c) {
+                        float mx;
+                        if constexpr (kForm == kCap) {
+                            mx = fminf(fminf(s[0][c], s[0][c + 2]), fminf(s[1][c], s[1][c + 2]));
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            float mx;
-                            if constexpr (kForm == kCap) {
-                                mx = fminf(fminf(s[0][n][c], s[0][n][c + 2]), fminf(s[1][n][c], s[1][n][c + 2]));
+                            for (int x = 4; x < 32; x *= 2)
+                                mx = fminf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+                        } else {
+                            mx = fmaxf(fmaxf(s[0][c], s[0][c + 2]), fmaxf(s[1][c], s[1][c + 2]));
 #pragma unroll
-                                for (int x = 4; x < 32; x *= 2)
-                                    mx = fminf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-                            } else {
-                                mx = fmaxf(fmaxf(s[0][n][c], s[0][n][c + 2]), fmaxf(s[1][n][c], s[1][n][c + 2]));
-#pragma unroll
-                                for (int x = 4; x < 32; x *= 2)
-                                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-                            }
-                            mx = fmaf(f, mx, f0);
-                            alpha[n][c] = 1.f;
-                            if (mx > m[n][c] + kShift + kGrow) {
-                                alpha[n][c] = m[n][c] == -INFINITY ? 0.f : ex2_approx(m[n][c] - (mx - kShift));
-                                m[n][c] = mx - kShift;
-                                raise = true;
-                            }
+                            for (int x = 4; x < 32; x *= 2)
+                                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
                         }
+                        mx = fmaf(f, mx, f0);
+                        alpha[c] = 1.f;
+                        if (mx > m[c] + kShift + kGrow) {
+                            alpha[c] = m[c] == -INFINITY ? 0.f : ex2_approx(m[c] - (mx - kShift));
+                            m[c] = mx - kShift;
+                            raise = true;
+                        }
+                    }
                     if (__any_sync(0xffffffffu, raise)) {
+                        l[0] *= alpha[0], l[1] *= alpha[1];
 #pragma unroll
-                        for (int n = 0; n < kN; ++n) {
-                            l[n][0] *= alpha[n][0], l[n][1] *= alpha[n][1];
+                        for (int j = 0; j < kTilesD; ++j)
 #pragma unroll
-                            for (int j = 0; j < kTilesD; ++j)
+                            for (int c = 0; c < 4; ++c)
+                                o[j][c] *= alpha[c & 1];
+                    }
+                    uint32_t w[2][2];  // P^T as an operand
+                    const float mu0 = f0 - (m[0] == -INFINITY ? 0.f : m[0]), mu1 = f0 - (m[1] == -INFINITY ? 0.f : m[1]);
 #pragma unroll
-                                for (int c = 0; c < 4; ++c)
-                                    o[j][n][c] *= alpha[n][c & 1];
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int a = 0; a < 2; ++a) {
+                            const float p0 = ex2_approx(fmaf(f, s[b][2 * a], mu0));
+                            const float p1 = ex2_approx(fmaf(f, s[b][2 * a + 1], mu1));
+                            l[0] += p0, l[1] += p1;
+                            w[b][a] = transpose_8x8(pack<kF16>(p0, p1));
                         }
-                    }
-                    uint32_t w[2][kN][2];  // P^T as an operand
-#pragma unroll
-                    for (int n = 0; n < kN; ++n) {
-                        const float mu0 = f0 - (m[n][0] == -INFINITY ? 0.f : m[n][0]);
-                        const float mu1 = f0 - (m[n][1] == -INFINITY ? 0.f : m[n][1]);
-#pragma unroll
-                        for (int b = 0; b < 2; ++b)
-#pragma unroll
-                            for (int a = 0; a < 2; ++a) {
-                                const float p0 = ex2_approx(fmaf(f, s[b][n][2 * a], mu0));
-                                const float p1 = ex2_approx(fmaf(f, s[b][n][2 * a + 1], mu1));
-                                l[n][0] += p0, l[n][1] += p1;
-                                w[b][n][a] = transpose_8x8(pack<kF16>(p0, p1));
-                            }
-                    }
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         uint32_t v[2][2][kD / 64];  // [keys 0-7, 8-15][first key, second][8 codes each]
@@ -586,10 +538,8 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
                                 dequant_four<kF16>(__byte_perm(v[1][0][i], v[1][1][i], sel), sc[1], y);
 #pragma unroll
                                 for (int e = 0; e < 2; ++e)
-#pragma unroll
-                                    for (int n = 0; n < kN; ++n)
-                                        mma_16x8x16<kF16>(o[4 * i + 2 * h + e][n], x[2 * e], x[2 * e + 1], y[2 * e],
-                                                          y[2 * e + 1], w[b][n][0], w[b][n][1]);
+                                    mma_16x8x16<kF16>(o[4 * i + 2 * h + e], x[2 * e], x[2 * e + 1], y[2 * e], y[2 * e + 1],
+                                                      w[b][0], w[b][1]);
                             }
                     }
                 };
@@ -605,55 +555,48 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
 
             // ---- the unit's end here
 #pragma unroll
-            for (int n = 0; n < kN; ++n)
+            for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int x = 4; x < 32; x *= 2)
-                        l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], x);
+                for (int x = 4; x < 32; x *= 2)
+                    l[c] += __shfl_xor_sync(0xffffffffu, l[c], x);
             const bool begins = seg.from == seg.first, ends = seg.to == seg.first + 4 * seg.r.T;
             if (begins && ends) {
-                // columns 8 n + 2 t and the next: kD / 8 elements from (kD / 8) g on
+                // columns 2 t and 2 t + 1: kD / 8 elements from (kD / 8) g on
 #pragma unroll
-                for (int n = 0; n < kN; ++n)
+                for (int c = 0; c < 2; ++c) {
+                    const long long at = row_at(seg, 2 * t + c);
+                    if (at < 0 || !known || !ok)
+                        continue;
+                    const float inv = l[c] == 0.f ? 0.f : kBack / l[c];  // a NaN stays one
+                    uint32_t w[kTilesD];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const long long at = row_at(seg, 8 * n + 2 * t + c);
-                        if (at < 0 || !known || !ok)
-                            continue;
-                        const float lc = l[n][c], inv = lc == 0.f ? 0.f : kBack / lc;  // a NaN stays one
-                        uint32_t w[kTilesD];
+                    for (int j = 0; j < kTilesD; ++j)
+                        w[j] = pack<kF16>(o[j][c] * inv, o[j][c + 2] * inv);
+                    uint4 *dst = reinterpret_cast<uint4 *>(p.out + at * kD + g * (kD / 8));
 #pragma unroll
-                        for (int j = 0; j < kTilesD; ++j)
-                            w[j] = pack<kF16>(o[j][n][c] * inv, o[j][n][c + 2] * inv);
-                        uint4 *dst = reinterpret_cast<uint4 *>(p.out + at * kD + g * (kD / 8));
-#pragma unroll
-                        for (int j = 0; j < kTilesD / 4; ++j)
-                            dst[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-                        if (p.lse && g == 0)
-                            p.lse[at] = lc == 0.f ? -INFINITY : (m[n][c] + log2f(lc)) * kLn2;
-                    }
+                    for (int j = 0; j < kTilesD / 4; ++j)
+                        dst[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+                    if (p.lse && g == 0)
+                        p.lse[at] = l[c] == 0.f ? -INFINITY : (m[c] + log2f(l[c])) * kLn2;
+                }
                 continue;
             }
             // a part: at most two of a run, the second at its end
             if (lane == 0)
-                sm.part[warp][n_parts] = FewPart{seg.first, begins, ends, seg.to == run1, seg.head, seg.r.row0, known ? seg.r.n : 0};
+                sm.part[warp][n_parts] =
+                    FewPart{seg.first, begins, ends, seg.to == run1, seg.head, seg.r.row0, known ? seg.r.n : 0};
             if (g == 0) {
 #pragma unroll
-                for (int n = 0; n < kN; ++n)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        sm.m[warp][n_parts][8 * n + 2 * t + c] = m[n][c];
-                        sm.l[warp][n_parts][8 * n + 2 * t + c] = l[n][c];
-                    }
+                for (int c = 0; c < 2; ++c) {
+                    sm.m[warp][n_parts][2 * t + c] = m[c];
+                    sm.l[warp][n_parts][2 * t + c] = l[c];
+                }
             }
             if (seg.to < run1) {
-                float4 *to = reinterpret_cast<float4 *>(p.part + (size_t)blockIdx.x * 2 * kSlot) + warp * kTilesD * kN * 32;
+                float4 *to = reinterpret_cast<float4 *>(p.part + (size_t)blockIdx.x * 2 * kSlot) + warp * kTilesD * 32;
 #pragma unroll
                 for (int j = 0; j < kTilesD; ++j)
-#pragma unroll
-                    for (int n = 0; n < kN; ++n)
-                        to[(j * kN + n) * 32 + lane] = make_float4(o[j][n][0], o[j][n][1], o[j][n][2], o[j][n][3]);
+                    to[j * 32 + lane] = make_float4(o[j][0], o[j][1], o[j][2], o[j][3]);
             } else {
                 last_here = true;  // the last of the run
             }
@@ -667,21 +610,18 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
     if (last_here) {
 #pragma unroll
         for (int j = 0; j < kTilesD; ++j)
-#pragma unroll
-            for (int n = 0; n < kN; ++n)
-                sm.last[warp][j * kN + n][lane] = make_float4(o[j][n][0], o[j][n][1], o[j][n][2], o[j][n][3]);
+            sm.last[warp][j][lane] = make_float4(o[j][0], o[j][1], o[j][2], o[j][3]);
     }
     __syncthreads();
-    // thread f of kTilesD kN 32 takes fragment f of every unit; at most two of them are also other CTAs', and go to
-    // the slots that the first parts lie in: once all have read those
-    const int frag = threadIdx.x, fj = frag / 32 / kN, fn = frag / 32 % kN;
-    const bool mine = frag < kTilesD * kN * 32;
+    // warp j takes fragment j of every unit, elements (kD / 8) g + 2 j and the next; at most two units are also other
+    // CTAs', and go to the slots that the first parts lie in: once all have read those
+    const bool mine = warp < kTilesD;
     const bool stop = *const_cast<volatile int *>(abort_flag) != 0;  // (nobody waits any more)
-    const float4 *firsts = reinterpret_cast<const float4 *>(p.part + (size_t)blockIdx.x * 2 * kSlot);
+    const float4 *firsts = reinterpret_cast<const float4 *>(p.part + (size_t)blockIdx.x * 2 * kSlot) + threadIdx.x;
     float4 kept[2];
     float kept_m[2][2], kept_l[2][2];
     bool keep[2] = {false, false};
-    for (int x = 0; x < 2 * kFewWarps;) {
+    for (int x = 0; mine && x < 2 * kFewWarps;) {
         const FewPart head = sm.part[x >> 1][x & 1];
         int y = x + 1;
         if (head.unit == kNoUnit) {
@@ -690,60 +630,56 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
         }
         while (y < 2 * kFewWarps && (sm.part[y >> 1][y & 1].unit == head.unit || sm.part[y >> 1][y & 1].unit == kNoUnit))
             ++y;
-        if (mine) {
-            bool ends = false;
-            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-            float M[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-            const int col0 = 8 * fn + 2 * t;
-            for (int z = x; z < y; ++z)
-                if (sm.part[z >> 1][z & 1].unit == head.unit)
+        bool ends = false;
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        float M[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+        for (int z = x; z < y; ++z)
+            if (sm.part[z >> 1][z & 1].unit == head.unit)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    M[c] = fmaxf(M[c], sm.m[z >> 1][z & 1][2 * t + c]);
+#pragma unroll 4
+        for (int z = x; z < y; ++z) {
+            const FewPart &part = sm.part[z >> 1][z & 1];
+            if (part.unit != head.unit)
+                continue;
+            ends = part.ends;
+            const float4 v = part.last ? sm.last[z >> 1][warp][lane] : __ldcg(firsts + (z >> 1) * kTilesD * 32);
+            float f[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float mz = sm.m[z >> 1][z & 1][2 * t + c];
+                f[c] = mz == -INFINITY ? 0.f : ex2_approx(mz - M[c]);
+                sum[c] = fmaf(f[c], sm.l[z >> 1][z & 1][2 * t + c], sum[c]);
+            }
+            a.x = fmaf(f[0], v.x, a.x), a.y = fmaf(f[1], v.y, a.y);
+            a.z = fmaf(f[0], v.z, a.z), a.w = fmaf(f[1], v.w, a.w);
+        }
+        if (head.begins && ends) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                FewSeg s{};
+                s.head = head.head, s.r.n = head.n, s.r.row0 = head.row0;
+                const long long at = row_at(s, 2 * t + c);
+                if (at < 0 || stop)
+                    continue;
+                const float inv = sum[c] == 0.f ? 0.f : kBack / sum[c];
+                *reinterpret_cast<uint32_t *>(p.out + at * kD + g * (kD / 8) + 2 * warp) =
+                    pack<kF16>((c ? a.y : a.x) * inv, (c ? a.w : a.z) * inv);
+                if (p.lse && warp == 0 && g == 0)
+                    p.lse[at] = sum[c] == 0.f ? -INFINITY : (M[c] + log2f(sum[c])) * kLn2;
+            }
+        } else {
+            // of the CTA's first tile on: slot 0, as for many rows
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (i == (head.unit <= 0 ? 0 : 1)) {
+                    keep[i] = true;
+                    kept[i] = a;
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
-                        M[c] = fmaxf(M[c], sm.m[z >> 1][z & 1][col0 + c]);
-#pragma unroll 4
-            for (int z = x; z < y; ++z) {
-                const FewPart &part = sm.part[z >> 1][z & 1];
-                if (part.unit != head.unit)
-                    continue;
-                ends = part.ends;
-                const float4 v = part.last ? sm.last[z >> 1][frag / 32][lane]
-                                           : __ldcg(firsts + (z >> 1) * kTilesD * kN * 32 + frag);
-                float f[2];
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const float mz = sm.m[z >> 1][z & 1][col0 + c];
-                    f[c] = mz == -INFINITY ? 0.f : ex2_approx(mz - M[c]);
-                    sum[c] = fmaf(f[c], sm.l[z >> 1][z & 1][col0 + c], sum[c]);
+                        kept_m[i][c] = M[c], kept_l[i][c] = sum[c];
                 }
-                a.x = fmaf(f[0], v.x, a.x), a.y = fmaf(f[1], v.y, a.y);
-                a.z = fmaf(f[0], v.z, a.z), a.w = fmaf(f[1], v.w, a.w);
-            }
-            if (head.begins && ends) {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    FewSeg s{};
-                    s.head = head.head, s.r.n = head.n, s.r.row0 = head.row0;
-                    const long long at = row_at(s, col0 + c);
-                    if (at < 0 || stop)
-                        continue;
-                    const float inv = sum[c] == 0.f ? 0.f : kBack / sum[c];
-                    *reinterpret_cast<uint32_t *>(p.out + at * kD + g * (kD / 8) + 2 * fj) =
-                        pack<kF16>((c ? a.y : a.x) * inv, (c ? a.w : a.z) * inv);
-                    if (p.lse && fj == 0 && g == 0)
-                        p.lse[at] = sum[c] == 0.f ? -INFINITY : (M[c] + log2f(sum[c])) * kLn2;
-                }
-            } else {
-                // of the CTA's first tile on: slot 0, as for many rows
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (i == (head.unit <= 0 ? 0 : 1)) {
-                        keep[i] = true;
-                        kept[i] = a;
-#pragma unroll
-                        for (int c = 0; c < 2; ++c)
-                            kept_m[i][c] = M[c], kept_l[i][c] = sum[c];
-                    }
-            }
         }
         x = y;
     }
@@ -755,10 +691,10 @@ __device__ __forceinline__ void few_rows(const PagedArgs &p, const PlanCta &cta,
         float *slot = p.part + ((size_t)blockIdx.x * 2 + i) * kSlot;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            const int col = 8 * fn + 2 * t + c;
-            *reinterpret_cast<float2 *>(slot + col * kD + g * (kD / 8) + 2 * fj) =
+            const int col = 2 * t + c;
+            *reinterpret_cast<float2 *>(slot + col * kD + g * (kD / 8) + 2 * warp) =
                 c ? make_float2(kept[i].y * kBack, kept[i].w * kBack) : make_float2(kept[i].x * kBack, kept[i].z * kBack);
-            if (fj == 0 && g == 0) {
+            if (warp == 0 && g == 0) {
                 slot[128 * kD + col] = kept_m[i][c];
                 slot[128 * kD + 128 + col] = kept_l[i][c];
             }
