@@ -744,8 +744,11 @@ def paged_plan(bank, req: Requests, slots, positions, status, plan, pool: PagePo
         _check(rc, "paged_plan")
 
 
-def _rows_of(t, rows: int, heads: int, d: int, dtype, what: str) -> TbRows:
+def _rows_of(t, rows: int, heads: int, d: int, dtype, what: str, dims: int = 3) -> TbRows:
+    """The rows of a (rows, heads, d) tensor, or with dims 4 of the first layer of a (layers, rows, heads, d) one."""
     shape, s = t.shape, t.stride()
+    if dims == 4:
+        shape, s = shape[1:], s[1:]
     if len(s) != 3 or s[2] != 1 or shape[0] < rows or shape[1] != heads or shape[2] != d:
         raise ValueError(f"{what}: shape {tuple(shape)}, ({rows}, {heads}, {d}) expected, rows contiguous")
     if t.dtype is not dtype:
@@ -877,15 +880,14 @@ def paged_kv_load_q4(pages: PagesQ4, slots, k, v, layer: int = 0, stream=None):
     [head_dim] of `layer` and the ones behind it (views of any layer, row and head strides, the same layer stride)."""
     c, dtype = _page_kind(pages, PagesQ4), pages.dtype
     rows, layers, stride = slots.shape[0], 1, 0
-    if len(k.shape) == 4:
+    if len(k.shape) == 4:  # (no k[0]: a view costs more than the rest of the call)
         layers, stride = k.shape[0], k.stride(0)
         if len(v.shape) != 4 or v.shape[0] != layers or (v.stride(0) != stride and layers > 1):
             raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}: one number of layers and one layer stride expected")
         if layers < 1:
             raise ValueError("no layers")
-        k, v = k[0], v[0]
-    ck = _rows_of(k, rows, c.n_kv_heads, c.head_dim, dtype, "k")
-    cv = _rows_of(v, rows, c.n_kv_heads, c.head_dim, dtype, "v")
+    ck = _rows_of(k, rows, c.n_kv_heads, c.head_dim, dtype, "k", len(k.shape))
+    cv = _rows_of(v, rows, c.n_kv_heads, c.head_dim, dtype, "v", len(k.shape))
     rc = load().paged_kv_load_q4(ctypes.byref(c), layer, layers, _arr(slots, _I64, rows, "slots"), rows,
                                  ctypes.byref(ck), ctypes.byref(cv), stride, _stream(stream))
     if rc:
