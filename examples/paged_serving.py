@@ -5,8 +5,9 @@ A small random model (two layers, grouped queries, a rotary embedding) drafts a
 tree for every request, verifies all trees in one pass and keeps the accepted
 paths.  Requests begin with prompts of different lengths, end at different
 times, and give their pages back.  No length is read on the host inside a step.
+With --q4 the cache holds 4 bits an element, and the model norms its heads.
 
-    python examples/paged_serving.py            # needs a GPU and the built library
+    python examples/paged_serving.py [--q4]     # needs a GPU and the built library
 """
 from __future__ import annotations
 
@@ -36,13 +37,14 @@ class Model:
         self.qkv = [weight(self.width, self.width + 2 * kv_heads * head_dim, std=self.width ** -0.5) for _ in range(layers)]
         self.out = [weight(self.width, self.width, std=self.width ** -0.5) for _ in range(layers)]
         self.head = weight(self.width, vocab, std=2.0 * self.width ** -0.5)
+        self.q_norm, self.k_norm = ([1.0 + weight(head_dim, std=0.1) for _ in range(layers)] for _ in range(2))
 
 
 class Server:
-    """The state of a batch of request slots, and its step."""
+    """The state of a batch of request slots, and its step; q4: over a cache of 4 bits, heads normed."""
 
-    def __init__(self, model: Model, batch=4, n_pages=256, page_size=16, max_pages=64, softcap=30.0):
-        self.m, self.B, self.softcap = model, batch, softcap
+    def __init__(self, model: Model, batch=4, n_pages=256, page_size=16, max_pages=64, softcap=30.0, q4=False):
+        self.m, self.B, self.softcap, self.q4 = model, batch, softcap, q4
         dev, i32 = "cuda", torch.int32
         self.bank = tv.Bank(8, torch.cuda.current_device())
         self.parents = [synth.chain(1), synth.rank_product_tree((3, 2, 1), 8), synth.rank_product_tree((4, 3, 2, 1), 26)]
@@ -52,8 +54,9 @@ class Server:
         self.rows = 64 * batch
         self.pool = tv.make_page_pool(n_pages, batch)
         shape = (model.layers, n_pages, model.H, page_size, model.d)
-        self.pages = tv.Pages(torch.empty(shape, dtype=torch.bfloat16, device=dev),
-                              torch.empty(shape, dtype=torch.bfloat16, device=dev))
+        self.pages = (tv.make_pages_q4(*shape, torch.bfloat16) if q4 else
+                      tv.Pages(torch.empty(shape, dtype=torch.bfloat16, device=dev),
+                               torch.empty(shape, dtype=torch.bfloat16, device=dev)))
         self.req = tv.Requests(row_start=torch.zeros(batch + 1, dtype=i32, device=dev),
                                tree=torch.full((batch,), -1, dtype=i32, device=dev),
                                lens=torch.zeros(batch, dtype=i32, device=dev),
@@ -79,13 +82,17 @@ class Server:
         m, rows = self.m, x.shape[0]
         qkv = (x @ m.qkv[layer]).view(rows, m.Hq + 2 * m.H, m.d)
         q = torch.empty((rows, m.Hq, m.d), dtype=x.dtype, device="cuda")
-        tv.paged_kv_store(self.pages, slots, qkv[:, m.Hq:m.Hq + m.H], qkv[:, m.Hq + m.H:], layer=layer,
-                          q=qkv[:, :m.Hq], q_out=q, positions=positions, rope_theta=10000.0)
+        args = dict(layer=layer, q=qkv[:, :m.Hq], q_out=q, positions=positions, rope_theta=10000.0)
+        k, v = qkv[:, m.Hq:m.Hq + m.H], qkv[:, m.Hq + m.H:]
+        if self.q4:
+            tv.paged_kv_store_q4(self.pages, slots, k, v, q_norm=m.q_norm[layer], k_norm=m.k_norm[layer], **args)
+        else:
+            tv.paged_kv_store(self.pages, slots, k, v, **args)
         if not attend:
             return x
         out = torch.zeros_like(q)
-        tv.paged_tree_attention(self.bank, self.req, self.pages, self.plan, q, out, self.ws, layer=layer,
-                                softcap=self.softcap)
+        attention = tv.paged_tree_attention_q4 if self.q4 else tv.paged_tree_attention
+        attention(self.bank, self.req, self.pages, self.plan, q, out, self.ws, layer=layer, softcap=self.softcap)
         return x + out.view(rows, m.width) @ m.out[layer]
 
     def admit(self, prompts):
@@ -134,7 +141,8 @@ class Server:
         tv.logits_process(self.bank, self.req, logits, logits, self.logit_ws, draft=draft, history=self.history,
                           history_len=self.said, prompt_len=self.asked, repetition=self.penalty,
                           presence=self.presence, argmax=argmax)
-        tv.paged_accept(self.bank, self.req, self.pages, self.results, draft=draft, argmax=argmax, vocab=m.vocab)
+        accept = tv.paged_accept_q4 if self.q4 else tv.paged_accept
+        accept(self.bank, self.req, self.pages, self.results, draft=draft, argmax=argmax, vocab=m.vocab)
         self._note(draft)
         return logits, argmax
 
@@ -188,7 +196,7 @@ def drafts(server: Server, trees):
 
 
 def main():
-    server = Server(Model())
+    server = Server(Model(), q4="--q4" in sys.argv[1:])
     server.admit({b: list(range(7 * b + 3, 7 * b + 3 + n)) for b, n in enumerate((5, 40, 17, 100))})
     for step in range(6):
         trees = [(b + step) % 3 for b in range(server.B)]
