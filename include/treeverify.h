@@ -827,15 +827,20 @@ TB_API tb_status paged_kv_store_q4(const tb_pages_q4 *pages, int layer, const in
 /* Reads rows back in 16 bits (a cached prefix for its prompt's attention, a
  * request that moves elsewhere): row r of layer `layer` + i, 0 <= i < n_layers, at
  * k->ptr + i * row_layer_stride + r * row_stride + head * head_stride (strides in
- * elements of pages->dtype, multiples of 8), likewise v; exact.  A slot outside
+ * elements of pages->dtype, multiples of 8), likewise v; exact (what passes the
+ * largest fp16 number, which no stored row does, is an infinity).  A slot outside
  * the pool (-1: padding) leaves its rows as they were; a slot may be named more
- * than once.  n_rows >= 0, n_layers >= 1; one kernel. */
+ * than once.  n_rows >= 0, n_layers >= 1; TB_EUNSUPPORTED for more than 2^30 rows
+ * or 2^20 kv heads.  One kernel. */
 TB_API tb_status paged_kv_load_q4(const tb_pages_q4 *pages, int layer, int n_layers, const int64_t *slots, int n_rows,
                                   const tb_rows *k, const tb_rows *v, int64_t row_layer_stride, tb_stream stream);
 
 /* paged_tree_attention over 4-bit pages: the same formulas, arguments, plan,
  * workspace and status word.  The elements enter the products exactly; a scale
- * of NaN in a slot that a row sees makes that row NaN. */
+ * of NaN in a slot that a row sees makes that row NaN.  Scales above 9216 (bytes
+ * 226 to 254), which no call stores, give no defined value.  TB_EUNSUPPORTED also
+ * for a page stride of 2^36 bytes or more, and for a scale of the scores that
+ * passes 32 bits times 2^20 log2(e). */
 TB_API tb_status paged_tree_attention_q4(const tb_bank *bank, const tb_requests *req, const tb_pages_q4 *pages,
                                          int layer, const void *plan, size_t plan_bytes, const void *q, int n_rows,
                                          int n_q_heads, float scale, float softcap, const float *slopes, void *out,

@@ -19,8 +19,8 @@
 // A tile's 128 slots are 128 / page_size pages (or a part of one): the lanes of a
 // producer warp look their pages up one tile ahead and issue one TMA box each.
 // Pages past the request's end, and ids outside the pool, are addressed past the
-// last page, where TMA fills zeros; such an id where some row looks is reported.  Slots of a landed tile that no row may see (a
-// page's rest behind the last token, before a document's beginning, between the
+// last page, where TMA fills zeros; such an id where some row looks is reported.
+// Slots of a landed tile that no row may see (a page's rest behind the last token, before a document's beginning, between the
 // kept first tokens and the window) can hold anything: their scores are replaced
 // (not multiplied) by -inf, and the softmax threads overwrite their V rows with
 // zeros before P V reads them, since 0 * NaN is NaN.
@@ -47,12 +47,21 @@
 // and 43.6 with packed pairs and one reciprocal for four caps, before holes in the table
 // were reported.
 //
-// 4-bit pages (kQ4): warps 0 and 1 copy pages as they lie into rings of packed
-// tiles of K and V, and warps 8-11 (K) and 0-2 (V) turn them into the tiles above, each element exactly: 32 codes and their scale per
-// thread, eight 16-byte pieces into the swizzled rows.  Warp 3 issues both products.
-// Within 8 elements those stand in the order 0 4 1 5 2 6 3 7, in which two are
-// unpacked at a time; the queries are staged in that order too, and the output's
-// columns put back.
+// 4-bit pages (kQ4), units of few rows: paged_attention_few.cuh.  The others: warps 0
+// and 1 copy pages as they lie into rings of packed tiles of K and V, and warps 8-11 (K)
+// and 0-2 (V) turn them into the tiles above, each element exactly: 32 codes and their
+// scale per thread, four 16-byte pieces into the swizzled rows.  Within 8 elements those
+// stand in the order 0 4 1 5 2 6 3 7, in which four codes come out of one shift; the
+// queries are staged in that order too, and the output's columns put back.  Warp 3 issues
+// both products, whichever is ready.  Bound by the way of a tile through its stages, 2600
+// to 3000 cycles (the 16-bit pages' 2060): the seven warps that unpack it, 16 products that
+// take 1800 to issue and run, and the instruction caches, which five roles' code contends
+// for (a chain of 4 nodes at 131000 keys, 4 query heads on each of 8 kv heads: 92 us, 19 %
+// of a copy's bandwidth; eight ragged trees with capped scores and a window 55 us).  The
+// trees took 81 us with four warps that unpacked both operands in unrolled code, 73 with
+// seven in short loops, 67 with one warp that issues whichever product is ready, 63 with
+// its addresses in uniform registers, 55 with units of 9 to 16 rows here and not among the
+// few.
 #pragma once
 
 #include "paged_q4.cuh"
@@ -325,11 +334,12 @@ struct PackedTile {
     }
 };
 
+template <int kD>
+constexpr int kTileBlocks = kBN * kD / kGroup / 32;
+
 // Part of a packed tile into one of 16-bit elements, by a warp: 32 elements of a key per lane and block, 8 keys
 // of 128 elements or 16 of 64; blocks first to first + n - 1.  holes: the pieces that are not there, whose
 // elements count as zeros.
-template <int kD>
-constexpr int kTileBlocks = kBN * kD / kGroup / 32;
 
 template <int kD, bool kF16>
 __device__ __forceinline__ void unpack_blocks(uint32_t packed, uint32_t tile, const PackedTile &pt, uint32_t holes, int first,
@@ -721,7 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
                         ok = copy_tile();
                     ok = ok && unpack(true, it, warp * kShare, warp < 2 ? kShare : kBlocks - 2 * kShare);
                 }
-                if (!ok && lane == 0 && warp < 2)
+                if (lane == 0 && warp < 2)  // (some other warp may have given up)
                     for (int x = max(copied - kPackedStages, 0); x < copied; ++x)
                         mbar_wait_drain(&full[x % kPackedStages], (uint32_t)(x / kPackedStages) & 1u);
                 __syncwarp();
