@@ -34,11 +34,12 @@ __device__ __forceinline__ float scale_of(uint32_t byte)
     return __half2float(__ushort_as_half((unsigned short)(byte << 7)));
 }
 
-// fl(x / n) for a number n of at most 4 significant bits and its rounded reciprocal: a product and one
-// correction.  y = fl(x inv) is x / n (1 + e) with |e| <= 2^-23, its remainder x - y n is a float, and y plus
-// remainder times inv is x / n but for e^2, 2^-46 of it, before the one rounding.  That cannot round
-// otherwise than x / n does: a midpoint between two floats has 25 bits, times n 29, so that x (24 bits) is
-// never n times a midpoint, and never nearer to one than 2^-29.
+// fl(x / n) for a number n of at most 4 significant bits and its reciprocal to one unit in the last place: a
+// product and one correction.  y = fl(x inv) is x / n (1 + e) with |e| <= 2^-22, its remainder x - y n is a
+// float (a few units of y's last place times n's), and y plus remainder times inv is x / n but for e^2 and
+// e 2^-23, 2^-43 of it, before the one rounding.  That cannot round otherwise than x / n does: a midpoint
+// between two floats has 25 bits, times n 29, so that x (24 bits) is never n times a midpoint, and never nearer
+// to one than 2^-29.
 __device__ __forceinline__ uint64_t quotient_two(uint64_t x, uint64_t minus_n, uint64_t inv)
 {
     const uint64_t y = mul_two(x, inv);
@@ -50,17 +51,19 @@ __device__ __forceinline__ uint32_t scale_byte(float top)
 {
     constexpr float kInv = 1.f / 7.f;
     const float y = __fmul_rn(top, kInv), t = __fmaf_rn(__fmaf_rn(y, -7.f, top), kInv, y);  // as above
-    // up to 4 significant bits; below 2^-14 (byte 8) up to a multiple of 2^-17
-    uint32_t b = ((__float_as_uint(t) + 0xfffffu) >> 20) - ((127 - 15) << 3);
-    if (!(t > 0x1p-14f))
-        b = (uint32_t)ceilf(t * 0x1p17f);
+    // up to 4 significant bits; below 2^-14 (byte 8) up to a multiple of 2^-17, which are the 4 bits of the
+    // sum with 2^-14 (rounded up, which changes nothing about that)
+    const bool small = !(t > 0x1p-14f);
+    const float u = small ? __fadd_ru(t, 0x1p-14f) : t;
+    const uint32_t b = ((__float_as_uint(u) + 0xfffffu) >> 20) - (((small ? 128 : 127) - 15) << 3);
     return top < INFINITY ? min(b, (uint32_t)kMaxScaleByte) : (uint32_t)kNanScaleByte;
 }
 
-// Codes of 8 elements (pairs), the first in the lowest 4 bits; inv = 1 / s rounded (0 where s is 0).
+// Codes of 8 elements (pairs), the first in the lowest 4 bits; inv = 1 / s as quotient_two wants it (0 where s
+// is 0); clamp: s may be the largest scale or NaN.
 __device__ __forceinline__ uint32_t quantize8(const uint64_t (&x)[4], float s, float inv, bool clamp)
 {
-    // adding 1.5 * 2^23 + 8 leaves rint(y) + 8 in the low bits, ties to even; of a NaN, 15
+    // adding 1.5 * 2^23 + 8 leaves rint(y) + 8, at most 15, in the lowest byte, ties to even
     constexpr float kRound = 12582912.f + 8.f;
     uint32_t b[4];  // two codes each
 #pragma unroll
@@ -71,7 +74,7 @@ __device__ __forceinline__ uint32_t quantize8(const uint64_t (&x)[4], float s, f
             y = two(fmaxf(fminf(f.x, 7.f), -7.f), fmaxf(fminf(f.y, 7.f), -7.f));
         }
         const float2 f = halves(add_two(y, two(kRound, kRound)));
-        b[i] = (__float_as_uint(f.y) << 4) + (__float_as_uint(f.x) & 15u);
+        b[i] = (__float_as_uint(f.y) << 4) + __float_as_uint(f.x);  // (of which the lowest byte)
     }
     return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
 }

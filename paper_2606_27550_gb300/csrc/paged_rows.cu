@@ -23,6 +23,7 @@ namespace tv {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kCtas = 4;  // of an SM
 constexpr int kMaxRows = 8;  // rows per CTA
 
 struct RowsArgs {
@@ -115,9 +116,9 @@ template <int kLanes>
 __device__ __forceinline__ float inverse_norm(const uint64_t (&x)[8], float eps, bool normed)
 {
     // two sums, each with what its roundings left
-    uint64_t hi = two(0.f, 0.f), lo = hi;
+    uint64_t hi = mul_two(x[0], x[0]), lo = two(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 1; i < 8; ++i) {
         const uint64_t b = mul_two(x[i], x[i]);  // 11 bits at most: the squares are exact
         const uint64_t s = add_two(hi, b), t = minus(s, hi);
         lo = add_two(lo, add_two(minus(hi, minus(s, t)), minus(b, t)));
@@ -189,15 +190,28 @@ __device__ __forceinline__ float max_or_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
 }
+__device__ __forceinline__ float max_or_nan(float a, float2 b)  // of magnitudes
+{
+    float y;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b.x), "f"(b.y));
+    return y;
+}
+// to one unit in the last place
+__device__ __forceinline__ float reciprocal(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 // Bound by HBM where rows stay in 16 bits: each element is read once and written once (8191 rows of 32 + 2 * 32
 // heads of 128, normed and turned: 74 us, 5.4 TB/s, 80 % of a copy's bandwidth; 87 us with a division for each
 // piece to find its place), and by its instructions where they become 4 bits (the same
-// rows: 92 us, the largest of 32, the scale and 32 corrected quotients on top; 149 us with a division each and
-// one number at a time).  One to eight rows per CTA: the sines serve all of a row's heads, and few rows still
-// reach all SMs (eight trees, 8 kv heads: 6 us).
+// rows: 91 us, 73 without norms; the largest of 32, the scale and 32 corrected quotients on top; 149 us with a
+// division each and one number at a time).  One to eight rows per CTA: the sines serve all of a row's heads, and
+// few rows still reach all SMs (eight trees, 32 + 2 * 8 heads: 5.3 us).
 template <int kD, bool kF16, bool kQ4>
-__global__ void __launch_bounds__(kThreads, 4) k_paged_rows(const __grid_constant__ RowsArgs p)
+__global__ void __launch_bounds__(kThreads, kCtas) k_paged_rows(const __grid_constant__ RowsArgs p)
 {
     constexpr int kHalf = kD / 2, kLanes = kHalf / 8;  // lanes of a head
     __shared__ __align__(16) float s_cos[kMaxRows][kHalf], s_sin[kMaxRows][kHalf];
@@ -206,8 +220,9 @@ __global__ void __launch_bounds__(kThreads, 4) k_paged_rows(const __grid_constan
     pdl_wait();
     pdl_trigger();
     const int r0 = blockIdx.x * p.rows_per_cta, n_rows = min(p.rows_per_cta, p.n_rows - r0);
+    const int threads = blockDim.x;
     const bool norms = p.q_weight || p.k_weight;
-    for (int x = threadIdx.x; x < n_rows; x += kThreads)
+    for (int x = threadIdx.x; x < n_rows; x += threads)
         s_slot[x] = p.slots[r0 + x];
     if (norms && threadIdx.x < kD) {
         const int x = threadIdx.x;
@@ -218,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_paged_rows(const __grid_constan
                 s_weight[i][x] = p.weight_offset + unpack_pair<kF16>(w[i][x]).x;
     }
     if (p.turn)
-        for (int x = threadIdx.x; x < n_rows * kHalf; x += kThreads) {
+        for (int x = threadIdx.x; x < n_rows * kHalf; x += threads) {
             const float2 cs = cos_sin(turn_of(p.rope, r0 + x / kHalf, x % kHalf));
             s_cos[x / kHalf][x % kHalf] = cs.x;
             s_sin[x / kHalf][x % kHalf] = cs.y;
@@ -227,11 +242,11 @@ __global__ void __launch_bounds__(kThreads, 4) k_paged_rows(const __grid_constan
     // A thread keeps its place in a row, (head, 16 bytes of either half), and takes row after row; where a row
     // has fewer places than the CTA threads, several rows stand abreast.  Whole warps go through the loops: a
     // head's lanes add up together, and what lies outside does a valid row's work and writes nothing.
-    const int per_row = (p.Hq + 2 * p.Hkv) * kLanes, abreast = per_row < kThreads ? kThreads / per_row : 1;
-    const int sub = per_row < kThreads ? (int)threadIdx.x / per_row : 0;
+    const int per_row = (p.Hq + 2 * p.Hkv) * kLanes, abreast = per_row < threads ? threads / per_row : 1;
+    const int sub = per_row < threads ? (int)threadIdx.x / per_row : 0;
     constexpr int kAhead = 2;  // rows per thread in flight
-    const int c = (int)(threadIdx.x % kLanes) * 8;  // (kThreads is a multiple of a head's lanes)
-    for (int y0 = 0; y0 < per_row; y0 += kThreads) {
+    const int c = (int)(threadIdx.x % kLanes) * 8;  // (the threads are a multiple of a head's lanes)
+    for (int y0 = 0; y0 < per_row; y0 += threads) {
         const int y = y0 + (int)threadIdx.x - sub * per_row;
         const bool live = y < per_row && sub < abreast;
         int h = live ? y / kLanes : 0;
@@ -324,12 +339,12 @@ __global__ void __launch_bounds__(kThreads, 4) k_paged_rows(const __grid_constan
                         float top = 0.f;
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
-                            top = max_or_nan(max_or_nan(top, fabsf(halves(x[j]).x)), fabsf(halves(x[j]).y));
+                            top = max_or_nan(top, halves(x[j]));
                         top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
                         top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
                         sb[i] = scale_byte(top);
                         const float s = scale_of(sb[i]);
-                        word[i] = quantize8(x, s, s == 0.f ? 0.f : __frcp_rn(s),
+                        word[i] = quantize8(x, s, s == 0.f ? 0.f : reciprocal(s),
                                              __any_sync(0xffffffffu, sb[i] >= kMaxScaleByte));
                     }
                     // the head's scales from its lanes 0 and 4 (kD = 64: lane 0)
@@ -484,9 +499,21 @@ tb_status store_rows(RowsArgs &a, bool q4, int layer, int n_layers, int n_kv_hea
         a.eps = norm->eps;
         a.weight_offset = norm->weight_offset;
     }
-    // one row per CTA while there are SMs for more, up to kMaxRows of them otherwise
-    const int per = n_rows / (8 * n_sm);
-    a.rows_per_cta = per < 1 ? 1 : per > kMaxRows ? kMaxRows : per;
+    // The rows of a CTA: all CTAs that the SMs hold at once have as many, or in several rounds, kMaxRows at most.
+    const auto rows_for = [&](int threads) {
+        const long long slots = (long long)(kCtas * kThreads / threads) * n_sm, rounds = (n_rows - 1) / (kMaxRows * slots) + 1;
+        return (int)((n_rows - 1) / (rounds * slots)) + 1;
+    };
+    // Fewer threads than kThreads, if a row's places (or whole rows) fill them and not kThreads, where CTAs have one
+    // row or get fewer.  With 384 places 192 threads: 358 rows 5.3 us (6.2 with 256), 700 rows 6.8 (8.6), 4000
+    // rows 24.6 (26.0); where both have as many rows, 1000 rows 9.6 (8.9), 2400 rows 16.6 (14.8).
+    const int per_row = (a.Hq + 2 * a.Hkv) * (d / 16);
+    const auto fills = [&](int t) { return per_row % t == 0 || t % per_row == 0; };
+    int threads = kThreads;
+    for (int t = kThreads - 32; t >= kThreads / 2 && !fills(threads); t -= 32)
+        if (fills(t) && (rows_for(t) == 1 || rows_for(t) < rows_for(kThreads)))
+            threads = t;
+    a.rows_per_cta = rows_for(threads);
     using Kernel = void (*)(RowsArgs);
     static const Kernel kernels[2][2][2] = {
         {{k_paged_rows<64, false, false>, k_paged_rows<64, false, true>},
@@ -494,7 +521,7 @@ tb_status store_rows(RowsArgs &a, bool q4, int layer, int n_layers, int n_kv_hea
         {{k_paged_rows<128, false, false>, k_paged_rows<128, false, true>},
          {k_paged_rows<128, true, false>, k_paged_rows<128, true, true>}}};
     const int grid = (n_rows + a.rows_per_cta - 1) / a.rows_per_cta;
-    return launch_result(launch_kernel(kernels[d == 128][dtype == TB_F16][q4], dim3(grid), dim3(kThreads), 0, stream,
+    return launch_result(launch_kernel(kernels[d == 128][dtype == TB_F16][q4], dim3(grid), dim3(threads), 0, stream,
                                        true, a),
                          fn);
 }

@@ -133,6 +133,34 @@ def test_store_q4_and_load(rows, Hq, H, d, P, dtype, sections, norm, side):
         assert np.array_equal(got[good], stored[name]) and (got[~good] == 7.0).all()
 
 
+# (query heads, kv heads, head_dim): 16-byte places of a row that fill 256, 192, 224, 160 or 128 threads, or whole rows
+# of which do, or none
+@pytest.mark.parametrize("Hq,H,d", [(16, 8, 128), (32, 8, 128), (40, 8, 128), (24, 8, 128), (0, 8, 128), (4, 1, 64),
+                                    (33, 1, 128), (1, 1, 64)])
+@pytest.mark.parametrize("rows", [3, 700, 5003])
+def test_shapes_of_the_work(Hq, H, d, rows):
+    s = Scene(rows, Hq, H, d, 16, BF, (d // 2,), "both" if Hq else "k", seed=2)
+    pages = tv.make_pages_q4(1, s.n_pages, H, 16, d, BF)
+    tv.paged_kv_store_q4(pages, s.slots, s.k, s.v, **s.args)
+    got = [torch.zeros((rows, H, d), dtype=BF, device="cuda") for _ in range(2)]
+    tv.paged_kv_load_q4(pages, s.slots, *got)
+    torch.cuda.synchronize()
+    good, _, _ = s.places()
+    at = np.unique(np.concatenate([np.arange(min(rows, 10)), np.arange(rows - 3, rows), np.arange(0, rows, 97)]))
+    for name, x in (("k", got[0]), ("v", got[1]), ("q", s.q_out)):
+        if x is None:
+            continue
+        part = Scene.__new__(Scene)
+        part.__dict__.update(s.__dict__)
+        part.pos, part.k, part.q, part.v = s.pos[:, at], s.k[at], s.q[at], s.v[at]
+        want = part.expected(name) if name != "v" else f32(part.v)
+        if name == "q":
+            assert torch.equal(bits(x[at]), bits(rows_like(want, BF)))
+        else:
+            want = q4.values(*q4.quantize(want)) * good[at][:, None, None]
+            assert np.array_equal(x[at].double().cpu().numpy(), want)
+
+
 @pytest.mark.parametrize("d,dtype", [(64, BF), (128, HF), (128, BF)])
 def test_load_of_layers(d, dtype):
     torch.manual_seed(d)
