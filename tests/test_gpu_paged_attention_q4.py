@@ -200,6 +200,20 @@ def test_rows_past_the_batch_and_scale(bank, tree):  # noqa: F811
     Scene(15, [100, 0, 30], list(tree), 4, 2, 128, 16).check(bank, scale=0.3, extra_rows=9)
 
 
+@pytest.mark.parametrize("lens,tree,keep", [([5000, 40, 9], (0, 1, 2), 2), ([5000, 40], (7, 5), 63), ([30], (5,), 7),
+                                            ([20000, 300], (1, 7), 1)])
+def test_fewer_rows_than_the_plan_has(bank, lens, tree, keep):  # noqa: F811
+    """Rows of the plan past the call's n_rows are left out, in whole units and in split ones."""
+    s = Scene(16, lens, list(tree), 4, 2, 64, 16)
+    s.run(bank)
+    out, lse = torch.full_like(s.out, 3.0), torch.full_like(s.lse, 3.0)
+    tv.paged_tree_attention_q4(bank, s.req, s.pages, s.plan, s.q[:keep], out[:keep], s.ws, lse=lse[:keep])
+    torch.cuda.synchronize()
+    assert tv.tb_workspace_status(s.ws) == tv.TB_OK
+    assert torch.equal(out[:keep], s.out[:keep]) and torch.equal(lse[:keep], s.lse[:keep])
+    assert bool((out[keep:] == 3).all()) and bool((lse[keep:] == 3).all())
+
+
 @pytest.mark.parametrize("tree", [(5, 0), (0, 0)])
 def test_offsets_past_32_bits(bank, tree):  # noqa: F811
     n = (1 << 32) // (2 * tv.q4_page_bytes(128, 128)) + 40
