@@ -789,7 +789,8 @@ typedef struct tb_head_norm {
  * for about one in a thousand), and the rotation is taken as
  *   a' = fl(fl(a c) - fl(b s)),   b' = fl(fl(b c) + fl(a s))
  * so that its results are those of the same formulas in any 32-bit arithmetic
- * (paged_kv_store's may differ from them in the last bit).  One kernel. */
+ * (paged_kv_store's may differ from them in the last bit).  TB_EUNSUPPORTED for
+ * more than 2^20 kv heads.  One kernel. */
 TB_API tb_status paged_kv_store_norm(const tb_pages *pages, int layer, const int64_t *slots, int n_rows,
                                      const tb_rows *k, const tb_rows *v, const tb_rows *q, const tb_rows *q_out,
                                      int n_q_heads, const tb_head_norm *norm, const tb_rope *rope, tb_stream stream);

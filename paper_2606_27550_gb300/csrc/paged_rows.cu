@@ -472,6 +472,8 @@ tb_status store_rows(RowsArgs &a, bool q4, int layer, int n_layers, int n_kv_hea
     tb_status st = check_store(layer, n_layers, slots, n_rows, k, v, q, q_out, n_q_heads, fn);
     if (st != TB_OK || (st = check_norm(norm, fn)) != TB_OK)
         return st;
+    if (n_kv_heads > 1 << 20)
+        return record_error(TB_EUNSUPPORTED, "%s: %d kv heads", fn, n_kv_heads);
     const bool has_q = q && q->ptr;
     a.turn = rope && rope->theta != 0.f;
     if (a.turn && (st = rope_axes(rope, d, n_rows, &a.rope, fn)) != TB_OK)
@@ -520,7 +522,7 @@ tb_status store_rows(RowsArgs &a, bool q4, int layer, int n_layers, int n_kv_hea
          {k_paged_rows<64, true, false>, k_paged_rows<64, true, true>}},
         {{k_paged_rows<128, false, false>, k_paged_rows<128, false, true>},
          {k_paged_rows<128, true, false>, k_paged_rows<128, true, true>}}};
-    const int grid = (n_rows + a.rows_per_cta - 1) / a.rows_per_cta;
+    const int grid = (n_rows - 1) / a.rows_per_cta + 1;
     return launch_result(launch_kernel(kernels[d == 128][dtype == TB_F16][q4], dim3(grid), dim3(threads), 0, stream,
                                        true, a),
                          fn);

@@ -98,6 +98,28 @@ def test_refusals_of_the_stores(lib, s, name):  # noqa: F811
     assert fake_cuda.launches(lib) == []
 
 
+def test_too_many_heads_for_a_store(lib, s):  # noqa: F811
+    pages = tv.make_pages_q4(2, 6, 2, 16, 64, BF, device="cpu").as_c()
+    pages.n_kv_heads, pages.layer_stride, pages.page_stride = (1 << 20) + 1, 1 << 40, 1 << 36
+    rows = tv.TbRows(s.kv.data_ptr(), 0, 0)
+    rc = lib.paged_kv_store_q4(ctypes.byref(pages), 0, s.slots.data_ptr(), 9, ctypes.byref(rows), ctypes.byref(rows), None,
+                               None, 0, None, None, STREAM)
+    assert rc == tv.TB_EUNSUPPORTED and fake_cuda.launches(lib) == []
+
+
+@pytest.mark.parametrize("rows,Hq,H,block,grid", [
+    (1, 16, 8, 256, 1), (9, 32, 8, 192, 9), (760, 32, 8, 192, 760), (1000, 32, 8, 128, 1000), (2400, 32, 8, 128, 1200),
+    (8191, 32, 32, 256, 1171), (9, 40, 8, 224, 9), (9, 64, 8, 160, 9), (9, 33, 3, 256, 9), (40000, 32, 32, 256, 5000)])
+def test_the_shape_of_a_store(lib, s, rows, Hq, H, block, grid):  # noqa: F811
+    """CTAs as wide as the 16-byte places of a row, of one row while the SMs hold as many, of 8 at most: 1024 threads on
+    each of 152 SMs are 608 CTAs of 256, 760 of 192 and 1216 of 128, of which 1000 rows take one each."""
+    kv, q = (torch.zeros(128, dtype=BF).expand(rows, h, 128) for h in (H, Hq))
+    pages = tv.make_pages_q4(1, 2, H, 16, 128, BF, device="cpu")
+    tv.paged_kv_store_q4(pages, torch.full((rows,), -1, dtype=torch.int64), kv, kv, q=q, q_out=q, stream=STREAM)
+    (launch,) = fake_cuda.launches(lib)
+    assert launch.block == block and launch.grid == (grid, 1, 1)
+
+
 def test_refusals_of_load(lib, s):  # noqa: F811
     refused(tv.TB_EINVAL, s.load, layer=2)
     refused(tv.TB_EINVAL, s.load, layer=-1)
