@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 import numpy as np
@@ -744,8 +745,13 @@ def paged_plan(bank, req: Requests, slots, positions, status, plan, pool: PagePo
         _check(rc, "paged_plan")
 
 
-def _rows_of(t, rows: int, heads: int, d: int, dtype, what: str, dims: int = 3) -> TbRows:
-    """The rows of a (rows, heads, d) tensor, or with dims 4 of the first layer of a (layers, rows, heads, d) one."""
+# The operands of the stores and the load as the bytes of their C structs (TbRows, TbRope, TbHeadNorm), which ctypes
+# passes by address: building a Structure and a reference to it costs two to three times as much.
+_ROWS, _ROPE, _NORM = (struct.Struct(f).pack for f in ("=Qqq", "=fi4iQq", "=QQff"))
+
+
+def _rows_of(t, rows: int, heads: int, d: int, dtype, what: str, dims: int = 3) -> bytes:
+    """The TbRows of a (rows, heads, d) tensor, or with dims 4 of the first layer of a (layers, rows, heads, d) one."""
     shape, s = t.shape, t.stride()
     if dims == 4:
         shape, s = shape[1:], s[1:]
@@ -753,7 +759,7 @@ def _rows_of(t, rows: int, heads: int, d: int, dtype, what: str, dims: int = 3) 
         raise ValueError(f"{what}: shape {tuple(shape)}, ({rows}, {heads}, {d}) expected, rows contiguous")
     if t.dtype is not dtype:
         raise TypeError(f"{what}: {t.dtype}, the pages' {dtype} expected")
-    return TbRows(t.data_ptr(), s[0], s[1])
+    return _ROWS(t.data_ptr(), s[0], s[1])
 
 
 def _queries_and_rope(q, q_out, rows: int, d: int, dtype, positions, sections, rope_theta: float):
@@ -770,7 +776,7 @@ def _queries_and_rope(q, q_out, rows: int, d: int, dtype, positions, sections, r
             raise ValueError(f"{axes} position axes: at most 4")
         if stride < rows:
             raise ValueError(f"positions: {stride} of {rows} rows")
-        rope = TbRope(rope_theta, axes, (*sections,), _arr(positions, _I32, axes * stride, "positions"), stride)
+        rope = _ROPE(rope_theta, axes, *(*sections, 0, 0, 0, 0)[:4], _arr(positions, _I32, axes * stride, "positions"), stride)
     return heads, cq, co, rope
 
 
@@ -782,8 +788,8 @@ def paged_kv_store(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None
     rows, H, d = slots.shape[0], c.n_kv_heads, c.head_dim
     ck, cv = _rows_of(k, rows, H, d, dtype, "k"), _rows_of(v, rows, H, d, dtype, "v")
     heads, cq, co, rope = _queries_and_rope(q, q_out, rows, d, dtype, positions, sections, rope_theta)
-    rc = load().paged_kv_store(ctypes.byref(c), layer, _arr(slots, _I64, rows, "slots"), rows, ctypes.byref(ck),
-                               ctypes.byref(cv), _ref(cq), _ref(co), heads, _ref(rope), _stream(stream))
+    rc = load().paged_kv_store(ctypes.byref(c), layer, _arr(slots, _I64, rows, "slots"), rows, ck, cv, cq, co, heads,
+                               rope, _stream(stream))
     if rc:
         _check(rc, "paged_kv_store")
 
@@ -791,7 +797,7 @@ def paged_kv_store(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None
 def _norm_of(q_norm, k_norm, eps: float, weight_offset: float, d: int, dtype):
     if q_norm is None and k_norm is None:
         return None
-    return TbHeadNorm(_arr(q_norm, dtype, d, "q_norm"), _arr(k_norm, dtype, d, "k_norm"), eps, weight_offset)
+    return _NORM(_arr(q_norm, dtype, d, "q_norm") or 0, _arr(k_norm, dtype, d, "k_norm") or 0, eps, weight_offset)
 
 
 def _page_kind(pages, kind):
@@ -808,8 +814,8 @@ def _store_rows(name: str, kind, pages, layer: int, slots, k, v, q, q_out, q_nor
     ck, cv = _rows_of(k, rows, H, d, dtype, "k"), _rows_of(v, rows, H, d, dtype, "v")
     heads, cq, co, rope = _queries_and_rope(q, q_out, rows, d, dtype, positions, sections, rope_theta)
     norm = _norm_of(q_norm, k_norm, eps, weight_offset, d, dtype)
-    rc = getattr(load(), name)(ctypes.byref(c), layer, _arr(slots, _I64, rows, "slots"), rows, ctypes.byref(ck),
-                               ctypes.byref(cv), _ref(cq), _ref(co), heads, _ref(norm), _ref(rope), _stream(stream))
+    rc = getattr(load(), name)(ctypes.byref(c), layer, _arr(slots, _I64, rows, "slots"), rows, ck, cv, cq, co, heads,
+                               norm, rope, _stream(stream))
     if rc:
         _check(rc, name)
 
@@ -888,8 +894,8 @@ def paged_kv_load_q4(pages: PagesQ4, slots, k, v, layer: int = 0, stream=None):
             raise ValueError("no layers")
     ck = _rows_of(k, rows, c.n_kv_heads, c.head_dim, dtype, "k", len(k.shape))
     cv = _rows_of(v, rows, c.n_kv_heads, c.head_dim, dtype, "v", len(k.shape))
-    rc = load().paged_kv_load_q4(ctypes.byref(c), layer, layers, _arr(slots, _I64, rows, "slots"), rows,
-                                 ctypes.byref(ck), ctypes.byref(cv), stride, _stream(stream))
+    rc = load().paged_kv_load_q4(ctypes.byref(c), layer, layers, _arr(slots, _I64, rows, "slots"), rows, ck, cv, stride,
+                                 _stream(stream))
     if rc:
         _check(rc, "paged_kv_load_q4")
 

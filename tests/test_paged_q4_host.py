@@ -98,6 +98,12 @@ def test_refusals_of_the_stores(lib, s, name):  # noqa: F811
     assert fake_cuda.launches(lib) == []
 
 
+def test_packed_operands_are_the_c_structs():
+    assert tv._ROWS(1 << 40, -8, 1 << 33) == bytes(tv.TbRows(1 << 40, -8, 1 << 33))
+    assert tv._ROPE(1e4, 3, 16, 24, 24, 0, 77, 9) == bytes(tv.TbRope(1e4, 3, (16, 24, 24, 0), 77, 9))
+    assert tv._NORM(0, 1 << 50, 1e-6, 1.0) == bytes(tv.TbHeadNorm(None, 1 << 50, 1e-6, 1.0))
+
+
 def test_too_many_heads_for_a_store(lib, s):  # noqa: F811
     pages = tv.make_pages_q4(2, 6, 2, 16, 64, BF, device="cpu").as_c()
     pages.n_kv_heads, pages.layer_stride, pages.page_stride = (1 << 20) + 1, 1 << 40, 1 << 36
