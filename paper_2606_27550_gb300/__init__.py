@@ -801,10 +801,11 @@ def _norm_of(q_norm, k_norm, eps: float, weight_offset: float, d: int, dtype):
 
 
 def _page_kind(pages, kind):
-    """The C struct of pages, which have to be of the kind that the call reads them as."""
-    if type(pages) is not kind:
+    """The C struct of pages, which has to be of the kind that the call reads it as (whatever class holds it)."""
+    c = getattr(pages, "_c", None)
+    if c is None or isinstance(c, TbPagesQ4) is not (kind is PagesQ4):
         raise TypeError(f"pages: {type(pages).__name__}, {kind.__name__} expected")
-    return pages._c
+    return c
 
 
 def _store_rows(name: str, kind, pages, layer: int, slots, k, v, q, q_out, q_norm, k_norm, eps, weight_offset,
