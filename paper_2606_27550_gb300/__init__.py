@@ -776,7 +776,11 @@ def _queries_and_rope(q, q_out, rows: int, d: int, dtype, positions, sections, r
             raise ValueError(f"{axes} position axes: at most 4")
         if stride < rows:
             raise ValueError(f"positions: {stride} of {rows} rows")
-        rope = _ROPE(rope_theta, axes, *(*sections, 0, 0, 0, 0)[:4], _arr(positions, _I32, axes * stride, "positions"), stride)
+        address = _arr(positions, _I32, axes * stride, "positions")
+        try:
+            rope = _ROPE(rope_theta, axes, *(*sections, 0, 0, 0, 0)[:4], address, stride)
+        except (OverflowError, struct.error):  # past 32 bits: as C takes it (a theta is infinite), for the library to refuse
+            rope = bytes(TbRope(rope_theta, axes, (*sections,), address, stride))
     return heads, cq, co, rope
 
 
@@ -797,7 +801,11 @@ def paged_kv_store(pages: Pages, slots, k, v, layer: int = 0, q=None, q_out=None
 def _norm_of(q_norm, k_norm, eps: float, weight_offset: float, d: int, dtype):
     if q_norm is None and k_norm is None:
         return None
-    return _NORM(_arr(q_norm, dtype, d, "q_norm") or 0, _arr(k_norm, dtype, d, "k_norm") or 0, eps, weight_offset)
+    weights = _arr(q_norm, dtype, d, "q_norm") or 0, _arr(k_norm, dtype, d, "k_norm") or 0
+    try:
+        return _NORM(*weights, eps, weight_offset)
+    except OverflowError:
+        return bytes(TbHeadNorm(*weights, eps, weight_offset))
 
 
 def _page_kind(pages, kind):

@@ -44,3 +44,20 @@ def test_pages_of_a_callers_own_class(lib, s):  # noqa: F811
                 with pytest.raises(TypeError):
                     fn(pages=pages)
     assert fake_cuda.launches(lib) == []
+
+
+BIG = 2 ** 40 * 1e30  # past 32 bits
+
+
+@pytest.mark.parametrize("name", ["store", "store_norm", "store_q4"])
+def test_numbers_past_32_bits_are_refused_by_the_library(lib, s, name):  # noqa: F811
+    """A theta, eps or offset whose 32-bit value is infinite, a section past 32 bits: refused as other bad values are."""
+    fn = (lambda **kw: Setup16.store(s, pages=s.pages16, **kw)) if name == "store" else getattr(s, name)
+    bad = [dict(rope_theta=BIG), dict(rope_theta=-BIG), dict(sections=(2 ** 31,)), dict(sections=(-2 ** 31 - 1,))]
+    if name != "store":
+        bad += [dict(eps=BIG), dict(weight_offset=-BIG)]
+    for kw in bad:
+        with pytest.raises(tv.TreeVerifyError) as e:
+            fn(**kw)
+        assert e.value.status == tv.TB_EINVAL
+    assert fake_cuda.launches(lib) == []
