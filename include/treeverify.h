@@ -784,9 +784,11 @@ typedef struct tb_head_norm {
 } tb_head_norm;
 
 /* paged_kv_store with norms: q and k are normed, then turned, then rounded to
- * their type, in one pass; v is stored as it is.  norm NULL: none.  The angles'
- * sines and cosines are right to half a unit in the last place of 32 bits (but
- * for about one in a thousand), and the rotation is taken as
+ * their type, in one pass; v is stored as it is.  norm NULL: none.  An angle is
+ * the position times the pair's turn per position, which is held to one unit of
+ * 2^-64 (three for theta near 2); its sine and cosine are right to half a unit in
+ * the last place of 32 bits (but for about one in a thousand), however small the
+ * angle, and the rotation is taken as
  *   a' = fl(fl(a c) - fl(b s)),   b' = fl(fl(b c) + fl(a s))
  * so that its results are those of the same formulas in any 32-bit arithmetic
  * (paged_kv_store's may differ from them in the last bit).  TB_EUNSUPPORTED for

@@ -73,12 +73,17 @@ __device__ float2 cos_sin(uint64_t turn)
 {
     const int quarter = (int)((turn + (1ull << 61)) >> 62);
     const int64_t r = (int64_t)(turn - ((uint64_t)quarter << 62));  // in [-2^61, 2^61)
-    const int r_hi = (int)(r >> 32);
-    const float h = __int2float_rn(r_hi);
-    const float l = __fadd_rn(__int2float_rn(r_hi - __float2int_rn(h)), __fmul_rn(__uint2float_rn((uint32_t)r), 0x1p-32f));
-    // times 2 pi / 2^32
-    Two y = product(near_sum(h, l), Two{6.28318548202514648f * 0x1p-32f, -1.74845553146951715e-07f * 0x1p-32f});
+    // its leading bits, wherever they stand: 24 in one float, the next 32 rounded to 24 in another (2^-47 of it).
+    // Small angles take the same way as large ones
+    const uint64_t size = r < 0 ? 0 - (uint64_t)r : (uint64_t)r;
+    const int zeros = __clzll((long long)(size | 1));
+    const uint64_t m = size << zeros;
+    const float h = __uint2float_rn((uint32_t)(m >> 40)), l = __fmul_rn(__uint2float_rn((uint32_t)(m >> 8)), 0x1p-32f);
+    // times 2 pi / 2^24, then 2^-zeros and the sign
+    Two y = product(near_sum(h, l), Two{6.28318548202514648f * 0x1p-24f, -1.74845553146951715e-07f * 0x1p-24f});
     y = near_sum(y.hi, y.lo);
+    const float unit = __int_as_float((int)((uint32_t)(127 - zeros) << 23 | (r < 0 ? 0x80000000u : 0u)));
+    y = Two{__fmul_rn(y.hi, unit), __fmul_rn(y.lo, unit)};
     const Two z = product(y, y);
     // sin y = y + y z S(z), cos y = 1 + z C(z)
     float f = __fmaf_rn(z.hi, __fmaf_rn(z.hi, -1.f / 39916800.f, 1.f / 362880.f), -1.f / 5040.f);
