@@ -429,7 +429,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attention(const __grid_co
     __shared__ std::conditional_t<kQ4, None, SegInfo[2]> info;
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *sK = smem, *sV = smem + (size_t)kKStages * kTile;
-    // 4-bit pages: the packed tiles of K and V, filled by the producers and emptied by warps 8-11
+    // 4-bit pages: the packed tiles of K, filled by warp 0 and emptied by warps 8-11, and of V, filled by warp 1 and
+    // emptied by warps 0-2
     uint8_t *const packed = sV + (size_t)kVStages * kTile;
     __shared__ __align__(8) uint64_t packed_full[kQ4 ? 2 : 1][kPackedStages], packed_empty[kQ4 ? 2 : 1][kPackedStages];
     __shared__ uint32_t packed_holes[kQ4 ? 2 : 1][kPackedStages];

@@ -21,11 +21,13 @@
 // in the CTA's slots of the workspace, the last in shared memory once all rings are
 // done with), and the CTA joins them in order.
 //
-// Bound by its instructions: about 740 of a warp per piece, most of them for the 4-bit
-// operands, whose masks and shifts run at half rate (64 requests of one token, 8 kv heads
-// of 128 with 4 query heads each, prefixes of 512 to 16384: 155 us, 55 % of a copy's bandwidth; 16
-// requests at 65536 keys: 65 %), and by about 10 us to the first piece and through the
-// join.  The batch took 582 us through the tiles of many rows, 246 with pieces that all warps
+// Bound by its instructions and by the way from one to the next: about 740 of a warp per piece, 288
+// of them from codes to operands (masks and shifts at half rate) and 76 for scales and pairs, with four
+// warps on a scheduler, which find 62 % of its slots; the largest wait is for fixed latencies (64
+// requests of one token, 8 kv heads of 128 with 4 query heads each, prefixes of 512 to 16384: 155 us, 55 %
+// of a copy's bandwidth; 16 requests at 65536 keys: 65 %); and by about 10 us to the first piece and through
+// the join.  The registers that the kernel spills (372 bytes of stores at head_dim 128) are not the
+// loop's: 0.07 % of that call's instructions touch local memory.  The batch took 582 us through the tiles of many rows, 246 with pieces that all warps
 // shared, 172 with runs and copies of each warp's own, 157 with one shift for four codes.
 #pragma once
 

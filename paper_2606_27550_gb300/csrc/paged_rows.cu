@@ -8,7 +8,8 @@
 // cosines and the norm's reciprocal root are computed with a second float that
 // holds what the first leaves (a sum's or product's rounding error is a float
 // itself: Dekker 1971, Knuth's two-sum).  Another program that follows the formulas
-// gets the same codes.
+// gets the same values, and the same keys but for such near-ties (fewer than 1 of 10^7 elements, as a sine's
+// last bit moves an element by 2^-23 of the head's size; without a rotation and norms, all of them).
 //
 // A CTA takes a few rows: their (cos, sin) once into shared memory (they serve
 // all heads), then every (row, head, 16-byte piece of the lower half of the head
@@ -212,8 +213,9 @@ __device__ __forceinline__ float reciprocal(float x)
 // Bound by HBM where rows stay in 16 bits: each element is read once and written once (8191 rows of 32 + 2 * 32
 // heads of 128, normed and turned: 74 us, 5.4 TB/s, 80 % of a copy's bandwidth; 87 us with a division for each
 // piece to find its place), and by its instructions where they become 4 bits (the same
-// rows: 91 us, 73 without norms; the largest of 32, the scale and 32 corrected quotients on top; 149 us with a
-// division each and one number at a time).  One to eight rows per CTA: the sines serve all of a row's heads, and
+// rows: 91 us, 73 without norms, 79 without the rotation, 63 with neither, which rows of 16 bits take too; the
+// largest of 32, the scale and 32 corrected quotients on top; 149 us with a division each and one number at a time)
+// and what they wait for: 70 % of the issue slots are taken.  One to eight rows per CTA: the sines serve all of a row's heads, and
 // few rows still reach all SMs (eight trees, 32 + 2 * 8 heads: 5.3 us).
 template <int kD, bool kF16, bool kQ4>
 __global__ void __launch_bounds__(kThreads, kCtas) k_paged_rows(const __grid_constant__ RowsArgs p)
@@ -377,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_paged_rows(const __grid_con
 struct LoadArgs {
     const uint8_t *k_pages, *v_pages;  // of the first layer
     long long layer_stride, page_stride, head_stride;
-    int n_pages, page_log2, Hkv, n_rows, n_layers;
+    int n_pages, page_log2, Hkv, n_rows;
     const int64_t *slots;
     Rows k, v;
     long long row_layer_stride;
@@ -642,7 +644,6 @@ extern "C" tb_status paged_kv_load_q4(const tb_pages_q4 *pages, int layer, int n
         ++a.page_log2;
     a.Hkv = pages->n_kv_heads;
     a.n_rows = n_rows;
-    a.n_layers = n_layers;
     a.slots = slots;
     a.k = rows_of(k);
     a.v = rows_of(v);
